@@ -62,7 +62,8 @@ typedef enum {
 
 typedef enum {
     CONV2D_OPERAND_BF16 = 0,  /* bfloat16: the upper 16 bits of an IEEE fp32 */
-    CONV2D_OPERAND_FP16 = 1   /* IEEE binary16 */
+    CONV2D_OPERAND_FP16 = 1,  /* IEEE binary16 */
+    CONV2D_OPERAND_FP32 = 2   /* IEEE binary32: the operators of sequence_b200.h only */
 } conv2d_operand_t;
 
 /* `flags` bits */

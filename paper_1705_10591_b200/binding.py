@@ -1,4 +1,4 @@
-"""ctypes binding of libconv2d_b200.so: same names and argument order as the C header.
+"""ctypes binding of libconv2d_b200.so: same names and argument order as the C headers.
 
 Pointers are passed as integers (``tensor.data_ptr()`` / ``ndarray.ctypes.data``),
 streams as the integer ``torch.cuda.current_stream().cuda_stream``.  Nothing here
@@ -11,8 +11,10 @@ import ctypes
 from pathlib import Path
 
 ALGO_AUTO, ALGO_FFMA, ALGO_TF32, ALGO_16BIT = 0, 1, 2, 3
-OPERAND_BF16, OPERAND_FP16 = 0, 1
+OPERAND_BF16, OPERAND_FP16, OPERAND_FP32 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 FLAG_WEIGHTS_PACKED = 1
+FLAG_SCAN_SOFTPLUS = 1
 
 _LIB_PATH = Path(__file__).resolve().parent / "libconv2d_b200.so"
 _lib = None
@@ -69,6 +71,25 @@ def load_library() -> ctypes.CDLL:
     lib.conv2d_status_string.restype = ctypes.c_char_p
     lib.conv2d_launch_count.argtypes = []
     lib.conv2d_launch_count.restype = ctypes.c_ulonglong
+    ll, f = ctypes.c_longlong, ctypes.c_float
+    for name, args in {
+        "conv1d_fwd_causal": [vp] * 7 + [i] * 4 + [ll] * 2 + [i, i, vp],
+        "conv1d_step_causal": [vp] * 6 + [i] * 3 + [ll] * 2 + [i, i, vp],
+        "conv1d_bwd_causal_workspace_size": [i] * 4 + [ctypes.POINTER(sz)],
+        "conv1d_bwd_causal": [vp] * 11 + [i] * 4 + [ll] * 3 + [i, i, vp, sz, vp],
+        "scan_states_size": [i] * 4 + [ctypes.POINTER(sz)],
+        "scan_fwd_selective_workspace_size": [i] * 5 + [ctypes.POINTER(sz)],
+        "scan_fwd_selective": [vp] * 13 + [i] * 5 + [ll] * 6 + [i, u, vp, sz, vp],
+        "scan_step_selective": [vp] * 11 + [i] * 4 + [ll] * 6 + [i, u, vp],
+        "scan_bwd_selective_workspace_size": [i] * 5 + [ctypes.POINTER(sz)],
+        "scan_bwd_selective": [vp] * 21 + [i] * 5 + [ll] * 11 + [i, u, vp, sz, vp],
+        "norm_fwd_groups_workspace_size": [i] * 4 + [ctypes.POINTER(sz)],
+        "norm_fwd_groups": [vp] * 6 + [i] * 4 + [ll] * 2 + [f, i, i, vp, sz, vp],
+        "norm_bwd_groups_workspace_size": [i] * 4 + [ctypes.POINTER(sz)],
+        "norm_bwd_groups": [vp] * 9 + [i] * 4 + [ll] * 3 + [i, i, vp, sz, vp],
+    }.items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = i
     _lib = lib
     return lib
 
@@ -180,3 +201,118 @@ def conv2d_fwd_host(x_host_ptr, w_host_ptr, y_host_ptr, x_ptr, w_ptr, y_ptr, N, 
 def conv2d_get_status(workspace_ptr=0, stream=0) -> None:
     """Waits for the stream; raises if a kernel reported a device-side timeout."""
     _check(load_library().conv2d_get_status(workspace_ptr or None, stream or None), "conv2d_get_status")
+
+
+# ---- operators along a sequence (sequence_b200.h).  Pointers that are optional there may be 0.
+
+def _size(name, *args) -> int:
+    out = ctypes.c_size_t(0)
+    _check(getattr(load_library(), name)(*args, ctypes.byref(out)), name)
+    return int(out.value)
+
+
+def conv1d_fwd_causal(x_ptr, w_ptr, bias_ptr, state_in_ptr, lengths_ptr, y_ptr, state_out_ptr, B, L, D, K, ldx, ldy,
+                      operand=OPERAND_BF16, act=ACT_NONE, stream=0) -> None:
+    """Causal convolution of every channel with its own K taps; x, y [B*L, D] with rows ldx, ldy elements apart."""
+    _check(load_library().conv1d_fwd_causal(x_ptr or None, w_ptr or None, bias_ptr or None, state_in_ptr or None, lengths_ptr or None,
+                                            y_ptr or None, state_out_ptr or None, B, L, D, K, ldx, ldy, operand, act, stream or None),
+           "conv1d_fwd_causal")
+
+
+def conv1d_step_causal(x_ptr, w_ptr, bias_ptr, state_in_ptr, y_ptr, state_out_ptr, B, D, K, ldx, ldy,
+                       operand=OPERAND_BF16, act=ACT_NONE, stream=0) -> None:
+    """One token of every sequence; the two states [B, K-1, D] may be one buffer."""
+    _check(load_library().conv1d_step_causal(x_ptr or None, w_ptr or None, bias_ptr or None, state_in_ptr or None, y_ptr or None,
+                                             state_out_ptr or None, B, D, K, ldx, ldy, operand, act, stream or None),
+           "conv1d_step_causal")
+
+
+def conv1d_bwd_causal_workspace_size(B, L, D, K) -> int:
+    return _size("conv1d_bwd_causal_workspace_size", B, L, D, K)
+
+
+def conv1d_bwd_causal(x_ptr, w_ptr, bias_ptr, state_in_ptr, lengths_ptr, dy_ptr, dstate_out_ptr, dx_ptr, dw_ptr, dbias_ptr,
+                      dstate_in_ptr, B, L, D, K, ldx, lddy, lddx, operand=OPERAND_BF16, act=ACT_NONE,
+                      workspace_ptr=0, workspace_bytes=0, stream=0) -> None:
+    """dw [D, K] and dbias [D] are fp32, whatever the operand type."""
+    _check(load_library().conv1d_bwd_causal(x_ptr or None, w_ptr or None, bias_ptr or None, state_in_ptr or None, lengths_ptr or None,
+                                            dy_ptr or None, dstate_out_ptr or None, dx_ptr or None, dw_ptr or None, dbias_ptr or None,
+                                            dstate_in_ptr or None, B, L, D, K, ldx, lddy, lddx, operand, act,
+                                            workspace_ptr or None, workspace_bytes, stream or None),
+           "conv1d_bwd_causal")
+
+
+def scan_states_size(B, L, D, N) -> int:
+    """Bytes of the states that scan_fwd_selective leaves for scan_bwd_selective."""
+    return _size("scan_states_size", B, L, D, N)
+
+
+def scan_fwd_selective_workspace_size(B, L, D, N, G=1) -> int:
+    return _size("scan_fwd_selective_workspace_size", B, L, D, N, G)
+
+
+def scan_fwd_selective(u_ptr, delta_ptr, A_ptr, Bm_ptr, Cm_ptr, Dskip_ptr, z_ptr, delta_bias_ptr, state_in_ptr, lengths_ptr,
+                       y_ptr, state_out_ptr, states_ptr, B, L, D, N, G, ldu, lddelta, ldB, ldC, ldz, ldy,
+                       operand=OPERAND_BF16, flags=0, workspace_ptr=0, workspace_bytes=0, stream=0) -> None:
+    """Selective state space scan of [B*L, D]; A, Dskip, delta_bias and the states are fp32."""
+    _check(load_library().scan_fwd_selective(u_ptr or None, delta_ptr or None, A_ptr or None, Bm_ptr or None, Cm_ptr or None,
+                                             Dskip_ptr or None, z_ptr or None, delta_bias_ptr or None, state_in_ptr or None,
+                                             lengths_ptr or None, y_ptr or None, state_out_ptr or None, states_ptr or None,
+                                             B, L, D, N, G, ldu, lddelta, ldB, ldC, ldz, ldy, operand, flags,
+                                             workspace_ptr or None, workspace_bytes, stream or None),
+           "scan_fwd_selective")
+
+
+def scan_step_selective(u_ptr, delta_ptr, A_ptr, Bm_ptr, Cm_ptr, Dskip_ptr, z_ptr, delta_bias_ptr, state_in_ptr, y_ptr,
+                        state_out_ptr, B, D, N, G, ldu, lddelta, ldB, ldC, ldz, ldy, operand=OPERAND_BF16, flags=0, stream=0) -> None:
+    """One token of every sequence; the two states [B, D, N] may be one buffer."""
+    _check(load_library().scan_step_selective(u_ptr or None, delta_ptr or None, A_ptr or None, Bm_ptr or None, Cm_ptr or None,
+                                              Dskip_ptr or None, z_ptr or None, delta_bias_ptr or None, state_in_ptr or None,
+                                              y_ptr or None, state_out_ptr or None, B, D, N, G, ldu, lddelta, ldB, ldC, ldz, ldy,
+                                              operand, flags, stream or None),
+           "scan_step_selective")
+
+
+def scan_bwd_selective_workspace_size(B, L, D, N, G=1) -> int:
+    return _size("scan_bwd_selective_workspace_size", B, L, D, N, G)
+
+
+def scan_bwd_selective(u_ptr, delta_ptr, A_ptr, Bm_ptr, Cm_ptr, Dskip_ptr, z_ptr, delta_bias_ptr, lengths_ptr, states_ptr,
+                       dy_ptr, dstate_out_ptr, du_ptr, ddelta_ptr, dA_ptr, dB_ptr, dC_ptr, dDskip_ptr, dz_ptr, ddelta_bias_ptr,
+                       dstate_in_ptr, B, L, D, N, G, ldu, lddelta, ldB, ldC, ldz, lddy, lddu, ldddelta, lddB, lddC, lddz,
+                       operand=OPERAND_BF16, flags=0, workspace_ptr=0, workspace_bytes=0, stream=0) -> None:
+    """states: as scan_fwd_selective of the same inputs left them; dA, dDskip, ddelta_bias and dstate_in are fp32."""
+    _check(load_library().scan_bwd_selective(u_ptr or None, delta_ptr or None, A_ptr or None, Bm_ptr or None, Cm_ptr or None,
+                                             Dskip_ptr or None, z_ptr or None, delta_bias_ptr or None, lengths_ptr or None,
+                                             states_ptr or None, dy_ptr or None, dstate_out_ptr or None, du_ptr or None,
+                                             ddelta_ptr or None, dA_ptr or None, dB_ptr or None, dC_ptr or None, dDskip_ptr or None,
+                                             dz_ptr or None, ddelta_bias_ptr or None, dstate_in_ptr or None, B, L, D, N, G,
+                                             ldu, lddelta, ldB, ldC, ldz, lddy, lddu, ldddelta, lddB, lddC, lddz, operand, flags,
+                                             workspace_ptr or None, workspace_bytes, stream or None),
+           "scan_bwd_selective")
+
+
+def norm_fwd_groups_workspace_size(N, S, C, G) -> int:
+    return _size("norm_fwd_groups_workspace_size", N, S, C, G)
+
+
+def norm_fwd_groups(x_ptr, gamma_ptr, beta_ptr, y_ptr, mean_ptr, rstd_ptr, N, S, C, G, ldx, ldy, eps,
+                    operand=OPERAND_BF16, act=ACT_NONE, workspace_ptr=0, workspace_bytes=0, stream=0) -> None:
+    """Group norm over S positions and C / G channels of [N*S, C], then the activation; gamma, beta [C] are fp32."""
+    _check(load_library().norm_fwd_groups(x_ptr or None, gamma_ptr or None, beta_ptr or None, y_ptr or None, mean_ptr or None,
+                                          rstd_ptr or None, N, S, C, G, ldx, ldy, eps, operand, act,
+                                          workspace_ptr or None, workspace_bytes, stream or None),
+           "norm_fwd_groups")
+
+
+def norm_bwd_groups_workspace_size(N, S, C, G) -> int:
+    return _size("norm_bwd_groups_workspace_size", N, S, C, G)
+
+
+def norm_bwd_groups(x_ptr, gamma_ptr, beta_ptr, mean_ptr, rstd_ptr, dy_ptr, dx_ptr, dgamma_ptr, dbeta_ptr, N, S, C, G,
+                    ldx, lddy, lddx, operand=OPERAND_BF16, act=ACT_NONE, workspace_ptr=0, workspace_bytes=0, stream=0) -> None:
+    """mean, rstd [N, G] as norm_fwd_groups left them; dgamma, dbeta [C] are fp32."""
+    _check(load_library().norm_bwd_groups(x_ptr or None, gamma_ptr or None, beta_ptr or None, mean_ptr or None, rstd_ptr or None,
+                                          dy_ptr or None, dx_ptr or None, dgamma_ptr or None, dbeta_ptr or None, N, S, C, G,
+                                          ldx, lddy, lddx, operand, act, workspace_ptr or None, workspace_bytes, stream or None),
+           "norm_bwd_groups")

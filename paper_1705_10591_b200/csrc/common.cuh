@@ -152,6 +152,9 @@ cudaError_t launch_pdl_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, 
     return own_error(cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...));
 }
 
+// CONV2D_OK when the current device is of compute capability 10.x.
+conv2d_status_t check_device();
+
 // Launchers.  Each returns CONV2D_OK, CONV2D_ERR_UNSUPPORTED (no instance) or CONV2D_ERR_CUDA.
 conv2d_status_t launch_single_channel(const float* x, const float* w, float* y, const Shape& sh, cudaStream_t stream);
 double single_channel_flat_cost(const Shape& sh);      // estimated scheduler cycles of a warp for four outputs of all maps

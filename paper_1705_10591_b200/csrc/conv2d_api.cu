@@ -125,6 +125,8 @@ cudaError_t latch_status(const void* workspace, unsigned* timed_out, cudaStream_
     return e;
 }
 
+}  // namespace
+
 conv2d_status_t check_device()
 {
     int dev = 0;
@@ -134,7 +136,6 @@ conv2d_status_t check_device()
     return major == 10 ? CONV2D_OK : CONV2D_ERR_ARCH;
 }
 
-}  // namespace
 }  // namespace conv2d_b200
 
 using namespace conv2d_b200;
@@ -590,7 +591,7 @@ const char* conv2d_status_string(conv2d_status_t status)
         case CONV2D_OK: return "ok";
         case CONV2D_ERR_NULL: return "a required pointer is NULL";
         case CONV2D_ERR_SHAPE: return "invalid shape (non-positive extent, filter larger than image, or too large)";
-        case CONV2D_ERR_ALIGN: return "pointer not 16-byte aligned";
+        case CONV2D_ERR_ALIGN: return "pointer not 16-byte aligned (sequence operators: not aligned to its elements)";
         case CONV2D_ERR_WORKSPACE: return "workspace too small";
         case CONV2D_ERR_UNSUPPORTED: return "no kernel instance for this algorithm/shape/flags";
         case CONV2D_ERR_ARCH: return "device is not compute capability 10.x (B200)";

@@ -1,0 +1,710 @@
+// Group norm with an activation, channels last.
+//
+//   m, q = mean and variance of the S x E elements of sample n and group g (E = C / G),  x^ = (x - m) / sqrt(q + eps),
+//   y = act(gamma x^ + beta);   backward, with d = dy act'(.):
+//   s1[n,c] = sum_s d,  s2[n,c] = sum_s d x^,  dbeta = sum_n s1,  dgamma = sum_n s2,
+//   dx = rstd (gamma d - mean(gamma s1) - x^ mean(gamma s2))
+//
+// Memory decides: the floor is one reading of the inputs and one writing of the output.  Statistics come before the output, so the
+// elements have to stay on chip in between:
+//   rows     S = 1: the elements of a group lie together and stay in the registers of 1 to 32 lanes.
+//   slab     a thread-block cluster takes the rows of a few groups of one sample, every block a part of the rows, which stay in its shared
+//            memory; the blocks exchange their statistics through distributed shared memory.
+//   stream   slabs that do not fit, or too few of them to fill the machine: one kernel for the statistics of parts, one that reads
+//            the elements again (from L2 where they are still there).
+// Statistics of a part are taken around one of its own values and joined by counts and means, so that a mean far
+// from zero costs no digits.
+#include <cooperative_groups.h>
+
+#include "seq_common.cuh"
+
+namespace conv2d_b200 {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+
+template <typename T>
+struct NormArgs {
+    const T *x, *dy;
+    const float *gamma, *beta;
+    T *y, *dx;
+    float *mean, *rstd;
+    float4* part_stats;                 // [N][G][parts]: what the parts of a slab have found (stream)
+    float* channels;                    // [N * parts or chunks][2][C]: partial sums of dbeta, dgamma
+    int N, S, C, G, E;
+    long long ldx, ldy, lddy, lddx;
+    float eps;
+    int act;
+    int lanes, chunks, chunk;           // rows: lanes of a group; chunks of samples, samples of a chunk
+    int tile_groups, tiles, parts, part_rows;
+};
+
+// ------------------------------------------------------------------------------------------------------------- rows
+
+__device__ __forceinline__ float lanes_sum(float v, int lanes)
+{
+    for (int m = 1; m < lanes; m *= 2) v += __shfl_xor_sync(0xffffffffu, v, m);
+    return v;
+}
+
+template <int V>
+__device__ __forceinline__ void load_params(const float* p, float dflt, int c, bool real, float (&out)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] = p && real ? p[c + i] : dflt;
+}
+
+// A thread keeps NV packs of one group, lane l the packs l, l + lanes, ..; ROWS samples are under way together.
+template <typename T, int V, int NV, int ROWS>
+__global__ void __launch_bounds__(kThreads) norm_rows_fwd_kernel(const NormArgs<T> a)
+{
+    ptx::grid_dep_wait();
+    const unsigned cols = (kThreads + (unsigned)a.G * a.lanes - 1) / kThreads;
+    const unsigned col = blockIdx.x % cols * kThreads + threadIdx.x;
+    const int g = (int)(col / a.lanes), l = (int)(col % a.lanes);
+    const long long n0 = (long long)(blockIdx.x / cols) * a.chunk, n1 = min(n0 + a.chunk, (long long)a.N);
+    int c[NV];
+    bool real[NV];
+    float gamma[NV][V], beta[NV][V];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int e = (l + k * a.lanes) * V;
+        real[k] = g < a.G && e < a.E;
+        c[k] = g * a.E + e;
+        load_params<V>(a.gamma, 1.f, c[k], real[k], gamma[k]);
+        load_params<V>(a.beta, 0.f, c[k], real[k], beta[k]);
+    }
+    const float inv = 1.f / a.E;
+    for (long long n = n0; n < n1; n += ROWS) {
+        Pack<T, V> p[ROWS][NV];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int k = 0; k < NV; ++k) p[r][k] = real[k] && n + r < n1 ? load_pack<T, V>(a.x + (n + r) * a.ldx + c[k]) : zero_pack<T, V>();
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            float x[NV][V], sum = 0.f, sq = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                unpack(p[r][k], x[k]);
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum += x[k][i];
+            }
+            const float mean = lanes_sum(sum, a.lanes) * inv;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    x[k][i] -= mean;
+                    if (real[k]) sq = fmaf(x[k][i], x[k][i], sq);
+                }
+            const float rstd = rsqrtf(fmaf(lanes_sum(sq, a.lanes), inv, a.eps));
+            if (n + r >= n1) continue;
+            if (l == 0 && g < a.G) {
+                if (a.mean) a.mean[(n + r) * a.G + g] = mean;
+                if (a.rstd) a.rstd[(n + r) * a.G + g] = rstd;
+            }
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                if (!real[k]) continue;
+                float o[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] = activate(fmaf(x[k][i] * rstd, gamma[k][i], beta[k][i]), a.act);
+                store_pack(a.y + (n + r) * a.ldy + c[k], pack<T, V>(o));
+            }
+        }
+    }
+}
+
+template <typename T, int V, int NV, int ROWS>
+__global__ void __launch_bounds__(kThreads) norm_rows_bwd_kernel(const NormArgs<T> a)
+{
+    ptx::grid_dep_wait();
+    const unsigned cols = (kThreads + (unsigned)a.G * a.lanes - 1) / kThreads;
+    const unsigned col = blockIdx.x % cols * kThreads + threadIdx.x;
+    const int g = (int)(col / a.lanes), l = (int)(col % a.lanes);
+    const long long chunk = blockIdx.x / cols, n0 = chunk * a.chunk, n1 = min(n0 + a.chunk, (long long)a.N);
+    int c[NV];
+    bool real[NV];
+    float gamma[NV][V], beta[NV][V], sum1[NV][V] = {}, sum2[NV][V] = {};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int e = (l + k * a.lanes) * V;
+        real[k] = g < a.G && e < a.E;
+        c[k] = g * a.E + e;
+        load_params<V>(a.gamma, 1.f, c[k], real[k], gamma[k]);
+        load_params<V>(a.beta, 0.f, c[k], real[k], beta[k]);
+    }
+    const float inv = 1.f / a.E;
+    for (long long n = n0; n < n1; n += ROWS) {
+        Pack<T, V> p[ROWS][NV], q[ROWS][NV];
+        float mean[ROWS], rstd[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const bool in = g < a.G && n + r < n1;
+            mean[r] = in ? a.mean[(n + r) * a.G + g] : 0.f;
+            rstd[r] = in ? a.rstd[(n + r) * a.G + g] : 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                p[r][k] = real[k] && in ? load_pack<T, V>(a.x + (n + r) * a.ldx + c[k]) : zero_pack<T, V>();
+                q[r][k] = real[k] && in ? load_pack<T, V>(a.dy + (n + r) * a.lddy + c[k]) : zero_pack<T, V>();
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            float xn[NV][V], d[NV][V], m1 = 0.f, m2 = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                unpack(p[r][k], xn[k]);
+                unpack(q[r][k], d[k]);
+                if (!real[k] || n + r >= n1) continue;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    xn[k][i] = (xn[k][i] - mean[r]) * rstd[r];
+                    d[k][i] *= activate_slope(fmaf(xn[k][i], gamma[k][i], beta[k][i]), a.act);
+                    sum1[k][i] += d[k][i];
+                    sum2[k][i] = fmaf(d[k][i], xn[k][i], sum2[k][i]);
+                    d[k][i] *= gamma[k][i];
+                    m1 += d[k][i];
+                    m2 = fmaf(d[k][i], xn[k][i], m2);
+                }
+            }
+            m1 = lanes_sum(m1, a.lanes) * inv;
+            m2 = lanes_sum(m2, a.lanes) * inv;
+            if (n + r >= n1) continue;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                if (!real[k]) continue;
+                float o[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] = rstd[r] * (d[k][i] - m1 - xn[k][i] * m2);
+                store_pack(a.dx + (n + r) * a.lddx + c[k], pack<T, V>(o));
+            }
+        }
+    }
+    if (!a.channels) return;
+    float* out = a.channels + (size_t)chunk * 2 * a.C;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        if (!real[k]) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[c[k] + i] = sum1[k][i], out[a.C + c[k] + i] = sum2[k][i];
+    }
+}
+
+// ----------------------------------------------------------------------------------------------------- slab and stream
+
+// What a block takes: `groups` groups of sample n from channel c0 on, rows r0 .. r1.  A thread keeps to one pack of channels and takes every
+// `step`th row; wider rows than the block has threads (one group then) are taken a block's width at a time.
+template <typename T, int V>
+struct Part {
+    int part, groups, c0, width, packs, step, turns, r0, r1;
+    long long n;
+    __device__ explicit Part(const NormArgs<T>& a)
+    {
+        unsigned bx = blockIdx.x;
+        part = (int)(bx % a.parts);
+        bx /= a.parts;
+        const int tile = (int)(bx % a.tiles);
+        n = bx / a.tiles;
+        groups = min(a.tile_groups, a.G - tile * a.tile_groups);
+        c0 = tile * a.tile_groups * a.E;
+        width = groups * a.E;
+        packs = width / V;
+        step = packs <= kThreads ? kThreads / packs : 1;
+        turns = packs <= kThreads ? 1 : (packs + kThreads - 1) / kThreads;
+        r0 = min(part * a.part_rows, a.S), r1 = min(r0 + a.part_rows, a.S);
+    }
+    // the pack of this thread in turn q, or -1
+    __device__ int pack_of(int q) const
+    {
+        const int tid = threadIdx.x;
+        if (turns == 1) return tid < step * packs ? tid % packs : -1;
+        const int p = tid + q * kThreads;
+        return p < packs ? p : -1;
+    }
+    __device__ int first_row() const { return turns == 1 ? r0 + (int)threadIdx.x / packs : r0; }
+};
+
+// Sum over the threads that hold group gi of what `value` gives for a thread index, by one warp.
+template <typename T, int V, typename F>
+__device__ __forceinline__ float group_sum(const Part<T, V>& p, int E, int gi, F value)
+{
+    const int lane = threadIdx.x & 31;
+    float s = 0.f;
+    if (p.turns == 1) {
+        const int ev = E / V;
+        for (int k = lane; k < p.step * ev; k += 32) s += value(k / ev * p.packs + gi * ev + k % ev);
+    } else {
+        for (int k = lane; k < kThreads; k += 32) s += value(k);
+    }
+    return lanes_sum(s, 32);
+}
+
+enum { kSlab = 0, kStreamStats = 1, kStreamApply = 2 };
+
+template <typename T, int V, int MODE>
+__global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<T> a)
+{
+    ptx::grid_dep_wait();
+    extern __shared__ float4 smem4[];
+    __shared__ float ecount[kThreads], emean[kThreads], em2[kThreads];
+    float4* gstat = smem4;                                   // [tile_groups] count, mean, sum of squares about it; then mean, rstd
+    float2* gnorm = reinterpret_cast<float2*>(gstat + a.tile_groups);
+    Pack<T, V>* kept = reinterpret_cast<Pack<T, V>*>(reinterpret_cast<float4*>(gnorm) + (a.tile_groups + 1) / 2);
+    const Part<T, V> p(a);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int g0 = p.c0 / a.E;
+    const T* x = a.x + p.n * a.S * a.ldx + p.c0;
+
+    if (MODE != kStreamApply) {
+        float shift = 0.f, s1 = 0.f, s2 = 0.f;
+        int count = 0;
+        for (int q = 0; q < p.turns; ++q) {
+            const int pk = p.pack_of(q);
+            if (pk < 0) continue;
+            for (int r = p.first_row(); r < p.r1; r += 4 * p.step) {
+                Pack<T, V> in[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (r + j * p.step < p.r1) in[j] = load_pack<T, V>(x + (r + j * p.step) * a.ldx + pk * V);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (r + j * p.step >= p.r1) break;
+                    if (MODE == kSlab) kept[(size_t)(r + j * p.step - p.r0) * p.packs + pk] = in[j];
+                    float v[V];
+                    unpack(in[j], v);
+                    if (count == 0) shift = v[0];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float d = v[i] - shift;
+                        s1 += d;
+                        s2 = fmaf(d, d, s2);
+                    }
+                    count += V;
+                }
+            }
+        }
+        const float cnt = (float)count, off = count ? s1 / cnt : 0.f;
+        ecount[threadIdx.x] = cnt;
+        emean[threadIdx.x] = shift + off;
+        em2[threadIdx.x] = s2 - s1 * off;
+        __syncthreads();
+        for (int gi = warp; gi < p.groups; gi += kWarps) {
+            const float n = group_sum(p, a.E, gi, [&](int t) { return ecount[t]; });
+            const float base = group_sum(p, a.E, gi, [&](int t) { return ecount[t] * emean[t]; });
+            const float mean = n > 0.f ? base / n : 0.f;
+            const float m2 = group_sum(p, a.E, gi, [&](int t) {
+                const float d = emean[t] - mean;
+                return ecount[t] > 0.f ? fmaf(ecount[t] * d, d, em2[t]) : 0.f;
+            });
+            if (lane == 0) {
+                const float4 st = make_float4(n, mean, m2, 0.f);
+                if (MODE == kSlab) gstat[gi] = st;
+                else a.part_stats[((size_t)p.n * a.G + g0 + gi) * a.parts + p.part] = st;
+            }
+        }
+        if (MODE == kStreamStats) return;
+    }
+    if (MODE == kSlab) cg::this_cluster().sync();
+    for (int gi = warp; gi < p.groups; gi += kWarps) {
+        auto stat = [&](int k) {
+            if (MODE == kSlab) return cg::this_cluster().map_shared_rank(gstat, k)[gi];
+            return a.part_stats[((size_t)p.n * a.G + g0 + gi) * a.parts + k];
+        };
+        float n = 0.f, base = 0.f, m2 = 0.f;
+        for (int k = lane; k < a.parts; k += 32) {
+            const float4 st = stat(k);
+            n += st.x;
+            base = fmaf(st.x, st.y, base);
+        }
+        n = lanes_sum(n, 32);
+        const float mean = lanes_sum(base, 32) / n;
+        for (int k = lane; k < a.parts; k += 32) {
+            const float4 st = stat(k);
+            const float d = st.y - mean;
+            if (st.x > 0.f) m2 += fmaf(st.x * d, d, st.z);
+        }
+        const float rstd = rsqrtf(lanes_sum(m2, 32) / n + a.eps);
+        if (lane == 0) {
+            gnorm[gi] = make_float2(mean, rstd);
+            if (p.part == 0) {
+                if (a.mean) a.mean[p.n * a.G + g0 + gi] = mean;
+                if (a.rstd) a.rstd[p.n * a.G + g0 + gi] = rstd;
+            }
+        }
+    }
+    __syncthreads();
+    T* y = a.y + p.n * a.S * a.ldy + p.c0;
+    for (int q = 0; q < p.turns; ++q) {
+        const int pk = p.pack_of(q);
+        if (pk < 0) continue;
+        const float2 st = gnorm[pk * V / a.E];
+        float scale[V], beta[V];
+        load_params<V>(a.gamma, 1.f, p.c0 + pk * V, true, scale);
+        load_params<V>(a.beta, 0.f, p.c0 + pk * V, true, beta);
+        for (int r = p.first_row(); r < p.r1; r += 4 * p.step) {
+            Pack<T, V> in[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int rr = r + j * p.step;
+                if (rr < p.r1) in[j] = MODE == kSlab ? kept[(size_t)(rr - p.r0) * p.packs + pk] : load_pack<T, V>(x + rr * a.ldx + pk * V);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (r + j * p.step >= p.r1) break;
+                float v[V];
+                unpack(in[j], v);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = activate(fmaf((v[i] - st.x) * st.y, scale[i], beta[i]), a.act);
+                store_pack(y + (r + j * p.step) * a.ldy + pk * V, pack<T, V>(v));
+            }
+        }
+    }
+    if (MODE == kSlab) cg::this_cluster().sync();            // the statistics stay readable until all blocks have them
+}
+
+template <typename T, int V, int MODE>
+__global__ void __launch_bounds__(kThreads) norm_slab_bwd_kernel(const NormArgs<T> a)
+{
+    ptx::grid_dep_wait();
+    extern __shared__ float4 smem4[];
+    __shared__ float e1[kThreads], e2[kThreads];
+    float4* gsum = smem4;                                    // [tile_groups] sums over the part of gamma d and gamma d x^
+    float2* gmean = reinterpret_cast<float2*>(gsum + a.tile_groups);
+    float* csum = reinterpret_cast<float*>(reinterpret_cast<float4*>(gmean) + (a.tile_groups + 1) / 2);       // [2][kThreads * V]
+    Pack<T, V>* kept = reinterpret_cast<Pack<T, V>*>(csum + (MODE == kStreamApply ? 0 : 2 * kThreads * V));
+    const Part<T, V> p(a);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int g0 = p.c0 / a.E, rows = p.r1 - p.r0;
+    const T* x = a.x + p.n * a.S * a.ldx + p.c0;
+    const T* dy = a.dy + p.n * a.S * a.lddy + p.c0;
+
+    if (MODE != kStreamApply) {
+        float m1 = 0.f, m2 = 0.f;
+        for (int q = 0; q < p.turns; ++q) {
+            const int pk = p.pack_of(q);
+            float s1[V] = {}, s2[V] = {};
+            if (pk >= 0) {
+                const int g = g0 + pk * V / a.E;
+                const float mean = a.mean[p.n * a.G + g], rstd = a.rstd[p.n * a.G + g];
+                float gamma[V], beta[V];
+                load_params<V>(a.gamma, 1.f, p.c0 + pk * V, true, gamma);
+                load_params<V>(a.beta, 0.f, p.c0 + pk * V, true, beta);
+                for (int r = p.first_row(); r < p.r1; r += 2 * p.step) {
+                    Pack<T, V> xin[2], gin[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int rr = r + j * p.step;
+                        if (rr < p.r1) xin[j] = load_pack<T, V>(x + rr * a.ldx + pk * V), gin[j] = load_pack<T, V>(dy + rr * a.lddy + pk * V);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int rr = r + j * p.step;
+                        if (rr >= p.r1) break;
+                        if (MODE == kSlab) {
+                            kept[(size_t)(rr - p.r0) * p.packs + pk] = xin[j];
+                            kept[(size_t)(rows + rr - p.r0) * p.packs + pk] = gin[j];
+                        }
+                        float v[V], d[V];
+                        unpack(xin[j], v);
+                        unpack(gin[j], d);
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            const float xn = (v[i] - mean) * rstd;
+                            d[i] *= activate_slope(fmaf(xn, gamma[i], beta[i]), a.act);
+                            s1[i] += d[i];
+                            s2[i] = fmaf(d[i], xn, s2[i]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) m1 = fmaf(gamma[i], s1[i], m1), m2 = fmaf(gamma[i], s2[i], m2);
+            }
+            if (a.channels) {
+                float* out = a.channels + ((size_t)p.n * a.parts + p.part) * 2 * a.C + p.c0;
+                if (p.step == 1) {
+                    if (pk >= 0) {
+#pragma unroll
+                        for (int i = 0; i < V; ++i) out[pk * V + i] = s1[i], out[a.C + pk * V + i] = s2[i];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) csum[threadIdx.x * V + i] = s1[i], csum[(kThreads + threadIdx.x) * V + i] = s2[i];
+                    __syncthreads();
+                    for (int k = threadIdx.x; k < 2 * p.width; k += kThreads) {
+                        const int which = k / p.width, c = k % p.width;
+                        float s = 0.f;
+                        for (int j = 0; j < p.step; ++j) s += csum[which * kThreads * V + j * p.width + c];
+                        out[which * a.C + c] = s;
+                    }
+                }
+            }
+        }
+        e1[threadIdx.x] = m1, e2[threadIdx.x] = m2;
+        __syncthreads();
+        for (int gi = warp; gi < p.groups; gi += kWarps) {
+            const float t1 = group_sum(p, a.E, gi, [&](int t) { return e1[t]; });
+            const float t2 = group_sum(p, a.E, gi, [&](int t) { return e2[t]; });
+            if (lane == 0) {
+                const float4 st = make_float4(t1, t2, 0.f, 0.f);
+                if (MODE == kSlab) gsum[gi] = st;
+                else a.part_stats[((size_t)p.n * a.G + g0 + gi) * a.parts + p.part] = st;
+            }
+        }
+        if (MODE == kStreamStats) return;
+    }
+    if (MODE == kSlab) cg::this_cluster().sync();
+    for (int gi = warp; gi < p.groups; gi += kWarps) {
+        float t1 = 0.f, t2 = 0.f;
+        for (int k = lane; k < a.parts; k += 32) {
+            const float4 st = MODE == kSlab ? cg::this_cluster().map_shared_rank(gsum, k)[gi]
+                                            : a.part_stats[((size_t)p.n * a.G + g0 + gi) * a.parts + k];
+            t1 += st.x, t2 += st.y;
+        }
+        t1 = lanes_sum(t1, 32), t2 = lanes_sum(t2, 32);
+        const float inv = 1.f / ((float)a.S * a.E);
+        if (lane == 0) gmean[gi] = make_float2(t1 * inv, t2 * inv);
+    }
+    __syncthreads();
+    T* dx = a.dx + p.n * a.S * a.lddx + p.c0;
+    for (int q = 0; q < p.turns; ++q) {
+        const int pk = p.pack_of(q);
+        if (pk < 0) continue;
+        const int gi = pk * V / a.E;
+        const float2 m = gmean[gi];
+        const float mean = a.mean[p.n * a.G + g0 + gi], rstd = a.rstd[p.n * a.G + g0 + gi];
+        float gamma[V], beta[V];
+        load_params<V>(a.gamma, 1.f, p.c0 + pk * V, true, gamma);
+        load_params<V>(a.beta, 0.f, p.c0 + pk * V, true, beta);
+        for (int r = p.first_row(); r < p.r1; r += 2 * p.step) {
+            Pack<T, V> xin[2], gin[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int rr = r + j * p.step;
+                if (rr >= p.r1) continue;
+                if (MODE == kSlab) {
+                    xin[j] = kept[(size_t)(rr - p.r0) * p.packs + pk];
+                    gin[j] = kept[(size_t)(rows + rr - p.r0) * p.packs + pk];
+                } else {
+                    xin[j] = load_pack<T, V>(x + rr * a.ldx + pk * V);
+                    gin[j] = load_pack<T, V>(dy + rr * a.lddy + pk * V);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (r + j * p.step >= p.r1) break;
+                float v[V], d[V];
+                unpack(xin[j], v);
+                unpack(gin[j], d);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float xn = (v[i] - mean) * rstd;
+                    d[i] *= activate_slope(fmaf(xn, gamma[i], beta[i]), a.act) * gamma[i];
+                    v[i] = rstd * (d[i] - m.x - xn * m.y);
+                }
+                store_pack(dx + (r + j * p.step) * a.lddx + pk * V, pack<T, V>(v));
+            }
+        }
+    }
+    if (MODE == kSlab) cg::this_cluster().sync();
+}
+
+// --------------------------------------------------------------------------------------------------------------- plan
+
+constexpr size_t kSlabBytes = 96 * 1024;      // rows that a block keeps: two blocks an SM
+constexpr int kMaxCluster = 8, kSms = 148;
+
+// How a call is cut.  The sizes decide, and whether rows can be moved in packs of 16 bytes; the workspace has room for either.
+struct NormPlan {
+    bool rows, slab;
+    int lanes, nv, chunks, chunk;             // rows
+    int tile_groups, tiles, parts, part_rows; // slab, stream
+    size_t stats, channels;                   // floats of workspace
+};
+
+NormPlan make_norm_plan(int N, int S, int C, int G, int esize, int V, bool bwd)
+{
+    NormPlan p{};
+    const int E = C / G, ev = E / V;
+    int lanes = 1;
+    while (lanes < 32 && lanes < ev) lanes *= 2;
+    const int nv = (ev + lanes - 1) / lanes;
+    if (S == 1 && nv <= (bwd ? 4 : 8)) {
+        p.rows = true;
+        p.lanes = lanes;
+        p.nv = nv <= 1 ? 1 : nv <= 2 ? 2 : nv <= 4 ? 4 : 8;
+        // as many chunks of samples as fill the machine (eight blocks an SM), at least four samples each
+        const long long cols = ((long long)G * lanes + kThreads - 1) / kThreads;
+        long long chunks = (8LL * kSms + cols - 1) / cols;
+        if (chunks > (N + 3) / 4) chunks = (N + 3) / 4;
+        p.chunk = (int)((N + chunks - 1) / chunks);
+        p.chunks = (N + p.chunk - 1) / p.chunk;
+        p.channels = bwd ? (size_t)p.chunks * 2 * C : 0;
+        return p;
+    }
+    // groups of a tile: rows of 128 bytes or more, but not more packs than threads
+    p.tile_groups = (128 + E * esize - 1) / (E * esize);
+    if (p.tile_groups > G) p.tile_groups = G;
+    while (p.tile_groups > 1 && p.tile_groups * ev > kThreads) --p.tile_groups;
+    p.tiles = (G + p.tile_groups - 1) / p.tile_groups;
+    const size_t row = (size_t)p.tile_groups * E * esize * (bwd ? 2 : 1);
+    const long long slabs = (long long)N * p.tiles;
+    // a cluster of the fewest blocks that hold the slab; more while there are SMs left and rows to share out
+    int parts = 1;
+    while (parts < kMaxCluster && (size_t)((S + parts - 1) / parts) * row > kSlabBytes) parts *= 2;
+    p.slab = (size_t)((S + parts - 1) / parts) * row <= kSlabBytes;
+    while (p.slab && parts < kMaxCluster && slabs * parts < 2 * kSms && S / parts >= 32) parts *= 2;
+    if (p.slab && slabs * parts < kSms / 2 && (double)S * row * slabs > 4e6) p.slab = false;
+    if (!p.slab) {
+        const long long want = (8LL * kSms + slabs - 1) / slabs;
+        parts = (int)(want < 1 ? 1 : want > 1024 ? 1024 : want);
+        if (parts > (S + 15) / 16) parts = (S + 15) / 16;
+    }
+    p.part_rows = (S + parts - 1) / parts;
+    p.parts = p.slab ? parts : (S + p.part_rows - 1) / p.part_rows;
+    p.stats = p.slab ? 0 : (size_t)N * G * p.parts * 4;
+    p.channels = bwd ? (size_t)N * p.parts * 2 * C : 0;
+    return p;
+}
+
+// Every element type and pack width that the sizes allow.
+size_t workspace_floats(int N, int S, int C, int G, bool bwd)
+{
+    size_t most = 0;
+    for (int esize = 2; esize <= 4; esize += 2)
+        for (int V = 1; V <= 16 / esize; V = V == 1 ? 16 / esize : 17) {
+            if ((C / G) % V) continue;
+            const NormPlan p = make_norm_plan(N, S, C, G, esize, V, bwd);
+            if (p.stats + p.channels > most) most = p.stats + p.channels;
+        }
+    return most;
+}
+
+// Column (which, c) of the partial sums [parts][2][C].
+struct ParamStore {
+    float *dgamma, *dbeta;
+    int C;
+    __device__ void operator()(long long col, float s) const
+    {
+        if (col < C) {
+            if (dbeta) dbeta[col] = s;
+        } else if (dgamma) {
+            dgamma[col - C] = s;
+        }
+    }
+};
+
+template <typename T>
+NormArgs<T> make_args(const NormSeq& s, const NormPlan& p)
+{
+    NormArgs<T> a{};
+    a.x = static_cast<const T*>(s.x), a.dy = static_cast<const T*>(s.dy), a.gamma = s.gamma, a.beta = s.beta;
+    a.y = static_cast<T*>(s.y), a.dx = static_cast<T*>(s.dx), a.mean = s.mean, a.rstd = s.rstd;
+    a.part_stats = reinterpret_cast<float4*>(s.ws);
+    a.channels = s.dgamma || s.dbeta ? s.ws + p.stats : nullptr;
+    a.N = s.N, a.S = s.S, a.C = s.C, a.G = s.G, a.E = s.C / s.G;
+    a.ldx = s.ldx, a.ldy = s.ldy, a.lddy = s.lddy, a.lddx = s.lddx, a.eps = s.eps, a.act = s.act;
+    a.lanes = p.lanes, a.chunks = p.chunks, a.chunk = p.chunk;
+    a.tile_groups = p.tile_groups, a.tiles = p.tiles, a.parts = p.parts, a.part_rows = p.part_rows;
+    return a;
+}
+
+template <typename... KArgs, typename... Args>
+conv2d_status_t launched(void (*kernel)(KArgs...), long long blocks, size_t smem, unsigned cluster, cudaStream_t stream, Args... args)
+{
+    if (blocks > 0x7fffffffLL) return CONV2D_ERR_SHAPE;
+    const cudaError_t e = cluster > 1 ? launch_pdl_cluster(kernel, dim3((unsigned)blocks), dim3(kThreads), smem, stream, cluster, args...)
+                                      : launch_pdl(kernel, dim3((unsigned)blocks), dim3(kThreads), smem, stream, args...);
+    if (e != cudaSuccess) return CONV2D_ERR_CUDA;
+    count_launch();
+    return CONV2D_OK;
+}
+
+template <typename T, int V>
+conv2d_status_t fwd(const NormSeq& s, cudaStream_t stream)
+{
+    const NormPlan p = make_norm_plan(s.N, s.S, s.C, s.G, sizeof(T), V, false);
+    const NormArgs<T> a = make_args<T>(s, p);
+    if (p.rows) {
+        const long long blocks = (long long)ceil_div_u((long long)s.G * p.lanes, kThreads) * p.chunks;
+        if (p.nv == 1) return launched(norm_rows_fwd_kernel<T, V, 1, 4>, blocks, 0, 1, stream, a);
+        if (p.nv == 2) return launched(norm_rows_fwd_kernel<T, V, 2, 2>, blocks, 0, 1, stream, a);
+        if (p.nv == 4) return launched(norm_rows_fwd_kernel<T, V, 4, 1>, blocks, 0, 1, stream, a);
+        return launched(norm_rows_fwd_kernel<T, V, 8, 1>, blocks, 0, 1, stream, a);
+    }
+    const long long blocks = (long long)s.N * p.tiles * p.parts;
+    const size_t fixed = (size_t)p.tile_groups * 16 + (p.tile_groups + 1) / 2 * 16;
+    if (p.slab) {
+        const size_t smem = fixed + (size_t)p.part_rows * p.tile_groups * a.E * sizeof(T);
+        static SmemLimit limit;
+        if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_fwd_kernel<T, V, kSlab>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+        return launched(norm_slab_fwd_kernel<T, V, kSlab>, blocks, smem, p.parts, stream, a);
+    }
+    const conv2d_status_t st = launched(norm_slab_fwd_kernel<T, V, kStreamStats>, blocks, fixed, 1, stream, a);
+    return st != CONV2D_OK ? st : launched(norm_slab_fwd_kernel<T, V, kStreamApply>, blocks, fixed, 1, stream, a);
+}
+
+template <typename T, int V>
+conv2d_status_t bwd(const NormSeq& s, cudaStream_t stream)
+{
+    const NormPlan p = make_norm_plan(s.N, s.S, s.C, s.G, sizeof(T), V, true);
+    const NormArgs<T> a = make_args<T>(s, p);
+    conv2d_status_t st;
+    long long parts = (long long)s.N * p.parts;
+    if (p.rows) {
+        parts = p.chunks;
+        const long long blocks = (long long)ceil_div_u((long long)s.G * p.lanes, kThreads) * p.chunks;
+        if (p.nv == 1) st = launched(norm_rows_bwd_kernel<T, V, 1, 4>, blocks, 0, 1, stream, a);
+        else if (p.nv == 2) st = launched(norm_rows_bwd_kernel<T, V, 2, 2>, blocks, 0, 1, stream, a);
+        else st = launched(norm_rows_bwd_kernel<T, V, 4, 1>, blocks, 0, 1, stream, a);
+    } else {
+        const long long blocks = (long long)s.N * p.tiles * p.parts;
+        const size_t fixed = (size_t)p.tile_groups * 16 + (p.tile_groups + 1) / 2 * 16, sums = sizeof(float) * 2 * kThreads * V;
+        if (p.slab) {
+            const size_t smem = fixed + sums + (size_t)p.part_rows * p.tile_groups * a.E * sizeof(T) * 2;
+            static SmemLimit limit;
+            if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_bwd_kernel<T, V, kSlab>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+            st = launched(norm_slab_bwd_kernel<T, V, kSlab>, blocks, smem, p.parts, stream, a);
+        } else {
+            st = launched(norm_slab_bwd_kernel<T, V, kStreamStats>, blocks, fixed + sums, 1, stream, a);
+            if (st == CONV2D_OK) st = launched(norm_slab_bwd_kernel<T, V, kStreamApply>, blocks, fixed, 1, stream, a);
+        }
+    }
+    if (st != CONV2D_OK || !a.channels) return st;
+    return launch_column_sums(a.channels, parts, 2LL * s.C, 2LL * s.C, ParamStore{s.dgamma, s.dbeta, s.C}, stream);
+}
+
+// Packs of 16 bytes where every row of every tensor begins on such a boundary and no pack crosses from one group to the next.
+template <typename T>
+bool wide(const NormSeq& s)
+{
+    constexpr int e = sizeof(T), V = 16 / e;
+    return (s.C / s.G) % V == 0 && rows_aligned(s.x, s.ldx, e, 16) && rows_aligned(s.y, s.ldy, e, 16) && rows_aligned(s.dy, s.lddy, e, 16)
+        && rows_aligned(s.dx, s.lddx, e, 16);
+}
+
+template <typename T> conv2d_status_t fwd_typed(const NormSeq& s, cudaStream_t st) { return wide<T>(s) ? fwd<T, 16 / sizeof(T)>(s, st) : fwd<T, 1>(s, st); }
+template <typename T> conv2d_status_t bwd_typed(const NormSeq& s, cudaStream_t st) { return wide<T>(s) ? bwd<T, 16 / sizeof(T)>(s, st) : bwd<T, 1>(s, st); }
+
+}  // namespace
+
+size_t norm_fwd_workspace_bytes(int N, int S, int C, int G) { return sizeof(float) * workspace_floats(N, S, C, G, false); }
+size_t norm_bwd_workspace_bytes(int N, int S, int C, int G) { return sizeof(float) * workspace_floats(N, S, C, G, true); }
+
+conv2d_status_t launch_norm_fwd(const NormSeq& s, conv2d_operand_t type, cudaStream_t stream)
+{
+    if (type == CONV2D_OPERAND_BF16) return fwd_typed<bf16>(s, stream);
+    if (type == CONV2D_OPERAND_FP16) return fwd_typed<fp16>(s, stream);
+    return fwd_typed<float>(s, stream);
+}
+conv2d_status_t launch_norm_bwd(const NormSeq& s, conv2d_operand_t type, cudaStream_t stream)
+{
+    if (type == CONV2D_OPERAND_BF16) return bwd_typed<bf16>(s, stream);
+    if (type == CONV2D_OPERAND_FP16) return bwd_typed<fp16>(s, stream);
+    return bwd_typed<float>(s, stream);
+}
+
+}  // namespace conv2d_b200

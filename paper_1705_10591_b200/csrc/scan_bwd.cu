@@ -1,0 +1,156 @@
+// Launchers of the backward scan.
+#include "scan_bwd.cuh"
+
+namespace conv2d_b200 {
+namespace {
+
+// Columns of the partial sums by channel: dA, then dDskip, then ddelta_bias.
+struct ChannelStore {
+    float *dA, *dD, *dbias;
+    int D, N, NQ;
+    __device__ void operator()(long long col, float s) const
+    {
+        const long long quads = (long long)D * NQ;
+        if (col < quads) {
+            if (col % NQ < N) dA[col / NQ * N + col % NQ] = s;
+        } else if (col < quads + D) {
+            if (dD) dD[col - quads] = s;
+        } else if (dbias) {
+            dbias[col - quads - D] = s;
+        }
+    }
+};
+
+// dB, dC from the blocks' partial sums; a thread per row, group, tensor and state.
+template <typename T>
+__global__ void __launch_bounds__(256) scan_bwd_rows_kernel(const float* __restrict__ in, const int* lengths, T* dB, T* dC, int parts, long long rows, int L,
+                                                            int G, int N, int NP, long long lddB, long long lddC)
+{
+    ptx::grid_dep_wait();
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int i = (int)(id % (2 * NP)), n = i % NP;
+    const long long rg = id / (2 * NP), row = rg / G;
+    const int g = (int)(rg % G);
+    if (row >= rows || n >= N) return;
+    float s = 0.f;
+    if (row % L < sequence_length(lengths, (int)(row / L), L)) {
+        const float* p = in + (((size_t)g * parts) * rows + row) * (2 * NP) + i;
+        for (int k = 0; k < parts; ++k) s += p[(size_t)k * rows * (2 * NP)];
+    }
+    if (i < NP) dB[row * lddB + (long long)g * N + n] = from_float<T>(s);
+    else dC[row * lddC + (long long)g * N + n] = from_float<T>(s);
+}
+
+// How the backward pass is cut: channel sets a block takes in turn, segments of time.
+struct BwdCut { int nl, cb, sets, blocks_group, segs, rows; };
+BwdCut bwd_cut(int B, int L, int D, int N, int G)
+{
+    BwdCut c;
+    c.nl = lanes_for(N);
+    c.cb = 128 / c.nl;
+    const int E = D / G;
+    c.sets = env_int("CONV2D_B200_SCAN_SETS", 0);
+    if (c.sets <= 0) c.sets = 1;
+    c.blocks_group = (int)ceil_div_u(E, (long long)c.cb * c.sets);
+    int segs = env_int("CONV2D_B200_SCAN_BWD_SEGS", 0);
+    if (segs <= 0) segs = 1;
+    c.rows = (int)(ceil_div_u(ceil_div_u(L, segs), kCheckpointRows) * kCheckpointRows);
+    c.segs = (int)ceil_div_u(L, c.rows);
+    return c;
+}
+
+struct BwdLayout { size_t local, steps, per_channel, per_row, total; };   // offsets in floats, each a multiple of four
+BwdLayout bwd_layout(const BwdCut& c, int B, int L, int D, int N, int G)
+{
+    auto up4 = [](size_t n) { return (n + 3) / 4 * 4; };
+    const size_t NQ = round4(N), bs = (size_t)B * c.segs;
+    BwdLayout o;
+    o.local = 0;
+    o.steps = o.local + (c.segs > 1 ? bs * D * NQ : 0);
+    o.per_channel = o.steps + (c.segs > 1 ? up4(bs * D) : 0);
+    o.per_row = o.per_channel + bs * channel_floats(D, (int)NQ);
+    o.total = o.per_row + (size_t)G * c.blocks_group * B * L * 2 * c.nl * kSpt;
+    return o;
+}
+
+template <typename T, int NL, int V>
+conv2d_status_t bwd(const ScanSeq& s, cudaStream_t stream)
+{
+    using Tile = ScanBwdTile<NL>;
+    ScanBwdArgs<T> a;
+    a.u = static_cast<const T*>(s.u), a.delta = static_cast<const T*>(s.delta), a.z = static_cast<const T*>(s.z), a.dy = static_cast<const T*>(s.dy);
+    a.Bm = static_cast<const T*>(s.Bm), a.Cm = static_cast<const T*>(s.Cm);
+    a.A = s.A, a.Dskip = s.Dskip, a.delta_bias = s.delta_bias, a.states = s.states_in, a.dstate_out = s.dstate_out, a.lengths = s.lengths;
+    a.du = static_cast<T*>(s.du), a.ddelta = static_cast<T*>(s.ddelta), a.dz = static_cast<T*>(s.dz), a.dstate_in = s.dstate_in;
+    a.B = s.B, a.L = s.L, a.D = s.D, a.N = s.N, a.G = s.G, a.E = s.D / s.G;
+    a.ldu = s.ldu, a.lddelta = s.lddelta, a.ldB = s.ldB, a.ldC = s.ldC, a.ldz = s.ldz, a.lddy = s.lddy;
+    a.lddu = s.lddu, a.ldddelta = s.ldddelta, a.lddz = s.lddz, a.softplus = s.softplus;
+    const BwdCut c = bwd_cut(s.B, s.L, s.D, s.N, s.G);
+    const BwdLayout o = bwd_layout(c, s.B, s.L, s.D, s.N, s.G);
+    a.segs = c.segs, a.seg_rows = c.rows, a.blocks_group = c.blocks_group, a.sets = c.sets;
+    a.local = s.ws + o.local, a.steps = s.ws + o.steps, a.per_channel = s.ws + o.per_channel, a.per_row = s.ws + o.per_row;
+    const long long jobs = (long long)s.B * a.segs * s.G, blocks = jobs * c.blocks_group, rows = (long long)s.B * s.L;
+    const int carry_group = (int)ceil_div_u(a.E, Tile::CB);
+    const long long join = (long long)s.B * s.D * round4(s.N), per_row = rows * s.G * 2 * Tile::NP;
+    if (jobs * carry_group > 0x7fffffffLL || per_row / 256 > 0x7ffffff0LL) return CONV2D_ERR_SHAPE;
+    if (a.segs > 1) {
+        if (launch_pdl(scan_bwd_carry_kernel<T, NL, V>, dim3((unsigned)(jobs * carry_group)), dim3(128), 0, stream, a, carry_group) != cudaSuccess)
+            return CONV2D_ERR_CUDA;
+        count_launch();
+        if (launch_pdl(scan_join_kernel<true>, dim3(ceil_div_u(join, 256)), dim3(256), 0, stream, a.local, a.steps, s.A, s.dstate_out, s.dstate_in,
+                       s.B, a.segs, s.D, s.N) != cudaSuccess) return CONV2D_ERR_CUDA;
+        count_launch();
+    }
+    const size_t smem = sizeof(float) * (Tile::fixed_floats + a.sets * Tile::template set_floats<V>());
+    static SmemLimit limit;
+    if (raise_smem_limit(reinterpret_cast<const void*>(scan_bwd_kernel<T, NL, V>), smem, limit) != cudaSuccess
+        || launch_pdl(scan_bwd_kernel<T, NL, V>, dim3((unsigned)blocks), dim3(128), smem, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
+    count_launch();
+    const conv2d_status_t st = launch_column_sums(a.per_channel, (long long)s.B * a.segs, (long long)s.D * (round4(s.N) + 2), channel_floats(s.D, round4(s.N)),
+                                                  ChannelStore{s.dA, s.dD, s.ddelta_bias, s.D, s.N, round4(s.N)}, stream);
+    if (st != CONV2D_OK) return st;
+    if (launch_pdl(scan_bwd_rows_kernel<T>, dim3(ceil_div_u(per_row, 256)), dim3(256), 0, stream, a.per_row, s.lengths, static_cast<T*>(s.dB),
+                   static_cast<T*>(s.dC), c.blocks_group, rows, s.L, s.G, s.N, Tile::NP, s.lddB, s.lddC) != cudaSuccess) return CONV2D_ERR_CUDA;
+    count_launch();
+    return CONV2D_OK;
+}
+
+template <typename T, int V>
+conv2d_status_t bwd_lanes(const ScanSeq& s, cudaStream_t stream)
+{
+    switch (lanes_for(s.N)) {
+        case 1: return bwd<T, 1, V>(s, stream);
+        case 2: return bwd<T, 2, V>(s, stream);
+        case 4: return bwd<T, 4, V>(s, stream);
+        case 8: return bwd<T, 8, V>(s, stream);
+        case 16: return bwd<T, 16, V>(s, stream);
+        case 32: return bwd<T, 32, V>(s, stream);
+    }
+    return CONV2D_ERR_UNSUPPORTED;
+}
+
+template <typename T>
+conv2d_status_t bwd_typed(const ScanSeq& s, cudaStream_t stream)
+{
+    constexpr int e = sizeof(T), n = 4 * e;
+    const bool wide = (s.D / s.G) % 4 == 0 && rows_aligned(s.u, s.ldu, e, n) && rows_aligned(s.delta, s.lddelta, e, n)
+                   && rows_aligned(s.z, s.ldz, e, n) && rows_aligned(s.dy, s.lddy, e, n) && rows_aligned(s.du, s.lddu, e, n)
+                   && rows_aligned(s.ddelta, s.ldddelta, e, n) && rows_aligned(s.dz, s.lddz, e, n);
+    return wide ? bwd_lanes<T, 4>(s, stream) : bwd_lanes<T, 1>(s, stream);
+}
+
+}  // namespace
+
+size_t scan_bwd_workspace_bytes(int B, int L, int D, int N, int G)
+{
+    return sizeof(float) * bwd_layout(bwd_cut(B, L, D, N, G), B, L, D, N, G).total;
+}
+
+conv2d_status_t launch_scan_bwd(const ScanSeq& s, conv2d_operand_t type, cudaStream_t stream)
+{
+    if (type == CONV2D_OPERAND_BF16) return bwd_typed<bf16>(s, stream);
+    if (type == CONV2D_OPERAND_FP16) return bwd_typed<fp16>(s, stream);
+    return bwd_typed<float>(s, stream);
+}
+
+}  // namespace conv2d_b200

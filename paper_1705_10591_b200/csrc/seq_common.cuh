@@ -1,0 +1,171 @@
+// What the operators along a sequence share: element types, vector loads and stores, activations.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+#include "ptx.cuh"
+#include "sequence_b200.h"
+
+namespace conv2d_b200 {
+
+using bf16 = __nv_bfloat16;
+using fp16 = __half;
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(bf16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(fp16 v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16 from_float<bf16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ fp16 from_float<fp16>(float v) { return __float2half_rn(v); }
+
+// V adjacent elements as they lie in memory, moved by one access (two for eight fp32).
+template <typename T, int V>
+struct alignas(sizeof(T) * V > 16 ? 16 : sizeof(T) * V) Pack { T e[V]; };
+
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> load_pack(const T* p) { return *reinterpret_cast<const Pack<T, V>*>(p); }
+template <typename T, int V> __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& v) { *reinterpret_cast<Pack<T, V>*>(p) = v; }
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> zero_pack()
+{
+    Pack<T, V> z;
+#pragma unroll
+    for (int i = 0; i < V; ++i) z.e[i] = from_float<T>(0.f);
+    return z;
+}
+template <typename T, int V> __device__ __forceinline__ void unpack(const Pack<T, V>& p, float (&f)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = to_float(p.e[i]);
+}
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> pack(const float (&f)[V])
+{
+    Pack<T, V> p;
+#pragma unroll
+    for (int i = 0; i < V; ++i) p.e[i] = from_float<T>(f[i]);
+    return p;
+}
+
+// 1 / (1 + e^-v) from the hardware's exponential and reciprocal: a few 2^-23 relative for |v| < 10, |v| 2^-23 beyond.
+__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+
+// The activation is the same for a whole launch: a uniform branch beside the memory access that it follows.
+__device__ __forceinline__ float activate(float v, int act)
+{
+    if (act == CONV2D_ACT_SILU) return v * sigmoid(v);
+    if (act == CONV2D_ACT_RELU) return v < 0.f ? 0.f : v;      // (NaN stays NaN)
+    if (act == CONV2D_ACT_GELU) return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+    return v;
+}
+// Its derivative at v.
+__device__ __forceinline__ float activate_slope(float v, int act)
+{
+    if (act == CONV2D_ACT_SILU) {
+        const float s = sigmoid(v);
+        return s * fmaf(v, 1.f - s, 1.f);
+    }
+    if (act == CONV2D_ACT_RELU) return v > 0.f ? 1.f : (v <= 0.f ? 0.f : v);
+    if (act == CONV2D_ACT_GELU)
+        return fmaf(v * 0.39894228040143268f, __expf(-0.5f * v * v), 0.5f * (1.f + erff(v * 0.70710678118654752f)));
+    return 1.f;
+}
+
+// Rows of sequence b that hold tokens.
+__device__ __forceinline__ int sequence_length(const int* lengths, int b, int L)
+{
+    if (!lengths) return L;
+    const int n = lengths[b];
+    return n < 0 ? 0 : (n > L ? L : n);
+}
+
+inline int element_size(conv2d_operand_t type) { return type == CONV2D_OPERAND_FP32 ? 4 : 2; }
+
+// Whether rows that begin at p and lie ld elements apart can be moved in units of `bytes`.
+inline bool rows_aligned(const void* p, long long ld, int esize, int bytes)
+{
+    return !p || (reinterpret_cast<uintptr_t>(p) % bytes == 0 && (ld * esize) % bytes == 0);
+}
+
+inline unsigned ceil_div_u(long long a, long long b) { return (unsigned)((a + b - 1) / b); }
+
+// Column sums of partial sums [parts][cols], `ld` floats apart, added in a fixed order: 32 columns by 8 shares of the parts a block;
+// `store` takes them.
+template <typename Store>
+__global__ void __launch_bounds__(256) column_sums_kernel(const float* __restrict__ in, long long parts, long long cols, long long ld, Store store)
+{
+    ptx::grid_dep_wait();
+    __shared__ float sums[8][32];
+    const long long col = (long long)blockIdx.x * 32 + threadIdx.x;
+    float s = 0.f;
+    if (col < cols) {
+#pragma unroll 4
+        for (long long p = threadIdx.y; p < parts; p += 8) s += in[p * ld + col];
+    }
+    sums[threadIdx.y][threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.y || col >= cols) return;
+    s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += sums[j][threadIdx.x];
+    store(col, s);
+}
+template <typename Store>
+conv2d_status_t launch_column_sums(const float* in, long long parts, long long cols, long long ld, Store store, cudaStream_t stream)
+{
+    if (launch_pdl(column_sums_kernel<Store>, dim3(ceil_div_u(cols, 32)), dim3(32, 8), 0, stream, in, parts, cols, ld, store) != cudaSuccess)
+        return CONV2D_ERR_CUDA;
+    count_launch();
+    return CONV2D_OK;
+}
+
+// Arguments of the launchers, as the entry points check them.
+struct ConvSeq {
+    const void *x, *w, *bias, *state_in, *dy, *dstate_out;
+    void *y, *state_out, *dx, *dstate_in;
+    float *dw, *dbias;
+    const int* lengths;
+    int B, L, D, K;
+    long long ldx, ldy, lddy, lddx;
+    conv2d_activation_t act;
+    float* partials;
+};
+conv2d_status_t launch_conv1d_fwd(const ConvSeq& a, conv2d_operand_t type, cudaStream_t stream);
+conv2d_status_t launch_conv1d_bwd(const ConvSeq& a, conv2d_operand_t type, cudaStream_t stream);
+size_t conv1d_bwd_workspace_bytes(int B, int L, int D, int K);
+
+struct ScanSeq {
+    const void *u, *delta, *Bm, *Cm, *z, *dy;
+    const float *A, *Dskip, *delta_bias, *state_in, *states_in, *dstate_out;
+    const int* lengths;
+    void *y, *du, *ddelta, *dB, *dC, *dz;
+    float *state_out, *states, *dA, *dD, *ddelta_bias, *dstate_in;
+    int B, L, D, N, G;
+    long long ldu, lddelta, ldB, ldC, ldz, ldy, lddy, lddu, ldddelta, lddB, lddC, lddz;
+    bool softplus;
+    float* ws;
+};
+conv2d_status_t launch_scan_fwd(const ScanSeq& a, conv2d_operand_t type, cudaStream_t stream);
+conv2d_status_t launch_scan_bwd(const ScanSeq& a, conv2d_operand_t type, cudaStream_t stream);
+conv2d_status_t launch_scan_step(const ScanSeq& a, conv2d_operand_t type, cudaStream_t stream);
+size_t scan_states_bytes(int B, int L, int D, int N);
+size_t scan_fwd_workspace_bytes(int B, int L, int D, int N, int G);
+size_t scan_bwd_workspace_bytes(int B, int L, int D, int N, int G);
+
+struct NormSeq {
+    const void *x, *dy;
+    const float *gamma, *beta;
+    void *y, *dx;
+    float *mean, *rstd, *dgamma, *dbeta;
+    int N, S, C, G;
+    long long ldx, ldy, lddy, lddx;
+    float eps;
+    conv2d_activation_t act;
+    float* ws;
+};
+conv2d_status_t launch_norm_fwd(const NormSeq& a, conv2d_operand_t type, cudaStream_t stream);
+conv2d_status_t launch_norm_bwd(const NormSeq& a, conv2d_operand_t type, cudaStream_t stream);
+size_t norm_fwd_workspace_bytes(int N, int S, int C, int G);
+size_t norm_bwd_workspace_bytes(int N, int S, int C, int G);
+
+}  // namespace conv2d_b200
