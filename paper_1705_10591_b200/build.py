@@ -15,7 +15,7 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libconv2d_b200.so"
 SOURCES = ["conv2d_api.cu", "single_channel.cu", "single_channel_flat.cu", "general_ffma.cu", "general_ffma_r1.cu", "general_ffma_r2.cu",
            "general_ffma_r3.cu", "general_ffma_r4.cu", "general_ffma_r5.cu", "general_ffma_r7.cu", "general_tf32.cu",
-           "pointwise_tma.cu", "sequence_api.cu", "conv1d_causal.cu", "scan_fwd.cu", "scan_bwd.cu", "norm_groups.cu"]
+           "pointwise_tma.cu", "sequence_api.cu", "conv1d_causal.cu", "scan_fwd.cu", "scan_step.cu", "scan_bwd.cu", "norm_groups.cu"]
 
 
 def _stale() -> bool:

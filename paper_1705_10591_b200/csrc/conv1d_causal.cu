@@ -69,23 +69,30 @@ __global__ void __launch_bounds__(kThreads) conv1d_fwd_kernel(const FwdArgs<T> a
         Pack<T, V> in[kAhead];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) in[j] = t + j < live ? load_pack<T, V>(x + (t + j) * a.ldx) : zero_pack<T, V>();
+        float out[kAhead * V];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            if (t + j >= live) break;
 #pragma unroll
             for (int k = 0; k < K - 1; ++k)
 #pragma unroll
                 for (int i = 0; i < V; ++i) win[k][i] = win[k + 1][i];
             unpack(in[j], win[K - 1]);
-            float out[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 float s = bias[i];
 #pragma unroll
                 for (int k = 0; k < K; ++k) s = fmaf(w[k][i], win[k][i], s);
-                out[i] = activate(s, a.act);
+                out[j * V + i] = s;
             }
-            store_pack(y + (t + j) * a.ldy, pack<T, V>(out));
+        }
+        activate(out, a.act);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (t + j >= live) break;
+            float o[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) o[i] = out[j * V + i];
+            store_pack(y + (t + j) * a.ldy, pack<T, V>(o));
         }
     }
     for (int t = max(t0, len); t < t1; ++t) store_pack(y + t * a.ldy, zero_pack<T, V>());
@@ -142,9 +149,9 @@ __global__ void __launch_bounds__(kBwdThreads) conv1d_bwd_kernel(const BwdArgs<T
         // the first piece also has the K-1 rows of the state
         const int first = piece == 0 && a.dstate_in ? -(K - 1) : t0;
         const int stop = min(t1, len);
-        float xw[K][V] = {}, gw[K][V] = {};   // rows t-(K-1) .. t of xe and of g
+        float xw[K > 1 ? K - 1 : 1][V], gw[K][V] = {};        // rows t-(K-1) .. t-1 of xe, t-(K-1) .. t of g
 #pragma unroll
-        for (int k = 0; k < K - 1; ++k) unpack(row(t0 - (K - 1) + k), xw[k + 1]);
+        for (int k = 0; k < K - 1; ++k) unpack(row(t0 - (K - 1) + k), xw[k]);
         // t walks the rows of g; the row of dx that it completes is t-(K-1)
         for (int t = t0; t < stop + K - 1; t += kAhead) {
             Pack<T, V> xin[kAhead], gin[kAhead];
@@ -153,30 +160,42 @@ __global__ void __launch_bounds__(kBwdThreads) conv1d_bwd_kernel(const BwdArgs<T
                 xin[j] = row(t + j);
                 gin[j] = t + j < len ? load_pack<T, V>(dy + (t + j) * a.lddy) : zero_pack<T, V>();
             }
+            // a of the rows, then g
+            float pre[kAhead * V], g[kAhead * V], xk[kAhead + K - 1][V];
+#pragma unroll
+            for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) xk[k][i] = xw[k][i];
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
-                const int tt = t + j;
-                if (tt >= stop + K - 1) break;
-#pragma unroll
-                for (int k = 0; k < K - 1; ++k)
-#pragma unroll
-                    for (int i = 0; i < V; ++i) xw[k][i] = xw[k + 1][i], gw[k][i] = gw[k + 1][i];
-                unpack(xin[j], xw[K - 1]);
-                float g[V];
-                unpack(gin[j], g);
-                const bool real = tt < len;
+                float gi[V];
+                unpack(xin[j], xk[K - 1 + j]);
+                unpack(gin[j], gi);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     float s = bias[i];
 #pragma unroll
-                    for (int k = 0; k < K; ++k) s = fmaf(w[k][i], xw[k][i], s);
-                    g[i] = real ? g[i] * activate_slope(s, a.act) : 0.f;
-                    gw[K - 1][i] = g[i];
-                    if (tt < stop) {    // each row of g counts once, in its own piece
-                        db[i] += g[i];
+                    for (int k = 0; k < K; ++k) s = fmaf(w[k][i], xk[j + k][i], s);
+                    pre[j * V + i] = s;
+                    g[j * V + i] = gi[i];
+                }
+            }
+            times_slope(g, pre, a.act);
 #pragma unroll
-                        for (int k = 0; k < K; ++k) dw[k][i] = fmaf(g[i], xw[k][i], dw[k][i]);
-                    }
+            for (int j = 0; j < kAhead; ++j) {
+                const int tt = t + j;
+                const bool real = tt < len, own = tt < stop;      // each row of g counts once, in its own piece
+#pragma unroll
+                for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) gw[k][i] = gw[k + 1][i];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float gi = real ? g[j * V + i] : 0.f, go = own ? gi : 0.f;
+                    gw[K - 1][i] = gi;
+                    db[i] += go;
+#pragma unroll
+                    for (int k = 0; k < K; ++k) dw[k][i] = fmaf(go, xk[j + k][i], dw[k][i]);
                 }
                 const int td = tt - (K - 1);
                 if (td < first || td >= stop) continue;
@@ -197,6 +216,10 @@ __global__ void __launch_bounds__(kBwdThreads) conv1d_bwd_kernel(const BwdArgs<T
                 if (td >= 0) store_pack(dx + td * a.lddx, pack<T, V>(out));
                 else store_pack(a.dstate_in + ((size_t)b * (K - 1) + (td + K - 1)) * a.D + c, pack<T, V>(out));
             }
+#pragma unroll
+            for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) xw[k][i] = xk[kAhead + k][i];
         }
         for (int t = max(t0, len); t < t1; ++t) store_pack(dx + t * a.lddx, zero_pack<T, V>());
     }

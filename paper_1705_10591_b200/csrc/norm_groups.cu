@@ -48,6 +48,14 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes)
     for (int m = 1; m < lanes; m *= 2) v += __shfl_xor_sync(0xffffffffu, v, m);
     return v;
 }
+// Several sums over the same lanes, under way together.
+template <int N> __device__ __forceinline__ void lanes_sums(float (&v)[N], int lanes)
+{
+    for (int m = 1; m < lanes; m *= 2) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], m);
+    }
+}
 
 template <int V>
 __device__ __forceinline__ void load_params(const float* p, float dflt, int c, bool real, float (&out)[V])
@@ -83,35 +91,51 @@ __global__ void __launch_bounds__(kThreads) norm_rows_fwd_kernel(const NormArgs<
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
             for (int k = 0; k < NV; ++k) p[r][k] = real[k] && n + r < n1 ? load_pack<T, V>(a.x + (n + r) * a.ldx + c[k]) : zero_pack<T, V>();
+        float x[ROWS][NV * V], mean[ROWS], rstd[ROWS];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            float x[NV][V], sum = 0.f, sq = 0.f;
+            mean[r] = 0.f;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                unpack(p[r][k], x[k]);
+                float v[V];
+                unpack(p[r][k], v);
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum += x[k][i];
+                for (int i = 0; i < V; ++i) x[r][k * V + i] = v[i], mean[r] += v[i];
             }
-            const float mean = lanes_sum(sum, a.lanes) * inv;
+        }
+        lanes_sums(mean, a.lanes);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            mean[r] *= inv;
+            rstd[r] = 0.f;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    x[k][i] -= mean;
-                    if (real[k]) sq = fmaf(x[k][i], x[k][i], sq);
+                    const float d = x[r][k * V + i] -= mean[r];
+                    if (real[k]) rstd[r] = fmaf(d, d, rstd[r]);
                 }
-            const float rstd = rsqrtf(fmaf(lanes_sum(sq, a.lanes), inv, a.eps));
+        }
+        lanes_sums(rstd, a.lanes);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            rstd[r] = rsqrtf(fmaf(rstd[r], inv, a.eps));
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[r][k * V + i] = fmaf(x[r][k * V + i] * rstd[r], gamma[k][i], beta[k][i]);
+            activate(x[r], a.act);
             if (n + r >= n1) continue;
             if (l == 0 && g < a.G) {
-                if (a.mean) a.mean[(n + r) * a.G + g] = mean;
-                if (a.rstd) a.rstd[(n + r) * a.G + g] = rstd;
+                if (a.mean) a.mean[(n + r) * a.G + g] = mean[r];
+                if (a.rstd) a.rstd[(n + r) * a.G + g] = rstd[r];
             }
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 if (!real[k]) continue;
                 float o[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) o[i] = activate(fmaf(x[k][i] * rstd, gamma[k][i], beta[k][i]), a.act);
+                for (int i = 0; i < V; ++i) o[i] = x[r][k * V + i];
                 store_pack(a.y + (n + r) * a.ldy + c[k], pack<T, V>(o));
             }
         }
@@ -152,34 +176,46 @@ __global__ void __launch_bounds__(kThreads) norm_rows_bwd_kernel(const NormArgs<
                 q[r][k] = real[k] && in ? load_pack<T, V>(a.dy + (n + r) * a.lddy + c[k]) : zero_pack<T, V>();
             }
         }
+        float xn[ROWS][NV * V], d[ROWS][NV * V], m[2 * ROWS];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            float xn[NV][V], d[NV][V], m1 = 0.f, m2 = 0.f;
+            float pre[NV * V];
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                unpack(p[r][k], xn[k]);
-                unpack(q[r][k], d[k]);
-                if (!real[k] || n + r >= n1) continue;
+                float v[V], w[V];
+                unpack(p[r][k], v);
+                unpack(q[r][k], w);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    xn[k][i] = (xn[k][i] - mean[r]) * rstd[r];
-                    d[k][i] *= activate_slope(fmaf(xn[k][i], gamma[k][i], beta[k][i]), a.act);
-                    sum1[k][i] += d[k][i];
-                    sum2[k][i] = fmaf(d[k][i], xn[k][i], sum2[k][i]);
-                    d[k][i] *= gamma[k][i];
-                    m1 += d[k][i];
-                    m2 = fmaf(d[k][i], xn[k][i], m2);
+                    xn[r][k * V + i] = real[k] ? (v[i] - mean[r]) * rstd[r] : 0.f;
+                    d[r][k * V + i] = w[i];                  // (zero outside the group and behind the last sample)
+                    pre[k * V + i] = fmaf(xn[r][k * V + i], gamma[k][i], beta[k][i]);
                 }
             }
-            m1 = lanes_sum(m1, a.lanes) * inv;
-            m2 = lanes_sum(m2, a.lanes) * inv;
+            times_slope(d[r], pre, a.act);
+            m[2 * r] = m[2 * r + 1] = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float& e = d[r][k * V + i];
+                    sum1[k][i] += e;
+                    sum2[k][i] = fmaf(e, xn[r][k * V + i], sum2[k][i]);
+                    e *= gamma[k][i];
+                    m[2 * r] += e;
+                    m[2 * r + 1] = fmaf(e, xn[r][k * V + i], m[2 * r + 1]);
+                }
+        }
+        lanes_sums(m, a.lanes);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
             if (n + r >= n1) continue;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 if (!real[k]) continue;
                 float o[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) o[i] = rstd[r] * (d[k][i] - m1 - xn[k][i] * m2);
+                for (int i = 0; i < V; ++i) o[i] = rstd[r] * (d[r][k * V + i] - m[2 * r] * inv - xn[r][k * V + i] * (m[2 * r + 1] * inv));
                 store_pack(a.dx + (n + r) * a.lddx + c[k], pack<T, V>(o));
             }
         }
@@ -358,7 +394,8 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
                 float v[V];
                 unpack(in[j], v);
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = activate(fmaf((v[i] - st.x) * st.y, scale[i], beta[i]), a.act);
+                for (int i = 0; i < V; ++i) v[i] = fmaf((v[i] - st.x) * st.y, scale[i], beta[i]);
+                activate(v, a.act);
                 store_pack(y + (r + j * p.step) * a.ldy + pk * V, pack<T, V>(v));
             }
         }
@@ -408,16 +445,14 @@ __global__ void __launch_bounds__(kThreads) norm_slab_bwd_kernel(const NormArgs<
                             kept[(size_t)(rr - p.r0) * p.packs + pk] = xin[j];
                             kept[(size_t)(rows + rr - p.r0) * p.packs + pk] = gin[j];
                         }
-                        float v[V], d[V];
+                        float v[V], d[V], pre[V];
                         unpack(xin[j], v);
                         unpack(gin[j], d);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) {
-                            const float xn = (v[i] - mean) * rstd;
-                            d[i] *= activate_slope(fmaf(xn, gamma[i], beta[i]), a.act);
-                            s1[i] += d[i];
-                            s2[i] = fmaf(d[i], xn, s2[i]);
-                        }
+                        for (int i = 0; i < V; ++i) v[i] = (v[i] - mean) * rstd, pre[i] = fmaf(v[i], gamma[i], beta[i]);
+                        times_slope(d, pre, a.act);
+#pragma unroll
+                        for (int i = 0; i < V; ++i) s1[i] += d[i], s2[i] = fmaf(d[i], v[i], s2[i]);
                     }
                 }
 #pragma unroll
@@ -496,15 +531,14 @@ __global__ void __launch_bounds__(kThreads) norm_slab_bwd_kernel(const NormArgs<
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 if (r + j * p.step >= p.r1) break;
-                float v[V], d[V];
+                float v[V], d[V], pre[V];
                 unpack(xin[j], v);
                 unpack(gin[j], d);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float xn = (v[i] - mean) * rstd;
-                    d[i] *= activate_slope(fmaf(xn, gamma[i], beta[i]), a.act) * gamma[i];
-                    v[i] = rstd * (d[i] - m.x - xn * m.y);
-                }
+                for (int i = 0; i < V; ++i) v[i] = (v[i] - mean) * rstd, pre[i] = fmaf(v[i], gamma[i], beta[i]);
+                times_slope(d, pre, a.act);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = rstd * (d[i] * gamma[i] - m.x - v[i] * m.y);
                 store_pack(dx + (r + j * p.step) * a.lddx + pk * V, pack<T, V>(v));
             }
         }

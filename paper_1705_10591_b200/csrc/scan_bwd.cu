@@ -46,7 +46,7 @@ struct BwdCut { int nl, cb, sets, blocks_group, segs, rows; };
 BwdCut bwd_cut(int B, int L, int D, int N, int G)
 {
     BwdCut c;
-    c.nl = lanes_for(N);
+    c.nl = bwd_lanes_for(N);
     c.cb = 128 / c.nl;
     const int E = D / G;
     c.sets = env_int("CONV2D_B200_SCAN_SETS", 0);
@@ -118,7 +118,7 @@ conv2d_status_t bwd(const ScanSeq& s, cudaStream_t stream)
 template <typename T, int V>
 conv2d_status_t bwd_lanes(const ScanSeq& s, cudaStream_t stream)
 {
-    switch (lanes_for(s.N)) {
+    switch (bwd_lanes_for(s.N)) {
         case 1: return bwd<T, 1, V>(s, stream);
         case 2: return bwd<T, 2, V>(s, stream);
         case 4: return bwd<T, 4, V>(s, stream);

@@ -15,6 +15,15 @@
 
 namespace conv2d_b200 {
 
+constexpr int kSpt = 4;                 // states of a thread
+
+inline int bwd_lanes_for(int N)
+{
+    int nl = 1;
+    while (nl * kSpt < N) nl *= 2;
+    return nl;
+}
+
 template <typename T>
 struct ScanBwdArgs {
     const T *u, *delta, *Bm, *Cm, *z, *dy;

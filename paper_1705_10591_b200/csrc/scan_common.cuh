@@ -1,17 +1,19 @@
 // What the forward and the backward scan share: how a warp holds states, sums over lanes, step sizes, segments of time.
 //
-// A thread holds four adjacent states of one channel; NL lanes next to each other hold a channel's states (up to 4 NL, the
-// power of two that covers N) and the 32 / NL groups of lanes of a warp adjacent channels.  So a sum over the states is a sum over NL lanes, a
-// sum over channels one over 32 / NL lanes and the warps, and the states never leave the registers.
+// A thread holds SPT adjacent states of one channel (eight or four).  A warp takes CL = 32 / NL adjacent channels: lane l the
+// channel l % CL and the states from SPT * (l / CL) on, so that NL lanes hold a channel's states (SPT * NL, the power of two that covers N), B and C are the same
+// for CL adjacent lanes (one access of 16 bytes costs 2.4 cycles of shared memory then, 4 where neighbours differ), and the states
+// never leave the registers.
 #pragma once
 
 #include "seq_common.cuh"
 
 namespace conv2d_b200 {
 
-constexpr int kSpt = 4;                 // states of a thread
 constexpr int kCheckpointRows = 16;     // the forward pass keeps the state before every 16th row for the backward pass
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
 __device__ __forceinline__ float ex2(float v)
 {
@@ -19,9 +21,29 @@ __device__ __forceinline__ float ex2(float v)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
+// Decays exp(s A) = 2^(s A2) of two states.  The hardware's 2^x is low by 1.2e-8 of itself on average for x in -[0.001, 0.01], 0.6e-8 and 2.2e-8 a factor
+// of ten to either side (measured over 2^20 values of each range), which states that remember a thousand rows would add up; the argument takes
+// that much more.  2^kExpBias is 1: a step of zero leaves the state as it is.
+constexpr float kExpBias = 1.2e-8f * kLog2e;
+__device__ __forceinline__ float2 decay(float2 s, float2 A2)
+{
+    const float2 e = __ffma2_rn(s, A2, both(kExpBias));
+    return make_float2(ex2(e.x), ex2(e.y));
+}
 
-// log(1 + e^v)
-__device__ __forceinline__ float softplus(float v) { return (v > 0.f ? v : 0.f) + log1pf(__expf(-fabsf(v))); }
+// log(1 + e^v) = max(v, 0) + log(1 + w), w = e^-|v| in (0, 1], and log(1 + w) / w as a polynomial (interpolated at Chebyshev nodes; 3e-8, 2e-7
+// with its roundings), so that small steps keep their digits and one special-function operation does.
+__device__ __forceinline__ float2 softplus(float2 v)
+{
+    const float2 w = make_float2(ex2(-kLog2e * fabsf(v.x)), ex2(-kLog2e * fabsf(v.y)));
+    constexpr float c[9] = {1.0f, -0.49999502301216125f, 0.33319270610809326f, -0.24844369292259216f, 0.19111430644989014f,
+                            -0.13674770295619965f, 0.07836166769266129f, -0.02958850748836994f, 0.005253457929939032f};
+    float2 p = both(c[8]);
+#pragma unroll
+    for (int i = 7; i >= 0; --i) p = __ffma2_rn(p, w, both(c[i]));
+    return __ffma2_rn(p, w, make_float2(v.x > 0.f ? v.x : 0.f, v.y > 0.f ? v.y : 0.f));
+}
+__device__ __forceinline__ float softplus(float v) { return softplus(both(v)).x; }
 
 // Sums of NV values over the LANES lanes that differ in the bits LANES/2 * UNIT .. UNIT of the lane index.  While more than one value is left a lane hands half of
 // them over and goes on with the sums of the other half, so that NV - 1 exchanges do for log2(LANES) * NV; at the end v[0 .. left) hold the
@@ -62,13 +84,59 @@ __host__ __device__ constexpr int round4(int n) { return (n + 3) / 4 * 4; }
 // Floats of one block of sums by channel: [D][NQ] for dA, [2][D] for dDskip and ddelta_bias, rounded so that the next begins on 16 bytes.
 __host__ __device__ inline long long channel_floats(int D, int NQ) { return (long long)D * NQ + (2LL * D + 3) / 4 * 4; }
 
-// Lanes that hold a channel's N states.
-inline int lanes_for(int N)
+// Lanes that hold a channel's N states, `spt` each.
+inline int lanes_for(int N, int spt)
 {
     int nl = 1;
-    while (nl * kSpt < N) nl *= 2;
+    while (nl * spt < N) nl *= 2;
     return nl;
 }
+
+// The largest unit, up to 16 bytes, in which rows of `width` elements that begin at p, ld elements apart, can be copied.
+inline int copy_unit(const void* p, long long ld, long long width, int esize)
+{
+    int unit = 16;
+    while (unit > esize && !(rows_aligned(p, ld, esize, unit) && width * esize % unit == 0)) unit /= 2;
+    return unit;
+}
+
+// Copies a tile of ROWS rows of BYTES bytes into shared memory, where they lie one behind the other: rows from `live_rows` on and bytes from
+// `live_bytes` on as zeros.  Units of 4 bytes and more go by asynchronous copies, which the caller commits and waits for.
+template <int ROWS, int BYTES, int UNIT, int THREADS>
+__device__ __forceinline__ void copy_tile_by(unsigned char* dst, const unsigned char* src, long long ld_bytes, int live_rows, int live_bytes, int tid)
+{
+    constexpr int PER_ROW = BYTES / UNIT, COUNT = ROWS * PER_ROW;
+#pragma unroll
+    for (int k = 0; k < (COUNT + THREADS - 1) / THREADS; ++k) {
+        const int i = tid + k * THREADS;
+        if (COUNT % THREADS != 0 && i >= COUNT) break;
+        const int r = i / PER_ROW, c = i % PER_ROW * UNIT;
+        const bool real = r < live_rows && c < live_bytes;
+        const unsigned char* from = real ? src + r * ld_bytes + c : src;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst + i * UNIT);
+        if (UNIT == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(real ? 16 : 0) : "memory");
+        else if (UNIT >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(UNIT < 4 ? 4 : UNIT), "r"(real ? UNIT : 0) : "memory");
+        else *reinterpret_cast<unsigned short*>(dst + i * UNIT) = real ? *reinterpret_cast<const unsigned short*>(from) : (unsigned short)0;
+    }
+}
+template <int ROWS, int BYTES, int THREADS>
+__device__ __forceinline__ void copy_tile(void* dst, const void* src, long long ld_bytes, int live_rows, int live_bytes, int unit, int tid)
+{
+    unsigned char* d = static_cast<unsigned char*>(dst);
+    const unsigned char* s = static_cast<const unsigned char*>(src);
+    if (BYTES >= 16 && unit == 16) copy_tile_by<ROWS, BYTES, BYTES >= 16 ? 16 : 2, THREADS>(d, s, ld_bytes, live_rows, live_bytes, tid);
+    else if (BYTES >= 8 && unit >= 8) copy_tile_by<ROWS, BYTES, BYTES >= 8 ? 8 : 2, THREADS>(d, s, ld_bytes, live_rows, live_bytes, tid);
+    else if (unit >= 4) copy_tile_by<ROWS, BYTES, 4, THREADS>(d, s, ld_bytes, live_rows, live_bytes, tid);
+    else copy_tile_by<ROWS, BYTES, 2, THREADS>(d, s, ld_bytes, live_rows, live_bytes, tid);
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Waits until all but the last PENDING groups of this thread's copies have arrived.
+template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
+// Barrier among the THREADS helping threads of a block (the block's own barrier is number 0).
+template <int THREADS> __device__ __forceinline__ void helpers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
+
+// Four adjacent elements in shared memory.
+template <typename T> __device__ __forceinline__ void load4(const T* p, float (&v)[4]) { unpack(load_pack<T, 4>(p), v); }
 
 // Joins the segments of sequences that were walked from zero: forward, h_in of a segment from the one before it,
 //   H <- exp(A sum s) H + local,

@@ -1,28 +1,49 @@
-// Launchers of the forward scan and of its single-token form.
+// Launchers of the forward scan.
 #include "scan_fwd.cuh"
 
 namespace conv2d_b200 {
 namespace {
 
-// Segments of time.  A segmented walk takes every exponential twice, so sequences stay whole where their blocks fill the machine.
-struct FwdSegments { int segs, rows; };
-FwdSegments fwd_segments(int B, int L, int D, int N, int G)
+// States of a lane: four, so that a channel's states make several lanes' work; eight where four would take more lanes than a warp has.
+int states_of_lane(int N) { return N > 64 ? 8 : 4; }
+
+// Segments of time.  A segmented walk takes every exponential twice, so sequences stay whole unless their blocks leave two thirds of the machine
+// idle; then there are two blocks for every SM, of 64 rows at least.
+struct FwdCut { int segs, rows; };
+FwdCut fwd_cut(int B, int L, int D, int N, int G)
 {
-    const int nl = lanes_for(N), W = nl >= 8 ? 8 : 4, cb = W * 32 / nl, tile = nl <= 2 ? 16 : 32;
+    const int nl = lanes_for(N, states_of_lane(N)), cb = (nl >= 8 ? 8 : 4) * 32 / nl;
     const long long blocks = (long long)B * G * ceil_div_u(D / G, cb);
-    int segs = env_int("CONV2D_B200_SCAN_SEGS", 0);
-    if (segs <= 0) segs = 1;
-    (void)blocks;
-    FwdSegments s;
-    s.rows = (int)(ceil_div_u(ceil_div_u(L, segs), tile) * tile);
-    s.segs = (int)ceil_div_u(L, s.rows);
-    return s;
+    long long segs = blocks * 3 <= 148 ? 2 * 148 / blocks : 1;
+    if (segs > L / 64) segs = L / 64;
+    segs = env_int("CONV2D_B200_SCAN_SEGS", (int)segs);
+    if (segs < 1) segs = 1;
+    FwdCut c;
+    c.rows = (int)(ceil_div_u(ceil_div_u(L, segs), 32) * 32);
+    c.segs = (int)ceil_div_u(L, c.rows);
+    return c;
 }
 
-template <typename T, int NL, int V>
+template <typename T, int NL, int SPT, bool STATE_ONLY>
+conv2d_status_t walk(ScanFwdArgs<T> a, cudaStream_t stream)
+{
+    using Tile = ScanFwdTile<NL, SPT>;
+    constexpr size_t smem = Tile::smem(sizeof(T));
+    a.blocks_group = (int)ceil_div_u(a.E, Tile::CB);
+    const long long blocks = (long long)a.B * a.segs * a.G * a.blocks_group;
+    if (blocks > 0x7fffffffLL) return CONV2D_ERR_SHAPE;
+    static SmemLimit limit;
+    if (raise_smem_limit(reinterpret_cast<const void*>(scan_fwd_kernel<T, NL, SPT, STATE_ONLY>), smem, limit) != cudaSuccess
+        || launch_pdl(scan_fwd_kernel<T, NL, SPT, STATE_ONLY>, dim3((unsigned)blocks), dim3(Tile::TH), smem, stream, a) != cudaSuccess)
+        return CONV2D_ERR_CUDA;
+    count_launch();
+    return CONV2D_OK;
+}
+
+template <typename T, int NL, int SPT>
 conv2d_status_t fwd(const ScanSeq& s, cudaStream_t stream)
 {
-    using Tile = ScanFwdTile<NL>;
+    constexpr int e = sizeof(T);
     ScanFwdArgs<T> a;
     a.u = static_cast<const T*>(s.u), a.delta = static_cast<const T*>(s.delta), a.z = static_cast<const T*>(s.z);
     a.Bm = static_cast<const T*>(s.Bm), a.Cm = static_cast<const T*>(s.Cm);
@@ -30,163 +51,35 @@ conv2d_status_t fwd(const ScanSeq& s, cudaStream_t stream)
     a.y = static_cast<T*>(s.y), a.state_out = s.state_out, a.states = s.states;
     a.B = s.B, a.L = s.L, a.D = s.D, a.N = s.N, a.G = s.G, a.E = s.D / s.G;
     a.ldu = s.ldu, a.lddelta = s.lddelta, a.ldB = s.ldB, a.ldC = s.ldC, a.ldz = s.ldz, a.ldy = s.ldy, a.softplus = s.softplus;
-    const FwdSegments seg = fwd_segments(s.B, s.L, s.D, s.N, s.G);
-    a.segs = seg.segs, a.seg_rows = seg.rows, a.blocks_group = (int)ceil_div_u(a.E, Tile::CB);
+    const FwdCut cut = fwd_cut(s.B, s.L, s.D, s.N, s.G);
+    a.segs = cut.segs, a.seg_rows = cut.rows, a.blocks_group = 0;
+    a.u_unit = copy_unit(s.u, s.ldu, a.E, e), a.delta_unit = copy_unit(s.delta, s.lddelta, a.E, e), a.z_unit = copy_unit(s.z, s.ldz, a.E, e);
+    a.B_unit = copy_unit(s.Bm, s.ldB, a.N, e), a.C_unit = copy_unit(s.Cm, s.ldC, a.N, e);
+    a.y_quads = a.E % 4 == 0 && rows_aligned(s.y, s.ldy, e, 4 * e);
     a.local = s.ws;
     a.steps = s.ws ? s.ws + (size_t)s.B * a.segs * s.D * round4(s.N) : nullptr;
-    const long long blocks = (long long)s.B * a.segs * s.G * a.blocks_group;
-    if (blocks > 0x7fffffffLL) return CONV2D_ERR_SHAPE;
-    static SmemLimit whole, part;
     if (a.segs > 1) {
-        if (raise_smem_limit(reinterpret_cast<const void*>(scan_fwd_kernel<T, NL, V, true>), Tile::smem, part) != cudaSuccess
-            || launch_pdl(scan_fwd_kernel<T, NL, V, true>, dim3((unsigned)blocks), dim3(Tile::W * 32), Tile::smem, stream, a) != cudaSuccess)
-            return CONV2D_ERR_CUDA;
-        count_launch();
+        const conv2d_status_t st = walk<T, NL, SPT, true>(a, stream);
+        if (st != CONV2D_OK) return st;
         if (launch_pdl(scan_join_kernel<false>, dim3(ceil_div_u((long long)s.B * s.D * round4(s.N), 256)), dim3(256), 0, stream, a.local, a.steps, s.A,
                        s.state_in, (float*)nullptr, s.B, a.segs, s.D, s.N) != cudaSuccess) return CONV2D_ERR_CUDA;
         count_launch();
     }
-    if (raise_smem_limit(reinterpret_cast<const void*>(scan_fwd_kernel<T, NL, V, false>), Tile::smem, whole) != cudaSuccess
-        || launch_pdl(scan_fwd_kernel<T, NL, V, false>, dim3((unsigned)blocks), dim3(Tile::W * 32), Tile::smem, stream, a) != cudaSuccess)
-        return CONV2D_ERR_CUDA;
-    count_launch();
-    return CONV2D_OK;
-}
-
-template <typename T, int V>
-conv2d_status_t fwd_lanes(const ScanSeq& s, cudaStream_t stream)
-{
-    switch (lanes_for(s.N)) {
-        case 1: return fwd<T, 1, V>(s, stream);
-        case 2: return fwd<T, 2, V>(s, stream);
-        case 4: return fwd<T, 4, V>(s, stream);
-        case 8: return fwd<T, 8, V>(s, stream);
-        case 16: return fwd<T, 16, V>(s, stream);
-        case 32: return fwd<T, 32, V>(s, stream);
-    }
-    return CONV2D_ERR_UNSUPPORTED;
+    return walk<T, NL, SPT, false>(a, stream);
 }
 
 template <typename T>
 conv2d_status_t fwd_typed(const ScanSeq& s, cudaStream_t stream)
 {
-    constexpr int e = sizeof(T), n = 4 * e;
-    const bool wide = (s.D / s.G) % 4 == 0 && rows_aligned(s.u, s.ldu, e, n) && rows_aligned(s.delta, s.lddelta, e, n)
-                   && rows_aligned(s.z, s.ldz, e, n) && rows_aligned(s.y, s.ldy, e, n);
-    return wide ? fwd_lanes<T, 4>(s, stream) : fwd_lanes<T, 1>(s, stream);
-}
-
-// One token: every state is read and written once, which is all the time there is.  A thread takes four adjacent states of one
-// channel, for ROWS sequences at once (their loads are under way together, and A is loaded once for all).
-template <typename T>
-struct StepArgs {
-    const T *u, *delta, *Bm, *Cm, *z;
-    const float *A, *Dskip, *delta_bias, *state_in;
-    T* y;
-    float* state_out;
-    int B, D, N, G, E, NL;
-    unsigned across;                    // blocks for the channels of ROWS sequences
-    long long ldu, lddelta, ldB, ldC, ldz, ldy;
-    bool softplus;
-};
-
-template <typename T, int ROWS, bool QUADS>
-__global__ void __launch_bounds__(128) scan_step_kernel(const StepArgs<T> a)
-{
-    ptx::grid_dep_wait();
-    const unsigned id = blockIdx.x % a.across * 128 + threadIdx.x;
-    const int n0 = (int)(id % a.NL) * kSpt;
-    const bool mine = id / a.NL < (unsigned)a.D;
-    const int d = mine ? (int)(id / a.NL) : 0, g = d / a.E;
-    const long long b0 = (long long)(blockIdx.x / a.across) * ROWS;
-    float A2[kSpt] = {}, h[ROWS][kSpt] = {}, Bv[ROWS][kSpt] = {}, Cv[ROWS][kSpt] = {}, u[ROWS], s[ROWS], z[ROWS];
-    auto quad = [&](const float* p, float (&v)[kSpt]) {
-        if (!mine) return;
-        if (QUADS) {
-            if (n0 < a.N) {
-                const float4 q = *reinterpret_cast<const float4*>(p + n0);
-                v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kSpt; ++i)
-                if (n0 + i < a.N) v[i] = p[n0 + i];
-        }
-    };
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const long long b = b0 + r;
-        u[r] = s[r] = z[r] = 0.f;
-        if (b >= a.B || !mine) continue;
-        quad(a.state_in + ((size_t)b * a.D + d) * a.N, h[r]);
-        u[r] = to_float(a.u[b * a.ldu + d]);
-        s[r] = to_float(a.delta[b * a.lddelta + d]);
-        if (a.z) z[r] = to_float(a.z[b * a.ldz + d]);
-#pragma unroll
-        for (int i = 0; i < kSpt; ++i) {
-            if (n0 + i >= a.N) continue;
-            Bv[r][i] = to_float(a.Bm[b * a.ldB + g * a.N + n0 + i]);
-            Cv[r][i] = to_float(a.Cm[b * a.ldC + g * a.N + n0 + i]);
-        }
+    if (states_of_lane(s.N) == 8) return fwd<T, 16, 8>(s, stream);
+    switch (lanes_for(s.N, 4)) {
+        case 1: return fwd<T, 1, 4>(s, stream);
+        case 2: return fwd<T, 2, 4>(s, stream);
+        case 4: return fwd<T, 4, 4>(s, stream);
+        case 8: return fwd<T, 8, 4>(s, stream);
+        case 16: return fwd<T, 16, 4>(s, stream);
     }
-    quad(a.A + (size_t)d * a.N, A2);
-#pragma unroll
-    for (int i = 0; i < kSpt; ++i) A2[i] *= kLog2e;
-    const float bias = a.delta_bias && mine ? a.delta_bias[d] : 0.f, skip = a.Dskip && mine ? a.Dskip[d] : 0.f;
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const long long b = b0 + r;
-        s[r] += bias;
-        if (a.softplus) s[r] = softplus(s[r]);
-        float v = 0.f;
-#pragma unroll
-        for (int i = 0; i < kSpt; ++i) {
-            h[r][i] = fmaf(ex2(s[r] * A2[i]), h[r][i], s[r] * u[r] * Bv[r][i]);
-            v = fmaf(Cv[r][i], h[r][i], v);
-        }
-        for (int m = 1; m < a.NL; m *= 2) v += __shfl_xor_sync(0xffffffffu, v, m);
-        if (b >= a.B || !mine) continue;
-        float* out = a.state_out + ((size_t)b * a.D + d) * a.N;
-        if (QUADS) {
-            if (n0 < a.N) *reinterpret_cast<float4*>(out + n0) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kSpt; ++i)
-                if (n0 + i < a.N) out[n0 + i] = h[r][i];
-        }
-        if (n0 == 0) {
-            v = fmaf(skip, u[r], v);
-            if (a.z) v *= z[r] * sigmoid(z[r]);
-            a.y[b * a.ldy + d] = from_float<T>(v);
-        }
-    }
-}
-
-template <typename T, int ROWS, bool QUADS>
-conv2d_status_t step(StepArgs<T> a, cudaStream_t stream)
-{
-    a.across = ceil_div_u((long long)a.D * a.NL, 128);
-    const long long blocks = (long long)a.across * ceil_div_u(a.B, ROWS);
-    if (blocks > 0x7fffffffLL) return CONV2D_ERR_SHAPE;
-    if (launch_pdl(scan_step_kernel<T, ROWS, QUADS>, dim3((unsigned)blocks), dim3(128), 0, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
-    count_launch();
-    return CONV2D_OK;
-}
-
-template <typename T>
-conv2d_status_t step_typed(const ScanSeq& s, cudaStream_t stream)
-{
-    StepArgs<T> a;
-    a.u = static_cast<const T*>(s.u), a.delta = static_cast<const T*>(s.delta), a.z = static_cast<const T*>(s.z);
-    a.Bm = static_cast<const T*>(s.Bm), a.Cm = static_cast<const T*>(s.Cm);
-    a.A = s.A, a.Dskip = s.Dskip, a.delta_bias = s.delta_bias, a.state_in = s.state_in, a.y = static_cast<T*>(s.y), a.state_out = s.state_out;
-    a.B = s.B, a.D = s.D, a.N = s.N, a.G = s.G, a.E = s.D / s.G, a.NL = lanes_for(s.N);
-    a.ldu = s.ldu, a.lddelta = s.lddelta, a.ldB = s.ldB, a.ldC = s.ldC, a.ldz = s.ldz, a.ldy = s.ldy, a.softplus = s.softplus;
-    const bool quads = s.N % 4 == 0 && rows_aligned(s.A, 4, 4, 16) && rows_aligned(s.state_in, 4, 4, 16) && rows_aligned(s.state_out, 4, 4, 16);
-    // four sequences a thread once one each would be more threads than the machine holds
-    const bool many = (long long)s.B * s.D * a.NL > (long long)sm_count() * 2048;
-    if (quads) return many ? step<T, 4, true>(a, stream) : step<T, 1, true>(a, stream);
-    return many ? step<T, 4, false>(a, stream) : step<T, 1, false>(a, stream);
+    return CONV2D_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -197,7 +90,7 @@ size_t scan_states_bytes(int B, int L, int D, int N)
 }
 size_t scan_fwd_workspace_bytes(int B, int L, int D, int N, int G)
 {
-    const FwdSegments s = fwd_segments(B, L, D, N, G);
+    const FwdCut s = fwd_cut(B, L, D, N, G);
     return s.segs > 1 ? sizeof(float) * (size_t)B * s.segs * D * (round4(N) + 1) : 0;
 }
 
@@ -207,11 +100,4 @@ conv2d_status_t launch_scan_fwd(const ScanSeq& s, conv2d_operand_t type, cudaStr
     if (type == CONV2D_OPERAND_FP16) return fwd_typed<fp16>(s, stream);
     return fwd_typed<float>(s, stream);
 }
-conv2d_status_t launch_scan_step(const ScanSeq& s, conv2d_operand_t type, cudaStream_t stream)
-{
-    if (type == CONV2D_OPERAND_BF16) return step_typed<bf16>(s, stream);
-    if (type == CONV2D_OPERAND_FP16) return step_typed<fp16>(s, stream);
-    return step_typed<float>(s, stream);
-}
-
 }  // namespace conv2d_b200

@@ -3,11 +3,13 @@
 //   h_t = exp(s_t A) h_{t-1} + s_t u_t B_t,   v_t = C_t . h_t + Dskip u_t,   y_t = v_t silu(z_t)
 //
 // Every (row, channel, state) takes an exponential of its own, so the special-function units (16 a clock and SM) set the pace, not memory.
-// A block takes CB channels of one sequence and walks its rows in tiles of TT: the tile's u, delta, z, B and C come in by wide loads
-// one tile ahead; s and s u are computed once per row and channel and put into shared memory beside B and C; then every warp
-// walks the tile with its states in registers, and the sums over the states go back through shared memory so that y is stored
-// in rows.  Sequences that would leave the machine idle are cut into segments, whose end states are computed first, from zero
-// (STATE_ONLY), joined, and given to the walk proper.
+// A block takes the channels of its W scanning warps and walks the rows of a sequence in tiles of TT; four more warps do what is done once
+// per row and channel, so that the scanning warps, of which a batch of a few thousand channels gives one or two to a scheduler, only scan: while
+// tile k is scanned, they bring tile k + 3 in (asynchronous copies), put s and s u of tile k + 1 into shared memory beside its B and C in fp32,
+// and gate and store the sums over the states of tile k - 1.  A scanning warp takes eight rows at a time: the exponentials and inputs of all
+// eight first, independent of each other, then the recurrence over them.
+// A batch of few channels has less than one warp for each scheduler.  Then sequences are cut into segments, whose end states are computed
+// first, from zero (STATE_ONLY), joined, and given to the walk proper; every exponential is taken twice then.
 #pragma once
 
 #include "scan_common.cuh"
@@ -24,29 +26,35 @@ struct ScanFwdArgs {
     int B, L, D, N, G, E;                          // E = D / G channels of a group
     int segs, seg_rows, blocks_group;              // seg_rows: a multiple of the tile; blocks_group: blocks of a group's channels
     long long ldu, lddelta, ldB, ldC, ldz, ldy;
-    bool softplus;
+    int u_unit, delta_unit, z_unit, B_unit, C_unit;   // bytes in which rows can be copied
+    bool y_quads, softplus;                           // y_quads: y can be stored four elements at a time
 };
 
-template <int NL>
+template <int NL, int SPT>
 struct ScanFwdTile {
-    static constexpr int W = NL >= 8 ? 8 : 4, CL = 32 / NL, CB = W * CL, NP = NL * kSpt, TT = NL <= 2 ? 16 : 32, YS = CB + CL;
-    static constexpr size_t smem = sizeof(float) * (2 * TT * CB + 2 * TT * NP + TT * YS);
+    static constexpr int CL = 32 / NL, NP = NL * SPT, R = 8, W = NL >= 8 ? 8 : 4, CB = W * CL, TT = CB >= 64 || NP >= 64 ? 16 : 32;
+    static constexpr int SCAN = 32 * W, HELP = 128, TH = SCAN + HELP, RAWS = 4;
+    static constexpr int YS = CB + 4;                 // (the lanes that store a row's sums hit different banks)
+    static constexpr size_t raw(size_t esize) { return esize * TT * (3 * CB + 2 * NP); }              // one tile as it lies in memory
+    static constexpr size_t smem(size_t esize) { return RAWS * raw(esize) + sizeof(float) * 2 * (2 * TT * CB + 2 * TT * NP + TT * YS); }
 };
 
-template <typename T, int NL, int V, bool STATE_ONLY>
-__global__ void __launch_bounds__(ScanFwdTile<NL>::W * 32) scan_fwd_kernel(const ScanFwdArgs<T> a)
+template <typename T, int NL, int SPT, bool STATE_ONLY>
+__global__ void __launch_bounds__(ScanFwdTile<NL, SPT>::TH) scan_fwd_kernel(const ScanFwdArgs<T> a)
 {
-    using Tile = ScanFwdTile<NL>;
-    constexpr int CL = Tile::CL, CB = Tile::CB, NP = Tile::NP, TT = Tile::TT, YS = Tile::YS, TH = Tile::W * 32;
-    constexpr int PPR = CB / V, PK = (TT * PPR + TH - 1) / TH, BK = (TT * NP + TH - 1) / TH;
+    using Tile = ScanFwdTile<NL, SPT>;
+    constexpr int CL = Tile::CL, CB = Tile::CB, NP = Tile::NP, R = Tile::R, TT = Tile::TT, HT = Tile::HELP, YS = Tile::YS, P = SPT / 2, ES = sizeof(T);
+    constexpr int OWN = NL >= R ? 1 : R / NL, SHARE = NL > R ? NL / R : 1;      // rows of a lane after a sum; lanes that have the same row
+    constexpr int UNITS = TT * CB / 4, UK = (UNITS + HT - 1) / HT, BUNITS = TT * NP / 4, BK = (BUNITS + HT - 1) / HT, UROWS = HT / (CB / 4);
+    constexpr int DD = TT * CB, BC = 2 * TT * NP, YB = TT * YS, RAW = TT * (3 * CB + 2 * NP), RAWS = Tile::RAWS;
     ptx::grid_dep_wait();
     extern __shared__ float4 smem4[];
-    float2* dd = reinterpret_cast<float2*>(smem4);            // [TT][CB] (s, s u)
-    float* Bs = reinterpret_cast<float*>(dd + TT * CB);       // [TT][NP]
-    float* Cs = Bs + TT * NP;
-    float* ys = Cs + TT * NP;                                 // [TT][YS]
+    float2* dd = reinterpret_cast<float2*>(smem4);            // [2][TT][CB] (s, s u)
+    float* bc = reinterpret_cast<float*>(dd + 2 * DD);        // [2] of B, C [TT][NP]
+    float* ys = bc + 2 * BC;                                  // [2][TT][YS]
+    T* raw = reinterpret_cast<T*>(ys + 2 * YB);               // [RAWS] of u, delta, z [TT][CB], B, C [TT][NP]
 
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned bx = blockIdx.x;
     const int cb = (int)(bx % a.blocks_group);
     bx /= a.blocks_group;
@@ -57,156 +65,203 @@ __global__ void __launch_bounds__(ScanFwdTile<NL>::W * 32) scan_fwd_kernel(const
     const int len = sequence_length(a.lengths, (int)b, a.L);
     const int c0 = cb * CB;                                   // first channel, counted within the group
     const int nch = min(CB, a.E - c0);
-    const int d0 = g * a.E + c0;
+    const int d0 = g * a.E + c0, NQ = round4(a.N);
     const int t_begin = seg * a.seg_rows, t_end = min(t_begin + a.seg_rows, a.L), live = min(t_end, len);
+    const int tiles = live > t_begin ? (live - t_begin + TT - 1) / TT : 0;
     const long long row0 = b * a.L;
 
-    // the states of this thread
-    const int ch = warp * CL + lane / NL, n0 = (lane % NL) * kSpt;
-    const bool mine = ch < nch;
-    const int d = d0 + ch, NQ = round4(a.N);
-    float2 A2[kSpt / 2], h[kSpt / 2];
-    {
-        float av[kSpt], hv[kSpt];
+    if (warp < Tile::W) {                                     // ---- the scanning warps
+        const int ch = warp * CL + lane % CL, sl = lane / CL, n0 = sl * SPT;
+        const bool mine = ch < nch;
+        const int d = d0 + ch;
+        float2 A2[P], h[P];
+        {
+            float av[SPT], hv[SPT];
 #pragma unroll
-        for (int i = 0; i < kSpt; ++i) {
-            const bool real = mine && n0 + i < a.N;
-            av[i] = real ? a.A[(size_t)d * a.N + n0 + i] * kLog2e : 0.f;
-            hv[i] = 0.f;
-            if (!STATE_ONLY && real) {
-                if (a.segs > 1) hv[i] = a.local[(((size_t)b * a.segs + seg) * a.D + d) * NQ + n0 + i];
-                else if (a.state_in) hv[i] = a.state_in[((size_t)b * a.D + d) * a.N + n0 + i];
+            for (int i = 0; i < SPT; ++i) {
+                const bool real = mine && n0 + i < a.N;
+                av[i] = real ? a.A[(size_t)d * a.N + n0 + i] * kLog2e : 0.f;
+                hv[i] = 0.f;
+                if (!STATE_ONLY && real) {
+                    if (a.segs > 1) hv[i] = a.local[(((size_t)b * a.segs + seg) * a.D + d) * NQ + n0 + i];
+                    else if (a.state_in) hv[i] = a.state_in[((size_t)b * a.D + d) * a.N + n0 + i];
+                }
             }
+#pragma unroll
+            for (int k = 0; k < P; ++k) A2[k] = make_float2(av[2 * k], av[2 * k + 1]), h[k] = make_float2(hv[2 * k], hv[2 * k + 1]);
         }
-        A2[0] = make_float2(av[0], av[1]), A2[1] = make_float2(av[2], av[3]);
-        h[0] = make_float2(hv[0], hv[1]), h[1] = make_float2(hv[2], hv[3]);
-    }
-    float steps = 0.f;
-
-    // loads of a tile: pack `pk` of the rows tid / PPR + i * (TH / PPR), and elements tid + i * TH of B and C
-    const int pk = (tid % PPR) * V, prow = tid / PPR;
-    const bool pk_real = pk < nch;                            // (V divides E: a pack lies inside or outside)
-    float bias[V], skip[V];
+        float steps = 0.f;
+        auto keep = [&](float* p) {                           // the thread's states, at [..][NQ] of its channel
+            if (!mine || n0 >= NQ) return;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        bias[i] = a.delta_bias && pk_real ? a.delta_bias[d0 + pk + i] : 0.f;
-        skip[i] = !STATE_ONLY && a.Dskip && pk_real ? a.Dskip[d0 + pk + i] : 0.f;
-    }
-    Pack<T, V> pu[PK], pd[PK], pz[PK];
-    T pb[BK], pc[BK];
-    auto fetch = [&](int t0) {
+            for (int k = 0; k < SPT / 4; ++k)
+                if (n0 + 4 * k < NQ) *reinterpret_cast<float4*>(p + n0 + 4 * k) = make_float4(h[2 * k].x, h[2 * k].y, h[2 * k + 1].x, h[2 * k + 1].y);
+        };
+        // B or C of the thread's states, in pairs
+        auto pairs = [&](const float* p, float2 (&v)[P]) {
 #pragma unroll
-        for (int i = 0; i < PK; ++i) {
-            const int r = prow + i * (TH / PPR), t = t0 + r;
-            const bool real = pk_real && r < TT && t < live;
-            const long long row = row0 + t;
-            pu[i] = real ? load_pack<T, V>(a.u + row * a.ldu + d0 + pk) : zero_pack<T, V>();
-            pd[i] = real ? load_pack<T, V>(a.delta + row * a.lddelta + d0 + pk) : zero_pack<T, V>();
-            if (!STATE_ONLY) pz[i] = real && a.z ? load_pack<T, V>(a.z + row * a.ldz + d0 + pk) : zero_pack<T, V>();
-        }
-#pragma unroll
-        for (int i = 0; i < BK; ++i) {
-            const int e = tid + i * TH, t = t0 + e / NP, n = e % NP;
-            const bool real = e < TT * NP && n < a.N && t < live;
-            pb[i] = real ? a.Bm[(row0 + t) * a.ldB + g * a.N + n] : from_float<T>(0.f);
-            if (!STATE_ONLY) pc[i] = real ? a.Cm[(row0 + t) * a.ldC + g * a.N + n] : from_float<T>(0.f);
-        }
-    };
-
-    if (t_begin < live) fetch(t_begin);
-    for (int t0 = t_begin; t0 < live; t0 += TT) {
-        Pack<T, V> cu[PK], cz[PK];
-#pragma unroll
-        for (int i = 0; i < PK; ++i) {
-            const int r = prow + i * (TH / PPR);
-            cu[i] = pu[i];
-            if (!STATE_ONLY) cz[i] = pz[i];
-            if (TT * PPR % TH != 0 && r >= TT) continue;
-            float u[V], s[V];
-            unpack(pu[i], u);
-            unpack(pd[i], s);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                s[j] += bias[j];
-                if (a.softplus) s[j] = softplus(s[j]);
-                if (t0 + r >= live) s[j] = 0.f;               // padding: the state stays
-                dd[r * CB + pk + j] = make_float2(s[j], s[j] * u[j]);
+            for (int k = 0; k < SPT / 4; ++k) {
+                const float4 q = *reinterpret_cast<const float4*>(p + 4 * k);
+                v[2 * k] = make_float2(q.x, q.y), v[2 * k + 1] = make_float2(q.z, q.w);
             }
-        }
-#pragma unroll
-        for (int i = 0; i < BK; ++i) {
-            const int e = tid + i * TH;
-            if (TT * NP % TH != 0 && e >= TT * NP) continue;
-            Bs[e] = to_float(pb[i]);
-            if (!STATE_ONLY) Cs[e] = to_float(pc[i]);
-        }
-        __syncthreads();
-        if (t0 + TT < live) fetch(t0 + TT);
+        };
+        __syncthreads();                                      // tile 0 is there
+        for (int k = 0; k < tiles; ++k) {
+            const int t0 = t_begin + k * TT;
+            float* yb = ys + (k & 1) * YB;
 #pragma unroll 1
-        for (int tt = 0; tt < TT; tt += 4) {
-            if (!STATE_ONLY && a.states && tt % kCheckpointRows == 0 && t0 + tt < live && mine && n0 < NQ) {
-                const int cks = (a.L + kCheckpointRows - 1) / kCheckpointRows, ck = (t0 + tt) / kCheckpointRows;
-                *reinterpret_cast<float4*>(a.states + (((size_t)b * cks + ck) * a.D + d) * NQ + n0) = make_float4(h[0].x, h[0].y, h[1].x, h[1].y);
-            }
-            float out[4];
+            for (int r0 = 0; r0 < TT; r0 += R) {
+                if (!STATE_ONLY && a.states && r0 % kCheckpointRows == 0 && t0 + r0 < live) {
+                    const int cks = (a.L + kCheckpointRows - 1) / kCheckpointRows, ck = (t0 + r0) / kCheckpointRows;
+                    keep(a.states + (((size_t)b * cks + ck) * a.D + d) * NQ);
+                }
+                const float2* sp = dd + (k & 1) * DD + r0 * CB + ch;
+                const float *Bp = bc + (k & 1) * BC + r0 * NP + n0, *Cp = Bp + TT * NP;
+                float2 e[R][P], in[R][P];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 s = dd[(tt + j) * CB + ch];
-                const float4 bv = *reinterpret_cast<const float4*>(Bs + (tt + j) * NP + n0);
-                const float2 s2 = make_float2(s.x, s.x), su2 = make_float2(s.y, s.y);
-                float2 e0 = __fmul2_rn(s2, A2[0]), e1 = __fmul2_rn(s2, A2[1]);
-                e0.x = ex2(e0.x), e0.y = ex2(e0.y), e1.x = ex2(e1.x), e1.y = ex2(e1.y);
-                h[0] = __ffma2_rn(e0, h[0], __fmul2_rn(su2, make_float2(bv.x, bv.y)));
-                h[1] = __ffma2_rn(e1, h[1], __fmul2_rn(su2, make_float2(bv.z, bv.w)));
-                if (STATE_ONLY) {
-                    steps += s.x;
-                } else {
-                    const float4 cv = *reinterpret_cast<const float4*>(Cs + (tt + j) * NP + n0);
-                    const float2 o = __ffma2_rn(h[1], make_float2(cv.z, cv.w), __fmul2_rn(h[0], make_float2(cv.x, cv.y)));
+                for (int j = 0; j < R; ++j) {
+                    const float2 s = sp[j * CB];
+                    float2 bv[P];
+                    pairs(Bp + j * NP, bv);
+                    if (STATE_ONLY) steps += s.x;
+#pragma unroll
+                    for (int i = 0; i < P; ++i) e[j][i] = decay(both(s.x), A2[i]), in[j][i] = __fmul2_rn(both(s.y), bv[i]);
+                }
+                float out[R];
+#pragma unroll
+                for (int j = 0; j < R; ++j) {
+                    float2 o = both(0.f), cv[P];
+                    if (!STATE_ONLY) pairs(Cp + j * NP, cv);
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        h[i] = __ffma2_rn(e[j][i], h[i], in[j][i]);
+                        if (!STATE_ONLY) o = i ? __ffma2_rn(h[i], cv[i], o) : __fmul2_rn(h[i], cv[i]);
+                    }
                     out[j] = o.x + o.y;
                 }
-            }
-            if (!STATE_ONLY) {
-                constexpr int left = NL >= 4 ? 1 : 4 / NL;
-                const int first = sum_over_lanes<4, NL, 1>(out, lane);
-                if (first_of_equals<4, NL, 1>(lane)) {
+                if (!STATE_ONLY) {
+                    sum_over_lanes<R, NL, CL>(out, lane);     // leaves rows OWN * (sl / SHARE) ..
+                    if (sl % SHARE == 0) {
 #pragma unroll
-                    for (int j = 0; j < left; ++j) ys[(tt + first + j) * YS + ch] = out[j];
+                        for (int i = 0; i < OWN; ++i) yb[(r0 + sl / SHARE * OWN + i) * YS + ch] = out[i];
+                    }
                 }
             }
+            __syncthreads();
         }
-        __syncthreads();
-        if (!STATE_ONLY) {
-#pragma unroll
-            for (int i = 0; i < PK; ++i) {
-                const int r = prow + i * (TH / PPR);
-                if (!pk_real || r >= TT || t0 + r >= live) continue;
-                float u[V], z[V], o[V];
-                unpack(cu[i], u);
-                unpack(cz[i], z);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    o[j] = fmaf(skip[j], u[j], ys[r * YS + pk + j]);
-                    if (a.z) o[j] *= z[j] * sigmoid(z[j]);
-                }
-                store_pack(a.y + (row0 + t0 + r) * a.ldy + d0 + pk, pack<T, V>(o));
-            }
-        }
-    }
-    if (!STATE_ONLY) {
-        if (pk_real)
-            for (int t = max(t_begin, live) + prow; t < t_end; t += TH / PPR) store_pack(a.y + (row0 + t) * a.ldy + d0 + pk, zero_pack<T, V>());
-        if (a.state_out && seg == a.segs - 1 && mine) {
-            const float hv[kSpt] = {h[0].x, h[0].y, h[1].x, h[1].y};
-#pragma unroll
-            for (int i = 0; i < kSpt; ++i)
-                if (n0 + i < a.N) a.state_out[((size_t)b * a.D + d) * a.N + n0 + i] = hv[i];
-        }
-    } else if (mine && n0 < NQ) {
         const size_t at = ((size_t)b * a.segs + seg) * a.D + d;
-        *reinterpret_cast<float4*>(a.local + at * NQ + n0) = make_float4(h[0].x, h[0].y, h[1].x, h[1].y);
-        if (n0 == 0) a.steps[at] = steps;
+        if (STATE_ONLY) {
+            keep(a.local + at * NQ);
+            if (mine && sl == 0) a.steps[at] = steps;
+        } else if (a.state_out && seg == a.segs - 1 && mine) {
+#pragma unroll
+            for (int i = 0; i < SPT; ++i)
+                if (n0 + i < a.N) a.state_out[((size_t)b * a.D + d) * a.N + n0 + i] = i % 2 ? h[i / 2].y : h[i / 2].x;
+        }
+        return;
     }
+
+    // ---- the helping warps: four adjacent channels of a row at a time, the channels are the thread's own for the whole call
+    const int tid = threadIdx.x - Tile::SCAN, uc = tid % (CB / 4) * 4, ur = tid / (CB / 4);
+    float bias[4], skip[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        bias[i] = a.delta_bias && uc + i < nch ? a.delta_bias[d0 + uc + i] : 0.f;
+        skip[i] = !STATE_ONLY && a.Dskip && uc + i < nch ? a.Dskip[d0 + uc + i] : 0.f;
+    }
+    auto fetch = [&](int k) {
+        if (k < tiles) {
+            T* p = raw + k % RAWS * RAW;
+            const int rows = live - t_begin - k * TT;
+            const long long row = row0 + t_begin + k * TT;
+            copy_tile<TT, CB * ES, HT>(p, a.u + row * a.ldu + d0, a.ldu * ES, rows, nch * ES, a.u_unit, tid);
+            copy_tile<TT, CB * ES, HT>(p + TT * CB, a.delta + row * a.lddelta + d0, a.lddelta * ES, rows, nch * ES, a.delta_unit, tid);
+            if (!STATE_ONLY && a.z) copy_tile<TT, CB * ES, HT>(p + 2 * TT * CB, a.z + row * a.ldz + d0, a.ldz * ES, rows, nch * ES, a.z_unit, tid);
+            copy_tile<TT, NP * ES, HT>(p + 3 * TT * CB, a.Bm + row * a.ldB + (long long)g * a.N, a.ldB * ES, rows, a.N * ES, a.B_unit, tid);
+            if (!STATE_ONLY)
+                copy_tile<TT, NP * ES, HT>(p + 3 * TT * CB + TT * NP, a.Cm + row * a.ldC + (long long)g * a.N, a.ldC * ES, rows, a.N * ES, a.C_unit, tid);
+        }
+        copies_commit();
+    };
+    auto convert = [&](int k) {
+        const T* rw = raw + k % RAWS * RAW;
+        const int rows = live - t_begin - k * TT;
+#pragma unroll
+        for (int i = 0; i < UK; ++i) {
+            const int r = ur + i * UROWS;
+            if (UNITS % HT != 0 && r >= TT) continue;
+            float u[4], s[4];
+            load4(rw + r * CB + uc, u);
+            load4(rw + TT * CB + r * CB + uc, s);
+            float2 s2[2] = {make_float2(s[0] + bias[0], s[1] + bias[1]), make_float2(s[2] + bias[2], s[3] + bias[3])};
+            if (a.softplus) s2[0] = softplus(s2[0]), s2[1] = softplus(s2[1]);
+            if (r >= rows) s2[0] = s2[1] = both(0.f);         // padding: the state stays
+            float4* to = reinterpret_cast<float4*>(dd + (k & 1) * DD + r * CB + uc);
+            to[0] = make_float4(s2[0].x, s2[0].x * u[0], s2[0].y, s2[0].y * u[1]);
+            to[1] = make_float4(s2[1].x, s2[1].x * u[2], s2[1].y, s2[1].y * u[3]);
+        }
+        float* to = bc + (k & 1) * BC;
+#pragma unroll
+        for (int i = 0; i < BK; ++i) {
+            const int e = (tid + i * HT) * 4;
+            if (BUNITS % HT != 0 && e >= TT * NP) continue;
+            float v[4];
+            load4(rw + 3 * TT * CB + e, v);
+            *reinterpret_cast<float4*>(to + e) = make_float4(v[0], v[1], v[2], v[3]);
+            if (!STATE_ONLY) {
+                load4(rw + 3 * TT * CB + TT * NP + e, v);
+                *reinterpret_cast<float4*>(to + TT * NP + e) = make_float4(v[0], v[1], v[2], v[3]);
+            }
+        }
+    };
+    auto finish = [&](int k) {
+        const T* rw = raw + k % RAWS * RAW;
+        const float* yb = ys + (k & 1) * YB;
+        const int rows = live - t_begin - k * TT;
+#pragma unroll
+        for (int i = 0; i < UK; ++i) {
+            const int r = ur + i * UROWS;
+            if (uc >= nch || r >= TT || r >= rows) continue;
+            float u[4], o[4];
+            load4(rw + r * CB + uc, u);
+            const float4 y4 = *reinterpret_cast<const float4*>(yb + r * YS + uc);
+            o[0] = fmaf(skip[0], u[0], y4.x), o[1] = fmaf(skip[1], u[1], y4.y), o[2] = fmaf(skip[2], u[2], y4.z), o[3] = fmaf(skip[3], u[3], y4.w);
+            if (a.z) {
+                float z[4];
+                load4(rw + 2 * TT * CB + r * CB + uc, z);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] *= z[j] * sigmoid(z[j]);
+            }
+            T* to = a.y + (row0 + t_begin + k * TT + r) * a.ldy + d0 + uc;
+            if (a.y_quads) {
+                store_pack(to, pack<T, 4>(o));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (uc + j < nch) to[j] = from_float<T>(o[j]);
+            }
+        }
+    };
+    fetch(0);
+    fetch(1);
+    fetch(2);
+    copies_wait<2>();
+    helpers_sync<HT>();                                       // (every helper's copies have arrived)
+    if (tiles) convert(0);
+    __syncthreads();
+    for (int k = 0; k < tiles; ++k) {
+        // the buffer of tile k + 3 is that of tile k - 1, whose u and z `finish` still reads: it comes first
+        if (!STATE_ONLY && k > 0) finish(k - 1);
+        copies_wait<1>();
+        helpers_sync<HT>();
+        fetch(k + 3);
+        if (k + 1 < tiles) convert(k + 1);
+        __syncthreads();
+    }
+    if (STATE_ONLY) return;
+    if (tiles) finish(tiles - 1);
+    for (int t = max(t_begin, live) + ur; t < t_end; t += UROWS)
+        for (int j = 0; j < 4 && uc + j < nch; ++j) a.y[(row0 + t) * a.ldy + d0 + uc + j] = from_float<T>(0.f);
 }
 
 }  // namespace conv2d_b200

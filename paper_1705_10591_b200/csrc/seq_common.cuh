@@ -50,25 +50,40 @@ template <typename T, int V> __device__ __forceinline__ Pack<T, V> pack(const fl
 // 1 / (1 + e^-v) from the hardware's exponential and reciprocal: a few 2^-23 relative for |v| < 10, |v| 2^-23 beyond.
 __device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
 
-// The activation is the same for a whole launch: a uniform branch beside the memory access that it follows.
-__device__ __forceinline__ float activate(float v, int act)
-{
-    if (act == CONV2D_ACT_SILU) return v * sigmoid(v);
-    if (act == CONV2D_ACT_RELU) return v < 0.f ? 0.f : v;      // (NaN stays NaN)
-    if (act == CONV2D_ACT_GELU) return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
-    return v;
-}
-// Its derivative at v.
-__device__ __forceinline__ float activate_slope(float v, int act)
+// v <- act(v) for N values.  The activation is the same for a whole launch, a uniform branch; it is taken once for many values, since a branch for
+// each would keep their operations apart (group norm of 8 x 4096 x 512 in fp16: 49 us so).
+template <int N>
+__device__ __forceinline__ void activate(float (&v)[N], int act)
 {
     if (act == CONV2D_ACT_SILU) {
-        const float s = sigmoid(v);
-        return s * fmaf(v, 1.f - s, 1.f);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] *= sigmoid(v[i]);
+    } else if (act == CONV2D_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];      // (NaN stays NaN)
+    } else if (act == CONV2D_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * (1.f + erff(v[i] * 0.70710678118654752f));
     }
-    if (act == CONV2D_ACT_RELU) return v > 0.f ? 1.f : (v <= 0.f ? 0.f : v);
-    if (act == CONV2D_ACT_GELU)
-        return fmaf(v * 0.39894228040143268f, __expf(-0.5f * v * v), 0.5f * (1.f + erff(v * 0.70710678118654752f)));
-    return 1.f;
+}
+// g <- g act'(v)
+template <int N>
+__device__ __forceinline__ void times_slope(float (&g)[N], const float (&v)[N], int act)
+{
+    if (act == CONV2D_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float s = sigmoid(v[i]);
+            g[i] *= s * fmaf(v[i], 1.f - s, 1.f);
+        }
+    } else if (act == CONV2D_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = v[i] > 0.f ? g[i] : (v[i] <= 0.f ? 0.f : g[i] * v[i]);
+    } else if (act == CONV2D_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            g[i] *= fmaf(v[i] * 0.39894228040143268f, __expf(-0.5f * v[i] * v[i]), 0.5f * (1.f + erff(v[i] * 0.70710678118654752f)));
+    }
 }
 
 // Rows of sequence b that hold tokens.
