@@ -2,16 +2,78 @@
 //
 //   a[b,t,d] = bias[d] + sum_k w[d,k] xe[b,t-(K-1)+k,d],   y = act(a),   xe = (state_in rows | x rows)
 //
-// 2K flops an element: memory decides.  A thread owns V adjacent channels (16 bytes where the rows allow it) and walks
-// down a piece of the sequence with the last K rows in registers, so that every element is loaded once but for the K-1
-// rows before the piece; the loads of four rows are under way together.
+// 2K flops an element: memory decides, if the loads are far enough ahead and little is done beside them.  A thread owns V adjacent channels (8 or
+// 16 bytes where the rows allow it) and walks down a piece of the sequence with the last K rows in registers, so that every element is loaded once
+// but for the K-1 rows before the piece.  The rows come in by asynchronous copies into a ring of shared memory that belongs to the thread, three
+// groups of four rows ahead; loads into registers were too few at a time (4 x 4096 x 4096 in bf16: 88 us, backward 638).  Products and
+// activations are packed, two channels an instruction.
 #include "seq_common.cuh"
 
 namespace conv2d_b200 {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kAhead = 4;               // rows whose loads are under way together
+constexpr int kGroup = 4, kRing = 4;    // rows of a group, groups of the ring
+
+// A thread's ring of rows of one tensor: its packs of V elements, V * sizeof(T) >= 4 bytes.  Narrower ones are loaded when they are needed.
+template <typename T, int V, int THREADS>
+struct RowRing {
+    static constexpr int bytes = V * (int)sizeof(T);
+    static constexpr bool async = bytes >= 4;
+    static constexpr size_t smem = async ? (size_t)kRing * kGroup * THREADS * bytes : 0;
+    unsigned char* mine;
+    const T* p;                         // row 0 of the sequence, this thread's channels
+    long long ld;
+    __device__ void issue(int q, int t, int live) const
+    {
+        if (!async) return;
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+            const bool real = t + j < live;
+            copy_async<async ? bytes : 4>(mine + (size_t)((q & (kRing - 1)) * kGroup + j) * THREADS * bytes, p + (real ? (t + j) * ld : 0), real);
+        }
+    }
+    __device__ Pack<T, V> get(int q, int t, int j, int live) const
+    {
+        if (async) return *reinterpret_cast<const Pack<T, V>*>(mine + (size_t)((q & (kRing - 1)) * kGroup + j) * THREADS * bytes);
+        return t + j < live ? load_pack<T, V>(p + (t + j) * ld) : zero_pack<T, V>();
+    }
+};
+
+// Pairs of channels (one channel and zero for V = 1).
+template <int V> constexpr int kPairs = (V + 1) / 2;
+template <typename T, int V>
+__device__ __forceinline__ void pairs(const Pack<T, V>& p, float2 (&f)[kPairs<V>])
+{
+#pragma unroll
+    for (int i = 0; i < kPairs<V>; ++i) f[i] = make_float2(to_float(p.e[2 * i]), V > 1 ? to_float(p.e[V > 1 ? 2 * i + 1 : 0]) : 0.f);
+}
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> pack_of(const float2 (&f)[kPairs<V>])
+{
+    Pack<T, V> p;
+#pragma unroll
+    for (int i = 0; i < V; ++i) p.e[i] = from_float<T>(i % 2 ? f[i / 2].y : f[i / 2].x);
+    return p;
+}
+// w[k][pair], bias[pair] of the channels from c on
+template <typename T, int V, int K>
+__device__ __forceinline__ void load_taps(const T* w, const T* bias, int c, float2 (&wt)[K][kPairs<V>], float2 (&bt)[kPairs<V>])
+{
+    float f[K + 1][V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        f[K][i] = bias ? to_float(bias[c + i]) : 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) f[k][i] = to_float(w[(size_t)(c + i) * K + k]);
+    }
+#pragma unroll
+    for (int i = 0; i < kPairs<V>; ++i) {
+        bt[i] = make_float2(f[K][2 * i], V > 1 ? f[K][V > 1 ? 2 * i + 1 : 0] : 0.f);
+#pragma unroll
+        for (int k = 0; k < K; ++k) wt[k][i] = make_float2(f[k][2 * i], V > 1 ? f[k][V > 1 ? 2 * i + 1 : 0] : 0.f);
+    }
+}
 
 template <typename T>
 struct FwdArgs {
@@ -26,7 +88,9 @@ struct FwdArgs {
 template <typename T, int V, int K>
 __global__ void __launch_bounds__(kThreads) conv1d_fwd_kernel(const FwdArgs<T> a)
 {
+    constexpr int P = kPairs<V>;
     ptx::grid_dep_wait();
+    extern __shared__ float4 smem4[];
     const unsigned id = blockIdx.x * kThreads + threadIdx.x;      // (the launcher keeps the number of threads below 2^31)
     const int c = (int)(id % a.packs) * V;
     const unsigned rest = id / a.packs;
@@ -34,27 +98,27 @@ __global__ void __launch_bounds__(kThreads) conv1d_fwd_kernel(const FwdArgs<T> a
     const long long b = rest / a.pieces;
     if (b >= a.B) return;
     const int len = sequence_length(a.lengths, (int)b, a.L);
-    const T* x = a.x + b * a.L * a.ldx + c;
     T* y = a.y + b * a.L * a.ldy + c;
     const int t0 = piece * a.rows, t1 = min(t0 + a.rows, a.L), live = min(t1, len);
-
-    float w[K][V], bias[V];
+    using Ring = RowRing<T, V, kThreads>;
+    const Ring x{reinterpret_cast<unsigned char*>(smem4) + threadIdx.x * Ring::bytes, a.x + b * a.L * a.ldx + c, a.ldx};
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        bias[i] = a.bias ? to_float(a.bias[c + i]) : 0.f;
-#pragma unroll
-        for (int k = 0; k < K; ++k) w[k][i] = to_float(a.w[(size_t)(c + i) * K + k]);
+    for (int q = 0; q < kRing - 1; ++q) {
+        x.issue(q, t0 + q * kGroup, live);
+        copies_commit();
     }
+
+    float2 w[K][P], bias[P];
+    load_taps<T, V, K>(a.w, a.bias, c, w, bias);
     // the row t of the extended sequence, as stored (t < len)
     auto row = [&](int t) -> Pack<T, V> {
-        if (t >= 0) return load_pack<T, V>(x + t * a.ldx);
+        if (t >= 0) return load_pack<T, V>(x.p + t * a.ldx);
         return a.state_in ? load_pack<T, V>(a.state_in + ((size_t)b * (K - 1) + (t + K - 1)) * a.D + c) : zero_pack<T, V>();
     };
-
-    float win[K][V];                    // win[k]: row t-(K-1)+k
+    float2 win[kGroup + K - 1][P];      // rows t-(K-1) .. t+3
     if (t0 < live) {
 #pragma unroll
-        for (int k = 0; k < K - 1; ++k) unpack(row(t0 - (K - 1) + k), win[k + 1]);
+        for (int k = 0; k < K - 1; ++k) pairs<T, V>(row(t0 - (K - 1) + k), win[k]);
     }
     if (piece == 0 && a.state_out) {
         // the last K-1 rows of (state_in | x[0 .. len)); all are read before any is written, and no other piece reads state_in
@@ -65,35 +129,37 @@ __global__ void __launch_bounds__(kThreads) conv1d_fwd_kernel(const FwdArgs<T> a
 #pragma unroll
         for (int k = 0; k < K - 1; ++k) store_pack(a.state_out + ((size_t)b * (K - 1) + k) * a.D + c, last[k]);
     }
-    for (int t = t0; t < live; t += kAhead) {
-        Pack<T, V> in[kAhead];
+    int q = 0;
+#pragma unroll 1
+    for (int t = t0; t < live; t += kGroup, ++q) {
+        copies_wait<kRing - 2>();
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) in[j] = t + j < live ? load_pack<T, V>(x + (t + j) * a.ldx) : zero_pack<T, V>();
-        float out[kAhead * V];
+        for (int j = 0; j < kGroup; ++j) pairs<T, V>(x.get(q, t, j, live), win[K - 1 + j]);
+        x.issue(q + kRing - 1, t + (kRing - 1) * kGroup, live);
+        copies_commit();
+        float out[kGroup * 2 * P];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
+        for (int j = 0; j < kGroup; ++j) {
 #pragma unroll
-            for (int k = 0; k < K - 1; ++k)
+            for (int i = 0; i < P; ++i) {
+                float2 s = bias[i];
 #pragma unroll
-                for (int i = 0; i < V; ++i) win[k][i] = win[k + 1][i];
-            unpack(in[j], win[K - 1]);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float s = bias[i];
-#pragma unroll
-                for (int k = 0; k < K; ++k) s = fmaf(w[k][i], win[k][i], s);
-                out[j * V + i] = s;
+                for (int k = 0; k < K; ++k) s = __ffma2_rn(w[k][i], win[j + k][i], s);
+                out[2 * (j * P + i)] = s.x, out[2 * (j * P + i) + 1] = s.y;
             }
         }
         activate(out, a.act);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (t + j >= live) break;
-            float o[V];
+        for (int j = 0; j < kGroup; ++j) {
+            float2 o[P];
 #pragma unroll
-            for (int i = 0; i < V; ++i) o[i] = out[j * V + i];
-            store_pack(y + (t + j) * a.ldy, pack<T, V>(o));
+            for (int i = 0; i < P; ++i) o[i] = make_float2(out[2 * (j * P + i)], out[2 * (j * P + i) + 1]);
+            if (t + j < live) store_pack(y + (t + j) * a.ldy, pack_of<T, V>(o));
         }
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+            for (int i = 0; i < P; ++i) win[k][i] = win[kGroup + k][i];
     }
     for (int t = max(t0, len); t < t1; ++t) store_pack(y + t * a.ldy, zero_pack<T, V>());
 }
@@ -114,126 +180,154 @@ struct BwdArgs {
     int act;
 };
 
-constexpr int kBwdThreads = 256;
-constexpr int kBwdRows = 32;            // rows of a piece: K-1 rows of x before and K-1 of both inputs after it are read again
+constexpr int kBwdRows = 64;            // rows of a piece: K-1 rows of x before and K-1 of both inputs after it are read again
 
 template <typename T, int V, int K>
-__global__ void __launch_bounds__(kBwdThreads) conv1d_bwd_kernel(const BwdArgs<T> a)
+__global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a)
 {
+    constexpr int P = kPairs<V>;
     ptx::grid_dep_wait();
-    extern __shared__ float sums[];     // [blockDim.y][K+1][blockDim.x * V]
-    const int pk = blockIdx.y * blockDim.x + threadIdx.x;
-    const int c = pk * V;
-    float dw[K][V] = {}, db[V] = {}, w[K][V], bias[V];
-    if (pk < a.packs) {
+    extern __shared__ float4 smem4[];   // the rings, then the sums [blockDim.y][K+1][blockDim.x * V]
+    using Ring = RowRing<T, V, kThreads>;
+    const int tid = threadIdx.y * blockDim.x + threadIdx.x;
+    const int pk = blockIdx.y * blockDim.x + threadIdx.x, c = pk * V;
+    float2 dw[K][P], db[P], w[K][P], bias[P];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            bias[i] = a.bias ? to_float(a.bias[c + i]) : 0.f;
+    for (int i = 0; i < P; ++i) {
+        db[i] = both(0.f);
 #pragma unroll
-            for (int k = 0; k < K; ++k) w[k][i] = to_float(a.w[(size_t)(c + i) * K + k]);
-        }
+        for (int k = 0; k < K; ++k) dw[k][i] = both(0.f);
     }
+    if (pk < a.packs) load_taps<T, V, K>(a.w, a.bias, c, w, bias);
     for (unsigned job = blockIdx.x * blockDim.y + threadIdx.y; job < a.jobs && pk < a.packs; job += gridDim.x * blockDim.y) {
         const int piece = (int)(job % a.pieces);
         const long long b = job / a.pieces;
         const int len = sequence_length(a.lengths, (int)b, a.L);
-        const T* x = a.x + b * a.L * a.ldx + c;
-        const T* dy = a.dy + b * a.L * a.lddy + c;
-        T* dx = a.dx + b * a.L * a.lddx + c;
         const int t0 = piece * kBwdRows, t1 = min(t0 + kBwdRows, a.L);
-        auto row = [&](int t) -> Pack<T, V> {
-            if (t >= len) return zero_pack<T, V>();
-            if (t >= 0) return load_pack<T, V>(x + t * a.ldx);
-            return a.state_in ? load_pack<T, V>(a.state_in + ((size_t)b * (K - 1) + (t + K - 1)) * a.D + c) : zero_pack<T, V>();
-        };
+        const Ring x{reinterpret_cast<unsigned char*>(smem4) + tid * Ring::bytes, a.x + b * a.L * a.ldx + c, a.ldx};
+        const Ring dy{reinterpret_cast<unsigned char*>(smem4) + Ring::smem + tid * Ring::bytes, a.dy + b * a.L * a.lddy + c, a.lddy};
+        T* dx = a.dx + b * a.L * a.lddx + c;
         // the first piece also has the K-1 rows of the state
         const int first = piece == 0 && a.dstate_in ? -(K - 1) : t0;
-        const int stop = min(t1, len);
-        float xw[K > 1 ? K - 1 : 1][V], gw[K][V] = {};        // rows t-(K-1) .. t-1 of xe, t-(K-1) .. t of g
+        const int stop = min(t1, len), end = stop + K - 1;    // t walks the rows of g; the row of dx that it completes is t-(K-1)
 #pragma unroll
-        for (int k = 0; k < K - 1; ++k) unpack(row(t0 - (K - 1) + k), xw[k]);
-        // t walks the rows of g; the row of dx that it completes is t-(K-1)
-        for (int t = t0; t < stop + K - 1; t += kAhead) {
-            Pack<T, V> xin[kAhead], gin[kAhead];
+        for (int q = 0; q < kRing - 1; ++q) {
+            x.issue(q, t0 + q * kGroup, len);
+            dy.issue(q, t0 + q * kGroup, len);
+            copies_commit();
+        }
+        float2 xw[kGroup + K - 1][P], gw[kGroup + K - 1][P];  // rows t-(K-1) .. t+3 of xe and of g
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                xin[j] = row(t + j);
-                gin[j] = t + j < len ? load_pack<T, V>(dy + (t + j) * a.lddy) : zero_pack<T, V>();
+        for (int k = 0; k < K - 1; ++k) {
+            const int t = t0 - (K - 1) + k;
+            Pack<T, V> p = zero_pack<T, V>();
+            if (t >= 0 && t < len) p = load_pack<T, V>(x.p + t * a.ldx);
+            if (t < 0 && a.state_in) p = load_pack<T, V>(a.state_in + ((size_t)b * (K - 1) + (t + K - 1)) * a.D + c);
+            pairs<T, V>(p, xw[k]);
+#pragma unroll
+            for (int i = 0; i < P; ++i) gw[k][i] = both(0.f);
+        }
+        int q = 0;
+#pragma unroll 1
+        for (int t = t0; t < end; t += kGroup, ++q) {
+            copies_wait<kRing - 2>();
+            float g[kGroup * 2 * P], pre[kGroup * 2 * P];
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) {
+                float2 gi[P];
+                pairs<T, V>(x.get(q, t, j, len), xw[K - 1 + j]);
+                pairs<T, V>(dy.get(q, t, j, len), gi);        // (zero behind the sequence)
+#pragma unroll
+                for (int i = 0; i < P; ++i) g[2 * (j * P + i)] = gi[i].x, g[2 * (j * P + i) + 1] = gi[i].y;
             }
-            // a of the rows, then g
-            float pre[kAhead * V], g[kAhead * V], xk[kAhead + K - 1][V];
+            x.issue(q + kRing - 1, t + (kRing - 1) * kGroup, len);
+            dy.issue(q + kRing - 1, t + (kRing - 1) * kGroup, len);
+            copies_commit();
 #pragma unroll
-            for (int k = 0; k < K - 1; ++k)
+            for (int j = 0; j < kGroup; ++j) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) xk[k][i] = xw[k][i];
+                for (int i = 0; i < P; ++i) {
+                    float2 s = bias[i];
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                float gi[V];
-                unpack(xin[j], xk[K - 1 + j]);
-                unpack(gin[j], gi);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float s = bias[i];
-#pragma unroll
-                    for (int k = 0; k < K; ++k) s = fmaf(w[k][i], xk[j + k][i], s);
-                    pre[j * V + i] = s;
-                    g[j * V + i] = gi[i];
+                    for (int k = 0; k < K; ++k) s = __ffma2_rn(w[k][i], xw[j + k][i], s);
+                    pre[2 * (j * P + i)] = s.x, pre[2 * (j * P + i) + 1] = s.y;
                 }
             }
             times_slope(g, pre, a.act);
+            if (t + kGroup > len) {     // behind the sequence an overflowing slope must not make zeros NaN
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const int tt = t + j;
-                const bool real = tt < len, own = tt < stop;      // each row of g counts once, in its own piece
+                for (int j = 0; j < kGroup; ++j)
 #pragma unroll
-                for (int k = 0; k < K - 1; ++k)
+                    for (int i = 0; i < 2 * P; ++i)
+                        if (t + j >= len) g[2 * j * P + i] = 0.f;
+            }
 #pragma unroll
-                    for (int i = 0; i < V; ++i) gw[k][i] = gw[k + 1][i];
+            for (int j = 0; j < kGroup; ++j)
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float gi = real ? g[j * V + i] : 0.f, go = own ? gi : 0.f;
-                    gw[K - 1][i] = gi;
-                    db[i] += go;
+                for (int i = 0; i < P; ++i) gw[K - 1 + j][i] = make_float2(g[2 * (j * P + i)], g[2 * (j * P + i) + 1]);
+            // each row of g counts once, in its own piece
+            if (t + kGroup <= stop) {
 #pragma unroll
-                    for (int k = 0; k < K; ++k) dw[k][i] = fmaf(go, xk[j + k][i], dw[k][i]);
+                for (int j = 0; j < kGroup; ++j)
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        db[i] = __fadd2_rn(db[i], gw[K - 1 + j][i]);
+#pragma unroll
+                        for (int k = 0; k < K; ++k) dw[k][i] = __ffma2_rn(gw[K - 1 + j][i], xw[j + k][i], dw[k][i]);
+                    }
+            } else {
+#pragma unroll
+                for (int j = 0; j < kGroup; ++j) {
+                    if (t + j >= stop) break;
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        db[i] = __fadd2_rn(db[i], gw[K - 1 + j][i]);
+#pragma unroll
+                        for (int k = 0; k < K; ++k) dw[k][i] = __ffma2_rn(gw[K - 1 + j][i], xw[j + k][i], dw[k][i]);
+                    }
                 }
-                const int td = tt - (K - 1);
+            }
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) {
+                const int td = t + j - (K - 1);
                 if (td < first || td >= stop) continue;
-                float out[V];
+                float2 out[P];
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float s = 0.f;
+                for (int i = 0; i < P; ++i) {
+                    out[i] = __fmul2_rn(w[0][i], gw[j + K - 1][i]);
 #pragma unroll
-                    for (int k = 0; k < K; ++k) s = fmaf(w[k][i], gw[K - 1 - k][i], s);
-                    out[i] = s;
+                    for (int k = 1; k < K; ++k) out[i] = __ffma2_rn(w[k][i], gw[j + K - 1 - k][i], out[i]);
                 }
                 if (a.dstate_out && td >= len - (K - 1)) {
-                    float e[V];
-                    unpack(load_pack<T, V>(a.dstate_out + ((size_t)b * (K - 1) + (td - len + K - 1)) * a.D + c), e);
+                    float2 e[P];
+                    pairs<T, V>(load_pack<T, V>(a.dstate_out + ((size_t)b * (K - 1) + (td - len + K - 1)) * a.D + c), e);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) out[i] += e[i];
+                    for (int i = 0; i < P; ++i) out[i] = __fadd2_rn(out[i], e[i]);
                 }
-                if (td >= 0) store_pack(dx + td * a.lddx, pack<T, V>(out));
-                else store_pack(a.dstate_in + ((size_t)b * (K - 1) + (td + K - 1)) * a.D + c, pack<T, V>(out));
+                if (td >= 0) store_pack(dx + td * a.lddx, pack_of<T, V>(out));
+                else store_pack(a.dstate_in + ((size_t)b * (K - 1) + (td + K - 1)) * a.D + c, pack_of<T, V>(out));
             }
 #pragma unroll
             for (int k = 0; k < K - 1; ++k)
 #pragma unroll
-                for (int i = 0; i < V; ++i) xw[k][i] = xk[kAhead + k][i];
+                for (int i = 0; i < P; ++i) xw[k][i] = xw[kGroup + k][i], gw[k][i] = gw[kGroup + k][i];
         }
+        copies_wait<0>();               // (the ring is free for the next piece)
         for (int t = max(t0, len); t < t1; ++t) store_pack(dx + t * a.lddx, zero_pack<T, V>());
     }
     if (!a.partials) return;
     const int width = blockDim.x * V;
+    float* sums = reinterpret_cast<float*>(smem4);            // (over the rings)
+    __syncthreads();
     float* own = sums + (size_t)threadIdx.y * (K + 1) * width + threadIdx.x * V;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) own[k * width + i] = dw[k][i];
-        own[K * width + i] = db[i];
+        for (int k = 0; k < K; ++k) own[k * width + i] = i % 2 ? dw[k][i / 2].y : dw[k][i / 2].x;
+        own[K * width + i] = i % 2 ? db[i / 2].y : db[i / 2].x;
     }
     __syncthreads();
-    for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < (K + 1) * width; i += kBwdThreads) {
+    for (int i = tid; i < (K + 1) * width; i += kThreads) {
         const int k = i / width, ch = blockIdx.y * width + i % width;
         if (ch >= a.D) continue;
         float s = 0.f;
@@ -258,7 +352,7 @@ struct TapStore {
 };
 
 // Blocks of the backward pass: tx channel packs by ty pieces at a time; as many shares of the pieces (each a partial sum of the taps'
-// gradients) as fill the machine twice.
+// gradients) as fill the machine four times.
 struct BwdPlan { int pieces, tx, ty; long long jobs, parts, across; };
 BwdPlan bwd_plan(int B, int L, int D, int V)
 {
@@ -266,7 +360,7 @@ BwdPlan bwd_plan(int B, int L, int D, int V)
     const int packs = D / V;
     p.tx = 1;
     while (p.tx < 32 && p.tx < packs) p.tx *= 2;
-    p.ty = kBwdThreads / p.tx;
+    p.ty = kThreads / p.tx;
     p.across = ceil_div_u(packs, p.tx);
     p.pieces = (int)ceil_div_u(L, kBwdRows);
     p.jobs = (long long)B * p.pieces;
@@ -284,13 +378,13 @@ conv2d_status_t fwd(const ConvSeq& s, cudaStream_t stream)
     a.y = static_cast<T*>(s.y), a.state_out = static_cast<T*>(s.state_out);
     a.B = s.B, a.L = s.L, a.D = s.D, a.ldx = s.ldx, a.ldy = s.ldy, a.act = s.act;
     a.packs = s.D / V;
-    // Short pieces until the machine is full: 8 rows are the fewest (not below K-1), 32 the most
-    a.rows = 32;
+    // Short pieces until the machine is full: 8 rows are the fewest (not below K-1), 64 the most
+    a.rows = 64;
     while (a.rows > 8 && (long long)a.packs * s.B * ceil_div_u(s.L, a.rows) < (long long)sm_count() * 1024) a.rows /= 2;
     a.pieces = (int)ceil_div_u(s.L, a.rows);
     const long long threads = (long long)a.packs * a.pieces * s.B;
     if (threads > 0x7fffff00LL) return CONV2D_ERR_SHAPE;
-    if (launch_pdl(conv1d_fwd_kernel<T, V, K>, dim3(ceil_div_u(threads, kThreads)), dim3(kThreads), 0, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
+    if (launch_pdl(conv1d_fwd_kernel<T, V, K>, dim3(ceil_div_u(threads, kThreads)), dim3(kThreads), RowRing<T, V, kThreads>::smem, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;
 }
@@ -307,7 +401,7 @@ conv2d_status_t bwd(const ConvSeq& s, cudaStream_t stream)
     a.pieces = p.pieces, a.packs = s.D / V, a.jobs = (unsigned)p.jobs;
     a.partials = s.dw || s.dbias ? s.partials : nullptr;
     if (p.across > 65535 || p.jobs > 0x7fff0000LL) return CONV2D_ERR_SHAPE;
-    const size_t smem = (size_t)kBwdThreads * V * (K + 1) * sizeof(float);
+    const size_t rings = 2 * RowRing<T, V, kThreads>::smem, sums = (size_t)kThreads * V * (K + 1) * sizeof(float), smem = rings > sums ? rings : sums;
     static SmemLimit limit;
     if (raise_smem_limit(reinterpret_cast<const void*>(conv1d_bwd_kernel<T, V, K>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
     if (launch_pdl(conv1d_bwd_kernel<T, V, K>, dim3((unsigned)p.parts, (unsigned)p.across), dim3(p.tx, p.ty), smem, stream, a) != cudaSuccess)
@@ -361,8 +455,7 @@ bool wide(const ConvSeq& s)
 template <typename T>
 conv2d_status_t fwd_typed(const ConvSeq& s, cudaStream_t stream)
 {
-    constexpr int V = 16 / sizeof(T);
-    return wide<T, V>(s) ? fwd_taps<T, V>(s, stream) : fwd_taps<T, 1>(s, stream);
+    return wide<T, 4>(s) ? fwd_taps<T, 4>(s, stream) : fwd_taps<T, 1>(s, stream);
 }
 template <typename T>
 conv2d_status_t bwd_typed(const ConvSeq& s, cudaStream_t stream)

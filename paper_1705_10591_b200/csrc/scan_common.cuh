@@ -11,16 +11,7 @@
 namespace conv2d_b200 {
 
 constexpr int kCheckpointRows = 16;     // the forward pass keeps the state before every 16th row for the backward pass
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
-
-__device__ __forceinline__ float ex2(float v)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 // Decays exp(s A) = 2^(s A2) of two states.  The hardware's 2^x is low by 1.2e-8 of itself on average for x in -[0.001, 0.01], 0.6e-8 and 2.2e-8 a factor
 // of ten to either side (measured over 2^20 values of each range), which states that remember a thousand rows would add up; the argument takes
 // that much more.  2^kExpBias is 1: a step of zero leaves the state as it is.
@@ -113,9 +104,7 @@ __device__ __forceinline__ void copy_tile_by(unsigned char* dst, const unsigned 
         const int r = i / PER_ROW, c = i % PER_ROW * UNIT;
         const bool real = r < live_rows && c < live_bytes;
         const unsigned char* from = real ? src + r * ld_bytes + c : src;
-        const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst + i * UNIT);
-        if (UNIT == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(real ? 16 : 0) : "memory");
-        else if (UNIT >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(UNIT < 4 ? 4 : UNIT), "r"(real ? UNIT : 0) : "memory");
+        if (UNIT >= 4) copy_async<UNIT < 4 ? 4 : UNIT>(dst + i * UNIT, from, real);
         else *reinterpret_cast<unsigned short*>(dst + i * UNIT) = real ? *reinterpret_cast<const unsigned short*>(from) : (unsigned short)0;
     }
 }
@@ -129,9 +118,6 @@ __device__ __forceinline__ void copy_tile(void* dst, const void* src, long long 
     else if (unit >= 4) copy_tile_by<ROWS, BYTES, 4, THREADS>(d, s, ld_bytes, live_rows, live_bytes, tid);
     else copy_tile_by<ROWS, BYTES, 2, THREADS>(d, s, ld_bytes, live_rows, live_bytes, tid);
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// Waits until all but the last PENDING groups of this thread's copies have arrived.
-template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 // Barrier among the THREADS helping threads of a block (the block's own barrier is number 0).
 template <int THREADS> __device__ __forceinline__ void helpers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
 

@@ -47,8 +47,30 @@ template <typename T, int V> __device__ __forceinline__ Pack<T, V> pack(const fl
     return p;
 }
 
-// 1 / (1 + e^-v) from the hardware's exponential and reciprocal: a few 2^-23 relative for |v| < 10, |v| 2^-23 beyond.
-__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float ex2(float v)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float rcp(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+
+// 1 / (1 + e^-v) from the hardware's exponential and reciprocal: a few 2^-23 relative for |v| < 10, |v| 2^-23 beyond.  Two at a time, as everything
+// here: the packed operations of the FMA pipe take one issue slot for two.
+__device__ __forceinline__ float2 sigmoid(float2 v)
+{
+    const float2 t = __fmul2_rn(v, both(-kLog2e));
+    const float2 d = __fadd2_rn(make_float2(ex2(t.x), ex2(t.y)), both(1.f));
+    return make_float2(rcp(d.x), rcp(d.y));
+}
+__device__ __forceinline__ float sigmoid(float v) { return rcp(1.f + ex2(-kLog2e * v)); }
 
 // v <- act(v) for N values.  The activation is the same for a whole launch, a uniform branch; it is taken once for many values, since a branch for
 // each would keep their operations apart (group norm of 8 x 4096 x 512 in fp16: 49 us so).
@@ -57,7 +79,11 @@ __device__ __forceinline__ void activate(float (&v)[N], int act)
 {
     if (act == CONV2D_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] *= sigmoid(v[i]);
+        for (int i = 0; i + 1 < N; i += 2) {
+            const float2 x = make_float2(v[i], v[i + 1]), y = __fmul2_rn(x, sigmoid(x));
+            v[i] = y.x, v[i + 1] = y.y;
+        }
+        if (N % 2) v[N - 1] *= sigmoid(v[N - 1]);
     } else if (act == CONV2D_ACT_RELU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];      // (NaN stays NaN)
@@ -72,9 +98,15 @@ __device__ __forceinline__ void times_slope(float (&g)[N], const float (&v)[N], 
 {
     if (act == CONV2D_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float s = sigmoid(v[i]);
-            g[i] *= s * fmaf(v[i], 1.f - s, 1.f);
+        for (int i = 0; i + 1 < N; i += 2) {
+            // s (1 + v (1 - s)) = s + v s (1 - s)
+            const float2 x = make_float2(v[i], v[i + 1]), s = sigmoid(x), r = __ffma2_rn(s, both(-1.f), both(1.f));
+            const float2 y = __fmul2_rn(make_float2(g[i], g[i + 1]), __fmul2_rn(s, __ffma2_rn(x, r, both(1.f))));
+            g[i] = y.x, g[i + 1] = y.y;
+        }
+        if (N % 2) {
+            const float s = sigmoid(v[N - 1]);
+            g[N - 1] *= s * fmaf(v[N - 1], 1.f - s, 1.f);
         }
     } else if (act == CONV2D_ACT_RELU) {
 #pragma unroll
@@ -85,6 +117,18 @@ __device__ __forceinline__ void times_slope(float (&g)[N], const float (&v)[N], 
             g[i] *= fmaf(v[i] * 0.39894228040143268f, __expf(-0.5f * v[i] * v[i]), 0.5f * (1.f + erff(v[i] * 0.70710678118654752f)));
     }
 }
+
+// Asynchronous copy of BYTES (4, 8 or 16) into shared memory; zeros where `real` is false (the address is not read then).
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* to, const void* from, bool real)
+{
+    const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(real ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(from), "n"(BYTES), "r"(real ? BYTES : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Waits until all but the last PENDING groups of this thread's copies have arrived.
+template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 
 // Rows of sequence b that hold tokens.
 __device__ __forceinline__ int sequence_length(const int* lengths, int b, int L)
