@@ -14,48 +14,6 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kGroup = 4, kRing = 4;    // rows of a group, groups of the ring
-
-// A thread's ring of rows of one tensor: its packs of V elements, V * sizeof(T) >= 4 bytes.  Narrower ones are loaded when they are needed.
-template <typename T, int V, int THREADS>
-struct RowRing {
-    static constexpr int bytes = V * (int)sizeof(T);
-    static constexpr bool async = bytes >= 4;
-    static constexpr size_t smem = async ? (size_t)kRing * kGroup * THREADS * bytes : 0;
-    unsigned char* mine;
-    const T* p;                         // row 0 of the sequence, this thread's channels
-    long long ld;
-    __device__ void issue(int q, int t, int live) const
-    {
-        if (!async) return;
-#pragma unroll
-        for (int j = 0; j < kGroup; ++j) {
-            const bool real = t + j < live;
-            copy_async<async ? bytes : 4>(mine + (size_t)((q & (kRing - 1)) * kGroup + j) * THREADS * bytes, p + (real ? (t + j) * ld : 0), real);
-        }
-    }
-    __device__ Pack<T, V> get(int q, int t, int j, int live) const
-    {
-        if (async) return *reinterpret_cast<const Pack<T, V>*>(mine + (size_t)((q & (kRing - 1)) * kGroup + j) * THREADS * bytes);
-        return t + j < live ? load_pack<T, V>(p + (t + j) * ld) : zero_pack<T, V>();
-    }
-};
-
-// Pairs of channels (one channel and zero for V = 1).
-template <int V> constexpr int kPairs = (V + 1) / 2;
-template <typename T, int V>
-__device__ __forceinline__ void pairs(const Pack<T, V>& p, float2 (&f)[kPairs<V>])
-{
-#pragma unroll
-    for (int i = 0; i < kPairs<V>; ++i) f[i] = make_float2(to_float(p.e[2 * i]), V > 1 ? to_float(p.e[V > 1 ? 2 * i + 1 : 0]) : 0.f);
-}
-template <typename T, int V>
-__device__ __forceinline__ Pack<T, V> pack_of(const float2 (&f)[kPairs<V>])
-{
-    Pack<T, V> p;
-#pragma unroll
-    for (int i = 0; i < V; ++i) p.e[i] = from_float<T>(i % 2 ? f[i / 2].y : f[i / 2].x);
-    return p;
-}
 // w[k][pair], bias[pair] of the channels from c on
 template <typename T, int V, int K>
 __device__ __forceinline__ void load_taps(const T* w, const T* bias, int c, float2 (&wt)[K][kPairs<V>], float2 (&bt)[kPairs<V>])
@@ -100,7 +58,7 @@ __global__ void __launch_bounds__(kThreads) conv1d_fwd_kernel(const FwdArgs<T> a
     const int len = sequence_length(a.lengths, (int)b, a.L);
     T* y = a.y + b * a.L * a.ldy + c;
     const int t0 = piece * a.rows, t1 = min(t0 + a.rows, a.L), live = min(t1, len);
-    using Ring = RowRing<T, V, kThreads>;
+    using Ring = RowRing<T, V, kThreads, kGroup, kRing>;
     const Ring x{reinterpret_cast<unsigned char*>(smem4) + threadIdx.x * Ring::bytes, a.x + b * a.L * a.ldx + c, a.ldx};
 #pragma unroll
     for (int q = 0; q < kRing - 1; ++q) {
@@ -188,7 +146,7 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
     constexpr int P = kPairs<V>;
     ptx::grid_dep_wait();
     extern __shared__ float4 smem4[];   // the rings, then the sums [blockDim.y][K+1][blockDim.x * V]
-    using Ring = RowRing<T, V, kThreads>;
+    using Ring = RowRing<T, V, kThreads, kGroup, kRing>;
     const int tid = threadIdx.y * blockDim.x + threadIdx.x;
     const int pk = blockIdx.y * blockDim.x + threadIdx.x, c = pk * V;
     float2 dw[K][P], db[P], w[K][P], bias[P];
@@ -384,7 +342,7 @@ conv2d_status_t fwd(const ConvSeq& s, cudaStream_t stream)
     a.pieces = (int)ceil_div_u(s.L, a.rows);
     const long long threads = (long long)a.packs * a.pieces * s.B;
     if (threads > 0x7fffff00LL) return CONV2D_ERR_SHAPE;
-    if (launch_pdl(conv1d_fwd_kernel<T, V, K>, dim3(ceil_div_u(threads, kThreads)), dim3(kThreads), RowRing<T, V, kThreads>::smem, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
+    if (launch_pdl(conv1d_fwd_kernel<T, V, K>, dim3(ceil_div_u(threads, kThreads)), dim3(kThreads), RowRing<T, V, kThreads, kGroup, kRing>::smem, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;
 }
@@ -401,7 +359,7 @@ conv2d_status_t bwd(const ConvSeq& s, cudaStream_t stream)
     a.pieces = p.pieces, a.packs = s.D / V, a.jobs = (unsigned)p.jobs;
     a.partials = s.dw || s.dbias ? s.partials : nullptr;
     if (p.across > 65535 || p.jobs > 0x7fff0000LL) return CONV2D_ERR_SHAPE;
-    const size_t rings = 2 * RowRing<T, V, kThreads>::smem, sums = (size_t)kThreads * V * (K + 1) * sizeof(float), smem = rings > sums ? rings : sums;
+    const size_t rings = 2 * RowRing<T, V, kThreads, kGroup, kRing>::smem, sums = (size_t)kThreads * V * (K + 1) * sizeof(float), smem = rings > sums ? rings : sums;
     static SmemLimit limit;
     if (raise_smem_limit(reinterpret_cast<const void*>(conv1d_bwd_kernel<T, V, K>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
     if (launch_pdl(conv1d_bwd_kernel<T, V, K>, dim3((unsigned)p.parts, (unsigned)p.across), dim3(p.tx, p.ty), smem, stream, a) != cudaSuccess)

@@ -24,6 +24,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kGroup = 2, kRing = 8;    // rows of a group (four take the backward pass to 240 registers), groups of a ring
 
 template <typename T>
 struct NormArgs {
@@ -38,7 +39,7 @@ struct NormArgs {
     float eps;
     int act;
     int lanes, chunks, chunk;           // rows: lanes of a group; chunks of samples, samples of a chunk
-    int tile_groups, tiles, parts, part_rows;
+    int tile_groups, tiles, parts, part_rows, ev;   // ev: packs of a group
 };
 
 // ------------------------------------------------------------------------------------------------------------- rows
@@ -232,122 +233,200 @@ __global__ void __launch_bounds__(kThreads) norm_rows_bwd_kernel(const NormArgs<
 
 // ----------------------------------------------------------------------------------------------------- slab and stream
 
-// What a block takes: `groups` groups of sample n from channel c0 on, rows r0 .. r1.  A thread keeps to one pack of channels and takes every
-// `step`th row; wider rows than the block has threads (one group then) are taken a block's width at a time.
+// What a block takes: `groups` groups of sample n from channel c0 on, rows r0 .. r1.  A thread keeps to one pack of channels (pack, of group `group`) and
+// takes every `step`th row from `first` on, `count` in all; wider rows than the block has threads (one group then) are taken a block's
+// width at a time, in `turns`.
 template <typename T, int V>
 struct Part {
-    int part, groups, c0, width, packs, step, turns, r0, r1;
+    int part, groups, g0, c0, packs, ev, step, turns, r0, r1, pack, group, first, count;
     long long n;
     __device__ explicit Part(const NormArgs<T>& a)
     {
         unsigned bx = blockIdx.x;
         part = (int)(bx % a.parts);
         bx /= a.parts;
-        const int tile = (int)(bx % a.tiles);
+        const int tile = (int)(bx % a.tiles), tid = threadIdx.x;
         n = bx / a.tiles;
-        groups = min(a.tile_groups, a.G - tile * a.tile_groups);
-        c0 = tile * a.tile_groups * a.E;
-        width = groups * a.E;
-        packs = width / V;
-        step = packs <= kThreads ? kThreads / packs : 1;
-        turns = packs <= kThreads ? 1 : (packs + kThreads - 1) / kThreads;
+        g0 = tile * a.tile_groups;
+        groups = min(a.tile_groups, a.G - g0);
+        c0 = g0 * a.E;
+        ev = a.ev;
+        packs = groups * ev;
         r0 = min(part * a.part_rows, a.S), r1 = min(r0 + a.part_rows, a.S);
+        step = 1, turns = 1, first = r0, pack = tid, group = 0;
+        if (packs <= kThreads) {
+            const int row = tid / packs;
+            step = kThreads / packs;
+            pack = tid - row * packs;
+            group = pack / ev;
+            first = r0 + row;
+            if (row >= step) pack = -1;
+        } else {
+            turns = (packs + kThreads - 1) / kThreads;
+        }
+        count = pack >= 0 && first < r1 ? (r1 - first + step - 1) / step : 0;
     }
-    // the pack of this thread in turn q, or -1
+    // the pack of this thread in turn q, or -1; and its rows then
     __device__ int pack_of(int q) const
     {
-        const int tid = threadIdx.x;
-        if (turns == 1) return tid < step * packs ? tid % packs : -1;
-        const int p = tid + q * kThreads;
+        const int p = turns == 1 ? pack : pack + q * kThreads;
         return p < packs ? p : -1;
     }
-    __device__ int first_row() const { return turns == 1 ? r0 + (int)threadIdx.x / packs : r0; }
+    __device__ int count_of(int q) const { return pack_of(q) >= 0 ? count : 0; }
 };
 
-// Sum over the threads that hold group gi of what `value` gives for a thread index, by one warp.
-template <typename T, int V, typename F>
-__device__ __forceinline__ float group_sum(const Part<T, V>& p, int E, int gi, F value)
+// Sums over the threads that hold group gi of what `value` gives for a thread index, by one warp.
+template <int N, typename T, int V, typename F>
+__device__ __forceinline__ void group_sums(const Part<T, V>& p, int gi, float (&s)[N], F value)
 {
     const int lane = threadIdx.x & 31;
-    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = 0.f;
     if (p.turns == 1) {
-        const int ev = E / V;
-        for (int k = lane; k < p.step * ev; k += 32) s += value(k / ev * p.packs + gi * ev + k % ev);
+        // lanes by packs of the group (the next power of two) and rows
+        const int shift = p.ev >= 32 ? 5 : 32 - __clz(p.ev - 1), c0 = lane & ((1 << shift) - 1);
+        for (int row = lane >> shift; row < p.step; row += 32 >> shift)
+            for (int c = c0; c < p.ev; c += 1 << shift) value(row * p.packs + gi * p.ev + c, s);
     } else {
-        for (int k = lane; k < kThreads; k += 32) s += value(k);
+        for (int k = lane; k < kThreads; k += 32) value(k, s);
     }
-    return lanes_sum(s, 32);
+    lanes_sums(s, 32);
 }
 
 enum { kSlab = 0, kStreamStats = 1, kStreamApply = 2 };
 
+// The packs of one tensor that a thread takes: rows first, first + step, .. of its channels.  A slab's stay in shared memory, all under way at once;
+// a stream's go through a ring.
+template <typename T, int V, bool KEEP>
+struct ThreadRows {
+    using Ring = RowRing<T, V, kThreads, kGroup, kRing>;
+    static constexpr int bytes = V * (int)sizeof(T);
+    Ring ring;                          // (KEEP: mine is the first of all slots)
+    int count;
+    __device__ void begin() const
+    {
+        if (KEEP) {
+            const T* from = ring.p;
+            unsigned char* to = ring.mine;
+#pragma unroll 4
+            for (int i = 0; i < count; ++i, from += ring.ld, to += kThreads * bytes) {
+                if (Ring::async) copy_async<Ring::async ? bytes : 4>(to, from, true);
+                else store_pack(reinterpret_cast<T*>(to), load_pack<T, V>(from));
+            }
+        }
+    }
+    __device__ Pack<T, V> get(int q, int i, int j) const
+    {
+        if (KEEP) return *reinterpret_cast<const Pack<T, V>*>(ring.mine + (size_t)(i + j < count ? i + j : 0) * (kThreads * bytes));
+        return ring.get(q, i, j, count);
+    }
+};
+template <typename T, int V> constexpr size_t ring_bytes = RowRing<T, V, kThreads, kGroup, kRing>::smem;
+
+// Walks `count` rows of the thread in groups: `issue(q, i)` starts the copies of group q, `take(q, i)` uses it.
+template <bool KEEP, typename Issue, typename Take>
+__device__ __forceinline__ void walk_rows(int count, Issue issue, Take take)
+{
+    if (!KEEP) {
+#pragma unroll
+        for (int q = 0; q < kRing - 1; ++q) {
+            issue(q, q * kGroup);
+            copies_commit();
+        }
+    }
+    int q = 0;
+#pragma unroll 1
+    for (int i = 0; i < count; i += kGroup, ++q) {
+        if (!KEEP) copies_wait<kRing - 2>();
+        take(q, i);
+        if (!KEEP) {
+            issue(q + kRing - 1, i + (kRing - 1) * kGroup);
+            copies_commit();
+        }
+    }
+    if (!KEEP) copies_wait<0>();
+}
+
 template <typename T, int V, int MODE>
 __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<T> a)
 {
+    constexpr int P = kPairs<V>;
+    constexpr bool KEEP = MODE == kSlab;
     ptx::grid_dep_wait();
     extern __shared__ float4 smem4[];
     __shared__ float ecount[kThreads], emean[kThreads], em2[kThreads];
     float4* gstat = smem4;                                   // [tile_groups] count, mean, sum of squares about it; then mean, rstd
     float2* gnorm = reinterpret_cast<float2*>(gstat + a.tile_groups);
-    Pack<T, V>* kept = reinterpret_cast<Pack<T, V>*>(reinterpret_cast<float4*>(gnorm) + (a.tile_groups + 1) / 2);
+    unsigned char* rows = reinterpret_cast<unsigned char*>(reinterpret_cast<float4*>(gnorm) + (a.tile_groups + 1) / 2);
     const Part<T, V> p(a);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int g0 = p.c0 / a.E;
-    const T* x = a.x + p.n * a.S * a.ldx + p.c0;
+    const int g0 = p.g0;
+    const T* x = a.x + (p.n * a.S + p.first) * a.ldx + p.c0;
+    using Rows = ThreadRows<T, V, KEEP>;
+    auto rows_of = [&](int q) {
+        Rows r;
+        r.count = p.count_of(q);
+        // (turns take whole rows: a part's rows each)
+        r.ring = {rows + ((KEEP ? q * a.part_rows * kThreads : 0) + threadIdx.x) * Rows::bytes, x + (r.count ? p.pack_of(q) * V : 0), p.step * a.ldx};
+        return r;
+    };
 
     if (MODE != kStreamApply) {
-        float shift = 0.f, s1 = 0.f, s2 = 0.f;
+        if (KEEP) {
+            for (int q = 0; q < p.turns; ++q) rows_of(q).begin();
+            copies_commit();
+            copies_wait<0>();
+        }
+        float2 s1 = both(0.f), s2 = both(0.f);
+        float shift = 0.f;
         int count = 0;
         for (int q = 0; q < p.turns; ++q) {
-            const int pk = p.pack_of(q);
-            if (pk < 0) continue;
-            for (int r = p.first_row(); r < p.r1; r += 4 * p.step) {
-                Pack<T, V> in[4];
+            const Rows r = rows_of(q);
+            walk_rows<KEEP>(r.count, [&](int g, int i) { r.ring.issue(g, i, r.count); }, [&](int g, int i) {
+                float2 v[kGroup][P];
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (r + j * p.step < p.r1) in[j] = load_pack<T, V>(x + (r + j * p.step) * a.ldx + pk * V);
+                for (int j = 0; j < kGroup; ++j) pairs<T, V>(r.get(g, i, j), v[j]);
+                if (count == 0) shift = v[0][0].x;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (r + j * p.step >= p.r1) break;
-                    if (MODE == kSlab) kept[(size_t)(r + j * p.step - p.r0) * p.packs + pk] = in[j];
-                    float v[V];
-                    unpack(in[j], v);
-                    if (count == 0) shift = v[0];
+                for (int j = 0; j < kGroup; ++j) {
+                    if (i + j >= r.count) break;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float d = v[i] - shift;
-                        s1 += d;
-                        s2 = fmaf(d, d, s2);
+                    for (int k = 0; k < P; ++k) {
+                        const float2 d = __fadd2_rn(v[j][k], both(-shift));
+                        s1 = __fadd2_rn(s1, d);
+                        s2 = __ffma2_rn(d, d, s2);
                     }
                     count += V;
                 }
-            }
+            });
         }
-        const float cnt = (float)count, off = count ? s1 / cnt : 0.f;
+        if (V == 1) s1.y = s2.y = 0.f;
+        const float cnt = (float)count, t1 = s1.x + s1.y, off = count ? t1 / cnt : 0.f;
         ecount[threadIdx.x] = cnt;
         emean[threadIdx.x] = shift + off;
-        em2[threadIdx.x] = s2 - s1 * off;
+        em2[threadIdx.x] = (s2.x + s2.y) - t1 * off;
         __syncthreads();
         for (int gi = warp; gi < p.groups; gi += kWarps) {
-            const float n = group_sum(p, a.E, gi, [&](int t) { return ecount[t]; });
-            const float base = group_sum(p, a.E, gi, [&](int t) { return ecount[t] * emean[t]; });
-            const float mean = n > 0.f ? base / n : 0.f;
-            const float m2 = group_sum(p, a.E, gi, [&](int t) {
-                const float d = emean[t] - mean;
-                return ecount[t] > 0.f ? fmaf(ecount[t] * d, d, em2[t]) : 0.f;
+            float t[2], q[1];
+            group_sums(p, gi, t, [&](int k, float (&o)[2]) { o[0] += ecount[k], o[1] = fmaf(ecount[k], emean[k], o[1]); });
+            const float n = t[0], mean = n > 0.f ? t[1] / n : 0.f;
+            group_sums(p, gi, q, [&](int k, float (&o)[1]) {
+                const float d = emean[k] - mean;
+                if (ecount[k] > 0.f) o[0] += fmaf(ecount[k] * d, d, em2[k]);
             });
+            const float m2 = q[0];
             if (lane == 0) {
                 const float4 st = make_float4(n, mean, m2, 0.f);
-                if (MODE == kSlab) gstat[gi] = st;
+                if (KEEP) gstat[gi] = st;
                 else a.part_stats[((size_t)p.n * a.G + g0 + gi) * a.parts + p.part] = st;
             }
         }
         if (MODE == kStreamStats) return;
     }
-    if (MODE == kSlab) cg::this_cluster().sync();
+    if (KEEP) cg::this_cluster().sync();
     for (int gi = warp; gi < p.groups; gi += kWarps) {
         auto stat = [&](int k) {
-            if (MODE == kSlab) return cg::this_cluster().map_shared_rank(gstat, k)[gi];
+            if (KEEP) return cg::this_cluster().map_shared_rank(gstat, k)[gi];
             return a.part_stats[((size_t)p.n * a.G + g0 + gi) * a.parts + k];
         };
         float n = 0.f, base = 0.f, m2 = 0.f;
@@ -372,107 +451,166 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
             }
         }
     }
-    __syncthreads();
-    T* y = a.y + p.n * a.S * a.ldy + p.c0;
+    // the statistics stay readable until all blocks of the cluster have them
+    if (KEEP) cg::this_cluster().sync();
+    else __syncthreads();
+    const long long ystep = p.step * a.ldy;
     for (int q = 0; q < p.turns; ++q) {
+        const Rows r = rows_of(q);
+        if (r.count == 0) continue;
+        T* y = a.y + (p.n * a.S + p.first) * a.ldy + p.c0 + p.pack_of(q) * V;
         const int pk = p.pack_of(q);
-        if (pk < 0) continue;
-        const float2 st = gnorm[pk * V / a.E];
-        float scale[V], beta[V];
-        load_params<V>(a.gamma, 1.f, p.c0 + pk * V, true, scale);
+        const float2 st = gnorm[p.group];
+        float gamma[V], beta[V];
+        load_params<V>(a.gamma, 1.f, p.c0 + pk * V, true, gamma);
         load_params<V>(a.beta, 0.f, p.c0 + pk * V, true, beta);
-        for (int r = p.first_row(); r < p.r1; r += 4 * p.step) {
-            Pack<T, V> in[4];
+        float2 scale[P], add[P];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int rr = r + j * p.step;
-                if (rr < p.r1) in[j] = MODE == kSlab ? kept[(size_t)(rr - p.r0) * p.packs + pk] : load_pack<T, V>(x + rr * a.ldx + pk * V);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (r + j * p.step >= p.r1) break;
-                float v[V];
-                unpack(in[j], v);
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = fmaf((v[i] - st.x) * st.y, scale[i], beta[i]);
-                activate(v, a.act);
-                store_pack(y + (r + j * p.step) * a.ldy + pk * V, pack<T, V>(v));
-            }
+        for (int k = 0; k < P; ++k) {
+            scale[k] = make_float2(st.y * gamma[2 * k], V > 1 ? st.y * gamma[V > 1 ? 2 * k + 1 : 0] : 0.f);
+            add[k] = make_float2(beta[2 * k], V > 1 ? beta[V > 1 ? 2 * k + 1 : 0] : 0.f);
         }
+        walk_rows<KEEP>(r.count, [&](int g, int i) { r.ring.issue(g, i, r.count); }, [&](int g, int i) {
+            float o[kGroup * 2 * P];
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) {
+                float2 v[P];
+                pairs<T, V>(r.get(g, i, j), v);
+#pragma unroll
+                for (int k = 0; k < P; ++k) {
+                    v[k] = __ffma2_rn(__fadd2_rn(v[k], both(-st.x)), scale[k], add[k]);
+                    o[2 * (j * P + k)] = v[k].x, o[2 * (j * P + k) + 1] = v[k].y;
+                }
+            }
+            activate(o, a.act);
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) {
+                float2 v[P];
+#pragma unroll
+                for (int k = 0; k < P; ++k) v[k] = make_float2(o[2 * (j * P + k)], o[2 * (j * P + k) + 1]);
+                if (i + j < r.count) store_pack(y, pack_of<T, V>(v));
+                y += ystep;
+            }
+        });
     }
-    if (MODE == kSlab) cg::this_cluster().sync();            // the statistics stay readable until all blocks have them
 }
 
 template <typename T, int V, int MODE>
 __global__ void __launch_bounds__(kThreads) norm_slab_bwd_kernel(const NormArgs<T> a)
 {
+    constexpr int P = kPairs<V>;
+    constexpr bool KEEP = MODE == kSlab;
     ptx::grid_dep_wait();
     extern __shared__ float4 smem4[];
     __shared__ float e1[kThreads], e2[kThreads];
     float4* gsum = smem4;                                    // [tile_groups] sums over the part of gamma d and gamma d x^
     float2* gmean = reinterpret_cast<float2*>(gsum + a.tile_groups);
     float* csum = reinterpret_cast<float*>(reinterpret_cast<float4*>(gmean) + (a.tile_groups + 1) / 2);       // [2][kThreads * V]
-    Pack<T, V>* kept = reinterpret_cast<Pack<T, V>*>(csum + (MODE == kStreamApply ? 0 : 2 * kThreads * V));
+    unsigned char* rows = reinterpret_cast<unsigned char*>(csum + (MODE == kStreamApply ? 0 : 2 * kThreads * V));
     const Part<T, V> p(a);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int g0 = p.c0 / a.E, rows = p.r1 - p.r0;
-    const T* x = a.x + p.n * a.S * a.ldx + p.c0;
-    const T* dy = a.dy + p.n * a.S * a.lddy + p.c0;
+    const int g0 = p.g0, width = p.packs * V, kept = KEEP ? (p.turns == 1 ? (a.part_rows + p.step - 1) / p.step : a.part_rows) : 0;
+    const T* x = a.x + (p.n * a.S + p.first) * a.ldx + p.c0;
+    const T* dy = a.dy + (p.n * a.S + p.first) * a.lddy + p.c0;
+    using Rows = ThreadRows<T, V, KEEP>;
+    auto rows_of = [&](int q, bool second) {                 // of x, or of dy
+        const size_t before = KEEP ? ((size_t)second * p.turns + q) * kept * kThreads * Rows::bytes : second * ring_bytes<T, V>;
+        Rows r;
+        r.count = p.count_of(q);
+        r.ring = {rows + before + threadIdx.x * Rows::bytes, (second ? dy : x) + (r.count ? p.pack_of(q) * V : 0), p.step * (second ? a.lddy : a.ldx)};
+        return r;
+    };
+    // x^ and d of the rows of a group
+    struct Params { float2 gamma[P], beta[P]; float mean, rstd; };
+    auto params_of = [&](int pk) {
+        Params r;
+        const int g = g0 + p.group;
+        r.mean = a.mean[p.n * a.G + g], r.rstd = a.rstd[p.n * a.G + g];
+        float gamma[V], beta[V];
+        load_params<V>(a.gamma, 1.f, p.c0 + pk * V, true, gamma);
+        load_params<V>(a.beta, 0.f, p.c0 + pk * V, true, beta);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            r.gamma[k] = make_float2(gamma[2 * k], V > 1 ? gamma[V > 1 ? 2 * k + 1 : 0] : 0.f);
+            r.beta[k] = make_float2(beta[2 * k], V > 1 ? beta[V > 1 ? 2 * k + 1 : 0] : 0.f);
+        }
+        return r;
+    };
+    auto terms = [&](const Params& m, const Rows& rx, const Rows& rg, int g, int i, float2 (&xn)[kGroup][P], float (&d)[kGroup * 2 * P]) {
+        float pre[kGroup * 2 * P];
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+            float2 w[P];
+            pairs<T, V>(rx.get(g, i, j), xn[j]);
+            pairs<T, V>(rg.get(g, i, j), w);
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                xn[j][k] = __fmul2_rn(__fadd2_rn(xn[j][k], both(-m.mean)), both(m.rstd));
+                const float2 v = __ffma2_rn(xn[j][k], m.gamma[k], m.beta[k]);
+                pre[2 * (j * P + k)] = v.x, pre[2 * (j * P + k) + 1] = v.y;
+                d[2 * (j * P + k)] = w[k].x, d[2 * (j * P + k) + 1] = w[k].y;
+            }
+        }
+        times_slope(d, pre, a.act);
+    };
 
     if (MODE != kStreamApply) {
+        if (KEEP) {
+            for (int q = 0; q < p.turns; ++q) rows_of(q, false).begin(), rows_of(q, true).begin();
+            copies_commit();
+            copies_wait<0>();
+        }
         float m1 = 0.f, m2 = 0.f;
         for (int q = 0; q < p.turns; ++q) {
+            const Rows rx = rows_of(q, false), rg = rows_of(q, true);
             const int pk = p.pack_of(q);
-            float s1[V] = {}, s2[V] = {};
-            if (pk >= 0) {
-                const int g = g0 + pk * V / a.E;
-                const float mean = a.mean[p.n * a.G + g], rstd = a.rstd[p.n * a.G + g];
-                float gamma[V], beta[V];
-                load_params<V>(a.gamma, 1.f, p.c0 + pk * V, true, gamma);
-                load_params<V>(a.beta, 0.f, p.c0 + pk * V, true, beta);
-                for (int r = p.first_row(); r < p.r1; r += 2 * p.step) {
-                    Pack<T, V> xin[2], gin[2];
+            float2 s1[P], s2[P];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int rr = r + j * p.step;
-                        if (rr < p.r1) xin[j] = load_pack<T, V>(x + rr * a.ldx + pk * V), gin[j] = load_pack<T, V>(dy + rr * a.lddy + pk * V);
-                    }
+            for (int k = 0; k < P; ++k) s1[k] = s2[k] = both(0.f);
+            if (rx.count) {
+                const Params m = params_of(pk);
+                walk_rows<KEEP>(rx.count, [&](int g, int i) { rx.ring.issue(g, i, rx.count), rg.ring.issue(g, i, rx.count); }, [&](int g, int i) {
+                    float2 xn[kGroup][P];
+                    float d[kGroup * 2 * P];
+                    terms(m, rx, rg, g, i, xn, d);
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int rr = r + j * p.step;
-                        if (rr >= p.r1) break;
-                        if (MODE == kSlab) {
-                            kept[(size_t)(rr - p.r0) * p.packs + pk] = xin[j];
-                            kept[(size_t)(rows + rr - p.r0) * p.packs + pk] = gin[j];
+                    for (int j = 0; j < kGroup; ++j) {
+                        if (i + j >= rx.count) break;
+#pragma unroll
+                        for (int k = 0; k < P; ++k) {
+                            const float2 e = make_float2(d[2 * (j * P + k)], d[2 * (j * P + k) + 1]);
+                            s1[k] = __fadd2_rn(s1[k], e);
+                            s2[k] = __ffma2_rn(e, xn[j][k], s2[k]);
                         }
-                        float v[V], d[V], pre[V];
-                        unpack(xin[j], v);
-                        unpack(gin[j], d);
-#pragma unroll
-                        for (int i = 0; i < V; ++i) v[i] = (v[i] - mean) * rstd, pre[i] = fmaf(v[i], gamma[i], beta[i]);
-                        times_slope(d, pre, a.act);
-#pragma unroll
-                        for (int i = 0; i < V; ++i) s1[i] += d[i], s2[i] = fmaf(d[i], v[i], s2[i]);
                     }
-                }
+                });
 #pragma unroll
-                for (int i = 0; i < V; ++i) m1 = fmaf(gamma[i], s1[i], m1), m2 = fmaf(gamma[i], s2[i], m2);
+                for (int k = 0; k < P; ++k) {
+                    m1 = fmaf(m.gamma[k].x, s1[k].x, m1), m2 = fmaf(m.gamma[k].x, s2[k].x, m2);
+                    if (V > 1) m1 = fmaf(m.gamma[k].y, s1[k].y, m1), m2 = fmaf(m.gamma[k].y, s2[k].y, m2);
+                }
             }
             if (a.channels) {
                 float* out = a.channels + ((size_t)p.n * a.parts + p.part) * 2 * a.C + p.c0;
                 if (p.step == 1) {
                     if (pk >= 0) {
 #pragma unroll
-                        for (int i = 0; i < V; ++i) out[pk * V + i] = s1[i], out[a.C + pk * V + i] = s2[i];
+                        for (int i = 0; i < V; ++i) {
+                            out[pk * V + i] = i % 2 ? s1[i / 2].y : s1[i / 2].x;
+                            out[a.C + pk * V + i] = i % 2 ? s2[i / 2].y : s2[i / 2].x;
+                        }
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < V; ++i) csum[threadIdx.x * V + i] = s1[i], csum[(kThreads + threadIdx.x) * V + i] = s2[i];
+                    for (int i = 0; i < V; ++i) {
+                        csum[threadIdx.x * V + i] = i % 2 ? s1[i / 2].y : s1[i / 2].x;
+                        csum[(kThreads + threadIdx.x) * V + i] = i % 2 ? s2[i / 2].y : s2[i / 2].x;
+                    }
                     __syncthreads();
-                    for (int k = threadIdx.x; k < 2 * p.width; k += kThreads) {
-                        const int which = k / p.width, c = k % p.width;
+                    for (int k = threadIdx.x; k < 2 * width; k += kThreads) {
+                        const int which = k / width, c = k % width;
                         float s = 0.f;
-                        for (int j = 0; j < p.step; ++j) s += csum[which * kThreads * V + j * p.width + c];
+                        for (int j = 0; j < p.step; ++j) s += csum[which * kThreads * V + j * width + c];
                         out[which * a.C + c] = s;
                     }
                 }
@@ -481,75 +619,68 @@ __global__ void __launch_bounds__(kThreads) norm_slab_bwd_kernel(const NormArgs<
         e1[threadIdx.x] = m1, e2[threadIdx.x] = m2;
         __syncthreads();
         for (int gi = warp; gi < p.groups; gi += kWarps) {
-            const float t1 = group_sum(p, a.E, gi, [&](int t) { return e1[t]; });
-            const float t2 = group_sum(p, a.E, gi, [&](int t) { return e2[t]; });
+            float t[2];
+            group_sums(p, gi, t, [&](int k, float (&o)[2]) { o[0] += e1[k], o[1] += e2[k]; });
+            const float t1 = t[0], t2 = t[1];
             if (lane == 0) {
                 const float4 st = make_float4(t1, t2, 0.f, 0.f);
-                if (MODE == kSlab) gsum[gi] = st;
+                if (KEEP) gsum[gi] = st;
                 else a.part_stats[((size_t)p.n * a.G + g0 + gi) * a.parts + p.part] = st;
             }
         }
         if (MODE == kStreamStats) return;
     }
-    if (MODE == kSlab) cg::this_cluster().sync();
+    if (KEEP) cg::this_cluster().sync();
     for (int gi = warp; gi < p.groups; gi += kWarps) {
         float t1 = 0.f, t2 = 0.f;
         for (int k = lane; k < a.parts; k += 32) {
-            const float4 st = MODE == kSlab ? cg::this_cluster().map_shared_rank(gsum, k)[gi]
-                                            : a.part_stats[((size_t)p.n * a.G + g0 + gi) * a.parts + k];
+            const float4 st = KEEP ? cg::this_cluster().map_shared_rank(gsum, k)[gi] : a.part_stats[((size_t)p.n * a.G + g0 + gi) * a.parts + k];
             t1 += st.x, t2 += st.y;
         }
         t1 = lanes_sum(t1, 32), t2 = lanes_sum(t2, 32);
         const float inv = 1.f / ((float)a.S * a.E);
         if (lane == 0) gmean[gi] = make_float2(t1 * inv, t2 * inv);
     }
-    __syncthreads();
-    T* dx = a.dx + p.n * a.S * a.lddx + p.c0;
+    if (KEEP) cg::this_cluster().sync();
+    else __syncthreads();
+    const long long dxstep = p.step * a.lddx;
     for (int q = 0; q < p.turns; ++q) {
+        const Rows rx = rows_of(q, false), rg = rows_of(q, true);
+        if (rx.count == 0) continue;
         const int pk = p.pack_of(q);
-        if (pk < 0) continue;
-        const int gi = pk * V / a.E;
-        const float2 m = gmean[gi];
-        const float mean = a.mean[p.n * a.G + g0 + gi], rstd = a.rstd[p.n * a.G + g0 + gi];
-        float gamma[V], beta[V];
-        load_params<V>(a.gamma, 1.f, p.c0 + pk * V, true, gamma);
-        load_params<V>(a.beta, 0.f, p.c0 + pk * V, true, beta);
-        for (int r = p.first_row(); r < p.r1; r += 2 * p.step) {
-            Pack<T, V> xin[2], gin[2];
+        const float2 mm = gmean[p.group];
+        const Params m = params_of(pk);
+        T* dx = a.dx + (p.n * a.S + p.first) * a.lddx + p.c0 + pk * V;
+        walk_rows<KEEP>(rx.count, [&](int g, int i) { rx.ring.issue(g, i, rx.count), rg.ring.issue(g, i, rx.count); }, [&](int g, int i) {
+            float2 xn[kGroup][P];
+            float d[kGroup * 2 * P];
+            terms(m, rx, rg, g, i, xn, d);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int rr = r + j * p.step;
-                if (rr >= p.r1) continue;
-                if (MODE == kSlab) {
-                    xin[j] = kept[(size_t)(rr - p.r0) * p.packs + pk];
-                    gin[j] = kept[(size_t)(rows + rr - p.r0) * p.packs + pk];
-                } else {
-                    xin[j] = load_pack<T, V>(x + rr * a.ldx + pk * V);
-                    gin[j] = load_pack<T, V>(dy + rr * a.lddy + pk * V);
+            for (int j = 0; j < kGroup; ++j) {
+                float2 o[P];
+#pragma unroll
+                for (int k = 0; k < P; ++k) {
+                    const float2 e = __ffma2_rn(make_float2(d[2 * (j * P + k)], d[2 * (j * P + k) + 1]), m.gamma[k], both(-mm.x));
+                    o[k] = __fmul2_rn(both(m.rstd), __ffma2_rn(xn[j][k], both(-mm.y), e));
                 }
+                if (i + j < rx.count) store_pack(dx, pack_of<T, V>(o));
+                dx += dxstep;
             }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (r + j * p.step >= p.r1) break;
-                float v[V], d[V], pre[V];
-                unpack(xin[j], v);
-                unpack(gin[j], d);
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = (v[i] - mean) * rstd, pre[i] = fmaf(v[i], gamma[i], beta[i]);
-                times_slope(d, pre, a.act);
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = rstd * (d[i] * gamma[i] - m.x - v[i] * m.y);
-                store_pack(dx + (r + j * p.step) * a.lddx + pk * V, pack<T, V>(v));
-            }
-        }
+        });
     }
-    if (MODE == kSlab) cg::this_cluster().sync();
 }
 
 // --------------------------------------------------------------------------------------------------------------- plan
 
-constexpr size_t kSlabBytes = 96 * 1024;      // rows that a block keeps: two blocks an SM
+constexpr size_t kSlabBytes = 64 * 1024;      // rows that a block keeps: three blocks an SM
 constexpr int kMaxCluster = 8, kSms = 148;
+
+// Slots of 16 bytes (of an element, without packs) that the threads of a slab's block need, in bytes: threads that a row leaves over have some, too.
+size_t slab_bytes(int part_rows, int packs, int pack_bytes, bool bwd)
+{
+    const int step = packs <= kThreads ? kThreads / packs : 1, turns = packs <= kThreads ? 1 : (packs + kThreads - 1) / kThreads;
+    return (size_t)((part_rows + step - 1) / step) * turns * kThreads * pack_bytes * (bwd ? 2 : 1);
+}
 
 // How a call is cut.  The sizes decide, and whether rows can be moved in packs of 16 bytes; the workspace has room for either.
 struct NormPlan {
@@ -579,19 +710,29 @@ NormPlan make_norm_plan(int N, int S, int C, int G, int esize, int V, bool bwd)
         p.channels = bwd ? (size_t)p.chunks * 2 * C : 0;
         return p;
     }
-    // groups of a tile: rows of 128 bytes or more, but not more packs than threads
-    p.tile_groups = (128 + E * esize - 1) / (E * esize);
-    if (p.tile_groups > G) p.tile_groups = G;
-    while (p.tile_groups > 1 && p.tile_groups * ev > kThreads) --p.tile_groups;
-    p.tiles = (G + p.tile_groups - 1) / p.tile_groups;
-    const size_t row = (size_t)p.tile_groups * E * esize * (bwd ? 2 : 1);
-    const long long slabs = (long long)N * p.tiles;
-    // a cluster of the fewest blocks that hold the slab; more while there are SMs left and rows to share out
+    // groups of a tile: rows of 128 bytes or more, of 64 or 32 where the slab does not fit else, but not more packs than threads
+    const auto tile = [&](int bytes) {
+        int n = (bytes + E * esize - 1) / (E * esize);
+        if (n > G) n = G;
+        while (n > 1 && n * ev > kThreads) --n;
+        return n;
+    };
     int parts = 1;
-    while (parts < kMaxCluster && (size_t)((S + parts - 1) / parts) * row > kSlabBytes) parts *= 2;
-    p.slab = (size_t)((S + parts - 1) / parts) * row <= kSlabBytes;
-    while (p.slab && parts < kMaxCluster && slabs * parts < 2 * kSms && S / parts >= 32) parts *= 2;
-    if (p.slab && slabs * parts < kSms / 2 && (double)S * row * slabs > 4e6) p.slab = false;
+    const size_t slab_limit = (size_t)env_int("CONV2D_B200_NORM_SLAB_KB", (int)(kSlabBytes >> 10)) << 10;
+    for (int bytes = env_int("CONV2D_B200_NORM_ROW", 128); bytes >= 32; bytes /= 2) {
+        p.tile_groups = tile(bytes);
+        p.tiles = (G + p.tile_groups - 1) / p.tile_groups;
+        // a cluster of the fewest blocks that hold the slab; more while there are SMs left and rows to share out
+        const auto need = [&](int n) { return slab_bytes((S + n - 1) / n, p.tile_groups * ev, V * esize, bwd); };
+        parts = 1;
+        while (parts < kMaxCluster && need(parts) > slab_limit) parts *= 2;
+        p.slab = need(parts) <= slab_limit;
+        if (p.slab) break;
+    }
+    if (!p.slab) p.tile_groups = tile(128), p.tiles = (G + p.tile_groups - 1) / p.tile_groups;
+    const long long slabs = (long long)N * p.tiles;
+    while (p.slab && parts < kMaxCluster && slabs * parts < 4 * kSms && S / parts >= 32) parts *= 2;
+    if (p.slab && slabs * parts < kSms / 2 && (double)S * p.tile_groups * E * esize * slabs > 4e6) p.slab = false;
     if (!p.slab) {
         const long long want = (8LL * kSms + slabs - 1) / slabs;
         parts = (int)(want < 1 ? 1 : want > 1024 ? 1024 : want);
@@ -631,7 +772,7 @@ struct ParamStore {
     }
 };
 
-template <typename T>
+template <typename T, int V>
 NormArgs<T> make_args(const NormSeq& s, const NormPlan& p)
 {
     NormArgs<T> a{};
@@ -642,7 +783,7 @@ NormArgs<T> make_args(const NormSeq& s, const NormPlan& p)
     a.N = s.N, a.S = s.S, a.C = s.C, a.G = s.G, a.E = s.C / s.G;
     a.ldx = s.ldx, a.ldy = s.ldy, a.lddy = s.lddy, a.lddx = s.lddx, a.eps = s.eps, a.act = s.act;
     a.lanes = p.lanes, a.chunks = p.chunks, a.chunk = p.chunk;
-    a.tile_groups = p.tile_groups, a.tiles = p.tiles, a.parts = p.parts, a.part_rows = p.part_rows;
+    a.tile_groups = p.tile_groups, a.tiles = p.tiles, a.parts = p.parts, a.part_rows = p.part_rows, a.ev = a.E / V;
     return a;
 }
 
@@ -661,7 +802,7 @@ template <typename T, int V>
 conv2d_status_t fwd(const NormSeq& s, cudaStream_t stream)
 {
     const NormPlan p = make_norm_plan(s.N, s.S, s.C, s.G, sizeof(T), V, false);
-    const NormArgs<T> a = make_args<T>(s, p);
+    const NormArgs<T> a = make_args<T, V>(s, p);
     if (p.rows) {
         const long long blocks = (long long)ceil_div_u((long long)s.G * p.lanes, kThreads) * p.chunks;
         if (p.nv == 1) return launched(norm_rows_fwd_kernel<T, V, 1, 4>, blocks, 0, 1, stream, a);
@@ -672,20 +813,24 @@ conv2d_status_t fwd(const NormSeq& s, cudaStream_t stream)
     const long long blocks = (long long)s.N * p.tiles * p.parts;
     const size_t fixed = (size_t)p.tile_groups * 16 + (p.tile_groups + 1) / 2 * 16;
     if (p.slab) {
-        const size_t smem = fixed + (size_t)p.part_rows * p.tile_groups * a.E * sizeof(T);
+        const size_t smem = fixed + slab_bytes(p.part_rows, p.tile_groups * (a.E / V), V * sizeof(T), false);
         static SmemLimit limit;
         if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_fwd_kernel<T, V, kSlab>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
         return launched(norm_slab_fwd_kernel<T, V, kSlab>, blocks, smem, p.parts, stream, a);
     }
-    const conv2d_status_t st = launched(norm_slab_fwd_kernel<T, V, kStreamStats>, blocks, fixed, 1, stream, a);
-    return st != CONV2D_OK ? st : launched(norm_slab_fwd_kernel<T, V, kStreamApply>, blocks, fixed, 1, stream, a);
+    const size_t smem = fixed + ring_bytes<T, V>;
+    static SmemLimit stats, apply;
+    if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_fwd_kernel<T, V, kStreamStats>), smem, stats) != cudaSuccess
+        || raise_smem_limit(reinterpret_cast<const void*>(norm_slab_fwd_kernel<T, V, kStreamApply>), smem, apply) != cudaSuccess) return CONV2D_ERR_CUDA;
+    const conv2d_status_t st = launched(norm_slab_fwd_kernel<T, V, kStreamStats>, blocks, smem, 1, stream, a);
+    return st != CONV2D_OK ? st : launched(norm_slab_fwd_kernel<T, V, kStreamApply>, blocks, smem, 1, stream, a);
 }
 
 template <typename T, int V>
 conv2d_status_t bwd(const NormSeq& s, cudaStream_t stream)
 {
     const NormPlan p = make_norm_plan(s.N, s.S, s.C, s.G, sizeof(T), V, true);
-    const NormArgs<T> a = make_args<T>(s, p);
+    const NormArgs<T> a = make_args<T, V>(s, p);
     conv2d_status_t st;
     long long parts = (long long)s.N * p.parts;
     if (p.rows) {
@@ -698,13 +843,17 @@ conv2d_status_t bwd(const NormSeq& s, cudaStream_t stream)
         const long long blocks = (long long)s.N * p.tiles * p.parts;
         const size_t fixed = (size_t)p.tile_groups * 16 + (p.tile_groups + 1) / 2 * 16, sums = sizeof(float) * 2 * kThreads * V;
         if (p.slab) {
-            const size_t smem = fixed + sums + (size_t)p.part_rows * p.tile_groups * a.E * sizeof(T) * 2;
+            const size_t smem = fixed + sums + slab_bytes(p.part_rows, p.tile_groups * (a.E / V), V * sizeof(T), true);
             static SmemLimit limit;
             if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_bwd_kernel<T, V, kSlab>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
             st = launched(norm_slab_bwd_kernel<T, V, kSlab>, blocks, smem, p.parts, stream, a);
         } else {
-            st = launched(norm_slab_bwd_kernel<T, V, kStreamStats>, blocks, fixed + sums, 1, stream, a);
-            if (st == CONV2D_OK) st = launched(norm_slab_bwd_kernel<T, V, kStreamApply>, blocks, fixed, 1, stream, a);
+            const size_t first = fixed + sums + 2 * ring_bytes<T, V>, second = fixed + 2 * ring_bytes<T, V>;
+            static SmemLimit stats, apply;
+            if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_bwd_kernel<T, V, kStreamStats>), first, stats) != cudaSuccess
+                || raise_smem_limit(reinterpret_cast<const void*>(norm_slab_bwd_kernel<T, V, kStreamApply>), second, apply) != cudaSuccess) return CONV2D_ERR_CUDA;
+            st = launched(norm_slab_bwd_kernel<T, V, kStreamStats>, blocks, first, 1, stream, a);
+            if (st == CONV2D_OK) st = launched(norm_slab_bwd_kernel<T, V, kStreamApply>, blocks, second, 1, stream, a);
         }
     }
     if (st != CONV2D_OK || !a.channels) return st;

@@ -34,19 +34,6 @@ template <typename T, int V> __device__ __forceinline__ Pack<T, V> zero_pack()
     for (int i = 0; i < V; ++i) z.e[i] = from_float<T>(0.f);
     return z;
 }
-template <typename T, int V> __device__ __forceinline__ void unpack(const Pack<T, V>& p, float (&f)[V])
-{
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = to_float(p.e[i]);
-}
-template <typename T, int V> __device__ __forceinline__ Pack<T, V> pack(const float (&f)[V])
-{
-    Pack<T, V> p;
-#pragma unroll
-    for (int i = 0; i < V; ++i) p.e[i] = from_float<T>(f[i]);
-    return p;
-}
-
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 __device__ __forceinline__ float ex2(float v)
 {
@@ -129,6 +116,88 @@ __device__ __forceinline__ void copy_async(void* to, const void* from, bool real
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // Waits until all but the last PENDING groups of this thread's copies have arrived.
 template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
+
+
+// A thread's ring of RING groups of GROUP rows of one tensor in shared memory, by asynchronous copies: its packs of V elements,
+// V * sizeof(T) >= 4 bytes.  Narrower ones are loaded when they are needed.
+template <typename T, int V, int THREADS, int GROUP, int RING>
+struct RowRing {
+    static constexpr int bytes = V * (int)sizeof(T);
+    static constexpr bool async = bytes >= 4;
+    static constexpr size_t smem = async ? (size_t)RING * GROUP * THREADS * bytes : 0;
+    unsigned char* mine;
+    const T* p;                         // row 0, this thread's channels
+    long long ld;
+    __device__ void issue(int q, int t, int live) const
+    {
+        if (!async) return;
+#pragma unroll
+        for (int j = 0; j < GROUP; ++j) {
+            const bool real = t + j < live;
+            copy_async<async ? bytes : 4>(mine + (size_t)((q & (RING - 1)) * GROUP + j) * THREADS * bytes, p + (real ? (t + j) * ld : 0), real);
+        }
+    }
+    __device__ Pack<T, V> get(int q, int t, int j, int live) const
+    {
+        if (async) return *reinterpret_cast<const Pack<T, V>*>(mine + (size_t)((q & (RING - 1)) * GROUP + j) * THREADS * bytes);
+        return t + j < live ? load_pack<T, V>(p + (t + j) * ld) : zero_pack<T, V>();
+    }
+};
+
+// Pairs of channels (one channel and zero for V = 1).
+template <int V> constexpr int kPairs = (V + 1) / 2;
+__device__ __forceinline__ float2 to_pair(uint32_t bits, bf16) { return make_float2(__uint_as_float(bits << 16), __uint_as_float(bits & 0xffff0000u)); }
+__device__ __forceinline__ float2 to_pair(uint32_t bits, fp16) { return __half22float2(*reinterpret_cast<const __half2*>(&bits)); }
+__device__ __forceinline__ uint32_t from_pair(float2 f, bf16)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t from_pair(float2 f, fp16)
+{
+    const __half2 h = __floats2half2_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <typename T, int V>
+__device__ __forceinline__ void pairs(const Pack<T, V>& p, float2 (&f)[kPairs<V>])
+{
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) f[i] = to_pair(reinterpret_cast<const uint32_t*>(&p)[i], T());
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPairs<V>; ++i) f[i] = make_float2(to_float(p.e[2 * i]), V > 1 ? to_float(p.e[V > 1 ? 2 * i + 1 : 0]) : 0.f);
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> pack_of(const float2 (&f)[kPairs<V>])
+{
+    Pack<T, V> p;
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) reinterpret_cast<uint32_t*>(&p)[i] = from_pair(f[i], T());
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) p.e[i] = from_float<T>(i % 2 ? f[i / 2].y : f[i / 2].x);
+    }
+    return p;
+}
+
+// The same as arrays.
+template <typename T, int V> __device__ __forceinline__ void unpack(const Pack<T, V>& p, float (&f)[V])
+{
+    float2 q[kPairs<V>];
+    pairs<T, V>(p, q);
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = i % 2 ? q[i / 2].y : q[i / 2].x;
+}
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> pack(const float (&f)[V])
+{
+    float2 q[kPairs<V>];
+#pragma unroll
+    for (int i = 0; i < kPairs<V>; ++i) q[i] = make_float2(f[2 * i], V > 1 ? f[V > 1 ? 2 * i + 1 : 0] : 0.f);
+    return pack_of<T, V>(q);
+}
 
 // Rows of sequence b that hold tokens.
 __device__ __forceinline__ int sequence_length(const int* lengths, int b, int L)
