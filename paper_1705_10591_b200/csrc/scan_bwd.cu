@@ -46,14 +46,18 @@ struct BwdCut { int nl, cb, sets, blocks_group, segs, rows; };
 BwdCut bwd_cut(int B, int L, int D, int N, int G)
 {
     BwdCut c;
-    c.nl = bwd_lanes_for(N);
-    c.cb = 128 / c.nl;
+    c.nl = lanes_for(N, kSpt);
+    c.cb = c.nl == 1 ? 64 : 128 / c.nl;
     const int E = D / G;
-    c.sets = env_int("CONV2D_B200_SCAN_SETS", 0);
-    if (c.sets <= 0) c.sets = 1;
+    // a block's partial sums of dB and dC are for at least 32 channels, or the workspace would be larger than the tensors
+    c.sets = env_int("CONV2D_B200_SCAN_SETS", c.cb >= 32 ? 1 : 32 / c.cb);
     c.blocks_group = (int)ceil_div_u(E, (long long)c.cb * c.sets);
-    int segs = env_int("CONV2D_B200_SCAN_BWD_SEGS", 0);
-    if (segs <= 0) segs = 1;
+    // segments of time, where the blocks leave two thirds of the machine idle: two blocks for every SM then, of 64 rows at least
+    const long long blocks = (long long)B * G * c.blocks_group;
+    long long segs = blocks * 3 <= 148 ? 2 * 148 / blocks : 1;
+    if (segs > L / 64) segs = L / 64;
+    segs = env_int("CONV2D_B200_SCAN_BWD_SEGS", (int)segs);
+    if (segs < 1) segs = 1;
     c.rows = (int)(ceil_div_u(ceil_div_u(L, segs), kCheckpointRows) * kCheckpointRows);
     c.segs = (int)ceil_div_u(L, c.rows);
     return c;
@@ -77,6 +81,7 @@ template <typename T, int NL, int V>
 conv2d_status_t bwd(const ScanSeq& s, cudaStream_t stream)
 {
     using Tile = ScanBwdTile<NL>;
+    constexpr int e = sizeof(T);
     ScanBwdArgs<T> a;
     a.u = static_cast<const T*>(s.u), a.delta = static_cast<const T*>(s.delta), a.z = static_cast<const T*>(s.z), a.dy = static_cast<const T*>(s.dy);
     a.Bm = static_cast<const T*>(s.Bm), a.Cm = static_cast<const T*>(s.Cm);
@@ -94,17 +99,20 @@ conv2d_status_t bwd(const ScanSeq& s, cudaStream_t stream)
     const long long join = (long long)s.B * s.D * round4(s.N), per_row = rows * s.G * 2 * Tile::NP;
     if (jobs * carry_group > 0x7fffffffLL || per_row / 256 > 0x7ffffff0LL) return CONV2D_ERR_SHAPE;
     if (a.segs > 1) {
-        if (launch_pdl(scan_bwd_carry_kernel<T, NL, V>, dim3((unsigned)(jobs * carry_group)), dim3(128), 0, stream, a, carry_group) != cudaSuccess)
+        if (launch_pdl(scan_bwd_carry_kernel<T, NL, V>, dim3((unsigned)(jobs * carry_group)), dim3(Tile::SCAN), 0, stream, a, carry_group) != cudaSuccess)
             return CONV2D_ERR_CUDA;
         count_launch();
         if (launch_pdl(scan_join_kernel<true>, dim3(ceil_div_u(join, 256)), dim3(256), 0, stream, a.local, a.steps, s.A, s.dstate_out, s.dstate_in,
                        s.B, a.segs, s.D, s.N) != cudaSuccess) return CONV2D_ERR_CUDA;
         count_launch();
     }
-    const size_t smem = sizeof(float) * (Tile::fixed_floats + a.sets * Tile::template set_floats<V>());
+    a.u_unit = copy_unit(s.u, s.ldu, a.E, e), a.delta_unit = copy_unit(s.delta, s.lddelta, a.E, e), a.z_unit = copy_unit(s.z, s.ldz, a.E, e);
+    a.dy_unit = copy_unit(s.dy, s.lddy, a.E, e), a.B_unit = copy_unit(s.Bm, s.ldB, a.N, e), a.C_unit = copy_unit(s.Cm, s.ldC, a.N, e);
+    a.out_quads = a.E % 4 == 0 && rows_aligned(s.du, s.lddu, e, 4 * e) && rows_aligned(s.ddelta, s.ldddelta, e, 4 * e) && rows_aligned(s.dz, s.lddz, e, 4 * e);
+    const size_t smem = Tile::fixed(e) + a.sets * Tile::set_bytes;
     static SmemLimit limit;
-    if (raise_smem_limit(reinterpret_cast<const void*>(scan_bwd_kernel<T, NL, V>), smem, limit) != cudaSuccess
-        || launch_pdl(scan_bwd_kernel<T, NL, V>, dim3((unsigned)blocks), dim3(128), smem, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
+    if (raise_smem_limit(reinterpret_cast<const void*>(scan_bwd_kernel<T, NL>), smem, limit) != cudaSuccess
+        || launch_pdl(scan_bwd_kernel<T, NL>, dim3((unsigned)blocks), dim3(Tile::TH), smem, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
     count_launch();
     const conv2d_status_t st = launch_column_sums(a.per_channel, (long long)s.B * a.segs, (long long)s.D * (round4(s.N) + 2), channel_floats(s.D, round4(s.N)),
                                                   ChannelStore{s.dA, s.dD, s.ddelta_bias, s.D, s.N, round4(s.N)}, stream);
@@ -118,7 +126,7 @@ conv2d_status_t bwd(const ScanSeq& s, cudaStream_t stream)
 template <typename T, int V>
 conv2d_status_t bwd_lanes(const ScanSeq& s, cudaStream_t stream)
 {
-    switch (bwd_lanes_for(s.N)) {
+    switch (lanes_for(s.N, kSpt)) {
         case 1: return bwd<T, 1, V>(s, stream);
         case 2: return bwd<T, 2, V>(s, stream);
         case 4: return bwd<T, 4, V>(s, stream);

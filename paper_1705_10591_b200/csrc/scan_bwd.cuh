@@ -5,10 +5,12 @@
 //   dz = dy v silu'(z),  dDskip = sum_t g u
 //
 // The forward pass keeps the state before every 16th row.  A block walks the tiles of 16 rows from the last to the first; in a tile the
-// decays a and the states h of all 16 rows are computed again, from the kept one, into registers (a thread has four states of one
-// channel: 128 registers), so that the walk back needs no exponential.  Sums over the states go over the lanes of a channel, sums
+// states h of all 16 rows are computed again, from the kept one, into registers (a thread has four states of one channel: 64
+// registers; the decays beside them would make it one block an SM, so those are taken twice).  Sums over the states go over the lanes of a channel, sums
 // over the channels (dB, dC) over the other lanes, the warps and the channel sets that the block takes in turn, and from there as one
 // partial sum of the block into the workspace; those are added by a kernel of their own in a fixed order.
+// As in the forward pass four helping warps do what is done once per row and channel while the four scanning warps scan: copies, step sizes and
+// gates of the next tile, outputs and sums over the warps of the last one.
 #pragma once
 
 #include "scan_common.cuh"
@@ -16,13 +18,6 @@
 namespace conv2d_b200 {
 
 constexpr int kSpt = 4;                 // states of a thread
-
-inline int bwd_lanes_for(int N)
-{
-    int nl = 1;
-    while (nl * kSpt < N) nl *= 2;
-    return nl;
-}
 
 template <typename T>
 struct ScanBwdArgs {
@@ -37,41 +32,47 @@ struct ScanBwdArgs {
     int B, L, D, N, G, E;
     int segs, seg_rows, blocks_group, sets;
     long long ldu, lddelta, ldB, ldC, ldz, lddy, lddu, ldddelta, lddz;
-    bool softplus;
+    int u_unit, delta_unit, z_unit, dy_unit, B_unit, C_unit;         // bytes in which rows can be copied
+    bool out_quads, softplus;                                         // out_quads: du, ddelta, dz can be stored four elements at a time
 };
 
 template <int NL>
 struct ScanBwdTile {
-    static constexpr int W = 4, TH = W * 32, CL = 32 / NL, CB = W * CL, NP = NL * kSpt, TT = kCheckpointRows, YS = CB + CL;
-    // (s, s u, g) of the tile, B and C, three sums over states, the warps' sums over channels and the block's
-    static constexpr size_t fixed_floats = 4 * TT * CB + 2 * TT * NP + 3 * TT * YS + W * TT * 2 * NP + TT * 2 * NP;
-    // a set's carried gradient, dA and A of every thread, and its sums for dDskip and ddelta_bias
-    template <int V> static constexpr size_t set_floats() { return TH * (3 * kSpt + 2 * V); }
+    static constexpr int W = NL == 1 ? 2 : 4, SCAN = 32 * W, HELP = 128, TH = SCAN + HELP, RAWS = 4;
+    static constexpr int CL = 32 / NL, CB = W * CL, NP = NL * kSpt, TT = kCheckpointRows, YS = CB + 4;
+    static constexpr int PARTS = NP >= 128 ? 1 : 2;           // buffers of the warps' sums over channels
+    static constexpr size_t raw(size_t esize) { return esize * TT * (4 * CB + 2 * NP); }
+    // tiles as they lie in memory; twice (s, s u) and g of a tile, B and C, and three sums over states; the warps' sums over channels, and the block's
+    static constexpr size_t fixed(size_t esize)
+    {
+        return RAWS * raw(esize) + sizeof(float) * (2 * (3 * TT * CB + 2 * TT * NP + 3 * TT * YS) + PARTS * W * TT * 2 * NP + TT * 2 * NP);
+    }
+    // of a channel set: the carried gradient, dA and A of every scanning thread, and the helpers' sums for dDskip and ddelta_bias
+    static constexpr size_t set_bytes = sizeof(float) * (SCAN * 3 * kSpt + HELP * 8);
 };
 
-// Loads of a tile: pack `pk` of the rows tid / PPR + i * (TH / PPR), and elements tid + i * TH of B and C.
-template <typename T, int NL, int V>
-__global__ void __launch_bounds__(128) scan_bwd_kernel(const ScanBwdArgs<T> a)
+template <typename T, int NL>
+__global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const ScanBwdArgs<T> a)
 {
     using Tile = ScanBwdTile<NL>;
-    constexpr int W = Tile::W, TH = Tile::TH, CL = Tile::CL, CB = Tile::CB, NP = Tile::NP, TT = Tile::TT, YS = Tile::YS;
-    constexpr int PPR = CB / V, PK = (TT * PPR + TH - 1) / TH, BK = (TT * NP + TH - 1) / TH, RS = TH / PPR;
+    constexpr int W = Tile::W, HT = Tile::HELP, CL = Tile::CL, CB = Tile::CB, NP = Tile::NP, TT = Tile::TT, YS = Tile::YS, RAWS = Tile::RAWS, ES = sizeof(T);
+    constexpr int UNITS = TT * CB / 4, UK = (UNITS + HT - 1) / HT, UROWS = HT / (CB / 4), BUNITS = TT * NP / 4, BK = (BUNITS + HT - 1) / HT;
+    constexpr int QQ = TT * CB, BC = 2 * TT * NP, SB = 3 * TT * YS, PB = W * TT * 2 * NP, RAW = TT * (4 * CB + 2 * NP), SETS_TH = Tile::SCAN;
     ptx::grid_dep_wait();
     extern __shared__ float4 smem4[];
-    float4* q4 = smem4;                                       // [TT][CB] (s, s u, g, -)
-    float* Bs = reinterpret_cast<float*>(q4 + TT * CB);       // [TT][NP]
-    float* Cs = Bs + TT * NP;
-    float* vs = Cs + TT * NP;                                 // [TT][YS] sum_n C h, sum_n A2 q, sum_n e B
-    float* s1 = vs + TT * YS;
-    float* s2 = s1 + TT * YS;
-    float* parts = s2 + TT * YS;                              // [W][TT][2][NP]
-    float* acc = parts + W * TT * 2 * NP;                     // [TT][2][NP]
-    float4* carry4 = reinterpret_cast<float4*>(acc + TT * 2 * NP);   // [sets][TH]
-    float4* dA4 = carry4 + a.sets * TH;
-    float4* A24 = dA4 + a.sets * TH;
-    float* chan = reinterpret_cast<float*>(A24 + a.sets * TH);       // [sets][2][V][TH]
+    float2* dd = reinterpret_cast<float2*>(smem4);            // [2][TT][CB] (s, s u)
+    float* gg = reinterpret_cast<float*>(dd + 2 * QQ);        // [2][TT][CB] g
+    float* bc = gg + 2 * QQ;                                  // [2] of B, C [TT][NP]
+    float* sums = bc + 2 * BC;                                // [2] of sum_n C h, sum_n A2 q, sum_n e B [TT][YS]
+    float* parts = sums + 2 * SB;                             // [PARTS][W][TT][2][NP]
+    float* acc = parts + Tile::PARTS * PB;                    // [TT][2][NP]
+    float4* carry4 = reinterpret_cast<float4*>(acc + TT * 2 * NP);   // [sets][SCAN]
+    float4* dA4 = carry4 + a.sets * SETS_TH;
+    float4* A24 = dA4 + a.sets * SETS_TH;
+    float* chan = reinterpret_cast<float*>(A24 + a.sets * SETS_TH);  // [sets][8][HELP]: dDskip, ddelta_bias of the helper's four channels
+    T* raw = reinterpret_cast<T*>(chan + a.sets * 8 * HT);           // [RAWS] of u, delta, z, dy [TT][CB], B, C [TT][NP]
 
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned bx = blockIdx.x;
     const int cb = (int)(bx % a.blocks_group);
     bx /= a.blocks_group;
@@ -82,131 +83,75 @@ __global__ void __launch_bounds__(128) scan_bwd_kernel(const ScanBwdArgs<T> a)
     const int len = sequence_length(a.lengths, (int)b, a.L);
     const int t_begin = seg * a.seg_rows, t_end = min(t_begin + a.seg_rows, a.L), live = min(t_end, len);
     const long long row0 = b * a.L;
-    const int ch = warp * CL + lane / NL, n0 = (lane % NL) * kSpt, NQ = round4(a.N);
-    const int cks = (a.L + TT - 1) / TT;
-    const int sets = min(a.sets, (a.E - cb * CB * a.sets + CB - 1) / CB);    // of this block, at least one
-    const int pk = (tid % PPR) * V, prow = tid / PPR;
+    const int NQ = round4(a.N), cks = (a.L + TT - 1) / TT;
+    const int c_base = cb * CB * a.sets, sets = min(a.sets, (a.E - c_base + CB - 1) / CB);      // at least one
+    const int tiles = live > t_begin ? (live - t_begin + TT - 1) / TT : 0, jobs = tiles * sets;
+    // job k: set k % sets of the tile tiles - 1 - k / sets
+    float* per_channel = a.per_channel + ((size_t)b * a.segs + seg) * channel_floats(a.D, NQ);
 
-    for (int set = 0; set < sets; ++set) {
-        const int c0 = (cb * a.sets + set) * CB, d = g * a.E + c0 + ch;
-        const bool mine = c0 + ch < a.E;
-        float av[kSpt], cv[kSpt];
-#pragma unroll
-        for (int i = 0; i < kSpt; ++i) {
-            const bool real = mine && n0 + i < a.N;
-            av[i] = real ? a.A[(size_t)d * a.N + n0 + i] * kLog2e : 0.f;
-            cv[i] = 0.f;
-            if (real && a.segs > 1) cv[i] = a.local[(((size_t)b * a.segs + seg) * a.D + d) * NQ + n0 + i];
-            else if (real && a.dstate_out) cv[i] = a.dstate_out[((size_t)b * a.D + d) * a.N + n0 + i];
-        }
-        A24[set * TH + tid] = make_float4(av[0], av[1], av[2], av[3]);
-        carry4[set * TH + tid] = make_float4(cv[0], cv[1], cv[2], cv[3]);
-        dA4[set * TH + tid] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int i = 0; i < 2 * V; ++i) chan[(set * 2 * V + i) * TH + tid] = 0.f;
-    }
-    for (int i = tid; i < TT * 2 * NP; i += TH) acc[i] = 0.f;
-
-    Pack<T, V> pu[PK], pd[PK], pz[PK], pg[PK];
-    T pb[BK], pc[BK];
-    auto fetch = [&](int t0, int set) {
-        const int c = (cb * a.sets + set) * CB + pk, d = g * a.E + c;
-#pragma unroll
-        for (int i = 0; i < PK; ++i) {
-            const int r = prow + i * RS, t = t0 + r;
-            const bool real = c < a.E && r < TT && t < live;
-            const long long row = row0 + t;
-            pu[i] = real ? load_pack<T, V>(a.u + row * a.ldu + d) : zero_pack<T, V>();
-            pd[i] = real ? load_pack<T, V>(a.delta + row * a.lddelta + d) : zero_pack<T, V>();
-            pg[i] = real ? load_pack<T, V>(a.dy + row * a.lddy + d) : zero_pack<T, V>();
-            pz[i] = real && a.z ? load_pack<T, V>(a.z + row * a.ldz + d) : zero_pack<T, V>();
-        }
-        if (set == 0) {
-#pragma unroll
-            for (int i = 0; i < BK; ++i) {
-                const int e = tid + i * TH, t = t0 + e / NP, n = e % NP;
-                const bool real = e < TT * NP && n < a.N && t < live;
-                pb[i] = real ? a.Bm[(row0 + t) * a.ldB + g * a.N + n] : from_float<T>(0.f);
-                pc[i] = real ? a.Cm[(row0 + t) * a.ldC + g * a.N + n] : from_float<T>(0.f);
-            }
-        }
-    };
-
-    const int tiles = live > t_begin ? (live - t_begin + TT - 1) / TT : 0;
-    if (tiles) fetch(t_begin + (tiles - 1) * TT, 0);
-    for (int tile = tiles - 1; tile >= 0; --tile) {
-        const int t0 = t_begin + tile * TT;
+    if (warp < W) {                                           // ---- the scanning warps
+        const int tid = threadIdx.x, chl = warp * CL + lane % CL, n0 = lane / CL * kSpt;
         for (int set = 0; set < sets; ++set) {
-            const int c0 = (cb * a.sets + set) * CB;
-            const bool pk_real = c0 + pk < a.E;
-            Pack<T, V> cu[PK], cd[PK], cz[PK], cg[PK];
+            const int c = c_base + set * CB + chl, d = g * a.E + c;
+            float av[kSpt], cv[kSpt];
 #pragma unroll
-            for (int i = 0; i < PK; ++i) {
-                const int r = prow + i * RS;
-                cu[i] = pu[i], cd[i] = pd[i], cz[i] = pz[i], cg[i] = pg[i];
-                if (TT * PPR % TH != 0 && r >= TT) continue;
-                float u[V], s[V], z[V], dy[V];
-                unpack(pu[i], u);
-                unpack(pd[i], s);
-                unpack(pz[i], z);
-                unpack(pg[i], dy);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    if (a.delta_bias && pk_real) s[j] += a.delta_bias[g * a.E + c0 + pk + j];
-                    if (a.softplus) s[j] = softplus(s[j]);
-                    if (t0 + r >= live || !pk_real) s[j] = 0.f;
-                    const float gate = a.z ? dy[j] * z[j] * sigmoid(z[j]) : dy[j];
-                    q4[r * CB + pk + j] = make_float4(s[j], s[j] * u[j], gate, 0.f);
-                }
+            for (int i = 0; i < kSpt; ++i) {
+                const bool real = c < a.E && n0 + i < a.N;
+                av[i] = real ? a.A[(size_t)d * a.N + n0 + i] * kLog2e : 0.f;
+                cv[i] = 0.f;
+                if (real && a.segs > 1) cv[i] = a.local[(((size_t)b * a.segs + seg) * a.D + d) * NQ + n0 + i];
+                else if (real && a.dstate_out) cv[i] = a.dstate_out[((size_t)b * a.D + d) * a.N + n0 + i];
             }
-            if (set == 0) {
-#pragma unroll
-                for (int i = 0; i < BK; ++i) {
-                    const int e = tid + i * TH;
-                    if (TT * NP % TH != 0 && e >= TT * NP) continue;
-                    Bs[e] = to_float(pb[i]);
-                    Cs[e] = to_float(pc[i]);
-                }
-            }
-            __syncthreads();
-            if (set + 1 < sets) fetch(t0, set + 1);
-            else if (tile > 0) fetch(t0 - TT, 0);
-
-            const int d = g * a.E + c0 + ch;
-            const bool mine = c0 + ch < a.E;
-            const float4 A4 = A24[set * TH + tid];
+            A24[set * SETS_TH + tid] = make_float4(av[0], av[1], av[2], av[3]);
+            carry4[set * SETS_TH + tid] = make_float4(cv[0], cv[1], cv[2], cv[3]);
+            dA4[set * SETS_TH + tid] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        float4 kept = make_float4(0.f, 0.f, 0.f, 0.f);        // the state that the forward pass kept, loaded one job ahead
+        auto load_kept = [&](int tile, int set) {
+            const int c = c_base + set * CB + chl, d = g * a.E + c;
+            if (c < a.E && n0 < NQ) kept = *reinterpret_cast<const float4*>(a.states + (((size_t)b * cks + t_begin / TT + tile) * a.D + d) * NQ + n0);
+            else kept = make_float4(0.f, 0.f, 0.f, 0.f);
+        };
+        if (jobs) load_kept(tiles - 1, 0);
+        int tile = tiles - 1, set = 0;
+        __syncthreads();                                      // job 0 is there
+#pragma unroll 1
+        for (int k = 0; k < jobs; ++k) {
+            const float4 A4 = A24[set * SETS_TH + tid];
             const float2 A2[2] = {make_float2(A4.x, A4.y), make_float2(A4.z, A4.w)};
-            float4 h4 = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (mine && n0 < NQ) h4 = *reinterpret_cast<const float4*>(a.states + (((size_t)b * cks + t0 / TT) * a.D + d) * NQ + n0);
-            const float2 h0[2] = {make_float2(h4.x, h4.y), make_float2(h4.z, h4.w)};
-            float2 ea[TT][2], h[TT][2];
+            const float2 h0[2] = {make_float2(kept.x, kept.y), make_float2(kept.z, kept.w)};
+            const int next_set = set + 1 < sets ? set + 1 : 0, next_tile = next_set ? tile : tile - 1;
+            if (k + 1 < jobs) load_kept(next_tile, next_set);
+            const float2* sp = dd + (k & 1) * QQ + chl;
+            const float* gp = gg + (k & 1) * QQ + chl;
+            const float *Bp = bc + (tile & 1) * BC + n0, *Cp = Bp + TT * NP;
+            float *vs = sums + (k & 1) * SB + chl, *s1 = vs + TT * YS, *s2 = s1 + TT * YS;
+            float* pp = parts + (Tile::PARTS > 1 ? (k & 1) * PB : 0) + warp * TT * 2 * NP + n0;
+            float2 h[TT][2];
 #pragma unroll
             for (int tq = 0; tq < TT; tq += 4) {
                 float v[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int t = tq + j;
-                    const float4 q = q4[t * CB + ch];
-                    const float4 bv = *reinterpret_cast<const float4*>(Bs + t * NP + n0), cv = *reinterpret_cast<const float4*>(Cs + t * NP + n0);
-                    const float2 s_2 = make_float2(q.x, q.x), su2 = make_float2(q.y, q.y);
+                    const float2 q = sp[t * CB];
+                    const float4 bv = *reinterpret_cast<const float4*>(Bp + t * NP), cv = *reinterpret_cast<const float4*>(Cp + t * NP);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float2 e = __fmul2_rn(s_2, A2[i]);
-                        e.x = ex2(e.x), e.y = ex2(e.y);
-                        ea[t][i] = e;
-                        h[t][i] = __ffma2_rn(e, t ? h[t - 1][i] : h0[i], __fmul2_rn(su2, i ? make_float2(bv.z, bv.w) : make_float2(bv.x, bv.y)));
-                    }
+                    for (int i = 0; i < 2; ++i)
+                        h[t][i] = __ffma2_rn(decay(both(q.x), A2[i]), t ? h[t - 1][i] : h0[i],
+                                             __fmul2_rn(both(q.y), i ? make_float2(bv.z, bv.w) : make_float2(bv.x, bv.y)));
                     const float2 o = __ffma2_rn(h[t][1], make_float2(cv.z, cv.w), __fmul2_rn(h[t][0], make_float2(cv.x, cv.y)));
                     v[j] = o.x + o.y;
                 }
                 constexpr int left = NL >= 4 ? 1 : 4 / NL;
-                const int first = sum_over_lanes<4, NL, 1>(v, lane);
-                if (first_of_equals<4, NL, 1>(lane)) {
+                const int first = sum_over_lanes<4, NL, CL>(v, lane);
+                if (first_of_equals<4, NL, CL>(lane)) {
 #pragma unroll
-                    for (int j = 0; j < left; ++j) vs[(tq + first + j) * YS + ch] = v[j];
+                    for (int j = 0; j < left; ++j) vs[(tq + first + j) * YS] = v[j];
                 }
             }
-            const float4 c4 = carry4[set * TH + tid], w4 = dA4[set * TH + tid];
+            if (Tile::PARTS == 1) __syncthreads();            // (the helpers have added the last job's sums)
+            const float4 c4 = carry4[set * SETS_TH + tid], w4 = dA4[set * SETS_TH + tid];
             float2 carry[2] = {make_float2(c4.x, c4.y), make_float2(c4.z, c4.w)}, dA[2] = {make_float2(w4.x, w4.y), make_float2(w4.z, w4.w)};
 #pragma unroll
             for (int tq = TT - 4; tq >= 0; tq -= 4) {
@@ -214,134 +159,251 @@ __global__ void __launch_bounds__(128) scan_bwd_kernel(const ScanBwdArgs<T> a)
 #pragma unroll
                 for (int j = 3; j >= 0; --j) {
                     const int t = tq + j;
-                    const float4 q = q4[t * CB + ch];
-                    const float4 bv = *reinterpret_cast<const float4*>(Bs + t * NP + n0), cv = *reinterpret_cast<const float4*>(Cs + t * NP + n0);
-                    const float2 s_2 = make_float2(q.x, q.x), su2 = make_float2(q.y, q.y), g2 = make_float2(q.z, q.z);
-                    float2 Aq = make_float2(0.f, 0.f), eB = make_float2(0.f, 0.f);
+                    const float2 q = sp[t * CB];
+                    const float4 bv = *reinterpret_cast<const float4*>(Bp + t * NP), cv = *reinterpret_cast<const float4*>(Cp + t * NP);
+                    const float2 s_2 = both(q.x), su2 = both(q.y), g2 = both(gp[t * CB]);
+                    float2 Aq, eB;
                     float d_sums[8];                          // e s u, then g h, of the four states
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const float2 e = __ffma2_rn(i ? make_float2(cv.z, cv.w) : make_float2(cv.x, cv.y), g2, carry[i]);
-                        const float2 qq = __fmul2_rn(e, __fmul2_rn(ea[t][i], t ? h[t - 1][i] : h0[i]));
+                        carry[i] = __fmul2_rn(decay_again(s_2, A2[i]), e);
+                        const float2 qq = __fmul2_rn(carry[i], t ? h[t - 1][i] : h0[i]), bi = i ? make_float2(bv.z, bv.w) : make_float2(bv.x, bv.y);
                         dA[i] = __ffma2_rn(s_2, qq, dA[i]);
-                        Aq = __ffma2_rn(A2[i], qq, Aq);
-                        eB = __ffma2_rn(e, i ? make_float2(bv.z, bv.w) : make_float2(bv.x, bv.y), eB);
+                        Aq = i ? __ffma2_rn(A2[i], qq, Aq) : __fmul2_rn(A2[i], qq);
+                        eB = i ? __ffma2_rn(e, bi, eB) : __fmul2_rn(e, bi);
                         const float2 db = __fmul2_rn(e, su2), dc = __fmul2_rn(g2, h[t][i]);
                         d_sums[2 * i] = db.x, d_sums[2 * i + 1] = db.y, d_sums[4 + 2 * i] = dc.x, d_sums[5 + 2 * i] = dc.y;
-                        carry[i] = __fmul2_rn(ea[t][i], e);
                     }
                     n_sums[j] = Aq.x + Aq.y;
                     n_sums[4 + j] = eB.x + eB.y;
                     constexpr int left = CL >= 8 ? 1 : 8 / CL;
-                    const int first = sum_over_lanes<8, CL, NL>(d_sums, lane);
-                    if (first_of_equals<8, CL, NL>(lane)) {
+                    const int first = sum_over_lanes<8, CL, 1>(d_sums, lane);
+                    if (first_of_equals<8, CL, 1>(lane)) {
 #pragma unroll
-                        for (int k = 0; k < left; ++k) {
-                            const int id = first + k;
-                            parts[((warp * TT + t) * 2 + (id >> 2)) * NP + n0 + (id & 3)] = d_sums[k];
-                        }
+                        for (int i = 0; i < left; ++i) pp[(t * 2 + ((first + i) >> 2)) * NP + ((first + i) & 3)] = d_sums[i];
                     }
                 }
                 constexpr int left = NL >= 8 ? 1 : 8 / NL;
-                const int first = sum_over_lanes<8, NL, 1>(n_sums, lane);
-                if (first_of_equals<8, NL, 1>(lane)) {
+                const int first = sum_over_lanes<8, NL, CL>(n_sums, lane);
+                if (first_of_equals<8, NL, CL>(lane)) {
 #pragma unroll
-                    for (int k = 0; k < left; ++k) {
-                        const int id = first + k;
-                        (id >> 2 ? s2 : s1)[(tq + (id & 3)) * YS + ch] = n_sums[k];
+                    for (int i = 0; i < left; ++i) {
+                        const int id = first + i;
+                        (id >> 2 ? s2 : s1)[(tq + (id & 3)) * YS] = n_sums[i];
                     }
                 }
             }
-            carry4[set * TH + tid] = make_float4(carry[0].x, carry[0].y, carry[1].x, carry[1].y);
-            dA4[set * TH + tid] = make_float4(dA[0].x, dA[0].y, dA[1].x, dA[1].y);
+            carry4[set * SETS_TH + tid] = make_float4(carry[0].x, carry[0].y, carry[1].x, carry[1].y);
+            dA4[set * SETS_TH + tid] = make_float4(dA[0].x, dA[0].y, dA[1].x, dA[1].y);
+            set = next_set, tile = next_tile;
             __syncthreads();
+        }
+        for (int set = 0; set < sets; ++set) {
+            const int c = c_base + set * CB + chl, d = g * a.E + c;
+            if (c >= a.E) continue;
+            if (n0 < NQ) *reinterpret_cast<float4*>(per_channel + (size_t)d * NQ + n0) = dA4[set * SETS_TH + tid];
+            if (a.dstate_in && a.segs == 1) {
+                const float4 c4 = carry4[set * SETS_TH + tid];
+                const float cv[kSpt] = {c4.x, c4.y, c4.z, c4.w};
+#pragma unroll
+                for (int i = 0; i < kSpt; ++i)
+                    if (n0 + i < a.N) a.dstate_in[((size_t)b * a.D + d) * a.N + n0 + i] = cv[i];
+            }
+        }
+        return;
+    }
 
-            float sum_d[V] = {}, sum_b[V] = {};
+    // ---- the helping warps: four adjacent channels of a row at a time, the same of every set
+    const int tid = threadIdx.x - Tile::SCAN, uc = tid % (CB / 4) * 4, ur = tid / (CB / 4);
+    for (int i = tid; i < sets * 8 * HT; i += HT) chan[i] = 0.f;
+    for (int i = tid; i < TT * 2 * NP; i += HT) acc[i] = 0.f;
+    auto fetch = [&](int k) {
+        if (k < jobs) {
+            const int tile = tiles - 1 - k / sets, set = k % sets;
+            T* p = raw + k % RAWS * RAW;
+            const int c0 = c_base + set * CB, nch = min(CB, a.E - c0), d0 = g * a.E + c0, rows = live - t_begin - tile * TT;
+            const long long row = row0 + t_begin + tile * TT;
+            copy_tile<TT, CB * ES, HT>(p, a.u + row * a.ldu + d0, a.ldu * ES, rows, nch * ES, a.u_unit, tid);
+            copy_tile<TT, CB * ES, HT>(p + QQ, a.delta + row * a.lddelta + d0, a.lddelta * ES, rows, nch * ES, a.delta_unit, tid);
+            if (a.z) copy_tile<TT, CB * ES, HT>(p + 2 * QQ, a.z + row * a.ldz + d0, a.ldz * ES, rows, nch * ES, a.z_unit, tid);
+            copy_tile<TT, CB * ES, HT>(p + 3 * QQ, a.dy + row * a.lddy + d0, a.lddy * ES, rows, nch * ES, a.dy_unit, tid);
+            if (set == 0) {
+                copy_tile<TT, NP * ES, HT>(p + 4 * QQ, a.Bm + row * a.ldB + (long long)g * a.N, a.ldB * ES, rows, a.N * ES, a.B_unit, tid);
+                copy_tile<TT, NP * ES, HT>(p + 4 * QQ + TT * NP, a.Cm + row * a.ldC + (long long)g * a.N, a.ldC * ES, rows, a.N * ES, a.C_unit, tid);
+            }
+        }
+        copies_commit();
+    };
+    auto convert = [&](int k) {
+        const int tile = tiles - 1 - k / sets, set = k % sets, c0 = c_base + set * CB, rows = live - t_begin - tile * TT;
+        const T* rw = raw + k % RAWS * RAW;
 #pragma unroll
-            for (int i = 0; i < PK; ++i) {
-                const int r = prow + i * RS;
-                if (!pk_real || r >= TT || t0 + r >= live) continue;
-                float u[V], raw[V], z[V], dy[V], du[V], dd[V], dz[V];
-                unpack(cu[i], u);
-                unpack(cd[i], raw);
-                unpack(cz[i], z);
-                unpack(cg[i], dy);
+        for (int i = 0; i < UK; ++i) {
+            const int r = ur + i * UROWS;
+            if (UNITS % HT != 0 && r >= TT) continue;
+            float u[4], s[4], gr[4];
+            load4(rw + r * CB + uc, u);
+            load4(rw + QQ + r * CB + uc, s);
+            load4(rw + 3 * QQ + r * CB + uc, gr);
+            float2 s2[2], g2[2] = {make_float2(gr[0], gr[1]), make_float2(gr[2], gr[3])};
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const int c = g * a.E + c0 + pk + j, at = r * YS + pk + j;
-                    const float4 q = q4[r * CB + pk + j];
-                    const float skip = a.Dskip ? a.Dskip[c] : 0.f;
-                    du[j] = fmaf(q.x, s2[at], skip * q.z);
-                    dd[j] = fmaf(kLn2, s1[at], u[j] * s2[at]);
-                    if (a.softplus) dd[j] *= sigmoid(a.delta_bias ? raw[j] + a.delta_bias[c] : raw[j]);
-                    if (a.z) {
-                        const float sg = sigmoid(z[j]);
-                        dz[j] = dy[j] * fmaf(skip, u[j], vs[at]) * sg * fmaf(z[j], 1.f - sg, 1.f);
-                    }
-                    sum_d[j] = fmaf(q.z, u[j], sum_d[j]);
-                    sum_b[j] += dd[j];
+            for (int j = 0; j < 4; ++j)
+                if (a.delta_bias && c0 + uc + j < a.E) s[j] += a.delta_bias[g * a.E + c0 + uc + j];
+            s2[0] = make_float2(s[0], s[1]), s2[1] = make_float2(s[2], s[3]);
+            if (a.softplus) s2[0] = softplus(s2[0]), s2[1] = softplus(s2[1]);
+            if (r >= rows) s2[0] = s2[1] = both(0.f);
+            if (a.z) {
+                float z[4];
+                load4(rw + 2 * QQ + r * CB + uc, z);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float2 zz = make_float2(z[2 * j], z[2 * j + 1]);
+                    g2[j] = __fmul2_rn(g2[j], __fmul2_rn(zz, sigmoid(zz)));
                 }
-                const long long row = row0 + t0 + r;
-                store_pack(a.du + row * a.lddu + g * a.E + c0 + pk, pack<T, V>(du));
-                store_pack(a.ddelta + row * a.ldddelta + g * a.E + c0 + pk, pack<T, V>(dd));
-                if (a.z) store_pack(a.dz + row * a.lddz + g * a.E + c0 + pk, pack<T, V>(dz));
             }
+            const float sv[4] = {s2[0].x, s2[0].y, s2[1].x, s2[1].y}, gv[4] = {g2[0].x, g2[0].y, g2[1].x, g2[1].y};
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                chan[((set * 2) * V + j) * TH + tid] += sum_d[j];
-                chan[((set * 2 + 1) * V + j) * TH + tid] += sum_b[j];
+            for (int j = 0; j < 4; ++j) {
+                const float sj = c0 + uc + j < a.E ? sv[j] : 0.f;
+                dd[(k & 1) * QQ + r * CB + uc + j] = make_float2(sj, sj * u[j]);
             }
-            const bool out = set == sets - 1;
-            for (int i = tid; i < TT * 2 * NP; i += TH) {
-                float s = acc[i];
+            *reinterpret_cast<float4*>(gg + (k & 1) * QQ + r * CB + uc) = make_float4(gv[0], gv[1], gv[2], gv[3]);
+        }
+        if (set == 0) {
+            float* to = bc + (tile & 1) * BC;
 #pragma unroll
-                for (int w = 0; w < W; ++w) s += parts[w * TT * 2 * NP + i];
-                acc[i] = out ? 0.f : s;
-                const int t = t0 + i / (2 * NP);
-                if (out && t < live)
-                    a.per_row[((((size_t)g * a.blocks_group + cb) * a.B * a.L) + row0 + t) * (2 * NP) + i % (2 * NP)] = s;
+            for (int i = 0; i < BK; ++i) {
+                const int e = (tid + i * HT) * 4;
+                if (BUNITS % HT != 0 && e >= TT * NP) continue;
+                float v[4];
+                load4(rw + 4 * QQ + e, v);
+                *reinterpret_cast<float4*>(to + e) = make_float4(v[0], v[1], v[2], v[3]);
+                load4(rw + 4 * QQ + TT * NP + e, v);
+                *reinterpret_cast<float4*>(to + TT * NP + e) = make_float4(v[0], v[1], v[2], v[3]);
             }
         }
-    }
-
-    // rows of padding, and what a block has summed over its rows
-    for (int set = 0; set < sets; ++set) {
-        const int c0 = (cb * a.sets + set) * CB, d = g * a.E + c0 + ch;
-        if (c0 + pk < a.E) {
-            for (int t = max(t_begin, live) + prow; t < t_end; t += RS) {
-                const long long row = row0 + t;
-                store_pack(a.du + row * a.lddu + g * a.E + c0 + pk, zero_pack<T, V>());
-                store_pack(a.ddelta + row * a.ldddelta + g * a.E + c0 + pk, zero_pack<T, V>());
-                if (a.z) store_pack(a.dz + row * a.lddz + g * a.E + c0 + pk, zero_pack<T, V>());
+    };
+    auto add_parts = [&](int k) {
+        const int tile = tiles - 1 - k / sets, set = k % sets, t0 = t_begin + tile * TT;
+        const float* pp = parts + (Tile::PARTS > 1 ? (k & 1) * PB : 0);
+        const bool out = set == sets - 1;
+        float* to = a.per_row + ((((size_t)g * a.blocks_group + cb) * a.B * a.L) + row0 + t0) * (2 * NP);
+        for (int i = tid; i < TT * 2 * NP; i += HT) {
+            float s = acc[i];
+#pragma unroll
+            for (int w = 0; w < W; ++w) s += pp[w * TT * 2 * NP + i];
+            acc[i] = out ? 0.f : s;
+            if (out && t0 + i / (2 * NP) < live) to[i] = s;
+        }
+    };
+    auto finish = [&](int k) {
+        const int tile = tiles - 1 - k / sets, set = k % sets, c0 = c_base + set * CB, rows = live - t_begin - tile * TT, nch = a.E - c0;
+        const T* rw = raw + k % RAWS * RAW;
+        const float *vs = sums + (k & 1) * SB, *s1 = vs + TT * YS, *s2 = s1 + TT * YS;
+        float* mine = chan + set * 8 * HT + tid;
+#pragma unroll
+        for (int i = 0; i < UK; ++i) {
+            const int r = ur + i * UROWS;
+            if (uc >= nch || r >= TT || r >= rows) continue;
+            float u[4], rd[4], gy[4], du[4], ds[4];
+            load4(rw + r * CB + uc, u);
+            load4(rw + QQ + r * CB + uc, rd);
+            load4(rw + 3 * QQ + r * CB + uc, gy);
+            const float4 v4 = *reinterpret_cast<const float4*>(vs + r * YS + uc), a4 = *reinterpret_cast<const float4*>(s1 + r * YS + uc),
+                         e4 = *reinterpret_cast<const float4*>(s2 + r * YS + uc);
+            const float v[4] = {v4.x, v4.y, v4.z, v4.w}, sa[4] = {a4.x, a4.y, a4.z, a4.w}, se[4] = {e4.x, e4.y, e4.z, e4.w};
+            const long long row = row0 + t_begin + tile * TT + r;
+            const int d0 = g * a.E + c0 + uc;
+            float skip[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool real = uc + j < nch;
+                skip[j] = a.Dskip && real ? a.Dskip[d0 + j] : 0.f;
+                const float bias = a.delta_bias && real ? a.delta_bias[d0 + j] : 0.f;
+                const float sj = dd[(k & 1) * QQ + r * CB + uc + j].x, gj = gg[(k & 1) * QQ + r * CB + uc + j];
+                du[j] = fmaf(sj, se[j], skip[j] * gj);
+                ds[j] = fmaf(kLn2, sa[j], u[j] * se[j]);
+                if (a.softplus) ds[j] *= sigmoid(rd[j] + bias);
+                mine[j * HT] = fmaf(gj, u[j], mine[j * HT]);
+                mine[(4 + j) * HT] += ds[j];
+            }
+            T* to_u = a.du + row * a.lddu + d0;
+            T* to_d = a.ddelta + row * a.ldddelta + d0;
+            if (a.out_quads) {
+                store_pack(to_u, pack<T, 4>(du));
+                store_pack(to_d, pack<T, 4>(ds));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (uc + j < nch) to_u[j] = from_float<T>(du[j]), to_d[j] = from_float<T>(ds[j]);
+            }
+            if (a.z) {
+                float z[4];
+                load4(rw + 2 * QQ + r * CB + uc, z);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float sg = sigmoid(z[j]);
+                    z[j] = gy[j] * fmaf(skip[j], u[j], v[j]) * sg * fmaf(z[j], 1.f - sg, 1.f);
+                }
+                T* to_z = a.dz + row * a.lddz + d0;
+                if (a.out_quads) {
+                    store_pack(to_z, pack<T, 4>(z));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (uc + j < nch) to_z[j] = from_float<T>(z[j]);
+                }
             }
         }
-        float* out = a.per_channel + ((size_t)b * a.segs + seg) * channel_floats(a.D, NQ);
-        if (c0 + ch < a.E && n0 < NQ) *reinterpret_cast<float4*>(out + (size_t)d * NQ + n0) = dA4[set * TH + tid];
-        if (a.dstate_in && a.segs == 1 && c0 + ch < a.E) {
-            const float4 c4 = carry4[set * TH + tid];
-            const float cv[kSpt] = {c4.x, c4.y, c4.z, c4.w};
-#pragma unroll
-            for (int i = 0; i < kSpt; ++i)
-                if (n0 + i < a.N) a.dstate_in[((size_t)b * a.D + d) * a.N + n0 + i] = cv[i];
-        }
-    }
+    };
+    fetch(0);
+    fetch(1);
+    fetch(2);
+    copies_wait<2>();
+    helpers_sync<HT>();                                       // (every helper's copies have arrived)
+    if (jobs) convert(0);
     __syncthreads();
-    for (int i = tid; i < sets * 2 * CB; i += TH) {
-        const int c = i % CB, which = i / CB % 2, set = i / (2 * CB), cc = (cb * a.sets + set) * CB + c;
+    for (int k = 0; k < jobs; ++k) {
+        if (k > 0) add_parts(k - 1);
+        if (Tile::PARTS == 1) __syncthreads();
+        // the buffer of job k + 3 is that of job k - 1, which `finish` still reads, as it does the (s, s u) and g that job k + 1 replaces
+        if (k > 0) finish(k - 1);
+        copies_wait<1>();
+        helpers_sync<HT>();
+        fetch(k + 3);
+        if (k + 1 < jobs) convert(k + 1);
+        __syncthreads();
+    }
+    if (jobs) {
+        add_parts(jobs - 1);
+        finish(jobs - 1);
+    }
+    for (int set = 0; set < sets; ++set) {                    // rows of padding
+        const int c = c_base + set * CB + uc;
+        for (int t = max(t_begin, live) + ur; t < t_end; t += UROWS)
+            for (int j = 0; j < 4 && c + j < a.E; ++j) {
+                const long long row = row0 + t;
+                a.du[row * a.lddu + g * a.E + c + j] = a.ddelta[row * a.ldddelta + g * a.E + c + j] = from_float<T>(0.f);
+                if (a.z) a.dz[row * a.lddz + g * a.E + c + j] = from_float<T>(0.f);
+            }
+    }
+    helpers_sync<HT>();
+    for (int i = tid; i < sets * 2 * CB; i += HT) {
+        const int c = i % CB, which = i / CB % 2, set = i / (2 * CB), cc = c_base + set * CB + c;
         if (cc >= a.E) continue;
         float s = 0.f;
-        for (int r = 0; r < RS; ++r) s += chan[((set * 2 + which) * V + c % V) * TH + r * PPR + c / V];
-        float* out = a.per_channel + ((size_t)b * a.segs + seg) * channel_floats(a.D, NQ) + (size_t)a.D * NQ;
-        out[(size_t)which * a.D + g * a.E + cc] = s;
+        for (int r = 0; r < UROWS; ++r) s += chan[(set * 8 + which * 4 + c % 4) * HT + r * (CB / 4) + c / 4];
+        per_channel[(size_t)a.D * NQ + (size_t)which * a.D + g * a.E + cc] = s;
     }
 }
 
 // What a segment hands to the one before it when it is walked from zero: carry <- a_t (C_t g_t + carry), and the sum of its steps.
 template <typename T, int NL, int V>
-__global__ void __launch_bounds__(128) scan_bwd_carry_kernel(const ScanBwdArgs<T> a, int blocks_group)
+__global__ void __launch_bounds__(ScanBwdTile<NL>::SCAN) scan_bwd_carry_kernel(const ScanBwdArgs<T> a, int blocks_group)
 {
     using Tile = ScanBwdTile<NL>;
-    constexpr int TH = Tile::TH, CL = Tile::CL, CB = Tile::CB, NP = Tile::NP, TT = Tile::TT;
+    constexpr int TH = Tile::SCAN, CL = Tile::CL, CB = Tile::CB, NP = Tile::NP, TT = Tile::TT;
     constexpr int PPR = CB / V, PK = (TT * PPR + TH - 1) / TH, BK = (TT * NP + TH - 1) / TH, RS = TH / PPR;
     ptx::grid_dep_wait();
     __shared__ __align__(16) float2 sg[TT * CB];
@@ -357,7 +419,7 @@ __global__ void __launch_bounds__(128) scan_bwd_carry_kernel(const ScanBwdArgs<T
     const int len = sequence_length(a.lengths, (int)b, a.L);
     const int t_begin = seg * a.seg_rows, live = min(min(t_begin + a.seg_rows, a.L), len);
     const long long row0 = b * a.L;
-    const int ch = warp * CL + lane / NL, n0 = (lane % NL) * kSpt, NQ = round4(a.N), d = g * a.E + c0 + ch;
+    const int ch = warp * CL + lane % CL, n0 = lane / CL * kSpt, NQ = round4(a.N), d = g * a.E + c0 + ch;
     const bool mine = c0 + ch < a.E;
     const int pk = (tid % PPR) * V, prow = tid / PPR;
     const bool pk_real = c0 + pk < a.E;
@@ -420,9 +482,8 @@ __global__ void __launch_bounds__(128) scan_bwd_carry_kernel(const ScanBwdArgs<T
             const float2 q = sg[t * CB + ch];
             const float4 cv = *reinterpret_cast<const float4*>(Cs + t * NP + n0);
             const float2 s_2 = make_float2(q.x, q.x), g2 = make_float2(q.y, q.y);
-            float2 e0 = __fmul2_rn(s_2, A2[0]), e1 = __fmul2_rn(s_2, A2[1]);
-            e0.x = ex2(e0.x), e0.y = ex2(e0.y), e1.x = ex2(e1.x), e1.y = ex2(e1.y);
-            carry[0] = __fmul2_rn(e0, __ffma2_rn(make_float2(cv.x, cv.y), g2, carry[0]));
+            const float2 e0 = decay(s_2, A2[0]), e1 = decay(s_2, A2[1]);
+                carry[0] = __fmul2_rn(e0, __ffma2_rn(make_float2(cv.x, cv.y), g2, carry[0]));
             carry[1] = __fmul2_rn(e1, __ffma2_rn(make_float2(cv.z, cv.w), g2, carry[1]));
             steps += q.x;
         }

@@ -21,6 +21,14 @@ __device__ __forceinline__ float2 decay(float2 s, float2 A2)
     const float2 e = __ffma2_rn(s, A2, both(kExpBias));
     return make_float2(ex2(e.x), ex2(e.y));
 }
+// The same where it has been taken before: not to be kept in a register from there.
+__device__ __forceinline__ float2 decay_again(float2 s, float2 A2)
+{
+    float2 e = __ffma2_rn(s, A2, both(kExpBias));
+    asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+    asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+    return e;
+}
 
 // log(1 + e^v) = max(v, 0) + log(1 + w), w = e^-|v| in (0, 1], and log(1 + w) / w as a polynomial (interpolated at Chebyshev nodes; 3e-8, 2e-7
 // with its roundings), so that small steps keep their digits and one special-function operation does.
