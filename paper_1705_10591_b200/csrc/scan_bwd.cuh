@@ -6,9 +6,10 @@
 //
 // The forward pass keeps the state before every 16th row.  A block walks the tiles of 16 rows from the last to the first; in a tile the
 // states h of all 16 rows are computed again, from the kept one, into registers (a thread has four states of one channel: 64
-// registers; the decays beside them would make it one block an SM, so those are taken twice).  Sums over the states go over the lanes of a channel, sums
-// over the channels (dB, dC) over the other lanes, the warps and the channel sets that the block takes in turn, and from there as one
-// partial sum of the block into the workspace; those are added by a kernel of their own in a fixed order.
+// registers; the decays beside them would make it one block an SM, so those are taken twice).  Sums over the states go over the lanes of a channel.
+// Sums over the channels (dB, dC) are the larger part, eight values a row: two lanes join theirs, one going on with dB and one with dC (going
+// on over all lanes took 32 of 95 instructions a row), and the rest is added through shared memory, over the warps and the channel sets that the block
+// takes in turn, and goes into the workspace as one partial sum of the block; those are added by a kernel of their own in a fixed order.
 // As in the forward pass four helping warps do what is done once per row and channel while the four scanning warps scan: copies, step sizes and
 // gates of the next tile, outputs and sums over the warps of the last one.
 #pragma once
@@ -40,12 +41,12 @@ template <int NL>
 struct ScanBwdTile {
     static constexpr int W = NL == 1 ? 2 : 4, SCAN = 32 * W, HELP = 128, TH = SCAN + HELP, RAWS = 4;
     static constexpr int CL = 32 / NL, CB = W * CL, NP = NL * kSpt, TT = kCheckpointRows, YS = CB + 4;
-    static constexpr int PARTS = NP >= 128 ? 1 : 2;           // buffers of the warps' sums over channels
+    static constexpr int PV = CL > 1 ? 1 : 2;                 // quads of a row that a lane leaves for the sums over channels
     static constexpr size_t raw(size_t esize) { return esize * TT * (4 * CB + 2 * NP); }
     // tiles as they lie in memory; twice (s, s u) and g of a tile, B and C, and three sums over states; the warps' sums over channels, and the block's
     static constexpr size_t fixed(size_t esize)
     {
-        return RAWS * raw(esize) + sizeof(float) * (2 * (3 * TT * CB + 2 * TT * NP + 3 * TT * YS) + PARTS * W * TT * 2 * NP + TT * 2 * NP);
+        return RAWS * raw(esize) + sizeof(float) * (2 * (3 * TT * CB + 2 * TT * NP + 3 * TT * YS) + W * TT * PV * 128 + TT * 2 * NP);
     }
     // of a channel set: the carried gradient, dA and A of every scanning thread, and the helpers' sums for dDskip and ddelta_bias
     static constexpr size_t set_bytes = sizeof(float) * (SCAN * 3 * kSpt + HELP * 8);
@@ -57,16 +58,16 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
     using Tile = ScanBwdTile<NL>;
     constexpr int W = Tile::W, HT = Tile::HELP, CL = Tile::CL, CB = Tile::CB, NP = Tile::NP, TT = Tile::TT, YS = Tile::YS, RAWS = Tile::RAWS, ES = sizeof(T);
     constexpr int UNITS = TT * CB / 4, UK = (UNITS + HT - 1) / HT, UROWS = HT / (CB / 4), BUNITS = TT * NP / 4, BK = (BUNITS + HT - 1) / HT;
-    constexpr int QQ = TT * CB, BC = 2 * TT * NP, SB = 3 * TT * YS, PB = W * TT * 2 * NP, RAW = TT * (4 * CB + 2 * NP), SETS_TH = Tile::SCAN;
+    constexpr int QQ = TT * CB, BC = 2 * TT * NP, SB = 3 * TT * YS, RAW = TT * (4 * CB + 2 * NP), SETS_TH = Tile::SCAN, PV = Tile::PV;
     ptx::grid_dep_wait();
     extern __shared__ float4 smem4[];
     float2* dd = reinterpret_cast<float2*>(smem4);            // [2][TT][CB] (s, s u)
     float* gg = reinterpret_cast<float*>(dd + 2 * QQ);        // [2][TT][CB] g
     float* bc = gg + 2 * QQ;                                  // [2] of B, C [TT][NP]
     float* sums = bc + 2 * BC;                                // [2] of sum_n C h, sum_n A2 q, sum_n e B [TT][YS]
-    float* parts = sums + 2 * SB;                             // [PARTS][W][TT][2][NP]
-    float* acc = parts + Tile::PARTS * PB;                    // [TT][2][NP]
-    float4* carry4 = reinterpret_cast<float4*>(acc + TT * 2 * NP);   // [sets][SCAN]
+    float4* parts = reinterpret_cast<float4*>(sums + 2 * SB); // [W][TT][PV][32]: of four states, dB in the lower channel lanes and dC in the upper
+    float4* acc = parts + W * TT * PV * 32;                   // [TT][2][NP / 4]
+    float4* carry4 = acc + TT * 2 * NP / 4;                   // [sets][SCAN]
     float4* dA4 = carry4 + a.sets * SETS_TH;
     float4* A24 = dA4 + a.sets * SETS_TH;
     float* chan = reinterpret_cast<float*>(A24 + a.sets * SETS_TH);  // [sets][8][HELP]: dDskip, ddelta_bias of the helper's four channels
@@ -126,44 +127,31 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
             const float* gp = gg + (k & 1) * QQ + chl;
             const float *Bp = bc + (tile & 1) * BC + n0, *Cp = Bp + TT * NP;
             float *vs = sums + (k & 1) * SB + chl, *s1 = vs + TT * YS, *s2 = s1 + TT * YS;
-            float* pp = parts + (Tile::PARTS > 1 ? (k & 1) * PB : 0) + warp * TT * 2 * NP + n0;
+            float4* pp = parts + warp * TT * PV * 32 + lane;
             float2 h[TT][2];
 #pragma unroll
-            for (int tq = 0; tq < TT; tq += 4) {
-                float v[4];
+            for (int t = 0; t < TT; ++t) {
+                const float2 q = sp[t * CB];
+                const float4 bv = *reinterpret_cast<const float4*>(Bp + t * NP);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int t = tq + j;
-                    const float2 q = sp[t * CB];
-                    const float4 bv = *reinterpret_cast<const float4*>(Bp + t * NP), cv = *reinterpret_cast<const float4*>(Cp + t * NP);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        h[t][i] = __ffma2_rn(decay(both(q.x), A2[i]), t ? h[t - 1][i] : h0[i],
-                                             __fmul2_rn(both(q.y), i ? make_float2(bv.z, bv.w) : make_float2(bv.x, bv.y)));
-                    const float2 o = __ffma2_rn(h[t][1], make_float2(cv.z, cv.w), __fmul2_rn(h[t][0], make_float2(cv.x, cv.y)));
-                    v[j] = o.x + o.y;
-                }
-                constexpr int left = NL >= 4 ? 1 : 4 / NL;
-                const int first = sum_over_lanes<4, NL, CL>(v, lane);
-                if (first_of_equals<4, NL, CL>(lane)) {
-#pragma unroll
-                    for (int j = 0; j < left; ++j) vs[(tq + first + j) * YS] = v[j];
-                }
+                for (int i = 0; i < 2; ++i)
+                    h[t][i] = __ffma2_rn(decay(both(q.x), A2[i]), t ? h[t - 1][i] : h0[i],
+                                         __fmul2_rn(both(q.y), i ? make_float2(bv.z, bv.w) : make_float2(bv.x, bv.y)));
             }
-            if (Tile::PARTS == 1) __syncthreads();            // (the helpers have added the last job's sums)
+            __syncthreads();                                  // the helpers have added the last job's sums over channels
             const float4 c4 = carry4[set * SETS_TH + tid], w4 = dA4[set * SETS_TH + tid];
             float2 carry[2] = {make_float2(c4.x, c4.y), make_float2(c4.z, c4.w)}, dA[2] = {make_float2(w4.x, w4.y), make_float2(w4.z, w4.w)};
 #pragma unroll
             for (int tq = TT - 4; tq >= 0; tq -= 4) {
-                float n_sums[8];                              // sum_n A2 q of four rows, then sum_n e B
+                float n_sums[8], v[4];                        // sum_n A2 q of four rows, then sum_n e B; sum_n C h
 #pragma unroll
                 for (int j = 3; j >= 0; --j) {
                     const int t = tq + j;
                     const float2 q = sp[t * CB];
                     const float4 bv = *reinterpret_cast<const float4*>(Bp + t * NP), cv = *reinterpret_cast<const float4*>(Cp + t * NP);
                     const float2 s_2 = both(q.x), su2 = both(q.y), g2 = both(gp[t * CB]);
-                    float2 Aq, eB;
-                    float d_sums[8];                          // e s u, then g h, of the four states
+                    float2 Aq, eB, o;
+                    float db[4], dc[4];                       // e s u and g h of the four states
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const float2 e = __ffma2_rn(i ? make_float2(cv.z, cv.w) : make_float2(cv.x, cv.y), g2, carry[i]);
@@ -172,16 +160,30 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
                         dA[i] = __ffma2_rn(s_2, qq, dA[i]);
                         Aq = i ? __ffma2_rn(A2[i], qq, Aq) : __fmul2_rn(A2[i], qq);
                         eB = i ? __ffma2_rn(e, bi, eB) : __fmul2_rn(e, bi);
-                        const float2 db = __fmul2_rn(e, su2), dc = __fmul2_rn(g2, h[t][i]);
-                        d_sums[2 * i] = db.x, d_sums[2 * i + 1] = db.y, d_sums[4 + 2 * i] = dc.x, d_sums[5 + 2 * i] = dc.y;
+                        const float2 x = __fmul2_rn(e, su2), y = __fmul2_rn(g2, h[t][i]), ci = i ? make_float2(cv.z, cv.w) : make_float2(cv.x, cv.y);
+                        o = i ? __ffma2_rn(h[t][i], ci, o) : __fmul2_rn(h[t][i], ci);
+                        db[2 * i] = x.x, db[2 * i + 1] = x.y, dc[2 * i] = y.x, dc[2 * i + 1] = y.y;
                     }
                     n_sums[j] = Aq.x + Aq.y;
                     n_sums[4 + j] = eB.x + eB.y;
-                    constexpr int left = CL >= 8 ? 1 : 8 / CL;
-                    const int first = sum_over_lanes<8, CL, 1>(d_sums, lane);
-                    if (first_of_equals<8, CL, 1>(lane)) {
+                    v[j] = o.x + o.y;
+                    if (CL > 1) {
+                        const bool upper = lane & (CL / 2);
+                        float r[4];
 #pragma unroll
-                        for (int i = 0; i < left; ++i) pp[(t * 2 + ((first + i) >> 2)) * NP + ((first + i) & 3)] = d_sums[i];
+                        for (int i = 0; i < 4; ++i) r[i] = (upper ? dc[i] : db[i]) + __shfl_xor_sync(0xffffffffu, upper ? db[i] : dc[i], CL / 2);
+                        pp[t * 32] = make_float4(r[0], r[1], r[2], r[3]);
+                    } else {
+                        pp[t * 64] = make_float4(db[0], db[1], db[2], db[3]);
+                        pp[t * 64 + 32] = make_float4(dc[0], dc[1], dc[2], dc[3]);
+                    }
+                }
+                {
+                    constexpr int left = NL >= 4 ? 1 : 4 / NL;
+                    const int first = sum_over_lanes<4, NL, CL>(v, lane);
+                    if (first_of_equals<4, NL, CL>(lane)) {
+#pragma unroll
+                        for (int i = 0; i < left; ++i) vs[(tq + first + i) * YS] = v[i];
                     }
                 }
                 constexpr int left = NL >= 8 ? 1 : 8 / NL;
@@ -217,11 +219,26 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
     // ---- the helping warps: four adjacent channels of a row at a time, the same of every set
     const int tid = threadIdx.x - Tile::SCAN, uc = tid % (CB / 4) * 4, ur = tid / (CB / 4);
     for (int i = tid; i < sets * 8 * HT; i += HT) chan[i] = 0.f;
-    for (int i = tid; i < TT * 2 * NP; i += HT) acc[i] = 0.f;
-    auto fetch = [&](int k) {
-        if (k < jobs) {
-            const int tile = tiles - 1 - k / sets, set = k % sets;
-            T* p = raw + k % RAWS * RAW;
+    // job k of each of three streams (copies, conversions, outputs), counted along
+    struct Job { int k, tile, set; };
+    auto next = [&](Job& j) {
+        ++j.k;
+        if (++j.set == sets) j.set = 0, --j.tile;
+    };
+    float bias[4], skip[4], sum_d[4] = {}, sum_b[4] = {};
+    auto params = [&](int set) {                              // of the helper's four channels
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = c_base + set * CB + uc + j;
+            bias[j] = a.delta_bias && c < a.E ? a.delta_bias[g * a.E + c] : 0.f;
+            skip[j] = a.Dskip && c < a.E ? a.Dskip[g * a.E + c] : 0.f;
+        }
+    };
+    params(0);
+    auto fetch = [&](const Job& job) {
+        const int tile = job.tile, set = job.set;
+        if (job.k < jobs) {
+            T* p = raw + job.k % RAWS * RAW;
             const int c0 = c_base + set * CB, nch = min(CB, a.E - c0), d0 = g * a.E + c0, rows = live - t_begin - tile * TT;
             const long long row = row0 + t_begin + tile * TT;
             copy_tile<TT, CB * ES, HT>(p, a.u + row * a.ldu + d0, a.ldu * ES, rows, nch * ES, a.u_unit, tid);
@@ -235,9 +252,10 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
         }
         copies_commit();
     };
-    auto convert = [&](int k) {
-        const int tile = tiles - 1 - k / sets, set = k % sets, c0 = c_base + set * CB, rows = live - t_begin - tile * TT;
+    auto convert = [&](const Job& job) {
+        const int k = job.k, tile = job.tile, set = job.set, c0 = c_base + set * CB, rows = live - t_begin - tile * TT;
         const T* rw = raw + k % RAWS * RAW;
+        if (sets > 1) params(set);
 #pragma unroll
         for (int i = 0; i < UK; ++i) {
             const int r = ur + i * UROWS;
@@ -247,10 +265,7 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
             load4(rw + QQ + r * CB + uc, s);
             load4(rw + 3 * QQ + r * CB + uc, gr);
             float2 s2[2], g2[2] = {make_float2(gr[0], gr[1]), make_float2(gr[2], gr[3])};
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (a.delta_bias && c0 + uc + j < a.E) s[j] += a.delta_bias[g * a.E + c0 + uc + j];
-            s2[0] = make_float2(s[0], s[1]), s2[1] = make_float2(s[2], s[3]);
+            s2[0] = make_float2(s[0] + bias[0], s[1] + bias[1]), s2[1] = make_float2(s[2] + bias[2], s[3] + bias[3]);
             if (a.softplus) s2[0] = softplus(s2[0]), s2[1] = softplus(s2[1]);
             if (r >= rows) s2[0] = s2[1] = both(0.f);
             if (a.z) {
@@ -284,24 +299,44 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
             }
         }
     };
-    auto add_parts = [&](int k) {
-        const int tile = tiles - 1 - k / sets, set = k % sets, t0 = t_begin + tile * TT;
-        const float* pp = parts + (Tile::PARTS > 1 ? (k & 1) * PB : 0);
-        const bool out = set == sets - 1;
-        float* to = a.per_row + ((((size_t)g * a.blocks_group + cb) * a.B * a.L) + row0 + t0) * (2 * NP);
-        for (int i = tid; i < TT * 2 * NP; i += HT) {
-            float s = acc[i];
+    // sums over channels of a job: a thread takes four states of dB or dC of a row, their RL lanes of every warp
+    constexpr int RL = CL > 1 ? CL / 2 : 1, TASKS = TT * 2 * NL;
+    auto add_parts = [&](const Job& job) {
+        const int t0 = t_begin + job.tile * TT;
+        const bool out = job.set == sets - 1;
+        float4* to = reinterpret_cast<float4*>(a.per_row + ((((size_t)g * a.blocks_group + cb) * a.B * a.L) + row0 + t0) * (2 * NP));
 #pragma unroll
-            for (int w = 0; w < W; ++w) s += pp[w * TT * 2 * NP + i];
-            acc[i] = out ? 0.f : s;
-            if (out && t0 + i / (2 * NP) < live) to[i] = s;
+        for (int i = 0; i < (TASKS + HT - 1) / HT; ++i) {
+            const int task = tid + i * HT, t = task / (2 * NL), sl = task / 2 % NL, which = task % 2;
+            if (TASKS % HT != 0 && task >= TASKS) continue;
+            const float4* p = parts + t * PV * 32 + (CL > 1 ? sl * CL + which * RL : which * 32 + sl);
+            float2 lo = both(0.f), hi = both(0.f);
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+#pragma unroll
+                for (int r = 0; r < RL; ++r) {                // (begun at different lanes, in different banks)
+                    const float4 v = p[w * TT * PV * 32 + ((r + task / 2) & (RL - 1))];
+                    lo = __fadd2_rn(lo, make_float2(v.x, v.y)), hi = __fadd2_rn(hi, make_float2(v.z, v.w));
+                }
+            const int at = (t * 2 + which) * (NP / 4) + sl;
+            if (sets > 1) {
+                const float4 v = acc[at];
+                if (job.set > 0) lo = __fadd2_rn(lo, make_float2(v.x, v.y)), hi = __fadd2_rn(hi, make_float2(v.z, v.w));
+                acc[at] = make_float4(lo.x, lo.y, hi.x, hi.y);
+            }
+            if (out && t0 + t < live) to[at] = make_float4(lo.x, lo.y, hi.x, hi.y);
         }
     };
-    auto finish = [&](int k) {
-        const int tile = tiles - 1 - k / sets, set = k % sets, c0 = c_base + set * CB, rows = live - t_begin - tile * TT, nch = a.E - c0;
+    auto finish = [&](const Job& job) {
+        const int k = job.k, tile = job.tile, set = job.set, c0 = c_base + set * CB, rows = live - t_begin - tile * TT, nch = a.E - c0;
         const T* rw = raw + k % RAWS * RAW;
         const float *vs = sums + (k & 1) * SB, *s1 = vs + TT * YS, *s2 = s1 + TT * YS;
         float* mine = chan + set * 8 * HT + tid;
+        if (sets > 1) {
+            params(set);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum_d[j] = mine[j * HT], sum_b[j] = mine[(4 + j) * HT];
+        }
 #pragma unroll
         for (int i = 0; i < UK; ++i) {
             const int r = ur + i * UROWS;
@@ -315,18 +350,14 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
             const float v[4] = {v4.x, v4.y, v4.z, v4.w}, sa[4] = {a4.x, a4.y, a4.z, a4.w}, se[4] = {e4.x, e4.y, e4.z, e4.w};
             const long long row = row0 + t_begin + tile * TT + r;
             const int d0 = g * a.E + c0 + uc;
-            float skip[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const bool real = uc + j < nch;
-                skip[j] = a.Dskip && real ? a.Dskip[d0 + j] : 0.f;
-                const float bias = a.delta_bias && real ? a.delta_bias[d0 + j] : 0.f;
                 const float sj = dd[(k & 1) * QQ + r * CB + uc + j].x, gj = gg[(k & 1) * QQ + r * CB + uc + j];
                 du[j] = fmaf(sj, se[j], skip[j] * gj);
                 ds[j] = fmaf(kLn2, sa[j], u[j] * se[j]);
-                if (a.softplus) ds[j] *= sigmoid(rd[j] + bias);
-                mine[j * HT] = fmaf(gj, u[j], mine[j * HT]);
-                mine[(4 + j) * HT] += ds[j];
+                if (a.softplus) ds[j] *= sigmoid(rd[j] + bias[j]);
+                sum_d[j] = fmaf(gj, u[j], sum_d[j]);
+                sum_b[j] += ds[j];
             }
             T* to_u = a.du + row * a.lddu + d0;
             T* to_d = a.ddelta + row * a.ldddelta + d0;
@@ -356,28 +387,41 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
                 }
             }
         }
+        if (sets > 1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mine[j * HT] = sum_d[j], mine[(4 + j) * HT] = sum_b[j];
+        }
     };
-    fetch(0);
-    fetch(1);
-    fetch(2);
+    Job in{0, tiles - 1, 0}, mid = in, last = in;
+    for (int i = 0; i < 3; ++i, next(in)) fetch(in);
     copies_wait<2>();
     helpers_sync<HT>();                                       // (every helper's copies have arrived)
-    if (jobs) convert(0);
+    if (jobs) convert(mid);
+    next(mid);
     __syncthreads();
     for (int k = 0; k < jobs; ++k) {
-        if (k > 0) add_parts(k - 1);
-        if (Tile::PARTS == 1) __syncthreads();
+        if (k > 0) add_parts(last);
+        __syncthreads();
         // the buffer of job k + 3 is that of job k - 1, which `finish` still reads, as it does the (s, s u) and g that job k + 1 replaces
-        if (k > 0) finish(k - 1);
+        if (k > 0) {
+            finish(last);
+            next(last);
+        }
         copies_wait<1>();
         helpers_sync<HT>();
-        fetch(k + 3);
-        if (k + 1 < jobs) convert(k + 1);
+        fetch(in);
+        next(in);
+        if (k + 1 < jobs) convert(mid);
+        next(mid);
         __syncthreads();
     }
     if (jobs) {
-        add_parts(jobs - 1);
-        finish(jobs - 1);
+        add_parts(last);
+        finish(last);
+    }
+    if (sets == 1) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) chan[j * HT + tid] = sum_d[j], chan[(4 + j) * HT + tid] = sum_b[j];
     }
     for (int set = 0; set < sets; ++set) {                    // rows of padding
         const int c = c_base + set * CB + uc;
