@@ -32,7 +32,7 @@ struct ScanBwdArgs {
     float *dstate_in;
     int B, L, D, N, G, E;
     int segs, seg_rows, blocks_group, sets;
-    long long ldu, lddelta, ldB, ldC, ldz, lddy, lddu, ldddelta, lddz;
+    int ldu, lddelta, ldB, ldC, ldz, lddy, lddu, ldddelta, lddz;
     int u_unit, delta_unit, z_unit, dy_unit, B_unit, C_unit;         // bytes in which rows can be copied
     bool out_quads, softplus;                                         // out_quads: du, ddelta, dz can be stored four elements at a time
 };
@@ -141,15 +141,21 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
             __syncthreads();                                  // the helpers have added the last job's sums over channels
             const float4 c4 = carry4[set * SETS_TH + tid], w4 = dA4[set * SETS_TH + tid];
             float2 carry[2] = {make_float2(c4.x, c4.y), make_float2(c4.z, c4.w)}, dA[2] = {make_float2(w4.x, w4.y), make_float2(w4.z, w4.w)};
+            // (a row's operands are read before the sums of the row before are stored: the compiler may not move them across)
+            struct Row { float2 q; float g; float4 b, c; };
+            auto read = [&](int t) {
+                return Row{sp[t * CB], gp[t * CB], *reinterpret_cast<const float4*>(Bp + t * NP), *reinterpret_cast<const float4*>(Cp + t * NP)};
+            };
+            Row next_row = read(TT - 1);
 #pragma unroll
             for (int tq = TT - 4; tq >= 0; tq -= 4) {
                 float n_sums[8], v[4];                        // sum_n A2 q of four rows, then sum_n e B; sum_n C h
 #pragma unroll
                 for (int j = 3; j >= 0; --j) {
                     const int t = tq + j;
-                    const float2 q = sp[t * CB];
-                    const float4 bv = *reinterpret_cast<const float4*>(Bp + t * NP), cv = *reinterpret_cast<const float4*>(Cp + t * NP);
-                    const float2 s_2 = both(q.x), su2 = both(q.y), g2 = both(gp[t * CB]);
+                    const float2 q = next_row.q, s_2 = both(q.x), su2 = both(q.y), g2 = both(next_row.g);
+                    const float4 bv = next_row.b, cv = next_row.c;
+                    if (t > 0) next_row = read(t - 1);
                     float2 Aq, eB, o;
                     float db[4], dc[4];                       // e s u and g h of the four states
 #pragma unroll
@@ -235,19 +241,22 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
         }
     };
     params(0);
+    const int db0 = g * a.E + c_base;
+    const T *ub = a.u + row0 * a.ldu + db0, *db = a.delta + row0 * a.lddelta + db0, *zb = a.z + row0 * a.ldz + db0, *gb = a.dy + row0 * a.lddy + db0;
+    const T *Bb = a.Bm + row0 * a.ldB + (long long)g * a.N, *Cb = a.Cm + row0 * a.ldC + (long long)g * a.N;
+    T *dub = a.du + row0 * a.lddu + db0 + uc, *ddb = a.ddelta + row0 * a.ldddelta + db0 + uc, *dzb = a.dz + row0 * a.lddz + db0 + uc;
     auto fetch = [&](const Job& job) {
         const int tile = job.tile, set = job.set;
         if (job.k < jobs) {
             T* p = raw + job.k % RAWS * RAW;
-            const int c0 = c_base + set * CB, nch = min(CB, a.E - c0), d0 = g * a.E + c0, rows = live - t_begin - tile * TT;
-            const long long row = row0 + t_begin + tile * TT;
-            copy_tile<TT, CB * ES, HT>(p, a.u + row * a.ldu + d0, a.ldu * ES, rows, nch * ES, a.u_unit, tid);
-            copy_tile<TT, CB * ES, HT>(p + QQ, a.delta + row * a.lddelta + d0, a.lddelta * ES, rows, nch * ES, a.delta_unit, tid);
-            if (a.z) copy_tile<TT, CB * ES, HT>(p + 2 * QQ, a.z + row * a.ldz + d0, a.ldz * ES, rows, nch * ES, a.z_unit, tid);
-            copy_tile<TT, CB * ES, HT>(p + 3 * QQ, a.dy + row * a.lddy + d0, a.lddy * ES, rows, nch * ES, a.dy_unit, tid);
+            const int c0 = set * CB, nch = min(CB, a.E - c_base - c0), t = t_begin + tile * TT, rows = live - t;
+            copy_tile<TT, CB, HT>(p, ub + (long long)t * a.ldu + c0, a.ldu, rows, nch, a.u_unit, tid);
+            copy_tile<TT, CB, HT>(p + QQ, db + (long long)t * a.lddelta + c0, a.lddelta, rows, nch, a.delta_unit, tid);
+            if (a.z) copy_tile<TT, CB, HT>(p + 2 * QQ, zb + (long long)t * a.ldz + c0, a.ldz, rows, nch, a.z_unit, tid);
+            copy_tile<TT, CB, HT>(p + 3 * QQ, gb + (long long)t * a.lddy + c0, a.lddy, rows, nch, a.dy_unit, tid);
             if (set == 0) {
-                copy_tile<TT, NP * ES, HT>(p + 4 * QQ, a.Bm + row * a.ldB + (long long)g * a.N, a.ldB * ES, rows, a.N * ES, a.B_unit, tid);
-                copy_tile<TT, NP * ES, HT>(p + 4 * QQ + TT * NP, a.Cm + row * a.ldC + (long long)g * a.N, a.ldC * ES, rows, a.N * ES, a.C_unit, tid);
+                copy_tile<TT, NP, HT>(p + 4 * QQ, Bb + (long long)t * a.ldB, a.ldB, rows, a.N, a.B_unit, tid);
+                copy_tile<TT, NP, HT>(p + 4 * QQ + TT * NP, Cb + (long long)t * a.ldC, a.ldC, rows, a.N, a.C_unit, tid);
             }
         }
         copies_commit();
@@ -301,10 +310,11 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
     };
     // sums over channels of a job: a thread takes four states of dB or dC of a row, their RL lanes of every warp
     constexpr int RL = CL > 1 ? CL / 2 : 1, TASKS = TT * 2 * NL;
+    float* per_row = a.per_row + (((size_t)g * a.blocks_group + cb) * a.B * a.L + row0) * (2 * NP);
     auto add_parts = [&](const Job& job) {
         const int t0 = t_begin + job.tile * TT;
         const bool out = job.set == sets - 1;
-        float4* to = reinterpret_cast<float4*>(a.per_row + ((((size_t)g * a.blocks_group + cb) * a.B * a.L) + row0 + t0) * (2 * NP));
+        float4* to = reinterpret_cast<float4*>(per_row + (size_t)t0 * (2 * NP));
 #pragma unroll
         for (int i = 0; i < (TASKS + HT - 1) / HT; ++i) {
             const int task = tid + i * HT, t = task / (2 * NL), sl = task / 2 % NL, which = task % 2;
@@ -348,8 +358,7 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
             const float4 v4 = *reinterpret_cast<const float4*>(vs + r * YS + uc), a4 = *reinterpret_cast<const float4*>(s1 + r * YS + uc),
                          e4 = *reinterpret_cast<const float4*>(s2 + r * YS + uc);
             const float v[4] = {v4.x, v4.y, v4.z, v4.w}, sa[4] = {a4.x, a4.y, a4.z, a4.w}, se[4] = {e4.x, e4.y, e4.z, e4.w};
-            const long long row = row0 + t_begin + tile * TT + r;
-            const int d0 = g * a.E + c0 + uc;
+            const int t = t_begin + tile * TT + r;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float sj = dd[(k & 1) * QQ + r * CB + uc + j].x, gj = gg[(k & 1) * QQ + r * CB + uc + j];
@@ -359,8 +368,8 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
                 sum_d[j] = fmaf(gj, u[j], sum_d[j]);
                 sum_b[j] += ds[j];
             }
-            T* to_u = a.du + row * a.lddu + d0;
-            T* to_d = a.ddelta + row * a.ldddelta + d0;
+            T* to_u = dub + (long long)t * a.lddu + set * CB;
+            T* to_d = ddb + (long long)t * a.ldddelta + set * CB;
             if (a.out_quads) {
                 store_pack(to_u, pack<T, 4>(du));
                 store_pack(to_d, pack<T, 4>(ds));
@@ -377,7 +386,7 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
                     const float sg = sigmoid(z[j]);
                     z[j] = gy[j] * fmaf(skip[j], u[j], v[j]) * sg * fmaf(z[j], 1.f - sg, 1.f);
                 }
-                T* to_z = a.dz + row * a.lddz + d0;
+                T* to_z = dzb + (long long)t * a.lddz + set * CB;
                 if (a.out_quads) {
                     store_pack(to_z, pack<T, 4>(z));
                 } else {
@@ -427,9 +436,9 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
         const int c = c_base + set * CB + uc;
         for (int t = max(t_begin, live) + ur; t < t_end; t += UROWS)
             for (int j = 0; j < 4 && c + j < a.E; ++j) {
-                const long long row = row0 + t;
-                a.du[row * a.lddu + g * a.E + c + j] = a.ddelta[row * a.ldddelta + g * a.E + c + j] = from_float<T>(0.f);
-                if (a.z) a.dz[row * a.lddz + g * a.E + c + j] = from_float<T>(0.f);
+                const int at = set * CB + j;
+                dub[(long long)t * a.lddu + at] = ddb[(long long)t * a.ldddelta + at] = from_float<T>(0.f);
+                if (a.z) dzb[(long long)t * a.lddz + at] = from_float<T>(0.f);
             }
     }
     helpers_sync<HT>();

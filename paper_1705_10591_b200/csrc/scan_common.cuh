@@ -99,32 +99,31 @@ inline int copy_unit(const void* p, long long ld, long long width, int esize)
     return unit;
 }
 
-// Copies a tile of ROWS rows of BYTES bytes into shared memory, where they lie one behind the other: rows from `live_rows` on and bytes from
-// `live_bytes` on as zeros.  Units of 4 bytes and more go by asynchronous copies, which the caller commits and waits for.
-template <int ROWS, int BYTES, int UNIT, int THREADS>
-__device__ __forceinline__ void copy_tile_by(unsigned char* dst, const unsigned char* src, long long ld_bytes, int live_rows, int live_bytes, int tid)
+// Copies a tile of ROWS rows of COLS elements, `ld` elements apart, into shared memory, where they lie one behind the other: rows from `live_rows` on
+// and columns from `live_cols` on as zeros.  Units of 4 bytes and more go by asynchronous copies, which the caller commits and waits for.
+template <int ROWS, int COLS, int UNIT, int THREADS, typename T>
+__device__ __forceinline__ void copy_tile_by(T* dst, const T* src, int ld, int live_rows, int live_cols, int tid)
 {
-    constexpr int PER_ROW = BYTES / UNIT, COUNT = ROWS * PER_ROW;
+    constexpr int E = UNIT / (int)sizeof(T), PER_ROW = COLS / E, COUNT = ROWS * PER_ROW;
 #pragma unroll
     for (int k = 0; k < (COUNT + THREADS - 1) / THREADS; ++k) {
         const int i = tid + k * THREADS;
         if (COUNT % THREADS != 0 && i >= COUNT) break;
-        const int r = i / PER_ROW, c = i % PER_ROW * UNIT;
-        const bool real = r < live_rows && c < live_bytes;
-        const unsigned char* from = real ? src + r * ld_bytes + c : src;
-        if (UNIT >= 4) copy_async<UNIT < 4 ? 4 : UNIT>(dst + i * UNIT, from, real);
-        else *reinterpret_cast<unsigned short*>(dst + i * UNIT) = real ? *reinterpret_cast<const unsigned short*>(from) : (unsigned short)0;
+        const int r = i / PER_ROW, c = i % PER_ROW * E;
+        const bool real = r < live_rows && c < live_cols;
+        const T* from = src + (real ? (long long)r * ld + c : 0);
+        if constexpr (UNIT >= 4) copy_async<UNIT>(dst + i * E, from, real);
+        else dst[i] = real ? *from : from_float<T>(0.f);
     }
 }
-template <int ROWS, int BYTES, int THREADS>
-__device__ __forceinline__ void copy_tile(void* dst, const void* src, long long ld_bytes, int live_rows, int live_bytes, int unit, int tid)
+template <int ROWS, int COLS, int THREADS, typename T>
+__device__ __forceinline__ void copy_tile(T* dst, const T* src, int ld, int live_rows, int live_cols, int unit, int tid)
 {
-    unsigned char* d = static_cast<unsigned char*>(dst);
-    const unsigned char* s = static_cast<const unsigned char*>(src);
-    if (BYTES >= 16 && unit == 16) copy_tile_by<ROWS, BYTES, BYTES >= 16 ? 16 : 2, THREADS>(d, s, ld_bytes, live_rows, live_bytes, tid);
-    else if (BYTES >= 8 && unit >= 8) copy_tile_by<ROWS, BYTES, BYTES >= 8 ? 8 : 2, THREADS>(d, s, ld_bytes, live_rows, live_bytes, tid);
-    else if (unit >= 4) copy_tile_by<ROWS, BYTES, 4, THREADS>(d, s, ld_bytes, live_rows, live_bytes, tid);
-    else copy_tile_by<ROWS, BYTES, 2, THREADS>(d, s, ld_bytes, live_rows, live_bytes, tid);
+    constexpr int BYTES = COLS * (int)sizeof(T), NARROW = (int)sizeof(T);
+    if (BYTES >= 16 && unit == 16) copy_tile_by<ROWS, COLS, BYTES >= 16 ? 16 : NARROW, THREADS>(dst, src, ld, live_rows, live_cols, tid);
+    else if (BYTES >= 8 && unit >= 8) copy_tile_by<ROWS, COLS, BYTES >= 8 ? 8 : NARROW, THREADS>(dst, src, ld, live_rows, live_cols, tid);
+    else if (unit >= 4) copy_tile_by<ROWS, COLS, 4, THREADS>(dst, src, ld, live_rows, live_cols, tid);
+    else copy_tile_by<ROWS, COLS, NARROW, THREADS>(dst, src, ld, live_rows, live_cols, tid);
 }
 // Barrier among the THREADS helping threads of a block (the block's own barrier is number 0).
 template <int THREADS> __device__ __forceinline__ void helpers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
@@ -150,12 +149,22 @@ __global__ void __launch_bounds__(256) scan_join_kernel(float* local, const floa
     const bool real = n < N;
     const float a2 = real ? A[(size_t)d * N + n] * kLog2e : 0.f;
     float H = first && real ? first[((size_t)b * D + d) * N + n] : 0.f;
-    for (int i = 0; i < segs; ++i) {
-        const int seg = REVERSE ? segs - 1 - i : i;
-        float* p = local + (((size_t)b * segs + seg) * D + d) * NQ + n;
-        const float l = *p;
-        *p = H;
-        H = fmaf(ex2(a2 * steps[((size_t)b * segs + seg) * D + d]), H, l);
+    constexpr int AHEAD = 8;                                  // segments whose loads are under way together
+    for (int i0 = 0; i0 < segs; i0 += AHEAD) {
+        float l[AHEAD], s[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int i = min(i0 + j, segs - 1);
+            const size_t at = ((size_t)b * segs + (REVERSE ? segs - 1 - i : i)) * D + d;
+            l[j] = local[at * NQ + n], s[j] = steps[at];
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int i = i0 + j;
+            if (i >= segs) break;
+            local[(((size_t)b * segs + (REVERSE ? segs - 1 - i : i)) * D + d) * NQ + n] = H;
+            H = fmaf(ex2(a2 * s[j]), H, l[j]);
+        }
     }
     if (last && real) last[((size_t)b * D + d) * N + n] = H;
 }

@@ -25,7 +25,7 @@ struct ScanFwdArgs {
     float *state_out, *states, *local, *steps;     // local: [B][segs][D][NQ] states that segments begin with (end with, STATE_ONLY)
     int B, L, D, N, G, E;                          // E = D / G channels of a group
     int segs, seg_rows, blocks_group;              // seg_rows: a multiple of the tile; blocks_group: blocks of a group's channels
-    long long ldu, lddelta, ldB, ldC, ldz, ldy;
+    int ldu, lddelta, ldB, ldC, ldz, ldy;
     int u_unit, delta_unit, z_unit, B_unit, C_unit;   // bytes in which rows can be copied
     bool y_quads, softplus;                           // y_quads: y can be stored four elements at a time
 };
@@ -169,17 +169,18 @@ __global__ void __launch_bounds__(ScanFwdTile<NL, SPT>::TH) scan_fwd_kernel(cons
         bias[i] = a.delta_bias && uc + i < nch ? a.delta_bias[d0 + uc + i] : 0.f;
         skip[i] = !STATE_ONLY && a.Dskip && uc + i < nch ? a.Dskip[d0 + uc + i] : 0.f;
     }
+    const T *ub = a.u + row0 * a.ldu + d0, *db = a.delta + row0 * a.lddelta + d0, *zb = a.z + row0 * a.ldz + d0;
+    const T *Bb = a.Bm + row0 * a.ldB + (long long)g * a.N, *Cb = a.Cm + row0 * a.ldC + (long long)g * a.N;
+    T* yb = a.y + row0 * a.ldy + d0 + uc;
     auto fetch = [&](int k) {
         if (k < tiles) {
             T* p = raw + k % RAWS * RAW;
-            const int rows = live - t_begin - k * TT;
-            const long long row = row0 + t_begin + k * TT;
-            copy_tile<TT, CB * ES, HT>(p, a.u + row * a.ldu + d0, a.ldu * ES, rows, nch * ES, a.u_unit, tid);
-            copy_tile<TT, CB * ES, HT>(p + TT * CB, a.delta + row * a.lddelta + d0, a.lddelta * ES, rows, nch * ES, a.delta_unit, tid);
-            if (!STATE_ONLY && a.z) copy_tile<TT, CB * ES, HT>(p + 2 * TT * CB, a.z + row * a.ldz + d0, a.ldz * ES, rows, nch * ES, a.z_unit, tid);
-            copy_tile<TT, NP * ES, HT>(p + 3 * TT * CB, a.Bm + row * a.ldB + (long long)g * a.N, a.ldB * ES, rows, a.N * ES, a.B_unit, tid);
-            if (!STATE_ONLY)
-                copy_tile<TT, NP * ES, HT>(p + 3 * TT * CB + TT * NP, a.Cm + row * a.ldC + (long long)g * a.N, a.ldC * ES, rows, a.N * ES, a.C_unit, tid);
+            const int t = t_begin + k * TT, rows = live - t;
+            copy_tile<TT, CB, HT>(p, ub + (long long)t * a.ldu, a.ldu, rows, nch, a.u_unit, tid);
+            copy_tile<TT, CB, HT>(p + TT * CB, db + (long long)t * a.lddelta, a.lddelta, rows, nch, a.delta_unit, tid);
+            if (!STATE_ONLY && a.z) copy_tile<TT, CB, HT>(p + 2 * TT * CB, zb + (long long)t * a.ldz, a.ldz, rows, nch, a.z_unit, tid);
+            copy_tile<TT, NP, HT>(p + 3 * TT * CB, Bb + (long long)t * a.ldB, a.ldB, rows, a.N, a.B_unit, tid);
+            if (!STATE_ONLY) copy_tile<TT, NP, HT>(p + 3 * TT * CB + TT * NP, Cb + (long long)t * a.ldC, a.ldC, rows, a.N, a.C_unit, tid);
         }
         copies_commit();
     };
@@ -216,7 +217,7 @@ __global__ void __launch_bounds__(ScanFwdTile<NL, SPT>::TH) scan_fwd_kernel(cons
     };
     auto finish = [&](int k) {
         const T* rw = raw + k % RAWS * RAW;
-        const float* yb = ys + (k & 1) * YB;
+        const float* yk = ys + (k & 1) * YB;
         const int rows = live - t_begin - k * TT;
 #pragma unroll
         for (int i = 0; i < UK; ++i) {
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(ScanFwdTile<NL, SPT>::TH) scan_fwd_kernel(cons
             if (uc >= nch || r >= TT || r >= rows) continue;
             float u[4], o[4];
             load4(rw + r * CB + uc, u);
-            const float4 y4 = *reinterpret_cast<const float4*>(yb + r * YS + uc);
+            const float4 y4 = *reinterpret_cast<const float4*>(yk + r * YS + uc);
             o[0] = fmaf(skip[0], u[0], y4.x), o[1] = fmaf(skip[1], u[1], y4.y), o[2] = fmaf(skip[2], u[2], y4.z), o[3] = fmaf(skip[3], u[3], y4.w);
             if (a.z) {
                 float z[4];
@@ -232,7 +233,7 @@ __global__ void __launch_bounds__(ScanFwdTile<NL, SPT>::TH) scan_fwd_kernel(cons
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[j] *= z[j] * sigmoid(z[j]);
             }
-            T* to = a.y + (row0 + t_begin + k * TT + r) * a.ldy + d0 + uc;
+            T* to = yb + (long long)(t_begin + k * TT + r) * a.ldy;
             if (a.y_quads) {
                 store_pack(to, pack<T, 4>(o));
             } else {
@@ -261,7 +262,7 @@ __global__ void __launch_bounds__(ScanFwdTile<NL, SPT>::TH) scan_fwd_kernel(cons
     if (STATE_ONLY) return;
     if (tiles) finish(tiles - 1);
     for (int t = max(t_begin, live) + ur; t < t_end; t += UROWS)
-        for (int j = 0; j < 4 && uc + j < nch; ++j) a.y[(row0 + t) * a.ldy + d0 + uc + j] = from_float<T>(0.f);
+        for (int j = 0; j < 4 && uc + j < nch; ++j) yb[(long long)t * a.ldy + j] = from_float<T>(0.f);
 }
 
 }  // namespace conv2d_b200

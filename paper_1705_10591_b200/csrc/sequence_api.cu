@@ -18,8 +18,8 @@ bool extents_ok(long long B, long long L, long long D)
 }
 bool element_aligned(const void* p, size_t size) { return reinterpret_cast<uintptr_t>(p) % size == 0; }
 
-// A tensor of rows: distance at least the row's length (a tensor that is not given has none), and no offset beyond 63 bits.
-bool rows_ok(const void* p, long long ld, long long width) { return !p || (ld >= width && ld <= (1LL << 31)); }
+// A tensor of rows: distance at least the row's length (a tensor that is not given has none), in 32 bits.
+bool rows_ok(const void* p, long long ld, long long width) { return !p || (ld >= width && ld <= 0x7fffffffLL); }
 
 template <typename... P>
 bool all_aligned(size_t size, P... p) { return (element_aligned(p, size) && ...); }
