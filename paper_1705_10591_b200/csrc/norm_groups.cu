@@ -23,7 +23,8 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kRowThreads = 256;        // rows
+constexpr int kThreads = 256, kWarps = kThreads / 32;        // slab, stream
 constexpr int kGroup = 2, kRing = 8;    // rows of a group (four take the backward pass to 240 registers), groups of a ring
 
 template <typename T>
@@ -52,7 +53,9 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes)
 // Several sums over the same lanes, under way together.
 template <int N> __device__ __forceinline__ void lanes_sums(float (&v)[N], int lanes)
 {
-    for (int m = 1; m < lanes; m *= 2) {
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) {
+        if (m >= lanes) break;
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], m);
     }
@@ -65,169 +68,265 @@ __device__ __forceinline__ void load_params(const float* p, float dflt, int c, b
     for (int i = 0; i < V; ++i) out[i] = p && real ? p[c + i] : dflt;
 }
 
-// A thread keeps NV packs of one group, lane l the packs l, l + lanes, ..; ROWS samples are under way together.
-template <typename T, int V, int NV, int ROWS>
-__global__ void __launch_bounds__(kThreads) norm_rows_fwd_kernel(const NormArgs<T> a)
+// gamma and beta of a pack, 1 and 0 where there are none
+template <int V>
+__device__ __forceinline__ void load_scale(const float* gamma, const float* beta, int c, bool real, float2 (&g)[kPairs<V>], float2 (&b)[kPairs<V>])
 {
-    ptx::grid_dep_wait();
-    const unsigned cols = (kThreads + (unsigned)a.G * a.lanes - 1) / kThreads;
-    const unsigned col = blockIdx.x % cols * kThreads + threadIdx.x;
-    const int g = (int)(col / a.lanes), l = (int)(col % a.lanes);
-    const long long n0 = (long long)(blockIdx.x / cols) * a.chunk, n1 = min(n0 + a.chunk, (long long)a.N);
-    int c[NV];
-    bool real[NV];
-    float gamma[NV][V], beta[NV][V];
+    float gf[V], bf[V];
+    load_params<V>(gamma, 1.f, c, real, gf);
+    load_params<V>(beta, 0.f, c, real, bf);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int e = (l + k * a.lanes) * V;
-        real[k] = g < a.G && e < a.E;
-        c[k] = g * a.E + e;
-        load_params<V>(a.gamma, 1.f, c[k], real[k], gamma[k]);
-        load_params<V>(a.beta, 0.f, c[k], real[k], beta[k]);
+    for (int k = 0; k < kPairs<V>; ++k) {
+        g[k] = make_float2(gf[2 * k], V > 1 ? gf[V > 1 ? 2 * k + 1 : 0] : 0.f);
+        b[k] = make_float2(bf[2 * k], V > 1 ? bf[V > 1 ? 2 * k + 1 : 0] : 0.f);
     }
-    const float inv = 1.f / a.E;
-    for (long long n = n0; n < n1; n += ROWS) {
-        Pack<T, V> p[ROWS][NV];
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-            for (int k = 0; k < NV; ++k) p[r][k] = real[k] && n + r < n1 ? load_pack<T, V>(a.x + (n + r) * a.ldx + c[k]) : zero_pack<T, V>();
-        float x[ROWS][NV * V], mean[ROWS], rstd[ROWS];
+}
+
+// A thread's packs of a chunk of samples: NV of one group, lane l the packs l, l + lanes, ..; they come in through a ring of four groups of ROWS samples.
+template <typename T, int V, int NV, int ROWS>
+struct SampleRing {
+    static constexpr int RING = 4, bytes = V * (int)sizeof(T);
+    static constexpr bool async = bytes >= 4;
+    static constexpr size_t smem = async ? (size_t)RING * ROWS * NV * kRowThreads * bytes : 0;
+    unsigned char* mine;
+    const T* p;                         // of the chunk's first sample, pack 0
+    long long ld;
+    int apart;                          // elements from one of the thread's packs to the next
+    __device__ void issue(int q, int n, int count, const bool (&real)[NV]) const
+    {
+        if (!async) return;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            mean[r] = 0.f;
+            const bool in = n + r < count;
+            const T* from = p + (in ? (n + r) * ld : 0);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                copy_async<async ? bytes : 4>(mine + (size_t)(((q & (RING - 1)) * ROWS + r) * NV + k) * (kRowThreads * bytes), from + (real[k] ? k * apart : 0), in && real[k]);
+        }
+    }
+    __device__ Pack<T, V> get(int q, int n, int r, int k, int count, const bool (&real)[NV]) const
+    {
+        if (async) return *reinterpret_cast<const Pack<T, V>*>(mine + (size_t)(((q & (RING - 1)) * ROWS + r) * NV + k) * (kRowThreads * bytes));
+        return n + r < count && real[k] ? load_pack<T, V>(p + (n + r) * ld + k * apart) : zero_pack<T, V>();
+    }
+};
+
+template <typename T, int V, int NV, int ROWS>
+__global__ void __launch_bounds__(kRowThreads) norm_rows_fwd_kernel(const NormArgs<T> a)
+{
+    constexpr int P = kPairs<V>;
+    ptx::grid_dep_wait();
+    extern __shared__ float4 smem4[];
+    const unsigned cols = (kRowThreads + (unsigned)a.G * a.lanes - 1) / kRowThreads;
+    const unsigned col = blockIdx.x % cols * kRowThreads + threadIdx.x;
+    const int g = (int)(col / a.lanes), l = (int)(col % a.lanes);
+    const long long n0 = (long long)(blockIdx.x / cols) * a.chunk;
+    const int count = (int)min((long long)a.chunk, a.N - n0), c = g * a.E + l * V, apart = a.lanes * V;
+    bool real[NV];
+    float2 gamma[NV][P], beta[NV][P];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        real[k] = g < a.G && (l + k * a.lanes) * V < a.E;
+        load_scale<V>(a.gamma, a.beta, c + k * apart, real[k], gamma[k], beta[k]);
+    }
+    using Ring = SampleRing<T, V, NV, ROWS>;
+    const Ring x{reinterpret_cast<unsigned char*>(smem4) + threadIdx.x * Ring::bytes, a.x + (real[0] ? n0 * a.ldx + c : 0), a.ldx, apart};
+#pragma unroll
+    for (int q = 0; q < Ring::RING - 1; ++q) {
+        x.issue(q, q * ROWS, count, real);
+        copies_commit();
+    }
+    const float inv = 1.f / a.E;
+    const bool first = l == 0 && g < a.G;
+    T* y = a.y + n0 * a.ldy + c;
+    float *mean_out = a.mean && first ? a.mean + n0 * a.G + g : nullptr, *rstd_out = a.rstd && first ? a.rstd + n0 * a.G + g : nullptr;
+    int q = 0;
+#pragma unroll 1
+    for (int n = 0; n < count; n += ROWS, ++q) {
+        copies_wait<Ring::RING - 2>();
+        float2 v[ROWS][NV][P];
+        float mean[ROWS], rstd[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            float2 s = both(0.f);
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                float v[V];
-                unpack(p[r][k], v);
+                pairs<T, V>(x.get(q, n, r, k, count, real), v[r][k]);
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[r][k * V + i] = v[i], mean[r] += v[i];
+                for (int i = 0; i < P; ++i) s = __fadd2_rn(s, v[r][k][i]);
             }
+            mean[r] = V > 1 ? s.x + s.y : s.x;
         }
+        x.issue(q + Ring::RING - 1, n + (Ring::RING - 1) * ROWS, count, real);
+        copies_commit();
         lanes_sums(mean, a.lanes);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             mean[r] *= inv;
-            rstd[r] = 0.f;
+            float2 s = both(0.f);
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
+            for (int k = 0; k < NV; ++k) {
+                float2 t = both(0.f);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = x[r][k * V + i] -= mean[r];
-                    if (real[k]) rstd[r] = fmaf(d, d, rstd[r]);
+                for (int i = 0; i < P; ++i) {
+                    v[r][k][i] = __fadd2_rn(v[r][k][i], both(-mean[r]));
+                    t = __ffma2_rn(v[r][k][i], v[r][k][i], t);
                 }
+                if (real[k]) s = __fadd2_rn(s, t);
+            }
+            rstd[r] = V > 1 ? s.x + s.y : s.x;
         }
         lanes_sums(rstd, a.lanes);
+        float o[ROWS * NV * 2 * P];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             rstd[r] = rsqrtf(fmaf(rstd[r], inv, a.eps));
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[r][k * V + i] = fmaf(x[r][k * V + i] * rstd[r], gamma[k][i], beta[k][i]);
-            activate(x[r], a.act);
-            if (n + r >= n1) continue;
-            if (l == 0 && g < a.G) {
-                if (a.mean) a.mean[(n + r) * a.G + g] = mean[r];
-                if (a.rstd) a.rstd[(n + r) * a.G + g] = rstd[r];
-            }
+                for (int i = 0; i < P; ++i) {
+                    const float2 w = __ffma2_rn(__fmul2_rn(v[r][k][i], both(rstd[r])), gamma[k][i], beta[k][i]);
+                    o[2 * ((r * NV + k) * P + i)] = w.x, o[2 * ((r * NV + k) * P + i) + 1] = w.y;
+                }
+        }
+        activate(o, a.act);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            if (n + r >= count) break;
+            if (mean_out) *mean_out = mean[r], mean_out += a.G;
+            if (rstd_out) *rstd_out = rstd[r], rstd_out += a.G;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                if (!real[k]) continue;
-                float o[V];
+                float2 w[P];
 #pragma unroll
-                for (int i = 0; i < V; ++i) o[i] = x[r][k * V + i];
-                store_pack(a.y + (n + r) * a.ldy + c[k], pack<T, V>(o));
+                for (int i = 0; i < P; ++i) w[i] = make_float2(o[2 * ((r * NV + k) * P + i)], o[2 * ((r * NV + k) * P + i) + 1]);
+                if (real[k]) store_pack(y + k * apart, pack_of<T, V>(w));
             }
+            y += a.ldy;
         }
     }
 }
 
 template <typename T, int V, int NV, int ROWS>
-__global__ void __launch_bounds__(kThreads) norm_rows_bwd_kernel(const NormArgs<T> a)
+__global__ void __launch_bounds__(kRowThreads) norm_rows_bwd_kernel(const NormArgs<T> a)
 {
+    constexpr int P = kPairs<V>;
     ptx::grid_dep_wait();
-    const unsigned cols = (kThreads + (unsigned)a.G * a.lanes - 1) / kThreads;
-    const unsigned col = blockIdx.x % cols * kThreads + threadIdx.x;
+    extern __shared__ float4 smem4[];
+    const unsigned cols = (kRowThreads + (unsigned)a.G * a.lanes - 1) / kRowThreads;
+    const unsigned col = blockIdx.x % cols * kRowThreads + threadIdx.x;
     const int g = (int)(col / a.lanes), l = (int)(col % a.lanes);
-    const long long chunk = blockIdx.x / cols, n0 = chunk * a.chunk, n1 = min(n0 + a.chunk, (long long)a.N);
-    int c[NV];
+    const long long chunk = blockIdx.x / cols, n0 = chunk * a.chunk;
+    const int count = (int)min((long long)a.chunk, a.N - n0), c = g * a.E + l * V, apart = a.lanes * V;
     bool real[NV];
-    float gamma[NV][V], beta[NV][V], sum1[NV][V] = {}, sum2[NV][V] = {};
+    float2 gamma[NV][P], beta[NV][P], sum1[NV][P], sum2[NV][P];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        const int e = (l + k * a.lanes) * V;
-        real[k] = g < a.G && e < a.E;
-        c[k] = g * a.E + e;
-        load_params<V>(a.gamma, 1.f, c[k], real[k], gamma[k]);
-        load_params<V>(a.beta, 0.f, c[k], real[k], beta[k]);
+        real[k] = g < a.G && (l + k * a.lanes) * V < a.E;
+        load_scale<V>(a.gamma, a.beta, c + k * apart, real[k], gamma[k], beta[k]);
+#pragma unroll
+        for (int i = 0; i < P; ++i) sum1[k][i] = sum2[k][i] = both(0.f);
+    }
+    using Ring = SampleRing<T, V, NV, ROWS>;
+    const Ring x{reinterpret_cast<unsigned char*>(smem4) + threadIdx.x * Ring::bytes, a.x + (real[0] ? n0 * a.ldx + c : 0), a.ldx, apart};
+    const Ring dy{x.mine + Ring::smem, a.dy + (real[0] ? n0 * a.lddy + c : 0), a.lddy, apart};
+#pragma unroll
+    for (int q = 0; q < Ring::RING - 1; ++q) {
+        x.issue(q, q * ROWS, count, real);
+        dy.issue(q, q * ROWS, count, real);
+        copies_commit();
     }
     const float inv = 1.f / a.E;
-    for (long long n = n0; n < n1; n += ROWS) {
-        Pack<T, V> p[ROWS][NV], q[ROWS][NV];
-        float mean[ROWS], rstd[ROWS];
+    const float *mean_in = a.mean + n0 * a.G + (g < a.G ? g : 0), *rstd_in = a.rstd + n0 * a.G + (g < a.G ? g : 0);
+    T* dx = a.dx + n0 * a.lddx + c;
+    float mean[ROWS], rstd[ROWS];                            // of the next samples, read one group ahead
+    auto read = [&](int n) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            const bool in = g < a.G && n + r < n1;
-            mean[r] = in ? a.mean[(n + r) * a.G + g] : 0.f;
-            rstd[r] = in ? a.rstd[(n + r) * a.G + g] : 0.f;
+            const bool in = n + r < count;
+            mean[r] = in ? mean_in[(long long)(n + r) * a.G] : 0.f;
+            rstd[r] = in ? rstd_in[(long long)(n + r) * a.G] : 0.f;
+        }
+    };
+    read(0);
+    int q = 0;
+#pragma unroll 1
+    for (int n = 0; n < count; n += ROWS, ++q) {
+        copies_wait<Ring::RING - 2>();
+        float2 xn[ROWS][NV][P];
+        float d[ROWS * NV * 2 * P], pre[ROWS * NV * 2 * P], m[2 * ROWS], scale[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            scale[r] = rstd[r];
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                p[r][k] = real[k] && in ? load_pack<T, V>(a.x + (n + r) * a.ldx + c[k]) : zero_pack<T, V>();
-                q[r][k] = real[k] && in ? load_pack<T, V>(a.dy + (n + r) * a.lddy + c[k]) : zero_pack<T, V>();
+                float2 w[P];
+                pairs<T, V>(x.get(q, n, r, k, count, real), xn[r][k]);
+                pairs<T, V>(dy.get(q, n, r, k, count, real), w);     // (zero outside the group and behind the last sample)
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    const int at = 2 * ((r * NV + k) * P + i);
+                    xn[r][k][i] = __fmul2_rn(__fadd2_rn(xn[r][k][i], both(-mean[r])), both(rstd[r]));
+                    const float2 z = __ffma2_rn(xn[r][k][i], gamma[k][i], beta[k][i]);
+                    d[at] = w[i].x, d[at + 1] = w[i].y, pre[at] = z.x, pre[at + 1] = z.y;
+                }
             }
         }
-        float xn[ROWS][NV * V], d[ROWS][NV * V], m[2 * ROWS];
+        x.issue(q + Ring::RING - 1, n + (Ring::RING - 1) * ROWS, count, real);
+        dy.issue(q + Ring::RING - 1, n + (Ring::RING - 1) * ROWS, count, real);
+        copies_commit();
+        if (n + ROWS < count) read(n + ROWS);
+        times_slope(d, pre, a.act);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            float pre[NV * V];
+            float2 m1 = both(0.f), m2 = both(0.f);
+            if (n + r < count) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                float v[V], w[V];
-                unpack(p[r][k], v);
-                unpack(q[r][k], w);
+                for (int k = 0; k < NV; ++k) {
+                    if (!real[k]) continue;
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    xn[r][k * V + i] = real[k] ? (v[i] - mean[r]) * rstd[r] : 0.f;
-                    d[r][k * V + i] = w[i];                  // (zero outside the group and behind the last sample)
-                    pre[k * V + i] = fmaf(xn[r][k * V + i], gamma[k][i], beta[k][i]);
+                    for (int i = 0; i < P; ++i) {
+                        const int at = 2 * ((r * NV + k) * P + i);
+                        float2 e = make_float2(d[at], d[at + 1]);
+                        sum1[k][i] = __fadd2_rn(sum1[k][i], e);
+                        sum2[k][i] = __ffma2_rn(e, xn[r][k][i], sum2[k][i]);
+                        e = __fmul2_rn(e, gamma[k][i]);
+                        m1 = __fadd2_rn(m1, e);
+                        m2 = __ffma2_rn(e, xn[r][k][i], m2);
+                        d[at] = e.x, d[at + 1] = e.y;
+                    }
                 }
             }
-            times_slope(d[r], pre, a.act);
-            m[2 * r] = m[2 * r + 1] = 0.f;
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float& e = d[r][k * V + i];
-                    sum1[k][i] += e;
-                    sum2[k][i] = fmaf(e, xn[r][k * V + i], sum2[k][i]);
-                    e *= gamma[k][i];
-                    m[2 * r] += e;
-                    m[2 * r + 1] = fmaf(e, xn[r][k * V + i], m[2 * r + 1]);
-                }
+            m[2 * r] = V > 1 ? m1.x + m1.y : m1.x, m[2 * r + 1] = V > 1 ? m2.x + m2.y : m2.x;
         }
         lanes_sums(m, a.lanes);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
-            if (n + r >= n1) continue;
+            if (n + r >= count) break;
+            const float2 m1 = both(-m[2 * r] * inv), m2 = both(-m[2 * r + 1] * inv);
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                if (!real[k]) continue;
-                float o[V];
+                float2 w[P];
 #pragma unroll
-                for (int i = 0; i < V; ++i) o[i] = rstd[r] * (d[r][k * V + i] - m[2 * r] * inv - xn[r][k * V + i] * (m[2 * r + 1] * inv));
-                store_pack(a.dx + (n + r) * a.lddx + c[k], pack<T, V>(o));
+                for (int i = 0; i < P; ++i) {
+                    const int at = 2 * ((r * NV + k) * P + i);
+                    w[i] = __fmul2_rn(both(scale[r]), __ffma2_rn(xn[r][k][i], m2, __fadd2_rn(make_float2(d[at], d[at + 1]), m1)));
+                }
+                if (real[k]) store_pack(dx + k * apart, pack_of<T, V>(w));
             }
+            dx += a.lddx;
         }
     }
     if (!a.channels) return;
-    float* out = a.channels + (size_t)chunk * 2 * a.C;
+    float* out = a.channels + (size_t)chunk * 2 * a.C + c;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         if (!real[k]) continue;
 #pragma unroll
-        for (int i = 0; i < V; ++i) out[c[k] + i] = sum1[k][i], out[a.C + c[k] + i] = sum2[k][i];
+        for (int i = 0; i < V; ++i) {
+            out[k * apart + i] = i % 2 ? sum1[k][i / 2].y : sum1[k][i / 2].x;
+            out[a.C + k * apart + i] = i % 2 ? sum2[k][i / 2].y : sum2[k][i / 2].x;
+        }
     }
 }
 
@@ -461,15 +560,10 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
         T* y = a.y + (p.n * a.S + p.first) * a.ldy + p.c0 + p.pack_of(q) * V;
         const int pk = p.pack_of(q);
         const float2 st = gnorm[p.group];
-        float gamma[V], beta[V];
-        load_params<V>(a.gamma, 1.f, p.c0 + pk * V, true, gamma);
-        load_params<V>(a.beta, 0.f, p.c0 + pk * V, true, beta);
         float2 scale[P], add[P];
+        load_scale<V>(a.gamma, a.beta, p.c0 + pk * V, true, scale, add);
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-            scale[k] = make_float2(st.y * gamma[2 * k], V > 1 ? st.y * gamma[V > 1 ? 2 * k + 1 : 0] : 0.f);
-            add[k] = make_float2(beta[2 * k], V > 1 ? beta[V > 1 ? 2 * k + 1 : 0] : 0.f);
-        }
+        for (int k = 0; k < P; ++k) scale[k] = __fmul2_rn(scale[k], both(st.y));
         walk_rows<KEEP>(r.count, [&](int g, int i) { r.ring.issue(g, i, r.count); }, [&](int g, int i) {
             float o[kGroup * 2 * P];
 #pragma unroll
@@ -526,14 +620,7 @@ __global__ void __launch_bounds__(kThreads) norm_slab_bwd_kernel(const NormArgs<
         Params r;
         const int g = g0 + p.group;
         r.mean = a.mean[p.n * a.G + g], r.rstd = a.rstd[p.n * a.G + g];
-        float gamma[V], beta[V];
-        load_params<V>(a.gamma, 1.f, p.c0 + pk * V, true, gamma);
-        load_params<V>(a.beta, 0.f, p.c0 + pk * V, true, beta);
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-            r.gamma[k] = make_float2(gamma[2 * k], V > 1 ? gamma[V > 1 ? 2 * k + 1 : 0] : 0.f);
-            r.beta[k] = make_float2(beta[2 * k], V > 1 ? beta[V > 1 ? 2 * k + 1 : 0] : 0.f);
-        }
+        load_scale<V>(a.gamma, a.beta, p.c0 + pk * V, true, r.gamma, r.beta);
         return r;
     };
     auto terms = [&](const Params& m, const Rows& rx, const Rows& rg, int g, int i, float2 (&xn)[kGroup][P], float (&d)[kGroup * 2 * P]) {
@@ -697,12 +784,12 @@ NormPlan make_norm_plan(int N, int S, int C, int G, int esize, int V, bool bwd)
     int lanes = 1;
     while (lanes < 32 && lanes < ev) lanes *= 2;
     const int nv = (ev + lanes - 1) / lanes;
-    if (S == 1 && nv <= (bwd ? 4 : 8)) {
+    if (S == 1 && nv <= 4) {
         p.rows = true;
         p.lanes = lanes;
-        p.nv = nv <= 1 ? 1 : nv <= 2 ? 2 : nv <= 4 ? 4 : 8;
+        p.nv = nv <= 1 ? 1 : nv <= 2 ? 2 : 4;
         // as many chunks of samples as fill the machine (eight blocks an SM), at least four samples each
-        const long long cols = ((long long)G * lanes + kThreads - 1) / kThreads;
+        const long long cols = ((long long)G * lanes + kRowThreads - 1) / kRowThreads;
         long long chunks = (8LL * kSms + cols - 1) / cols;
         if (chunks > (N + 3) / 4) chunks = (N + 3) / 4;
         p.chunk = (int)((N + chunks - 1) / chunks);
@@ -788,14 +875,31 @@ NormArgs<T> make_args(const NormSeq& s, const NormPlan& p)
 }
 
 template <typename... KArgs, typename... Args>
-conv2d_status_t launched(void (*kernel)(KArgs...), long long blocks, size_t smem, unsigned cluster, cudaStream_t stream, Args... args)
+conv2d_status_t launched(void (*kernel)(KArgs...), long long blocks, int threads, size_t smem, unsigned cluster, cudaStream_t stream, Args... args)
 {
     if (blocks > 0x7fffffffLL) return CONV2D_ERR_SHAPE;
-    const cudaError_t e = cluster > 1 ? launch_pdl_cluster(kernel, dim3((unsigned)blocks), dim3(kThreads), smem, stream, cluster, args...)
-                                      : launch_pdl(kernel, dim3((unsigned)blocks), dim3(kThreads), smem, stream, args...);
+    const cudaError_t e = cluster > 1 ? launch_pdl_cluster(kernel, dim3((unsigned)blocks), dim3(threads), smem, stream, cluster, args...)
+                                      : launch_pdl(kernel, dim3((unsigned)blocks), dim3(threads), smem, stream, args...);
     if (e != cudaSuccess) return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;
+}
+
+template <typename T, int V, int NV, int ROWS>
+conv2d_status_t rows_fwd(const NormArgs<T>& a, cudaStream_t stream)
+{
+    constexpr size_t smem = SampleRing<T, V, NV, ROWS>::smem;
+    static SmemLimit limit;
+    if (raise_smem_limit(reinterpret_cast<const void*>(norm_rows_fwd_kernel<T, V, NV, ROWS>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+    return launched(norm_rows_fwd_kernel<T, V, NV, ROWS>, (long long)ceil_div_u((long long)a.G * a.lanes, kRowThreads) * a.chunks, kRowThreads, smem, 1, stream, a);
+}
+template <typename T, int V, int NV, int ROWS>
+conv2d_status_t rows_bwd(const NormArgs<T>& a, cudaStream_t stream)
+{
+    constexpr size_t smem = 2 * SampleRing<T, V, NV, ROWS>::smem;
+    static SmemLimit limit;
+    if (raise_smem_limit(reinterpret_cast<const void*>(norm_rows_bwd_kernel<T, V, NV, ROWS>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+    return launched(norm_rows_bwd_kernel<T, V, NV, ROWS>, (long long)ceil_div_u((long long)a.G * a.lanes, kRowThreads) * a.chunks, kRowThreads, smem, 1, stream, a);
 }
 
 template <typename T, int V>
@@ -804,11 +908,9 @@ conv2d_status_t fwd(const NormSeq& s, cudaStream_t stream)
     const NormPlan p = make_norm_plan(s.N, s.S, s.C, s.G, sizeof(T), V, false);
     const NormArgs<T> a = make_args<T, V>(s, p);
     if (p.rows) {
-        const long long blocks = (long long)ceil_div_u((long long)s.G * p.lanes, kThreads) * p.chunks;
-        if (p.nv == 1) return launched(norm_rows_fwd_kernel<T, V, 1, 4>, blocks, 0, 1, stream, a);
-        if (p.nv == 2) return launched(norm_rows_fwd_kernel<T, V, 2, 2>, blocks, 0, 1, stream, a);
-        if (p.nv == 4) return launched(norm_rows_fwd_kernel<T, V, 4, 1>, blocks, 0, 1, stream, a);
-        return launched(norm_rows_fwd_kernel<T, V, 8, 1>, blocks, 0, 1, stream, a);
+        if (p.nv == 1) return rows_fwd<T, V, 1, 2>(a, stream);
+        if (p.nv == 2) return rows_fwd<T, V, 2, 1>(a, stream);
+        return rows_fwd<T, V, 4, 1>(a, stream);
     }
     const long long blocks = (long long)s.N * p.tiles * p.parts;
     const size_t fixed = (size_t)p.tile_groups * 16 + (p.tile_groups + 1) / 2 * 16;
@@ -816,14 +918,14 @@ conv2d_status_t fwd(const NormSeq& s, cudaStream_t stream)
         const size_t smem = fixed + slab_bytes(p.part_rows, p.tile_groups * (a.E / V), V * sizeof(T), false);
         static SmemLimit limit;
         if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_fwd_kernel<T, V, kSlab>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-        return launched(norm_slab_fwd_kernel<T, V, kSlab>, blocks, smem, p.parts, stream, a);
+        return launched(norm_slab_fwd_kernel<T, V, kSlab>, blocks, kThreads, smem, p.parts, stream, a);
     }
     const size_t smem = fixed + ring_bytes<T, V>;
     static SmemLimit stats, apply;
     if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_fwd_kernel<T, V, kStreamStats>), smem, stats) != cudaSuccess
         || raise_smem_limit(reinterpret_cast<const void*>(norm_slab_fwd_kernel<T, V, kStreamApply>), smem, apply) != cudaSuccess) return CONV2D_ERR_CUDA;
-    const conv2d_status_t st = launched(norm_slab_fwd_kernel<T, V, kStreamStats>, blocks, smem, 1, stream, a);
-    return st != CONV2D_OK ? st : launched(norm_slab_fwd_kernel<T, V, kStreamApply>, blocks, smem, 1, stream, a);
+    const conv2d_status_t st = launched(norm_slab_fwd_kernel<T, V, kStreamStats>, blocks, kThreads, smem, 1, stream, a);
+    return st != CONV2D_OK ? st : launched(norm_slab_fwd_kernel<T, V, kStreamApply>, blocks, kThreads, smem, 1, stream, a);
 }
 
 template <typename T, int V>
@@ -835,10 +937,9 @@ conv2d_status_t bwd(const NormSeq& s, cudaStream_t stream)
     long long parts = (long long)s.N * p.parts;
     if (p.rows) {
         parts = p.chunks;
-        const long long blocks = (long long)ceil_div_u((long long)s.G * p.lanes, kThreads) * p.chunks;
-        if (p.nv == 1) st = launched(norm_rows_bwd_kernel<T, V, 1, 4>, blocks, 0, 1, stream, a);
-        else if (p.nv == 2) st = launched(norm_rows_bwd_kernel<T, V, 2, 2>, blocks, 0, 1, stream, a);
-        else st = launched(norm_rows_bwd_kernel<T, V, 4, 1>, blocks, 0, 1, stream, a);
+        if (p.nv == 1) st = rows_bwd<T, V, 1, 2>(a, stream);
+        else if (p.nv == 2) st = rows_bwd<T, V, 2, 1>(a, stream);
+        else st = rows_bwd<T, V, 4, 1>(a, stream);
     } else {
         const long long blocks = (long long)s.N * p.tiles * p.parts;
         const size_t fixed = (size_t)p.tile_groups * 16 + (p.tile_groups + 1) / 2 * 16, sums = sizeof(float) * 2 * kThreads * V;
@@ -846,14 +947,14 @@ conv2d_status_t bwd(const NormSeq& s, cudaStream_t stream)
             const size_t smem = fixed + sums + slab_bytes(p.part_rows, p.tile_groups * (a.E / V), V * sizeof(T), true);
             static SmemLimit limit;
             if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_bwd_kernel<T, V, kSlab>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-            st = launched(norm_slab_bwd_kernel<T, V, kSlab>, blocks, smem, p.parts, stream, a);
+            st = launched(norm_slab_bwd_kernel<T, V, kSlab>, blocks, kThreads, smem, p.parts, stream, a);
         } else {
             const size_t first = fixed + sums + 2 * ring_bytes<T, V>, second = fixed + 2 * ring_bytes<T, V>;
             static SmemLimit stats, apply;
             if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_bwd_kernel<T, V, kStreamStats>), first, stats) != cudaSuccess
                 || raise_smem_limit(reinterpret_cast<const void*>(norm_slab_bwd_kernel<T, V, kStreamApply>), second, apply) != cudaSuccess) return CONV2D_ERR_CUDA;
-            st = launched(norm_slab_bwd_kernel<T, V, kStreamStats>, blocks, first, 1, stream, a);
-            if (st == CONV2D_OK) st = launched(norm_slab_bwd_kernel<T, V, kStreamApply>, blocks, second, 1, stream, a);
+            st = launched(norm_slab_bwd_kernel<T, V, kStreamStats>, blocks, kThreads, first, 1, stream, a);
+            if (st == CONV2D_OK) st = launched(norm_slab_bwd_kernel<T, V, kStreamApply>, blocks, kThreads, second, 1, stream, a);
         }
     }
     if (st != CONV2D_OK || !a.channels) return st;
