@@ -25,7 +25,7 @@ namespace cg = cooperative_groups;
 
 constexpr int kRowThreads = 256;        // rows
 constexpr int kThreads = 256, kWarps = kThreads / 32;        // slab, stream
-constexpr int kGroup = 2, kRing = 8;    // rows of a group (four take the backward pass to 240 registers), groups of a ring
+constexpr int kGroup = 2, kRing = 4;    // rows of a group (four take the backward pass to 240 registers), groups of a ring
 
 template <typename T>
 struct NormArgs {
@@ -394,6 +394,9 @@ __device__ __forceinline__ void group_sums(const Part<T, V>& p, int gi, float (&
 
 enum { kSlab = 0, kStreamStats = 1, kStreamApply = 2 };
 
+// Slots that a thread needs for its rows: whole groups.
+__host__ __device__ constexpr int thread_slots(int rows) { return (rows + kGroup - 1) / kGroup * kGroup; }
+
 // The packs of one tensor that a thread takes: rows first, first + step, .. of its channels.  A slab's stay in shared memory, all under way at once;
 // a stream's go through a ring.
 template <typename T, int V, bool KEEP>
@@ -416,7 +419,8 @@ struct ThreadRows {
     }
     __device__ Pack<T, V> get(int q, int i, int j) const
     {
-        if (KEEP) return *reinterpret_cast<const Pack<T, V>*>(ring.mine + (size_t)(i + j < count ? i + j : 0) * (kThreads * bytes));
+        // (slots are there for whole groups; what lies behind the last row is not used)
+        if (KEEP) return *reinterpret_cast<const Pack<T, V>*>(ring.mine + i * (kThreads * bytes) + j * (kThreads * bytes));
         return ring.get(q, i, j, count);
     }
 };
@@ -466,7 +470,7 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
         Rows r;
         r.count = p.count_of(q);
         // (turns take whole rows: a part's rows each)
-        r.ring = {rows + ((KEEP ? q * a.part_rows * kThreads : 0) + threadIdx.x) * Rows::bytes, x + (r.count ? p.pack_of(q) * V : 0), p.step * a.ldx};
+        r.ring = {rows + ((KEEP ? q * thread_slots(a.part_rows) * kThreads : 0) + threadIdx.x) * Rows::bytes, x + (r.count ? p.pack_of(q) * V : 0), p.step * a.ldx};
         return r;
     };
 
@@ -590,7 +594,7 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
 }
 
 template <typename T, int V, int MODE>
-__global__ void __launch_bounds__(kThreads) norm_slab_bwd_kernel(const NormArgs<T> a)
+__global__ void __launch_bounds__(kThreads, 2) norm_slab_bwd_kernel(const NormArgs<T> a)
 {
     constexpr int P = kPairs<V>;
     constexpr bool KEEP = MODE == kSlab;
@@ -603,7 +607,7 @@ __global__ void __launch_bounds__(kThreads) norm_slab_bwd_kernel(const NormArgs<
     unsigned char* rows = reinterpret_cast<unsigned char*>(csum + (MODE == kStreamApply ? 0 : 2 * kThreads * V));
     const Part<T, V> p(a);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int g0 = p.g0, width = p.packs * V, kept = KEEP ? (p.turns == 1 ? (a.part_rows + p.step - 1) / p.step : a.part_rows) : 0;
+    const int g0 = p.g0, width = p.packs * V, kept = KEEP ? thread_slots(p.turns == 1 ? (a.part_rows + p.step - 1) / p.step : a.part_rows) : 0;
     const T* x = a.x + (p.n * a.S + p.first) * a.ldx + p.c0;
     const T* dy = a.dy + (p.n * a.S + p.first) * a.lddy + p.c0;
     using Rows = ThreadRows<T, V, KEEP>;
@@ -766,7 +770,7 @@ constexpr int kMaxCluster = 8, kSms = 148;
 size_t slab_bytes(int part_rows, int packs, int pack_bytes, bool bwd)
 {
     const int step = packs <= kThreads ? kThreads / packs : 1, turns = packs <= kThreads ? 1 : (packs + kThreads - 1) / kThreads;
-    return (size_t)((part_rows + step - 1) / step) * turns * kThreads * pack_bytes * (bwd ? 2 : 1);
+    return (size_t)thread_slots((part_rows + step - 1) / step) * turns * kThreads * pack_bytes * (bwd ? 2 : 1);
 }
 
 // How a call is cut.  The sizes decide, and whether rows can be moved in packs of 16 bytes; the workspace has room for either.
@@ -805,24 +809,26 @@ NormPlan make_norm_plan(int N, int S, int C, int G, int esize, int V, bool bwd)
         return n;
     };
     int parts = 1;
-    const size_t slab_limit = (size_t)env_int("CONV2D_B200_NORM_SLAB_KB", (int)(kSlabBytes >> 10)) << 10;
-    for (int bytes = env_int("CONV2D_B200_NORM_ROW", 128); bytes >= 32; bytes /= 2) {
+    for (int bytes = 128; bytes >= 32; bytes /= 2) {
         p.tile_groups = tile(bytes);
         p.tiles = (G + p.tile_groups - 1) / p.tile_groups;
         // a cluster of the fewest blocks that hold the slab; more while there are SMs left and rows to share out
         const auto need = [&](int n) { return slab_bytes((S + n - 1) / n, p.tile_groups * ev, V * esize, bwd); };
         parts = 1;
-        while (parts < kMaxCluster && need(parts) > slab_limit) parts *= 2;
-        p.slab = need(parts) <= slab_limit;
+        while (parts < kMaxCluster && need(parts) > kSlabBytes) parts *= 2;
+        p.slab = need(parts) <= kSlabBytes;
         if (p.slab) break;
     }
-    if (!p.slab) p.tile_groups = tile(128), p.tiles = (G + p.tile_groups - 1) / p.tile_groups;
-    const long long slabs = (long long)N * p.tiles;
-    while (p.slab && parts < kMaxCluster && slabs * parts < 4 * kSms && S / parts >= 32) parts *= 2;
-    if (p.slab && slabs * parts < kSms / 2 && (double)S * p.tile_groups * E * esize * slabs > 4e6) p.slab = false;
+    while (p.slab && parts < kMaxCluster && (long long)N * p.tiles * parts < kSms && S / parts >= 64) parts *= 2;
+    // Large tensors are faster as a stream (32 x 3136 x 256 in bf16, forward and backward: 99 us, as slabs 138), whose second reading L2
+    // serves in part; slabs save a launch and the reading below that (4 x 1024 x 256: 8 us forward, 10 as a stream).
+    const int choice = env_int("CONV2D_B200_NORM_STREAM", 0);
+    if (choice == 0 ? (size_t)N * S * C * esize > (bwd ? 16u : 24u) << 20 : choice > 0) p.slab = false;
     if (!p.slab) {
-        const long long want = (8LL * kSms + slabs - 1) / slabs;
-        parts = (int)(want < 1 ? 1 : want > 1024 ? 1024 : want);
+        p.tile_groups = tile(128), p.tiles = (G + p.tile_groups - 1) / p.tile_groups;
+        // two blocks an SM (one of the backward pass): more are more beginnings and endings
+        const long long slabs = (long long)N * p.tiles, want = ((bwd ? 1LL : 2LL) * kSms + slabs - 1) / slabs;
+        parts = (int)(want > 1024 ? 1024 : want);
         if (parts > (S + 15) / 16) parts = (S + 15) / 16;
     }
     p.part_rows = (S + parts - 1) / parts;
@@ -837,7 +843,7 @@ size_t workspace_floats(int N, int S, int C, int G, bool bwd)
 {
     size_t most = 0;
     for (int esize = 2; esize <= 4; esize += 2)
-        for (int V = 1; V <= 16 / esize; V = V == 1 ? 16 / esize : 17) {
+        for (int V = 1; V <= 16 / esize; V *= 2) {
             if ((C / G) % V) continue;
             const NormPlan p = make_norm_plan(N, S, C, G, esize, V, bwd);
             if (p.stats + p.channels > most) most = p.stats + p.channels;
@@ -961,17 +967,31 @@ conv2d_status_t bwd(const NormSeq& s, cudaStream_t stream)
     return launch_column_sums(a.channels, parts, 2LL * s.C, 2LL * s.C, ParamStore{s.dgamma, s.dbeta, s.C}, stream);
 }
 
-// Packs of 16 bytes where every row of every tensor begins on such a boundary and no pack crosses from one group to the next.
+// The widest packs, up to 16 bytes, in which no pack crosses from one group to the next and every row of every tensor begins on a boundary of them.
 template <typename T>
-bool wide(const NormSeq& s)
+bool packs_of(const NormSeq& s, int V)
 {
-    constexpr int e = sizeof(T), V = 16 / e;
-    return (s.C / s.G) % V == 0 && rows_aligned(s.x, s.ldx, e, 16) && rows_aligned(s.y, s.ldy, e, 16) && rows_aligned(s.dy, s.lddy, e, 16)
-        && rows_aligned(s.dx, s.lddx, e, 16);
+    constexpr int e = sizeof(T);
+    return (s.C / s.G) % V == 0 && rows_aligned(s.x, s.ldx, e, V * e) && rows_aligned(s.y, s.ldy, e, V * e) && rows_aligned(s.dy, s.lddy, e, V * e)
+        && rows_aligned(s.dx, s.lddx, e, V * e);
 }
 
-template <typename T> conv2d_status_t fwd_typed(const NormSeq& s, cudaStream_t st) { return wide<T>(s) ? fwd<T, 16 / sizeof(T)>(s, st) : fwd<T, 1>(s, st); }
-template <typename T> conv2d_status_t bwd_typed(const NormSeq& s, cudaStream_t st) { return wide<T>(s) ? bwd<T, 16 / sizeof(T)>(s, st) : bwd<T, 1>(s, st); }
+template <typename T>
+conv2d_status_t fwd_typed(const NormSeq& s, cudaStream_t stream)
+{
+    if constexpr (sizeof(T) == 2)
+        if (packs_of<T>(s, 8)) return fwd<T, 8>(s, stream);
+    if (packs_of<T>(s, 4)) return fwd<T, 4>(s, stream);
+    return packs_of<T>(s, 2) ? fwd<T, 2>(s, stream) : fwd<T, 1>(s, stream);
+}
+template <typename T>
+conv2d_status_t bwd_typed(const NormSeq& s, cudaStream_t stream)
+{
+    if constexpr (sizeof(T) == 2)
+        if (packs_of<T>(s, 8)) return bwd<T, 8>(s, stream);
+    if (packs_of<T>(s, 4)) return bwd<T, 4>(s, stream);
+    return packs_of<T>(s, 2) ? bwd<T, 2>(s, stream) : bwd<T, 1>(s, stream);
+}
 
 }  // namespace
 

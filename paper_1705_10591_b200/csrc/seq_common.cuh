@@ -107,7 +107,7 @@ __device__ __forceinline__ void times_slope(float (&g)[N], const float (&v)[N], 
 
 // Asynchronous copy of BYTES (4, 8 or 16) into shared memory; zeros where `real` is false (the address is not read then).
 template <int BYTES>
-__device__ __forceinline__ void copy_async(void* to, const void* from, bool real)
+__device__ __forceinline__ void copy_async(void* to, const void* from, bool real = true)
 {
     const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
     if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(real ? 16 : 0) : "memory");
@@ -128,18 +128,23 @@ struct RowRing {
     unsigned char* mine;
     const T* p;                         // row 0, this thread's channels
     long long ld;
+    // copies of rows t .. t + GROUP - 1, those from `live` on as zeros
     __device__ void issue(int q, int t, int live) const
     {
         if (!async) return;
+        const T* from = p + (long long)t * ld;
+        unsigned char* to = mine + (q & (RING - 1)) * (GROUP * THREADS * bytes);
+        if (t + GROUP <= live) {
 #pragma unroll
-        for (int j = 0; j < GROUP; ++j) {
-            const bool real = t + j < live;
-            copy_async<async ? bytes : 4>(mine + (size_t)((q & (RING - 1)) * GROUP + j) * THREADS * bytes, p + (real ? (t + j) * ld : 0), real);
+            for (int j = 0; j < GROUP; ++j, from += ld) copy_async<async ? bytes : 4>(to + j * (THREADS * bytes), from, true);
+        } else {
+#pragma unroll
+            for (int j = 0; j < GROUP; ++j, from += ld) copy_async<async ? bytes : 4>(to + j * (THREADS * bytes), t + j < live ? from : p, t + j < live);
         }
     }
     __device__ Pack<T, V> get(int q, int t, int j, int live) const
     {
-        if (async) return *reinterpret_cast<const Pack<T, V>*>(mine + (size_t)((q & (RING - 1)) * GROUP + j) * THREADS * bytes);
+        if (async) return *reinterpret_cast<const Pack<T, V>*>(mine + (q & (RING - 1)) * (GROUP * THREADS * bytes) + j * (THREADS * bytes));
         return t + j < live ? load_pack<T, V>(p + (t + j) * ld) : zero_pack<T, V>();
     }
 };
