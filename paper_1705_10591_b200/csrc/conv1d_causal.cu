@@ -138,6 +138,7 @@ struct BwdArgs {
     int act;
 };
 
+constexpr int kBwdGroup = 2, kBwdRing = 4;     // (groups of four rows take 168 registers, three blocks an SM: 130 us on 4 x 4096 x 4096)
 constexpr int kBwdRows = 64;            // rows of a piece: K-1 rows of x before and K-1 of both inputs after it are read again
 
 template <typename T, int V, int K>
@@ -146,7 +147,7 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
     constexpr int P = kPairs<V>;
     ptx::grid_dep_wait();
     extern __shared__ float4 smem4[];   // the rings, then the sums [blockDim.y][K+1][blockDim.x * V]
-    using Ring = RowRing<T, V, kThreads, kGroup, kRing>;
+    using Ring = RowRing<T, V, kThreads, kBwdGroup, kBwdRing>;
     const int tid = threadIdx.y * blockDim.x + threadIdx.x;
     const int pk = blockIdx.y * blockDim.x + threadIdx.x, c = pk * V;
     float2 dw[K][P], db[P], w[K][P], bias[P];
@@ -169,12 +170,12 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
         const int first = piece == 0 && a.dstate_in ? -(K - 1) : t0;
         const int stop = min(t1, len), end = stop + K - 1;    // t walks the rows of g; the row of dx that it completes is t-(K-1)
 #pragma unroll
-        for (int q = 0; q < kRing - 1; ++q) {
-            x.issue(q, t0 + q * kGroup, len);
-            dy.issue(q, t0 + q * kGroup, len);
+        for (int q = 0; q < kBwdRing - 1; ++q) {
+            x.issue(q, t0 + q * kBwdGroup, len);
+            dy.issue(q, t0 + q * kBwdGroup, len);
             copies_commit();
         }
-        float2 xw[kGroup + K - 1][P], gw[kGroup + K - 1][P];  // rows t-(K-1) .. t+3 of xe and of g
+        float2 xw[kBwdGroup + K - 1][P], gw[kBwdGroup + K - 1][P];  // rows t-(K-1) .. t+3 of xe and of g
 #pragma unroll
         for (int k = 0; k < K - 1; ++k) {
             const int t = t0 - (K - 1) + k;
@@ -187,22 +188,22 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
         }
         int q = 0;
 #pragma unroll 1
-        for (int t = t0; t < end; t += kGroup, ++q) {
-            copies_wait<kRing - 2>();
-            float g[kGroup * 2 * P], pre[kGroup * 2 * P];
+        for (int t = t0; t < end; t += kBwdGroup, ++q) {
+            copies_wait<kBwdRing - 2>();
+            float g[kBwdGroup * 2 * P], pre[kBwdGroup * 2 * P];
 #pragma unroll
-            for (int j = 0; j < kGroup; ++j) {
+            for (int j = 0; j < kBwdGroup; ++j) {
                 float2 gi[P];
                 pairs<T, V>(x.get(q, t, j, len), xw[K - 1 + j]);
                 pairs<T, V>(dy.get(q, t, j, len), gi);        // (zero behind the sequence)
 #pragma unroll
                 for (int i = 0; i < P; ++i) g[2 * (j * P + i)] = gi[i].x, g[2 * (j * P + i) + 1] = gi[i].y;
             }
-            x.issue(q + kRing - 1, t + (kRing - 1) * kGroup, len);
-            dy.issue(q + kRing - 1, t + (kRing - 1) * kGroup, len);
+            x.issue(q + kBwdRing - 1, t + (kBwdRing - 1) * kBwdGroup, len);
+            dy.issue(q + kBwdRing - 1, t + (kBwdRing - 1) * kBwdGroup, len);
             copies_commit();
 #pragma unroll
-            for (int j = 0; j < kGroup; ++j) {
+            for (int j = 0; j < kBwdGroup; ++j) {
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
                     float2 s = bias[i];
@@ -212,21 +213,21 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
                 }
             }
             times_slope(g, pre, a.act);
-            if (t + kGroup > len) {     // behind the sequence an overflowing slope must not make zeros NaN
+            if (t + kBwdGroup > len) {     // behind the sequence an overflowing slope must not make zeros NaN
 #pragma unroll
-                for (int j = 0; j < kGroup; ++j)
+                for (int j = 0; j < kBwdGroup; ++j)
 #pragma unroll
                     for (int i = 0; i < 2 * P; ++i)
                         if (t + j >= len) g[2 * j * P + i] = 0.f;
             }
 #pragma unroll
-            for (int j = 0; j < kGroup; ++j)
+            for (int j = 0; j < kBwdGroup; ++j)
 #pragma unroll
                 for (int i = 0; i < P; ++i) gw[K - 1 + j][i] = make_float2(g[2 * (j * P + i)], g[2 * (j * P + i) + 1]);
             // each row of g counts once, in its own piece
-            if (t + kGroup <= stop) {
+            if (t + kBwdGroup <= stop) {
 #pragma unroll
-                for (int j = 0; j < kGroup; ++j)
+                for (int j = 0; j < kBwdGroup; ++j)
 #pragma unroll
                     for (int i = 0; i < P; ++i) {
                         db[i] = __fadd2_rn(db[i], gw[K - 1 + j][i]);
@@ -235,7 +236,7 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
                     }
             } else {
 #pragma unroll
-                for (int j = 0; j < kGroup; ++j) {
+                for (int j = 0; j < kBwdGroup; ++j) {
                     if (t + j >= stop) break;
 #pragma unroll
                     for (int i = 0; i < P; ++i) {
@@ -246,7 +247,7 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
                 }
             }
 #pragma unroll
-            for (int j = 0; j < kGroup; ++j) {
+            for (int j = 0; j < kBwdGroup; ++j) {
                 const int td = t + j - (K - 1);
                 if (td < first || td >= stop) continue;
                 float2 out[P];
@@ -268,7 +269,7 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
 #pragma unroll
             for (int k = 0; k < K - 1; ++k)
 #pragma unroll
-                for (int i = 0; i < P; ++i) xw[k][i] = xw[kGroup + k][i], gw[k][i] = gw[kGroup + k][i];
+                for (int i = 0; i < P; ++i) xw[k][i] = xw[kBwdGroup + k][i], gw[k][i] = gw[kBwdGroup + k][i];
         }
         copies_wait<0>();               // (the ring is free for the next piece)
         for (int t = max(t0, len); t < t1; ++t) store_pack(dx + t * a.lddx, zero_pack<T, V>());
@@ -359,7 +360,7 @@ conv2d_status_t bwd(const ConvSeq& s, cudaStream_t stream)
     a.pieces = p.pieces, a.packs = s.D / V, a.jobs = (unsigned)p.jobs;
     a.partials = s.dw || s.dbias ? s.partials : nullptr;
     if (p.across > 65535 || p.jobs > 0x7fff0000LL) return CONV2D_ERR_SHAPE;
-    const size_t rings = 2 * RowRing<T, V, kThreads, kGroup, kRing>::smem, sums = (size_t)kThreads * V * (K + 1) * sizeof(float), smem = rings > sums ? rings : sums;
+    const size_t rings = 2 * RowRing<T, V, kThreads, kBwdGroup, kBwdRing>::smem, sums = (size_t)kThreads * V * (K + 1) * sizeof(float), smem = rings > sums ? rings : sums;
     static SmemLimit limit;
     if (raise_smem_limit(reinterpret_cast<const void*>(conv1d_bwd_kernel<T, V, K>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
     if (launch_pdl(conv1d_bwd_kernel<T, V, K>, dim3((unsigned)p.parts, (unsigned)p.across), dim3(p.tx, p.ty), smem, stream, a) != cudaSuccess)

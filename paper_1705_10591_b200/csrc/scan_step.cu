@@ -7,7 +7,8 @@ namespace {
 constexpr int kSpt = 4;                 // states of a thread
 
 // One token: every state is read and written once, which is all the time there is.  A thread takes four adjacent states of one
-// channel, for ROWS sequences at once (their loads are under way together, and A is loaded once for all).
+// channel, of one sequence, or of four at once where there are many (their loads are under way together, A is loaded once for all, and each
+// of the lanes of a channel does for one of the sequences what is done once for a channel: step size, gate, output).
 template <typename T>
 struct StepArgs {
     const T *u, *delta, *Bm, *Cm, *z;
@@ -17,79 +18,91 @@ struct StepArgs {
     int B, D, N, G, E, NL;
     unsigned across;                    // blocks for the channels of ROWS sequences
     long long ldu, lddelta, ldB, ldC, ldz, ldy;
-    bool softplus;
+    bool softplus, B_wide, C_wide;
 };
+
+// Four adjacent floats of which `real` exist.
+template <bool QUADS>
+__device__ __forceinline__ void load_states(const float* p, int real, float (&v)[kSpt])
+{
+    if (QUADS) {
+        const float4 q = real > 0 ? *reinterpret_cast<const float4*>(p) : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kSpt; ++i) v[i] = i < real ? p[i] : 0.f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void load_inputs(const T* p, int real, bool wide, float (&v)[kSpt])
+{
+    if (wide) {
+        unpack(real > 0 ? load_pack<T, kSpt>(p) : zero_pack<T, kSpt>(), v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kSpt; ++i) v[i] = i < real ? to_float(p[i]) : 0.f;
+    }
+}
 
 template <typename T, int ROWS, bool QUADS>
 __global__ void __launch_bounds__(128) scan_step_kernel(const StepArgs<T> a)
 {
     ptx::grid_dep_wait();
     const unsigned id = blockIdx.x % a.across * 128 + threadIdx.x;
-    const int n0 = (int)(id % a.NL) * kSpt;
+    const int sl = (int)(id % a.NL), n0 = sl * kSpt;
     const bool mine = id / a.NL < (unsigned)a.D;
-    const int d = mine ? (int)(id / a.NL) : 0, g = d / a.E;
+    const int d = mine ? (int)(id / a.NL) : 0, g = d / a.E, real = mine ? a.N - n0 : 0;
     const long long b0 = (long long)(blockIdx.x / a.across) * ROWS;
-    float A2[kSpt] = {}, h[ROWS][kSpt] = {}, Bv[ROWS][kSpt] = {}, Cv[ROWS][kSpt] = {}, u[ROWS], s[ROWS], z[ROWS];
-    auto quad = [&](const float* p, float (&v)[kSpt]) {
-        if (!mine) return;
-        if (QUADS) {
-            if (n0 < a.N) {
-                const float4 q = *reinterpret_cast<const float4*>(p + n0);
-                v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kSpt; ++i)
-                if (n0 + i < a.N) v[i] = p[n0 + i];
-        }
-    };
+    // ROWS = 4 (a channel has four lanes or more): this lane's own sequence is b0 + sl % 4
+    const int lane = threadIdx.x & 31, own = ROWS > 1 ? sl % ROWS : 0;
+    const long long bo = b0 + own < a.B ? b0 + own : b0;
+    float h[ROWS][kSpt], Bv[ROWS][kSpt], Cv[ROWS][kSpt], A2[kSpt];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         const long long b = b0 + r;
-        u[r] = s[r] = z[r] = 0.f;
-        if (b >= a.B || !mine) continue;
-        quad(a.state_in + ((size_t)b * a.D + d) * a.N, h[r]);
-        u[r] = to_float(a.u[b * a.ldu + d]);
-        s[r] = to_float(a.delta[b * a.lddelta + d]);
-        if (a.z) z[r] = to_float(a.z[b * a.ldz + d]);
-#pragma unroll
-        for (int i = 0; i < kSpt; ++i) {
-            if (n0 + i >= a.N) continue;
-            Bv[r][i] = to_float(a.Bm[b * a.ldB + g * a.N + n0 + i]);
-            Cv[r][i] = to_float(a.Cm[b * a.ldC + g * a.N + n0 + i]);
-        }
+        const int there = b < a.B ? real : 0;
+        load_states<QUADS>(a.state_in + ((size_t)b * a.D + d) * a.N + n0, there, h[r]);
+        load_inputs(a.Bm + b * a.ldB + (long long)g * a.N + n0, there, a.B_wide, Bv[r]);
+        load_inputs(a.Cm + b * a.ldC + (long long)g * a.N + n0, there, a.C_wide, Cv[r]);
     }
-    quad(a.A + (size_t)d * a.N, A2);
+    load_states<QUADS>(a.A + (size_t)d * a.N + n0, real, A2);
+    const float u = mine ? to_float(a.u[bo * a.ldu + d]) : 0.f, z = mine && a.z ? to_float(a.z[bo * a.ldz + d]) : 0.f;
+    float s = mine ? to_float(a.delta[bo * a.lddelta + d]) : 0.f;
+    if (a.delta_bias && mine) s += a.delta_bias[d];
+    if (a.softplus) s = softplus(s);
+    const float su = s * u, skip = a.Dskip && mine ? a.Dskip[d] : 0.f;
 #pragma unroll
     for (int i = 0; i < kSpt; ++i) A2[i] *= kLog2e;
-    const float bias = a.delta_bias && mine ? a.delta_bias[d] : 0.f, skip = a.Dskip && mine ? a.Dskip[d] : 0.f;
+    float v[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-        const long long b = b0 + r;
-        s[r] += bias;
-        if (a.softplus) s[r] = softplus(s[r]);
-        float v = 0.f;
+        const int from = (lane & ~(ROWS - 1)) | r;
+        const float sr = ROWS > 1 ? __shfl_sync(0xffffffffu, s, from) : s, sur = ROWS > 1 ? __shfl_sync(0xffffffffu, su, from) : su;
+        v[r] = 0.f;
 #pragma unroll
-        for (int i = 0; i < kSpt; ++i) {
-            h[r][i] = fmaf(ex2(s[r] * A2[i]), h[r][i], s[r] * u[r] * Bv[r][i]);
-            v = fmaf(Cv[r][i], h[r][i], v);
+        for (int i = 0; i < kSpt; i += 2) {
+            const float2 e = decay(both(sr), make_float2(A2[i], A2[i + 1]));
+            const float2 x = __ffma2_rn(e, make_float2(h[r][i], h[r][i + 1]), __fmul2_rn(both(sur), make_float2(Bv[r][i], Bv[r][i + 1])));
+            h[r][i] = x.x, h[r][i + 1] = x.y;
+            v[r] = fmaf(Cv[r][i], x.x, v[r]);
+            v[r] = fmaf(Cv[r][i + 1], x.y, v[r]);
         }
-        for (int m = 1; m < a.NL; m *= 2) v += __shfl_xor_sync(0xffffffffu, v, m);
-        if (b >= a.B || !mine) continue;
-        float* out = a.state_out + ((size_t)b * a.D + d) * a.N;
+        if (b0 + r >= a.B || real <= 0) continue;
+        float* out = a.state_out + ((size_t)(b0 + r) * a.D + d) * a.N + n0;
         if (QUADS) {
-            if (n0 < a.N) *reinterpret_cast<float4*>(out + n0) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
+            *reinterpret_cast<float4*>(out) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
         } else {
 #pragma unroll
             for (int i = 0; i < kSpt; ++i)
-                if (n0 + i < a.N) out[n0 + i] = h[r][i];
-        }
-        if (n0 == 0) {
-            v = fmaf(skip, u[r], v);
-            if (a.z) v *= z[r] * sigmoid(z[r]);
-            a.y[b * a.ldy + d] = from_float<T>(v);
+                if (i < real) out[i] = h[r][i];
         }
     }
+    if (ROWS > 1) sum_over_lanes<ROWS, ROWS, 1>(v, lane);     // leaves the sum of this lane's own sequence
+    for (int m = ROWS; m < a.NL; m *= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], m);
+    if (sl >= ROWS || !mine || b0 + own >= a.B) return;
+    float y = fmaf(skip, u, v[0]);
+    if (a.z) y *= z * sigmoid(z);
+    a.y[(b0 + own) * a.ldy + d] = from_float<T>(y);
 }
 
 template <typename T, int ROWS, bool QUADS>
@@ -113,8 +126,9 @@ conv2d_status_t step_typed(const ScanSeq& s, cudaStream_t stream)
     a.B = s.B, a.D = s.D, a.N = s.N, a.G = s.G, a.E = s.D / s.G, a.NL = lanes_for(s.N, kSpt);
     a.ldu = s.ldu, a.lddelta = s.lddelta, a.ldB = s.ldB, a.ldC = s.ldC, a.ldz = s.ldz, a.ldy = s.ldy, a.softplus = s.softplus;
     const bool quads = s.N % 4 == 0 && rows_aligned(s.A, 4, 4, 16) && rows_aligned(s.state_in, 4, 4, 16) && rows_aligned(s.state_out, 4, 4, 16);
-    // four sequences a thread once one each would be more threads than the machine holds
-    const bool many = (long long)s.B * s.D * a.NL > (long long)sm_count() * 2048;
+    a.B_wide = s.N % kSpt == 0 && rows_aligned(s.Bm, s.ldB, sizeof(T), kSpt * sizeof(T)), a.C_wide = s.N % kSpt == 0 && rows_aligned(s.Cm, s.ldC, sizeof(T), kSpt * sizeof(T));
+    // four sequences a thread once one each would be more threads than the machine holds (and a channel has four lanes to share them)
+    const bool many = a.NL >= 4 && (long long)s.B * s.D * a.NL > (long long)sm_count() * 2048;
     if (quads) return many ? step<T, 4, true>(a, stream) : step<T, 1, true>(a, stream);
     return many ? step<T, 4, false>(a, stream) : step<T, 1, false>(a, stream);
 }
