@@ -14,6 +14,10 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kGroup = 4, kRing = 4;    // rows of a group, groups of the ring
+
+// Groups of rows all of which are there, and others: two versions of a loop's body.
+struct Whole { static constexpr bool value = true; };
+struct Cut { static constexpr bool value = false; };
 // w[k][pair], bias[pair] of the channels from c on
 template <typename T, int V, int K>
 __device__ __forceinline__ void load_taps(const T* w, const T* bias, int c, float2 (&wt)[K][kPairs<V>], float2 (&bt)[kPairs<V>])
@@ -87,9 +91,8 @@ __global__ void __launch_bounds__(kThreads) conv1d_fwd_kernel(const FwdArgs<T> a
 #pragma unroll
         for (int k = 0; k < K - 1; ++k) store_pack(a.state_out + ((size_t)b * (K - 1) + k) * a.D + c, last[k]);
     }
-    int q = 0;
-#pragma unroll 1
-    for (int t = t0; t < live; t += kGroup, ++q) {
+    T* to = y + (long long)t0 * a.ldy;
+    auto group = [&](int q, int t, auto whole) {
         copies_wait<kRing - 2>();
 #pragma unroll
         for (int j = 0; j < kGroup; ++j) pairs<T, V>(x.get(q, t, j, live), win[K - 1 + j]);
@@ -108,17 +111,21 @@ __global__ void __launch_bounds__(kThreads) conv1d_fwd_kernel(const FwdArgs<T> a
         }
         activate(out, a.act);
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j) {
+        for (int j = 0; j < kGroup; ++j, to += a.ldy) {
             float2 o[P];
 #pragma unroll
             for (int i = 0; i < P; ++i) o[i] = make_float2(out[2 * (j * P + i)], out[2 * (j * P + i) + 1]);
-            if (t + j < live) store_pack(y + (t + j) * a.ldy, pack_of<T, V>(o));
+            if (decltype(whole)::value || t + j < live) store_pack(to, pack_of<T, V>(o));
         }
 #pragma unroll
         for (int k = 0; k < K - 1; ++k)
 #pragma unroll
             for (int i = 0; i < P; ++i) win[k][i] = win[kGroup + k][i];
-    }
+    };
+    int q = 0, t = t0;
+#pragma unroll 1
+    for (; t + kGroup <= live; t += kGroup, ++q) group(q, t, Whole());
+    if (t < live) group(q, t, Cut());
     for (int t = max(t0, len); t < t1; ++t) store_pack(y + t * a.ldy, zero_pack<T, V>());
 }
 
@@ -138,7 +145,7 @@ struct BwdArgs {
     int act;
 };
 
-constexpr int kBwdGroup = 2, kBwdRing = 4;     // (groups of four rows take 168 registers, three blocks an SM: 130 us on 4 x 4096 x 4096)
+constexpr int kBwdGroup = 2, kBwdRing = 4;     // (groups of four rows: 130 us on 4 x 4096 x 4096, 122 so)
 constexpr int kBwdRows = 64;            // rows of a piece: K-1 rows of x before and K-1 of both inputs after it are read again
 
 template <typename T, int V, int K>
@@ -186,9 +193,7 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
 #pragma unroll
             for (int i = 0; i < P; ++i) gw[k][i] = both(0.f);
         }
-        int q = 0;
-#pragma unroll 1
-        for (int t = t0; t < end; t += kBwdGroup, ++q) {
+        auto group = [&](int q, int t, auto whole) {
             copies_wait<kBwdRing - 2>();
             float g[kBwdGroup * 2 * P], pre[kBwdGroup * 2 * P];
 #pragma unroll
@@ -213,7 +218,7 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
                 }
             }
             times_slope(g, pre, a.act);
-            if (t + kBwdGroup > len) {     // behind the sequence an overflowing slope must not make zeros NaN
+            if (!decltype(whole)::value) {      // behind the sequence an overflowing slope must not make zeros NaN
 #pragma unroll
                 for (int j = 0; j < kBwdGroup; ++j)
 #pragma unroll
@@ -221,35 +226,23 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
                         if (t + j >= len) g[2 * j * P + i] = 0.f;
             }
 #pragma unroll
-            for (int j = 0; j < kBwdGroup; ++j)
+            for (int j = 0; j < kBwdGroup; ++j) {
 #pragma unroll
                 for (int i = 0; i < P; ++i) gw[K - 1 + j][i] = make_float2(g[2 * (j * P + i)], g[2 * (j * P + i) + 1]);
-            // each row of g counts once, in its own piece
-            if (t + kBwdGroup <= stop) {
+                // each row of g counts once, in its own piece
+                if (!decltype(whole)::value && t + j >= stop) continue;
 #pragma unroll
-                for (int j = 0; j < kBwdGroup; ++j)
+                for (int i = 0; i < P; ++i) {
+                    db[i] = __fadd2_rn(db[i], gw[K - 1 + j][i]);
 #pragma unroll
-                    for (int i = 0; i < P; ++i) {
-                        db[i] = __fadd2_rn(db[i], gw[K - 1 + j][i]);
-#pragma unroll
-                        for (int k = 0; k < K; ++k) dw[k][i] = __ffma2_rn(gw[K - 1 + j][i], xw[j + k][i], dw[k][i]);
-                    }
-            } else {
-#pragma unroll
-                for (int j = 0; j < kBwdGroup; ++j) {
-                    if (t + j >= stop) break;
-#pragma unroll
-                    for (int i = 0; i < P; ++i) {
-                        db[i] = __fadd2_rn(db[i], gw[K - 1 + j][i]);
-#pragma unroll
-                        for (int k = 0; k < K; ++k) dw[k][i] = __ffma2_rn(gw[K - 1 + j][i], xw[j + k][i], dw[k][i]);
-                    }
+                    for (int k = 0; k < K; ++k) dw[k][i] = __ffma2_rn(gw[K - 1 + j][i], xw[j + k][i], dw[k][i]);
                 }
             }
+            T* to = dx + (long long)(t - (K - 1)) * a.lddx;
 #pragma unroll
-            for (int j = 0; j < kBwdGroup; ++j) {
+            for (int j = 0; j < kBwdGroup; ++j, to += a.lddx) {
                 const int td = t + j - (K - 1);
-                if (td < first || td >= stop) continue;
+                if (!decltype(whole)::value && (td < first || td >= stop)) continue;
                 float2 out[P];
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
@@ -257,20 +250,33 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
 #pragma unroll
                     for (int k = 1; k < K; ++k) out[i] = __ffma2_rn(w[k][i], gw[j + K - 1 - k][i], out[i]);
                 }
+                if (decltype(whole)::value) {
+                    store_pack(to, pack_of<T, V>(out));
+                    continue;
+                }
                 if (a.dstate_out && td >= len - (K - 1)) {
                     float2 e[P];
                     pairs<T, V>(load_pack<T, V>(a.dstate_out + ((size_t)b * (K - 1) + (td - len + K - 1)) * a.D + c), e);
 #pragma unroll
                     for (int i = 0; i < P; ++i) out[i] = __fadd2_rn(out[i], e[i]);
                 }
-                if (td >= 0) store_pack(dx + td * a.lddx, pack_of<T, V>(out));
+                if (td >= 0) store_pack(to, pack_of<T, V>(out));
                 else store_pack(a.dstate_in + ((size_t)b * (K - 1) + (td + K - 1)) * a.D + c, pack_of<T, V>(out));
             }
 #pragma unroll
             for (int k = 0; k < K - 1; ++k)
 #pragma unroll
                 for (int i = 0; i < P; ++i) xw[k][i] = xw[kBwdGroup + k][i], gw[k][i] = gw[kBwdGroup + k][i];
-        }
+        };
+        // a group is whole where all its rows of g are the piece's own and all rows of dx that it completes are, too (and so none of
+        // the last K-1, to which a gradient of the state behind the sequence comes)
+        int q = 0, t = t0;
+#pragma unroll 1
+        for (; t < end && t < t0 + K - 1; t += kBwdGroup, ++q) group(q, t, Cut());
+#pragma unroll 1
+        for (; t + kBwdGroup <= stop; t += kBwdGroup, ++q) group(q, t, Whole());
+#pragma unroll 1
+        for (; t < end; t += kBwdGroup, ++q) group(q, t, Cut());
         copies_wait<0>();               // (the ring is free for the next piece)
         for (int t = max(t0, len); t < t1; ++t) store_pack(dx + t * a.lddx, zero_pack<T, V>());
     }

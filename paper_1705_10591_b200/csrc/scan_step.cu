@@ -57,13 +57,17 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const StepArgs<T> a)
     const int lane = threadIdx.x & 31, own = ROWS > 1 ? sl % ROWS : 0;
     const long long bo = b0 + own < a.B ? b0 + own : b0;
     float h[ROWS][kSpt], Bv[ROWS][kSpt], Cv[ROWS][kSpt], A2[kSpt];
+    const size_t at = ((size_t)b0 * a.D + d) * a.N + n0, next = (size_t)a.D * a.N;
+    {
+        const float* ph = a.state_in + at;
+        const T *pb = a.Bm + b0 * a.ldB + (long long)g * a.N + n0, *pc = a.Cm + b0 * a.ldC + (long long)g * a.N + n0;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const long long b = b0 + r;
-        const int there = b < a.B ? real : 0;
-        load_states<QUADS>(a.state_in + ((size_t)b * a.D + d) * a.N + n0, there, h[r]);
-        load_inputs(a.Bm + b * a.ldB + (long long)g * a.N + n0, there, a.B_wide, Bv[r]);
-        load_inputs(a.Cm + b * a.ldC + (long long)g * a.N + n0, there, a.C_wide, Cv[r]);
+        for (int r = 0; r < ROWS; ++r, ph += next, pb += a.ldB, pc += a.ldC) {
+            const int there = b0 + r < a.B ? real : 0;
+            load_states<QUADS>(ph, there, h[r]);
+            load_inputs(pb, there, a.B_wide, Bv[r]);
+            load_inputs(pc, there, a.C_wide, Cv[r]);
+        }
     }
     load_states<QUADS>(a.A + (size_t)d * a.N + n0, real, A2);
     const float u = mine ? to_float(a.u[bo * a.ldu + d]) : 0.f, z = mine && a.z ? to_float(a.z[bo * a.ldz + d]) : 0.f;
@@ -88,7 +92,7 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const StepArgs<T> a)
             v[r] = fmaf(Cv[r][i + 1], x.y, v[r]);
         }
         if (b0 + r >= a.B || real <= 0) continue;
-        float* out = a.state_out + ((size_t)(b0 + r) * a.D + d) * a.N + n0;
+        float* out = a.state_out + at + r * next;
         if (QUADS) {
             *reinterpret_cast<float4*>(out) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
         } else {
