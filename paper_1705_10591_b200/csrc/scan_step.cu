@@ -15,7 +15,7 @@ struct StepArgs {
     const float *A, *Dskip, *delta_bias, *state_in;
     T* y;
     float* state_out;
-    int B, D, N, G, E, NL;
+    int B, D, N, G, E, NL, loops;       // loops: ROWS sequences after each other of a block
     unsigned across;                    // blocks for the channels of ROWS sequences
     long long ldu, lddelta, ldB, ldC, ldz, ldy;
     bool softplus, B_wide, C_wide;
@@ -44,76 +44,108 @@ __device__ __forceinline__ void load_inputs(const T* p, int real, bool wide, flo
     }
 }
 
+// Many sequences (QUADS, ROWS = 4): the states of the next four come in by asynchronous copies while these are stepped, `loops` fours in a row.
 template <typename T, int ROWS, bool QUADS>
 __global__ void __launch_bounds__(128) scan_step_kernel(const StepArgs<T> a)
 {
+    constexpr bool AHEAD = ROWS > 1 && QUADS;
     ptx::grid_dep_wait();
+    __shared__ float4 ring[AHEAD ? 2 * ROWS * 128 : 1];
     const unsigned id = blockIdx.x % a.across * 128 + threadIdx.x;
     const int sl = (int)(id % a.NL), n0 = sl * kSpt;
     const bool mine = id / a.NL < (unsigned)a.D;
     const int d = mine ? (int)(id / a.NL) : 0, g = d / a.E, real = mine ? a.N - n0 : 0;
-    const long long b0 = (long long)(blockIdx.x / a.across) * ROWS;
     // ROWS = 4 (a channel has four lanes or more): this lane's own sequence is b0 + sl % 4
     const int lane = threadIdx.x & 31, own = ROWS > 1 ? sl % ROWS : 0;
-    const long long bo = b0 + own < a.B ? b0 + own : b0;
-    float h[ROWS][kSpt], Bv[ROWS][kSpt], Cv[ROWS][kSpt], A2[kSpt];
-    const size_t at = ((size_t)b0 * a.D + d) * a.N + n0, next = (size_t)a.D * a.N;
-    {
-        const float* ph = a.state_in + at;
-        const T *pb = a.Bm + b0 * a.ldB + (long long)g * a.N + n0, *pc = a.Cm + b0 * a.ldC + (long long)g * a.N + n0;
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r, ph += next, pb += a.ldB, pc += a.ldC) {
-            const int there = b0 + r < a.B ? real : 0;
-            load_states<QUADS>(ph, there, h[r]);
-            load_inputs(pb, there, a.B_wide, Bv[r]);
-            load_inputs(pc, there, a.C_wide, Cv[r]);
-        }
-    }
+    const size_t next = (size_t)a.D * a.N;
+    float A2[kSpt];
     load_states<QUADS>(a.A + (size_t)d * a.N + n0, real, A2);
-    const float u = mine ? to_float(a.u[bo * a.ldu + d]) : 0.f, z = mine && a.z ? to_float(a.z[bo * a.ldz + d]) : 0.f;
-    float s = mine ? to_float(a.delta[bo * a.lddelta + d]) : 0.f;
-    if (a.delta_bias && mine) s += a.delta_bias[d];
-    if (a.softplus) s = softplus(s);
-    const float su = s * u, skip = a.Dskip && mine ? a.Dskip[d] : 0.f;
 #pragma unroll
     for (int i = 0; i < kSpt; ++i) A2[i] *= kLog2e;
-    float v[ROWS];
+    const float bias = a.delta_bias && mine ? a.delta_bias[d] : 0.f, skip = a.Dskip && mine ? a.Dskip[d] : 0.f;
+    const long long first = (long long)(blockIdx.x / a.across) * ROWS * a.loops;
+    auto fetch = [&](int k) {
+        const long long b0 = first + (long long)k * ROWS;
+        const float* p = a.state_in + ((size_t)b0 * a.D + d) * a.N + n0;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const int from = (lane & ~(ROWS - 1)) | r;
-        const float sr = ROWS > 1 ? __shfl_sync(0xffffffffu, s, from) : s, sur = ROWS > 1 ? __shfl_sync(0xffffffffu, su, from) : su;
-        v[r] = 0.f;
-#pragma unroll
-        for (int i = 0; i < kSpt; i += 2) {
-            const float2 e = decay(both(sr), make_float2(A2[i], A2[i + 1]));
-            const float2 x = __ffma2_rn(e, make_float2(h[r][i], h[r][i + 1]), __fmul2_rn(both(sur), make_float2(Bv[r][i], Bv[r][i + 1])));
-            h[r][i] = x.x, h[r][i + 1] = x.y;
-            v[r] = fmaf(Cv[r][i], x.x, v[r]);
-            v[r] = fmaf(Cv[r][i + 1], x.y, v[r]);
+        for (int r = 0; r < ROWS; ++r, p += next) {
+            const bool there = k < a.loops && b0 + r < a.B && real > 0;
+            copy_async<16>(ring + ((k & 1) * ROWS + r) * 128 + threadIdx.x, there ? p : a.state_in, there);
         }
-        if (b0 + r >= a.B || real <= 0) continue;
-        float* out = a.state_out + at + r * next;
-        if (QUADS) {
-            *reinterpret_cast<float4*>(out) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
-        } else {
+        copies_commit();
+    };
+    if (AHEAD) fetch(0);
+    for (int k = 0; k < a.loops; ++k) {
+        const long long b0 = first + (long long)k * ROWS;
+        if (b0 >= a.B) break;
+        if (AHEAD) fetch(k + 1);
+        const long long bo = b0 + own < a.B ? b0 + own : b0;
+        float h[ROWS][kSpt], Bv[ROWS][kSpt], Cv[ROWS][kSpt];
+        const size_t at = ((size_t)b0 * a.D + d) * a.N + n0;
+        {
+            const float* ph = a.state_in + at;
+            const T *pb = a.Bm + b0 * a.ldB + (long long)g * a.N + n0, *pc = a.Cm + b0 * a.ldC + (long long)g * a.N + n0;
 #pragma unroll
-            for (int i = 0; i < kSpt; ++i)
-                if (i < real) out[i] = h[r][i];
+            for (int r = 0; r < ROWS; ++r, ph += next, pb += a.ldB, pc += a.ldC) {
+                const int there = b0 + r < a.B ? real : 0;
+                if (!AHEAD) load_states<QUADS>(ph, there, h[r]);
+                load_inputs(pb, there, a.B_wide, Bv[r]);
+                load_inputs(pc, there, a.C_wide, Cv[r]);
+            }
         }
+        const float u = mine ? to_float(a.u[bo * a.ldu + d]) : 0.f, z = mine && a.z ? to_float(a.z[bo * a.ldz + d]) : 0.f;
+        float s = mine ? to_float(a.delta[bo * a.lddelta + d]) + bias : 0.f;
+        if (a.softplus) s = softplus(s);
+        const float su = s * u;
+        if (AHEAD) {
+            copies_wait<1>();
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const float4 q = ring[((k & 1) * ROWS + r) * 128 + threadIdx.x];
+                h[r][0] = q.x, h[r][1] = q.y, h[r][2] = q.z, h[r][3] = q.w;
+            }
+        }
+        float v[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const int from = (lane & ~(ROWS - 1)) | r;
+            const float sr = ROWS > 1 ? __shfl_sync(0xffffffffu, s, from) : s, sur = ROWS > 1 ? __shfl_sync(0xffffffffu, su, from) : su;
+            v[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kSpt; i += 2) {
+                const float2 e = decay(both(sr), make_float2(A2[i], A2[i + 1]));
+                const float2 x = __ffma2_rn(e, make_float2(h[r][i], h[r][i + 1]), __fmul2_rn(both(sur), make_float2(Bv[r][i], Bv[r][i + 1])));
+                h[r][i] = x.x, h[r][i + 1] = x.y;
+                v[r] = fmaf(Cv[r][i], x.x, v[r]);
+                v[r] = fmaf(Cv[r][i + 1], x.y, v[r]);
+            }
+            if (b0 + r >= a.B || real <= 0) continue;
+            float* out = a.state_out + at + r * next;
+            if (QUADS) {
+                *reinterpret_cast<float4*>(out) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kSpt; ++i)
+                    if (i < real) out[i] = h[r][i];
+            }
+        }
+        if (ROWS > 1) sum_over_lanes<ROWS, ROWS, 1>(v, lane); // leaves the sum of this lane's own sequence
+        for (int m = ROWS; m < a.NL; m *= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], m);
+        if (sl >= ROWS || !mine || b0 + own >= a.B) continue;
+        float y = fmaf(skip, u, v[0]);
+        if (a.z) y *= z * sigmoid(z);
+        a.y[(b0 + own) * a.ldy + d] = from_float<T>(y);
     }
-    if (ROWS > 1) sum_over_lanes<ROWS, ROWS, 1>(v, lane);     // leaves the sum of this lane's own sequence
-    for (int m = ROWS; m < a.NL; m *= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], m);
-    if (sl >= ROWS || !mine || b0 + own >= a.B) return;
-    float y = fmaf(skip, u, v[0]);
-    if (a.z) y *= z * sigmoid(z);
-    a.y[(b0 + own) * a.ldy + d] = from_float<T>(y);
 }
 
 template <typename T, int ROWS, bool QUADS>
 conv2d_status_t step(StepArgs<T> a, cudaStream_t stream)
 {
     a.across = ceil_div_u((long long)a.D * a.NL, 128);
-    const long long blocks = (long long)a.across * ceil_div_u(a.B, ROWS);
+    // (fours in a row while the blocks are two for every place an SM has)
+    a.loops = 1;
+    while (ROWS > 1 && a.loops < 8 && (long long)a.across * ceil_div_u(a.B, 2 * ROWS * a.loops) >= 2LL * 5 * sm_count()) a.loops *= 2;
+    const long long blocks = (long long)a.across * ceil_div_u(a.B, ROWS * a.loops);
     if (blocks > 0x7fffffffLL) return CONV2D_ERR_SHAPE;
     if (launch_pdl(scan_step_kernel<T, ROWS, QUADS>, dim3((unsigned)blocks), dim3(128), 0, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
     count_launch();
