@@ -15,9 +15,6 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kGroup = 4, kRing = 4;    // rows of a group, groups of the ring
 
-// Groups of rows all of which are there, and others: two versions of a loop's body.
-struct Whole { static constexpr bool value = true; };
-struct Cut { static constexpr bool value = false; };
 // w[k][pair], bias[pair] of the channels from c on
 template <typename T, int V, int K>
 __device__ __forceinline__ void load_taps(const T* w, const T* bias, int c, float2 (&wt)[K][kPairs<V>], float2 (&bt)[kPairs<V>])

@@ -426,7 +426,7 @@ struct ThreadRows {
 };
 template <typename T, int V> constexpr size_t ring_bytes = RowRing<T, V, kThreads, kGroup, kRing>::smem;
 
-// Walks `count` rows of the thread in groups: `issue(q, i)` starts the copies of group q, `take(q, i)` uses it.
+// Walks `count` rows of the thread in groups: `issue(q, i)` starts the copies of group q, `take(q, i, whole)` uses it.
 template <bool KEEP, typename Issue, typename Take>
 __device__ __forceinline__ void walk_rows(int count, Issue issue, Take take)
 {
@@ -439,15 +439,16 @@ __device__ __forceinline__ void walk_rows(int count, Issue issue, Take take)
     }
     int q = 0;
 #pragma unroll 1
-    for (int i = 0; i < count; i += kGroup, ++q) {
+    for (int i = 0; i + kGroup <= count; i += kGroup, ++q) {
         if (!KEEP) copies_wait<kRing - 2>();
-        take(q, i);
+        take(q, i, Whole());
         if (!KEEP) {
             issue(q + kRing - 1, i + (kRing - 1) * kGroup);
             copies_commit();
         }
     }
     if (!KEEP) copies_wait<0>();
+    if (q * kGroup < count) take(q, q * kGroup, Cut());
 }
 
 template <typename T, int V, int MODE>
@@ -485,23 +486,23 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
         int count = 0;
         for (int q = 0; q < p.turns; ++q) {
             const Rows r = rows_of(q);
-            walk_rows<KEEP>(r.count, [&](int g, int i) { r.ring.issue(g, i, r.count); }, [&](int g, int i) {
+            walk_rows<KEEP>(r.count, [&](int g, int i) { r.ring.issue(g, i, r.count); }, [&](int g, int i, auto whole) {
                 float2 v[kGroup][P];
 #pragma unroll
                 for (int j = 0; j < kGroup; ++j) pairs<T, V>(r.get(g, i, j), v[j]);
-                if (count == 0) shift = v[0][0].x;
+                if (i == 0 && q == 0) shift = v[0][0].x;
 #pragma unroll
                 for (int j = 0; j < kGroup; ++j) {
-                    if (i + j >= r.count) break;
+                    if (!decltype(whole)::value && i + j >= r.count) break;
 #pragma unroll
                     for (int k = 0; k < P; ++k) {
                         const float2 d = __fadd2_rn(v[j][k], both(-shift));
                         s1 = __fadd2_rn(s1, d);
                         s2 = __ffma2_rn(d, d, s2);
                     }
-                    count += V;
                 }
             });
+            count += V * r.count;
         }
         if (V == 1) s1.y = s2.y = 0.f;
         const float cnt = (float)count, t1 = s1.x + s1.y, off = count ? t1 / cnt : 0.f;
@@ -568,7 +569,7 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
         load_scale<V>(a.gamma, a.beta, p.c0 + pk * V, true, scale, add);
 #pragma unroll
         for (int k = 0; k < P; ++k) scale[k] = __fmul2_rn(scale[k], both(st.y));
-        walk_rows<KEEP>(r.count, [&](int g, int i) { r.ring.issue(g, i, r.count); }, [&](int g, int i) {
+        walk_rows<KEEP>(r.count, [&](int g, int i) { r.ring.issue(g, i, r.count); }, [&](int g, int i, auto whole) {
             float o[kGroup * 2 * P];
 #pragma unroll
             for (int j = 0; j < kGroup; ++j) {
@@ -586,7 +587,7 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
                 float2 v[P];
 #pragma unroll
                 for (int k = 0; k < P; ++k) v[k] = make_float2(o[2 * (j * P + k)], o[2 * (j * P + k) + 1]);
-                if (i + j < r.count) store_pack(y, pack_of<T, V>(v));
+                if (decltype(whole)::value || i + j < r.count) store_pack(y, pack_of<T, V>(v));
                 y += ystep;
             }
         });
@@ -660,13 +661,13 @@ __global__ void __launch_bounds__(kThreads, 2) norm_slab_bwd_kernel(const NormAr
             for (int k = 0; k < P; ++k) s1[k] = s2[k] = both(0.f);
             if (rx.count) {
                 const Params m = params_of(pk);
-                walk_rows<KEEP>(rx.count, [&](int g, int i) { rx.ring.issue(g, i, rx.count), rg.ring.issue(g, i, rx.count); }, [&](int g, int i) {
+                walk_rows<KEEP>(rx.count, [&](int g, int i) { rx.ring.issue(g, i, rx.count), rg.ring.issue(g, i, rx.count); }, [&](int g, int i, auto whole) {
                     float2 xn[kGroup][P];
                     float d[kGroup * 2 * P];
                     terms(m, rx, rg, g, i, xn, d);
 #pragma unroll
                     for (int j = 0; j < kGroup; ++j) {
-                        if (i + j >= rx.count) break;
+                        if (!decltype(whole)::value && i + j >= rx.count) break;
 #pragma unroll
                         for (int k = 0; k < P; ++k) {
                             const float2 e = make_float2(d[2 * (j * P + k)], d[2 * (j * P + k) + 1]);
@@ -742,7 +743,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_slab_bwd_kernel(const NormAr
         const float2 mm = gmean[p.group];
         const Params m = params_of(pk);
         T* dx = a.dx + (p.n * a.S + p.first) * a.lddx + p.c0 + pk * V;
-        walk_rows<KEEP>(rx.count, [&](int g, int i) { rx.ring.issue(g, i, rx.count), rg.ring.issue(g, i, rx.count); }, [&](int g, int i) {
+        walk_rows<KEEP>(rx.count, [&](int g, int i) { rx.ring.issue(g, i, rx.count), rg.ring.issue(g, i, rx.count); }, [&](int g, int i, auto whole) {
             float2 xn[kGroup][P];
             float d[kGroup * 2 * P];
             terms(m, rx, rg, g, i, xn, d);
@@ -754,7 +755,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_slab_bwd_kernel(const NormAr
                     const float2 e = __ffma2_rn(make_float2(d[2 * (j * P + k)], d[2 * (j * P + k) + 1]), m.gamma[k], both(-mm.x));
                     o[k] = __fmul2_rn(both(m.rstd), __ffma2_rn(xn[j][k], both(-mm.y), e));
                 }
-                if (i + j < rx.count) store_pack(dx, pack_of<T, V>(o));
+                if (decltype(whole)::value || i + j < rx.count) store_pack(dx, pack_of<T, V>(o));
                 dx += dxstep;
             }
         });

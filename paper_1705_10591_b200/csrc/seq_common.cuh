@@ -204,6 +204,10 @@ template <typename T, int V> __device__ __forceinline__ Pack<T, V> pack(const fl
     return pack_of<T, V>(q);
 }
 
+// Groups of rows all of which are there, and others: two versions of a loop's body, the first without checks.
+struct Whole { static constexpr bool value = true; };
+struct Cut { static constexpr bool value = false; };
+
 // Rows of sequence b that hold tokens.
 __device__ __forceinline__ int sequence_length(const int* lengths, int b, int L)
 {
