@@ -49,8 +49,10 @@ BwdCut bwd_cut(int B, int L, int D, int N, int G)
     c.nl = lanes_for(N, kSpt);
     c.cb = c.nl == 1 ? 64 : 128 / c.nl;
     const int E = D / G;
-    // a block's partial sums of dB and dC are for at least 32 channels, or the workspace would be larger than the tensors
-    c.sets = env_int("CONV2D_B200_SCAN_SETS", c.cb >= 32 ? 1 : 32 / c.cb);
+    // a block's partial sums of dB and dC are for 32 channels, or the workspace would be larger than the tensors (16 channels with more than 64
+    // states: more sets do not fit into shared memory)
+    const int sets = c.cb >= 32 ? 1 : 32 / c.cb;
+    c.sets = env_int("CONV2D_B200_SCAN_SETS", sets > 4 ? 4 : sets);
     c.blocks_group = (int)ceil_div_u(E, (long long)c.cb * c.sets);
     // segments of time, where the blocks leave two thirds of the machine idle: two blocks for every SM then, of 64 rows at least
     const long long blocks = (long long)B * G * c.blocks_group;
@@ -109,6 +111,7 @@ conv2d_status_t bwd(const ScanSeq& s, cudaStream_t stream)
     a.u_unit = copy_unit(s.u, s.ldu, a.E, e), a.delta_unit = copy_unit(s.delta, s.lddelta, a.E, e), a.z_unit = copy_unit(s.z, s.ldz, a.E, e);
     a.dy_unit = copy_unit(s.dy, s.lddy, a.E, e), a.B_unit = copy_unit(s.Bm, s.ldB, a.N, e), a.C_unit = copy_unit(s.Cm, s.ldC, a.N, e);
     a.out_quads = a.E % 4 == 0 && rows_aligned(s.du, s.lddu, e, 4 * e) && rows_aligned(s.ddelta, s.ldddelta, e, 4 * e) && rows_aligned(s.dz, s.lddz, e, 4 * e);
+    static_assert(Tile::fixed(e) + (Tile::CB >= 32 ? 1 : 4) * Tile::set_bytes <= 227 * 1024, "the sets that bwd_cut allows");
     const size_t smem = Tile::fixed(e) + a.sets * Tile::set_bytes;
     static SmemLimit limit;
     if (raise_smem_limit(reinterpret_cast<const void*>(scan_bwd_kernel<T, NL>), smem, limit) != cudaSuccess

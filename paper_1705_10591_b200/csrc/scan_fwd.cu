@@ -29,6 +29,7 @@ conv2d_status_t walk(ScanFwdArgs<T> a, cudaStream_t stream)
 {
     using Tile = ScanFwdTile<NL, SPT>;
     constexpr size_t smem = Tile::smem(sizeof(T));
+    static_assert(smem <= 227 * 1024, "shared memory of a block");
     a.blocks_group = (int)ceil_div_u(a.E, Tile::CB);
     const long long blocks = (long long)a.B * a.segs * a.G * a.blocks_group;
     if (blocks > 0x7fffffffLL) return CONV2D_ERR_SHAPE;

@@ -240,10 +240,12 @@ class ScanCase:
                 self.state, self.n, self.soft)
 
 
-@pytest.fixture(params=["whole", "segments"])
+@pytest.fixture(params=["whole", "segments", "default"])
 def cut(request, monkeypatch):
-    """Sequences walked whole, and cut into segments that are joined; one and several channel sets of a block."""
-    if request.param == "segments":
+    """Sequences walked whole, and cut into segments that are joined; one and several channel sets of a block; and as the sizes decide."""
+    if request.param == "default":
+        pass
+    elif request.param == "segments":
         monkeypatch.setenv("CONV2D_B200_SCAN_SEGS", "3")
         monkeypatch.setenv("CONV2D_B200_SCAN_BWD_SEGS", "2")
         monkeypatch.setenv("CONV2D_B200_SCAN_SETS", "2")
@@ -294,8 +296,37 @@ def test_scan(lib, case, cut, with_state):
             assert (rows.result()[b, n:] == 0).all()
 
 
+@pytest.mark.parametrize("whole", [True, False])
+def test_padding_leaves_the_state_as_it_is(lib, monkeypatch, whole):
+    """Padding does nothing to the state: walked whole, it has the bits of the shorter sequence's, and so has y.  Cut by the sizes, 200 rows are segments and 37
+    rows are none: the first segment's rows have the same bits, but its share of the state, h0 exp(A sum delta) + (the segment from zero), is rounded in
+    another order than a walk from h0, so the state is compared with the formula, each within the roundings of a walk."""
+    if whole:
+        monkeypatch.setenv("CONV2D_B200_SCAN_SEGS", "1")
+    long = ScanCase(lib, ("fp32", 1, 200, 40, 16, 1, True, True, True, True, [37], 0, 0))
+    st = torch.full((1, 40, 16), SENTINEL, device="cuda")
+    y = long.forward(state_out=st).result()
+    short = ScanCase(lib, ("fp32", 1, 200, 40, 16, 1, True, True, True, True, None, 0, 0))
+    for rows in ("ur", "dr", "br", "cr", "zr"):
+        getattr(short, rows).view().copy_(getattr(long, rows).view())
+    short.L, st2 = 37, torch.full_like(st, SENTINEL)
+    y2 = short.forward(state_out=st2).result()
+    assert torch.equal(y[:, :37], y2) and (y[:, 37:] == 0).all()
+    if whole:
+        assert torch.equal(st, st2)
+    want, size = ref.scan_fwd(*long.reference())[1]
+    for got in (st, st2):
+        check(got, want, size, long.roundings, "state")
+    # and a sequence without a token hands the given state on
+    none = ScanCase(lib, ("fp32", 2, 9, 8, 16, 1, True, True, True, True, [0, 0], 0, 0))
+    st = torch.empty(2, 8, 16, device="cuda")
+    none.forward(state_out=st)
+    assert torch.equal(st, none.sd)
+
+
 @pytest.mark.parametrize("type, B, D, N, G, gated", [("bf16", 3, 24, 16, 2, True), ("fp32", 2, 7, 5, 1, True), ("fp16", 1, 12, 64, 1, False),
-                                                     ("fp32", 400, 96, 32, 3, True), ("bf16", 1, 5, 128, 5, True)])
+                                                     ("fp32", 400, 96, 32, 3, True), ("bf16", 1, 5, 128, 5, True), ("bf16", 333, 1000, 16, 1, True),
+                                                     ("fp32", 1021, 160, 13, 2, False)])
 def test_scan_step(lib, type, B, D, N, G, gated):
     c = ScanCase(lib, (type, B, 1, D, N, G, True, gated, True, True, None, 3, 1))
     for in_place in (False, True):
@@ -347,9 +378,16 @@ NORM = [  # type, N, S, C, G, activation, shift of the mean, pad, offset
 ]
 
 
+@pytest.fixture(params=["default", "stream", "slab"])
+def variant(request, monkeypatch):
+    """Slabs on chip, streams, and whichever the sizes decide for (a slab that does not fit is a stream whatever is asked for)."""
+    if request.param != "default":
+        monkeypatch.setenv("CONV2D_B200_NORM_STREAM", "1" if request.param == "stream" else "-1")
+
+
 @pytest.mark.parametrize("params", [True, False])
 @pytest.mark.parametrize("case", NORM, ids=lambda c: f"{c[0]}-{'x'.join(map(str, c[1:5]))}-{c[5]}")
-def test_norm(lib, case, params):
+def test_norm(lib, case, params, variant):
     type, N, S, C, G, act, shift, pad, offset = case
     t, eps = TYPES[type], 1e-5
     x = draw(300, N, S, C, shift=shift, dtype=t)
@@ -380,6 +418,30 @@ def test_norm(lib, case, params):
     check(dxr.result(), *dx, 2 * chain, "dx")
     check(dg.result(), *dgamma, 2 * chain + min(N * S, 4096), "dgamma")
     check(db.result(), *dbeta, 2 * chain + min(N * S, 4096), "dbeta")
+
+
+def test_norm_of_many_rows_and_wide_groups(lib):
+    """More samples than a chunk, groups of several packs a lane, groups wider than a block has threads: forward against torch in 64 bits."""
+    for type, N, S, C, G in (("bf16", 5000, 1, 512, 2), ("fp16", 3000, 1, 96, 32), ("fp32", 700, 1, 1024, 2), ("bf16", 3, 40, 9000, 1), ("fp32", 2, 7, 3000, 3),
+                             ("bf16", 6, 700, 320, 32), ("fp16", 300, 49, 80, 8)):
+        t = TYPES[type]
+        x = draw(310, N, S, C, shift=0.5, dtype=t)
+        xd, mean, rstd = cuda(x, t), torch.empty(N, G, device="cuda"), torch.empty(N, G, device="cuda")
+        y, ws = torch.empty_like(xd), workspace(lib.norm_fwd_groups_workspace_size(N, S, C, G))
+        lib.norm_fwd_groups(xd.data_ptr(), 0, 0, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), N, S, C, G, C, C, 1e-5, operand(lib, type), lib.ACT_SILU,
+                            ws.data_ptr(), ws.numel(), stream())
+        (want, size), (m, ms), (r, rs), _ = ref.norm_fwd(x, torch.ones(C, dtype=F), torch.zeros(C, dtype=F), G, 1e-5, "silu")
+        chain = 64 + min(2048, S * C // G)
+        for got, ref_, sz, what in ((y, want, size, "y"), (mean, m, ms, "mean"), (rstd, r, rs, "rstd")):
+            check(got, ref_, sz, chain, (what, type, N, S, C, G))
+        dy = draw(311, N, S, C, dtype=t)
+        gd, dx, dg, db = cuda(dy, t), torch.empty_like(xd), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+        ws = workspace(lib.norm_bwd_groups_workspace_size(N, S, C, G))
+        lib.norm_bwd_groups(xd.data_ptr(), 0, 0, mean.data_ptr(), rstd.data_ptr(), gd.data_ptr(), dx.data_ptr(), dg.data_ptr(), db.data_ptr(), N, S, C, G, C, C, C,
+                            operand(lib, type), lib.ACT_SILU, ws.data_ptr(), ws.numel(), stream())
+        want = ref.norm_bwd(x, torch.ones(C, dtype=F), torch.zeros(C, dtype=F), G, 1e-5, "silu", dy)
+        for got, (value, sz), what in zip((dx, dg, db), want, ("dx", "dgamma", "dbeta")):
+            check(got, value, sz, 2 * chain + (0 if what == "dx" else N * S), (what, type, N, S, C, G))
 
 
 def test_norm_of_constant_groups(lib):
