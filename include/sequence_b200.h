@@ -11,6 +11,7 @@
  *   - Tensors are dense but for the distance between rows: row r of a tensor begins r * ld elements after its first
  *     element, ld at least the length of a row (a slice of a wider tensor's columns has the wider tensor's ld).  Row of
  *     sequence b and token t: b * L + t.
+ *     There are at most 2^30 rows and 2^22 channels, ld is below 2^31; offsets may exceed 32 bits.
  *   - Addresses need the alignment of their elements only; rows on 16-byte boundaries are faster.
  *   - `lengths`: NULL, or B device integers (values outside 0 .. L are taken as the nearest of these): sequence b has
  *     lengths[b] tokens and the rows behind them are padding.  Padding is not read, whatever it holds, and the rows of outputs that
@@ -19,7 +20,7 @@
  *   - Workspaces: the size comes from the query of the same name; any alignment of 16 bytes.  They hold nothing between calls,
  *     so calls in a row on one stream may share one, calls that can overlap must not.
  *   - Results do not depend on timing: the same call gives the same bits (no atomic additions).
- *   - Errors: CONV2D_ERR_NULL, _SHAPE (extents, a row distance below the row's length), _ALIGN, _UNSUPPORTED (an unknown type, activation or
+ *   - Errors: CONV2D_ERR_NULL, _SHAPE (extents beyond these, a row distance below the row's length), _ALIGN, _UNSUPPORTED (an unknown type, activation or
  *     flag, more taps or states than stated), _WORKSPACE, as argument errors before anything is enqueued; _ARCH, _CUDA.
  */
 #ifndef SEQUENCE_B200_H

@@ -53,6 +53,7 @@ BwdCut bwd_cut(int B, int L, int D, int N, int G)
     // states: more sets do not fit into shared memory)
     const int sets = c.cb >= 32 ? 1 : 32 / c.cb;
     c.sets = env_int("CONV2D_B200_SCAN_SETS", sets > 4 ? 4 : sets);
+    if (c.sets < 1) c.sets = 1;
     c.blocks_group = (int)ceil_div_u(E, (long long)c.cb * c.sets);
     // segments of time, where the blocks leave two thirds of the machine idle: two blocks for every SM then, of 64 rows at least
     const long long blocks = (long long)B * G * c.blocks_group;

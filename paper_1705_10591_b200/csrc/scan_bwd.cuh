@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
 #pragma unroll
             for (int i = 0; i < kSpt; ++i) {
                 const bool real = c < a.E && n0 + i < a.N;
-                av[i] = real ? a.A[(size_t)d * a.N + n0 + i] * kLog2e : 0.f;
+                av[i] = real ? decay_rate(a.A[(size_t)d * a.N + n0 + i]) : 0.f;
                 cv[i] = 0.f;
                 if (real && a.segs > 1) cv[i] = a.local[(((size_t)b * a.segs + seg) * a.D + d) * NQ + n0 + i];
                 else if (real && a.dstate_out) cv[i] = a.dstate_out[((size_t)b * a.D + d) * a.N + n0 + i];
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::SCAN) scan_bwd_carry_kernel(c
     float2 A2[2], carry[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     float av[kSpt], bias[V], steps = 0.f;
 #pragma unroll
-    for (int i = 0; i < kSpt; ++i) av[i] = mine && n0 + i < a.N ? a.A[(size_t)d * a.N + n0 + i] * kLog2e : 0.f;
+    for (int i = 0; i < kSpt; ++i) av[i] = mine && n0 + i < a.N ? decay_rate(a.A[(size_t)d * a.N + n0 + i]) : 0.f;
     A2[0] = make_float2(av[0], av[1]), A2[1] = make_float2(av[2], av[3]);
 #pragma unroll
     for (int i = 0; i < V; ++i) bias[i] = a.delta_bias && pk_real ? a.delta_bias[g * a.E + c0 + pk + i] : 0.f;
@@ -536,7 +536,7 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::SCAN) scan_bwd_carry_kernel(c
             const float4 cv = *reinterpret_cast<const float4*>(Cs + t * NP + n0);
             const float2 s_2 = make_float2(q.x, q.x), g2 = make_float2(q.y, q.y);
             const float2 e0 = decay(s_2, A2[0]), e1 = decay(s_2, A2[1]);
-                carry[0] = __fmul2_rn(e0, __ffma2_rn(make_float2(cv.x, cv.y), g2, carry[0]));
+            carry[0] = __fmul2_rn(e0, __ffma2_rn(make_float2(cv.x, cv.y), g2, carry[0]));
             carry[1] = __fmul2_rn(e1, __ffma2_rn(make_float2(cv.z, cv.w), g2, carry[1]));
             steps += q.x;
         }

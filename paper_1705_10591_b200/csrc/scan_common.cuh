@@ -12,6 +12,14 @@ namespace conv2d_b200 {
 
 constexpr int kCheckpointRows = 16;     // the forward pass keeps the state before every 16th row for the backward pass
 
+// A2 = A log2(e).  What lies below fp32 (A of -infinity: a state that forgets everything) is taken as its lowest value, so that a step of zero, as rows of
+// padding have it, is a decay of one there too.
+__device__ __forceinline__ float decay_rate(float A)
+{
+    const float v = A * kLog2e;
+    return v < -3.4e38f ? -3.4e38f : v;
+}
+
 // Decays exp(s A) = 2^(s A2) of two states.  The hardware's 2^x is low by 1.2e-8 of itself on average for x in -[0.001, 0.01], 0.6e-8 and 2.2e-8 a factor
 // of ten to either side (measured over 2^20 values of each range), which states that remember a thousand rows would add up; the argument takes
 // that much more.  2^kExpBias is 1: a step of zero leaves the state as it is.
@@ -147,7 +155,7 @@ __global__ void __launch_bounds__(256) scan_join_kernel(float* local, const floa
     const long long b = bd / D;
     if (b >= B) return;
     const bool real = n < N;
-    const float a2 = real ? A[(size_t)d * N + n] * kLog2e : 0.f;
+    const float a2 = real ? decay_rate(A[(size_t)d * N + n]) : 0.f;
     float H = first && real ? first[((size_t)b * D + d) * N + n] : 0.f;
     constexpr int AHEAD = 8;                                  // segments whose loads are under way together
     for (int i0 = 0; i0 < segs; i0 += AHEAD) {

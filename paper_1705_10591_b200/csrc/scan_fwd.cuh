@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(ScanFwdTile<NL, SPT>::TH) scan_fwd_kernel(cons
 #pragma unroll
             for (int i = 0; i < SPT; ++i) {
                 const bool real = mine && n0 + i < a.N;
-                av[i] = real ? a.A[(size_t)d * a.N + n0 + i] * kLog2e : 0.f;
+                av[i] = real ? decay_rate(a.A[(size_t)d * a.N + n0 + i]) : 0.f;
                 hv[i] = 0.f;
                 if (!STATE_ONLY && real) {
                     if (a.segs > 1) hv[i] = a.local[(((size_t)b * a.segs + seg) * a.D + d) * NQ + n0 + i];

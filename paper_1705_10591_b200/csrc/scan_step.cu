@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const StepArgs<T> a)
     float A2[kSpt];
     load_states<QUADS>(a.A + (size_t)d * a.N + n0, real, A2);
 #pragma unroll
-    for (int i = 0; i < kSpt; ++i) A2[i] *= kLog2e;
+    for (int i = 0; i < kSpt; ++i) A2[i] = decay_rate(A2[i]);
     const float bias = a.delta_bias && mine ? a.delta_bias[d] : 0.f, skip = a.Dskip && mine ? a.Dskip[d] : 0.f;
     const long long first = (long long)(blockIdx.x / a.across) * ROWS * a.loops;
     auto fetch = [&](int k) {

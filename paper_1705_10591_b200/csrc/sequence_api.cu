@@ -11,10 +11,11 @@ constexpr int kMaxTaps = 8, kMaxStates = 128;
 bool known(conv2d_operand_t t) { return t == CONV2D_OPERAND_BF16 || t == CONV2D_OPERAND_FP16 || t == CONV2D_OPERAND_FP32; }
 bool known(conv2d_activation_t a) { return a >= CONV2D_ACT_NONE && a <= CONV2D_ACT_GELU; }
 
-// Extents of B sequences of L rows of D channels: rows are counted in 32 bits, elements in 64.
+// Extents of B sequences of L rows of D channels: rows are counted in 32 bits (and by blocks, one of which may lie behind the last row), elements in 64;
+// workspaces stay below 2^63 bytes.
 bool extents_ok(long long B, long long L, long long D)
 {
-    return B > 0 && L > 0 && D > 0 && B * L <= 0x7fffffffLL && D <= (1 << 24);
+    return B > 0 && L > 0 && D > 0 && B * L <= (1LL << 30) && D <= (1 << 22);
 }
 bool element_aligned(const void* p, size_t size) { return reinterpret_cast<uintptr_t>(p) % size == 0; }
 

@@ -324,6 +324,79 @@ def test_padding_leaves_the_state_as_it_is(lib, monkeypatch, whole):
     assert torch.equal(st, none.sd)
 
 
+def backward(c, states, dy, dlast, optional=True):
+    """du, ddelta, dA, dB, dC, dDskip, dz, ddelta_bias and dstate_in; those that a caller may leave out only where `optional`."""
+    lib, B, L, D, N, G = c.lib, c.B, c.L, c.D, c.N, c.G
+    new = lambda *s, t=torch.float32: Rows(s, t)  # noqa: E731
+    du, dd, dz, dB, dC = new(B, L, D, t=c.t), new(B, L, D, t=c.t), new(B, L, D, t=c.t), new(B, L, G * N, t=c.t), new(B, L, G * N, t=c.t)
+    dA, dk, db, ds = new(D, N), new(D), new(D), new(B, D, N)
+    g, dl = cuda(dy, c.t), None if dlast is None else cuda(dlast)
+    nbytes = lib.scan_bwd_selective_workspace_size(B, L, D, N, G)
+    ws = workspace(nbytes)
+    p = lambda v: v.ptr if optional else 0  # noqa: E731
+    lib.scan_bwd_selective(*c.inputs(), c.p(c.lengths), states.data_ptr(), g.data_ptr(), c.p(dl), du.ptr, dd.ptr, dA.ptr, dB.ptr, dC.ptr,
+                           p(dk) if c.kd is not None else 0, dz.ptr if c.zr else 0, p(db), p(ds), B, L, D, N, G, c.ur.ld, c.dr.ld, c.br.ld, c.cr.ld,
+                           c.zr.ld if c.zr else D, D, du.ld, dd.ld, dB.ld, dC.ld, dz.ld, operand(lib, c.type), c.flags(), ws.data_ptr(), nbytes, stream())
+    return [v.result() for v in (du, dd, dA, dB, dC, dk, dz, db, ds)]
+
+
+def test_states_that_forget_everything(lib, cut):
+    """A of -infinity is A of -1e30: a decay of zero, and of one over padding; nothing becomes NaN."""
+    out = []
+    for value in (float("-inf"), -1e30):
+        c = ScanCase(lib, ("fp32", 2, 150, 12, 8, 1, True, True, True, True, [150, 21], 0, 0))
+        c.Ad[3, 2:6] = value
+        states, st = workspace(lib.scan_states_size(c.B, c.L, c.D, c.N)), torch.empty(2, 12, 8, device="cuda")
+        y = c.forward(state_out=st, states=states).result()
+        one = st.clone()
+        yo = torch.empty(2, 12, device="cuda")
+        lib.scan_step_selective(c.ur.ptr, c.dr.ptr, c.Ad.data_ptr(), c.br.ptr, c.cr.ptr, 0, 0, 0, st.data_ptr(), yo.data_ptr(), one.data_ptr(), 2, 12, 8, 1,
+                                12, 12, 8, 8, 12, 12, lib.OPERAND_FP32, 1, stream())
+        grads = backward(c, states, mask_rows(draw(232, 2, 150, 12), c.n, 0.0), draw(233, 2, 12, 8))
+        out.append([y, st, yo, one] + grads)
+    for a, b in zip(*out):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+def test_outputs_that_may_be_left_out(lib):
+    """What is left out changes no bit of the rest; the convolution's backward pass needs no workspace without dw and dbias."""
+    c = ScanCase(lib, ("bf16", 2, 50, 24, 16, 2, True, True, True, True, [50, 9], 8, 8))
+    states, st = workspace(lib.scan_states_size(2, 50, 24, 16)), torch.empty(2, 24, 16, device="cuda")
+    y = c.forward(state_out=st, states=states).result()
+    assert torch.equal(c.forward().result(), y)
+    dy, dl = mask_rows(draw(234, 2, 50, 24, dtype=c.t), c.n, 0.0), draw(235, 2, 24, 16)
+    some, every = backward(c, states, dy, dl, optional=False), backward(c, states, dy, dl)
+    for i, (a, b) in enumerate(zip(some, every)):
+        assert (a == SENTINEL).all() if i in (5, 7, 8) else torch.equal(a, b), i
+    t = torch.bfloat16
+    x, w, g = cuda(draw(236, 2, 70, 24, dtype=t), t), cuda(draw(237, 24, 4, dtype=t), t), cuda(draw(238, 2, 70, 24, dtype=t), t)
+    need = lib.conv1d_bwd_causal_workspace_size(2, 70, 24, 4)
+    ws, out = workspace(need), []
+    for dw, db in ((True, True), (True, False), (False, True), (False, False)):
+        dx, wg, bg = torch.full_like(x, SENTINEL), torch.full((24, 4), SENTINEL, device="cuda"), torch.full((24,), SENTINEL, device="cuda")
+        use = dw or db
+        lib.conv1d_bwd_causal(x.data_ptr(), w.data_ptr(), 0, 0, 0, g.data_ptr(), 0, dx.data_ptr(), wg.data_ptr() if dw else 0, bg.data_ptr() if db else 0, 0,
+                              2, 70, 24, 4, 24, 24, 24, lib.OPERAND_BF16, lib.ACT_SILU, ws.data_ptr() if use else 0, need if use else 0, stream())
+        out.append((dx, wg, bg))
+        for got, full, given in zip(out[-1], out[0], (True, dw, db)):
+            assert torch.equal(got, full) if given else (got == SENTINEL).all()
+    for S in (1, 60):
+        x, g = draw(239, 3, S, 32, shift=0.3), draw(240, 3, S, 32)
+        xd, gd, y, y2 = cuda(x), cuda(g), torch.empty(3, S, 32, device="cuda"), torch.empty(3, S, 32, device="cuda")
+        ws = workspace(max(lib.norm_fwd_groups_workspace_size(3, S, 32, 4), lib.norm_bwd_groups_workspace_size(3, S, 32, 4)))
+        m, r, dx, dx2, dg, db = (torch.full(s, SENTINEL, device="cuda") for s in ((3, 4), (3, 4), (3, S, 32), (3, S, 32), (32,), (32,)))
+        f = lambda y, m, r: lib.norm_fwd_groups(xd.data_ptr(), 0, 0, y.data_ptr(), m, r, 3, S, 32, 4, 32, 32, 1e-5, lib.OPERAND_FP32, lib.ACT_GELU,  # noqa: E731
+                                                ws.data_ptr(), ws.numel(), stream())
+        f(y, m.data_ptr(), r.data_ptr()), f(y2, 0, 0)
+        assert torch.equal(y, y2)
+        b = lambda dx, dg, db: lib.norm_bwd_groups(xd.data_ptr(), 0, 0, m.data_ptr(), r.data_ptr(), gd.data_ptr(), dx.data_ptr(), dg, db, 3, S, 32, 4,  # noqa: E731
+                                                   32, 32, 32, lib.OPERAND_FP32, lib.ACT_GELU, ws.data_ptr(), ws.numel(), stream())
+        b(dx, dg.data_ptr(), db.data_ptr()), b(dx2, 0, 0)
+        only = torch.full((32,), SENTINEL, device="cuda")
+        b(dx2, 0, only.data_ptr())
+        assert torch.equal(dx, dx2) and torch.equal(db, only)
+
+
 @pytest.mark.parametrize("type, B, D, N, G, gated", [("bf16", 3, 24, 16, 2, True), ("fp32", 2, 7, 5, 1, True), ("fp16", 1, 12, 64, 1, False),
                                                      ("fp32", 400, 96, 32, 3, True), ("bf16", 1, 5, 128, 5, True), ("bf16", 333, 1000, 16, 1, True),
                                                      ("fp32", 1021, 160, 13, 2, False)])
@@ -569,6 +642,38 @@ def test_captured_calls_replay_and_share_a_workspace(lib):
         for b, want in zip(blocks, direct):
             for k, v in b.outputs().items():
                 assert torch.equal(v, want[k]), k
+
+
+def test_captured_single_tokens(lib):
+    """Steps in place, captured: three replays are three tokens; many sequences (several fours a block) as well as few."""
+    for B, D, N in ((3, 40, 16), (1500, 256, 16)):
+        w, x, y = cuda(draw(480, D, 4, scale=0.5)), cuda(draw(481, B, D)), torch.empty(B, D, device="cuda")
+        c = ScanCase(lib, ("fp32", B, 1, D, N, 1, True, True, True, True, None, 0, 0))
+        conv, scan = cuda(draw(482, B, 3, D)), c.sd
+        begin = conv.clone(), scan.clone()
+
+        def token(s):
+            lib.conv1d_step_causal(x.data_ptr(), w.data_ptr(), 0, conv.data_ptr(), y.data_ptr(), conv.data_ptr(), B, D, 4, D, D, lib.OPERAND_FP32, lib.ACT_SILU, s)
+            lib.scan_step_selective(y.data_ptr(), c.dr.ptr, c.Ad.data_ptr(), c.br.ptr, c.cr.ptr, c.kd.data_ptr(), c.zr.ptr, c.bd.data_ptr(), scan.data_ptr(),
+                                    out.data_ptr(), scan.data_ptr(), B, D, N, 1, D, D, N, N, D, D, lib.OPERAND_FP32, 1, s)
+
+        out = torch.empty(B, D, device="cuda")
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        for _ in range(3):
+            token(side.cuda_stream)
+        side.synchronize()
+        want = out.clone(), conv.clone(), scan.clone()
+        conv.copy_(begin[0]), scan.copy_(begin[1])
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            token(torch.cuda.current_stream().cuda_stream)
+        for _ in range(3):
+            graph.replay()
+        torch.cuda.synchronize()
+        for got, ref_ in zip((out, conv, scan), want):
+            assert torch.equal(got, ref_)
 
 
 def test_calls_on_two_streams_at_once(lib):

@@ -41,7 +41,8 @@ CONV = dict(x_ptr=OK, w_ptr=OK, bias_ptr=OK, state_in_ptr=OK, lengths_ptr=OK, y_
 
 def test_convolution_refusals(lib):
     shapes = [(dict(B=0), SHAPE), (dict(L=0), SHAPE), (dict(D=-1), SHAPE), (dict(K=0), SHAPE), (dict(K=9), UNSUPPORTED), (dict(ldx=7), SHAPE),
-              (dict(B=1 << 16, L=1 << 15), SHAPE), (dict(D=1 << 25, ldx=1 << 25), SHAPE), (dict(operand=3), UNSUPPORTED),
+              (dict(B=1 << 16, L=1 << 15), SHAPE), (dict(D=1 << 25, ldx=1 << 25), SHAPE), (dict(B=1, L=(1 << 30) + 1), SHAPE),
+              (dict(D=(1 << 22) + 1, ldx=1 << 23), SHAPE), (dict(ldx=1 << 31), SHAPE), (dict(operand=3), UNSUPPORTED),
               (dict(operand=-1), UNSUPPORTED), (dict(act=4), UNSUPPORTED), (dict(act=-1), UNSUPPORTED)]
     refused(lib, lib.conv1d_fwd_causal, CONV, shapes + [
         (dict(x_ptr=0), NULL), (dict(w_ptr=0), NULL), (dict(y_ptr=0), NULL), (dict(ldy=7), SHAPE), (dict(x_ptr=OK + 1), ALIGN),
@@ -124,4 +125,7 @@ def test_workspace_sizes_do_not_wrap(lib):
     assert lib.scan_states_size(8, 1 << 20, 4096, 16) == 8 * (1 << 16) * 4096 * 16 * 4
     assert lib.scan_bwd_selective_workspace_size(8, 1 << 20, 4096, 16, 1) > 1 << 32
     assert lib.conv1d_bwd_causal_workspace_size(8, 1 << 20, 8192, 4) < 1 << 28
+    # the largest extents there are: 2^62 bytes for the partial sums alone
+    assert lib.scan_bwd_selective_workspace_size(1, 1 << 30, 1 << 22, 128, 1 << 22) > 1 << 62
+    assert lib.scan_states_size(1, 1 << 30, 1 << 22, 128) == (1 << 26) * (1 << 22) * 128 * 4
     assert lib.norm_bwd_groups_workspace_size(1 << 20, 4, 4096, 32) >= (1 << 20) * 2 * 4096 * 4
