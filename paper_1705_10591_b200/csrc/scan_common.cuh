@@ -6,6 +6,8 @@
 // never leave the registers.
 #pragma once
 
+#include <type_traits>
+
 #include "seq_common.cuh"
 
 namespace conv2d_b200 {
@@ -55,27 +57,34 @@ __device__ __forceinline__ float softplus(float v) { return softplus(both(v)).x;
 // Sums of NV values over the LANES lanes that differ in the bits LANES/2 * UNIT .. UNIT of the lane index.  While more than one value is left a lane hands half of
 // them over and goes on with the sums of the other half, so that NV - 1 exchanges do for log2(LANES) * NV; at the end v[0 .. left) hold the
 // values first .. first + left, left = max(1, NV / LANES), in every lane whose further bits are anything.
+// A stage of it: of log2(LANES), further ones do nothing.  (`stage` is known when compiled)
+template <int NV, int LANES, int UNIT>
+__device__ __forceinline__ void sum_stage(float (&v)[NV], int lane, int stage)
+{
+    const int m = LANES >> (stage + 1), cnt = NV >> stage;
+    if (m == 0) return;
+    const int mask = m * UNIT;
+    const bool upper = (lane & mask) != 0;
+    if (cnt > 1) {
+#pragma unroll
+        for (int i = 0; i < NV / 2; ++i) {
+            if (i < cnt / 2) {
+                const float send = upper ? v[i] : v[i + cnt / 2], keep = upper ? v[i + cnt / 2] : v[i];
+                v[i] = keep + __shfl_xor_sync(0xffffffffu, send, mask);
+            }
+        }
+    } else {
+        v[0] += __shfl_xor_sync(0xffffffffu, v[0], mask);
+    }
+}
 template <int NV, int LANES, int UNIT>
 __device__ __forceinline__ int sum_over_lanes(float (&v)[NV], int lane)
 {
-    int cnt = NV, first = 0;
+    int first = 0;
 #pragma unroll
-    for (int m = LANES / 2; m >= 1; m /= 2) {
-        const int mask = m * UNIT;
-        const bool upper = (lane & mask) != 0;
-        if (cnt > 1) {
-            cnt /= 2;
-#pragma unroll
-            for (int i = 0; i < NV / 2; ++i) {
-                if (i < cnt) {
-                    const float send = upper ? v[i] : v[i + cnt], keep = upper ? v[i + cnt] : v[i];
-                    v[i] = keep + __shfl_xor_sync(0xffffffffu, send, mask);
-                }
-            }
-            if (upper) first += cnt;
-        } else {
-            v[0] += __shfl_xor_sync(0xffffffffu, v[0], mask);
-        }
+    for (int stage = 0; LANES >> (stage + 1); ++stage) {
+        sum_stage<NV, LANES, UNIT>(v, lane, stage);
+        if (NV >> stage > 1 && (lane & (LANES >> (stage + 1)) * UNIT)) first += NV >> (stage + 1);
     }
     return first;
 }

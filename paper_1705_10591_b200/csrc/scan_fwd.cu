@@ -12,7 +12,7 @@ int states_of_lane(int N) { return N > 64 ? 8 : 4; }
 struct FwdCut { int segs, rows; };
 FwdCut fwd_cut(int B, int L, int D, int N, int G)
 {
-    const int nl = lanes_for(N, states_of_lane(N)), cb = (nl >= 8 ? 8 : 4) * 32 / nl;
+    const int nl = lanes_for(N, states_of_lane(N)), cb = (nl >= 16 ? 8 : 4) * 32 / nl;
     const long long blocks = (long long)B * G * ceil_div_u(D / G, cb);
     long long segs = blocks * 3 <= 148 ? 2 * 148 / blocks : 1;
     if (segs > L / 64) segs = L / 64;
@@ -56,6 +56,7 @@ conv2d_status_t fwd(const ScanSeq& s, cudaStream_t stream)
     a.segs = cut.segs, a.seg_rows = cut.rows, a.blocks_group = 0;
     a.u_unit = copy_unit(s.u, s.ldu, a.E, e), a.delta_unit = copy_unit(s.delta, s.lddelta, a.E, e), a.z_unit = copy_unit(s.z, s.ldz, a.E, e);
     a.B_unit = copy_unit(s.Bm, s.ldB, a.N, e), a.C_unit = copy_unit(s.Cm, s.ldC, a.N, e);
+    a.wide = a.u_unit == 16 && a.delta_unit == 16 && (!s.z || a.z_unit == 16) && a.B_unit == 16 && a.C_unit == 16;
     a.y_quads = a.E % 4 == 0 && rows_aligned(s.y, s.ldy, e, 4 * e);
     a.local = s.ws;
     a.steps = s.ws ? s.ws + (size_t)s.B * a.segs * s.D * round4(s.N) : nullptr;
