@@ -147,6 +147,26 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
                 return Row{sp[t * CB], gp[t * CB], *reinterpret_cast<const float4*>(Bp + t * NP), *reinterpret_cast<const float4*>(Cp + t * NP)};
             };
             Row next_row = read(TT - 1);
+            // The sums over the lanes of four rows are joined between the next four rows: a warp issues in order, and would wait for each exchange
+            float n_prev[8], v_prev[4];
+            auto join = [&](int stage) {
+                sum_stage<4, NL, CL>(v_prev, lane, stage);
+                sum_stage<8, NL, CL>(n_prev, lane, stage);
+            };
+            auto store = [&](int tq) {
+                constexpr int v_left = NL >= 4 ? 1 : 4 / NL, n_left = NL >= 8 ? 1 : 8 / NL;
+                if (first_of_equals<4, NL, CL>(lane)) {
+#pragma unroll
+                    for (int i = 0; i < v_left; ++i) vs[(tq + first_value<4, NL, CL>(lane) + i) * YS] = v_prev[i];
+                }
+                if (first_of_equals<8, NL, CL>(lane)) {
+#pragma unroll
+                    for (int i = 0; i < n_left; ++i) {
+                        const int id = first_value<8, NL, CL>(lane) + i;
+                        (id >> 2 ? s2 : s1)[(tq + (id & 3)) * YS] = n_prev[i];
+                    }
+                }
+            };
 #pragma unroll
             for (int tq = TT - 4; tq >= 0; tq -= 4) {
                 float n_sums[8], v[4];                        // sum_n A2 q of four rows, then sum_n e B; sum_n C h
@@ -183,25 +203,19 @@ __global__ void __launch_bounds__(ScanBwdTile<NL>::TH, 2) scan_bwd_kernel(const 
                         pp[t * 64] = make_float4(db[0], db[1], db[2], db[3]);
                         pp[t * 64 + 32] = make_float4(dc[0], dc[1], dc[2], dc[3]);
                     }
-                }
-                {
-                    constexpr int left = NL >= 4 ? 1 : 4 / NL;
-                    const int first = sum_over_lanes<4, NL, CL>(v, lane);
-                    if (first_of_equals<4, NL, CL>(lane)) {
-#pragma unroll
-                        for (int i = 0; i < left; ++i) vs[(tq + first + i) * YS] = v[i];
+                    if (tq < TT - 4) {
+                        join(3 - j);
+                        if (j == 0) join(4), store(tq + 4);
                     }
                 }
-                constexpr int left = NL >= 8 ? 1 : 8 / NL;
-                const int first = sum_over_lanes<8, NL, CL>(n_sums, lane);
-                if (first_of_equals<8, NL, CL>(lane)) {
 #pragma unroll
-                    for (int i = 0; i < left; ++i) {
-                        const int id = first + i;
-                        (id >> 2 ? s2 : s1)[(tq + (id & 3)) * YS] = n_sums[i];
-                    }
-                }
+                for (int i = 0; i < 8; ++i) n_prev[i] = n_sums[i];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v_prev[i] = v[i];
             }
+#pragma unroll
+            for (int stage = 0; NL >> (stage + 1); ++stage) join(stage);
+            store(0);
             carry4[set * SETS_TH + tid] = make_float4(carry[0].x, carry[0].y, carry[1].x, carry[1].y);
             dA4[set * SETS_TH + tid] = make_float4(dA[0].x, dA[0].y, dA[1].x, dA[1].y);
             set = next_set, tile = next_tile;

@@ -78,14 +78,18 @@ __device__ __forceinline__ void sum_stage(float (&v)[NV], int lane, int stage)
     }
 }
 template <int NV, int LANES, int UNIT>
-__device__ __forceinline__ int sum_over_lanes(float (&v)[NV], int lane)
+__device__ __forceinline__ void sum_over_lanes(float (&v)[NV], int lane)
+{
+#pragma unroll
+    for (int stage = 0; LANES >> (stage + 1); ++stage) sum_stage<NV, LANES, UNIT>(v, lane, stage);
+}
+template <int NV, int LANES, int UNIT>
+__device__ __forceinline__ int first_value(int lane)
 {
     int first = 0;
 #pragma unroll
-    for (int stage = 0; LANES >> (stage + 1); ++stage) {
-        sum_stage<NV, LANES, UNIT>(v, lane, stage);
+    for (int stage = 0; LANES >> (stage + 1); ++stage)
         if (NV >> stage > 1 && (lane & (LANES >> (stage + 1)) * UNIT)) first += NV >> (stage + 1);
-    }
     return first;
 }
 // Whether this lane is the one of its equals that stores them: the bits that sum_over_lanes went through with a single value left are zero.
