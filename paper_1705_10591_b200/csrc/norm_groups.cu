@@ -12,6 +12,10 @@
 //            memory; the blocks exchange their statistics through distributed shared memory.
 //   stream   slabs that do not fit, or too few of them to fill the machine: one kernel for the statistics of parts, one that reads
 //            the elements again (from L2 where they are still there).
+// Measured: rows 28.9 us for 8192 x 4096 in bf16 (4.7 TB/s; the floor is 20.8, what is left is the two sums over lanes in a row and the few samples
+// that a thread has under way).  Stream, forward, 8 x 4096 x 512 in fp16 27 us (statistics 10.6 at 3.2 TB/s, output 19.3 under a profiler: issue
+// slots, about 40 instructions a pack of eight elements with its activation, and half-filled second turns of blocks); training step of 32 x 3136 x 256 in
+// bf16 92.4 us: 12.4 + 23.9 forward, 29.7 + 30.5 backward, 3.3 for the parameters' gradients.
 // Statistics of a part are taken around one of its own values and joined by counts and means, so that a mean far
 // from zero costs no digits.
 #include <cooperative_groups.h>
@@ -334,8 +338,9 @@ __global__ void __launch_bounds__(kRowThreads) norm_rows_bwd_kernel(const NormAr
 
 // What a block takes: `groups` groups of sample n from channel c0 on, rows r0 .. r1.  A thread keeps to one pack of channels (pack, of group `group`) and
 // takes every `step`th row from `first` on, `count` in all; wider rows than the block has threads (one group then) are taken a block's
-// width at a time, in `turns`.
-template <typename T, int V>
+// width at a time, in `turns`.  The second kernel of a stream walks its rows backwards: what the first has read last is what L2 still holds (32 x 3136 x 512
+// in bf16 forward 70.6 us, 68.6 so; no difference for tensors that fit).
+template <typename T, int V, bool BACKWARDS>
 struct Part {
     int part, groups, g0, c0, packs, ev, step, turns, r0, r1, pack, group, first, count;
     long long n;
@@ -364,7 +369,10 @@ struct Part {
             turns = (packs + kThreads - 1) / kThreads;
         }
         count = pack >= 0 && first < r1 ? (r1 - first + step - 1) / step : 0;
+        if (BACKWARDS && count) first += (count - 1) * step;
     }
+    // rows from one of the thread's to its next
+    __device__ long long stride() const { return BACKWARDS ? -step : step; }
     // the pack of this thread in turn q, or -1; and its rows then
     __device__ int pack_of(int q) const
     {
@@ -375,8 +383,8 @@ struct Part {
 };
 
 // Sums over the threads that hold group gi of what `value` gives for a thread index, by one warp.
-template <int N, typename T, int V, typename F>
-__device__ __forceinline__ void group_sums(const Part<T, V>& p, int gi, float (&s)[N], F value)
+template <int N, typename P, typename F>
+__device__ __forceinline__ void group_sums(const P& p, int gi, float (&s)[N], F value)
 {
     const int lane = threadIdx.x & 31;
 #pragma unroll
@@ -462,7 +470,7 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
     float4* gstat = smem4;                                   // [tile_groups] count, mean, sum of squares about it; then mean, rstd
     float2* gnorm = reinterpret_cast<float2*>(gstat + a.tile_groups);
     unsigned char* rows = reinterpret_cast<unsigned char*>(reinterpret_cast<float4*>(gnorm) + (a.tile_groups + 1) / 2);
-    const Part<T, V> p(a);
+    const Part<T, V, MODE == kStreamApply> p(a);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int g0 = p.g0;
     const T* x = a.x + (p.n * a.S + p.first) * a.ldx + p.c0;
@@ -471,7 +479,7 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
         Rows r;
         r.count = p.count_of(q);
         // (turns take whole rows: a part's rows each)
-        r.ring = {rows + ((KEEP ? q * thread_slots(a.part_rows) * kThreads : 0) + threadIdx.x) * Rows::bytes, x + (r.count ? p.pack_of(q) * V : 0), p.step * a.ldx};
+        r.ring = {rows + ((KEEP ? q * thread_slots(a.part_rows) * kThreads : 0) + threadIdx.x) * Rows::bytes, x + (r.count ? p.pack_of(q) * V : 0), p.stride() * a.ldx};
         return r;
     };
 
@@ -558,7 +566,7 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
     // the statistics stay readable until all blocks of the cluster have them
     if (KEEP) cg::this_cluster().sync();
     else __syncthreads();
-    const long long ystep = p.step * a.ldy;
+    const long long ystep = p.stride() * a.ldy;
     for (int q = 0; q < p.turns; ++q) {
         const Rows r = rows_of(q);
         if (r.count == 0) continue;
@@ -606,7 +614,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_slab_bwd_kernel(const NormAr
     float2* gmean = reinterpret_cast<float2*>(gsum + a.tile_groups);
     float* csum = reinterpret_cast<float*>(reinterpret_cast<float4*>(gmean) + (a.tile_groups + 1) / 2);       // [2][kThreads * V]
     unsigned char* rows = reinterpret_cast<unsigned char*>(csum + (MODE == kStreamApply ? 0 : 2 * kThreads * V));
-    const Part<T, V> p(a);
+    const Part<T, V, MODE == kStreamApply> p(a);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int g0 = p.g0, width = p.packs * V, kept = KEEP ? thread_slots(p.turns == 1 ? (a.part_rows + p.step - 1) / p.step : a.part_rows) : 0;
     const T* x = a.x + (p.n * a.S + p.first) * a.ldx + p.c0;
@@ -616,7 +624,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_slab_bwd_kernel(const NormAr
         const size_t before = KEEP ? ((size_t)second * p.turns + q) * kept * kThreads * Rows::bytes : second * ring_bytes<T, V>;
         Rows r;
         r.count = p.count_of(q);
-        r.ring = {rows + before + threadIdx.x * Rows::bytes, (second ? dy : x) + (r.count ? p.pack_of(q) * V : 0), p.step * (second ? a.lddy : a.ldx)};
+        r.ring = {rows + before + threadIdx.x * Rows::bytes, (second ? dy : x) + (r.count ? p.pack_of(q) * V : 0), p.stride() * (second ? a.lddy : a.ldx)};
         return r;
     };
     // x^ and d of the rows of a group
@@ -735,7 +743,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_slab_bwd_kernel(const NormAr
     }
     if (KEEP) cg::this_cluster().sync();
     else __syncthreads();
-    const long long dxstep = p.step * a.lddx;
+    const long long dxstep = p.stride() * a.lddx;
     for (int q = 0; q < p.turns; ++q) {
         const Rows rx = rows_of(q, false), rg = rows_of(q, true);
         if (rx.count == 0) continue;
@@ -821,7 +829,7 @@ NormPlan make_norm_plan(int N, int S, int C, int G, int esize, int V, bool bwd)
         if (p.slab) break;
     }
     while (p.slab && parts < kMaxCluster && (long long)N * p.tiles * parts < kSms && S / parts >= 64) parts *= 2;
-    // Large tensors are faster as a stream (32 x 3136 x 256 in bf16, forward and backward: 99 us, as slabs 138), whose second reading L2
+    // Large tensors are faster as a stream (32 x 3136 x 256 in bf16, forward and backward: 92 us, as slabs 138), whose second reading L2
     // serves in part; slabs save a launch and the reading below that (4 x 1024 x 256: 8 us forward, 10 as a stream).
     const int choice = env_int("CONV2D_B200_NORM_STREAM", 0);
     if (choice == 0 ? (size_t)N * S * C * esize > (bwd ? 16u : 24u) << 20 : choice > 0) p.slab = false;
