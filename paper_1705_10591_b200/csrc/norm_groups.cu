@@ -29,7 +29,10 @@ namespace cg = cooperative_groups;
 
 constexpr int kRowThreads = 256;        // rows
 constexpr int kThreads = 256, kWarps = kThreads / 32;        // slab, stream
-constexpr int kGroup = 2, kRing = 4;    // rows of a group (four take the backward pass to 240 registers), groups of a ring
+constexpr int kRing = 4;                // groups of a ring
+// Rows of a group: two (four take the backward pass to 240 registers); eight of single elements, whose loads, where they are too narrow to be copied
+// asynchronously, wait for memory once a group (1 x 5795 x 4064 in groups of 127, bf16: 138 us with two).
+template <int V> constexpr int kGroup = V == 1 ? 8 : 2;
 
 template <typename T>
 struct NormArgs {
@@ -402,14 +405,14 @@ __device__ __forceinline__ void group_sums(const P& p, int gi, float (&s)[N], F 
 
 enum { kSlab = 0, kStreamStats = 1, kStreamApply = 2 };
 
-// Slots that a thread needs for its rows: whole groups.
-__host__ __device__ constexpr int thread_slots(int rows) { return (rows + kGroup - 1) / kGroup * kGroup; }
+// Slots that a thread needs for its rows: whole groups of `group`.
+__host__ __device__ constexpr int thread_slots(int rows, int group) { return (rows + group - 1) / group * group; }
 
 // The packs of one tensor that a thread takes: rows first, first + step, .. of its channels.  A slab's stay in shared memory, all under way at once;
 // a stream's go through a ring.
 template <typename T, int V, bool KEEP>
 struct ThreadRows {
-    using Ring = RowRing<T, V, kThreads, kGroup, kRing>;
+    using Ring = RowRing<T, V, kThreads, kGroup<V>, kRing>;
     static constexpr int bytes = V * (int)sizeof(T);
     Ring ring;                          // (KEEP: mine is the first of all slots)
     int count;
@@ -432,31 +435,31 @@ struct ThreadRows {
         return ring.get(q, i, j, count);
     }
 };
-template <typename T, int V> constexpr size_t ring_bytes = RowRing<T, V, kThreads, kGroup, kRing>::smem;
+template <typename T, int V> constexpr size_t ring_bytes = RowRing<T, V, kThreads, kGroup<V>, kRing>::smem;
 
 // Walks `count` rows of the thread in groups: `issue(q, i)` starts the copies of group q, `take(q, i, whole)` uses it.
-template <bool KEEP, typename Issue, typename Take>
+template <bool KEEP, int GROUP, typename Issue, typename Take>
 __device__ __forceinline__ void walk_rows(int count, Issue issue, Take take)
 {
     if (!KEEP) {
 #pragma unroll
         for (int q = 0; q < kRing - 1; ++q) {
-            issue(q, q * kGroup);
+            issue(q, q * GROUP);
             copies_commit();
         }
     }
     int q = 0;
 #pragma unroll 1
-    for (int i = 0; i + kGroup <= count; i += kGroup, ++q) {
+    for (int i = 0; i + GROUP <= count; i += GROUP, ++q) {
         if (!KEEP) copies_wait<kRing - 2>();
         take(q, i, Whole());
         if (!KEEP) {
-            issue(q + kRing - 1, i + (kRing - 1) * kGroup);
+            issue(q + kRing - 1, i + (kRing - 1) * GROUP);
             copies_commit();
         }
     }
     if (!KEEP) copies_wait<0>();
-    if (q * kGroup < count) take(q, q * kGroup, Cut());
+    if (q * GROUP < count) take(q, q * GROUP, Cut());
 }
 
 template <typename T, int V, int MODE>
@@ -479,7 +482,7 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
         Rows r;
         r.count = p.count_of(q);
         // (turns take whole rows: a part's rows each)
-        r.ring = {rows + ((KEEP ? q * thread_slots(a.part_rows) * kThreads : 0) + threadIdx.x) * Rows::bytes, x + (r.count ? p.pack_of(q) * V : 0), p.stride() * a.ldx};
+        r.ring = {rows + ((KEEP ? q * thread_slots(a.part_rows, kGroup<V>) * kThreads : 0) + threadIdx.x) * Rows::bytes, x + (r.count ? p.pack_of(q) * V : 0), p.stride() * a.ldx};
         return r;
     };
 
@@ -494,13 +497,13 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
         int count = 0;
         for (int q = 0; q < p.turns; ++q) {
             const Rows r = rows_of(q);
-            walk_rows<KEEP>(r.count, [&](int g, int i) { r.ring.issue(g, i, r.count); }, [&](int g, int i, auto whole) {
-                float2 v[kGroup][P];
+            walk_rows<KEEP, kGroup<V>>(r.count, [&](int g, int i) { r.ring.issue(g, i, r.count); }, [&](int g, int i, auto whole) {
+                float2 v[kGroup<V>][P];
 #pragma unroll
-                for (int j = 0; j < kGroup; ++j) pairs<T, V>(r.get(g, i, j), v[j]);
+                for (int j = 0; j < kGroup<V>; ++j) pairs<T, V>(r.get(g, i, j), v[j]);
                 if (i == 0 && q == 0) shift = v[0][0].x;
 #pragma unroll
-                for (int j = 0; j < kGroup; ++j) {
+                for (int j = 0; j < kGroup<V>; ++j) {
                     if (!decltype(whole)::value && i + j >= r.count) break;
 #pragma unroll
                     for (int k = 0; k < P; ++k) {
@@ -577,10 +580,10 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
         load_scale<V>(a.gamma, a.beta, p.c0 + pk * V, true, scale, add);
 #pragma unroll
         for (int k = 0; k < P; ++k) scale[k] = __fmul2_rn(scale[k], both(st.y));
-        walk_rows<KEEP>(r.count, [&](int g, int i) { r.ring.issue(g, i, r.count); }, [&](int g, int i, auto whole) {
-            float o[kGroup * 2 * P];
+        walk_rows<KEEP, kGroup<V>>(r.count, [&](int g, int i) { r.ring.issue(g, i, r.count); }, [&](int g, int i, auto whole) {
+            float o[kGroup<V> * 2 * P];
 #pragma unroll
-            for (int j = 0; j < kGroup; ++j) {
+            for (int j = 0; j < kGroup<V>; ++j) {
                 float2 v[P];
                 pairs<T, V>(r.get(g, i, j), v);
 #pragma unroll
@@ -591,7 +594,7 @@ __global__ void __launch_bounds__(kThreads) norm_slab_fwd_kernel(const NormArgs<
             }
             activate(o, a.act);
 #pragma unroll
-            for (int j = 0; j < kGroup; ++j) {
+            for (int j = 0; j < kGroup<V>; ++j) {
                 float2 v[P];
 #pragma unroll
                 for (int k = 0; k < P; ++k) v[k] = make_float2(o[2 * (j * P + k)], o[2 * (j * P + k) + 1]);
@@ -616,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_slab_bwd_kernel(const NormAr
     unsigned char* rows = reinterpret_cast<unsigned char*>(csum + (MODE == kStreamApply ? 0 : 2 * kThreads * V));
     const Part<T, V, MODE == kStreamApply> p(a);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int g0 = p.g0, width = p.packs * V, kept = KEEP ? thread_slots(p.turns == 1 ? (a.part_rows + p.step - 1) / p.step : a.part_rows) : 0;
+    const int g0 = p.g0, width = p.packs * V, kept = KEEP ? thread_slots(p.turns == 1 ? (a.part_rows + p.step - 1) / p.step : a.part_rows, kGroup<V>) : 0;
     const T* x = a.x + (p.n * a.S + p.first) * a.ldx + p.c0;
     const T* dy = a.dy + (p.n * a.S + p.first) * a.lddy + p.c0;
     using Rows = ThreadRows<T, V, KEEP>;
@@ -636,10 +639,10 @@ __global__ void __launch_bounds__(kThreads, 2) norm_slab_bwd_kernel(const NormAr
         load_scale<V>(a.gamma, a.beta, p.c0 + pk * V, true, r.gamma, r.beta);
         return r;
     };
-    auto terms = [&](const Params& m, const Rows& rx, const Rows& rg, int g, int i, float2 (&xn)[kGroup][P], float (&d)[kGroup * 2 * P]) {
-        float pre[kGroup * 2 * P];
+    auto terms = [&](const Params& m, const Rows& rx, const Rows& rg, int g, int i, float2 (&xn)[kGroup<V>][P], float (&d)[kGroup<V> * 2 * P]) {
+        float pre[kGroup<V> * 2 * P];
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j) {
+        for (int j = 0; j < kGroup<V>; ++j) {
             float2 w[P];
             pairs<T, V>(rx.get(g, i, j), xn[j]);
             pairs<T, V>(rg.get(g, i, j), w);
@@ -669,12 +672,12 @@ __global__ void __launch_bounds__(kThreads, 2) norm_slab_bwd_kernel(const NormAr
             for (int k = 0; k < P; ++k) s1[k] = s2[k] = both(0.f);
             if (rx.count) {
                 const Params m = params_of(pk);
-                walk_rows<KEEP>(rx.count, [&](int g, int i) { rx.ring.issue(g, i, rx.count), rg.ring.issue(g, i, rx.count); }, [&](int g, int i, auto whole) {
-                    float2 xn[kGroup][P];
-                    float d[kGroup * 2 * P];
+                walk_rows<KEEP, kGroup<V>>(rx.count, [&](int g, int i) { rx.ring.issue(g, i, rx.count), rg.ring.issue(g, i, rx.count); }, [&](int g, int i, auto whole) {
+                    float2 xn[kGroup<V>][P];
+                    float d[kGroup<V> * 2 * P];
                     terms(m, rx, rg, g, i, xn, d);
 #pragma unroll
-                    for (int j = 0; j < kGroup; ++j) {
+                    for (int j = 0; j < kGroup<V>; ++j) {
                         if (!decltype(whole)::value && i + j >= rx.count) break;
 #pragma unroll
                         for (int k = 0; k < P; ++k) {
@@ -751,12 +754,12 @@ __global__ void __launch_bounds__(kThreads, 2) norm_slab_bwd_kernel(const NormAr
         const float2 mm = gmean[p.group];
         const Params m = params_of(pk);
         T* dx = a.dx + (p.n * a.S + p.first) * a.lddx + p.c0 + pk * V;
-        walk_rows<KEEP>(rx.count, [&](int g, int i) { rx.ring.issue(g, i, rx.count), rg.ring.issue(g, i, rx.count); }, [&](int g, int i, auto whole) {
-            float2 xn[kGroup][P];
-            float d[kGroup * 2 * P];
+        walk_rows<KEEP, kGroup<V>>(rx.count, [&](int g, int i) { rx.ring.issue(g, i, rx.count), rg.ring.issue(g, i, rx.count); }, [&](int g, int i, auto whole) {
+            float2 xn[kGroup<V>][P];
+            float d[kGroup<V> * 2 * P];
             terms(m, rx, rg, g, i, xn, d);
 #pragma unroll
-            for (int j = 0; j < kGroup; ++j) {
+            for (int j = 0; j < kGroup<V>; ++j) {
                 float2 o[P];
 #pragma unroll
                 for (int k = 0; k < P; ++k) {
@@ -776,10 +779,10 @@ constexpr size_t kSlabBytes = 64 * 1024;      // rows that a block keeps: three 
 constexpr int kMaxCluster = 8, kSms = 148;
 
 // Slots of 16 bytes (of an element, without packs) that the threads of a slab's block need, in bytes: threads that a row leaves over have some, too.
-size_t slab_bytes(int part_rows, int packs, int pack_bytes, bool bwd)
+size_t slab_bytes(int part_rows, int packs, int pack_bytes, int group, bool bwd)
 {
     const int step = packs <= kThreads ? kThreads / packs : 1, turns = packs <= kThreads ? 1 : (packs + kThreads - 1) / kThreads;
-    return (size_t)thread_slots((part_rows + step - 1) / step) * turns * kThreads * pack_bytes * (bwd ? 2 : 1);
+    return (size_t)thread_slots((part_rows + step - 1) / step, group) * turns * kThreads * pack_bytes * (bwd ? 2 : 1);
 }
 
 // How a call is cut.  The sizes decide, and whether rows can be moved in packs of 16 bytes; the workspace has room for either.
@@ -822,7 +825,7 @@ NormPlan make_norm_plan(int N, int S, int C, int G, int esize, int V, bool bwd)
         p.tile_groups = tile(bytes);
         p.tiles = (G + p.tile_groups - 1) / p.tile_groups;
         // a cluster of the fewest blocks that hold the slab; more while there are SMs left and rows to share out
-        const auto need = [&](int n) { return slab_bytes((S + n - 1) / n, p.tile_groups * ev, V * esize, bwd); };
+        const auto need = [&](int n) { return slab_bytes((S + n - 1) / n, p.tile_groups * ev, V * esize, V == 1 ? kGroup<1> : kGroup<2>, bwd); };
         parts = 1;
         while (parts < kMaxCluster && need(parts) > kSlabBytes) parts *= 2;
         p.slab = need(parts) <= kSlabBytes;
@@ -930,7 +933,7 @@ conv2d_status_t fwd(const NormSeq& s, cudaStream_t stream)
     const long long blocks = (long long)s.N * p.tiles * p.parts;
     const size_t fixed = (size_t)p.tile_groups * 16 + (p.tile_groups + 1) / 2 * 16;
     if (p.slab) {
-        const size_t smem = fixed + slab_bytes(p.part_rows, p.tile_groups * (a.E / V), V * sizeof(T), false);
+        const size_t smem = fixed + slab_bytes(p.part_rows, p.tile_groups * (a.E / V), V * sizeof(T), kGroup<V>, false);
         static SmemLimit limit;
         if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_fwd_kernel<T, V, kSlab>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
         return launched(norm_slab_fwd_kernel<T, V, kSlab>, blocks, kThreads, smem, p.parts, stream, a);
@@ -959,7 +962,7 @@ conv2d_status_t bwd(const NormSeq& s, cudaStream_t stream)
         const long long blocks = (long long)s.N * p.tiles * p.parts;
         const size_t fixed = (size_t)p.tile_groups * 16 + (p.tile_groups + 1) / 2 * 16, sums = sizeof(float) * 2 * kThreads * V;
         if (p.slab) {
-            const size_t smem = fixed + sums + slab_bytes(p.part_rows, p.tile_groups * (a.E / V), V * sizeof(T), true);
+            const size_t smem = fixed + sums + slab_bytes(p.part_rows, p.tile_groups * (a.E / V), V * sizeof(T), kGroup<V>, true);
             static SmemLimit limit;
             if (raise_smem_limit(reinterpret_cast<const void*>(norm_slab_bwd_kernel<T, V, kSlab>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
             st = launched(norm_slab_bwd_kernel<T, V, kSlab>, blocks, kThreads, smem, p.parts, stream, a);
