@@ -51,8 +51,11 @@ BwdCut bwd_cut(int B, int L, int D, int N, int G)
     const int E = D / G;
     // a block's partial sums of dB and dC are for 32 channels, or the workspace would be larger than the tensors (16 channels with more than 64
     // states: more sets do not fit into shared memory)
-    const int sets = c.cb >= 32 ? 1 : 32 / c.cb;
-    c.sets = env_int("CONV2D_B200_SCAN_SETS", sets > 4 ? 4 : sets);
+    int sets = c.cb >= 32 ? 1 : 32 / c.cb;
+    if (sets > 4) sets = 4;
+    // fewer where half the machine would have no block, cut into segments as below (1 x 246 x 128 in two groups, 64 states, with the forward pass: 100 us with four sets, 61 with one)
+    while (sets > 1 && (long long)B * G * ceil_div_u(E, (long long)c.cb * sets) * (L < 128 ? 1 : L / 64) * 2 <= 148) sets /= 2;
+    c.sets = env_int("CONV2D_B200_SCAN_SETS", sets);
     if (c.sets < 1) c.sets = 1;
     c.blocks_group = (int)ceil_div_u(E, (long long)c.cb * c.sets);
     // segments of time, where the blocks leave two thirds of the machine idle: two blocks for every SM then, of 64 rows at least
