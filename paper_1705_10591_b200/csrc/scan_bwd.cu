@@ -94,8 +94,8 @@ conv2d_status_t bwd(const ScanSeq& s, cudaStream_t stream)
     a.A = s.A, a.Dskip = s.Dskip, a.delta_bias = s.delta_bias, a.states = s.states_in, a.dstate_out = s.dstate_out, a.lengths = s.lengths;
     a.du = static_cast<T*>(s.du), a.ddelta = static_cast<T*>(s.ddelta), a.dz = static_cast<T*>(s.dz), a.dstate_in = s.dstate_in;
     a.B = s.B, a.L = s.L, a.D = s.D, a.N = s.N, a.G = s.G, a.E = s.D / s.G;
-    a.ldu = (int)s.ldu, a.lddelta = (int)s.lddelta, a.ldB = (int)s.ldB, a.ldC = (int)s.ldC, a.ldz = (int)s.ldz, a.lddy = (int)s.lddy;
-    a.lddu = (int)s.lddu, a.ldddelta = (int)s.ldddelta, a.lddz = (int)s.lddz, a.softplus = s.softplus;
+    a.ldu = (int)s.ldu, a.lddelta = (int)s.lddelta, a.ldB = (int)s.ldB, a.ldC = (int)s.ldC, a.ldz = s.z ? (int)s.ldz : 0, a.lddy = (int)s.lddy;
+    a.lddu = (int)s.lddu, a.ldddelta = (int)s.ldddelta, a.lddz = s.dz ? (int)s.lddz : 0, a.softplus = s.softplus;
     const BwdCut c = bwd_cut(s.B, s.L, s.D, s.N, s.G);
     const BwdLayout o = bwd_layout(c, s.B, s.L, s.D, s.N, s.G);
     a.segs = c.segs, a.seg_rows = c.rows, a.blocks_group = c.blocks_group, a.sets = c.sets;

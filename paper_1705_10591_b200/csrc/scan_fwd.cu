@@ -51,7 +51,7 @@ conv2d_status_t fwd(const ScanSeq& s, cudaStream_t stream)
     a.A = s.A, a.Dskip = s.Dskip, a.delta_bias = s.delta_bias, a.state_in = s.state_in, a.lengths = s.lengths;
     a.y = static_cast<T*>(s.y), a.state_out = s.state_out, a.states = s.states;
     a.B = s.B, a.L = s.L, a.D = s.D, a.N = s.N, a.G = s.G, a.E = s.D / s.G;
-    a.ldu = (int)s.ldu, a.lddelta = (int)s.lddelta, a.ldB = (int)s.ldB, a.ldC = (int)s.ldC, a.ldz = (int)s.ldz, a.ldy = (int)s.ldy, a.softplus = s.softplus;
+    a.ldu = (int)s.ldu, a.lddelta = (int)s.lddelta, a.ldB = (int)s.ldB, a.ldC = (int)s.ldC, a.ldz = s.z ? (int)s.ldz : 0, a.ldy = (int)s.ldy, a.softplus = s.softplus;
     const FwdCut cut = fwd_cut(s.B, s.L, s.D, s.N, s.G);
     a.segs = cut.segs, a.seg_rows = cut.rows, a.blocks_group = 0;
     a.u_unit = copy_unit(s.u, s.ldu, a.E, e), a.delta_unit = copy_unit(s.delta, s.lddelta, a.E, e), a.z_unit = copy_unit(s.z, s.ldz, a.E, e);

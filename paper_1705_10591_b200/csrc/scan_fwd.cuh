@@ -214,13 +214,12 @@ __global__ void __launch_bounds__(ScanFwdTile<NL, SPT>::TH, 2) scan_fwd_kernel(c
             const int t = t_begin + k * TT, rows = live - t;
             const T *u = ub + (long long)t * a.ldu, *s = db + (long long)t * a.lddelta, *z = zb + (long long)t * a.ldz;
             const T *Bt = Bb + (long long)t * a.ldB, *Ct = Cb + (long long)t * a.ldC;
-            const int zrows = !STATE_ONLY && a.z ? rows : 0;
             if (WIDE && a.wide) {
                 copy_tile_by<TT, CB, 16, HT>(p, u, a.ldu, rows, nch, tid);
                 copy_tile_by<TT, CB, 16, HT>(p + TT * CB, s, a.lddelta, rows, nch, tid);
                 copy_tile_by<TT, NP, 16, HT>(p + 3 * TT * CB, Bt, a.ldB, rows, a.N, tid);
                 if (!STATE_ONLY) {
-                    copy_tile_by<TT, CB, 16, HT>(p + 2 * TT * CB, z, a.ldz, zrows, nch, tid);
+                    if (a.z) copy_tile_by<TT, CB, 16, HT>(p + 2 * TT * CB, z, a.ldz, rows, nch, tid);
                     copy_tile_by<TT, NP, 16, HT>(p + 3 * TT * CB + TT * NP, Ct, a.ldC, rows, a.N, tid);
                 }
             } else {
@@ -228,7 +227,7 @@ __global__ void __launch_bounds__(ScanFwdTile<NL, SPT>::TH, 2) scan_fwd_kernel(c
                 copy_tile<TT, CB, HT>(p + TT * CB, s, a.lddelta, rows, nch, a.delta_unit, tid);
                 copy_tile<TT, NP, HT>(p + 3 * TT * CB, Bt, a.ldB, rows, a.N, a.B_unit, tid);
                 if (!STATE_ONLY) {
-                    copy_tile<TT, CB, HT>(p + 2 * TT * CB, z, a.ldz, zrows, nch, a.z_unit, tid);
+                    if (a.z) copy_tile<TT, CB, HT>(p + 2 * TT * CB, z, a.ldz, rows, nch, a.z_unit, tid);
                     copy_tile<TT, NP, HT>(p + 3 * TT * CB + TT * NP, Ct, a.ldC, rows, a.N, a.C_unit, tid);
                 }
             }

@@ -1,0 +1,44 @@
+"""Calls of the operators along a sequence that their headers allow and that are easily missed: row distances of tensors that are not given."""
+import pytest
+import torch
+
+from test_gpu_sequence import ScanCase, backward, draw, lib, operand, stream, workspace  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("type, L, D, N", [("bf16", 100, 64, 16), ("fp32", 50, 12, 16), ("fp16", 40, 30, 5)])
+@pytest.mark.parametrize("ldz", [0, 7, -5, 1 << 40])
+def test_the_row_distance_of_an_absent_gate_is_not_looked_at(lib, type, L, D, N, ldz, monkeypatch):  # noqa: F811
+    """Without z no address is made from ldz: whole sequences, segments, single tokens and gradients have the bits that they have with ldz = D."""
+    for segs in (None, "2"):
+        if segs:
+            monkeypatch.setenv("CONV2D_B200_SCAN_SEGS", segs)
+            monkeypatch.setenv("CONV2D_B200_SCAN_BWD_SEGS", segs)
+        c = ScanCase(lib, (type, 2, L, D, N, 1, True, False, True, True, [L, 21], 0, 0))
+        states = workspace(lib.scan_states_size(2, L, D, N))
+        want, last = c.forward(states=states).result(), torch.empty(2, D, N, device="cuda")
+        need = lib.scan_fwd_selective_workspace_size(2, L, D, N, 1)
+        ws, got = workspace(need), torch.empty_like(want)
+        lib.scan_fwd_selective(*c.inputs(), c.sd.data_ptr(), c.lengths.data_ptr(), got.data_ptr(), last.data_ptr(), 0, 2, L, D, N, 1, c.ur.ld, c.dr.ld,
+                               c.br.ld, c.cr.ld, ldz, D, operand(lib, type), c.flags(), ws.data_ptr(), need, stream())
+        assert torch.equal(got, want)
+    dy = draw(600, 2, L, D, dtype=c.t)
+    grads = backward(c, states, dy, None)
+    need = lib.scan_bwd_selective_workspace_size(2, L, D, N, 1)
+    ws, dyd = workspace(need), dy.to(c.t).cuda()
+    new = lambda *s, t=torch.float32: torch.empty(s, dtype=t, device="cuda")  # noqa: E731
+    out = [new(2, L, D, t=c.t), new(2, L, D, t=c.t), new(D, N), new(2, L, N, t=c.t), new(2, L, N, t=c.t), new(D), None, new(D), new(2, D, N)]
+    ptr = [0 if v is None else v.data_ptr() for v in out]
+    lib.scan_bwd_selective(*c.inputs(), c.lengths.data_ptr(), states.data_ptr(), dyd.data_ptr(), 0, *ptr, 2, L, D, N, 1, c.ur.ld, c.dr.ld, c.br.ld, c.cr.ld, ldz,
+                           D, D, D, N, N, ldz, operand(lib, type), c.flags(), ws.data_ptr(), need, stream())
+    for got, want in zip(out, grads):
+        assert got is None or torch.equal(got, want.reshape(got.shape))
+    # one token of either sequence, the rows L tokens apart
+    tokens = []
+    for z in (D, ldz):
+        y, st = torch.empty(2, D, dtype=c.t, device="cuda"), torch.empty(2, D, N, device="cuda")
+        lib.scan_step_selective(*c.inputs(), c.sd.data_ptr(), y.data_ptr(), st.data_ptr(), 2, D, N, 1, L * D, L * D, L * N, L * N, z, D, operand(lib, type),
+                                c.flags(), stream())
+        tokens.append((y, st))
+    assert torch.equal(tokens[0][0], tokens[1][0]) and torch.equal(tokens[0][1], tokens[1][1])
