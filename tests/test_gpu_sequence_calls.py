@@ -1,8 +1,11 @@
-"""Calls of the operators along a sequence that their headers allow and that are easily missed: row distances of tensors that are not given."""
+"""Calls of the operators along a sequence that their headers allow and that are easily missed: row distances of tensors that are not given,
+parts with fewer rows than threads."""
 import pytest
 import torch
 
-from test_gpu_sequence import ScanCase, backward, draw, lib, operand, stream, workspace  # noqa: F401
+import sequence_reference as ref
+from sequence_reference import TYPES, check
+from test_gpu_sequence import Rows, ScanCase, backward, draw, lib, operand, stream, workspace  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -42,3 +45,27 @@ def test_the_row_distance_of_an_absent_gate_is_not_looked_at(lib, type, L, D, N,
                                 c.flags(), stream())
         tokens.append((y, st))
     assert torch.equal(tokens[0][0], tokens[1][0]) and torch.equal(tokens[0][1], tokens[1][1])
+
+
+@pytest.mark.parametrize("type, N, S, C, G", [("bf16", 1, 1, 2304, 1), ("fp32", 3, 2, 16, 2), ("fp16", 1, 17, 24, 3), ("bf16", 2, 33, 8, 1), ("fp32", 5, 3, 130, 1)])
+def test_streams_of_fewer_rows_than_a_block_takes(lib, type, N, S, C, G, monkeypatch):  # noqa: F811
+    """Threads without a row, in parts shorter than a block's stride, at the end of a tensor: values as by the formula, nothing outside written."""
+    monkeypatch.setenv("CONV2D_B200_NORM_STREAM", "1")
+    t = TYPES[type]
+    x, dy = draw(610, N, S, C, shift=0.4, dtype=t), draw(611, N, S, C, dtype=t)
+    one, zero = torch.ones(C, dtype=torch.float64), torch.zeros(C, dtype=torch.float64)
+    xr, gr, yr, dxr = Rows((N, S, C), t, 0, 0, x), Rows((N, S, C), t, 0, 0, dy), Rows((N, S, C), t), Rows((N, S, C), t)
+    mean, rstd, dg, db = Rows((N, G), torch.float32), Rows((N, G), torch.float32), Rows((C,), torch.float32), Rows((C,), torch.float32)
+    ws = workspace(max(lib.norm_fwd_groups_workspace_size(N, S, C, G), lib.norm_bwd_groups_workspace_size(N, S, C, G)))
+    lib.norm_fwd_groups(xr.ptr, 0, 0, yr.ptr, mean.ptr, rstd.ptr, N, S, C, G, C, C, 1e-5, operand(lib, type), lib.ACT_SILU, ws.data_ptr(), ws.numel(), stream())
+    lib.norm_bwd_groups(xr.ptr, 0, 0, mean.ptr, rstd.ptr, gr.ptr, dxr.ptr, dg.ptr, db.ptr, N, S, C, G, C, C, C, operand(lib, type), lib.ACT_SILU,
+                        ws.data_ptr(), ws.numel(), stream())
+    (y, size), *_ = ref.norm_fwd(x, one, zero, G, 1e-5, "silu")
+    dx, dgamma, dbeta = ref.norm_bwd(x, one, zero, G, 1e-5, "silu", dy)
+    # a thread adds at most S * C / 256 + 8 values in a row (a part has whole rows, and at most eight elements of each are one thread's unless a row is wider
+    # than the block); 40 for the trees over threads and parts and the operations of an element
+    chain = S * C // 256 + 48
+    check(yr.result(), y, size, chain, "y")
+    check(dxr.result(), *dx, 2 * chain, "dx")
+    check(dg.result(), *dgamma, 2 * chain + N * S, "dgamma")
+    check(db.result(), *dbeta, 2 * chain + N * S, "dbeta")
