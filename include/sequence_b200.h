@@ -36,7 +36,7 @@ typedef enum {
     CONV2D_ACT_NONE = 0,
     CONV2D_ACT_RELU = 1,
     CONV2D_ACT_SILU = 2,  /* v / (1 + e^-v) */
-    CONV2D_ACT_GELU = 3   /* v (1 + erf(v / sqrt 2)) / 2 */
+    CONV2D_ACT_GELU = 3   /* v (1 + erf(v / sqrt 2)) / 2, its digits kept where it is small */
 } conv2d_activation_t;
 
 /*

@@ -69,3 +69,38 @@ def test_streams_of_fewer_rows_than_a_block_takes(lib, type, N, S, C, G, monkeyp
     check(dxr.result(), *dx, 2 * chain, "dx")
     check(dg.result(), *dgamma, 2 * chain + N * S, "dgamma")
     check(db.result(), *dbeta, 2 * chain + N * S, "dbeta")
+
+
+@pytest.mark.parametrize("D", [4096, 4097])
+@pytest.mark.parametrize("type", ["fp32", "bf16", "fp16"])
+def test_gelu_keeps_its_digits_where_it_is_small(lib, type, D):  # noqa: F811
+    """v (1 + erf(v / sqrt 2)) / 2 for v down to -12, where 1 + erf cancels, and its slope: errors relative to the value.  One tap of one and a norm with
+    gamma = 0 give the activation exact arguments.
+    The bound is what a complementary error function good to 4 units of 2^-23 allows, in units of 2^-24 of the value: the argument v / sqrt 2 has two roundings,
+    which erfc magnifies by at most v^2 + 1 (its logarithmic slope is below 2 x^2 + 1), and there is one product: 2 (v^2 + 1) + 9 <= 12 (v^2 + 1).  The slope's
+    other term, v phi(v): an exponent v^2 / 2 with one rounding, a fast exponential of it, 2 + 1.173 v^2 / 2 units of 2^-23, and four products:
+    2.9 v^2 + 8 of that term.  However the library takes them, it is held to that."""
+    t, f = TYPES[type], torch.float64
+    v = torch.cat([torch.linspace(-12, -3, D // 2, dtype=f), torch.linspace(-3, 6, D - D // 2, dtype=f)]).to(t).to(f)
+    half_erfc, phi = 0.5 * torch.erfc(-v / 2 ** 0.5), torch.exp(-0.5 * v * v) / (2 * torch.pi) ** 0.5
+    y, slope = v * half_erfc, half_erfc + v * phi
+    y_size, slope_size = y.abs() * (1 + v * v), (half_erfc + (v * phi).abs()) * (1 + v * v)
+    x, w, one = v.to(t).cuda(), torch.ones(D, 1, dtype=t, device="cuda"), torch.ones(D, dtype=t, device="cuda")
+    out, dx = torch.empty_like(x), torch.empty_like(x)
+    args = operand(lib, type), lib.ACT_GELU
+    lib.conv1d_fwd_causal(x.data_ptr(), w.data_ptr(), 0, 0, 0, out.data_ptr(), 0, 1, 1, D, 1, D, D, *args, stream())
+    lib.conv1d_bwd_causal(x.data_ptr(), w.data_ptr(), 0, 0, 0, one.data_ptr(), 0, dx.data_ptr(), 0, 0, 0, 1, 1, D, 1, D, D, D, *args, 0, 0, stream())
+    check(out, y, y_size, 12, "convolution")
+    check(dx, slope, slope_size, 12, "gradient of the convolution")
+    for S in (1, 3):
+        ones = torch.ones(S, D, dtype=t, device="cuda")
+        gamma, beta, mean, rstd, dbeta = (torch.zeros(D, device="cuda"), v.float().cuda(), torch.empty(1, device="cuda"), torch.empty(1, device="cuda"),
+                                          torch.empty(D, device="cuda"))
+        xs, ys, dxs = draw(620, S, D, dtype=t).to(t).cuda(), torch.empty(S, D, dtype=t, device="cuda"), torch.empty(S, D, dtype=t, device="cuda")
+        ws = workspace(max(lib.norm_fwd_groups_workspace_size(1, S, D, 1), lib.norm_bwd_groups_workspace_size(1, S, D, 1)))
+        lib.norm_fwd_groups(xs.data_ptr(), gamma.data_ptr(), beta.data_ptr(), ys.data_ptr(), mean.data_ptr(), rstd.data_ptr(), 1, S, D, 1, D, D, 1e-5, *args,
+                            ws.data_ptr(), ws.numel(), stream())
+        lib.norm_bwd_groups(xs.data_ptr(), gamma.data_ptr(), beta.data_ptr(), mean.data_ptr(), rstd.data_ptr(), ones.data_ptr(), dxs.data_ptr(), 0, dbeta.data_ptr(),
+                            1, S, D, 1, D, D, D, *args, ws.data_ptr(), ws.numel(), stream())
+        check(ys, y.expand(S, D), y_size.expand(S, D), 12, "norm")
+        check(dbeta, S * slope, S * slope_size, 12 + S, "dbeta of the norm")
