@@ -140,7 +140,7 @@ struct BwdArgs {
     const int* lengths;
     T *dx, *dstate_in;
     float* partials;                    // [blockIdx.x][K+1][D]
-    int B, L, D, pieces, packs;
+    int B, L, D, pieces, packs;         // packs: of channels, from those that the pointers name on
     unsigned jobs;                      // pieces of all sequences
     long long ldx, lddy, lddx;
     int act;
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kThreads) conv1d_bwd_kernel(const BwdArgs<T> a
     __syncthreads();
     for (int i = tid; i < (K + 1) * width; i += kThreads) {
         const int k = i / width, ch = blockIdx.y * width + i % width;
-        if (ch >= a.D) continue;
+        if (ch >= a.packs * V) continue;
         float s = 0.f;
         for (int j = 0; j < (int)blockDim.y; ++j) s += sums[(size_t)j * (K + 1) * width + i];
         a.partials[((size_t)blockIdx.x * (K + 1) + k) * a.D + ch] = s;
@@ -366,13 +366,21 @@ conv2d_status_t bwd(const ConvSeq& s, cudaStream_t stream)
     const BwdPlan p = bwd_plan(s.B, s.L, s.D, V);
     a.pieces = p.pieces, a.packs = s.D / V, a.jobs = (unsigned)p.jobs;
     a.partials = s.dw || s.dbias ? s.partials : nullptr;
-    if (p.across > 65535 || p.jobs > 0x7fff0000LL) return CONV2D_ERR_SHAPE;
     const size_t rings = 2 * RowRing<T, V, kThreads, kBwdGroup, kBwdRing>::smem, sums = (size_t)kThreads * V * (K + 1) * sizeof(float), smem = rings > sums ? rings : sums;
     static SmemLimit limit;
     if (raise_smem_limit(reinterpret_cast<const void*>(conv1d_bwd_kernel<T, V, K>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-    if (launch_pdl(conv1d_bwd_kernel<T, V, K>, dim3((unsigned)p.parts, (unsigned)p.across), dim3(p.tx, p.ty), smem, stream, a) != cudaSuccess)
-        return CONV2D_ERR_CUDA;
-    count_launch();
+    // channels lie along the grid's y; more than 65535 blocks of them (2^21 channels, one a thread) take a launch for every so many
+    for (long long at = 0; at < p.across; at += 65535) {
+        BwdArgs<T> r = a;
+        const long long c = at * p.tx * V, across = p.across - at < 65535 ? p.across - at : 65535;
+        const auto shift = [c](auto& q) { if (q) q += c; };
+        shift(r.x), shift(r.bias), shift(r.state_in), shift(r.dy), shift(r.dstate_out), shift(r.dx), shift(r.dstate_in), shift(r.partials);
+        r.w += c * K;
+        r.packs = (int)((s.D - c) / V);
+        if (launch_pdl(conv1d_bwd_kernel<T, V, K>, dim3((unsigned)p.parts, (unsigned)across), dim3(p.tx, p.ty), smem, stream, r) != cudaSuccess)
+            return CONV2D_ERR_CUDA;
+        count_launch();
+    }
     if (!a.partials) return CONV2D_OK;
     return launch_column_sums(a.partials, p.parts, (long long)(K + 1) * s.D, (long long)(K + 1) * s.D, TapStore{s.dw, s.dbias, s.D, K}, stream);
 }

@@ -104,3 +104,22 @@ def test_gelu_keeps_its_digits_where_it_is_small(lib, type, D):  # noqa: F811
                             1, S, D, 1, D, D, D, *args, ws.data_ptr(), ws.numel(), stream())
         check(ys, y.expand(S, D), y_size.expand(S, D), 12, "norm")
         check(dbeta, S * slope, S * slope_size, 12 + S, "dbeta of the norm")
+
+
+@pytest.mark.parametrize("D", [2097121, (1 << 22) - 1])
+def test_gradients_of_as_many_channels_as_the_header_allows(lib, D):  # noqa: F811
+    """Channels one a thread, where rows are off every boundary, up to the header's 2^22: dx, dw and dbias of two rows and two taps."""
+    t, L, K = torch.bfloat16, 2, 2
+    x, w, dy = (torch.empty(n, dtype=t, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(i)) for i, n in enumerate((L * D, K * D, L * D)))
+    dx, dw, db = torch.empty_like(x), torch.empty(D, K, device="cuda"), torch.empty(D, device="cuda")
+    need = lib.conv1d_bwd_causal_workspace_size(1, L, D, K)
+    ws = workspace(need)
+    lib.conv1d_bwd_causal(x.data_ptr(), w.data_ptr(), 0, 0, 0, dy.data_ptr(), 0, dx.data_ptr(), dw.data_ptr(), db.data_ptr(), 0, 1, L, D, K, D, D, D,
+                          lib.OPERAND_BF16, lib.ACT_NONE, ws.data_ptr(), need, stream())
+    x, w, g = x.double().reshape(L, D), w.double().reshape(D, K), dy.double().reshape(L, D)
+    want = torch.stack([g[0] * w[:, 1] + g[1] * w[:, 0], g[1] * w[:, 1]])
+    size = torch.stack([(g[0] * w[:, 1]).abs() + (g[1] * w[:, 0]).abs(), (g[1] * w[:, 1]).abs()])
+    check(dx.reshape(L, D), want, size, 3, "dx")                                  # two products and a sum
+    check(dw[:, 1], (g * x).sum(0), (g * x).abs().sum(0), 8, "dw of the last tap")  # and the sums over a block's threads, of which two have rows
+    check(dw[:, 0], g[1] * x[0], (g[1] * x[0]).abs(), 8, "dw of the first tap")
+    check(db, g.sum(0), g.abs().sum(0), 8, "dbias")
