@@ -348,10 +348,21 @@ conv2d_status_t fwd(const ConvSeq& s, cudaStream_t stream)
     a.rows = 64;
     while (a.rows > 8 && (long long)a.packs * s.B * ceil_div_u(s.L, a.rows) < (long long)sm_count() * 1024) a.rows /= 2;
     a.pieces = (int)ceil_div_u(s.L, a.rows);
-    const long long threads = (long long)a.packs * a.pieces * s.B;
-    if (threads > 0x7fffff00LL) return CONV2D_ERR_SHAPE;
-    if (launch_pdl(conv1d_fwd_kernel<T, V, K>, dim3(ceil_div_u(threads, kThreads)), dim3(kThreads), RowRing<T, V, kThreads, kGroup, kRing>::smem, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
-    count_launch();
+    // (threads are counted in 32 bits)
+    const long long threads = (long long)a.packs * a.pieces;
+    const int most = sequences_of_launch(ceil_div_u(threads, kThreads), 0x7fffff00 / kThreads, s.B);
+    for (int b0 = 0; b0 < s.B; b0 += most) {
+        FwdArgs<T> r = a;
+        const size_t rows = (size_t)b0 * s.L, state = (size_t)b0 * (K - 1) * s.D;
+        r.x += rows * s.ldx, r.y += rows * s.ldy;
+        if (r.state_in) r.state_in += state;
+        if (r.state_out) r.state_out += state;
+        if (r.lengths) r.lengths += b0;
+        r.B = s.B - b0 < most ? s.B - b0 : most;
+        if (launch_pdl(conv1d_fwd_kernel<T, V, K>, dim3(ceil_div_u(threads * r.B, kThreads)), dim3(kThreads), RowRing<T, V, kThreads, kGroup, kRing>::smem, stream, r) != cudaSuccess)
+            return CONV2D_ERR_CUDA;
+        count_launch();
+    }
     return CONV2D_OK;
 }
 

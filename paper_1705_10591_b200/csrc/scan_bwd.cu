@@ -100,10 +100,11 @@ conv2d_status_t bwd(const ScanSeq& s, cudaStream_t stream)
     const BwdLayout o = bwd_layout(c, s.B, s.L, s.D, s.N, s.G);
     a.segs = c.segs, a.seg_rows = c.rows, a.blocks_group = c.blocks_group, a.sets = c.sets;
     a.local = s.ws + o.local, a.steps = s.ws + o.steps, a.per_channel = s.ws + o.per_channel, a.per_row = s.ws + o.per_row;
-    const long long jobs = (long long)s.B * a.segs * s.G, blocks = jobs * c.blocks_group, rows = (long long)s.B * s.L;
+    const long long jobs = (long long)s.B * a.segs * s.G, blocks = (long long)a.segs * s.G * c.blocks_group, rows = (long long)s.B * s.L;     // blocks: of a sequence
     const int carry_group = (int)ceil_div_u(a.E, Tile::CB);
     const long long join = (long long)s.B * s.D * round4(s.N), per_row = rows * s.G * 2 * Tile::NP;
-    if (jobs * carry_group > 0x7fffffffLL || per_row / 256 > 0x7ffffff0LL) return CONV2D_ERR_SHAPE;
+    // (segments are cut where there are few blocks; 2^39 elements of dB and dC are more than there is memory)
+    if ((a.segs > 1 && jobs * carry_group > 0x7fffffffLL) || per_row / 256 > 0x7ffffff0LL) return CONV2D_ERR_SHAPE;
     if (a.segs > 1) {
         if (launch_pdl(scan_bwd_carry_kernel<T, NL, V>, dim3((unsigned)(jobs * carry_group)), dim3(Tile::SCAN), 0, stream, a, carry_group) != cudaSuccess)
             return CONV2D_ERR_CUDA;
@@ -118,9 +119,24 @@ conv2d_status_t bwd(const ScanSeq& s, cudaStream_t stream)
     static_assert(Tile::fixed(e) + (Tile::CB >= 32 ? 1 : 4) * Tile::set_bytes <= 227 * 1024, "the sets that bwd_cut allows");
     const size_t smem = Tile::fixed(e) + a.sets * Tile::set_bytes;
     static SmemLimit limit;
-    if (raise_smem_limit(reinterpret_cast<const void*>(scan_bwd_kernel<T, NL>), smem, limit) != cudaSuccess
-        || launch_pdl(scan_bwd_kernel<T, NL>, dim3((unsigned)blocks), dim3(Tile::TH), smem, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
-    count_launch();
+    if (raise_smem_limit(reinterpret_cast<const void*>(scan_bwd_kernel<T, NL>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+    const int most = sequences_of_launch(blocks, 0x7fffffffLL, s.B);
+    for (int b0 = 0; b0 < s.B; b0 += most) {
+        ScanBwdArgs<T> r = a;           // (B stays: the partial sums of dB and dC are laid out by it)
+        const size_t first = (size_t)b0 * s.L, state = (size_t)b0 * s.D * s.N, seg = (size_t)b0 * a.segs, NQ = round4(s.N);
+        r.u += first * a.ldu, r.delta += first * a.lddelta, r.Bm += first * a.ldB, r.Cm += first * a.ldC, r.dy += first * a.lddy;
+        r.du += first * a.lddu, r.ddelta += first * a.ldddelta;
+        if (r.z) r.z += first * a.ldz, r.dz += first * a.lddz;
+        if (r.dstate_out) r.dstate_out += state;
+        if (r.dstate_in) r.dstate_in += state;
+        if (r.lengths) r.lengths += b0;
+        r.states += (size_t)b0 * ceil_div_u(s.L, kCheckpointRows) * s.D * NQ;
+        if (a.segs > 1) r.local += seg * s.D * NQ, r.steps += seg * s.D;
+        r.per_channel += seg * channel_floats(s.D, (int)NQ), r.per_row += first * 2 * Tile::NP;
+        const int count = s.B - b0 < most ? s.B - b0 : most;
+        if (launch_pdl(scan_bwd_kernel<T, NL>, dim3((unsigned)(blocks * count)), dim3(Tile::TH), smem, stream, r) != cudaSuccess) return CONV2D_ERR_CUDA;
+        count_launch();
+    }
     const conv2d_status_t st = launch_column_sums(a.per_channel, (long long)s.B * a.segs, (long long)s.D * (round4(s.N) + 2), channel_floats(s.D, round4(s.N)),
                                                   ChannelStore{s.dA, s.dD, s.ddelta_bias, s.D, s.N, round4(s.N)}, stream);
     if (st != CONV2D_OK) return st;

@@ -31,13 +31,25 @@ conv2d_status_t walk(ScanFwdArgs<T> a, cudaStream_t stream)
     constexpr size_t smem = Tile::smem(sizeof(T));
     static_assert(smem <= 227 * 1024, "shared memory of a block");
     a.blocks_group = (int)ceil_div_u(a.E, Tile::CB);
-    const long long blocks = (long long)a.B * a.segs * a.G * a.blocks_group;
-    if (blocks > 0x7fffffffLL) return CONV2D_ERR_SHAPE;
+    const long long blocks = (long long)a.segs * a.G * a.blocks_group;      // of a sequence
+    const int most = sequences_of_launch(blocks, 0x7fffffffLL, a.B);
     static SmemLimit limit;
-    if (raise_smem_limit(reinterpret_cast<const void*>(scan_fwd_kernel<T, NL, SPT, STATE_ONLY>), smem, limit) != cudaSuccess
-        || launch_pdl(scan_fwd_kernel<T, NL, SPT, STATE_ONLY>, dim3((unsigned)blocks), dim3(Tile::TH), smem, stream, a) != cudaSuccess)
-        return CONV2D_ERR_CUDA;
-    count_launch();
+    if (raise_smem_limit(reinterpret_cast<const void*>(scan_fwd_kernel<T, NL, SPT, STATE_ONLY>), smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+    for (int b0 = 0; b0 < a.B; b0 += most) {
+        ScanFwdArgs<T> r = a;
+        const size_t rows = (size_t)b0 * a.L, state = (size_t)b0 * a.D * a.N, NQ = round4(a.N);
+        r.u += rows * a.ldu, r.delta += rows * a.lddelta, r.Bm += rows * a.ldB, r.Cm += rows * a.ldC, r.y += rows * a.ldy;
+        if (r.z) r.z += rows * a.ldz;
+        if (r.state_in) r.state_in += state;
+        if (r.state_out) r.state_out += state;
+        if (r.lengths) r.lengths += b0;
+        if (r.states) r.states += (size_t)b0 * ceil_div_u(a.L, kCheckpointRows) * a.D * NQ;
+        if (a.segs > 1) r.local += (size_t)b0 * a.segs * a.D * NQ, r.steps += (size_t)b0 * a.segs * a.D;
+        r.B = a.B - b0 < most ? a.B - b0 : most;
+        if (launch_pdl(scan_fwd_kernel<T, NL, SPT, STATE_ONLY>, dim3((unsigned)(blocks * r.B)), dim3(Tile::TH), smem, stream, r) != cudaSuccess)
+            return CONV2D_ERR_CUDA;
+        count_launch();
+    }
     return CONV2D_OK;
 }
 

@@ -264,6 +264,13 @@ inline bool rows_aligned(const void* p, long long ld, int esize, int bytes)
 
 inline unsigned ceil_div_u(long long a, long long b) { return (unsigned)((a + b - 1) / b); }
 
+// Sequences of one launch whose grid has `blocks` blocks for each: a grid holds at most `most` blocks.
+inline int sequences_of_launch(long long blocks, long long most, int B)
+{
+    const long long forced = env_int("CONV2D_B200_SEQ_GRID", 0), n = (forced > 0 ? forced : most) / blocks;
+    return n < 1 ? 1 : n < B ? (int)n : B;
+}
+
 // Column sums of partial sums [parts][cols], `ld` floats apart, added in a fixed order: 32 columns by 8 shares of the parts a block;
 // `store` takes them.
 template <typename Store>

@@ -5,7 +5,7 @@ import torch
 
 import sequence_reference as ref
 from sequence_reference import TYPES, check
-from test_gpu_sequence import Rows, ScanCase, backward, draw, lib, operand, stream, workspace  # noqa: F401
+from test_gpu_sequence import SENTINEL, Rows, ScanCase, backward, cuda, draw, lib, mask_rows, operand, stream, workspace  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -123,3 +123,47 @@ def test_gradients_of_as_many_channels_as_the_header_allows(lib, D):  # noqa: F8
     check(dw[:, 1], (g * x).sum(0), (g * x).abs().sum(0), 8, "dw of the last tap")  # and the sums over a block's threads, of which two have rows
     check(dw[:, 0], g[1] * x[0], (g[1] * x[0]).abs(), 8, "dw of the first tap")
     check(db, g.sum(0), g.abs().sum(0), 8, "dbias")
+
+
+def test_more_threads_than_32_bits_count(lib):  # noqa: F811
+    """2^20 sequences of 2049 channels, one a thread: a token of each is 2.1e9 threads."""
+    t, B, D = torch.bfloat16, 1 << 20, 2049
+    if torch.cuda.mem_get_info()[0] < 3 * 2 * B * D:
+        pytest.skip("not enough free memory")
+    x = torch.empty(B, D, dtype=t, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    y, w = torch.empty_like(x), torch.full((D, 1), 0.5, dtype=t, device="cuda")
+    y.fill_(SENTINEL)
+    lib.conv1d_step_causal(x.data_ptr(), w.data_ptr(), 0, 0, y.data_ptr(), 0, B, D, 1, D, D, lib.OPERAND_BF16, lib.ACT_NONE, stream())
+    assert all(torch.equal(a, b * 0.5) for a, b in zip(y.split(1 << 16), x.split(1 << 16)))     # (halves are exact)
+
+
+@pytest.mark.parametrize("segs", ["1", "3"])
+@pytest.mark.parametrize("sequences", [1, 2])
+def test_sequences_of_several_launches(lib, monkeypatch, segs, sequences):  # noqa: F811
+    """Calls whose grids take several launches, as more blocks than a grid holds do, have the bits of one launch."""
+    case = ("bf16", 5, 100, 48, 16, 2, True, True, True, True, [100, 3, 0, 77, 41], 8, 8)
+    for name in ("SEGS", "BWD_SEGS", "SETS"):
+        monkeypatch.setenv("CONV2D_B200_SCAN_" + name, segs if name != "SETS" else "1")
+    c = ScanCase(lib, case)
+    B, L, D, N, G = c.B, c.L, c.D, c.N, c.G
+    dy, dlast = mask_rows(draw(630, B, L, D, dtype=c.t), c.n, 0.0), draw(631, B, D, N)
+    w, bias, ends_in = cuda(draw(632, D, 4, dtype=c.t), c.t), cuda(draw(633, D, dtype=c.t), c.t), cuda(draw(634, B, 3, D, dtype=c.t), c.t)
+
+    def everything():
+        states, last = workspace(lib.scan_states_size(B, L, D, N)), torch.empty(B, D, N, device="cuda")
+        y = c.forward(state_out=last, states=states).result()
+        kept = states.clone()
+        conv, ends = Rows((B, L, D), c.t, 8, 8), ends_in.clone()
+        lib.conv1d_fwd_causal(c.ur.ptr, w.data_ptr(), bias.data_ptr(), ends.data_ptr(), c.lengths.data_ptr(), conv.ptr, ends.data_ptr(), B, L, D, 4, c.ur.ld, conv.ld,
+                              operand(lib, c.type), lib.ACT_SILU, stream())
+        return [y, last, kept, conv.result(), ends] + backward(c, states, dy, dlast)
+
+    before = lib.conv2d_launch_count()
+    want = everything()
+    once = lib.conv2d_launch_count() - before
+    # as many blocks as `sequences` have in the scan, where a group of 24 channels is one; a sequence of the convolution has two
+    monkeypatch.setenv("CONV2D_B200_SEQ_GRID", str(sequences * int(segs) * G))
+    got = everything()
+    assert lib.conv2d_launch_count() - before > 2 * once
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
