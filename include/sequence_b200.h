@@ -105,6 +105,8 @@ conv2d_status_t scan_step_selective(const void* u, const void* delta, const floa
  * Backward: from dy [B*L][D] and, optional, dstate_out [B][D][N] (the gradient of state_out) the gradients of every input, du, ddelta,
  * dz (required exactly where z is given) [B*L][D], dB, dC [B*L][G*N] of `type`, and in fp32 dA [D][N], dDskip [D] (optional),
  * ddelta_bias [D] (optional), dstate_in [B][D][N] (optional).  `states` as the forward pass of the same inputs left it.
+ * The workspace grows with the tensors: 4 bytes for every element of u with up to 16 states, 16 with 64, 64 with 128 (more where channels are few), so
+ * that training with many states wants it larger than all tensors together; `states` takes N / 4 bytes for every element.  A batch can be taken in pieces.
  */
 conv2d_status_t scan_bwd_selective_workspace_size(int B, int L, int D, int N, int G, size_t* bytes);
 conv2d_status_t scan_bwd_selective(const void* u, const void* delta, const float* A, const void* Bm, const void* Cm,

@@ -49,8 +49,8 @@ BwdCut bwd_cut(int B, int L, int D, int N, int G)
     c.nl = lanes_for(N, kSpt);
     c.cb = c.nl == 1 ? 64 : 128 / c.nl;
     const int E = D / G;
-    // a block's partial sums of dB and dC are for 32 channels, or the workspace would be larger than the tensors (16 channels with more than 64
-    // states: more sets do not fit into shared memory)
+    // A block's partial sums of dB and dC are for 32 channels (64 with up to eight states, 16 with more than 64: more sets do not fit into shared memory), to
+    // keep the workspace down: they take 2 NP / 32 floats for each row and channel, 4 bytes with 16 states, 16 with 64 and 64 with 128.
     int sets = c.cb >= 32 ? 1 : 32 / c.cb;
     if (sets > 4) sets = 4;
     // fewer where half the machine would have no block, cut into segments as below (1 x 246 x 128 in two groups, 64 states, with the forward pass: 100 us with four sets, 61 with one)

@@ -77,6 +77,19 @@ SCAN = [  # type, B, L, D, N, G, lengths
     ("fp32", 1, 90, 4, 100, 1, [89]),
     ("fp32", 2, 70, 10, 20, 2, None),
     ("fp16", 4, 300, 70, 32, 1, None),
+    ("bf16", 2, 2000, 64, 64, 1, [2000, 1500]),          # four channel sets a block and segments, as the sizes decide
+    ("fp32", 20, 40, 128, 64, 1, None),                  # four channel sets a block, whole
+    ("fp32", 20, 40, 100, 128, 1, None),
+]
+SETS = [  # with four channel sets a block asked for: 32 channels (16 with more than 64 states) a block, the last one with 1, 2 or 3 sets, one partly filled
+    ("fp32", 2, 70, 37, 64, 1, [70, 33]),
+    ("bf16", 1, 100, 2 * 43, 40, 2, None),
+    ("fp32", 2, 50, 49, 64, 1, None),
+    ("fp32", 3, 40, 64, 33, 1, [40, 0, 17]),
+    ("fp32", 1, 64, 3 * 18, 100, 3, None),
+    ("fp16", 2, 37, 23, 128, 1, [36, 37]),
+    ("fp32", 1, 33, 27, 65, 1, None),
+    ("bf16", 2, 50, 100, 20, 1, [50, 49]),
 ]
 
 

@@ -1,4 +1,4 @@
-"""The operators along a sequence against 64-bit forms by whole tensors: sums over thousands of rows."""
+"""The operators along a sequence against 64-bit forms by whole tensors: sums over thousands of rows, and every number of channel sets of a block."""
 import pytest
 import torch
 
@@ -58,6 +58,26 @@ def scan(lib, c):  # noqa: F811
 def test_scan(lib, case):  # noqa: F811
     c = sums.Scan(case)
     compare(c, scan(lib, c))
+
+
+@pytest.mark.parametrize("segs", ["1", "2"])
+@pytest.mark.parametrize("case", sums.SETS, ids=name)
+def test_scan_of_four_sets_a_block(lib, monkeypatch, case, segs):  # noqa: F811
+    """32 channels a block, or 16 with more than 64 states, of which the last block has 1, 2 or 3 sets and one of them partly filled."""
+    monkeypatch.setenv("CONV2D_B200_SCAN_BWD_SEGS", segs)
+    monkeypatch.setenv("CONV2D_B200_SCAN_SETS", "4")
+    c = sums.Scan(case)
+    compare(c, scan(lib, c))
+
+
+@pytest.mark.parametrize("B, L, D, N", [(2, 2000, 64, 64), (20, 40, 128, 64), (20, 40, 100, 128), (4, 2048, 2048, 64)])
+def test_sizes_that_take_four_sets_by_themselves(lib, monkeypatch, B, L, D, N):  # noqa: F811
+    """The workspace holds a partial sum of dB and dC for every block: as many as with four sets, fewer than with two."""
+    sizes = [lib.scan_bwd_selective_workspace_size(B, L, D, N)]
+    for n in "42":
+        monkeypatch.setenv("CONV2D_B200_SCAN_SETS", n)
+        sizes.append(lib.scan_bwd_selective_workspace_size(B, L, D, N))
+    assert sizes[0] == sizes[1] < sizes[2]
 
 
 @pytest.mark.parametrize("variant", ["0", "1", "-1"])

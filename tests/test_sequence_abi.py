@@ -129,3 +129,11 @@ def test_workspace_sizes_do_not_wrap(lib):
     assert lib.scan_bwd_selective_workspace_size(1, 1 << 30, 1 << 22, 128, 1 << 22) > 1 << 62
     assert lib.scan_states_size(1, 1 << 30, 1 << 22, 128) == (1 << 26) * (1 << 22) * 128 * 4
     assert lib.norm_bwd_groups_workspace_size(1 << 20, 4, 4096, 32) >= (1 << 20) * 2 * 4096 * 4
+
+
+def test_the_backward_scan_wants_what_its_header_says(lib):
+    """Bytes of workspace and of kept states for each row and channel, of many channels: 4 with 16 states, 16 with 64, 64 with 128, and N / 4."""
+    for B, L, D in ((4, 2048, 2048), (8, 1000, 4096)):
+        for N, per in ((4, 4), (16, 4), (64, 16), (128, 64)):
+            assert lib.scan_bwd_selective_workspace_size(B, L, D, N, 1) <= 1.03 * per * B * L * D
+            assert N / 4 <= lib.scan_states_size(B, L, D, N) / (B * L * D) <= 1.01 * N / 4

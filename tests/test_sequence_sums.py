@@ -8,7 +8,7 @@ def name(c):
     return f"{c[0]}-{'x'.join(map(str, c[1:6]))}"
 
 
-CASES = [(sums.Conv, c) for c in sums.CONV] + [(sums.Scan, c) for c in sums.SCAN] + [(sums.Norm, c) for c in sums.NORM]
+CASES = [(sums.Conv, c) for c in sums.CONV] + [(sums.Scan, c) for c in sums.SCAN + sums.SETS] + [(sums.Norm, c) for c in sums.NORM]
 
 
 @pytest.mark.parametrize("kind, case", CASES, ids=lambda v: v.__name__ if isinstance(v, type) else name(v))
