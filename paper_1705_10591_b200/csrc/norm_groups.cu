@@ -373,7 +373,7 @@ struct Part {
         }
         count = pack >= 0 && first < r1 ? (r1 - first + step - 1) / step : 0;
         if (BACKWARDS && count) first += (count - 1) * step;
-        first = min(first, a.S - 1);    // (a thread without rows, too, names addresses within the tensor: its copies of no bytes have one)
+        if (V * sizeof(T) >= 4) first = min(first, a.S - 1);    // (a thread without rows, too, names addresses within the tensor: its copies of no bytes have one)
     }
     // rows from one of the thread's to its next
     __device__ long long stride() const { return BACKWARDS ? -step : step; }
