@@ -6,8 +6,9 @@
 // 16 bytes where the rows allow it) and walks down a piece of the sequence with the last K rows in registers, so that every element is loaded once
 // but for the K-1 rows before the piece.  The rows come in by asynchronous copies into a ring of shared memory that belongs to the thread, three
 // groups of four rows ahead; loads into registers were too few at a time (4 x 4096 x 4096 in bf16: 88 us, backward 638).  Products and
-// activations are packed, two channels an instruction.  52 us so (5.2 TB/s; the floor is 41), backward 118 (3.4 TB/s; the floor is 61: the taps' gradients
-// double the products, and issue slots and memory share the time).
+// activations are packed, two channels an instruction.  52 us so (5.2 TB/s; the floor is 41), backward 112 (3.6 TB/s; the floor is 61): 150 registers
+// leave three blocks of four warps an SM, which issue in 62 % of the cycles while memory and the FMA pipe are half busy, and every piece of 64 rows waits for its
+// taps, its window and its first rows in turn.
 #include "seq_common.cuh"
 
 namespace conv2d_b200 {

@@ -7,15 +7,18 @@
 //
 // Memory decides: the floor is one reading of the inputs and one writing of the output.  Statistics come before the output, so the
 // elements have to stay on chip in between:
-//   rows     S = 1: the elements of a group lie together and stay in the registers of 1 to 32 lanes.
+//   rows     S = 1 and at most four packs of 16 bytes a lane (groups of 1024 16-bit elements, 512 fp32, fewer where they are not aligned): the elements of a
+//            group lie together and stay in the registers of 1 to 32 lanes.
 //   slab     a thread-block cluster takes the rows of a few groups of one sample, every block a part of the rows, which stay in its shared
 //            memory; the blocks exchange their statistics through distributed shared memory.
-//   stream   slabs that do not fit, or too few of them to fill the machine: one kernel for the statistics of parts, one that reads
+//   stream   slabs that do not fit, and tensors above a size (make_norm_plan): one kernel for the statistics of parts, one that reads
 //            the elements again (from L2 where they are still there).
-// Measured: rows 28.9 us for 8192 x 4096 in bf16 (4.7 TB/s; the floor is 20.8, what is left is the two sums over lanes in a row and the few samples
-// that a thread has under way).  Stream, forward, 8 x 4096 x 512 in fp16 27 us (statistics 10.6 at 3.2 TB/s, output 19.3 under a profiler: issue
-// slots, about 40 instructions a pack of eight elements with its activation, and half-filled second turns of blocks); training step of 32 x 3136 x 256 in
-// bf16 92.4 us: 12.4 + 23.9 forward, 29.7 + 30.5 backward, 3.3 for the parameters' gradients.
+// Measured: rows 26.8 us for 8192 x 4096 in bf16 (5 TB/s; the floor is 20.5, what is left is the two sums over lanes in a row and the few samples
+// that a thread has under way), with the backward pass 92.  Stream, forward, 8 x 4096 x 512 in fp16 28 us; training step of 32 x 3136 x 256 in bf16 91.3 us:
+// 14 + 26 forward, 32 + 32 backward, 5.6 for the parameters' gradients (each alone, under a profiler).  The output kernel of the forward pass keeps the special-function
+// units busy for 64 % of its time, with 78 registers and so three blocks an SM, whose warps wait for them in turn; the others wait for latencies, at 40 to 48 % of memory's rate.
+// Where the plan falls short: it goes by bytes alone.  Wide groups of single rows are streams or slabs of one row (8192 x 4096 in one group, bf16: 133 us
+// forward, 704 with the backward pass, whose partial sums are one a sample), and a block takes one sample however short (16384 x 4 x 512: 1.2 and 3.7 ms).
 // Statistics of a part are taken around one of its own values and joined by counts and means, so that a mean far
 // from zero costs no digits.
 #include <cooperative_groups.h>
@@ -31,7 +34,7 @@ constexpr int kRowThreads = 256;        // rows
 constexpr int kThreads = 256, kWarps = kThreads / 32;        // slab, stream
 constexpr int kRing = 4;                // groups of a ring
 // Rows of a group: two (four take the backward pass to 240 registers); eight of single elements, whose loads, where they are too narrow to be copied
-// asynchronously, wait for memory once a group (1 x 5795 x 4064 in groups of 127, bf16: 138 us with two).
+// asynchronously, wait for memory once a group (1 x 5795 x 4064 in groups of 127 channels, bf16, forward: 151 us with two, 79 so).
 template <int V> constexpr int kGroup = V == 1 ? 8 : 2;
 
 template <typename T>

@@ -10,7 +10,7 @@
 // Sums over the channels (dB, dC) are the larger part, eight values a row: two lanes join theirs, one going on with dB and one with dC (going
 // on over all lanes took 32 of 95 instructions a row), and the rest is added through shared memory, over the warps and the channel sets that the block
 // takes in turn, and goes into the workspace as one partial sum of the block; those are added by a kernel of their own in a fixed order.
-// 4 x 2048 x 2048 of 16 states: about 435 us of the training step's 574.  The exponentials, twice, take 120 of them; shared memory is busy for two thirds of the
+// 4 x 2048 x 2048 of 16 states: about 433 us of the training step's 573.  The exponentials, twice, take 120 of them; shared memory is busy for two thirds of the
 // time on the SMs that have two blocks (256 blocks are not a multiple of 148), eight of its 20 cycles a row and warp for the sums over channels.
 // As in the forward pass four helping warps do what is done once per row and channel while the four scanning warps scan: copies, step sizes and
 // gates of the next tile, outputs and sums over the warps of the last one.

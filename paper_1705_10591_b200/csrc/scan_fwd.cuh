@@ -3,7 +3,7 @@
 //   h_t = exp(s_t A) h_{t-1} + s_t u_t B_t,   v_t = C_t . h_t + Dskip u_t,   y_t = v_t silu(z_t)
 //
 // Every (row, channel, state) takes an exponential of its own, so the special-function units (16 a clock and SM) set the pace, not memory:
-// 16384 x 4096 channels of 16 states take 239 us of them on all SMs, 276 on the 128 that such a call has blocks for, and 615 in all;
+// 16384 x 4096 channels of 16 states take 239 us of them on all SMs, 276 on the 128 that such a call has blocks for, and 605 in all;
 // without the helpers' work beside it the scan alone takes 495, so the rest is what two warps of a scheduler take from each other.
 // A block takes the channels of its W scanning warps and walks the rows of a sequence in tiles of TT; four more warps do what is done once
 // per row and channel, so that the scanning warps, of which a batch of a few thousand channels gives one or two to a scheduler, only scan: while

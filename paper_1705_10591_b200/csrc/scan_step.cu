@@ -9,7 +9,8 @@ constexpr int kSpt = 4;                 // states of a thread
 // One token: every state is read and written once, which is all the time there is.  A thread takes four adjacent states of one
 // channel, of one sequence, or of four at once where there are many (their loads are under way together, A is loaded once for all, and each
 // of the lanes of a channel does for one of the sequences what is done once for a channel: step size, gate, output).  256 x 4096 of 16 states in place:
-// 37.5 us, 3.8 TB/s (reads and writes of the same rows in turn; without the look-ahead 47); 8 sequences are bound by the host's part of a call.
+// 37.5 us, 3.8 TB/s (without the look-ahead 47; memory is not full: step sizes, inputs, B and C are not fetched ahead, so every four sequences a warp waits for them
+// once, eight of some 13 cycles between two instructions of a warp); 8 sequences are bound by the host's part of a call.
 template <typename T>
 struct StepArgs {
     const T *u, *delta, *Bm, *Cm, *z;
