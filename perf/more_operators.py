@@ -202,9 +202,8 @@ def _own(s):
                         B, L, Hk, H, K, V, Hk * K, Hk * K, H * V, H, H, H * V, scale, type, ws, n, stream)
     if not train:
         return s["o"], s["state_out"]
-    lib.delta_bwd_gated(_p(s["q"]), _p(s["k"]), _p(s["v"]), _p(s["g"]), _p(s["beta"]), _p(s["lengths"]), kept, _p(s["do"]), 0,
-                        _p(s["dq"]), _p(s["dk"]), _p(s["dv"]), _p(s["dg"]), _p(s["dbeta"]), 0, B, L, Hk, H, K, V,
-                        Hk * K, Hk * K, H * V, H, H, H * V, Hk * K, Hk * K, H * V, H, H, scale, type, ws, n, stream)
+    lib.delta_bwd_gated(_p(s["q"]), _p(s["k"]), _p(s["lengths"]), kept, _p(s["do"]), 0, _p(s["dq"]), _p(s["dk"]), _p(s["dv"]), _p(s["dg"]),
+                        _p(s["dbeta"]), 0, B, L, Hk, H, K, V, Hk * K, Hk * K, H * V, Hk * K, Hk * K, H * V, H, H, scale, type, ws, n, stream)
     return (s["o"],) + tuple(s["d" + name] for name in ("q", "k", "v", "g", "beta"))
 
 
