@@ -87,6 +87,15 @@ def load_library() -> ctypes.CDLL:
         "norm_fwd_groups": [vp] * 6 + [i] * 4 + [ll] * 2 + [f, i, i, vp, sz, vp],
         "norm_bwd_groups_workspace_size": [i] * 4 + [ctypes.POINTER(sz)],
         "norm_bwd_groups": [vp] * 9 + [i] * 4 + [ll] * 3 + [i, i, vp, sz, vp],
+        "delta_states_size": [i] * 7 + [ctypes.POINTER(sz)],
+        "delta_fwd_gated_workspace_size": [i] * 7 + [ctypes.POINTER(sz)],
+        "delta_fwd_gated": [vp] * 10 + [i] * 6 + [ll] * 6 + [f, i, vp, sz, vp],
+        "delta_step_gated": [vp] * 8 + [i] * 5 + [ll] * 6 + [f, i, vp],
+        "delta_bwd_gated_workspace_size": [i] * 7 + [ctypes.POINTER(sz)],
+        "delta_bwd_gated": [vp] * 12 + [i] * 6 + [ll] * 8 + [f, i, vp, sz, vp],
+        "norm_fwd_rms": [vp] * 9 + [i] * 4 + [ll] * 6 + [f, i, vp],
+        "norm_bwd_rms_workspace_size": [i] * 3 + [ctypes.POINTER(sz)],
+        "norm_bwd_rms": [vp] * 9 + [i] * 3 + [ll] * 6 + [i, vp, sz, vp],
     }.items():
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = i
@@ -316,3 +325,69 @@ def norm_bwd_groups(x_ptr, gamma_ptr, beta_ptr, mean_ptr, rstd_ptr, dy_ptr, dx_p
                                           dy_ptr or None, dx_ptr or None, dgamma_ptr or None, dbeta_ptr or None, N, S, C, G,
                                           ldx, lddy, lddx, operand, act, workspace_ptr or None, workspace_bytes, stream or None),
            "norm_bwd_groups")
+
+
+# ---- gated delta rule and RMS norm (recurrent_b200.h).  Pointers that are optional there may be 0.
+
+def delta_states_size(B, L, Hk, H, K, V, operand=OPERAND_BF16) -> int:
+    """Bytes of the states that delta_fwd_gated leaves for delta_bwd_gated."""
+    return _size("delta_states_size", B, L, Hk, H, K, V, operand)
+
+
+def delta_fwd_gated_workspace_size(B, L, Hk, H, K, V, operand=OPERAND_BF16) -> int:
+    return _size("delta_fwd_gated_workspace_size", B, L, Hk, H, K, V, operand)
+
+
+def delta_fwd_gated(q_ptr, k_ptr, v_ptr, g_ptr, beta_ptr, state_in_ptr, lengths_ptr, o_ptr, state_out_ptr, states_ptr, B, L, Hk, H, K, V,
+                    ldq, ldk, ldv, ldg, ldbeta, ldo, scale, operand=OPERAND_BF16, workspace_ptr=0, workspace_bytes=0, stream=0) -> None:
+    """Gated delta rule over sequences; q, k [B*L, Hk*K], v, o [B*L, H*V]; g, beta [B*L, H] and the states [B, H, K, V] are fp32."""
+    _check(load_library().delta_fwd_gated(q_ptr or None, k_ptr or None, v_ptr or None, g_ptr or None, beta_ptr or None, state_in_ptr or None,
+                                          lengths_ptr or None, o_ptr or None, state_out_ptr or None, states_ptr or None, B, L, Hk, H, K, V,
+                                          ldq, ldk, ldv, ldg, ldbeta, ldo, scale, operand, workspace_ptr or None, workspace_bytes, stream or None),
+           "delta_fwd_gated")
+
+
+def delta_step_gated(q_ptr, k_ptr, v_ptr, g_ptr, beta_ptr, state_in_ptr, o_ptr, state_out_ptr, B, Hk, H, K, V, ldq, ldk, ldv, ldg, ldbeta, ldo,
+                     scale, operand=OPERAND_BF16, stream=0) -> None:
+    """One token of every sequence; the two states [B, H, K, V] may be one buffer."""
+    _check(load_library().delta_step_gated(q_ptr or None, k_ptr or None, v_ptr or None, g_ptr or None, beta_ptr or None, state_in_ptr or None,
+                                           o_ptr or None, state_out_ptr or None, B, Hk, H, K, V, ldq, ldk, ldv, ldg, ldbeta, ldo, scale, operand,
+                                           stream or None),
+           "delta_step_gated")
+
+
+def delta_bwd_gated_workspace_size(B, L, Hk, H, K, V, operand=OPERAND_BF16) -> int:
+    return _size("delta_bwd_gated_workspace_size", B, L, Hk, H, K, V, operand)
+
+
+def delta_bwd_gated(q_ptr, k_ptr, lengths_ptr, states_ptr, dout_ptr, dstate_out_ptr, dq_ptr, dk_ptr, dv_ptr, dg_ptr, dbeta_ptr, dstate_in_ptr,
+                    B, L, Hk, H, K, V, ldq, ldk, lddo, lddq, lddk, lddv, lddg, lddbeta, scale, operand=OPERAND_BF16,
+                    workspace_ptr=0, workspace_bytes=0, stream=0) -> None:
+    """states: as delta_fwd_gated of the same inputs left them; dg, dbeta and dstate_in are fp32."""
+    _check(load_library().delta_bwd_gated(q_ptr or None, k_ptr or None, lengths_ptr or None, states_ptr or None, dout_ptr or None,
+                                          dstate_out_ptr or None, dq_ptr or None, dk_ptr or None, dv_ptr or None, dg_ptr or None,
+                                          dbeta_ptr or None, dstate_in_ptr or None, B, L, Hk, H, K, V, ldq, ldk, lddo, lddq, lddk, lddv, lddg, lddbeta,
+                                          scale, operand, workspace_ptr or None, workspace_bytes, stream or None),
+           "delta_bwd_gated")
+
+
+def norm_fwd_rms(x_ptr, residual_ptr, z_ptr, gamma_ptr, y_ptr, h_ptr, y8_ptr, scales_ptr, rstd_ptr, M, C, G, block, ldx, ldr, ldz, ldy, ldh, ld8,
+                 eps, operand=OPERAND_BF16, stream=0) -> None:
+    """RMS norm of [M, C] in G groups, with the residual's addition, a gate and an output in 8 bits; gamma [C / G], scales and rstd are fp32."""
+    _check(load_library().norm_fwd_rms(x_ptr or None, residual_ptr or None, z_ptr or None, gamma_ptr or None, y_ptr or None, h_ptr or None,
+                                       y8_ptr or None, scales_ptr or None, rstd_ptr or None, M, C, G, block, ldx, ldr, ldz, ldy, ldh, ld8, eps,
+                                       operand, stream or None),
+           "norm_fwd_rms")
+
+
+def norm_bwd_rms_workspace_size(M, C, G=1) -> int:
+    return _size("norm_bwd_rms_workspace_size", M, C, G)
+
+
+def norm_bwd_rms(h_ptr, z_ptr, gamma_ptr, rstd_ptr, dy_ptr, dh_ptr, dx_ptr, dz_ptr, dgamma_ptr, M, C, G, ldh, ldz, lddy, lddh, lddx, lddz,
+                 operand=OPERAND_BF16, workspace_ptr=0, workspace_bytes=0, stream=0) -> None:
+    """h, rstd as norm_fwd_rms left them; dgamma [C / G] is fp32."""
+    _check(load_library().norm_bwd_rms(h_ptr or None, z_ptr or None, gamma_ptr or None, rstd_ptr or None, dy_ptr or None, dh_ptr or None,
+                                       dx_ptr or None, dz_ptr or None, dgamma_ptr or None, M, C, G, ldh, ldz, lddy, lddh, lddx, lddz, operand,
+                                       workspace_ptr or None, workspace_bytes, stream or None),
+           "norm_bwd_rms")
