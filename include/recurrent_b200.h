@@ -23,8 +23,7 @@ extern "C" {
  *   without tokens) and may be the same buffer as state_in.
  * g is a log decay: 0 keeps, -infinity forgets (below -10000 is taken as that).  Sequences are computed in pieces of 64 tokens: a key, value,
  * query or gate that is not finite spoils the whole piece that it is in and all that follows in its head and sequence.
- * Products run on the tensor cores, their operands as sums of bf16 numbers: two for bf16 and fp16 tensors (16 bits of each operand; o of
- * bf16 tensors from states and updates rounded to one), three for fp32 (about 24 bits).
+ * Products run on the tensor cores, sums and states as operands in three bf16 numbers each (24 bits).
  * states (optional): what the backward pass continues from, delta_states_size bytes, aligned to 16; the caller keeps it until then.
  * B * H * ceil(L / 64) * ceil(V / 16) is below 2^31.
  */

@@ -29,6 +29,8 @@ constexpr size_t kStatusBytes = 256;
 // Reads and clears the device word that kernels without a workspace raise when a bounded wait expires.
 // Returns cudaSuccess and sets *raised, or the CUDA error.  The stream must already be idle.
 cudaError_t consume_device_timeout(bool* raised);
+// Address of that word on the current device, for kernels of other files.
+cudaError_t device_timeout_word(unsigned** word);
 
 // Every kernel launch goes through this so that conv2d_launch_count() is exact.
 void count_launch(int launches = 1);

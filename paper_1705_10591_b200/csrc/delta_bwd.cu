@@ -1,7 +1,7 @@
-// Gated delta rule, backward.  With dS the gradient of the state behind a piece (D_ij = e^(G_i - G_j), E and t as in the forward pass):
-//   dU = scale P^T dO + diag(e^(G_63 - G)) K dS,   W = dU - t^T (beta dU),   dV = beta W,   dbeta = rows of W . E,
-//   dS <- e^(G_63) dS + Q^T (scale e^G dO) - K^T (e^G dV)
-// walks the pieces from the last one back, 16 columns of V a warp, as the forward pass does; then every piece by itself:
+// Gated delta rule, backward.  With dS the gradient of the state behind a piece (D_ij = e^(G_i - G_j); E, t and P' as in the forward pass):
+//   X = diag(e^(G_63 - G)) K dS,   W = X + [-t; P']^T [beta X; scale dO],   dV = beta W,   dbeta = rows of W . E,
+//   dS <- e^(G_63) dS + [K; Q]^T [-e^G dV; scale e^G dO]
+// walks the pieces from the last one back; then every piece by itself:
 //   p = D o (scale dO (beta E)^T), j <= i;   y = -D o (dV (beta E)^T), j < i;
 //   dq = scale e^G dO S^T + p K;   dk = a + c,  a = y K - e^G dV S^T,  c = p^T Q + y^T K + e^(G_63 - G) beta E dS^T,
 //   dG_i = q_i.dq_i + k_i.a_i - k_i.c_i,   dg_t = sum of dG_i, i >= t, + <S after the piece, dS>
@@ -11,472 +11,413 @@
 namespace conv2d_b200 {
 namespace {
 
-template <typename T, int KD>
-__global__ void __launch_bounds__((kComputing + kLoaders) * 32, 1) delta_bwd_walk_kernel(const DeltaArgs a, int warps, int across, bool wide_do, bool wide_dv)
+template <typename T, int KD, int NV>
+__global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const DeltaArgs a, int across, bool wide_do, bool wide_dv)
 {
-    using W = Walk<T, KD>;
-    constexpr int IN = Parts<T>::in, SUM = Parts<T>::sum, STAGES = W::stages;
-    extern __shared__ __align__(1024) unsigned char raw[];
-    ptx::grid_dep_wait();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = 2 * (lane & 3);
-    const int v0 = (int)(blockIdx.x % across) * warps * 16, bh = blockIdx.x / across, h = bh % a.H, b = bh / a.H;
-    const int len = sequence_length(a.lengths, b, a.L), pieces = (len + kPiece - 1) / kPiece;
-    const bool computes = warp < warps;
-    const int v = v0 + warp * 16;
-    const T* values = static_cast<const T*>(a.dout);
-    const int cols = min(warps * 16, a.V - v0);
-    auto stage = [&](int i) { return Stage<T, KD>{raw + (STAGES == 2 ? (i & 1) * W::stage(warps) : 0), warps}; };
-    auto load = [&](int i, int id, int threads) {
-        load_piece<T, KD>(a, stage(i), values, a.lddo, wide_do, b, h, i, len - i * kPiece, v0, id, threads);
-        copies_commit();
-    };
-
-    float S[KD / 8][4];                                        // dS^T
-    const size_t state0 = ((size_t)b * a.H + h) * a.K * a.V;
-#pragma unroll
-    for (int n = 0; n < KD / 8; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int k = n * 8 + c + (e & 1), col = v + g + 8 * (e >> 1);
-            S[n][e] = a.dstate_out && computes && k < a.K && col < a.V ? a.dstate_out[state0 + (size_t)k * a.V + col] : 0.f;
-        }
-
-    if (pieces > 0 && STAGES == 2) {
-        load(pieces - 1, tid, blockDim.x);
-        copies_wait<0>();
+    using W = Walk<T, KD, NV>;
+    constexpr int IN = W::IN, C = W::C, STAGES = W::stages;
+    extern __shared__ unsigned char unaligned[];
+    unsigned char* raw = unaligned + ((1024 - (ptx::smem_u32(unaligned) & 1023)) & 1023);
+    unsigned char *squares = raw + STAGES * W::keys, *state = squares + W::squares, *rows = state + W::state;
+    WalkBars* bars = reinterpret_cast<WalkBars*>(rows + kSum * W::rows_part);
+    volatile uint32_t* abort_flag = &bars->abort;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int v0 = (int)(blockIdx.x % across) * NV, bh = blockIdx.x / across, h = bh % a.H, b = bh / a.H, hk = h / a.share;
+    if (tid == 0) {
+        bars->abort = 0;
+        ptx::mbar_init(&bars->keys[0], 1), ptx::mbar_init(&bars->keys[1], 1), ptx::mbar_init(&bars->squares, 1);
+        for (int i = 0; i < 3; ++i) ptx::mbar_init(&bars->done[i], 1);
+        ptx::fence_mbar_init();
     }
+    if (warp == kWorkers / 32) {
+        ptx::tmem_alloc(&bars->tmem, W::cols);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before_sync();
     __syncthreads();
-    for (int i = pieces - 1; i >= 0; --i) {
-        if (STAGES == 1) {
-            load(i, tid, blockDim.x);
-            copies_wait<0>();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = bars->tmem;
+    ptx::grid_dep_wait();
+    const int len = sequence_length(a.lengths, b, a.L), pieces = (len + kPiece - 1) / kPiece;
+    const size_t unit0 = (size_t)bh * a.pieces;
+
+    if (warp == kWorkers / 32) {
+        const uint32_t elected = ptx::elect_one();
+        const unsigned char* key_tiles = a.keys + ((size_t)b * a.Hk + hk) * a.pieces * W::keys;
+        auto load_keys = [&](int s) {                          // the s-th piece from the end
+            if (!elected || s >= pieces) return;
+            uint64_t* bar = &bars->keys[STAGES == 2 ? s & 1 : 0];
+            ptx::mbar_arrive_expect_tx(bar, W::keys);
+            ptx::bulk_g2s(raw + (STAGES == 2 ? s & 1 : 0) * W::keys, key_tiles + (size_t)(pieces - 1 - s) * W::keys, W::keys, bar);
+        };
+        auto load_squares = [&](int s) {
+            if (!elected || s >= pieces) return;
+            ptx::mbar_arrive_expect_tx(&bars->squares, W::squares);
+            ptx::bulk_g2s(squares, a.squares + (unit0 + pieces - 1 - s) * kSquares, W::squares, &bars->squares);
+        };
+        const uint32_t s_squares = ptx::smem_u32(squares), s_state = ptx::smem_u32(state), s_rows = ptx::smem_u32(rows);
+        constexpr uint32_t id1 = ptx::idesc_b16(128, NV, false) | ptx::kIdescBMajorMN, id3 = id1 | kIdescAMajorM;
+        load_keys(0), load_squares(0);
+        if (STAGES == 2) load_keys(1);
+        bool alive = true;
+        for (int s = 0; s < pieces; ++s) {
+            const uint32_t keys = ptx::smem_u32(raw) + (STAGES == 2 ? s & 1 : 0) * W::keys;
+            alive = alive && ptx::mbar_wait_bounded_warp(&bars->keys[STAGES == 2 ? s & 1 : 0], (STAGES == 2 ? s >> 1 : s) & 1, abort_flag, a.max_polls);
+            __syncthreads();                                   // dS is there
+            ptx::tc_fence_after_sync();
+            if (alive) {
+                multiply(tmem, IN, kSum, KD / 16, id1, elected, false, [&](int p, int k) { return rows_as_m(keys + p * W::key_part + (k >> 2) * W::HALF + (k & 3) * 32); },
+                         [&](int p, int k) { return rows_as_k<NV>(s_state + p * W::state_part + k * 16 * NV * 2); });
+                ptx::mma_commit(&bars->done[0], elected);
+                if (STAGES == 2 && s > 0) load_keys(s + 1);
+            }
+            alive = alive && ptx::mbar_wait_bounded_warp(&bars->squares, s & 1, abort_flag, a.max_polls);
+            __syncthreads();                                   // beta X and scale dO are there
+            ptx::tc_fence_after_sync();
+            if (alive) {                                       // (64 columns; the other 64 rows of the result are of whatever lies behind, and not read)
+                multiply(tmem + NV, kSum, kSum, 2 * kPiece / 16, id3, elected, false, [&](int p, int k) { return columns_as_m(s_squares + p * W::square_part + k * 16 * 128, W::square_part); },
+                         [&](int p, int k) { return rows_as_k<NV>(s_rows + p * W::rows_part + k * 16 * NV * 2); });
+                ptx::mma_commit(&bars->done[1], elected);
+            }
+            __syncthreads();                                   // -e^G dV and scale e^G dO are there, in their place
+            ptx::tc_fence_after_sync();
+            if (alive) {
+                multiply(tmem + 2 * NV, IN, kSum, 2 * kPiece / 16, id3, elected, false, [&](int p, int k) { return columns_as_m(keys + p * W::key_part + k * 16 * 128, W::HALF); },
+                         [&](int p, int k) { return rows_as_k<NV>(s_rows + p * W::rows_part + k * 16 * NV * 2); });
+                ptx::mma_commit(&bars->done[2], elected);
+                load_squares(s + 1);
+                if (STAGES == 1) {
+                    alive = ptx::mbar_wait_bounded_warp(&bars->done[2], s & 1, abort_flag, a.max_polls);
+                    if (alive) load_keys(s + 1);
+                }
+            }
+        }
+    } else {
+        const int quarter = warp & 3, row = quarter * 32 + lane, col0 = (warp >> 2) * C, token = row & (kPiece - 1), v = v0 + col0;
+        const bool is_key = row < kPiece;                      // a token of K (its E and dV), or of Q (its dO); and row `row` of dS
+        const uint32_t at = tmem + ((uint32_t)quarter << 21) + col0;
+        const int there = a.V - v, saved = a.VP - v;
+        float S[C], X[C], y[C];
+        const size_t state0 = ((size_t)bh * a.K + row) * a.V + v;
+#pragma unroll
+        for (int j = 0; j < C; ++j) S[j] = a.dstate_out && row < a.K && j < there ? a.dstate_out[state0 + j] : 0.f;
+        const T* dout = static_cast<const T*>(a.dout) + ((long long)b * a.L + token) * a.lddo + (long long)h * a.V + v;
+        T* dv = static_cast<T*>(a.dv) + ((long long)b * a.L + token) * a.lddv + (long long)h * a.V + v;
+        const float* factors = a.factors + unit0 * (kFactors * kPiece);
+        float next[C], eg = 0.f, ed = 0.f, beta = 0.f, whole = 0.f;
+        auto fetch = [&](int i) {
+            if (i < 0) return;
+            const float* f = factors + (size_t)i * (kFactors * kPiece);
+            eg = f[token], ed = f[kPiece + token], beta = f[2 * kPiece + token], whole = f[kPiece - 1];
+            if (is_key) load_row<float, C>(a.updates + ((unit0 + i) * kPiece + token) * a.VP + v, min(saved, C) / 16 * 16, true, next);
+            else load_row<T, C>(dout + (long long)i * kPiece * a.lddo, i * kPiece + token < len ? there : 0, wide_do, next);
+        };
+        auto put_state = [&](int i) {                          // dS behind piece i
+            if (row < KD) {
+                put_row<NV, C>(state, W::state_part, row, col0, S);
+                save_row<C>(a.dstates + ((unit0 + i) * KD + row) * a.VP + v, saved, S);
+            }
+            ptx::fence_proxy_async_smem();
+        };
+        if (pieces > 0) put_state(pieces - 1);
+        fetch(pieces - 1);
+        for (int i = pieces - 1; i >= 0; --i) {
+            const uint32_t parity = (pieces - 1 - i) & 1;
+            ptx::tc_fence_before_sync();
             __syncthreads();
-        } else if (!computes) {
-            if (i > 0) load(i - 1, tid - warps * 32, blockDim.x - warps * 32);
-            copies_wait<0>();
+            if (!is_key) {
+#pragma unroll
+                for (int j = 0; j < C; ++j) y[j] = a.scale * next[j];
+                put_row<NV, C>(rows, W::rows_part, row, col0, y);
+            }
+            // D1: K dS
+            ptx::mbar_wait_bounded(&bars->done[0], parity, abort_flag, a.max_polls);
+            ptx::tc_fence_after_sync();
+            if (is_key) {
+                tmem_row<C>(at, X);
+#pragma unroll
+                for (int j = 0; j < C; ++j) X[j] *= ed, y[j] = beta * X[j];
+                put_row<NV, C>(rows, W::rows_part, row, col0, y);
+            }
+            ptx::fence_proxy_async_smem();
+            ptx::tc_fence_before_sync();
+            __syncthreads();
+            // D2: W - X
+            ptx::mbar_wait_bounded(&bars->done[1], parity, abort_flag, a.max_polls);
+            ptx::tc_fence_after_sync();
+            float sum = 0.f;
+            if (is_key) {
+                tmem_row<C>(at + NV, y);
+#pragma unroll
+                for (int j = 0; j < C; ++j) {
+                    y[j] += X[j];
+                    sum = fmaf(y[j], next[j], sum);
+                    X[j] = beta * y[j];
+                    y[j] = -eg * X[j];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < C; ++j) y[j] *= eg;
+            }
+            put_row<NV, C>(rows, W::rows_part, row, col0, y);
+            ptx::fence_proxy_async_smem();
+            ptx::tc_fence_before_sync();
+            __syncthreads();
+            if (is_key) {
+                const size_t unit = unit0 + i;
+                save_row<C>(a.dupdates + (unit * kPiece + token) * a.VP + v, saved, X);
+                if (i * kPiece + token < len) store_row<T, C>(dv + (long long)i * kPiece * a.lddv, there, wide_dv, X);
+                if (saved > 0) {                               // (a sum over 32 columns stands for two of 16)
+                    float* part = a.dbeta_parts + (unit * (a.VP / 16) + v / 16) * kPiece + token;
+                    part[0] = sum;
+                    if (C == 32 && saved > 16) part[kPiece] = 0.f;
+                }
+            }
+            const float keep = whole;
+            fetch(i - 1);
+            // D3: dS <- e^G_63 dS + ..
+            ptx::mbar_wait_bounded(&bars->done[2], parity, abort_flag, a.max_polls);
+            ptx::tc_fence_after_sync();
+            tmem_row<C>(at + 2 * NV, y);
+#pragma unroll
+            for (int j = 0; j < C; ++j) S[j] = fmaf(keep, S[j], y[j]);
+            if (i > 0) put_state(i - 1);
         }
-        if (computes && v < a.V) {
-            const Stage<T, KD> s = stage(i);
-            const float* f = s.factors();
-            const size_t unit = ((size_t)b * a.H + h) * a.pieces + i;
-            float U[8][4] = {}, X[8][4] = {};
-            // dS^T K^T
+        if (a.dstate_in && row < a.K) {
 #pragma unroll
-            for (int n = 0; n < KD / 8; n += 2) {
-                uint32_t x[SUM][4];
-                left_of<SUM>(x, S[n], S[n + 1]);
-                bf16* to = a.dstates + (unit * SUM * a.VP + v + g) * KD + n * 8 + c;
-#pragma unroll
-                for (int p = 0; p < SUM; ++p, to += (size_t)a.VP * KD) {
-                    *reinterpret_cast<uint32_t*>(to) = x[p][0], *reinterpret_cast<uint32_t*>(to + 8 * KD) = x[p][1];
-                    *reinterpret_cast<uint32_t*>(to + 8) = x[p][2], *reinterpret_cast<uint32_t*>(to + 8 * KD + 8) = x[p][3];
-                }
-#pragma unroll
-                for (int m = 0; m < 8; m += 2) {
-#pragma unroll
-                    for (int p = 0; p < IN; ++p) {
-                        uint32_t r[4];
-                        right_nk<KD>(r, s.k() + p * (kPiece * KD * 2), m * 8, n * 8, lane);
-                        mma_parts<SUM>(U[m], U[m + 1], x, r, p);
-                    }
-                }
-            }
-            // dO^T P
-            const T* ds = s.values() + warp * 16 + g;
-            auto dout = [&](int j, float (&d)[4]) {            // a tile of dO^T, 8 tokens from 8 j on
-#pragma unroll
-                for (int e = 0; e < 4; ++e) d[e] = to_float(ds[(j * 8 + c + (e & 1)) * s.pitch() + 8 * (e >> 1)]);
-            };
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                uint32_t x[IN][4];
-                float d0[4], d1[4];
-                dout(j, d0), dout(j + 1, d1);
-                left_of<IN>(x, d0, d1);
-#pragma unroll
-                for (int m = 0; m <= j; m += 2) {
-#pragma unroll
-                    for (int p = 0; p < SUM; ++p) {
-                        uint32_t r[4];
-                        right_kn<kPiece>(r, s.p() + p * (kPiece * kPiece * 2), j * 8, m * 8, lane);
-#pragma unroll
-                        for (int q = 0; q < IN; ++q)
-                            if (p + q < SUM) mma(X[m], x[q], r[0], r[1]), mma(X[m + 1], x[q], r[2], r[3]);
-                    }
-                }
-            }
-#pragma unroll
-            for (int m = 0; m < 8; ++m) {
-                const float2 d = *reinterpret_cast<const float2*>(f + kPiece + m * 8 + c);
-                const float2 be = *reinterpret_cast<const float2*>(f + 2 * kPiece + m * 8 + c);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    U[m][e] = fmaf(a.scale, X[m][e], (e & 1 ? d.y : d.x) * U[m][e]);
-                    X[m][e] = -(e & 1 ? be.y : be.x) * U[m][e];
-                }
-            }
-            // W = dU - t^T (beta dU): tokens j * 8 .. + 15 on those up to there
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                uint32_t x[SUM][4];
-                left_of<SUM>(x, X[j], X[j + 1]);
-#pragma unroll
-                for (int m = 0; m <= j; m += 2) {
-#pragma unroll
-                    for (int p = 0; p < SUM; ++p) {
-                        uint32_t r[4];
-                        right_kn<kPiece>(r, s.t() + p * (kPiece * kPiece * 2), j * 8, m * 8, lane);
-                        mma_parts<SUM>(U[m], U[m + 1], x, r, p);
-                    }
-                }
-            }
-            // dbeta: this warp's share of W . E; dV
-            const bf16* es = a.updates + (unit * SUM * a.VP + v + g) * kPiece + c;
-            bf16* dvs = a.dupdates + (unit * SUM * a.VP + v + g) * kPiece + c;
-            float* parts = a.dbeta_parts + (unit * (a.VP / 16) + v / 16) * kPiece;
-#pragma unroll
-            for (int m = 0; m < 8; ++m) {
-                float2 e0 = make_float2(0.f, 0.f), e1 = e0;
-#pragma unroll
-                for (int p = SUM - 1; p >= 0; --p) {
-                    const bf16* at = es + (size_t)p * a.VP * kPiece + m * 8;
-                    const float2 lo = to_pair(*reinterpret_cast<const uint32_t*>(at), bf16()), hi = to_pair(*reinterpret_cast<const uint32_t*>(at + 8 * kPiece), bf16());
-                    e0.x += lo.x, e0.y += lo.y, e1.x += hi.x, e1.y += hi.y;
-                }
-                float2 sum = make_float2(fmaf(U[m][0], e0.x, U[m][2] * e1.x), fmaf(U[m][1], e0.y, U[m][3] * e1.y));
-#pragma unroll
-                for (int d = 4; d < 32; d *= 2) sum.x += __shfl_xor_sync(0xffffffffu, sum.x, d), sum.y += __shfl_xor_sync(0xffffffffu, sum.y, d);
-                if (g == 0) *reinterpret_cast<float2*>(parts + m * 8 + c) = sum;
-                const float2 be = *reinterpret_cast<const float2*>(f + 2 * kPiece + m * 8 + c);
-                U[m][0] *= be.x, U[m][1] *= be.y, U[m][2] *= be.x, U[m][3] *= be.y;
-                uint32_t x[SUM], y[SUM];
-                split<SUM>(U[m][0], U[m][1], x);
-                split<SUM>(U[m][2], U[m][3], y);
-#pragma unroll
-                for (int p = 0; p < SUM; ++p) {
-                    bf16* to = dvs + (size_t)p * a.VP * kPiece + m * 8;
-                    *reinterpret_cast<uint32_t*>(to) = x[p], *reinterpret_cast<uint32_t*>(to + 8 * kPiece) = y[p];
-                }
-            }
-            T* mine = reinterpret_cast<T*>(raw + STAGES * W::stage(warps)) + warp * kPiece * (16 + W::kPad);
-            store_columns(U, mine, static_cast<T*>(a.dv) + ((long long)b * a.L + (long long)i * kPiece) * a.lddv + (long long)h * a.V + v, a.lddv, len - i * kPiece,
-                          a.V - v, wide_dv, lane);
-            // dS <- e^G_63 dS + (scale e^G dO)^T Q - (e^G dV)^T K
-            const float whole = f[kPiece - 1];
-#pragma unroll
-            for (int n = 0; n < KD / 8; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) S[n][e] *= whole;
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                uint32_t x[SUM][4], y[SUM][4];
-                float d0[4], d1[4];
-                dout(j, d0), dout(j + 1, d1);
-                const float2 g0 = *reinterpret_cast<const float2*>(f + j * 8 + c), g1 = *reinterpret_cast<const float2*>(f + j * 8 + 8 + c);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x0 = e & 1 ? g0.y : g0.x, x1 = e & 1 ? g1.y : g1.x;
-                    d0[e] *= a.scale * x0, d1[e] *= a.scale * x1;
-                    U[j][e] *= -x0, U[j + 1][e] *= -x1;
-                }
-                left_of<SUM>(x, d0, d1);
-                left_of<SUM>(y, U[j], U[j + 1]);
-#pragma unroll
-                for (int n = 0; n < KD / 8; n += 2) {
-#pragma unroll
-                    for (int p = 0; p < IN; ++p) {
-                        uint32_t r[4];
-                        right_kn<KD>(r, s.q() + p * (kPiece * KD * 2), j * 8, n * 8, lane);
-                        mma_parts<SUM>(S[n], S[n + 1], x, r, p);
-                        right_kn<KD>(r, s.k() + p * (kPiece * KD * 2), j * 8, n * 8, lane);
-                        mma_parts<SUM>(S[n], S[n + 1], y, r, p);
-                    }
-                }
-            }
+            for (int j = 0; j < C; ++j)
+                if (j < there) a.dstate_in[state0 + j] = S[j];
         }
-        __syncthreads();
+        zero_rows(static_cast<T*>(a.dv) + (long long)b * a.L * a.lddv + (long long)h * a.V + v0, a.lddv, len, a.L, min(NV, a.V - v0), tid, kWorkers);
     }
-    if (a.dstate_in && computes) {
-#pragma unroll
-        for (int n = 0; n < KD / 8; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int k = n * 8 + c + (e & 1), col = v + g + 8 * (e >> 1);
-                if (k < a.K && col < a.V) a.dstate_in[state0 + (size_t)k * a.V + col] = S[n][e];
-            }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == kWorkers / 32) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, W::cols);
+        if (lane == 0 && *abort_flag) atomicExch(a.timeout, 1u);
     }
-    zero_rows(static_cast<T*>(a.dv) + (long long)b * a.L * a.lddv + (long long)h * a.V + v0, a.lddv, len, a.L, cols, tid, blockDim.x);
 }
 
-// One block for one piece of one value head.  Four warps by 16 tokens times two by halves of K; products over V in blocks of 64 columns.
+// One block for one piece of one value head: products over V in blocks of 32 columns, two in turn (while one's products run, the threads bring the next one's numbers and
+// split them), then products over tokens.
+//   D1 [dV; dO] S^T,   D2 [dV; dO] E^T,   D3 E dS^T (64 rows; the others are of what lies behind),   then of D2 [y; p],
+//   D4 [y; p] K,   D5 [y; p]^T [K; Q] (64 rows likewise).
+// In the last step a thread has half a row of a and c (keys) or of dq (queries).
 template <typename T, int KD>
 struct Piecewise {
-    static constexpr int IN = Parts<T>::in, SUM = Parts<T>::sum, BLOCK = 64;
-    static constexpr size_t dout = (size_t)IN * kPiece * BLOCK * 2, update = (size_t)SUM * BLOCK * kPiece * 2, state = (size_t)SUM * BLOCK * KD * 2;
-    static constexpr size_t over_v = dout + 2 * update + 2 * state;
-    static constexpr size_t keys = (size_t)IN * kPiece * KD * 2, square = (size_t)SUM * kPiece * kPiece * 2;
-    static constexpr size_t over_tokens = 2 * keys + 2 * square;
-    static constexpr size_t smem = over_v > over_tokens ? over_v : over_tokens;
+    static constexpr int IN = Parts<T>::in, NB = 32, HALF = 2 * kPiece * 128;
+    static constexpr int rows_part = 2 * kPiece * NB * 2, e_part = kPiece * NB * 2, state_part = KD * NB * 2;
+    static constexpr int at_e = kSum * rows_part, at_s = at_e + kSum * e_part, at_ds = at_s + kSum * state_part, block = at_ds + kSum * state_part;
+    static constexpr int keys = IN * (KD / 64) * HALF, key_part = (KD / 64) * HALF, square_part = 2 * kPiece * 128;
+    static constexpr int over_v = 2 * block, over_tokens = keys + kSum * square_part;
+    // (the 64 rows more reach as far as one tile behind the last one; 1024 to the first boundary of the swizzle)
+    static constexpr int reach = over_tokens + square_part, smem = (over_v > reach ? over_v : reach) + 1024;
+    static constexpr uint32_t d1 = 0, d3 = KD, d4 = 2 * KD, d2 = 3 * KD, d5 = 3 * KD;         // columns of tensor memory (D2 has been read when D5 is written)
+    static constexpr uint32_t cols = 4 * KD;
+};
+struct PieceBars {
+    uint64_t done[2], keys, last;
+    uint32_t tmem, abort;
+    float factors[kFactors * kPiece], dots[4][kPiece], sums[8];
 };
 
 template <typename T, int KD>
-__global__ void __launch_bounds__(256) delta_bwd_pieces_kernel(const DeltaArgs a)
+__global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_pieces_kernel(const DeltaArgs a, bool wide_do, bool wide_dq, bool wide_dk, bool wide_parts)
 {
-    using S = Piecewise<T, KD>;
-    constexpr int IN = S::IN, SUM = S::SUM, BLOCK = S::BLOCK, HALF = KD / 2, NT = HALF / 8;
-    extern __shared__ __align__(1024) unsigned char raw[];
-    __shared__ float f[kFactors * kPiece], dots[2][kPiece], sums[8];
-    ptx::grid_dep_wait();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = 2 * (lane & 3);
+    using W = Piecewise<T, KD>;
+    constexpr int IN = W::IN, NB = W::NB;
+    extern __shared__ unsigned char unaligned[];
+    __shared__ PieceBars bars;
+    unsigned char* raw = unaligned + ((1024 - (ptx::smem_u32(unaligned) & 1023)) & 1023);
+    volatile uint32_t* abort_flag = &bars.abort;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int piece = blockIdx.x % a.pieces, bh = blockIdx.x / a.pieces, h = bh % a.H, b = bh / a.H, hk = h / a.share;
-    const int live = min(sequence_length(a.lengths, b, a.L) - piece * kPiece, kPiece), there = min(a.L - piece * kPiece, kPiece);
     const long long row0 = (long long)b * a.L + (long long)piece * kPiece;
+    ptx::grid_dep_wait();
+    const int live = min(sequence_length(a.lengths, b, a.L) - piece * kPiece, kPiece), there = min(a.L - piece * kPiece, kPiece);
     const bool shared_key = a.dq_parts != nullptr;
     T *dq = static_cast<T*>(a.dq) + row0 * a.lddq + (long long)hk * a.K, *dk = static_cast<T*>(a.dk) + row0 * a.lddk + (long long)hk * a.K;
     const long long part0 = (row0 * a.H + h) * a.K;
-    auto put = [&](int row, int col, float q, float k) {
-        if (shared_key) {
-            const long long at = part0 + (long long)row * a.H * a.K + col;
-            a.dq_parts[at] = q, a.dk_parts[at] = k;
-        } else {
-            dq[row * a.lddq + col] = from_float<T>(q), dk[row * a.lddk + col] = from_float<T>(k);
-        }
-    };
     // padding
-    for (int i = tid; i < (there - max(live, 0)) * a.K; i += 256) put(max(live, 0) + i / a.K, i % a.K, 0.f, 0.f);
-    for (int i = max(live, 0) + tid; i < there; i += 256) a.dg[(row0 + i) * a.lddg + h] = 0.f, a.dbeta[(row0 + i) * a.lddbeta + h] = 0.f;
+    if (live < there) {
+        const int first = max(live, 0);
+        for (int i = tid; i < (there - first) * a.K; i += kWalkThreads) {
+            const int row = first + i / a.K, col = i % a.K;
+            if (shared_key) a.dq_parts[part0 + (long long)row * a.H * a.K + col] = 0.f, a.dk_parts[part0 + (long long)row * a.H * a.K + col] = 0.f;
+            else dq[row * a.lddq + col] = from_float<T>(0.f), dk[row * a.lddk + col] = from_float<T>(0.f);
+        }
+        for (int i = first + tid; i < there; i += kWalkThreads) a.dg[(row0 + i) * a.lddg + h] = 0.f, a.dbeta[(row0 + i) * a.lddbeta + h] = 0.f;
+    }
     if (live <= 0) return;
 
     const size_t unit = (size_t)bh * a.pieces + piece;
-    for (int i = tid; i < kFactors * kPiece; i += 256) f[i] = a.factors[unit * (kFactors * kPiece) + i];
-    const uint32_t base = ptx::smem_u32(raw);
-    const uint32_t s_do = base, s_dv = s_do + (uint32_t)S::dout, s_e = s_dv + (uint32_t)S::update, s_s = s_e + (uint32_t)S::update, s_ds = s_s + (uint32_t)S::state;
-    const int m0 = (warp & 3) * 16, side = warp >> 2;
-    float Q[NT][4] = {}, A[NT][4] = {}, C[NT][4] = {}, P[4][4] = {}, Y[4][4] = {};
-    float inner = 0.f;                                         // <S, dS>
-    const T* dout = static_cast<const T*>(a.dout) + row0 * a.lddo + (long long)h * a.V;
-    for (int v0 = 0; v0 < a.V; v0 += BLOCK) {
-        const int rows = min(a.VP - v0, BLOCK);
-        if (v0) __syncthreads();
-        for (int p = 0; p < SUM; ++p) {
-            const size_t at = (unit * SUM + p) * a.VP + v0;
-            copy_rows<kPiece>(a.dupdates + at * kPiece, s_dv + p * (BLOCK * kPiece * 2), BLOCK, rows, tid, 256);
-            copy_rows<kPiece>(a.updates + at * kPiece, s_e + p * (BLOCK * kPiece * 2), BLOCK, rows, tid, 256);
-            copy_rows<KD>(a.states + at * KD, s_s + p * (BLOCK * KD * 2), BLOCK, rows, tid, 256);
-            copy_rows<KD>(a.dstates + at * KD, s_ds + p * (BLOCK * KD * 2), BLOCK, rows, tid, 256);
+    if (tid == 0) {
+        bars.abort = 0;
+        ptx::mbar_init(&bars.done[0], 1), ptx::mbar_init(&bars.done[1], 1), ptx::mbar_init(&bars.keys, 1), ptx::mbar_init(&bars.last, 1);
+        ptx::fence_mbar_init();
+    }
+    if (warp == kWorkers / 32) {
+        ptx::tmem_alloc(&bars.tmem, W::cols);
+        ptx::tmem_relinquish();
+    }
+    for (int i = tid; i < kFactors * kPiece; i += kWalkThreads) bars.factors[i] = a.factors[unit * (kFactors * kPiece) + i];
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = bars.tmem, base = ptx::smem_u32(raw);
+    const int blocks = (a.VP + NB - 1) / NB;
+    const uint32_t keys = base, squares = base + W::keys;
+
+    if (warp == kWorkers / 32) {
+        const uint32_t elected = ptx::elect_one();
+        constexpr uint32_t idk = ptx::idesc_b16(128, KD, false), ide = ptx::idesc_b16(128, kPiece, false);
+        // tiles of rows of 32 numbers, K-major: 64-byte swizzle
+        auto narrow = [](uint32_t at) { return rows_as_k<32>(at); };
+        for (int j = 0; j < blocks; ++j) {
+            __syncthreads();
+            ptx::tc_fence_after_sync();
+            const uint32_t at = base + (j & 1) * W::block;
+            auto rows = [&](int p, int k) { return narrow(at + p * W::rows_part + k * 32); };
+            auto e = [&](int p, int k) { return narrow(at + W::at_e + p * W::e_part + k * 32); };
+            multiply(tmem + W::d1, kSum, kSum, NB / 16, idk, elected, j > 0, rows, [&](int p, int k) { return narrow(at + W::at_s + p * W::state_part + k * 32); });
+            multiply(tmem + W::d2, kSum, kSum, NB / 16, ide, elected, j > 0, rows, e);
+            multiply(tmem + W::d3, kSum, kSum, NB / 16, idk, elected, j > 0, e, [&](int p, int k) { return narrow(at + W::at_ds + p * W::state_part + k * 32); });
+            ptx::mma_commit(&bars.done[j & 1], elected);
         }
-        copies_commit();
-        for (int i = tid; i < kPiece * (BLOCK / 2); i += 256) {
-            const int row = i / (BLOCK / 2), col = i % (BLOCK / 2) * 2;
-            float x[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) x[j] = row < live && v0 + col + j < a.V ? to_float(dout[row * a.lddo + v0 + col + j]) : 0.f;
-            uint32_t w[IN];
-            split<IN>(x[0], x[1], w);
-#pragma unroll
-            for (int p = 0; p < IN; ++p)
-                *reinterpret_cast<uint32_t*>(raw + (unit_at<BLOCK>(s_do + p * (kPiece * BLOCK * 2), row, col >> 3) - base) + (col & 7) * 2) = w[p];
+        bool alive = ptx::mbar_wait_bounded_warp(&bars.done[(blocks - 1) & 1], ((blocks - 1) >> 1) & 1, abort_flag, a.max_polls);
+        if (alive && elected) {                                // (the tiles over V are done with)
+            ptx::mbar_arrive_expect_tx(&bars.keys, W::keys);
+            ptx::bulk_g2s(raw, a.keys + (((size_t)b * a.Hk + hk) * a.pieces + piece) * W::keys, W::keys, &bars.keys);
         }
-        copies_wait<0>();
+        alive = alive && ptx::mbar_wait_bounded_warp(&bars.keys, 0, abort_flag, a.max_polls);
+        __syncthreads();                                       // [y; p] is there
+        ptx::tc_fence_after_sync();
+        if (alive) {
+            auto tokens = [&](int p, int k) { return columns_as_m(keys + p * W::key_part + k * 16 * 128, W::HALF); };
+            multiply(tmem + W::d4, kSum, IN, kPiece / 16, idk | ptx::kIdescBMajorMN, elected, false, [&](int p, int k) { return rows_as_m(squares + p * W::square_part + k * 32); },
+                     tokens);
+            multiply(tmem + W::d5, kSum, IN, 2 * kPiece / 16, idk | ptx::kIdescBMajorMN | kIdescAMajorM, elected, false,
+                     [&](int p, int k) { return columns_as_m(squares + p * W::square_part + k * 16 * 128, W::square_part); }, tokens);
+            ptx::mma_commit(&bars.last, elected);
+        }
         __syncthreads();
-        for (int i = tid; i < BLOCK * KD / 8; i += 256) {      // (a unit of S times the same of dS)
-            float x[8] = {}, y[8] = {};
+    } else {
+        const int quarter = warp & 3, row = quarter * 32 + lane, side = warp >> 2, token = row & (kPiece - 1);
+        const bool is_key = row < kPiece;
+        float inner = 0.f;                                     // <S, dS>
+        {
+            const int r2 = tid >> 1, c2 = (tid & 1) * 16, r4 = tid >> 2, c4 = (tid & 3) * 8, t2 = r2 & (kPiece - 1);
+            const T* dout = static_cast<const T*>(a.dout) + (row0 + t2) * a.lddo + (long long)h * a.V;
+            float xr[16], xe[8], xs[16], xd[16];
+            auto fetch = [&](int v0) {
+                const int left = a.VP - v0;                    // a multiple of 16
+                if (r2 < kPiece) load_row<float, 16>(a.dupdates + (unit * kPiece + t2) * a.VP + v0 + c2, left - c2, true, xr);
+                else load_row<T, 16>(dout + v0 + c2, t2 < live ? a.V - v0 - c2 : 0, wide_do, xr);
+                load_row<float, 8>(a.updates + (unit * kPiece + r4) * a.VP + v0 + c4, left - c4, true, xe);
+                const size_t at = (unit * KD + r2) * a.VP + v0 + c2;
+                if (r2 < KD) load_row<float, 16>(a.states + at, left - c2, true, xs), load_row<float, 16>(a.dstates + at, left - c2, true, xd);
+            };
+            fetch(0);
+            for (int j = 0; j < blocks; ++j) {
+                unsigned char* at = raw + (j & 1) * W::block;
+                if (j >= 2) ptx::mbar_wait_bounded(&bars.done[j & 1], ((j >> 1) - 1) & 1, abort_flag, a.max_polls);
+                put_row<NB, 16>(at, W::rows_part, r2, c2, xr);
+                put_row<NB, 8>(at + W::at_e, W::e_part, r4, c4, xe);
+                if (r2 < KD) {
+                    put_row<NB, 16>(at + W::at_s, W::state_part, r2, c2, xs);
+                    put_row<NB, 16>(at + W::at_ds, W::state_part, r2, c2, xd);
 #pragma unroll
-            for (int p = SUM - 1; p >= 0; --p) {
-                const uint32_t at = unit_at<KD>((uint32_t)(p * (BLOCK * KD * 2)), i / (KD / 8), i % (KD / 8));
-                float w[8];
-                unpack(*reinterpret_cast<const Pack<bf16, 8>*>(raw + (s_s - base) + at), w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] += w[e];
-                unpack(*reinterpret_cast<const Pack<bf16, 8>*>(raw + (s_ds - base) + at), w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] += w[e];
+                    for (int i = 0; i < 16; ++i) inner = fmaf(xs[i], xd[i], inner);
+                }
+                ptx::fence_proxy_async_smem();
+                ptx::tc_fence_before_sync();
+                __syncthreads();
+                if (j + 1 < blocks) fetch((j + 1) * NB);
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) inner = fmaf(x[e], y[e], inner);
         }
+        ptx::mbar_wait_bounded(&bars.done[(blocks - 1) & 1], ((blocks - 1) >> 1) & 1, abort_flag, a.max_polls);
+        ptx::tc_fence_after_sync();
+        const float *eg = bars.factors, *ed = eg + kPiece, *be = eg + 2 * kPiece, *high = eg + 3 * kPiece, *low = eg + 4 * kPiece;
+        const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
+        {
+            float x[32];
+            tmem_row<32>(lanes + W::d2 + side * 32, x);
+            const float hi = high[token], lo = low[token];
 #pragma unroll
-        for (int k0 = 0; k0 < BLOCK; k0 += 16) {
-            if (k0 >= rows) break;
-            uint32_t xo[IN][4], xv[SUM][4], xe[SUM][4];
-#pragma unroll
-            for (int p = 0; p < IN; ++p) left_mk<BLOCK>(xo[p], s_do + p * (kPiece * BLOCK * 2), m0, k0, lane);
-#pragma unroll
-            for (int p = 0; p < SUM; ++p) {
-                left_km<kPiece>(xv[p], s_dv + p * (BLOCK * kPiece * 2), k0, m0, lane);
-                left_km<kPiece>(xe[p], s_e + p * (BLOCK * kPiece * 2), k0, m0, lane);
+            for (int j = 0; j < 32; ++j) {
+                const int other = side * 32 + j;
+                const float d = ex2(((hi - high[other]) + (lo - low[other])) * kLog2e) * be[other];
+                x[j] = is_key ? (other < token ? -d * x[j] : 0.f) : (other <= token ? a.scale * d * x[j] : 0.f);
             }
+            put_row<64, 32>(raw + W::keys, W::square_part, row, side * 32, x);
+        }
+        ptx::fence_proxy_async_smem();
+        ptx::tc_fence_before_sync();
+        __syncthreads();
+        ptx::mbar_wait_bounded(&bars.last, 0, abort_flag, a.max_polls);
+        ptx::tc_fence_after_sync();
+        // <S after, dS> = e^G_63 <S, dS> + sum over tokens of k . (e^(G_63 - G) beta E dS^T)
+        float after = eg[kPiece - 1] * inner, dot = 0.f;
+        const float x1 = is_key ? -eg[token] : a.scale * eg[token], x3 = ed[token] * be[token];
+        const T* mine = static_cast<const T*>(is_key ? a.k : a.q) + (row0 + token) * (is_key ? a.ldk : a.ldq) + (long long)hk * a.K;
 #pragma unroll
-            for (int n = 0; n < 4; n += 2) {                   // dO E^T, dV E^T: this warp's 32 of the columns
-                const int n0 = side * 32 + n * 8;
-                if (n0 > m0) continue;
+        for (int col = side * (KD / 2); col < (side + 1) * (KD / 2); col += 16) {
+            float x[16], y[16], z[16];
+            tmem_row<16>(lanes + W::d1 + col, x);
+            tmem_row<16>(lanes + W::d4 + col, y);
+            load_row<T, 16>(mine + col, token < live ? a.K - col : 0, false, z);
 #pragma unroll
-                for (int p = 0; p < SUM; ++p) {
-                    uint32_t r[4];
-                    right_kn<kPiece>(r, s_e + p * (BLOCK * kPiece * 2), k0, n0, lane);
+            for (int j = 0; j < 16; ++j) x[j] = fmaf(x1, x[j], y[j]), dot = fmaf(z[j], x[j], dot);
+            if (is_key) {
+                float w[16];
+                tmem_row<16>(lanes + W::d3 + col, y);
+                tmem_row<16>(lanes + W::d5 + col, w);
 #pragma unroll
-                    for (int q = 0; q < IN; ++q)
-                        if (p + q < SUM) mma(P[n], xo[q], r[0], r[1]), mma(P[n + 1], xo[q], r[2], r[3]);
-                    mma_parts<SUM>(Y[n], Y[n + 1], xv, r, p);
+                for (int j = 0; j < 16; ++j) {
+                    y[j] *= x3, after = fmaf(z[j], y[j], after);
+                    y[j] += w[j], dot = fmaf(-z[j], y[j], dot);
+                    x[j] += y[j];
                 }
             }
-#pragma unroll
-            for (int n = 0; n < NT; n += 2) {
-                const int n0 = side * HALF + n * 8;
-#pragma unroll
-                for (int p = 0; p < SUM; ++p) {
-                    uint32_t r[4];
-                    right_kn<KD>(r, s_s + p * (BLOCK * KD * 2), k0, n0, lane);
-#pragma unroll
-                    for (int q = 0; q < IN; ++q)
-                        if (p + q < SUM) mma(Q[n], xo[q], r[0], r[1]), mma(Q[n + 1], xo[q], r[2], r[3]);
-                    mma_parts<SUM>(A[n], A[n + 1], xv, r, p);
-                    right_kn<KD>(r, s_ds + p * (BLOCK * KD * 2), k0, n0, lane);
-                    mma_parts<SUM>(C[n], C[n + 1], xe, r, p);
-                }
+            if (token < live) {
+                if (shared_key) store_row<float, 16>((is_key ? a.dk_parts : a.dq_parts) + part0 + (long long)token * a.H * a.K + col, a.K - col, wide_parts, x);
+                else store_row<T, 16>(is_key ? dk + token * a.lddk + col : dq + token * a.lddq + col, a.K - col, is_key ? wide_dk : wide_dq, x);
             }
         }
-    }
-    __syncthreads();                                           // (the factors too; what lies over V is not read any more)
-    const uint32_t ks = base, qs = ks + (uint32_t)S::keys, s_p = qs + (uint32_t)S::keys, s_y = s_p + (uint32_t)S::square;
-    copy_keys<KD, IN>(a, ks, 0, b, hk, piece, live, tid, 256);
-    copy_keys<KD, IN>(a, qs, 1, b, hk, piece, live, tid, 256);
-    copies_commit();
-    const float *eg = f, *ed = f + kPiece, *be = f + 2 * kPiece, *high = f + 3 * kPiece, *low = f + 4 * kPiece;
+        bars.dots[side * 2 + (is_key ? 0 : 1)][token] = dot;
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
+        for (int d = 1; d < 32; d *= 2) after += __shfl_xor_sync(0xffffffffu, after, d);
+        if (lane == 0) bars.sums[warp] = after;
+        ptx::tc_fence_before_sync();
+        __syncthreads();
+        if (warp == 0) {                                       // sums from the last token back, two tokens a lane
+            float last = 0.f;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int i = m0 + g + 8 * half, j = side * 32 + n * 8 + c;
-            float pv[2], yv[2];
+            for (int w = 0; w < 8; ++w) last += bars.sums[w];
+            auto total = [&](int i) { return (bars.dots[0][i] + bars.dots[1][i]) + (bars.dots[2][i] + bars.dots[3][i]); };
+            const float x1 = total(63 - 2 * lane), x0 = total(62 - 2 * lane);
+            float s = x0 + x1;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float d = ex2(((high[i] - high[j + e]) + (low[i] - low[j + e])) * kLog2e) * be[j + e];
-                pv[e] = j + e <= i ? a.scale * d * P[n][2 * half + e] : 0.f;
-                yv[e] = j + e < i ? -d * Y[n][2 * half + e] : 0.f;
+            for (int d = 1; d < 32; d *= 2) {
+                const float y = __shfl_up_sync(0xffffffffu, s, d);
+                if (lane >= d) s += y;
             }
-            uint32_t wp[SUM], wy[SUM];
-            split<SUM>(pv[0], pv[1], wp);
-            split<SUM>(yv[0], yv[1], wy);
-            const uint32_t at = unit_at<kPiece>(0, i, j >> 3) + (j & 7) * 2;
-#pragma unroll
-            for (int p = 0; p < SUM; ++p) {
-                *reinterpret_cast<uint32_t*>(raw + (s_p - base) + p * (kPiece * kPiece * 2) + at) = wp[p];
-                *reinterpret_cast<uint32_t*>(raw + (s_y - base) + p * (kPiece * kPiece * 2) + at) = wy[p];
-            }
+            const int first = 62 - 2 * lane;
+            if (first < live) a.dg[(row0 + first) * a.lddg + h] = s + last;
+            if (first + 1 < live) a.dg[(row0 + first + 1) * a.lddg + h] = (s - x0) + last;
+        } else if (warp == 2 || warp == 3) {
+            const int r = (warp - 2) * 32 + lane, tiles = a.VP / 16;
+            const float* from = a.dbeta_parts + unit * tiles * kPiece + r;
+            float s = 0.f;
+            for (int i = 0; i < tiles; ++i) s += from[i * kPiece];
+            if (r < live) a.dbeta[(row0 + r) * a.lddbeta + h] = s;
         }
     }
-    const float g0 = eg[m0 + g], g1 = eg[m0 + g + 8], d0 = ed[m0 + g] * be[m0 + g], d1 = ed[m0 + g + 8] * be[m0 + g + 8];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float x = e < 2 ? g0 : g1;
-            Q[n][e] *= a.scale * x, A[n][e] *= -x, C[n][e] *= e < 2 ? d0 : d1;
-        }
-    }
-    copies_wait<0>();
-    __syncthreads();
-    // a number of K or Q, from its parts
-    auto number = [&](uint32_t tile, int row, int col) {
-        float2 x = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int p = IN - 1; p >= 0; --p) {
-            const float2 y = to_pair(*reinterpret_cast<const uint32_t*>(raw + (unit_at<KD>(tile + p * (kPiece * KD * 2), row, col >> 3) - base) + (col & 7) * 2), bf16());
-            x.x += y.x, x.y += y.y;
-        }
-        return x;
-    };
-    // <S after, dS> = e^G_63 <S, dS> + sum over tokens of k . (e^(G_63 - G) beta E dS^T)
-    float after = eg[kPiece - 1] * inner;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int col = side * HALF + n * 8 + c;
-        const float2 k0 = number(ks, m0 + g, col), k1 = number(ks, m0 + g + 8, col);
-        after = fmaf(k0.x, C[n][0], fmaf(k0.y, C[n][1], fmaf(k1.x, C[n][2], fmaf(k1.y, C[n][3], after))));
-    }
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) after += __shfl_xor_sync(0xffffffffu, after, d);
-    if (lane == 0) sums[warp] = after;
-    // products over tokens
-#pragma unroll
-    for (int k0 = 0; k0 < kPiece; k0 += 16) {
-        uint32_t r[4], x[SUM][4], y[SUM][4];
-        if (k0 <= m0) {                                        // p K, y K: tokens up to these
-#pragma unroll
-            for (int p = 0; p < SUM; ++p) {
-                left_mk<kPiece>(x[p], s_p + p * (kPiece * kPiece * 2), m0, k0, lane);
-                left_mk<kPiece>(y[p], s_y + p * (kPiece * kPiece * 2), m0, k0, lane);
-            }
-#pragma unroll
-            for (int n = 0; n < NT; n += 2) {
-#pragma unroll
-                for (int p = 0; p < IN; ++p) {
-                    right_kn<KD>(r, ks + p * (kPiece * KD * 2), k0, side * HALF + n * 8, lane);
-                    mma_parts<SUM>(Q[n], Q[n + 1], x, r, p);
-                    mma_parts<SUM>(A[n], A[n + 1], y, r, p);
-                }
-            }
-        }
-        if (k0 >= m0) {                                        // p^T Q, y^T K: tokens from these on
-#pragma unroll
-            for (int p = 0; p < SUM; ++p) {
-                left_km<kPiece>(x[p], s_p + p * (kPiece * kPiece * 2), k0, m0, lane);
-                left_km<kPiece>(y[p], s_y + p * (kPiece * kPiece * 2), k0, m0, lane);
-            }
-#pragma unroll
-            for (int n = 0; n < NT; n += 2) {
-#pragma unroll
-                for (int p = 0; p < IN; ++p) {
-                    right_kn<KD>(r, qs + p * (kPiece * KD * 2), k0, side * HALF + n * 8, lane);
-                    mma_parts<SUM>(C[n], C[n + 1], x, r, p);
-                    right_kn<KD>(r, ks + p * (kPiece * KD * 2), k0, side * HALF + n * 8, lane);
-                    mma_parts<SUM>(C[n], C[n + 1], y, r, p);
-                }
-            }
-        }
-    }
-    float dot[2] = {0.f, 0.f};
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int col = side * HALF + n * 8 + c;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int row = m0 + g + 8 * half;
-            const float2 k = number(ks, row, col), q = number(qs, row, col);
-            dot[half] = fmaf(q.x, Q[n][2 * half], fmaf(q.y, Q[n][2 * half + 1], dot[half]));
-            dot[half] = fmaf(k.x, A[n][2 * half] - C[n][2 * half], fmaf(k.y, A[n][2 * half + 1] - C[n][2 * half + 1], dot[half]));
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                if (row < live && col + e < a.K) put(row, col + e, Q[n][2 * half + e], A[n][2 * half + e] + C[n][2 * half + e]);
-        }
-    }
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        dot[half] += __shfl_xor_sync(0xffffffffu, dot[half], 1);
-        dot[half] += __shfl_xor_sync(0xffffffffu, dot[half], 2);
-        if (c == 0) dots[side][m0 + g + 8 * half] = dot[half];
-    }
-    __syncthreads();
-    if (warp == 0) {                                           // sums from the last token back, two tokens a lane
-        float last = 0.f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) last += sums[w];
-        const float x1 = dots[0][63 - 2 * lane] + dots[1][63 - 2 * lane], x0 = dots[0][62 - 2 * lane] + dots[1][62 - 2 * lane];
-        float s = x0 + x1;
-        for (int d = 1; d < 32; d *= 2) {
-            const float y = __shfl_up_sync(0xffffffffu, s, d);
-            if (lane >= d) s += y;
-        }
-        const int row = 62 - 2 * lane;
-        if (row < live) a.dg[(row0 + row) * a.lddg + h] = s + last;
-        if (row + 1 < live) a.dg[(row0 + row + 1) * a.lddg + h] = (s - x0) + last;
-    } else if (warp < 4 && warp >= 2) {
-        const int row = (warp - 2) * 32 + lane, tiles = a.VP / 16;
-        const float* from = a.dbeta_parts + unit * tiles * kPiece + row;
-        float s = 0.f;
-        for (int i = 0; i < tiles; ++i) s += from[i * kPiece];
-        if (row < live) a.dbeta[(row0 + row) * a.lddbeta + h] = s;
+    if (warp == kWorkers / 32) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, W::cols);
+        if (lane == 0 && *abort_flag) atomicExch(a.timeout, 1u);
     }
 }
 
@@ -496,38 +437,52 @@ __global__ void __launch_bounds__(256) delta_bwd_shared_kernel(const DeltaArgs a
     }
 }
 
-template <typename T, int KD>
-conv2d_status_t backward(const DeltaArgs& a, cudaStream_t stream)
+template <typename T, int KD, int NV>
+conv2d_status_t backward_walk(const DeltaArgs& a, cudaStream_t stream)
 {
-    using W = Walk<T, KD>;
-    static SmemLimit limit, limit_pieces;
-    const int warps = delta_warps(a), across = (int)ceil_div_u(a.VP / 16, warps);
-    const size_t smem = W::smem(warps);
-    if (raise_smem_limit((const void*)delta_bwd_walk_kernel<T, KD>, smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-    if (raise_smem_limit((const void*)delta_bwd_pieces_kernel<T, KD>, Piecewise<T, KD>::smem, limit_pieces) != cudaSuccess) return CONV2D_ERR_CUDA;
+    using W = Walk<T, KD, NV>;
+    static SmemLimit limit;
+    const int across = (int)ceil_div_u(a.V, NV);
+    if (raise_smem_limit((const void*)delta_bwd_walk_kernel<T, KD, NV>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
     const int per = 16 / (int)sizeof(T);
     const bool wide_do = a.V % per == 0 && rows_aligned(a.dout, a.lddo, sizeof(T), 16), wide_dv = a.V % per == 0 && rows_aligned(a.dv, a.lddv, sizeof(T), 16);
-    if (launch_pdl(delta_bwd_walk_kernel<T, KD>, dim3((unsigned)(a.B * a.H) * across), dim3((warps + kLoaders) * 32), smem, stream, a, warps, across, wide_do,
-                   wide_dv) != cudaSuccess)
+    if (launch_pdl(delta_bwd_walk_kernel<T, KD, NV>, dim3((unsigned)(a.B * a.H) * across), dim3(kWalkThreads), W::smem, stream, a, across, wide_do, wide_dv) !=
+        cudaSuccess)
         return CONV2D_ERR_CUDA;
     count_launch();
-    if (launch_pdl(delta_bwd_pieces_kernel<T, KD>, dim3((unsigned)(a.B * a.H) * (unsigned)a.pieces), dim3(256), Piecewise<T, KD>::smem, stream, a) != cudaSuccess)
+    return CONV2D_OK;
+}
+
+template <typename T, int KD>
+conv2d_status_t backward_pieces(const DeltaArgs& a, cudaStream_t stream)
+{
+    using W = Piecewise<T, KD>;
+    static SmemLimit limit;
+    if (raise_smem_limit((const void*)delta_bwd_pieces_kernel<T, KD>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+    const int per = 16 / (int)sizeof(T);
+    const bool wide_do = a.V % per == 0 && rows_aligned(a.dout, a.lddo, sizeof(T), 16), wide_dq = a.K % per == 0 && rows_aligned(a.dq, a.lddq, sizeof(T), 16),
+               wide_dk = a.K % per == 0 && rows_aligned(a.dk, a.lddk, sizeof(T), 16);
+    if (launch_pdl(delta_bwd_pieces_kernel<T, KD>, dim3((unsigned)(a.B * a.H) * (unsigned)a.pieces), dim3(kWalkThreads), W::smem, stream, a, wide_do, wide_dq, wide_dk,
+                   a.K % 4 == 0) != cudaSuccess)
         return CONV2D_ERR_CUDA;
     count_launch();
-    if (a.share > 1) {
-        const long long blocks = ((long long)a.B * a.L * a.Hk * a.K + 255) / 256, most = 16LL * sm_count();
-        if (launch_pdl(delta_bwd_shared_kernel<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
-        count_launch();
-    }
     return CONV2D_OK;
 }
 
 template <typename T>
 conv2d_status_t backward_typed(const DeltaArgs& a, cudaStream_t stream)
 {
-    if (a.K <= 32) return backward<T, 32>(a, stream);
-    if (a.K <= 64) return backward<T, 64>(a, stream);
-    return backward<T, 128>(a, stream);
+    const bool narrow = delta_columns<T>(a) == 32;
+    conv2d_status_t st;
+    if (a.K <= 64) st = narrow ? backward_walk<T, 64, 32>(a, stream) : backward_walk<T, 64, 64>(a, stream);
+    else if constexpr (sizeof(T) == 4) st = backward_walk<T, 128, 32>(a, stream);
+    else st = narrow ? backward_walk<T, 128, 32>(a, stream) : backward_walk<T, 128, 64>(a, stream);
+    if (st == CONV2D_OK) st = a.K <= 64 ? backward_pieces<T, 64>(a, stream) : backward_pieces<T, 128>(a, stream);
+    if (st != CONV2D_OK || a.share == 1) return st;
+    const long long blocks = ((long long)a.B * a.L * a.Hk * a.K + 255) / 256, most = 16LL * sm_count();
+    if (launch_pdl(delta_bwd_shared_kernel<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;
+    count_launch();
+    return CONV2D_OK;
 }
 
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
@@ -542,23 +497,20 @@ conv2d_status_t launch_delta_bwd(DeltaArgs a, conv2d_operand_t type, const void*
 {
     const DeltaLayout l(a.B, a.L, a.Hk, a.H, a.K, a.V, type);
     a.share = a.H / a.Hk, a.pieces = l.pieces, a.VP = l.VP;
+    if (device_timeout_word(&a.timeout) != cudaSuccess) return CONV2D_ERR_CUDA;
+    a.max_polls = (unsigned)env_int("CONV2D_B200_DELTA_MAX_POLLS", 1 << 22);
     unsigned char* kept = const_cast<unsigned char*>(static_cast<const unsigned char*>(states));      // (only read)
-    a.t = reinterpret_cast<bf16*>(kept), a.p = reinterpret_cast<bf16*>(kept + l.units * l.square());
-    a.factors = reinterpret_cast<float*>(kept + l.units * 2 * l.square());
-    a.states = reinterpret_cast<bf16*>(kept + l.prepared_bytes());
-    a.updates = reinterpret_cast<bf16*>(kept + l.prepared_bytes() + l.units * l.state_plane());
+    a.squares = kept, a.factors = reinterpret_cast<float*>(kept + l.units * kSquares);
+    a.states = reinterpret_cast<float*>(kept + l.prepared_bytes());
+    a.updates = reinterpret_cast<float*>(kept + l.prepared_bytes() + l.units * l.state());
     unsigned char* at = static_cast<unsigned char*>(workspace);
-    a.dstates = reinterpret_cast<bf16*>(at), at += l.units * l.state_plane();
-    a.dupdates = reinterpret_cast<bf16*>(at), at += l.units * l.update_plane();
-    const bool direct = delta_direct(a, type, l.KD);
-    if (!direct) a.planes = reinterpret_cast<bf16*>(at);
-    at += l.keys_bytes();
+    a.dstates = reinterpret_cast<float*>(at), at += l.units * l.state();
+    a.dupdates = reinterpret_cast<float*>(at), at += l.units * l.update();
+    a.keys = at, at += l.keys_bytes();
     a.dbeta_parts = reinterpret_cast<float*>(at), at += dbeta_bytes(l);
     if (a.share > 1) a.dq_parts = reinterpret_cast<float*>(at), a.dk_parts = reinterpret_cast<float*>(at + shared_bytes(l));
-    if (!direct) {
-        const conv2d_status_t st = launch_delta_prepare(a, type, false, stream);
-        if (st != CONV2D_OK) return st;
-    }
+    const conv2d_status_t st = launch_delta_prepare(a, type, false, stream);
+    if (st != CONV2D_OK) return st;
     if (type == CONV2D_OPERAND_BF16) return backward_typed<bf16>(a, stream);
     if (type == CONV2D_OPERAND_FP16) return backward_typed<fp16>(a, stream);
     return backward_typed<float>(a, stream);

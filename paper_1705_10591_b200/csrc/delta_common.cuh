@@ -1,13 +1,11 @@
 // What the kernels of the gated delta rule share: pieces of 64 tokens, numbers as sums of bf16 parts, matrix products of those, layouts.
 //
 // A head's state S (K x V) runs through pieces of 64 tokens.  Within one, with G_i the sum of the log decays up to token i, S the state before it,
-//   A_ij = e^(G_i - G_j) k_i.k_j (j < i),   P_ij = e^(G_i - G_j) q_i.k_j (j <= i),   t = (1 + A diag(beta))^-1 A   (strictly lower),
-//   R = V - diag(e^G) K S,   E = R - t diag(beta) R,   O = scale (diag(e^G) Q S + P diag(beta) E),
+//   A_ij = e^(G_i - G_j) k_i.k_j (j < i),   P_ij = e^(G_i - G_j) q_i.k_j (j <= i),   t = (1 + A diag(beta))^-1 A   (strictly lower),   P' = P (1 - diag(beta) t),
+//   R = V - diag(e^G) K S,   E = R - t diag(beta) R,   O = scale (diag(e^G) Q S + P' diag(beta) R),
 //   S <- e^(G_63) S + K^T diag(e^(G_63 - G) beta) E.
-// t holds neither the identity nor betas: both stay in fp32, and the backward pass uses the same t (beta may be zero).
-// Every warp of the kernels that walk the pieces owns 16 columns of V for all of K and computes transposed, S^T [16][K] in the accumulators of its
-// MMAs: accumulators have the layout of the next product's left operand, so R, E and S go from product to product in registers, and warps
-// only share what comes from memory (K, Q, t, P).
+// t and P' hold neither the identity nor the betas to their right: both stay in fp32, and the backward pass uses the same two (beta may be zero).
+// A piece is three products of 128 rows:  [K; Q] S,  [-t; P'] (beta R),  K^T (e^(G_63 - G) beta E).
 #pragma once
 
 #include "seq_common.cuh"
@@ -19,13 +17,15 @@ constexpr int kPiece = 64;
 constexpr int kFactors = 5;                                     // of a piece: e^G, e^(G_63 - G), beta, G in two floats
 constexpr int kMost = 128;                                      // numbers of a key
 
-// Numbers of bf16 that hold a tensor's element, and of those that hold sums and states: 16 bits with two (a rounding of 2^-8, of the rest of it again).
+// Numbers of bf16 that hold a tensor's element (exactly, but for the last bits of an fp32 number), and kSum of those that hold sums and states as
+// operands: 24 bits (a rounding of 2^-8, of the rest of it again, and again).  Two would be 16 bits: half the products of two sums, but results in fp32 (states,
+// gradients of gates) were off by 3e-6 to 9e-6 then, by less than 1e-6 so.
 template <typename T> struct Parts;
-template <> struct Parts<bf16> { static constexpr int in = 1, sum = 2, out = 1; };   // out: of what only goes to outputs of 8 bits
-template <> struct Parts<fp16> { static constexpr int in = 2, sum = 2, out = 2; };
-template <> struct Parts<float> { static constexpr int in = 3, sum = 3, out = 3; };
+template <> struct Parts<bf16> { static constexpr int in = 1; };
+template <> struct Parts<fp16> { static constexpr int in = 2; };
+template <> struct Parts<float> { static constexpr int in = 3; };
+constexpr int kSum = 3;
 inline int parts_in(conv2d_operand_t t) { return t == CONV2D_OPERAND_BF16 ? 1 : t == CONV2D_OPERAND_FP16 ? 2 : 3; }
-inline int parts_sum(conv2d_operand_t t) { return t == CONV2D_OPERAND_FP32 ? 3 : 2; }
 
 // a, b as N parts each, the two of a part side by side.
 template <int N>
@@ -56,8 +56,8 @@ __device__ __forceinline__ void ldsm_t(uint32_t (&r)[4], uint32_t at)
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at));
 }
 
-// A tile of rows of W bf16 numbers in shared memory, its 16-byte units spread over the banks: unit u of row r lies at u ^ (r & 7), of the four of a
-// row of 32 at u ^ (r / 2 & 3), so that eight rows' units of one number meet in no bank.
+// A tile of rows of W = 64 or 32 bf16 numbers, its 16-byte units spread over the banks as the tensor core's 128- and 64-byte swizzles have them: unit u of row r
+// lies at u ^ (r & 7), of the four of a row of 32 at u ^ (r / 2 & 3), so that eight rows' units of one number meet in no bank.
 template <int W>
 __device__ __forceinline__ uint32_t unit_at(uint32_t base, int row, int unit)
 {
@@ -118,22 +118,22 @@ __device__ __forceinline__ void mma_parts(float (&c0)[4], float (&c1)[4], const 
 }
 
 // Where things lie in what the forward pass leaves (`states`) and in workspaces.  A "unit" is one piece of one head of one sequence, number
-// (b * H + h) * pieces + c.  Sections in this order, sizes in bytes for each unit:
+// (b * H + h) * pieces + c; a "key unit" the same of a key head.  Sections in this order, sizes in bytes for each unit:
+constexpr size_t kSquares = (size_t)kSum * 2 * kPiece * kPiece * 2;      // [-t; P'], [part][128][64], units of 16 bytes swizzled as unit_at does
 struct DeltaLayout {
-    int B, L, Hk, H, K, V, KD, VP, pieces, in, sum;              // KD: K rounded up to 32, 64 or 128; VP: V to 16
+    int B, L, Hk, H, K, V, KD, VP, pieces, in;                   // KD: K rounded up to 64 or 128; VP: V to 16
     size_t units, keys;                                          // pieces of all value heads, of all key heads
     DeltaLayout(int B_, int L_, int Hk_, int H_, int K_, int V_, conv2d_operand_t type)
-        : B(B_), L(L_), Hk(Hk_), H(H_), K(K_), V(V_), KD(K_ <= 32 ? 32 : K_ <= 64 ? 64 : 128), VP((V_ + 15) / 16 * 16), pieces((int)(((long long)L_ + kPiece - 1) / kPiece)),
-          in(parts_in(type)), sum(parts_sum(type)), units((size_t)B_ * H_ * pieces), keys((size_t)B_ * Hk_ * pieces)
+        : B(B_), L(L_), Hk(Hk_), H(H_), K(K_), V(V_), KD(K_ <= 64 ? 64 : 128), VP((V_ + 15) / 16 * 16), pieces((int)(((long long)L_ + kPiece - 1) / kPiece)),
+          in(parts_in(type)), units((size_t)B_ * H_ * pieces), keys((size_t)B_ * Hk_ * pieces)
     {
     }
-    size_t square() const { return (size_t)sum * kPiece * kPiece * 2; }              // t, or P
-    size_t prepared_bytes() const { return units * (2 * square() + kFactors * kPiece * 4); }
-    size_t state_plane() const { return (size_t)sum * VP * KD * 2; }                 // S or its gradient, [part][V][K]
-    size_t update_plane() const { return (size_t)sum * VP * kPiece * 2; }            // E or dV, [part][V][token]
-    size_t saved_bytes() const { return units * (state_plane() + update_plane()); }
-    size_t key_plane() const { return (size_t)in * kPiece * KD * 2; }                // K, or Q, [part][token][K]
-    size_t keys_bytes() const { return keys * 2 * key_plane(); }
+    size_t prepared_bytes() const { return units * (kSquares + kFactors * kPiece * 4); }
+    size_t state() const { return (size_t)KD * VP * 4; }                             // S or its gradient, [K][V]
+    size_t update() const { return (size_t)kPiece * VP * 4; }                        // E or dV, [token][V]
+    size_t saved_bytes() const { return units * (state() + update()); }
+    size_t key_tile() const { return (size_t)in * 2 * kPiece * KD * 2; }             // [K; Q], [part][64 numbers][128][64], swizzled likewise
+    size_t keys_bytes() const { return keys * key_tile(); }
 };
 
 // What the kernels read and write; the typed pointers of T are cast by them.
@@ -146,13 +146,13 @@ struct DeltaArgs {
     int B, L, Hk, H, K, V, share, pieces, VP;
     long long ldq, ldk, ldv, ldg, ldbeta, ldo, lddo, lddq, lddk, lddv, lddg, lddbeta;
     float scale;
-    bf16 *t, *p;                  // [unit][part][64][64]
+    unsigned char *squares, *keys;    // tiles of units and of key units
     float* factors;               // [unit][kFactors][64]
-    bf16* planes;                 // [key unit][K, Q][part][64][KD]; NULL: the tensors themselves serve (bf16, K = KD, rows on 16 bytes)
-    bf16 *states, *updates;       // saved by the forward pass: [unit][part][VP][KD], [unit][part][VP][64]; NULL: not wanted
-    bf16 *dstates, *dupdates;     // the same of their gradients (dS after the piece, dV)
+    float *states, *updates;      // saved by the forward pass: [unit][KD][VP], [unit][64][VP]; NULL: not wanted
+    float *dstates, *dupdates;    // the same of their gradients (dS after the piece, dV)
     float* dbeta_parts;           // [unit][VP / 16][64]
     float *dq_parts, *dk_parts;   // [B*L][H*K] fp32: gradients of heads that share a key, before they are summed
+    unsigned *timeout, max_polls; // raised when a wait within a kernel runs out
 };
 
 // Pieces in flight are counted in 31 bits.
@@ -170,68 +170,4 @@ conv2d_status_t launch_delta_prepare(const DeltaArgs& a, conv2d_operand_t type, 
 size_t delta_states_bytes(const DeltaLayout& l);
 size_t delta_fwd_workspace_bytes(const DeltaLayout& l);
 size_t delta_bwd_workspace_bytes(const DeltaLayout& l);
-// Whether K and Q can be copied as they lie.
-inline bool delta_direct(const DeltaArgs& a, conv2d_operand_t type, int KD)
-{
-    return type == CONV2D_OPERAND_BF16 && a.K == KD && rows_aligned(a.q, a.ldq, 2, 16) && rows_aligned(a.k, a.ldk, 2, 16);
-}
-
-#ifdef __CUDACC__
-// Copies of K or Q (which = 0, 1) of a piece into a swizzled tile [part][64][KD], by `threads` threads of which this is number `id`; rows from `live` on
-// are zeros.  Complete after the caller's wait for its copies.
-template <int KD, int IN>
-__device__ __forceinline__ void copy_keys(const DeltaArgs& a, uint32_t to, int which, int b, int hk, int piece, int live, int id, int threads)
-{
-    constexpr int UNITS = KD / 8;
-    const char* from;
-    long long row_bytes;
-    if (a.planes) {
-        from = reinterpret_cast<const char*>(a.planes) + ((((size_t)b * a.Hk + hk) * a.pieces + piece) * 2 + which) * ((size_t)IN * kPiece * KD * 2);
-        row_bytes = KD * 2;
-    } else {
-        const long long ld = which ? a.ldq : a.ldk;
-        from = static_cast<const char*>(which ? a.q : a.k) + (((long long)b * a.L + (long long)piece * kPiece) * ld + (long long)hk * KD) * 2;
-        row_bytes = ld * 2;
-    }
-    for (int i = id; i < IN * kPiece * UNITS; i += threads) {
-        const int row = i / UNITS, unit = i % UNITS, token = row % kPiece;
-        const bool real = token < live;
-        const char* src = real ? from + row * row_bytes + unit * 16 : from;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(unit_at<KD>(to, row, unit)), "l"(src), "r"(real ? 16 : 0) : "memory");
-    }
-}
-// Copies of `rows` dense rows of W bf16 numbers, those from `live` on as zeros.
-template <int W>
-__device__ __forceinline__ void copy_rows(const bf16* from, uint32_t to, int rows, int live, int id, int threads)
-{
-    constexpr int UNITS = W / 8;
-    for (int i = id; i < rows * UNITS; i += threads) {
-        const int row = i / UNITS, unit = i % UNITS;
-        const bool real = row < live;
-        const bf16* src = real ? from + (size_t)row * W + unit * 8 : from;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(unit_at<W>(to, row, unit)), "l"(src), "r"(real ? 16 : 0) : "memory");
-    }
-}
-// A tile of tokens x columns of a tensor, as it lies, rows `pitch` elements apart in shared memory; zeros beyond `live` tokens and `cols` columns.  By copies of
-// 16 bytes where the rows allow it.
-template <typename T>
-__device__ __forceinline__ void copy_values(const T* from, long long ld, T* to, int pitch, int width, int live, int cols, bool wide, int id, int threads)
-{
-    constexpr int PER = 16 / (int)sizeof(T);
-    if (wide) {                   // cols and width are multiples of PER then
-        const int units = width / PER;
-        for (int i = id; i < kPiece * units; i += threads) {
-            const int row = i / units, c = i % units * PER;
-            const bool real = row < live && c < cols;
-            copy_async<16>(to + row * pitch + c, real ? from + row * ld + c : from, real);
-        }
-    } else {
-        for (int i = id; i < kPiece * width; i += threads) {
-            const int row = i / width, c = i % width;
-            to[row * pitch + c] = row < live && c < cols ? from[row * ld + c] : from_float<T>(0.f);
-        }
-    }
-}
-#endif
-
 }  // namespace conv2d_b200

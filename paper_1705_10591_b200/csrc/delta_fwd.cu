@@ -1,206 +1,199 @@
-// Gated delta rule, forward: a block walks the pieces of one head of one sequence for up to 64 columns of V.
+// Gated delta rule, forward.
 #include "delta_walk.cuh"
 
 namespace conv2d_b200 {
 namespace {
 
-template <typename T, int KD>
-__global__ void __launch_bounds__((kComputing + kLoaders) * 32, 1) delta_fwd_kernel(const DeltaArgs a, int warps, int across, bool wide_v, bool wide_o)
+template <typename T, int KD, int NV>
+__global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaArgs a, int across, bool wide_v, bool wide_o)
 {
-    using W = Walk<T, KD>;
-    constexpr int IN = Parts<T>::in, SUM = Parts<T>::sum, OUT = Parts<T>::out, STAGES = W::stages;
-    extern __shared__ __align__(1024) unsigned char raw[];
-    ptx::grid_dep_wait();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = 2 * (lane & 3);
-    const int v0 = (int)(blockIdx.x % across) * warps * 16, bh = blockIdx.x / across, h = bh % a.H, b = bh / a.H;
-    const int len = sequence_length(a.lengths, b, a.L), pieces = (len + kPiece - 1) / kPiece;
-    const bool computes = warp < warps;
-    const int v = v0 + warp * 16;                              // this warp's first column
-    const T* values = static_cast<const T*>(a.v);
-    const int cols = min(warps * 16, a.V - v0);
-    auto stage = [&](int i) { return Stage<T, KD>{raw + (STAGES == 2 ? (i & 1) * W::stage(warps) : 0), warps}; };
-    auto load = [&](int i, int id, int threads) {
-        load_piece<T, KD>(a, stage(i), values, a.ldv, wide_v, b, h, i, len - i * kPiece, v0, id, threads);
-        copies_commit();
-    };
-
-    float S[KD / 8][4];                                        // S^T: rows g and g + 8 of the warp's columns, K in pairs
-    const size_t state0 = ((size_t)b * a.H + h) * a.K * a.V;
-#pragma unroll
-    for (int n = 0; n < KD / 8; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int k = n * 8 + c + (e & 1), col = v + g + 8 * (e >> 1);
-            S[n][e] = a.state_in && computes && k < a.K && col < a.V ? a.state_in[state0 + (size_t)k * a.V + col] : 0.f;
-        }
-
-    if (pieces > 0 && STAGES == 2) {
-        load(0, tid, blockDim.x);
-        copies_wait<0>();
+    using W = Walk<T, KD, NV>;
+    constexpr int IN = W::IN, C = W::C, STAGES = W::stages;
+    extern __shared__ unsigned char unaligned[];
+    unsigned char* raw = unaligned + ((1024 - (ptx::smem_u32(unaligned) & 1023)) & 1023);
+    unsigned char *squares = raw + STAGES * W::keys, *state = squares + W::squares, *rows = state + W::state;
+    WalkBars* bars = reinterpret_cast<WalkBars*>(rows + kSum * W::rows_part);
+    volatile uint32_t* abort_flag = &bars->abort;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int v0 = (int)(blockIdx.x % across) * NV, bh = blockIdx.x / across, h = bh % a.H, b = bh / a.H, hk = h / a.share;
+    if (tid == 0) {
+        bars->abort = 0;
+        ptx::mbar_init(&bars->keys[0], 1), ptx::mbar_init(&bars->keys[1], 1), ptx::mbar_init(&bars->squares, 1);
+        for (int i = 0; i < 3; ++i) ptx::mbar_init(&bars->done[i], 1);
+        ptx::fence_mbar_init();
     }
+    if (warp == kWorkers / 32) {
+        ptx::tmem_alloc(&bars->tmem, W::cols);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before_sync();
     __syncthreads();
-    for (int i = 0; i < pieces; ++i) {
-        if (STAGES == 1) {
-            load(i, tid, blockDim.x);
-            copies_wait<0>();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = bars->tmem;
+    ptx::grid_dep_wait();
+    const int len = sequence_length(a.lengths, b, a.L), pieces = (len + kPiece - 1) / kPiece;
+    const size_t unit0 = (size_t)bh * a.pieces;
+
+    if (warp == kWorkers / 32) {
+        const uint32_t elected = ptx::elect_one();
+        const unsigned char* key_tiles = a.keys + ((size_t)b * a.Hk + hk) * a.pieces * W::keys;
+        auto load_keys = [&](int i) {
+            if (!elected || i >= pieces) return;
+            uint64_t* bar = &bars->keys[STAGES == 2 ? i & 1 : 0];
+            ptx::mbar_arrive_expect_tx(bar, W::keys);
+            ptx::bulk_g2s(raw + (STAGES == 2 ? i & 1 : 0) * W::keys, key_tiles + (size_t)i * W::keys, W::keys, bar);
+        };
+        auto load_squares = [&](int i) {
+            if (!elected || i >= pieces) return;
+            ptx::mbar_arrive_expect_tx(&bars->squares, W::squares);
+            ptx::bulk_g2s(squares, a.squares + (unit0 + i) * kSquares, W::squares, &bars->squares);
+        };
+        const uint32_t s_squares = ptx::smem_u32(squares), s_state = ptx::smem_u32(state), s_rows = ptx::smem_u32(rows);
+        constexpr uint32_t id1 = ptx::idesc_b16(128, NV, false) | ptx::kIdescBMajorMN, id3 = id1 | kIdescAMajorM;
+        load_keys(0), load_squares(0);
+        if (STAGES == 2) load_keys(1);
+        bool alive = true;
+        for (int i = 0; i < pieces; ++i) {
+            const uint32_t keys = ptx::smem_u32(raw) + (STAGES == 2 ? i & 1 : 0) * W::keys;
+            alive = alive && ptx::mbar_wait_bounded_warp(&bars->keys[STAGES == 2 ? i & 1 : 0], (STAGES == 2 ? i >> 1 : i) & 1, abort_flag, a.max_polls);
+            __syncthreads();                                   // S is there
+            ptx::tc_fence_after_sync();
+            if (alive) {
+                multiply(tmem, IN, kSum, KD / 16, id1, elected, false,
+                         [&](int p, int k) { return rows_as_m(keys + p * W::key_part + (k >> 2) * W::HALF + (k & 3) * 32); },
+                         [&](int p, int k) { return rows_as_k<NV>(s_state + p * W::state_part + k * 16 * NV * 2); });
+                ptx::mma_commit(&bars->done[0], elected);
+                // (everything of the piece before is done with)
+                if (STAGES == 2 && i > 0) load_keys(i + 1);
+            }
+            alive = alive && ptx::mbar_wait_bounded_warp(&bars->squares, i & 1, abort_flag, a.max_polls);
+            __syncthreads();                                   // beta R is there
+            ptx::tc_fence_after_sync();
+            if (alive) {
+                multiply(tmem + NV, kSum, kSum, kPiece / 16, id1, elected, false, [&](int p, int k) { return rows_as_m(s_squares + p * W::square_part + k * 32); },
+                         [&](int p, int k) { return rows_as_k<NV>(s_rows + p * W::rows_part + k * 16 * NV * 2); });
+                ptx::mma_commit(&bars->done[1], elected);
+            }
+            __syncthreads();                                   // what updates S is there, in the place of beta R
+            ptx::tc_fence_after_sync();
+            if (alive) {
+                multiply(tmem + 2 * NV, IN, kSum, kPiece / 16, id3, elected, false, [&](int p, int k) { return columns_as_m(keys + p * W::key_part + k * 16 * 128, W::HALF); },
+                         [&](int p, int k) { return rows_as_k<NV>(s_rows + p * W::rows_part + k * 16 * NV * 2); });
+                ptx::mma_commit(&bars->done[2], elected);
+                load_squares(i + 1);
+                if (STAGES == 1) {
+                    alive = ptx::mbar_wait_bounded_warp(&bars->done[2], i & 1, abort_flag, a.max_polls);
+                    if (alive) load_keys(i + 1);
+                }
+            }
+        }
+    } else {
+        const int quarter = warp & 3, row = quarter * 32 + lane, col0 = (warp >> 2) * C, token = row & (kPiece - 1), v = v0 + col0;
+        const bool is_key = row < kPiece;                      // a token of K, or of Q; and row `row` of S
+        const uint32_t at = tmem + ((uint32_t)quarter << 21) + col0;
+        const int there = a.V - v, saved = a.VP - v;           // columns of this thread that there are
+        float S[C], X[C];
+        const size_t state0 = ((size_t)bh * a.K + row) * a.V + v;
+#pragma unroll
+        for (int j = 0; j < C; ++j) S[j] = a.state_in && row < a.K && j < there ? a.state_in[state0 + j] : 0.f;
+        const T* values = static_cast<const T*>(a.v) + ((long long)b * a.L + token) * a.ldv + (long long)h * a.V + v;
+        T* out = static_cast<T*>(a.o) + ((long long)b * a.L + token) * a.ldo + (long long)h * a.V + v;
+        const float* factors = a.factors + unit0 * (kFactors * kPiece);
+        float next[C], eg = 0.f, ed = 0.f, beta = 0.f, whole = 0.f;
+        auto fetch = [&](int i) {                              // this token's value (of keys) and factors
+            if (i >= pieces) return;
+            const float* f = factors + (size_t)i * (kFactors * kPiece);
+            eg = f[token], ed = f[kPiece + token], beta = f[2 * kPiece + token], whole = f[kPiece - 1];
+            if (is_key) load_row<T, C>(values + (long long)i * kPiece * a.ldv, i * kPiece + token < len ? there : 0, wide_v, next);
+        };
+        auto put_state = [&](int i) {                          // S before piece i, for its product and for the backward pass
+            if (row < KD) {
+                put_row<NV, C>(state, W::state_part, row, col0, S);
+                if (a.states) save_row<C>(a.states + ((unit0 + i) * KD + row) * a.VP + v, saved, S);
+            }
+            ptx::fence_proxy_async_smem();
+        };
+        if (pieces > 0) put_state(0);
+        fetch(0);
+        for (int i = 0; i < pieces; ++i) {
+            const uint32_t parity = i & 1;
+            ptx::tc_fence_before_sync();
             __syncthreads();
-        } else if (!computes) {
-            if (i + 1 < pieces) load(i + 1, tid - warps * 32, blockDim.x - warps * 32);
-            copies_wait<0>();
+            // D1: of keys R = v - e^G k S, of queries e^G q S
+            ptx::mbar_wait_bounded(&bars->done[0], parity, abort_flag, a.max_polls);
+            ptx::tc_fence_after_sync();
+            tmem_row<C>(at, X);
+            if (is_key) {
+                float y[C];
+#pragma unroll
+                for (int j = 0; j < C; ++j) X[j] = fmaf(-eg, X[j], next[j]), y[j] = beta * X[j];
+                put_row<NV, C>(rows, W::rows_part, row, col0, y);
+                ptx::fence_proxy_async_smem();
+            } else {
+#pragma unroll
+                for (int j = 0; j < C; ++j) X[j] *= eg;
+            }
+            ptx::tc_fence_before_sync();
+            __syncthreads();
+            // D2: of keys E - R, of queries P' beta R
+            ptx::mbar_wait_bounded(&bars->done[1], parity, abort_flag, a.max_polls);
+            ptx::tc_fence_after_sync();
+            float y[C];
+            tmem_row<C>(at + NV, y);
+#pragma unroll
+            for (int j = 0; j < C; ++j) X[j] += y[j];
+            if (is_key) {
+                const float d = ed * beta;
+#pragma unroll
+                for (int j = 0; j < C; ++j) y[j] = d * X[j];
+                put_row<NV, C>(rows, W::rows_part, row, col0, y);
+                ptx::fence_proxy_async_smem();
+            }
+            ptx::tc_fence_before_sync();
+            __syncthreads();
+            if (is_key) {
+                if (a.updates) save_row<C>(a.updates + ((unit0 + i) * kPiece + token) * a.VP + v, saved, X);
+            } else if (i * kPiece + token < len) {
+#pragma unroll
+                for (int j = 0; j < C; ++j) X[j] *= a.scale;
+                store_row<T, C>(out + (long long)i * kPiece * a.ldo, there, wide_o, X);
+            }
+            const float keep = whole;
+            fetch(i + 1);
+            // D3: S <- e^G_63 S + K^T (..)
+            ptx::mbar_wait_bounded(&bars->done[2], parity, abort_flag, a.max_polls);
+            ptx::tc_fence_after_sync();
+            tmem_row<C>(at + 2 * NV, y);
+#pragma unroll
+            for (int j = 0; j < C; ++j) S[j] = fmaf(keep, S[j], y[j]);
+            if (i + 1 < pieces) put_state(i + 1);
         }
-        if (computes && v < a.V) {
-            const Stage<T, KD> s = stage(i);
-            const float* f = s.factors();
-            const size_t unit = ((size_t)b * a.H + h) * a.pieces + i;
-            float R[8][4] = {}, O[8][4] = {};
-            // S^T K^T and S^T Q^T
+        if (a.state_out && row < a.K) {
 #pragma unroll
-            for (int n = 0; n < KD / 8; n += 2) {
-                uint32_t x[SUM][4];
-                left_of<SUM>(x, S[n], S[n + 1]);
-                if (a.states) {
-                    bf16* to = a.states + (unit * SUM * a.VP + v + g) * KD + n * 8 + c;
-#pragma unroll
-                    for (int p = 0; p < SUM; ++p, to += (size_t)a.VP * KD) {
-                        *reinterpret_cast<uint32_t*>(to) = x[p][0], *reinterpret_cast<uint32_t*>(to + 8 * KD) = x[p][1];
-                        *reinterpret_cast<uint32_t*>(to + 8) = x[p][2], *reinterpret_cast<uint32_t*>(to + 8 * KD + 8) = x[p][3];
-                    }
-                }
-#pragma unroll
-                for (int m = 0; m < 8; m += 2) {
-#pragma unroll
-                    for (int p = 0; p < IN; ++p) {
-                        uint32_t r[4];
-                        right_nk<KD>(r, s.k() + p * (kPiece * KD * 2), m * 8, n * 8, lane);
-                        mma_parts<SUM>(R[m], R[m + 1], x, r, p);
-                        right_nk<KD>(r, s.q() + p * (kPiece * KD * 2), m * 8, n * 8, lane);
-#pragma unroll
-                        for (int j = 0; j < OUT; ++j)
-                            if (j + p < OUT) mma(O[m], x[j], r[0], r[1]), mma(O[m + 1], x[j], r[2], r[3]);
-                    }
-                }
-            }
-            // R = v - e^G S^T k, of this warp's columns; E = R - t (beta R)
-            const T* vs = s.values() + warp * 16 + g;
-            float E[8][4];
-#pragma unroll
-            for (int m = 0; m < 8; ++m) {
-                const float2 eg = *reinterpret_cast<const float2*>(f + m * 8 + c);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float d = e & 1 ? eg.y : eg.x;
-                    E[m][e] = fmaf(-d, R[m][e], to_float(vs[(m * 8 + c + (e & 1)) * s.pitch() + 8 * (e >> 1)]));
-                    O[m][e] *= d;
-                }
-            }
-#pragma unroll
-            for (int m = 0; m < 8; ++m) {
-                const float2 be = *reinterpret_cast<const float2*>(f + 2 * kPiece + m * 8 + c);
-                R[m][0] = -be.x * E[m][0], R[m][1] = -be.y * E[m][1], R[m][2] = -be.x * E[m][2], R[m][3] = -be.y * E[m][3];
-            }
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {                   // tokens j * 8 .. + 15 on tokens from there on
-                uint32_t x[SUM][4];
-                left_of<SUM>(x, R[j], R[j + 1]);
-#pragma unroll
-                for (int m = j; m < 8; m += 2) {
-#pragma unroll
-                    for (int p = 0; p < SUM; ++p) {
-                        uint32_t r[4];
-                        right_nk<kPiece>(r, s.t() + p * (kPiece * kPiece * 2), m * 8, j * 8, lane);
-                        mma_parts<SUM>(E[m], E[m + 1], x, r, p);
-                    }
-                }
-            }
-            if (a.updates) {
-#pragma unroll
-                for (int m = 0; m < 8; ++m) {
-                    uint32_t x[SUM], y[SUM];
-                    split<SUM>(E[m][0], E[m][1], x);
-                    split<SUM>(E[m][2], E[m][3], y);
-                    bf16* to = a.updates + (unit * SUM * a.VP + v + g) * kPiece + m * 8 + c;
-#pragma unroll
-                    for (int p = 0; p < SUM; ++p, to += (size_t)a.VP * kPiece)
-                        *reinterpret_cast<uint32_t*>(to) = x[p], *reinterpret_cast<uint32_t*>(to + 8 * kPiece) = y[p];
-                }
-            }
-            // O += P (beta E)
-#pragma unroll
-            for (int m = 0; m < 8; ++m) {
-                const float2 be = *reinterpret_cast<const float2*>(f + 2 * kPiece + m * 8 + c);
-                E[m][0] *= be.x, E[m][1] *= be.y, E[m][2] *= be.x, E[m][3] *= be.y;
-            }
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                uint32_t x[OUT][4];
-                left_of<OUT>(x, E[j], E[j + 1]);
-#pragma unroll
-                for (int m = j; m < 8; m += 2) {
-#pragma unroll
-                    for (int p = 0; p < OUT; ++p) {
-                        uint32_t r[4];
-                        right_nk<kPiece>(r, s.p() + p * (kPiece * kPiece * 2), m * 8, j * 8, lane);
-                        mma_parts<OUT>(O[m], O[m + 1], x, r, p);
-                    }
-                }
-            }
-            // S <- e^G_63 S + (e^(G_63 - G) beta E)^T K
-            const float whole = f[kPiece - 1];
-#pragma unroll
-            for (int n = 0; n < KD / 8; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) S[n][e] *= whole;
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                const float2 d0 = *reinterpret_cast<const float2*>(f + kPiece + j * 8 + c), d1 = *reinterpret_cast<const float2*>(f + kPiece + j * 8 + 8 + c);
-                const float u0[4] = {E[j][0] * d0.x, E[j][1] * d0.y, E[j][2] * d0.x, E[j][3] * d0.y};
-                const float u1[4] = {E[j + 1][0] * d1.x, E[j + 1][1] * d1.y, E[j + 1][2] * d1.x, E[j + 1][3] * d1.y};
-                uint32_t x[SUM][4];
-                left_of<SUM>(x, u0, u1);
-#pragma unroll
-                for (int n = 0; n < KD / 8; n += 2) {
-#pragma unroll
-                    for (int p = 0; p < IN; ++p) {
-                        uint32_t r[4];
-                        right_kn<KD>(r, s.k() + p * (kPiece * KD * 2), j * 8, n * 8, lane);
-                        mma_parts<SUM>(S[n], S[n + 1], x, r, p);
-                    }
-                }
-            }
-#pragma unroll
-            for (int m = 0; m < 8; ++m)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) O[m][e] *= a.scale;
-            T* mine = reinterpret_cast<T*>(raw + STAGES * W::stage(warps)) + warp * kPiece * (16 + W::kPad);
-            store_columns(O, mine, static_cast<T*>(a.o) + ((long long)b * a.L + (long long)i * kPiece) * a.ldo + (long long)h * a.V + v, a.ldo, len - i * kPiece,
-                          a.V - v, wide_o, lane);
+            for (int j = 0; j < C; ++j)
+                if (j < there) a.state_out[state0 + j] = S[j];
         }
-        __syncthreads();
+        zero_rows(static_cast<T*>(a.o) + (long long)b * a.L * a.ldo + (long long)h * a.V + v0, a.ldo, len, a.L, min(NV, a.V - v0), tid, kWorkers);
     }
-    if (a.state_out && computes) {
-#pragma unroll
-        for (int n = 0; n < KD / 8; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int k = n * 8 + c + (e & 1), col = v + g + 8 * (e >> 1);
-                if (k < a.K && col < a.V) a.state_out[state0 + (size_t)k * a.V + col] = S[n][e];
-            }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == kWorkers / 32) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, W::cols);
+        if (lane == 0 && *abort_flag) atomicExch(a.timeout, 1u);
     }
-    zero_rows(static_cast<T*>(a.o) + (long long)b * a.L * a.ldo + (long long)h * a.V + v0, a.ldo, len, a.L, cols, tid, blockDim.x);
 }
 
-template <typename T, int KD>
+template <typename T, int KD, int NV>
 conv2d_status_t walk(const DeltaArgs& a, cudaStream_t stream)
 {
-    using W = Walk<T, KD>;
+    using W = Walk<T, KD, NV>;
     static SmemLimit limit;
-    const int warps = delta_warps(a), across = (int)ceil_div_u(a.VP / 16, warps);
-    const size_t smem = W::smem(warps);
-    if (raise_smem_limit((const void*)delta_fwd_kernel<T, KD>, smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+    const int across = (int)ceil_div_u(a.V, NV);
+    if (raise_smem_limit((const void*)delta_fwd_kernel<T, KD, NV>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
     const int per = 16 / (int)sizeof(T);
     const bool wide_v = a.V % per == 0 && rows_aligned(a.v, a.ldv, sizeof(T), 16), wide_o = a.V % per == 0 && rows_aligned(a.o, a.ldo, sizeof(T), 16);
-    if (launch_pdl(delta_fwd_kernel<T, KD>, dim3((unsigned)(a.B * a.H) * across), dim3((warps + kLoaders) * 32), smem, stream, a, warps, across, wide_v, wide_o) !=
-        cudaSuccess)
+    if (launch_pdl(delta_fwd_kernel<T, KD, NV>, dim3((unsigned)(a.B * a.H) * across), dim3(kWalkThreads), W::smem, stream, a, across, wide_v, wide_o) != cudaSuccess)
         return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;
@@ -209,9 +202,10 @@ conv2d_status_t walk(const DeltaArgs& a, cudaStream_t stream)
 template <typename T>
 conv2d_status_t walk_typed(const DeltaArgs& a, cudaStream_t stream)
 {
-    if (a.K <= 32) return walk<T, 32>(a, stream);
-    if (a.K <= 64) return walk<T, 64>(a, stream);
-    return walk<T, 128>(a, stream);
+    const bool narrow = delta_columns<T>(a) == 32;
+    if (a.K <= 64) return narrow ? walk<T, 64, 32>(a, stream) : walk<T, 64, 64>(a, stream);
+    if constexpr (sizeof(T) == 4) return walk<T, 128, 32>(a, stream);
+    else return narrow ? walk<T, 128, 32>(a, stream) : walk<T, 128, 64>(a, stream);
 }
 
 }  // namespace
@@ -223,15 +217,16 @@ conv2d_status_t launch_delta_fwd(DeltaArgs a, conv2d_operand_t type, void* state
 {
     const DeltaLayout l(a.B, a.L, a.Hk, a.H, a.K, a.V, type);
     a.share = a.H / a.Hk, a.pieces = l.pieces, a.VP = l.VP;
+    if (device_timeout_word(&a.timeout) != cudaSuccess) return CONV2D_ERR_CUDA;
+    a.max_polls = (unsigned)env_int("CONV2D_B200_DELTA_MAX_POLLS", 1 << 22);
     // (sections of whole multiples of 16 bytes)
     unsigned char* at = static_cast<unsigned char*>(states ? states : workspace);
-    a.t = reinterpret_cast<bf16*>(at), a.p = reinterpret_cast<bf16*>(at + l.units * l.square());
-    a.factors = reinterpret_cast<float*>(at + l.units * 2 * l.square());
+    a.squares = at, a.factors = reinterpret_cast<float*>(at + l.units * kSquares);
     if (states) {
-        a.states = reinterpret_cast<bf16*>(at + l.prepared_bytes());
-        a.updates = reinterpret_cast<bf16*>(at + l.prepared_bytes() + l.units * l.state_plane());
+        a.states = reinterpret_cast<float*>(at + l.prepared_bytes());
+        a.updates = reinterpret_cast<float*>(at + l.prepared_bytes() + l.units * l.state());
     }
-    if (!delta_direct(a, type, l.KD)) a.planes = reinterpret_cast<bf16*>(static_cast<unsigned char*>(workspace) + l.prepared_bytes());
+    a.keys = static_cast<unsigned char*>(workspace) + l.prepared_bytes();
     const conv2d_status_t st = launch_delta_prepare(a, type, true, stream);
     if (st != CONV2D_OK) return st;
     if (type == CONV2D_OPERAND_BF16) return walk_typed<bf16>(a, stream);

@@ -1,85 +1,115 @@
-// What the two kernels that walk a sequence's pieces share: warps that compute, warps that load, the stages of shared memory between them.
+// What the two kernels that walk a sequence's pieces share: tensor-core products of tiles in shared memory, the threads' places in them, loads.
+//
+// A block walks one head of one sequence for NV columns of V.  A piece is three tcgen05 products with accumulators of 128 rows in tensor memory, each waiting for
+// what threads make of the one before: with 32 columns a piece is all latency, and registers, not memory, hand S and E on.
+//   D1 [128] = [K; Q] S            rows of K as they lie (K-major), S written by its threads, a row a thread (N-major)
+//   D2 [128] = [-t; P'] (beta R)
+//   D3 [128] = K^T (..)            the tile of K read the other way (M-major)
+// Eight warps own a quarter of the 128 rows and one half of the columns each: a thread has one row of D1 and D2 (a token of K or of Q) and of S (a number of
+// K).  A ninth warp issues the products and the copies of the next piece's tiles.
 #pragma once
 
 #include "delta_common.cuh"
 
 namespace conv2d_b200 {
 
-// Up to four warps of 16 columns compute, four others copy what the next piece needs into the other stage: one barrier of the block for a piece, no
-// waiting in loops.  One stage where two do not fit.
-constexpr int kLoaders = 4, kComputing = 4;
+constexpr int kWorkers = 256, kWalkThreads = kWorkers + 32;
 
-template <typename T, int KD>
+template <typename T, int KD, int NV>
 struct Walk {
-    static constexpr int IN = Parts<T>::in, SUM = Parts<T>::sum;
-    static constexpr size_t keys = (size_t)IN * kPiece * KD * 2, square = (size_t)SUM * kPiece * kPiece * 2;
-    static constexpr int kPad = 16 / (int)sizeof(T);                              // elements between rows of values, against bank conflicts
-    // K, Q, t, P, values of `warps` * 16 columns, factors
-    __host__ __device__ static constexpr size_t values(int warps) { return (size_t)kPiece * (warps * 16 + kPad) * sizeof(T); }
-    __host__ __device__ static constexpr size_t stage(int warps) { return 2 * keys + 2 * square + values(warps) + kFactors * kPiece * 4; }
-    __host__ __device__ static constexpr size_t staging(int warps) { return (size_t)warps * kPiece * (16 + kPad) * sizeof(T); }      // a warp's output rows
-    static constexpr int stages = 2 * stage(kComputing) + staging(kComputing) <= 232448 ? 2 : 1;
-    static size_t smem(int warps) { return stages * stage(warps) + staging(warps); }
+    static constexpr int IN = Parts<T>::in, HALF = 2 * kPiece * 128;              // bytes of 64 numbers of [K; Q]
+    static constexpr int keys = IN * (KD / 64) * HALF, key_part = (KD / 64) * HALF, square_part = 2 * kPiece * 128;
+    static constexpr int state_part = KD * NV * 2, rows_part = 2 * kPiece * NV * 2;      // S, and up to 128 rows of what D2 and D3 are products with
+    static constexpr int squares = (int)kSquares, state = kSum * state_part;
+    static constexpr int rest = squares + state + kSum * rows_part + 1024;        // (1024: barriers)
+    static constexpr int stages = 2 * keys + rest <= 232448 - 1024 ? 2 : 1;
+    static constexpr int smem = stages * keys + rest + 1024;                      // (1024: to the first boundary of the swizzle)
+    static constexpr int cols = NV == 32 ? 128 : 256;                             // of tensor memory: three times NV, a power of two
+    static constexpr int C = NV / 2;                                              // columns of a thread
+    static_assert(smem <= 232448, "a piece does not fit");
 };
 
-// Addresses of a stage.
-template <typename T, int KD>
-struct Stage {
-    unsigned char* at;
-    int warps;
-    __device__ uint32_t k() const { return ptx::smem_u32(at); }
-    __device__ uint32_t q() const { return k() + (uint32_t)Walk<T, KD>::keys; }
-    __device__ uint32_t t() const { return q() + (uint32_t)Walk<T, KD>::keys; }
-    __device__ uint32_t p() const { return t() + (uint32_t)Walk<T, KD>::square; }
-    __device__ T* values() const { return reinterpret_cast<T*>(at + 2 * Walk<T, KD>::keys + 2 * Walk<T, KD>::square); }
-    __device__ float* factors() const { return reinterpret_cast<float*>(at + Walk<T, KD>::stage(warps) - kFactors * kPiece * 4); }
-    __device__ int pitch() const { return warps * 16 + Walk<T, KD>::kPad; }
-};
-
-// Everything of a piece into a stage; by the loading warps, or by all.
-template <typename T, int KD>
-__device__ __forceinline__ void load_piece(const DeltaArgs& a, const Stage<T, KD>& s, const T* values, long long ldvalues, bool wide, int b, int h, int piece, int live,
-                                           int v0, int id, int threads)
+// Descriptors: [K; Q] and [-t; P'] have rows of 128 bytes, atoms of 8 rows.
+__device__ __forceinline__ uint64_t rows_as_m(uint32_t at) { return ptx::smem_desc_sw128(at, 16, 1024); }
+// columns as M, rows as K; `next`: distance to the following 64 columns
+__device__ __forceinline__ uint64_t columns_as_m(uint32_t at, uint32_t next) { return ptx::smem_desc_sw128(at, next, 1024); }
+// rows as K, their NV numbers as N
+template <int NV>
+__device__ __forceinline__ uint64_t rows_as_k(uint32_t at)
 {
-    constexpr int SUM = Parts<T>::sum;
-    const size_t unit = ((size_t)b * a.H + h) * a.pieces + piece;
-    const int hk = h / a.share;
-    copy_keys<KD, Parts<T>::in>(a, s.k(), 0, b, hk, piece, live, id, threads);
-    copy_keys<KD, Parts<T>::in>(a, s.q(), 1, b, hk, piece, live, id, threads);
-    copy_rows<kPiece>(a.t + unit * (SUM * kPiece * kPiece), s.t(), SUM * kPiece, SUM * kPiece, id, threads);
-    copy_rows<kPiece>(a.p + unit * (SUM * kPiece * kPiece), s.p(), SUM * kPiece, SUM * kPiece, id, threads);
-    const float* f = a.factors + unit * (kFactors * kPiece);
-    for (int i = id; i < 3 * kPiece / 4; i += threads) copy_async<16>(s.factors() + 4 * i, f + 4 * i);
-    copy_values(values + ((long long)b * a.L + (long long)piece * kPiece) * ldvalues + (long long)h * a.V + v0, ldvalues, s.values(), s.pitch(), s.warps * 16, live,
-                a.V - v0, wide, id, threads);
+    if (NV == 64) return ptx::smem_desc_sw128(at, 1024, 1024);
+    // 64-byte swizzle: atoms of 8 rows x 64 bytes
+    return (uint64_t)((at >> 4) & 0x3FFFu) | ((uint64_t)(512 >> 4) << 16) | ((uint64_t)(512 >> 4) << 32) | (1ull << 46) | (4ull << 61);
+}
+constexpr uint32_t kIdescAMajorM = 1u << 15;
+
+template <int N> __device__ __forceinline__ void tmem_row(uint32_t at, float (&f)[N])
+{
+    uint32_t v[N];
+    if constexpr (N == 16) ptx::tmem_ld16(at, v);
+    else ptx::tmem_ld32(at, v);
+    ptx::tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = __uint_as_float(v[i]);
 }
 
-// A warp's 16 columns of 64 tokens, transposed in accumulators, out as rows; rows from `live` on are left alone.
-template <typename T>
-__device__ __forceinline__ void store_columns(const float (&x)[8][4], T* mine, T* to, long long ld, int live, int cols, bool wide, int lane)
+// N numbers of row `row` from column `col` on (a multiple of 8), as parts, into a tile of rows of NV.
+template <int NV, int N>
+__device__ __forceinline__ void put_row(unsigned char* tile, int part_bytes, int row, int col, const float (&f)[N])
 {
-    constexpr int PITCH = 16 + 16 / (int)sizeof(T), PER = 16 / (int)sizeof(T);
-    const int g = lane >> 2, c = 2 * (lane & 3);
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
+    for (int u = 0; u < N / 8; ++u) {
+        uint32_t w[4][kSum];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) mine[(n * 8 + c + (e & 1)) * PITCH + g + 8 * (e >> 1)] = from_float<T>(x[n][e]);
+        for (int j = 0; j < 4; ++j) split<kSum>(f[8 * u + 2 * j], f[8 * u + 2 * j + 1], w[j]);
+#pragma unroll
+        for (int p = 0; p < kSum; ++p) *reinterpret_cast<uint4*>(tile + p * part_bytes + unit_at<NV>(0, row, col / 8 + u)) = make_uint4(w[0][p], w[1][p], w[2][p], w[3][p]);
     }
-    __syncwarp();
-    if (wide) {
-        constexpr int UNITS = 16 / PER;
+}
+
+// N elements of a row of a tensor, zeros beyond `there`.
+template <typename T, int N>
+__device__ __forceinline__ void load_row(const T* from, int there, bool wide, float (&f)[N])
+{
+    constexpr int PER = 16 / (int)sizeof(T);
+    if (there >= N && wide) {
 #pragma unroll
-        for (int i = lane; i < kPiece * UNITS; i += 32) {
-            const int row = i / UNITS, u = i % UNITS * PER;
-            if (row < live && u < cols) *reinterpret_cast<uint4*>(to + row * ld + u) = *reinterpret_cast<const uint4*>(mine + row * PITCH + u);
+        for (int i = 0; i < N; i += PER) {
+            float x[PER];
+            unpack(load_pack<T, PER>(from + i), x);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) f[i + j] = x[j];
         }
     } else {
-        for (int i = lane; i < kPiece * 16; i += 32) {
-            const int row = i / 16, u = i % 16;
-            if (row < live && u < cols) to[row * ld + u] = mine[row * PITCH + u];
-        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = i < there ? to_float(from[i]) : 0.f;
     }
-    __syncwarp();
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_row(T* to, int there, bool wide, const float (&f)[N])
+{
+    constexpr int PER = 16 / (int)sizeof(T);
+    if (there >= N && wide) {
+#pragma unroll
+        for (int i = 0; i < N; i += PER) {
+            float x[PER];
+#pragma unroll
+            for (int j = 0; j < PER; ++j) x[j] = f[i + j];
+            store_pack<T, PER>(to + i, pack<T, PER>(x));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < there) to[i] = from_float<T>(f[i]);
+    }
+}
+// The same into rows of fp32 that are whole multiples of 16 columns.
+template <int N>
+__device__ __forceinline__ void save_row(float* to, int there, const float (&f)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+        if (i < there) *reinterpret_cast<float4*>(to + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
 }
 
 // Rows of zeros behind a sequence: columns 0 .. cols - 1 of rows first .. L - 1.
@@ -89,12 +119,40 @@ __device__ __forceinline__ void zero_rows(T* to, long long ld, int first, int L,
     for (long long i = id; i < (long long)(L - first) * cols; i += threads) to[(first + i / cols) * ld + i % cols] = from_float<T>(0.f);
 }
 
-// How many warps a block computes with: as many as leave a block for every SM, since a warp's time for a piece is its own and only loading is shared.
-inline int delta_warps(const DeltaArgs& a)
+// Barriers of a block, behind its tiles.
+struct WalkBars {
+    uint64_t keys[2], squares, done[3];
+    uint32_t tmem, abort;
+};
+
+// The sum of products of parts, those of the last digits first: A has `a_parts` parts, B `b_parts`; `ks` steps of 16 along K.  `more`: onto what is there.
+template <typename DescA, typename DescB>
+__device__ __forceinline__ void multiply(uint32_t d, int a_parts, int b_parts, int ks, uint32_t idesc, uint32_t elected, bool more, DescA desc_a, DescB desc_b)
 {
-    int warps = kComputing;
-    while (warps > 1 && (a.VP / 16 < warps || (long long)a.B * a.H * ceil_div_u(a.VP / 16, warps) < sm_count())) warps /= 2;
-    return warps;
+#pragma unroll
+    for (int digits = kSum - 1; digits >= 0; --digits) {
+#pragma unroll
+        for (int p = 0; p <= digits; ++p) {
+            if (p >= a_parts || digits - p >= b_parts) continue;
+#pragma unroll
+            for (int k = 0; k < ks; ++k) {
+                ptx::mma_b16(d, desc_a(p, k), desc_b(digits - p, k), idesc, more, elected);
+                more = true;
+            }
+        }
+    }
+}
+
+// Columns a block walks with: 32, or 64 where those are fewer rounds of the machine's SMs (a piece takes about half as long again then).  Keys of 128 fp32 numbers, in
+// three parts, leave room for 32.
+template <typename T>
+int delta_columns(const DeltaArgs& a)
+{
+    if (a.V <= 32 || (sizeof(T) == 4 && a.K > 64)) return 32;
+    const long long heads = (long long)a.B * a.H, sms = sm_count();
+    const long long narrow = (heads * ceil_div_u(a.V, 32) + sms - 1) / sms, wide = (heads * ceil_div_u(a.V, 64) + sms - 1) / sms;
+    const int dflt = 3 * wide <= 2 * narrow ? 64 : 32;
+    return env_int("CONV2D_B200_DELTA_COLUMNS", dflt) == 64 ? 64 : 32;
 }
 
 }  // namespace conv2d_b200

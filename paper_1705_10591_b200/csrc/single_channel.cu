@@ -908,6 +908,22 @@ conv2d_status_t dispatch_rs(const float* x, const float* w, float* y, const Shap
 
 }  // namespace
 
+cudaError_t device_timeout_word(unsigned** word)
+{
+    static std::atomic<unsigned*> known[64];
+    int dev = 0;
+    const cudaError_t e = own_error(cudaGetDevice(&dev));
+    if (e != cudaSuccess) return e;
+    const bool recorded = dev >= 0 && dev < 64;
+    if (recorded && (*word = known[dev].load(std::memory_order_acquire)) != nullptr) return cudaSuccess;
+    void* p = nullptr;
+    const cudaError_t found = own_error(cudaGetSymbolAddress(&p, g_device_timeout));
+    if (found != cudaSuccess) return found;
+    *word = static_cast<unsigned*>(p);
+    if (recorded) known[dev].store(*word, std::memory_order_release);
+    return cudaSuccess;
+}
+
 cudaError_t consume_device_timeout(bool* raised)
 {
     unsigned flag = 0;

@@ -2,9 +2,8 @@
 
 Delta rule.  `delta_tokens` is the definition, token by token.  `delta_pieces` computes the same and the gradients from the formulas of pieces of 64 tokens, and
 can be told to err: every product of matrices is then off by u * (|a| @ |b|) * r, r drawn from -1 .. 1, where the kernels' are off by at most that.
-What comes of such errors, further products included, is what rounding may do to a result.  u for a product of n terms: operands in two bf16
-parts are off by 2^-16 each (a rounding of 2^-8, of the rest of it again) and what is left out, the product of the second parts, is 2^-16 too; in three parts
-2^-24 each and 3 * 2^-24 left out;
+What comes of such errors, further products included, is what rounding may do to a result.  u for a product of n terms: operands in three bf16
+parts are off by 2^-24 each (a rounding of 2^-8, of the rest of it again, and again) and what is left out, products of later parts, is 3 * 2^-24;
 the sum of n terms in fp32 by at most n 2^-24, of which errors of either sign leave about sqrt(n): taken as 16 * 2^-24 for n <= 128.  Exponentials of sums of decays
 are off by 2^-22 and by 2^-24 of their argument, which is below 90 where they are not zero: 2^-17, but only of what is nearly nothing; u covers 16 * 2^-24 of it.
 A check allows half a step of the result's type and, of errors drawn three times, four times the largest for each head: in norm, and (eight times) for a
@@ -17,9 +16,7 @@ import torch
 from sequence_reference import TYPES  # noqa: F401
 
 F = torch.float64
-U = {"bf16": 3 * 2.0 ** -16 + 2.0 ** -20, "fp16": 3 * 2.0 ** -16 + 2.0 ** -20, "fp32": 5 * 2.0 ** -24 + 2.0 ** -20}
-#: outputs of bf16 tensors are computed from states and updates in one part, off by 2^-8 each
-U_OUT = {"bf16": 2 * 2.0 ** -8, "fp16": U["fp16"], "fp32": U["fp32"]}
+U = 5 * 2.0 ** -24 + 2.0 ** -20
 PIECE = 64
 
 
@@ -46,13 +43,12 @@ class Errs:
     def __init__(self, u=0.0, seed=0):
         self.u, self.gen = u, torch.Generator().manual_seed(seed)
 
-    def mm(self, a, b, u=None):
+    def mm(self, a, b):
         c = a @ b
-        u = self.u if u is None else u
-        return c + u * (a.abs() @ b.abs()) * (2 * torch.rand(c.shape, generator=self.gen, dtype=F) - 1) if u else c
+        return c + self.u * (a.abs() @ b.abs()) * (2 * torch.rand(c.shape, generator=self.gen, dtype=F) - 1) if self.u else c
 
 
-def delta_pieces(q, k, v, g, beta, state, lengths, scale, dout=None, dlast=None, errs=None, u_out=None):
+def delta_pieces(q, k, v, g, beta, state, lengths, scale, dout=None, dlast=None, errs=None):
     """A dict of o, state (the last) and, with dout, dq, dk, dv, dg, dbeta, dstate."""
     B, L, H, V = v.shape
     Hk, K = q.shape[2:]
@@ -85,7 +81,7 @@ def delta_pieces(q, k, v, g, beta, state, lengths, scale, dout=None, dlast=None,
         R = v[:, :, c] - begin[:, :, c] * e.mm(kc, S)
         E = R - e.mm(t, beta[:, :, c] * R)
         kept.append((S, E, t, P))
-        out.append(scale * (begin[:, :, c] * e.mm(qc, S, u_out) + e.mm(P, beta[:, :, c] * E, u_out)))
+        out.append(scale * (begin[:, :, c] * e.mm(qc, S) + e.mm(P, beta[:, :, c] * E)))
         S = begin[:, :, c, -1:] * S + e.mm(kc.mT, end[:, :, c] * beta[:, :, c] * E)
     r = {"o": back(out, H), "state": S}
     if dout is None:
@@ -118,10 +114,10 @@ def delta_pieces(q, k, v, g, beta, state, lengths, scale, dout=None, dlast=None,
     return r
 
 
-def delta_allowed(type, *args, **kw):
+def delta_allowed(*args, **kw):
     """The 64-bit results and, three times, those of products that err as the kernels' may."""
     ref = delta_pieces(*args, **kw)
-    return ref, [delta_pieces(*args, **kw, errs=Errs(U[type], 100 + i), u_out=U_OUT[type]) for i in range(3)]
+    return ref, [delta_pieces(*args, **kw, errs=Errs(U, 100 + i)) for i in range(3)]
 
 
 def check_delta(got, name, ref, wrong):

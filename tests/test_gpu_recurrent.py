@@ -73,7 +73,7 @@ class Delta:
 
     def wanted(self, grads=True, last=True):
         args = (self.q, self.k, self.v, self.g, self.beta, self.state, self.n, self.scale)
-        return ref.delta_allowed(self.type, *args, **(dict(dout=self.dout, dlast=self.dlast if last else None) if grads else {}))
+        return ref.delta_allowed(*args, **(dict(dout=self.dout, dlast=self.dlast if last else None) if grads else {}))
 
     def check(self, results, wanted):
         B, L, Hk, H, K, V = self.dims

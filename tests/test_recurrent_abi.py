@@ -93,8 +93,8 @@ def test_without_a_gpu_nothing_falls_back(lib):  # noqa: F811
 
 def test_sizes_do_not_wrap(lib):  # noqa: F811
     pieces = 1 << 14
-    square, factors, state, update = 2 * 64 * 64 * 2, 5 * 64 * 4, 2 * 128 * 128 * 2, 2 * 128 * 64 * 2
-    assert lib.delta_states_size(8, 1 << 20, 16, 32, 128, 128) == 8 * 32 * pieces * (2 * square + factors + state + update)
-    assert lib.delta_fwd_gated_workspace_size(8, 1 << 20, 16, 32, 128, 128) == 8 * pieces * (32 * (2 * square + factors) + 16 * 2 * 64 * 128 * 2)
+    squares, factors, state, update = 3 * 2 * 64 * 64 * 2, 5 * 64 * 4, 128 * 128 * 4, 64 * 128 * 4
+    assert lib.delta_states_size(8, 1 << 20, 16, 32, 128, 128) == 8 * 32 * pieces * (squares + factors + state + update)
+    assert lib.delta_fwd_gated_workspace_size(8, 1 << 20, 16, 32, 128, 128) == 8 * pieces * (32 * (squares + factors) + 16 * 2 * 64 * 128 * 2)
     assert lib.delta_bwd_gated_workspace_size(8, 1 << 20, 16, 32, 128, 128, 2) > 8 * 32 * pieces * (state + update)
     assert lib.norm_bwd_rms_workspace_size(1 << 30, 16384, 1) < 1 << 28
