@@ -11,8 +11,8 @@
 namespace conv2d_b200 {
 namespace {
 
-template <typename T, int KD, int NV>
-__global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const DeltaArgs a, int across, bool wide_do, bool wide_dv)
+template <typename T, int KD, int NV, bool WIDE>
+__global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const DeltaArgs a, int across)
 {
     using W = Walk<T, KD, NV>;
     constexpr int IN = W::IN, C = W::C, STAGES = W::stages;
@@ -56,7 +56,6 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             ptx::bulk_g2s(squares, a.squares + (unit0 + pieces - 1 - s) * kSquares, W::squares, &bars->squares);
         };
         const uint32_t s_squares = ptx::smem_u32(squares), s_state = ptx::smem_u32(state), s_rows = ptx::smem_u32(rows);
-        constexpr uint32_t id1 = ptx::idesc_b16(128, NV, false) | ptx::kIdescBMajorMN, id3 = id1 | kIdescAMajorM;
         load_keys(0), load_squares(0);
         if (STAGES == 2) load_keys(1);
         bool alive = true;
@@ -66,24 +65,26 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             __syncthreads();                                   // dS is there
             ptx::tc_fence_after_sync();
             if (alive) {
-                multiply(tmem, IN, kSum, KD / 16, id1, elected, false, [&](int p, int k) { return rows_as_m(keys + p * W::key_part + (k >> 2) * W::HALF + (k & 3) * 32); },
-                         [&](int p, int k) { return rows_as_k<NV>(s_state + p * W::state_part + k * 16 * NV * 2); });
+                multiply_digits<NV, false, true>(tmem, IN, KD / 16, elected,
+                                                 [&](int p, int k) { return rows_as_m(keys + p * W::key_part + (k >> 2) * W::HALF + (k & 3) * 32); },
+                                                 [&](int k) { return rows_as_k<NV>(s_state + k * 16 * NV * 2, W::state_part); });
                 ptx::mma_commit(&bars->done[0], elected);
                 if (STAGES == 2 && s > 0) load_keys(s + 1);
             }
             alive = alive && ptx::mbar_wait_bounded_warp(&bars->squares, s & 1, abort_flag, a.max_polls);
             __syncthreads();                                   // beta X and scale dO are there
             ptx::tc_fence_after_sync();
-            if (alive) {                                       // (64 columns; the other 64 rows of the result are of whatever lies behind, and not read)
-                multiply(tmem + NV, kSum, kSum, 2 * kPiece / 16, id3, elected, false, [&](int p, int k) { return columns_as_m(s_squares + p * W::square_part + k * 16 * 128, W::square_part); },
-                         [&](int p, int k) { return rows_as_k<NV>(s_rows + p * W::rows_part + k * 16 * NV * 2); });
+            if (alive) {                                       // (64 rows; the other 64 of the result are of whatever lies behind, and not read)
+                multiply_digits<NV, false, true>(tmem + 3 * NV, kSum, 2 * kPiece / 16, elected,
+                                                 [&](int p, int k) { return rows_as_m(s_squares + p * W::square_part + (k >> 2) * (W::square_part / 2) + (k & 3) * 32); },
+                                                 [&](int k) { return rows_as_k<NV>(s_rows + k * 16 * NV * 2, W::rows_part); });
                 ptx::mma_commit(&bars->done[1], elected);
             }
             __syncthreads();                                   // -e^G dV and scale e^G dO are there, in their place
             ptx::tc_fence_after_sync();
             if (alive) {
-                multiply(tmem + 2 * NV, IN, kSum, 2 * kPiece / 16, id3, elected, false, [&](int p, int k) { return columns_as_m(keys + p * W::key_part + k * 16 * 128, W::HALF); },
-                         [&](int p, int k) { return rows_as_k<NV>(s_rows + p * W::rows_part + k * 16 * NV * 2); });
+                multiply_digits<NV, true, true>(tmem, IN, 2 * kPiece / 16, elected, [&](int p, int k) { return columns_as_m(keys + p * W::key_part + k * 16 * 128, W::HALF); },
+                                                [&](int k) { return rows_as_k<NV>(s_rows + k * 16 * NV * 2, W::rows_part); });
                 ptx::mma_commit(&bars->done[2], elected);
                 load_squares(s + 1);
                 if (STAGES == 1) {
@@ -104,18 +105,20 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
         const T* dout = static_cast<const T*>(a.dout) + ((long long)b * a.L + token) * a.lddo + (long long)h * a.V + v;
         T* dv = static_cast<T*>(a.dv) + ((long long)b * a.L + token) * a.lddv + (long long)h * a.V + v;
         const float* factors = a.factors + unit0 * (kFactors * kPiece);
-        float next[C], eg = 0.f, ed = 0.f, beta = 0.f, whole = 0.f;
+        SavedRow<C> update;                                    // E
+        Row<T, C> grad;                                        // dO
+        float eg = 0.f, ed = 0.f, beta = 0.f, whole = 0.f;
         auto fetch = [&](int i) {
             if (i < 0) return;
             const float* f = factors + (size_t)i * (kFactors * kPiece);
             eg = f[token], ed = f[kPiece + token], beta = f[2 * kPiece + token], whole = f[kPiece - 1];
-            if (is_key) load_row<float, C>(a.updates + ((unit0 + i) * kPiece + token) * a.VP + v, min(saved, C) / 16 * 16, true, next);
-            else load_row<T, C>(dout + (long long)i * kPiece * a.lddo, i * kPiece + token < len ? there : 0, wide_do, next);
+            if (is_key) update.load(a.updates + quad_at(unit0 + i, a.VP, kPiece, v, token), kPiece, saved);
+            else grad.template load<WIDE>(dout + (long long)i * kPiece * a.lddo, i * kPiece + token < len ? there : 0);
         };
         auto put_state = [&](int i) {                          // dS behind piece i
             if (row < KD) {
                 put_row<NV, C>(state, W::state_part, row, col0, S);
-                save_row<C>(a.dstates + ((unit0 + i) * KD + row) * a.VP + v, saved, S);
+                save_row<C>(a.dstates + quad_at(unit0 + i, a.VP, KD, v, row), KD, saved, S);
             }
             ptx::fence_proxy_async_smem();
         };
@@ -126,15 +129,16 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             ptx::tc_fence_before_sync();
             __syncthreads();
             if (!is_key) {
+                grad.get(y);
 #pragma unroll
-                for (int j = 0; j < C; ++j) y[j] = a.scale * next[j];
+                for (int j = 0; j < C; ++j) y[j] *= a.scale;
                 put_row<NV, C>(rows, W::rows_part, row, col0, y);
             }
             // D1: K dS
             ptx::mbar_wait_bounded(&bars->done[0], parity, abort_flag, a.max_polls);
             ptx::tc_fence_after_sync();
             if (is_key) {
-                tmem_row<C>(at, X);
+                tmem_digits<C>(at, NV, X);
 #pragma unroll
                 for (int j = 0; j < C; ++j) X[j] *= ed, y[j] = beta * X[j];
                 put_row<NV, C>(rows, W::rows_part, row, col0, y);
@@ -147,11 +151,11 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             ptx::tc_fence_after_sync();
             float sum = 0.f;
             if (is_key) {
-                tmem_row<C>(at + NV, y);
+                tmem_digits<C>(at + 3 * NV, NV, y);
 #pragma unroll
                 for (int j = 0; j < C; ++j) {
                     y[j] += X[j];
-                    sum = fmaf(y[j], next[j], sum);
+                    sum = fmaf(y[j], update.q[j / 4].e[j % 4], sum);
                     X[j] = beta * y[j];
                     y[j] = -eg * X[j];
                 }
@@ -165,8 +169,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             __syncthreads();
             if (is_key) {
                 const size_t unit = unit0 + i;
-                save_row<C>(a.dupdates + (unit * kPiece + token) * a.VP + v, saved, X);
-                if (i * kPiece + token < len) store_row<T, C>(dv + (long long)i * kPiece * a.lddv, there, wide_dv, X);
+                save_row<C>(a.dupdates + quad_at(unit, a.VP, kPiece, v, token), kPiece, saved, X);
+                if (i * kPiece + token < len) store_row<WIDE>(dv + (long long)i * kPiece * a.lddv, there, X);
                 if (saved > 0) {                               // (a sum over 32 columns stands for two of 16)
                     float* part = a.dbeta_parts + (unit * (a.VP / 16) + v / 16) * kPiece + token;
                     part[0] = sum;
@@ -178,7 +182,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             // D3: dS <- e^G_63 dS + ..
             ptx::mbar_wait_bounded(&bars->done[2], parity, abort_flag, a.max_polls);
             ptx::tc_fence_after_sync();
-            tmem_row<C>(at + 2 * NV, y);
+            tmem_digits<C>(at, NV, y);
 #pragma unroll
             for (int j = 0; j < C; ++j) S[j] = fmaf(keep, S[j], y[j]);
             if (i > 0) put_state(i - 1);
@@ -222,8 +226,8 @@ struct PieceBars {
     float factors[kFactors * kPiece], dots[4][kPiece], sums[8];
 };
 
-template <typename T, int KD>
-__global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_pieces_kernel(const DeltaArgs a, bool wide_do, bool wide_dq, bool wide_dk, bool wide_parts)
+template <typename T, int KD, bool WIDE>
+__global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_pieces_kernel(const DeltaArgs a)
 {
     using W = Piecewise<T, KD>;
     constexpr int IN = W::IN, NB = W::NB;
@@ -273,7 +277,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_pieces_kernel(const
         const uint32_t elected = ptx::elect_one();
         constexpr uint32_t idk = ptx::idesc_b16(128, KD, false), ide = ptx::idesc_b16(128, kPiece, false);
         // tiles of rows of 32 numbers, K-major: 64-byte swizzle
-        auto narrow = [](uint32_t at) { return rows_as_k<32>(at); };
+        auto narrow = [](uint32_t at) { return rows_as_k<32>(at, 512); };
         for (int j = 0; j < blocks; ++j) {
             __syncthreads();
             ptx::tc_fence_after_sync();
@@ -307,28 +311,43 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_pieces_kernel(const
         const bool is_key = row < kPiece;
         float inner = 0.f;                                     // <S, dS>
         {
-            const int r2 = tid >> 1, c2 = (tid & 1) * 16, r4 = tid >> 2, c4 = (tid & 3) * 8, t2 = r2 & (kPiece - 1);
-            const T* dout = static_cast<const T*>(a.dout) + (row0 + t2) * a.lddo + (long long)h * a.V;
-            float xr[16], xe[8], xs[16], xd[16];
+            // quads: of what the passes kept lanes have rows, of dO eight threads a row
+            constexpr int ROWS = kWorkers / KD, QUADS = 8 / ROWS;        // quads of a row at once, of a thread
+            const int k = tid % KD, q0 = tid / KD, t = tid % kPiece, p0 = tid / kPiece, r0 = tid >> 3, c = (tid & 7) * 4;
+            SavedRow<4> dv[2], e[2], s[QUADS], ds[QUADS];
+            Row<T, 4> dout[2];
+            const T* grads = static_cast<const T*>(a.dout) + row0 * a.lddo + (long long)h * a.V;
             auto fetch = [&](int v0) {
-                const int left = a.VP - v0;                    // a multiple of 16
-                if (r2 < kPiece) load_row<float, 16>(a.dupdates + (unit * kPiece + t2) * a.VP + v0 + c2, left - c2, true, xr);
-                else load_row<T, 16>(dout + v0 + c2, t2 < live ? a.V - v0 - c2 : 0, wide_do, xr);
-                load_row<float, 8>(a.updates + (unit * kPiece + r4) * a.VP + v0 + c4, left - c4, true, xe);
-                const size_t at = (unit * KD + r2) * a.VP + v0 + c2;
-                if (r2 < KD) load_row<float, 16>(a.states + at, left - c2, true, xs), load_row<float, 16>(a.dstates + at, left - c2, true, xd);
+#pragma unroll
+                for (int i = 0; i < QUADS; ++i) {
+                    const int v = v0 + 4 * (q0 + ROWS * i);
+                    s[i].load(a.states + quad_at(unit, a.VP, KD, v, k), KD, a.VP - v), ds[i].load(a.dstates + quad_at(unit, a.VP, KD, v, k), KD, a.VP - v);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int v = v0 + 4 * (p0 + 4 * i);
+                    dv[i].load(a.dupdates + quad_at(unit, a.VP, kPiece, v, t), kPiece, a.VP - v), e[i].load(a.updates + quad_at(unit, a.VP, kPiece, v, t), kPiece, a.VP - v);
+                    dout[i].template load<WIDE>(grads + (r0 + 32 * i) * a.lddo + v0 + c, r0 + 32 * i < live ? a.V - v0 - c : 0);
+                }
             };
             fetch(0);
             for (int j = 0; j < blocks; ++j) {
                 unsigned char* at = raw + (j & 1) * W::block;
                 if (j >= 2) ptx::mbar_wait_bounded(&bars.done[j & 1], ((j >> 1) - 1) & 1, abort_flag, a.max_polls);
-                put_row<NB, 16>(at, W::rows_part, r2, c2, xr);
-                put_row<NB, 8>(at + W::at_e, W::e_part, r4, c4, xe);
-                if (r2 < KD) {
-                    put_row<NB, 16>(at + W::at_s, W::state_part, r2, c2, xs);
-                    put_row<NB, 16>(at + W::at_ds, W::state_part, r2, c2, xd);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) inner = fmaf(xs[i], xd[i], inner);
+                for (int i = 0; i < QUADS; ++i) {
+                    put_four<NB>(at + W::at_s, W::state_part, k, 4 * (q0 + ROWS * i), s[i].q[0].e);
+                    put_four<NB>(at + W::at_ds, W::state_part, k, 4 * (q0 + ROWS * i), ds[i].q[0].e);
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) inner = fmaf(s[i].q[0].e[n], ds[i].q[0].e[n], inner);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float f[4];
+                    dout[i].get(f);
+                    put_four<NB>(at, W::rows_part, t, 4 * (p0 + 4 * i), dv[i].q[0].e);
+                    put_four<NB>(at + W::at_e, W::e_part, t, 4 * (p0 + 4 * i), e[i].q[0].e);
+                    put_four<NB>(at, W::rows_part, kPiece + r0 + 32 * i, c, f);
                 }
                 ptx::fence_proxy_async_smem();
                 ptx::tc_fence_before_sync();
@@ -355,18 +374,21 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_pieces_kernel(const
         ptx::fence_proxy_async_smem();
         ptx::tc_fence_before_sync();
         __syncthreads();
+        const T* mine = static_cast<const T*>(is_key ? a.k : a.q) + (row0 + token) * (is_key ? a.ldk : a.ldq) + (long long)hk * a.K;
+        Row<T, 16> other;                                      // of this token's key or query, a step ahead
+        other.template load<WIDE>(mine + side * (KD / 2), token < live ? a.K - side * (KD / 2) : 0);
         ptx::mbar_wait_bounded(&bars.last, 0, abort_flag, a.max_polls);
         ptx::tc_fence_after_sync();
         // <S after, dS> = e^G_63 <S, dS> + sum over tokens of k . (e^(G_63 - G) beta E dS^T)
         float after = eg[kPiece - 1] * inner, dot = 0.f;
         const float x1 = is_key ? -eg[token] : a.scale * eg[token], x3 = ed[token] * be[token];
-        const T* mine = static_cast<const T*>(is_key ? a.k : a.q) + (row0 + token) * (is_key ? a.ldk : a.ldq) + (long long)hk * a.K;
 #pragma unroll
         for (int col = side * (KD / 2); col < (side + 1) * (KD / 2); col += 16) {
             float x[16], y[16], z[16];
             tmem_row<16>(lanes + W::d1 + col, x);
             tmem_row<16>(lanes + W::d4 + col, y);
-            load_row<T, 16>(mine + col, token < live ? a.K - col : 0, false, z);
+            other.get(z);
+            if (col + 16 < (side + 1) * (KD / 2)) other.template load<WIDE>(mine + col + 16, token < live ? a.K - col - 16 : 0);
 #pragma unroll
             for (int j = 0; j < 16; ++j) x[j] = fmaf(x1, x[j], y[j]), dot = fmaf(z[j], x[j], dot);
             if (is_key) {
@@ -381,8 +403,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_pieces_kernel(const
                 }
             }
             if (token < live) {
-                if (shared_key) store_row<float, 16>((is_key ? a.dk_parts : a.dq_parts) + part0 + (long long)token * a.H * a.K + col, a.K - col, wide_parts, x);
-                else store_row<T, 16>(is_key ? dk + token * a.lddk + col : dq + token * a.lddq + col, a.K - col, is_key ? wide_dk : wide_dq, x);
+                if (shared_key) store_row<WIDE>((is_key ? a.dk_parts : a.dq_parts) + part0 + (long long)token * a.H * a.K + col, a.K - col, x);
+                else store_row<WIDE>(is_key ? dk + token * a.lddk + col : dq + token * a.lddq + col, a.K - col, x);
             }
         }
         bars.dots[side * 2 + (is_key ? 0 : 1)][token] = dot;
@@ -437,47 +459,51 @@ __global__ void __launch_bounds__(256) delta_bwd_shared_kernel(const DeltaArgs a
     }
 }
 
-template <typename T, int KD, int NV>
+template <typename T, int KD, int NV, bool WIDE>
 conv2d_status_t backward_walk(const DeltaArgs& a, cudaStream_t stream)
 {
     using W = Walk<T, KD, NV>;
     static SmemLimit limit;
     const int across = (int)ceil_div_u(a.V, NV);
-    if (raise_smem_limit((const void*)delta_bwd_walk_kernel<T, KD, NV>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-    const int per = 16 / (int)sizeof(T);
-    const bool wide_do = a.V % per == 0 && rows_aligned(a.dout, a.lddo, sizeof(T), 16), wide_dv = a.V % per == 0 && rows_aligned(a.dv, a.lddv, sizeof(T), 16);
-    if (launch_pdl(delta_bwd_walk_kernel<T, KD, NV>, dim3((unsigned)(a.B * a.H) * across), dim3(kWalkThreads), W::smem, stream, a, across, wide_do, wide_dv) !=
-        cudaSuccess)
+    if (raise_smem_limit((const void*)delta_bwd_walk_kernel<T, KD, NV, WIDE>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+    if (launch_pdl(delta_bwd_walk_kernel<T, KD, NV, WIDE>, dim3((unsigned)(a.B * a.H) * across), dim3(kWalkThreads), W::smem, stream, a, across) != cudaSuccess)
+        return CONV2D_ERR_CUDA;
+    count_launch();
+    return CONV2D_OK;
+}
+
+template <typename T, int KD, bool WIDE>
+conv2d_status_t backward_pieces(const DeltaArgs& a, cudaStream_t stream)
+{
+    using W = Piecewise<T, KD>;
+    static SmemLimit limit;
+    if (raise_smem_limit((const void*)delta_bwd_pieces_kernel<T, KD, WIDE>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+    if (launch_pdl(delta_bwd_pieces_kernel<T, KD, WIDE>, dim3((unsigned)(a.B * a.H) * (unsigned)a.pieces), dim3(kWalkThreads), W::smem, stream, a) != cudaSuccess)
         return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;
 }
 
 template <typename T, int KD>
-conv2d_status_t backward_pieces(const DeltaArgs& a, cudaStream_t stream)
+conv2d_status_t backward_wide(const DeltaArgs& a, cudaStream_t stream)
 {
-    using W = Piecewise<T, KD>;
-    static SmemLimit limit;
-    if (raise_smem_limit((const void*)delta_bwd_pieces_kernel<T, KD>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
     const int per = 16 / (int)sizeof(T);
-    const bool wide_do = a.V % per == 0 && rows_aligned(a.dout, a.lddo, sizeof(T), 16), wide_dq = a.K % per == 0 && rows_aligned(a.dq, a.lddq, sizeof(T), 16),
-               wide_dk = a.K % per == 0 && rows_aligned(a.dk, a.lddk, sizeof(T), 16);
-    if (launch_pdl(delta_bwd_pieces_kernel<T, KD>, dim3((unsigned)(a.B * a.H) * (unsigned)a.pieces), dim3(kWalkThreads), W::smem, stream, a, wide_do, wide_dq, wide_dk,
-                   a.K % 4 == 0) != cudaSuccess)
-        return CONV2D_ERR_CUDA;
-    count_launch();
-    return CONV2D_OK;
+    const bool wide_v = a.V % per == 0 && rows_aligned(a.dout, a.lddo, sizeof(T), 16) && rows_aligned(a.dv, a.lddv, sizeof(T), 16);
+    const bool wide = wide_v && a.K % 8 == 0 && rows_aligned(a.q, a.ldq, sizeof(T), 16) && rows_aligned(a.k, a.ldk, sizeof(T), 16) &&
+                      rows_aligned(a.dq, a.lddq, sizeof(T), 16) && rows_aligned(a.dk, a.lddk, sizeof(T), 16);
+    conv2d_status_t st = CONV2D_ERR_UNSUPPORTED;
+    if constexpr (sizeof(T) == 2 || KD == 64) {
+        if (delta_columns<T>(a, wide_v) == 64) st = backward_walk<T, KD, 64, true>(a, stream);
+    }
+    if (st == CONV2D_ERR_UNSUPPORTED) st = wide_v ? backward_walk<T, KD, 32, true>(a, stream) : backward_walk<T, KD, 32, false>(a, stream);
+    if (st != CONV2D_OK) return st;
+    return wide ? backward_pieces<T, KD, true>(a, stream) : backward_pieces<T, KD, false>(a, stream);
 }
 
 template <typename T>
 conv2d_status_t backward_typed(const DeltaArgs& a, cudaStream_t stream)
 {
-    const bool narrow = delta_columns<T>(a) == 32;
-    conv2d_status_t st;
-    if (a.K <= 64) st = narrow ? backward_walk<T, 64, 32>(a, stream) : backward_walk<T, 64, 64>(a, stream);
-    else if constexpr (sizeof(T) == 4) st = backward_walk<T, 128, 32>(a, stream);
-    else st = narrow ? backward_walk<T, 128, 32>(a, stream) : backward_walk<T, 128, 64>(a, stream);
-    if (st == CONV2D_OK) st = a.K <= 64 ? backward_pieces<T, 64>(a, stream) : backward_pieces<T, 128>(a, stream);
+    const conv2d_status_t st = a.K <= 64 ? backward_wide<T, 64>(a, stream) : backward_wide<T, 128>(a, stream);
     if (st != CONV2D_OK || a.share == 1) return st;
     const long long blocks = ((long long)a.B * a.L * a.Hk * a.K + 255) / 256, most = 16LL * sm_count();
     if (launch_pdl(delta_bwd_shared_kernel<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, stream, a) != cudaSuccess) return CONV2D_ERR_CUDA;

@@ -8,7 +8,7 @@
 // A piece is three products of 128 rows:  [K; Q] S,  [-t; P'] (beta R),  K^T (e^(G_63 - G) beta E).
 #pragma once
 
-#include "seq_common.cuh"
+#include "masked_load.cuh"
 #include "recurrent_b200.h"
 
 namespace conv2d_b200 {
@@ -17,9 +17,9 @@ constexpr int kPiece = 64;
 constexpr int kFactors = 5;                                     // of a piece: e^G, e^(G_63 - G), beta, G in two floats
 constexpr int kMost = 128;                                      // numbers of a key
 
-// Numbers of bf16 that hold a tensor's element (exactly, but for the last bits of an fp32 number), and kSum of those that hold sums and states as
-// operands: 24 bits (a rounding of 2^-8, of the rest of it again, and again).  Two would be 16 bits: half the products of two sums, but results in fp32 (states,
-// gradients of gates) were off by 3e-6 to 9e-6 then, by less than 1e-6 so.
+// Numbers of bf16 that hold a tensor's element, and kSum of those that hold sums and states as
+// operands: all of their 24 bits.  Two would be 16: half the products of two sums, but results in fp32 (states, gradients of gates) were off by 3e-6 to
+// 9e-6 then, by about 1e-6 so.
 template <typename T> struct Parts;
 template <> struct Parts<bf16> { static constexpr int in = 1; };
 template <> struct Parts<fp16> { static constexpr int in = 2; };
@@ -27,7 +27,8 @@ template <> struct Parts<float> { static constexpr int in = 3; };
 constexpr int kSum = 3;
 inline int parts_in(conv2d_operand_t t) { return t == CONV2D_OPERAND_BF16 ? 1 : t == CONV2D_OPERAND_FP16 ? 2 : 3; }
 
-// a, b as N parts each, the two of a part side by side.
+// a, b as N parts each, the two of a part side by side.  Rounded, not cut: the parts that are left out of products are smaller by half so, twice over, and of
+// either sign.
 template <int N>
 __device__ __forceinline__ void split(float a, float b, uint32_t (&out)[N])
 {
@@ -63,6 +64,35 @@ __device__ __forceinline__ uint32_t unit_at(uint32_t base, int row, int unit)
 {
     return base + row * (W * 2) + ((unit ^ (W >= 64 ? row & 7 : (row >> 1) & 3)) << 4);
 }
+
+// N elements of a row of a tensor as they lie, zeros beyond `there`: to be converted when they are used, since a conversion waits for the load.  WIDE: by accesses of
+// 16 bytes, `there` a multiple of those; a template's matter, since a branch between loads waits for them, too.
+template <typename T, int N>
+struct Row {
+    static constexpr int PER = 16 / (int)sizeof(T) < N ? 16 / (int)sizeof(T) : N;
+    Pack<T, PER> p[N / PER];
+    template <bool WIDE>
+    __device__ __forceinline__ void load(const T* from, int there)
+    {
+        if (WIDE) {
+#pragma unroll
+            for (int i = 0; i < N / PER; ++i) p[i] = load_masked<T, PER>(from + i * PER, i * PER < there);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) p[i / PER].e[i % PER] = load_masked<T, 1>(from + i, i < there).e[0];
+        }
+    }
+    __device__ __forceinline__ void get(float (&f)[N]) const
+    {
+#pragma unroll
+        for (int i = 0; i < N / PER; ++i) {
+            float x[PER];
+            unpack(p[i], x);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) f[i * PER + j] = x[j];
+        }
+    }
+};
 
 // Fragments of 16 x 16 blocks, by what lies along the tile's rows (m = lane / 8 picks one of four 8 x 8 blocks):
 //   rows of the product's right operand along n, k inside them   -> two tiles of 8 columns: {b0, b1}, {b0, b1}
@@ -119,7 +149,7 @@ __device__ __forceinline__ void mma_parts(float (&c0)[4], float (&c1)[4], const 
 
 // Where things lie in what the forward pass leaves (`states`) and in workspaces.  A "unit" is one piece of one head of one sequence, number
 // (b * H + h) * pieces + c; a "key unit" the same of a key head.  Sections in this order, sizes in bytes for each unit:
-constexpr size_t kSquares = (size_t)kSum * 2 * kPiece * kPiece * 2;      // [-t; P'], [part][128][64], units of 16 bytes swizzled as unit_at does
+constexpr size_t kSquares = (size_t)kSum * 2 * kPiece * kPiece * 2;      // [-t^T | P'^T], [part][two][64][64], units of 16 bytes swizzled as unit_at does
 struct DeltaLayout {
     int B, L, Hk, H, K, V, KD, VP, pieces, in;                   // KD: K rounded up to 64 or 128; VP: V to 16
     size_t units, keys;                                          // pieces of all value heads, of all key heads
@@ -129,8 +159,8 @@ struct DeltaLayout {
     {
     }
     size_t prepared_bytes() const { return units * (kSquares + kFactors * kPiece * 4); }
-    size_t state() const { return (size_t)KD * VP * 4; }                             // S or its gradient, [K][V]
-    size_t update() const { return (size_t)kPiece * VP * 4; }                        // E or dV, [token][V]
+    size_t state() const { return (size_t)KD * VP * 4; }                             // S or its gradient, [V/4][K][4]
+    size_t update() const { return (size_t)kPiece * VP * 4; }                        // E or dV, [V/4][token][4]
     size_t saved_bytes() const { return units * (state() + update()); }
     size_t key_tile() const { return (size_t)in * 2 * kPiece * KD * 2; }             // [K; Q], [part][64 numbers][128][64], swizzled likewise
     size_t keys_bytes() const { return keys * key_tile(); }
@@ -148,7 +178,7 @@ struct DeltaArgs {
     float scale;
     unsigned char *squares, *keys;    // tiles of units and of key units
     float* factors;               // [unit][kFactors][64]
-    float *states, *updates;      // saved by the forward pass: [unit][KD][VP], [unit][64][VP]; NULL: not wanted
+    float *states, *updates;      // saved by the forward pass: [unit][VP/4][KD][4], [unit][VP/4][64][4]; NULL: not wanted
     float *dstates, *dupdates;    // the same of their gradients (dS after the piece, dV)
     float* dbeta_parts;           // [unit][VP / 16][64]
     float *dq_parts, *dk_parts;   // [B*L][H*K] fp32: gradients of heads that share a key, before they are summed
@@ -165,7 +195,7 @@ inline bool delta_extents_ok(int B, int L, int H, int V)
 conv2d_status_t launch_delta_fwd(DeltaArgs a, conv2d_operand_t type, void* states, void* workspace, cudaStream_t stream);
 conv2d_status_t launch_delta_bwd(DeltaArgs a, conv2d_operand_t type, const void* states, void* workspace, cudaStream_t stream);
 conv2d_status_t launch_delta_step(const DeltaArgs& a, conv2d_operand_t type, cudaStream_t stream);
-// The first kernel of both passes: t, P and factors of every piece (backward: only the planes of keys and queries).
+// The first kernel of both passes: tiles and factors of every piece (backward: only the tiles of keys and queries).
 conv2d_status_t launch_delta_prepare(const DeltaArgs& a, conv2d_operand_t type, bool squares, cudaStream_t stream);
 size_t delta_states_bytes(const DeltaLayout& l);
 size_t delta_fwd_workspace_bytes(const DeltaLayout& l);

@@ -4,8 +4,8 @@
 namespace conv2d_b200 {
 namespace {
 
-template <typename T, int KD, int NV>
-__global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaArgs a, int across, bool wide_v, bool wide_o)
+template <typename T, int KD, int NV, bool WIDE>
+__global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaArgs a, int across)
 {
     using W = Walk<T, KD, NV>;
     constexpr int IN = W::IN, C = W::C, STAGES = W::stages;
@@ -49,7 +49,6 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
             ptx::bulk_g2s(squares, a.squares + (unit0 + i) * kSquares, W::squares, &bars->squares);
         };
         const uint32_t s_squares = ptx::smem_u32(squares), s_state = ptx::smem_u32(state), s_rows = ptx::smem_u32(rows);
-        constexpr uint32_t id1 = ptx::idesc_b16(128, NV, false) | ptx::kIdescBMajorMN, id3 = id1 | kIdescAMajorM;
         load_keys(0), load_squares(0);
         if (STAGES == 2) load_keys(1);
         bool alive = true;
@@ -59,9 +58,9 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
             __syncthreads();                                   // S is there
             ptx::tc_fence_after_sync();
             if (alive) {
-                multiply(tmem, IN, kSum, KD / 16, id1, elected, false,
-                         [&](int p, int k) { return rows_as_m(keys + p * W::key_part + (k >> 2) * W::HALF + (k & 3) * 32); },
-                         [&](int p, int k) { return rows_as_k<NV>(s_state + p * W::state_part + k * 16 * NV * 2); });
+                multiply_digits<NV, false, true>(tmem, IN, KD / 16, elected,
+                                                 [&](int p, int k) { return rows_as_m(keys + p * W::key_part + (k >> 2) * W::HALF + (k & 3) * 32); },
+                                                 [&](int k) { return rows_as_k<NV>(s_state + k * 16 * NV * 2, W::state_part); });
                 ptx::mma_commit(&bars->done[0], elected);
                 // (everything of the piece before is done with)
                 if (STAGES == 2 && i > 0) load_keys(i + 1);
@@ -70,15 +69,16 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
             __syncthreads();                                   // beta R is there
             ptx::tc_fence_after_sync();
             if (alive) {
-                multiply(tmem + NV, kSum, kSum, kPiece / 16, id1, elected, false, [&](int p, int k) { return rows_as_m(s_squares + p * W::square_part + k * 32); },
-                         [&](int p, int k) { return rows_as_k<NV>(s_rows + p * W::rows_part + k * 16 * NV * 2); });
+                multiply_digits<NV, true, true>(tmem + 3 * NV, kSum, kPiece / 16, elected,
+                                                [&](int p, int k) { return columns_as_m(s_squares + p * W::square_part + k * 16 * 128, W::square_part / 2); },
+                                                [&](int k) { return rows_as_k<NV>(s_rows + k * 16 * NV * 2, W::rows_part); });
                 ptx::mma_commit(&bars->done[1], elected);
             }
             __syncthreads();                                   // what updates S is there, in the place of beta R
             ptx::tc_fence_after_sync();
             if (alive) {
-                multiply(tmem + 2 * NV, IN, kSum, kPiece / 16, id3, elected, false, [&](int p, int k) { return columns_as_m(keys + p * W::key_part + k * 16 * 128, W::HALF); },
-                         [&](int p, int k) { return rows_as_k<NV>(s_rows + p * W::rows_part + k * 16 * NV * 2); });
+                multiply_digits<NV, true, true>(tmem, IN, kPiece / 16, elected, [&](int p, int k) { return columns_as_m(keys + p * W::key_part + k * 16 * 128, W::HALF); },
+                                                [&](int k) { return rows_as_k<NV>(s_rows + k * 16 * NV * 2, W::rows_part); });
                 ptx::mma_commit(&bars->done[2], elected);
                 load_squares(i + 1);
                 if (STAGES == 1) {
@@ -99,17 +99,18 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
         const T* values = static_cast<const T*>(a.v) + ((long long)b * a.L + token) * a.ldv + (long long)h * a.V + v;
         T* out = static_cast<T*>(a.o) + ((long long)b * a.L + token) * a.ldo + (long long)h * a.V + v;
         const float* factors = a.factors + unit0 * (kFactors * kPiece);
-        float next[C], eg = 0.f, ed = 0.f, beta = 0.f, whole = 0.f;
+        Row<T, C> next;
+        float eg = 0.f, ed = 0.f, beta = 0.f, whole = 0.f;
         auto fetch = [&](int i) {                              // this token's value (of keys) and factors
             if (i >= pieces) return;
             const float* f = factors + (size_t)i * (kFactors * kPiece);
             eg = f[token], ed = f[kPiece + token], beta = f[2 * kPiece + token], whole = f[kPiece - 1];
-            if (is_key) load_row<T, C>(values + (long long)i * kPiece * a.ldv, i * kPiece + token < len ? there : 0, wide_v, next);
+            if (is_key) next.template load<WIDE>(values + (long long)i * kPiece * a.ldv, i * kPiece + token < len ? there : 0);
         };
         auto put_state = [&](int i) {                          // S before piece i, for its product and for the backward pass
             if (row < KD) {
                 put_row<NV, C>(state, W::state_part, row, col0, S);
-                if (a.states) save_row<C>(a.states + ((unit0 + i) * KD + row) * a.VP + v, saved, S);
+                if (a.states) save_row<C>(a.states + quad_at(unit0 + i, a.VP, KD, v, row), KD, saved, S);
             }
             ptx::fence_proxy_async_smem();
         };
@@ -122,11 +123,12 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
             // D1: of keys R = v - e^G k S, of queries e^G q S
             ptx::mbar_wait_bounded(&bars->done[0], parity, abort_flag, a.max_polls);
             ptx::tc_fence_after_sync();
-            tmem_row<C>(at, X);
+            tmem_digits<C>(at, NV, X);
             if (is_key) {
                 float y[C];
+                next.get(y);
 #pragma unroll
-                for (int j = 0; j < C; ++j) X[j] = fmaf(-eg, X[j], next[j]), y[j] = beta * X[j];
+                for (int j = 0; j < C; ++j) X[j] = fmaf(-eg, X[j], y[j]), y[j] = beta * X[j];
                 put_row<NV, C>(rows, W::rows_part, row, col0, y);
                 ptx::fence_proxy_async_smem();
             } else {
@@ -139,7 +141,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
             ptx::mbar_wait_bounded(&bars->done[1], parity, abort_flag, a.max_polls);
             ptx::tc_fence_after_sync();
             float y[C];
-            tmem_row<C>(at + NV, y);
+            tmem_digits<C>(at + 3 * NV, NV, y);
 #pragma unroll
             for (int j = 0; j < C; ++j) X[j] += y[j];
             if (is_key) {
@@ -152,18 +154,18 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
             ptx::tc_fence_before_sync();
             __syncthreads();
             if (is_key) {
-                if (a.updates) save_row<C>(a.updates + ((unit0 + i) * kPiece + token) * a.VP + v, saved, X);
+                if (a.updates) save_row<C>(a.updates + quad_at(unit0 + i, a.VP, kPiece, v, token), kPiece, saved, X);
             } else if (i * kPiece + token < len) {
 #pragma unroll
                 for (int j = 0; j < C; ++j) X[j] *= a.scale;
-                store_row<T, C>(out + (long long)i * kPiece * a.ldo, there, wide_o, X);
+                store_row<WIDE>(out + (long long)i * kPiece * a.ldo, there, X);
             }
             const float keep = whole;
             fetch(i + 1);
-            // D3: S <- e^G_63 S + K^T (..)
+            // D3, in D1's place: S <- e^G_63 S + K^T (..)
             ptx::mbar_wait_bounded(&bars->done[2], parity, abort_flag, a.max_polls);
             ptx::tc_fence_after_sync();
-            tmem_row<C>(at + 2 * NV, y);
+            tmem_digits<C>(at, NV, y);
 #pragma unroll
             for (int j = 0; j < C; ++j) S[j] = fmaf(keep, S[j], y[j]);
             if (i + 1 < pieces) put_state(i + 1);
@@ -184,28 +186,33 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
     }
 }
 
-template <typename T, int KD, int NV>
+template <typename T, int KD, int NV, bool WIDE>
 conv2d_status_t walk(const DeltaArgs& a, cudaStream_t stream)
 {
     using W = Walk<T, KD, NV>;
     static SmemLimit limit;
     const int across = (int)ceil_div_u(a.V, NV);
-    if (raise_smem_limit((const void*)delta_fwd_kernel<T, KD, NV>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-    const int per = 16 / (int)sizeof(T);
-    const bool wide_v = a.V % per == 0 && rows_aligned(a.v, a.ldv, sizeof(T), 16), wide_o = a.V % per == 0 && rows_aligned(a.o, a.ldo, sizeof(T), 16);
-    if (launch_pdl(delta_fwd_kernel<T, KD, NV>, dim3((unsigned)(a.B * a.H) * across), dim3(kWalkThreads), W::smem, stream, a, across, wide_v, wide_o) != cudaSuccess)
+    if (raise_smem_limit((const void*)delta_fwd_kernel<T, KD, NV, WIDE>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+    if (launch_pdl(delta_fwd_kernel<T, KD, NV, WIDE>, dim3((unsigned)(a.B * a.H) * across), dim3(kWalkThreads), W::smem, stream, a, across) != cudaSuccess)
         return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;
 }
 
+template <typename T, int KD>
+conv2d_status_t walk_wide(const DeltaArgs& a, cudaStream_t stream)
+{
+    const bool wide = a.V % (16 / sizeof(T)) == 0 && rows_aligned(a.v, a.ldv, sizeof(T), 16) && rows_aligned(a.o, a.ldo, sizeof(T), 16);
+    if constexpr (sizeof(T) == 2 || KD == 64) {
+        if (delta_columns<T>(a, wide) == 64) return walk<T, KD, 64, true>(a, stream);
+    }
+    return wide ? walk<T, KD, 32, true>(a, stream) : walk<T, KD, 32, false>(a, stream);
+}
+
 template <typename T>
 conv2d_status_t walk_typed(const DeltaArgs& a, cudaStream_t stream)
 {
-    const bool narrow = delta_columns<T>(a) == 32;
-    if (a.K <= 64) return narrow ? walk<T, 64, 32>(a, stream) : walk<T, 64, 64>(a, stream);
-    if constexpr (sizeof(T) == 4) return walk<T, 128, 32>(a, stream);
-    else return narrow ? walk<T, 128, 32>(a, stream) : walk<T, 128, 64>(a, stream);
+    return a.K <= 64 ? walk_wide<T, 64>(a, stream) : walk_wide<T, 128>(a, stream);
 }
 
 }  // namespace

@@ -23,14 +23,9 @@ __global__ void __launch_bounds__(128) delta_step_kernel(const DeltaArgs a, int 
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         const int k = group + i * groups;
-        if (mine && k < a.K) {
-            const Pack<float, VW> p = load_pack<float, VW>(a.state_in + at + (size_t)k * a.V);
+        const Pack<float, VW> p = load_masked<float, VW>(a.state_in + at + (size_t)k * a.V, mine && k < a.K);
 #pragma unroll
-            for (int e = 0; e < VW; ++e) S[i][e] = p.e[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < VW; ++e) S[i][e] = 0.f;
-        }
+        for (int e = 0; e < VW; ++e) S[i][e] = p.e[e];
     }
     if (tid < a.K) {
         ks[tid] = to_float(static_cast<const T*>(a.k)[b * a.ldk + (long long)hk * a.K + tid]);

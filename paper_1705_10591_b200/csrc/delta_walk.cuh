@@ -3,7 +3,7 @@
 // A block walks one head of one sequence for NV columns of V.  A piece is three tcgen05 products with accumulators of 128 rows in tensor memory, each waiting for
 // what threads make of the one before: with 32 columns a piece is all latency, and registers, not memory, hand S and E on.
 //   D1 [128] = [K; Q] S            rows of K as they lie (K-major), S written by its threads, a row a thread (N-major)
-//   D2 [128] = [-t; P'] (beta R)
+//   D2 [128] = [-t; P'] (beta R)   both lie transposed, as rows of tokens j with 64 numbers each: M-major
 //   D3 [128] = K^T (..)            the tile of K read the other way (M-major)
 // Eight warps own a quarter of the 128 rows and one half of the columns each: a thread has one row of D1 and D2 (a token of K or of Q) and of S (a number of
 // K).  A ninth warp issues the products and the copies of the next piece's tiles.
@@ -24,33 +24,50 @@ struct Walk {
     static constexpr int rest = squares + state + kSum * rows_part + 1024;        // (1024: barriers)
     static constexpr int stages = 2 * keys + rest <= 232448 - 1024 ? 2 : 1;
     static constexpr int smem = stages * keys + rest + 1024;                      // (1024: to the first boundary of the swizzle)
-    static constexpr int cols = NV == 32 ? 128 : 256;                             // of tensor memory: three times NV, a power of two
+    static constexpr int cols = NV == 32 ? 256 : 512;                             // of tensor memory: twice three times NV, to a power of two
     static constexpr int C = NV / 2;                                              // columns of a thread
     static_assert(smem <= 232448, "a piece does not fit");
 };
 
-// Descriptors: [K; Q] and [-t; P'] have rows of 128 bytes, atoms of 8 rows.
+// Descriptors: [K; Q] and [-t^T | P'^T] have rows of 128 bytes, atoms of 8 rows.
 __device__ __forceinline__ uint64_t rows_as_m(uint32_t at) { return ptx::smem_desc_sw128(at, 16, 1024); }
 // columns as M, rows as K; `next`: distance to the following 64 columns
 __device__ __forceinline__ uint64_t columns_as_m(uint32_t at, uint32_t next) { return ptx::smem_desc_sw128(at, next, 1024); }
-// rows as K, their NV numbers as N
+// rows as K, their NV numbers as N; `next`: distance to the following NV
 template <int NV>
-__device__ __forceinline__ uint64_t rows_as_k(uint32_t at)
+__device__ __forceinline__ uint64_t rows_as_k(uint32_t at, uint32_t next)
 {
-    if (NV == 64) return ptx::smem_desc_sw128(at, 1024, 1024);
+    if (NV == 64) return ptx::smem_desc_sw128(at, next, 1024);
     // 64-byte swizzle: atoms of 8 rows x 64 bytes
-    return (uint64_t)((at >> 4) & 0x3FFFu) | ((uint64_t)(512 >> 4) << 16) | ((uint64_t)(512 >> 4) << 32) | (1ull << 46) | (4ull << 61);
+    return (uint64_t)((at >> 4) & 0x3FFFu) | ((uint64_t)(next >> 4) << 16) | ((uint64_t)(512 >> 4) << 32) | (1ull << 46) | (4ull << 61);
 }
 constexpr uint32_t kIdescAMajorM = 1u << 15;
 
+template <int N> __device__ __forceinline__ void tmem_get(uint32_t at, uint32_t (&v)[N])
+{
+    if constexpr (N == 16) ptx::tmem_ld16(at, v);
+    else ptx::tmem_ld32(at, v);
+}
 template <int N> __device__ __forceinline__ void tmem_row(uint32_t at, float (&f)[N])
 {
     uint32_t v[N];
-    if constexpr (N == 16) ptx::tmem_ld16(at, v);
-    else ptx::tmem_ld32(at, v);
+    tmem_get<N>(at, v);
     ptx::tmem_ld_wait();
 #pragma unroll
     for (int i = 0; i < N; ++i) f[i] = __uint_as_float(v[i]);
+}
+// The sum of products whose digits lie in three places, `step` columns apart.
+template <int N> __device__ __forceinline__ void tmem_digits(uint32_t at, uint32_t step, float (&f)[N])
+{
+#pragma unroll
+    for (int c = 0; c < N; c += 16) {
+        uint32_t v[kSum][16];
+#pragma unroll
+        for (int p = 0; p < kSum; ++p) ptx::tmem_ld16(at + p * step + c, v[p]);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) f[c + i] = (__uint_as_float(v[2][i]) + __uint_as_float(v[1][i])) + __uint_as_float(v[0][i]);
+    }
 }
 
 // N numbers of row `row` from column `col` on (a multiple of 8), as parts, into a tile of rows of NV.
@@ -67,35 +84,28 @@ __device__ __forceinline__ void put_row(unsigned char* tile, int part_bytes, int
     }
 }
 
-// N elements of a row of a tensor, zeros beyond `there`.
-template <typename T, int N>
-__device__ __forceinline__ void load_row(const T* from, int there, bool wide, float (&f)[N])
+// Four numbers likewise.
+template <int NV>
+__device__ __forceinline__ void put_four(unsigned char* tile, int part_bytes, int row, int col, const float (&f)[4])
 {
-    constexpr int PER = 16 / (int)sizeof(T);
-    if (there >= N && wide) {
+    uint32_t w[2][kSum];
+    split<kSum>(f[0], f[1], w[0]);
+    split<kSum>(f[2], f[3], w[1]);
 #pragma unroll
-        for (int i = 0; i < N; i += PER) {
-            float x[PER];
-            unpack(load_pack<T, PER>(from + i), x);
-#pragma unroll
-            for (int j = 0; j < PER; ++j) f[i + j] = x[j];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = i < there ? to_float(from[i]) : 0.f;
-    }
+    for (int p = 0; p < kSum; ++p) *reinterpret_cast<uint2*>(tile + p * part_bytes + unit_at<NV>(0, row, col / 8) + (col & 4) * 2) = make_uint2(w[0][p], w[1][p]);
 }
-template <typename T, int N>
-__device__ __forceinline__ void store_row(T* to, int there, bool wide, const float (&f)[N])
+
+template <bool WIDE, typename T, int N>
+__device__ __forceinline__ void store_row(T* to, int there, const float (&f)[N])
 {
     constexpr int PER = 16 / (int)sizeof(T);
-    if (there >= N && wide) {
+    if (WIDE) {
 #pragma unroll
         for (int i = 0; i < N; i += PER) {
             float x[PER];
 #pragma unroll
             for (int j = 0; j < PER; ++j) x[j] = f[i + j];
-            store_pack<T, PER>(to + i, pack<T, PER>(x));
+            if (i < there) store_pack<T, PER>(to + i, pack<T, PER>(x));
         }
     } else {
 #pragma unroll
@@ -103,14 +113,25 @@ __device__ __forceinline__ void store_row(T* to, int there, bool wide, const flo
             if (i < there) to[i] = from_float<T>(f[i]);
     }
 }
-// The same into rows of fp32 that are whole multiples of 16 columns.
+// What a pass keeps of a piece lies as [V/4][rows][4], so that the lanes of a warp, a row each, write and read whole lines (rows of V as they come: every
+// access of a warp touched 32 lines, and a training step's walks waited twice as long for their stores as for everything else).
+__device__ __forceinline__ size_t quad_at(size_t unit, int VP, int rows, int v, int row) { return unit * ((size_t)rows * VP) + ((size_t)(v >> 2) * rows + row) * 4; }
 template <int N>
-__device__ __forceinline__ void save_row(float* to, int there, const float (&f)[N])
+__device__ __forceinline__ void save_row(float* to, int rows, int there, const float (&f)[N])
 {
 #pragma unroll
     for (int i = 0; i < N; i += 4)
-        if (i < there) *reinterpret_cast<float4*>(to + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+        if (i < there) *reinterpret_cast<float4*>(to + (size_t)i * rows) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
 }
+template <int N>
+struct SavedRow {
+    Pack<float, 4> q[N / 4];
+    __device__ __forceinline__ void load(const float* from, int rows, int there)
+    {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) q[i] = load_masked<float, 4>(from + (size_t)i * 4 * rows, 4 * i < there);
+    }
+};
 
 // Rows of zeros behind a sequence: columns 0 .. cols - 1 of rows first .. L - 1.
 template <typename T>
@@ -125,7 +146,20 @@ struct WalkBars {
     uint32_t tmem, abort;
 };
 
-// The sum of products of parts, those of the last digits first: A has `a_parts` parts, B `b_parts`; `ks` steps of 16 along K.  `more`: onto what is there.
+// Products of parts with B's three side by side along N: part p of A, of `a_parts`, with the first 3 - p of B onto the digits from p on.  A is read once for
+// each of its parts so (it is A's 4 KB that an MMA waits for while N is below 128: with every pair of parts an MMA of its own the three
+// products of a piece took 2.4 times as long), and small terms are not added to large ones before the end.
+template <int NV, bool A_BY_M, bool B_BY_N, typename DescA, typename DescB>
+__device__ __forceinline__ void multiply_digits(uint32_t d, int a_parts, int ks, uint32_t elected, DescA desc_a, DescB desc_b)
+{
+#pragma unroll
+    for (int p = 0; p < a_parts; ++p) {
+        const uint32_t idesc = ptx::idesc_b16(128, (kSum - p) * NV, false) | (A_BY_M ? kIdescAMajorM : 0) | (B_BY_N ? ptx::kIdescBMajorMN : 0);
+#pragma unroll
+        for (int k = 0; k < ks; ++k) ptx::mma_b16(d + p * NV, desc_a(p, k), desc_b(k), idesc, p + k > 0, elected);
+    }
+}
+// The same one after the other onto one place, those of the last digits first; B has `b_parts` parts.  `more`: onto what is there.
 template <typename DescA, typename DescB>
 __device__ __forceinline__ void multiply(uint32_t d, int a_parts, int b_parts, int ks, uint32_t idesc, uint32_t elected, bool more, DescA desc_a, DescB desc_b)
 {
@@ -144,14 +178,14 @@ __device__ __forceinline__ void multiply(uint32_t d, int a_parts, int b_parts, i
 }
 
 // Columns a block walks with: 32, or 64 where those are fewer rounds of the machine's SMs (a piece takes about half as long again then).  Keys of 128 fp32 numbers, in
-// three parts, leave room for 32.
+// three parts, leave room for 32, and rows that rule out accesses of 16 bytes are walked with 32.
 template <typename T>
-int delta_columns(const DeltaArgs& a)
+int delta_columns(const DeltaArgs& a, bool wide)
 {
-    if (a.V <= 32 || (sizeof(T) == 4 && a.K > 64)) return 32;
+    if (!wide || a.V <= 32 || (sizeof(T) == 4 && a.K > 64)) return 32;
     const long long heads = (long long)a.B * a.H, sms = sm_count();
-    const long long narrow = (heads * ceil_div_u(a.V, 32) + sms - 1) / sms, wide = (heads * ceil_div_u(a.V, 64) + sms - 1) / sms;
-    const int dflt = 3 * wide <= 2 * narrow ? 64 : 32;
+    const long long by32 = (heads * ceil_div_u(a.V, 32) + sms - 1) / sms, by64 = (heads * ceil_div_u(a.V, 64) + sms - 1) / sms;
+    const int dflt = 3 * by64 <= 2 * by32 ? 64 : 32;
     return env_int("CONV2D_B200_DELTA_COLUMNS", dflt) == 64 ? 64 : 32;
 }
 

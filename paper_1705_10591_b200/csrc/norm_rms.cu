@@ -114,9 +114,9 @@ __global__ void __launch_bounds__(1024) rms_fwd_kernel(const RmsArgs a, Runs gro
     for (int j = 0; j < NP; ++j) {
         const int p = threadIdx.x + j * blockDim.x;
         const bool there = real && p < packs;
-        px[j] = there ? load_pack<T, V>(x + p * V) : zero_pack<T, V>();
-        if (a.residual) pr[j] = there ? load_pack<T, V>(res + p * V) : zero_pack<T, V>();
-        if (a.z) pz[j] = there ? load_pack<T, V>(static_cast<const T*>(a.z) + row * a.ldz + p * V) : zero_pack<T, V>();
+        px[j] = load_masked<T, V>(x + p * V, there);
+        if (a.residual) pr[j] = load_masked<T, V>(res + p * V, there);
+        if (a.z) pz[j] = load_masked<T, V>(static_cast<const T*>(a.z) + row * a.ldz + p * V, there);
     }
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
@@ -203,11 +203,11 @@ __global__ void __launch_bounds__(1024) rms_bwd_kernel(const RmsArgs a, Runs gro
         for (int j = 0; j < NP; ++j) {
             const int p = threadIdx.x + j * blockDim.x;
             const bool there = real && p < packs;
-            ph[j] = there ? load_pack<T, V>(static_cast<const T*>(a.x) + row * a.ldx + p * V) : zero_pack<T, V>();
-            py[j] = there ? load_pack<T, V>(static_cast<const T*>(a.dy) + row * a.lddy + p * V) : zero_pack<T, V>();
-            if (a.dh) pd[j] = there ? load_pack<T, V>(static_cast<const T*>(a.dh) + row * a.lddh + p * V) : zero_pack<T, V>();
-            if (a.z) pz[j] = there ? load_pack<T, V>(static_cast<const T*>(a.z) + row * a.ldz + p * V) : zero_pack<T, V>();
-            r[j] = there ? a.rstd_in[row * a.G + group[j]] : 0.f;
+            ph[j] = load_masked<T, V>(static_cast<const T*>(a.x) + row * a.ldx + p * V, there);
+            py[j] = load_masked<T, V>(static_cast<const T*>(a.dy) + row * a.lddy + p * V, there);
+            if (a.dh) pd[j] = load_masked<T, V>(static_cast<const T*>(a.dh) + row * a.lddh + p * V, there);
+            if (a.z) pz[j] = load_masked<T, V>(static_cast<const T*>(a.z) + row * a.ldz + p * V, there);
+            r[j] = load_masked<float, 1>(a.rstd_in + row * a.G + group[j], there).e[0];
         }
 #pragma unroll
         for (int j = 0; j < NP; ++j) {

@@ -1,7 +1,7 @@
 // Arguments of the RMS norm's launchers, as the entry points check them.
 #pragma once
 
-#include "seq_common.cuh"
+#include "masked_load.cuh"
 #include "recurrent_b200.h"
 
 namespace conv2d_b200 {
