@@ -14,12 +14,13 @@ namespace {
 template <typename T, int KD, int NV, bool WIDE>
 __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const DeltaArgs a, int across)
 {
-    using W = Walk<T, KD, NV>;
+    using W = Walk<T, KD, NV, 2 * kPiece>;
     constexpr int IN = W::IN, C = W::C, STAGES = W::stages;
     extern __shared__ unsigned char unaligned[];
     unsigned char* raw = unaligned + ((1024 - (ptx::smem_u32(unaligned) & 1023)) & 1023);
-    unsigned char *squares = raw + STAGES * W::keys, *state = squares + W::squares, *rows = state + W::state;
-    WalkBars* bars = reinterpret_cast<WalkBars*>(rows + kSum * W::rows_part);
+    unsigned char *squares = raw + STAGES * W::keys, *values = squares + W::at_values, *rows = values - kSum * W::rows_part, *state = rows - W::state;
+    unsigned char* outputs = values + W::values;
+    WalkBars* bars = reinterpret_cast<WalkBars*>(squares + W::squares);
     volatile uint32_t* abort_flag = &bars->abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int v0 = (int)(blockIdx.x % across) * NV, bh = blockIdx.x / across, h = bh % a.H, b = bh / a.H, hk = h / a.share;
@@ -53,7 +54,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
         auto load_squares = [&](int s) {
             if (!elected || s >= pieces) return;
             ptx::mbar_arrive_expect_tx(&bars->squares, W::squares);
-            ptx::bulk_g2s(squares, a.squares + (unit0 + pieces - 1 - s) * kSquares, W::squares, &bars->squares);
+            ptx::bulk_g2s(squares, a.prepared + (unit0 + pieces - 1 - s) * kPrepared, W::squares, &bars->squares);
         };
         const uint32_t s_squares = ptx::smem_u32(squares), s_state = ptx::smem_u32(state), s_rows = ptx::smem_u32(rows);
         load_keys(0), load_squares(0);
@@ -72,7 +73,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
                 if (STAGES == 2 && s > 0) load_keys(s + 1);
             }
             alive = alive && ptx::mbar_wait_bounded_warp(&bars->squares, s & 1, abort_flag, a.max_polls);
-            __syncthreads();                                   // beta X and scale dO are there
+            __syncthreads();                                   // beta X and scale dO are there, dO has been read
             ptx::tc_fence_after_sync();
             if (alive) {                                       // (64 rows; the other 64 of the result are of whatever lies behind, and not read)
                 multiply_digits<NV, false, true>(tmem + 3 * NV, kSum, 2 * kPiece / 16, elected,
@@ -93,7 +94,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
                 }
             }
         }
-    } else {
+    } else if (warp < kWorkers / 32) {
         const int quarter = warp & 3, row = quarter * 32 + lane, col0 = (warp >> 2) * C, token = row & (kPiece - 1), v = v0 + col0;
         const bool is_key = row < kPiece;                      // a token of K (its E and dV), or of Q (its dO); and row `row` of dS
         const uint32_t at = tmem + ((uint32_t)quarter << 21) + col0;
@@ -102,18 +103,10 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
         const size_t state0 = ((size_t)bh * a.K + row) * a.V + v;
 #pragma unroll
         for (int j = 0; j < C; ++j) S[j] = a.dstate_out && row < a.K && j < there ? a.dstate_out[state0 + j] : 0.f;
-        const T* dout = static_cast<const T*>(a.dout) + ((long long)b * a.L + token) * a.lddo + (long long)h * a.V + v;
-        T* dv = static_cast<T*>(a.dv) + ((long long)b * a.L + token) * a.lddv + (long long)h * a.V + v;
-        const float* factors = a.factors + unit0 * (kFactors * kPiece);
+        const float* factors = reinterpret_cast<const float*>(squares + kSquares);
         SavedRow<C> update;                                    // E
-        Row<T, C> grad;                                        // dO
-        float eg = 0.f, ed = 0.f, beta = 0.f, whole = 0.f;
         auto fetch = [&](int i) {
-            if (i < 0) return;
-            const float* f = factors + (size_t)i * (kFactors * kPiece);
-            eg = f[token], ed = f[kPiece + token], beta = f[2 * kPiece + token], whole = f[kPiece - 1];
-            if (is_key) update.load(a.updates + quad_at(unit0 + i, a.VP, kPiece, v, token), kPiece, saved);
-            else grad.template load<WIDE>(dout + (long long)i * kPiece * a.lddo, i * kPiece + token < len ? there : 0);
+            if (i >= 0 && is_key) update.load(a.updates + quad_at(unit0 + i, a.VP, kPiece, v, token), kPiece, saved);
         };
         auto put_state = [&](int i) {                          // dS behind piece i
             if (row < KD) {
@@ -128,8 +121,10 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             const uint32_t parity = (pieces - 1 - i) & 1;
             ptx::tc_fence_before_sync();
             __syncthreads();
+            ptx::mbar_wait_bounded(&bars->squares, parity, abort_flag, a.max_polls);
+            const float eg = factors[token], ed = factors[kPiece + token], beta = factors[2 * kPiece + token], whole = factors[kPiece - 1];
             if (!is_key) {
-                grad.get(y);
+                Tile<T, NV>::get(values, token, col0, y);
 #pragma unroll
                 for (int j = 0; j < C; ++j) y[j] *= a.scale;
                 put_row<NV, C>(rows, W::rows_part, row, col0, y);
@@ -170,21 +165,20 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             if (is_key) {
                 const size_t unit = unit0 + i;
                 save_row<C>(a.dupdates + quad_at(unit, a.VP, kPiece, v, token), kPiece, saved, X);
-                if (i * kPiece + token < len) store_row<WIDE>(dv + (long long)i * kPiece * a.lddv, there, X);
+                Tile<T, NV>::put(outputs, token, col0, X);
                 if (saved > 0) {                               // (a sum over 32 columns stands for two of 16)
                     float* part = a.dbeta_parts + (unit * (a.VP / 16) + v / 16) * kPiece + token;
                     part[0] = sum;
                     if (C == 32 && saved > 16) part[kPiece] = 0.f;
                 }
             }
-            const float keep = whole;
             fetch(i - 1);
             // D3: dS <- e^G_63 dS + ..
             ptx::mbar_wait_bounded(&bars->done[2], parity, abort_flag, a.max_polls);
             ptx::tc_fence_after_sync();
             tmem_digits<C>(at, NV, y);
 #pragma unroll
-            for (int j = 0; j < C; ++j) S[j] = fmaf(keep, S[j], y[j]);
+            for (int j = 0; j < C; ++j) S[j] = fmaf(whole, S[j], y[j]);
             if (i > 0) put_state(i - 1);
         }
         if (a.dstate_in && row < a.K) {
@@ -193,6 +187,11 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
                 if (j < there) a.dstate_in[state0 + j] = S[j];
         }
         zero_rows(static_cast<T*>(a.dv) + (long long)b * a.L * a.lddv + (long long)h * a.V + v0, a.lddv, len, a.L, min(NV, a.V - v0), tid, kWorkers);
+    } else {
+        const long long row0 = (long long)b * a.L, first = (long long)h * a.V + v0;
+        move_values<T, NV, WIDE, true>(static_cast<const T*>(a.dout) + row0 * a.lddo + first, a.lddo, static_cast<T*>(a.dv) + row0 * a.lddv + first, a.lddv, values, outputs, len,
+                                       pieces, a.V - v0, tid - kPieceThreads);
+        return;
     }
     ptx::tc_fence_before_sync();
     __syncthreads();
@@ -227,7 +226,7 @@ struct PieceBars {
 };
 
 template <typename T, int KD, bool WIDE>
-__global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_pieces_kernel(const DeltaArgs a)
+__global__ void __launch_bounds__(kPieceThreads, 1) delta_bwd_pieces_kernel(const DeltaArgs a)
 {
     using W = Piecewise<T, KD>;
     constexpr int IN = W::IN, NB = W::NB;
@@ -246,12 +245,12 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_pieces_kernel(const
     // padding
     if (live < there) {
         const int first = max(live, 0);
-        for (int i = tid; i < (there - first) * a.K; i += kWalkThreads) {
+        for (int i = tid; i < (there - first) * a.K; i += kPieceThreads) {
             const int row = first + i / a.K, col = i % a.K;
             if (shared_key) a.dq_parts[part0 + (long long)row * a.H * a.K + col] = 0.f, a.dk_parts[part0 + (long long)row * a.H * a.K + col] = 0.f;
             else dq[row * a.lddq + col] = from_float<T>(0.f), dk[row * a.lddk + col] = from_float<T>(0.f);
         }
-        for (int i = first + tid; i < there; i += kWalkThreads) a.dg[(row0 + i) * a.lddg + h] = 0.f, a.dbeta[(row0 + i) * a.lddbeta + h] = 0.f;
+        for (int i = first + tid; i < there; i += kPieceThreads) a.dg[(row0 + i) * a.lddg + h] = 0.f, a.dbeta[(row0 + i) * a.lddbeta + h] = 0.f;
     }
     if (live <= 0) return;
 
@@ -265,7 +264,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_pieces_kernel(const
         ptx::tmem_alloc(&bars.tmem, W::cols);
         ptx::tmem_relinquish();
     }
-    for (int i = tid; i < kFactors * kPiece; i += kWalkThreads) bars.factors[i] = a.factors[unit * (kFactors * kPiece) + i];
+    for (int i = tid; i < kFactors * kPiece; i += kPieceThreads) bars.factors[i] = reinterpret_cast<const float*>(a.prepared + unit * kPrepared + kSquares)[i];
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
@@ -462,7 +461,7 @@ __global__ void __launch_bounds__(256) delta_bwd_shared_kernel(const DeltaArgs a
 template <typename T, int KD, int NV, bool WIDE>
 conv2d_status_t backward_walk(const DeltaArgs& a, cudaStream_t stream)
 {
-    using W = Walk<T, KD, NV>;
+    using W = Walk<T, KD, NV, 2 * kPiece>;
     static SmemLimit limit;
     const int across = (int)ceil_div_u(a.V, NV);
     if (raise_smem_limit((const void*)delta_bwd_walk_kernel<T, KD, NV, WIDE>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
@@ -478,7 +477,7 @@ conv2d_status_t backward_pieces(const DeltaArgs& a, cudaStream_t stream)
     using W = Piecewise<T, KD>;
     static SmemLimit limit;
     if (raise_smem_limit((const void*)delta_bwd_pieces_kernel<T, KD, WIDE>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-    if (launch_pdl(delta_bwd_pieces_kernel<T, KD, WIDE>, dim3((unsigned)(a.B * a.H) * (unsigned)a.pieces), dim3(kWalkThreads), W::smem, stream, a) != cudaSuccess)
+    if (launch_pdl(delta_bwd_pieces_kernel<T, KD, WIDE>, dim3((unsigned)(a.B * a.H) * (unsigned)a.pieces), dim3(kPieceThreads), W::smem, stream, a) != cudaSuccess)
         return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;
@@ -526,7 +525,7 @@ conv2d_status_t launch_delta_bwd(DeltaArgs a, conv2d_operand_t type, const void*
     if (device_timeout_word(&a.timeout) != cudaSuccess) return CONV2D_ERR_CUDA;
     a.max_polls = (unsigned)env_int("CONV2D_B200_DELTA_MAX_POLLS", 1 << 22);
     unsigned char* kept = const_cast<unsigned char*>(static_cast<const unsigned char*>(states));      // (only read)
-    a.squares = kept, a.factors = reinterpret_cast<float*>(kept + l.units * kSquares);
+    a.prepared = kept;
     a.states = reinterpret_cast<float*>(kept + l.prepared_bytes());
     a.updates = reinterpret_cast<float*>(kept + l.prepared_bytes() + l.units * l.state());
     unsigned char* at = static_cast<unsigned char*>(workspace);

@@ -149,7 +149,8 @@ __device__ __forceinline__ void mma_parts(float (&c0)[4], float (&c1)[4], const 
 
 // Where things lie in what the forward pass leaves (`states`) and in workspaces.  A "unit" is one piece of one head of one sequence, number
 // (b * H + h) * pieces + c; a "key unit" the same of a key head.  Sections in this order, sizes in bytes for each unit:
-constexpr size_t kSquares = (size_t)kSum * 2 * kPiece * kPiece * 2;      // [-t^T | P'^T], [part][two][64][64], units of 16 bytes swizzled as unit_at does
+constexpr size_t kSquares = (size_t)kSum * 2 * kPiece * kPiece * 2;      // [-t^T | P'^T], [part][two][64][64], units of 16 bytes swizzled as unit_at does;
+constexpr size_t kPrepared = kSquares + kFactors * kPiece * 4;           // and the factors behind them
 struct DeltaLayout {
     int B, L, Hk, H, K, V, KD, VP, pieces, in;                   // KD: K rounded up to 64 or 128; VP: V to 16
     size_t units, keys;                                          // pieces of all value heads, of all key heads
@@ -158,7 +159,7 @@ struct DeltaLayout {
           in(parts_in(type)), units((size_t)B_ * H_ * pieces), keys((size_t)B_ * Hk_ * pieces)
     {
     }
-    size_t prepared_bytes() const { return units * (kSquares + kFactors * kPiece * 4); }
+    size_t prepared_bytes() const { return units * kPrepared; }
     size_t state() const { return (size_t)KD * VP * 4; }                             // S or its gradient, [V/4][K][4]
     size_t update() const { return (size_t)kPiece * VP * 4; }                        // E or dV, [V/4][token][4]
     size_t saved_bytes() const { return units * (state() + update()); }
@@ -176,8 +177,7 @@ struct DeltaArgs {
     int B, L, Hk, H, K, V, share, pieces, VP;
     long long ldq, ldk, ldv, ldg, ldbeta, ldo, lddo, lddq, lddk, lddv, lddg, lddbeta;
     float scale;
-    unsigned char *squares, *keys;    // tiles of units and of key units
-    float* factors;               // [unit][kFactors][64]
+    unsigned char *prepared, *keys;   // of units, and tiles of key units
     float *states, *updates;      // saved by the forward pass: [unit][VP/4][KD][4], [unit][VP/4][64][4]; NULL: not wanted
     float *dstates, *dupdates;    // the same of their gradients (dS after the piece, dV)
     float* dbeta_parts;           // [unit][VP / 16][64]

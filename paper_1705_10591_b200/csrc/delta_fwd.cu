@@ -7,12 +7,13 @@ namespace {
 template <typename T, int KD, int NV, bool WIDE>
 __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaArgs a, int across)
 {
-    using W = Walk<T, KD, NV>;
+    using W = Walk<T, KD, NV, kPiece>;
     constexpr int IN = W::IN, C = W::C, STAGES = W::stages;
     extern __shared__ unsigned char unaligned[];
     unsigned char* raw = unaligned + ((1024 - (ptx::smem_u32(unaligned) & 1023)) & 1023);
-    unsigned char *squares = raw + STAGES * W::keys, *state = squares + W::squares, *rows = state + W::state;
-    WalkBars* bars = reinterpret_cast<WalkBars*>(rows + kSum * W::rows_part);
+    unsigned char *squares = raw + STAGES * W::keys, *values = squares + W::at_values, *rows = values - kSum * W::rows_part, *state = rows - W::state;
+    unsigned char* outputs = values + W::values;
+    WalkBars* bars = reinterpret_cast<WalkBars*>(squares + W::squares);
     volatile uint32_t* abort_flag = &bars->abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int v0 = (int)(blockIdx.x % across) * NV, bh = blockIdx.x / across, h = bh % a.H, b = bh / a.H, hk = h / a.share;
@@ -46,7 +47,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
         auto load_squares = [&](int i) {
             if (!elected || i >= pieces) return;
             ptx::mbar_arrive_expect_tx(&bars->squares, W::squares);
-            ptx::bulk_g2s(squares, a.squares + (unit0 + i) * kSquares, W::squares, &bars->squares);
+            ptx::bulk_g2s(squares, a.prepared + (unit0 + i) * kPrepared, W::squares, &bars->squares);
         };
         const uint32_t s_squares = ptx::smem_u32(squares), s_state = ptx::smem_u32(state), s_rows = ptx::smem_u32(rows);
         load_keys(0), load_squares(0);
@@ -66,7 +67,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
                 if (STAGES == 2 && i > 0) load_keys(i + 1);
             }
             alive = alive && ptx::mbar_wait_bounded_warp(&bars->squares, i & 1, abort_flag, a.max_polls);
-            __syncthreads();                                   // beta R is there
+            __syncthreads();                                   // beta R is there, the values have been read
             ptx::tc_fence_after_sync();
             if (alive) {
                 multiply_digits<NV, true, true>(tmem + 3 * NV, kSum, kPiece / 16, elected,
@@ -87,7 +88,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
                 }
             }
         }
-    } else {
+    } else if (warp < kWorkers / 32) {
         const int quarter = warp & 3, row = quarter * 32 + lane, col0 = (warp >> 2) * C, token = row & (kPiece - 1), v = v0 + col0;
         const bool is_key = row < kPiece;                      // a token of K, or of Q; and row `row` of S
         const uint32_t at = tmem + ((uint32_t)quarter << 21) + col0;
@@ -96,17 +97,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
         const size_t state0 = ((size_t)bh * a.K + row) * a.V + v;
 #pragma unroll
         for (int j = 0; j < C; ++j) S[j] = a.state_in && row < a.K && j < there ? a.state_in[state0 + j] : 0.f;
-        const T* values = static_cast<const T*>(a.v) + ((long long)b * a.L + token) * a.ldv + (long long)h * a.V + v;
-        T* out = static_cast<T*>(a.o) + ((long long)b * a.L + token) * a.ldo + (long long)h * a.V + v;
-        const float* factors = a.factors + unit0 * (kFactors * kPiece);
-        Row<T, C> next;
-        float eg = 0.f, ed = 0.f, beta = 0.f, whole = 0.f;
-        auto fetch = [&](int i) {                              // this token's value (of keys) and factors
-            if (i >= pieces) return;
-            const float* f = factors + (size_t)i * (kFactors * kPiece);
-            eg = f[token], ed = f[kPiece + token], beta = f[2 * kPiece + token], whole = f[kPiece - 1];
-            if (is_key) next.template load<WIDE>(values + (long long)i * kPiece * a.ldv, i * kPiece + token < len ? there : 0);
-        };
+        const float* factors = reinterpret_cast<const float*>(squares + kSquares);
         auto put_state = [&](int i) {                          // S before piece i, for its product and for the backward pass
             if (row < KD) {
                 put_row<NV, C>(state, W::state_part, row, col0, S);
@@ -115,18 +106,19 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
             ptx::fence_proxy_async_smem();
         };
         if (pieces > 0) put_state(0);
-        fetch(0);
         for (int i = 0; i < pieces; ++i) {
             const uint32_t parity = i & 1;
             ptx::tc_fence_before_sync();
             __syncthreads();
             // D1: of keys R = v - e^G k S, of queries e^G q S
+            ptx::mbar_wait_bounded(&bars->squares, parity, abort_flag, a.max_polls);
+            const float eg = factors[token], ed = factors[kPiece + token], beta = factors[2 * kPiece + token], whole = factors[kPiece - 1];
             ptx::mbar_wait_bounded(&bars->done[0], parity, abort_flag, a.max_polls);
             ptx::tc_fence_after_sync();
             tmem_digits<C>(at, NV, X);
             if (is_key) {
                 float y[C];
-                next.get(y);
+                Tile<T, NV>::get(values, token, col0, y);
 #pragma unroll
                 for (int j = 0; j < C; ++j) X[j] = fmaf(-eg, X[j], y[j]), y[j] = beta * X[j];
                 put_row<NV, C>(rows, W::rows_part, row, col0, y);
@@ -155,19 +147,17 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
             __syncthreads();
             if (is_key) {
                 if (a.updates) save_row<C>(a.updates + quad_at(unit0 + i, a.VP, kPiece, v, token), kPiece, saved, X);
-            } else if (i * kPiece + token < len) {
+            } else {
 #pragma unroll
                 for (int j = 0; j < C; ++j) X[j] *= a.scale;
-                store_row<WIDE>(out + (long long)i * kPiece * a.ldo, there, X);
+                Tile<T, NV>::put(outputs, token, col0, X);
             }
-            const float keep = whole;
-            fetch(i + 1);
             // D3, in D1's place: S <- e^G_63 S + K^T (..)
             ptx::mbar_wait_bounded(&bars->done[2], parity, abort_flag, a.max_polls);
             ptx::tc_fence_after_sync();
             tmem_digits<C>(at, NV, y);
 #pragma unroll
-            for (int j = 0; j < C; ++j) S[j] = fmaf(keep, S[j], y[j]);
+            for (int j = 0; j < C; ++j) S[j] = fmaf(whole, S[j], y[j]);
             if (i + 1 < pieces) put_state(i + 1);
         }
         if (a.state_out && row < a.K) {
@@ -176,6 +166,11 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
                 if (j < there) a.state_out[state0 + j] = S[j];
         }
         zero_rows(static_cast<T*>(a.o) + (long long)b * a.L * a.ldo + (long long)h * a.V + v0, a.ldo, len, a.L, min(NV, a.V - v0), tid, kWorkers);
+    } else {
+        const long long row0 = (long long)b * a.L, col0 = (long long)h * a.V + v0;
+        move_values<T, NV, WIDE, false>(static_cast<const T*>(a.v) + row0 * a.ldv + col0, a.ldv, static_cast<T*>(a.o) + row0 * a.ldo + col0, a.ldo, values, outputs, len, pieces,
+                                        a.V - v0, tid - kPieceThreads);
+        return;
     }
     ptx::tc_fence_before_sync();
     __syncthreads();
@@ -189,7 +184,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
 template <typename T, int KD, int NV, bool WIDE>
 conv2d_status_t walk(const DeltaArgs& a, cudaStream_t stream)
 {
-    using W = Walk<T, KD, NV>;
+    using W = Walk<T, KD, NV, kPiece>;
     static SmemLimit limit;
     const int across = (int)ceil_div_u(a.V, NV);
     if (raise_smem_limit((const void*)delta_fwd_kernel<T, KD, NV, WIDE>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
@@ -228,7 +223,7 @@ conv2d_status_t launch_delta_fwd(DeltaArgs a, conv2d_operand_t type, void* state
     a.max_polls = (unsigned)env_int("CONV2D_B200_DELTA_MAX_POLLS", 1 << 22);
     // (sections of whole multiples of 16 bytes)
     unsigned char* at = static_cast<unsigned char*>(states ? states : workspace);
-    a.squares = at, a.factors = reinterpret_cast<float*>(at + l.units * kSquares);
+    a.prepared = at;
     if (states) {
         a.states = reinterpret_cast<float*>(at + l.prepared_bytes());
         a.updates = reinterpret_cast<float*>(at + l.prepared_bytes() + l.units * l.state());

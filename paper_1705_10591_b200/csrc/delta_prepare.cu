@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a
         const int h = hk * a.share + r;
         const size_t unit = ((size_t)b * a.H + h) * a.pieces + piece;
         if (warp == 0) {
-            float* factors = a.factors + unit * (kFactors * kPiece);
+            float* factors = reinterpret_cast<float*>(a.prepared + unit * kPrepared + kSquares);
             // (below -10000 taken as that: sums of infinities would have no differences; NaN stays)
             const double x[2] = {gate.x < -10000.f ? -10000.f : gate.x, gate.y < -10000.f ? -10000.f : gate.y};
             const float be[2] = {beta.x, beta.y};
@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a
         ptx::fence_proxy_async_smem();
         __syncthreads();
         if (tid == 0) {
-            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(a.squares + unit * kSquares), "r"(base), "n"((int)kSquares) : "memory");
+            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(a.prepared + unit * kPrepared), "r"(base), "n"((int)kSquares) : "memory");
             ptx::bulk_commit_group();
         }
     }

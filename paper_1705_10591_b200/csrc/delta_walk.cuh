@@ -6,22 +6,26 @@
 //   D2 [128] = [-t; P'] (beta R)   both lie transposed, as rows of tokens j with 64 numbers each: M-major
 //   D3 [128] = K^T (..)            the tile of K read the other way (M-major)
 // Eight warps own a quarter of the 128 rows and one half of the columns each: a thread has one row of D1 and D2 (a token of K or of Q) and of S (a number of
-// K).  A ninth warp issues the products and the copies of the next piece's tiles.
+// K).  A ninth warp issues the products and the copies of the next piece's tiles, and three more move values and outputs between their tensors and shared memory, whole
+// lines at a time.  (Threads that fetched and stored their rows themselves, 32 lines an access, held the memory pipe for 600 cycles of a piece; a bulk
+// copy for each row took twice as long again.)
 #pragma once
 
 #include "delta_common.cuh"
 
 namespace conv2d_b200 {
 
-constexpr int kWorkers = 256, kWalkThreads = kWorkers + 32;
+constexpr int kWorkers = 256, kMovers = 96, kPieceThreads = kWorkers + 32, kWalkThreads = kPieceThreads + kMovers;
 
-template <typename T, int KD, int NV>
+template <typename T, int KD, int NV, int ROWS>
 struct Walk {
     static constexpr int IN = Parts<T>::in, HALF = 2 * kPiece * 128;              // bytes of 64 numbers of [K; Q]
     static constexpr int keys = IN * (KD / 64) * HALF, key_part = (KD / 64) * HALF, square_part = 2 * kPiece * 128;
-    static constexpr int state_part = KD * NV * 2, rows_part = 2 * kPiece * NV * 2;      // S, and up to 128 rows of what D2 and D3 are products with
-    static constexpr int squares = (int)kSquares, state = kSum * state_part;
-    static constexpr int rest = squares + state + kSum * rows_part + 1024;        // (1024: barriers)
+    static constexpr int state_part = KD * NV * 2, rows_part = ROWS * NV * 2;     // S, and the ROWS rows of what D2 and D3 are products with
+    static constexpr int state = kSum * state_part, values = kPiece * NV * (int)sizeof(T);
+    // squares with their factors (and the barriers, to the next boundary of the swizzle), S, rows, values that come and go
+    static constexpr int squares = (int)kPrepared, at_values = (squares + 128 + 1023) / 1024 * 1024 + state + kSum * rows_part;
+    static constexpr int rest = at_values + 2 * values;
     static constexpr int stages = 2 * keys + rest <= 232448 - 1024 ? 2 : 1;
     static constexpr int smem = stages * keys + rest + 1024;                      // (1024: to the first boundary of the swizzle)
     static constexpr int cols = NV == 32 ? 256 : 512;                             // of tensor memory: twice three times NV, to a power of two
@@ -140,11 +144,113 @@ __device__ __forceinline__ void zero_rows(T* to, long long ld, int first, int L,
     for (long long i = id; i < (long long)(L - first) * cols; i += threads) to[(first + i / cols) * ld + i % cols] = from_float<T>(0.f);
 }
 
-// Barriers of a block, behind its tiles.
+// Barriers of a block, 128 bytes at most.
 struct WalkBars {
     uint64_t keys[2], squares, done[3];
     uint32_t tmem, abort;
 };
+
+// Tiles of 64 tokens x NV elements as they lie in their tensor, in units of 16 bytes swizzled like the operands.
+template <typename T, int NV>
+struct Tile {
+    static constexpr int PER = 16 / (int)sizeof(T), UNITS = NV / PER, EACH = (kPiece * UNITS + kMovers - 1) / kMovers;
+    static __device__ __forceinline__ uint32_t at(int row, int unit) { return unit_at<8 * UNITS>(0, row, unit); }
+    // N elements of a row
+    template <int N>
+    static __device__ __forceinline__ void get(const unsigned char* tile, int row, int col, float (&f)[N])
+    {
+#pragma unroll
+        for (int j = 0; j < N; j += PER) {
+            float z[PER];
+            unpack(load_pack<T, PER>(reinterpret_cast<const T*>(tile + at(row, (col + j) / PER))), z);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) f[j + e] = z[e];
+        }
+    }
+    template <int N>
+    static __device__ __forceinline__ void put(unsigned char* tile, int row, int col, const float (&f)[N])
+    {
+#pragma unroll
+        for (int j = 0; j < N; j += PER) {
+            float z[PER];
+#pragma unroll
+            for (int e = 0; e < PER; ++e) z[e] = f[j + e];
+            store_pack<T, PER>(reinterpret_cast<T*>(tile + at(row, (col + j) / PER)), pack<T, PER>(z));
+        }
+    }
+};
+// What a moving thread has under way of one tile; `id` of kMovers.
+template <typename T, int NV, bool WIDE>
+struct Mover {
+    using L = Tile<T, NV>;
+    Pack<T, L::PER> p[L::EACH];
+    __device__ __forceinline__ void fetch(const T* from, long long ld, int rows, int cols, int id)
+    {
+        if (!WIDE) return;
+#pragma unroll
+        for (int j = 0; j < L::EACH; ++j) {
+            const int u = id + j * kMovers, row = u / L::UNITS, col = u % L::UNITS * L::PER;
+            p[j] = load_masked<T, L::PER>(from + row * ld + col, row < rows && col < cols);
+        }
+    }
+    // into the tile: zeros behind the last row and column
+    __device__ __forceinline__ void put(unsigned char* tile, const T* from, long long ld, int rows, int cols, int id)
+    {
+        if (WIDE) {
+#pragma unroll
+            for (int j = 0; j < L::EACH; ++j) {
+                const int u = id + j * kMovers;
+                if (u < kPiece * L::UNITS) store_pack<T, L::PER>(reinterpret_cast<T*>(tile + L::at(u / L::UNITS, u % L::UNITS)), p[j]);
+            }
+        } else {
+#pragma unroll 4
+            for (int i = id; i < kPiece * NV; i += kMovers) {
+                const int row = i / NV, col = i % NV;
+                *reinterpret_cast<T*>(tile + L::at(row, col / L::PER) + col % L::PER * sizeof(T)) = load_masked<T, 1>(from + row * ld + col, row < rows && col < cols).e[0];
+            }
+        }
+    }
+    static __device__ __forceinline__ void store(T* to, long long ld, const unsigned char* tile, int rows, int cols, int id)
+    {
+        if (WIDE) {
+#pragma unroll
+            for (int j = 0; j < L::EACH; ++j) {
+                const int u = id + j * kMovers, row = u / L::UNITS, col = u % L::UNITS * L::PER;
+                if (row < rows && col < cols) store_pack<T, L::PER>(to + row * ld + col, load_pack<T, L::PER>(reinterpret_cast<const T*>(tile + L::at(row, col / L::PER))));
+            }
+        } else {
+            for (int i = id; i < kPiece * NV; i += kMovers) {
+                const int row = i / NV, col = i % NV;
+                if (row < rows && col < cols) to[row * ld + col] = *reinterpret_cast<const T*>(tile + L::at(row, col / L::PER) + col % L::PER * sizeof(T));
+            }
+        }
+    }
+};
+// The moving warps' part of a walk over `pieces` pieces, from the first on or from the last back, with the same three barriers a piece: values are fetched a piece
+// ahead and put when they have been read, outputs are stored a piece later.
+template <typename T, int NV, bool WIDE, bool BACK>
+__device__ __forceinline__ void move_values(const T* from, long long ldfrom, T* to, long long ldto, unsigned char* values, const unsigned char* outputs, int len, int pieces,
+                                            int cols, int id)
+{
+    Mover<T, NV, WIDE> m;
+    auto piece = [&](int s) { return BACK ? pieces - 1 - s : s; };
+    auto row = [&](int s) { return (long long)piece(s) * kPiece; };
+    auto rows = [&](int s) { return min(len - piece(s) * kPiece, kPiece); };
+    if (pieces > 0) {
+        m.fetch(from + row(0) * ldfrom, ldfrom, rows(0), cols, id);
+        m.put(values, from + row(0) * ldfrom, ldfrom, rows(0), cols, id);
+    }
+    for (int s = 0; s < pieces; ++s) {
+        __syncthreads();
+        if (s + 1 < pieces) m.fetch(from + row(s + 1) * ldfrom, ldfrom, rows(s + 1), cols, id);
+        if (s > 0) m.store(to + row(s - 1) * ldto, ldto, outputs, rows(s - 1), cols, id);
+        __syncthreads();
+        if (s + 1 < pieces) m.put(values, from + row(s + 1) * ldfrom, ldfrom, rows(s + 1), cols, id);
+        __syncthreads();
+    }
+    __syncthreads();                                           // (all have done their part)
+    if (pieces > 0) m.store(to + row(pieces - 1) * ldto, ldto, outputs, rows(pieces - 1), cols, id);
+}
 
 // Products of parts with B's three side by side along N: part p of A, of `a_parts`, with the first 3 - p of B onto the digits from p on.  A is read once for
 // each of its parts so (it is A's 4 KB that an MMA waits for while N is below 128: with every pair of parts an MMA of its own the three
