@@ -183,31 +183,25 @@ struct Tile {
 template <typename T, int NV, bool WIDE>
 struct Mover {
     using L = Tile<T, NV>;
-    Pack<T, L::PER> p[L::EACH];
+    static constexpr int TAKES = WIDE ? L::EACH : (kPiece * NV + kMovers - 1) / kMovers;       // single elements, or units
+    Pack<T, WIDE ? L::PER : 1> p[TAKES];
+    // from a tensor: zeros behind the last row and column
     __device__ __forceinline__ void fetch(const T* from, long long ld, int rows, int cols, int id)
     {
-        if (!WIDE) return;
+        constexpr int PER = WIDE ? L::PER : 1, ACROSS = NV / PER;
 #pragma unroll
-        for (int j = 0; j < L::EACH; ++j) {
-            const int u = id + j * kMovers, row = u / L::UNITS, col = u % L::UNITS * L::PER;
-            p[j] = load_masked<T, L::PER>(from + row * ld + col, row < rows && col < cols);
+        for (int j = 0; j < TAKES; ++j) {
+            const int u = id + j * kMovers, row = u / ACROSS, col = u % ACROSS * PER;
+            p[j] = load_masked<T, PER>(from + row * ld + col, row < rows && col < cols);
         }
     }
-    // into the tile: zeros behind the last row and column
-    __device__ __forceinline__ void put(unsigned char* tile, const T* from, long long ld, int rows, int cols, int id)
+    __device__ __forceinline__ void put(unsigned char* tile, int id) const
     {
-        if (WIDE) {
+        constexpr int PER = WIDE ? L::PER : 1, ACROSS = NV / PER;
 #pragma unroll
-            for (int j = 0; j < L::EACH; ++j) {
-                const int u = id + j * kMovers;
-                if (u < kPiece * L::UNITS) store_pack<T, L::PER>(reinterpret_cast<T*>(tile + L::at(u / L::UNITS, u % L::UNITS)), p[j]);
-            }
-        } else {
-#pragma unroll 4
-            for (int i = id; i < kPiece * NV; i += kMovers) {
-                const int row = i / NV, col = i % NV;
-                *reinterpret_cast<T*>(tile + L::at(row, col / L::PER) + col % L::PER * sizeof(T)) = load_masked<T, 1>(from + row * ld + col, row < rows && col < cols).e[0];
-            }
+        for (int j = 0; j < TAKES; ++j) {
+            const int u = id + j * kMovers, row = u / ACROSS, col = u % ACROSS * PER;
+            if (row < kPiece) store_pack<T, PER>(reinterpret_cast<T*>(tile + L::at(row, col / L::PER) + col % L::PER * sizeof(T)), p[j]);
         }
     }
     static __device__ __forceinline__ void store(T* to, long long ld, const unsigned char* tile, int rows, int cols, int id)
@@ -238,14 +232,14 @@ __device__ __forceinline__ void move_values(const T* from, long long ldfrom, T* 
     auto rows = [&](int s) { return min(len - piece(s) * kPiece, kPiece); };
     if (pieces > 0) {
         m.fetch(from + row(0) * ldfrom, ldfrom, rows(0), cols, id);
-        m.put(values, from + row(0) * ldfrom, ldfrom, rows(0), cols, id);
+        m.put(values, id);
     }
     for (int s = 0; s < pieces; ++s) {
         __syncthreads();
         if (s + 1 < pieces) m.fetch(from + row(s + 1) * ldfrom, ldfrom, rows(s + 1), cols, id);
         if (s > 0) m.store(to + row(s - 1) * ldto, ldto, outputs, rows(s - 1), cols, id);
         __syncthreads();
-        if (s + 1 < pieces) m.put(values, from + row(s + 1) * ldfrom, ldfrom, rows(s + 1), cols, id);
+        if (s + 1 < pieces) m.put(values, id);
         __syncthreads();
     }
     __syncthreads();                                           // (all have done their part)

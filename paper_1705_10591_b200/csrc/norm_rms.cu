@@ -99,8 +99,13 @@ __device__ __forceinline__ void store_codes(unsigned char* to, const float (&f)[
     store_pack<unsigned char, V>(to, p);
 }
 
+// (blocks of rows in packs have 512 threads at most, single elements 1024)
+template <int V> constexpr int kMostThreads = V > 1 ? 512 : 1024;
+
+// Every row has its block, and an SM four of 256 threads at once: walks over rows with the next row's numbers under way, as the backward pass takes them, need the
+// registers of half of those (8192 x 4096 to 8 bits 74 us so, 53 without).
 template <typename T, int V, int NP>
-__global__ void __launch_bounds__(1024) rms_fwd_kernel(const RmsArgs a, Runs groups, Runs blocks, int packs, int channels)
+__global__ void __launch_bounds__(kMostThreads<V>, V > 1 && NP <= 2 ? 2 : 1) rms_fwd_kernel(const RmsArgs a, Runs groups, Runs blocks, int packs, int channels)
 {
     extern __shared__ float shared[];
     ptx::grid_dep_wait();
@@ -176,16 +181,30 @@ __global__ void __launch_bounds__(1024) rms_fwd_kernel(const RmsArgs a, Runs gro
     }
 }
 
-// Backward: with n = dy gamma silu(z) and m = h r,   dx = r (n - m mean(n m)) + dh.  A block takes rows gridDim.x * blockDim.y apart and keeps its sums for
-// gamma in registers until the end.
+// Backward: with n = dy gamma silu(z) and m = h r,   dx = r (n - m mean(n m)) + dh.  A block takes rows gridDim.x * blockDim.y apart, the next one's numbers under way
+// while it computes, and keeps its sums for gamma in registers until the end, when they are added over its rows and groups.
 template <typename T, int V, int NP>
-__global__ void __launch_bounds__(1024) rms_bwd_kernel(const RmsArgs a, Runs groups, int packs, int channels)
+__global__ void __launch_bounds__(kMostThreads<V>, 1) rms_bwd_kernel(const RmsArgs a, Runs groups, int packs, int channels)
 {
     extern __shared__ float shared[];
     ptx::grid_dep_wait();
     const float inverse = 1.f / channels;
-    float w[NP][V], dw[NP][V];
+    float w[NP][V], dw[NP][V], r[NP];
     int group[NP];
+    Pack<T, V> ph[NP], py[NP], pd[NP], pz[NP];
+    const long long step = (long long)gridDim.x * blockDim.y;
+    auto fetch = [&](long long row) {
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+            const int p = threadIdx.x + j * blockDim.x;
+            const bool there = row < a.M && p < packs;
+            ph[j] = load_masked<T, V>(static_cast<const T*>(a.x) + row * a.ldx + p * V, there);
+            py[j] = load_masked<T, V>(static_cast<const T*>(a.dy) + row * a.lddy + p * V, there);
+            if (a.dh) pd[j] = load_masked<T, V>(static_cast<const T*>(a.dh) + row * a.lddh + p * V, there);
+            if (a.z) pz[j] = load_masked<T, V>(static_cast<const T*>(a.z) + row * a.ldz + p * V, there);
+            r[j] = load_masked<float, 1>(a.rstd_in + row * a.G + group[j], there).e[0];
+        }
+    };
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
         const int p = threadIdx.x + j * blockDim.x;
@@ -194,28 +213,20 @@ __global__ void __launch_bounds__(1024) rms_bwd_kernel(const RmsArgs a, Runs gro
 #pragma unroll
         for (int e = 0; e < V; ++e) dw[j][e] = 0.f, w[j][e] = p < packs ? w[j][e] : 0.f;
     }
-    for (long long row0 = (long long)blockIdx.x * blockDim.y; row0 < a.M; row0 += (long long)gridDim.x * blockDim.y) {
+    fetch((long long)blockIdx.x * blockDim.y + threadIdx.y);
+    for (long long row0 = (long long)blockIdx.x * blockDim.y; row0 < a.M; row0 += step) {
         const long long row = row0 + threadIdx.y;
         const bool real = row < a.M;
-        float m[NP][V], n[NP][V], s[NP], r[NP];
-        Pack<T, V> ph[NP], py[NP], pd[NP], pz[NP];
-#pragma unroll
-        for (int j = 0; j < NP; ++j) {
-            const int p = threadIdx.x + j * blockDim.x;
-            const bool there = real && p < packs;
-            ph[j] = load_masked<T, V>(static_cast<const T*>(a.x) + row * a.ldx + p * V, there);
-            py[j] = load_masked<T, V>(static_cast<const T*>(a.dy) + row * a.lddy + p * V, there);
-            if (a.dh) pd[j] = load_masked<T, V>(static_cast<const T*>(a.dh) + row * a.lddh + p * V, there);
-            if (a.z) pz[j] = load_masked<T, V>(static_cast<const T*>(a.z) + row * a.ldz + p * V, there);
-            r[j] = load_masked<float, 1>(a.rstd_in + row * a.G + group[j], there).e[0];
-        }
+        float m[NP][V], n[NP][V], d[NP][V], s[NP], rr[NP];
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
             const int p = threadIdx.x + j * blockDim.x;
             unpack<T, V>(ph[j], m[j]);
             unpack<T, V>(py[j], n[j]);
+            if (a.dh) unpack<T, V>(pd[j], d[j]);
+            rr[j] = r[j];
 #pragma unroll
-            for (int e = 0; e < V; ++e) m[j][e] *= r[j];
+            for (int e = 0; e < V; ++e) m[j][e] *= rr[j];
             if (a.z) {
                 float z[V], dz[V];
                 unpack<T, V>(pz[j], z);
@@ -235,46 +246,67 @@ __global__ void __launch_bounds__(1024) rms_bwd_kernel(const RmsArgs a, Runs gro
                 s[j] = fmaf(n[j][e], m[j][e], s[j]);
             }
         }
+        fetch(row + step);
         reduce_runs<Sum>(s, groups, packs, shared);
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
             const int p = threadIdx.x + j * blockDim.x;
             const float mean = s[j] * inverse;
 #pragma unroll
-            for (int e = 0; e < V; ++e) n[j][e] = r[j] * fmaf(-m[j][e], mean, n[j][e]);
+            for (int e = 0; e < V; ++e) n[j][e] = rr[j] * fmaf(-m[j][e], mean, n[j][e]);
             if (a.dh) {
-                float d[V];
-                unpack<T, V>(pd[j], d);
 #pragma unroll
-                for (int e = 0; e < V; ++e) n[j][e] += d[e];
+                for (int e = 0; e < V; ++e) n[j][e] += d[j][e];
             }
             if (real && p < packs) store_pack<T, V>(static_cast<T*>(a.dx) + row * a.lddx + p * V, pack<T, V>(n[j]));
         }
     }
     if (!a.dgamma) return;
-    float* part = a.ws + ((size_t)blockIdx.x * blockDim.y + threadIdx.y) * a.C;
+    __syncthreads();
+    float* mine = shared + threadIdx.y * a.C;
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
         const int p = threadIdx.x + j * blockDim.x;
         if (p >= packs) continue;
 #pragma unroll
-        for (int e = 0; e < V; ++e) part[p * V + e] = dw[j][e];
+        for (int e = 0; e < V; ++e) mine[p * V + e] = dw[j][e];
+    }
+    __syncthreads();
+    for (int c = threadIdx.y * blockDim.x + threadIdx.x; c < channels; c += blockDim.x * blockDim.y) {
+        float s = 0.f;
+        for (int i = c; i < a.C * (int)blockDim.y; i += channels) s += shared[i];
+        a.ws[(size_t)blockIdx.x * channels + c] = s;
     }
 }
 
-struct StoreSum {
-    float* out;
-    __device__ void operator()(long long col, float s) const { out[col] = s; }
-};
+// Sums over the blocks' parts, 32 columns by 32 shares of the parts a block.
+__global__ void __launch_bounds__(1024) rms_gamma_kernel(const float* __restrict__ parts, float* __restrict__ out, int blocks, int channels)
+{
+    __shared__ float sums[32][33];
+    ptx::grid_dep_wait();
+    const int c = blockIdx.x * 32 + threadIdx.x;
+    float s = 0.f;
+    if (c < channels) {
+#pragma unroll 8
+        for (int p = threadIdx.y; p < blocks; p += 32) s += parts[(size_t)p * channels + c];
+    }
+    sums[threadIdx.y][threadIdx.x] = s;
+    __syncthreads();
+    s = sums[threadIdx.x][threadIdx.y];
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
+    if (threadIdx.x == 0 && blockIdx.x * 32 + threadIdx.y < channels) out[blockIdx.x * 32 + threadIdx.y] = s;
+}
 
-// How a row's packs are spread: at least two a thread (four single elements), up to 1024 threads; small rows share a block of about 256.
+// How a row's packs are spread: at least two a thread (four single elements), up to 512 threads (1024); small rows share a block of about 256.
 struct RowPlan {
     int v, packs, threads, rows, np;
     RowPlan(int C, int v_) : v(v_), packs(C / v_)
     {
         const int each = v > 1 ? 2 : 4;
         threads = (packs + each - 1) / each;
-        threads = threads > 1024 ? 1024 : (threads + 31) / 32 * 32;
+        const int most = v > 1 ? 512 : 1024;
+        threads = threads > most ? most : (threads + 31) / 32 * 32;
         np = (packs + threads - 1) / threads;
         rows = threads >= 256 ? 1 : 256 / threads;
     }
@@ -314,13 +346,15 @@ conv2d_status_t backward(const RmsArgs& a, const RowPlan& p, cudaStream_t stream
 {
     static SmemLimit limit;
     const Runs groups = runs_of(a.C / a.G, p);
-    const size_t smem = shared_bytes(p, groups);
+    const size_t runs = shared_bytes(p, groups), sums = a.dgamma ? (size_t)p.rows * a.C * 4 : 0, smem = runs > sums ? runs : sums;
     if (raise_smem_limit((const void*)rms_bwd_kernel<T, V, NP>, smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-    const int blocks = bwd_blocks(a.M, p.rows);
-    if (launch_pdl(rms_bwd_kernel<T, V, NP>, dim3(blocks), dim3(p.threads, p.rows), smem, stream, a, groups, p.packs, a.C / a.G) != cudaSuccess) return CONV2D_ERR_CUDA;
+    const int blocks = bwd_blocks(a.M, p.rows), channels = a.C / a.G;
+    if (launch_pdl(rms_bwd_kernel<T, V, NP>, dim3(blocks), dim3(p.threads, p.rows), smem, stream, a, groups, p.packs, channels) != cudaSuccess) return CONV2D_ERR_CUDA;
     count_launch();
     if (!a.dgamma) return CONV2D_OK;
-    return launch_column_sums(a.ws, (long long)blocks * p.rows * a.G, a.C / a.G, a.C / a.G, StoreSum{a.dgamma}, stream);
+    if (launch_pdl(rms_gamma_kernel, dim3(ceil_div_u(channels, 32)), dim3(32, 32), 0, stream, a.ws, a.dgamma, blocks, channels) != cudaSuccess) return CONV2D_ERR_CUDA;
+    count_launch();
+    return CONV2D_OK;
 }
 
 // Whether rows can be moved in packs of 16 bytes of which none lies in two groups or two blocks of a scale.
@@ -341,7 +375,8 @@ conv2d_status_t rms_typed(const RmsArgs& a, bool bwd, cudaStream_t stream)
         const RowPlan p(a.C, V);
         if (p.np == 1) return bwd ? backward<T, V, 1>(a, p, stream) : forward<T, V, 1>(a, p, stream);
         if (p.np == 2) return bwd ? backward<T, V, 2>(a, p, stream) : forward<T, V, 2>(a, p, stream);
-        return bwd ? backward<T, V, 4>(a, p, stream) : forward<T, V, 4>(a, p, stream);
+        if (V == 8 || p.np <= 4) return bwd ? backward<T, V, 4>(a, p, stream) : forward<T, V, 4>(a, p, stream);
+        return bwd ? backward<T, V, 4 * 8 / V>(a, p, stream) : forward<T, V, 4 * 8 / V>(a, p, stream);
     }
     const RowPlan p(a.C, 1);
     if (p.np <= 4) return bwd ? backward<T, 1, 4>(a, p, stream) : forward<T, 1, 4>(a, p, stream);
@@ -357,19 +392,8 @@ conv2d_status_t rms(const RmsArgs& a, conv2d_operand_t type, bool bwd, cudaStrea
 
 }  // namespace
 
-// (rows of partial sums of whichever way the rows are spread)
-size_t rms_bwd_workspace_bytes(int M, int C, int G)
-{
-    (void)G;
-    size_t most = 0;
-    for (int v : {1, 4, 8}) {
-        if (C % v) continue;
-        const RowPlan p(C, v);
-        const size_t n = (size_t)bwd_blocks(M, p.rows) * p.rows * C * 4;
-        most = n > most ? n : most;
-    }
-    return (most + 15) / 16 * 16;
-}
+// (a row of partial sums for every block, whichever way the rows are spread)
+size_t rms_bwd_workspace_bytes(int M, int C, int G) { return ((size_t)bwd_blocks(M, 1) * (C / G) * 4 + 15) / 16 * 16; }
 conv2d_status_t launch_rms_fwd(const RmsArgs& a, conv2d_operand_t type, cudaStream_t stream) { return rms(a, type, false, stream); }
 conv2d_status_t launch_rms_bwd(const RmsArgs& a, conv2d_operand_t type, cudaStream_t stream) { return rms(a, type, true, stream); }
 
