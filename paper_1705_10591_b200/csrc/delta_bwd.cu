@@ -202,31 +202,70 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
     }
 }
 
-// One block for one piece of one value head: products over V in blocks of 32 columns, two in turn (while one's products run, the threads bring the next one's numbers and
-// split them), then products over tokens.
+// One block for one piece of one value head: products over V in blocks of 32 columns, two in turn (while one's products run, the threads split the next one's numbers, and
+// those of the one after it are under way), then products over tokens.
 //   D1 [dV; dO] S^T,   D2 [dV; dO] E^T,   D3 E dS^T (64 rows; the others are of what lies behind),   then of D2 [y; p],
 //   D4 [y; p] K,   D5 [y; p]^T [K; Q] (64 rows likewise).
-// In the last step a thread has half a row of a and c (keys) or of dq (queries).
+// In the last step a thread has a quarter of a row of a and c (keys) or of dq (queries).  What bounds it: the MMAs of 128 rows, of which those of keys alone are half, six for
+// every pair of numbers in three parts, are a half of its time; the rest is one thing after the other, since tensor memory has room for one block.
 template <typename T, int KD>
 struct Piecewise {
-    static constexpr int IN = Parts<T>::in, NB = 32, HALF = 2 * kPiece * 128;
+    static constexpr int IN = Parts<T>::in, NB = 32, HALF = 2 * kPiece * 128, WORKERS = 512, THREADS = WORKERS + 32;
     static constexpr int rows_part = 2 * kPiece * NB * 2, e_part = kPiece * NB * 2, state_part = KD * NB * 2;
     static constexpr int at_e = kSum * rows_part, at_s = at_e + kSum * e_part, at_ds = at_s + kSum * state_part, block = at_ds + kSum * state_part;
     static constexpr int keys = IN * (KD / 64) * HALF, key_part = (KD / 64) * HALF, square_part = 2 * kPiece * 128;
-    static constexpr int over_v = 2 * block, over_tokens = keys + kSum * square_part;
-    // (the 64 rows more reach as far as one tile behind the last one; 1024 to the first boundary of the swizzle)
-    static constexpr int reach = over_tokens + square_part, smem = (over_v > reach ? over_v : reach) + 1024;
+    // over V: two blocks; over tokens: keys and queries, [y; p], in whose place the results are collected; (the 64 rows more reach as far as one tile
+    // behind the last one)
+    static constexpr int over_v = 2 * block, over_tokens = keys + kSum * square_part + square_part, results = keys + 2 * kPiece * KD * 4;
+    static constexpr int most = over_v > over_tokens ? over_v : over_tokens, smem = (most > results ? most : results) + 1024;      // (1024 to the first boundary of the swizzle)
     static constexpr uint32_t d1 = 0, d3 = KD, d4 = 2 * KD, d2 = 3 * KD, d5 = 3 * KD;         // columns of tensor memory (D2 has been read when D5 is written)
     static constexpr uint32_t cols = 4 * KD;
 };
 struct PieceBars {
     uint64_t done[2], keys, last;
     uint32_t tmem, abort;
-    float factors[kFactors * kPiece], dots[4][kPiece], sums[8];
+    alignas(16) float factors[kFactors * kPiece];              // (read in fours)
+    float dots[8][kPiece], sums[16];
+};
+// What a thread has under way of 32 columns of V: quads, of what the passes kept its lanes have rows, of dO eight threads have a row.
+template <typename T, int KD, bool WIDE>
+struct Quads {
+    static constexpr int ACROSS = Piecewise<T, KD>::WORKERS / KD, N = 8 / ACROSS;        // quads of a row of S at once, of a thread
+    SavedRow<4> s[N], ds[N], dv, e;
+    Row<T, 4> dout;
+    __device__ __forceinline__ void fetch(const DeltaArgs& a, size_t unit, const T* grads, int live, int v0, int tid)
+    {
+        const int k = tid % KD, q = tid / KD, t = tid % kPiece, p = tid / kPiece, r = tid >> 3, c = (tid & 7) * 4;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int v = v0 + 4 * (q + ACROSS * i);
+            s[i].load(a.states + quad_at(unit, a.VP, KD, v, k), KD, a.VP - v), ds[i].load(a.dstates + quad_at(unit, a.VP, KD, v, k), KD, a.VP - v);
+        }
+        const int v = v0 + 4 * p;
+        dv.load(a.dupdates + quad_at(unit, a.VP, kPiece, v, t), kPiece, a.VP - v), e.load(a.updates + quad_at(unit, a.VP, kPiece, v, t), kPiece, a.VP - v);
+        dout.template load<WIDE>(grads + r * a.lddo + v0 + c, r < live ? a.V - v0 - c : 0);
+    }
+    __device__ __forceinline__ void put(unsigned char* at, float& inner, int tid) const
+    {
+        using W = Piecewise<T, KD>;
+        const int k = tid % KD, q = tid / KD, t = tid % kPiece, p = tid / kPiece, r = tid >> 3, c = (tid & 7) * 4;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            put_four<W::NB>(at + W::at_s, W::state_part, k, 4 * (q + ACROSS * i), s[i].q[0].e);
+            put_four<W::NB>(at + W::at_ds, W::state_part, k, 4 * (q + ACROSS * i), ds[i].q[0].e);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) inner = fmaf(s[i].q[0].e[n], ds[i].q[0].e[n], inner);
+        }
+        float f[4];
+        dout.get(f);
+        put_four<W::NB>(at, W::rows_part, t, 4 * p, dv.q[0].e);
+        put_four<W::NB>(at + W::at_e, W::e_part, t, 4 * p, e.q[0].e);
+        put_four<W::NB>(at, W::rows_part, kPiece + r, c, f);
+    }
 };
 
 template <typename T, int KD, bool WIDE>
-__global__ void __launch_bounds__(kPieceThreads, 1) delta_bwd_pieces_kernel(const DeltaArgs a)
+__global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces_kernel(const DeltaArgs a)
 {
     using W = Piecewise<T, KD>;
     constexpr int IN = W::IN, NB = W::NB;
@@ -245,26 +284,30 @@ __global__ void __launch_bounds__(kPieceThreads, 1) delta_bwd_pieces_kernel(cons
     // padding
     if (live < there) {
         const int first = max(live, 0);
-        for (int i = tid; i < (there - first) * a.K; i += kPieceThreads) {
+        for (int i = tid; i < (there - first) * a.K; i += W::THREADS) {
             const int row = first + i / a.K, col = i % a.K;
             if (shared_key) a.dq_parts[part0 + (long long)row * a.H * a.K + col] = 0.f, a.dk_parts[part0 + (long long)row * a.H * a.K + col] = 0.f;
             else dq[row * a.lddq + col] = from_float<T>(0.f), dk[row * a.lddk + col] = from_float<T>(0.f);
         }
-        for (int i = first + tid; i < there; i += kPieceThreads) a.dg[(row0 + i) * a.lddg + h] = 0.f, a.dbeta[(row0 + i) * a.lddbeta + h] = 0.f;
+        for (int i = first + tid; i < there; i += W::THREADS) a.dg[(row0 + i) * a.lddg + h] = 0.f, a.dbeta[(row0 + i) * a.lddbeta + h] = 0.f;
     }
     if (live <= 0) return;
 
     const size_t unit = (size_t)bh * a.pieces + piece;
+    const T* grads = static_cast<const T*>(a.dout) + row0 * a.lddo + (long long)h * a.V;
+    Quads<T, KD, WIDE> even, odd;
+    const bool works = warp < W::WORKERS / 32;
+    if (works) even.fetch(a, unit, grads, live, 0, tid);
     if (tid == 0) {
         bars.abort = 0;
         ptx::mbar_init(&bars.done[0], 1), ptx::mbar_init(&bars.done[1], 1), ptx::mbar_init(&bars.keys, 1), ptx::mbar_init(&bars.last, 1);
         ptx::fence_mbar_init();
     }
-    if (warp == kWorkers / 32) {
+    if (!works) {
         ptx::tmem_alloc(&bars.tmem, W::cols);
         ptx::tmem_relinquish();
     }
-    for (int i = tid; i < kFactors * kPiece; i += kPieceThreads) bars.factors[i] = reinterpret_cast<const float*>(a.prepared + unit * kPrepared + kSquares)[i];
+    for (int i = tid; i < kFactors * kPiece; i += W::THREADS) bars.factors[i] = reinterpret_cast<const float*>(a.prepared + unit * kPrepared + kSquares)[i];
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
@@ -272,9 +315,9 @@ __global__ void __launch_bounds__(kPieceThreads, 1) delta_bwd_pieces_kernel(cons
     const int blocks = (a.VP + NB - 1) / NB;
     const uint32_t keys = base, squares = base + W::keys;
 
-    if (warp == kWorkers / 32) {
+    if (!works) {
         const uint32_t elected = ptx::elect_one();
-        constexpr uint32_t idk = ptx::idesc_b16(128, KD, false), ide = ptx::idesc_b16(128, kPiece, false);
+        constexpr uint32_t idk = ptx::idesc_b16(128, KD, false);
         // tiles of rows of 32 numbers, K-major: 64-byte swizzle
         auto narrow = [](uint32_t at) { return rows_as_k<32>(at, 512); };
         for (int j = 0; j < blocks; ++j) {
@@ -284,7 +327,7 @@ __global__ void __launch_bounds__(kPieceThreads, 1) delta_bwd_pieces_kernel(cons
             auto rows = [&](int p, int k) { return narrow(at + p * W::rows_part + k * 32); };
             auto e = [&](int p, int k) { return narrow(at + W::at_e + p * W::e_part + k * 32); };
             multiply(tmem + W::d1, kSum, kSum, NB / 16, idk, elected, j > 0, rows, [&](int p, int k) { return narrow(at + W::at_s + p * W::state_part + k * 32); });
-            multiply(tmem + W::d2, kSum, kSum, NB / 16, ide, elected, j > 0, rows, e);
+            multiply(tmem + W::d2, kSum, kSum, NB / 16, ptx::idesc_b16(128, kPiece, false), elected, j > 0, rows, e);
             multiply(tmem + W::d3, kSum, kSum, NB / 16, idk, elected, j > 0, e, [&](int p, int k) { return narrow(at + W::at_ds + p * W::state_part + k * 32); });
             ptx::mma_commit(&bars.done[j & 1], elected);
         }
@@ -305,140 +348,162 @@ __global__ void __launch_bounds__(kPieceThreads, 1) delta_bwd_pieces_kernel(cons
             ptx::mma_commit(&bars.last, elected);
         }
         __syncthreads();
-    } else {
-        const int quarter = warp & 3, row = quarter * 32 + lane, side = warp >> 2, token = row & (kPiece - 1);
-        const bool is_key = row < kPiece;
-        float inner = 0.f;                                     // <S, dS>
-        {
-            // quads: of what the passes kept lanes have rows, of dO eight threads a row
-            constexpr int ROWS = kWorkers / KD, QUADS = 8 / ROWS;        // quads of a row at once, of a thread
-            const int k = tid % KD, q0 = tid / KD, t = tid % kPiece, p0 = tid / kPiece, r0 = tid >> 3, c = (tid & 7) * 4;
-            SavedRow<4> dv[2], e[2], s[QUADS], ds[QUADS];
-            Row<T, 4> dout[2];
-            const T* grads = static_cast<const T*>(a.dout) + row0 * a.lddo + (long long)h * a.V;
-            auto fetch = [&](int v0) {
-#pragma unroll
-                for (int i = 0; i < QUADS; ++i) {
-                    const int v = v0 + 4 * (q0 + ROWS * i);
-                    s[i].load(a.states + quad_at(unit, a.VP, KD, v, k), KD, a.VP - v), ds[i].load(a.dstates + quad_at(unit, a.VP, KD, v, k), KD, a.VP - v);
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int v = v0 + 4 * (p0 + 4 * i);
-                    dv[i].load(a.dupdates + quad_at(unit, a.VP, kPiece, v, t), kPiece, a.VP - v), e[i].load(a.updates + quad_at(unit, a.VP, kPiece, v, t), kPiece, a.VP - v);
-                    dout[i].template load<WIDE>(grads + (r0 + 32 * i) * a.lddo + v0 + c, r0 + 32 * i < live ? a.V - v0 - c : 0);
-                }
-            };
-            fetch(0);
-            for (int j = 0; j < blocks; ++j) {
-                unsigned char* at = raw + (j & 1) * W::block;
-                if (j >= 2) ptx::mbar_wait_bounded(&bars.done[j & 1], ((j >> 1) - 1) & 1, abort_flag, a.max_polls);
-#pragma unroll
-                for (int i = 0; i < QUADS; ++i) {
-                    put_four<NB>(at + W::at_s, W::state_part, k, 4 * (q0 + ROWS * i), s[i].q[0].e);
-                    put_four<NB>(at + W::at_ds, W::state_part, k, 4 * (q0 + ROWS * i), ds[i].q[0].e);
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) inner = fmaf(s[i].q[0].e[n], ds[i].q[0].e[n], inner);
-                }
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float f[4];
-                    dout[i].get(f);
-                    put_four<NB>(at, W::rows_part, t, 4 * (p0 + 4 * i), dv[i].q[0].e);
-                    put_four<NB>(at + W::at_e, W::e_part, t, 4 * (p0 + 4 * i), e[i].q[0].e);
-                    put_four<NB>(at, W::rows_part, kPiece + r0 + 32 * i, c, f);
-                }
-                ptx::fence_proxy_async_smem();
-                ptx::tc_fence_before_sync();
-                __syncthreads();
-                if (j + 1 < blocks) fetch((j + 1) * NB);
-            }
-        }
-        ptx::mbar_wait_bounded(&bars.done[(blocks - 1) & 1], ((blocks - 1) >> 1) & 1, abort_flag, a.max_polls);
-        ptx::tc_fence_after_sync();
-        const float *eg = bars.factors, *ed = eg + kPiece, *be = eg + 2 * kPiece, *high = eg + 3 * kPiece, *low = eg + 4 * kPiece;
-        const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
-        {
-            float x[32];
-            tmem_row<32>(lanes + W::d2 + side * 32, x);
-            const float hi = high[token], lo = low[token];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const int other = side * 32 + j;
-                const float d = ex2(((hi - high[other]) + (lo - low[other])) * kLog2e) * be[other];
-                x[j] = is_key ? (other < token ? -d * x[j] : 0.f) : (other <= token ? a.scale * d * x[j] : 0.f);
-            }
-            put_row<64, 32>(raw + W::keys, W::square_part, row, side * 32, x);
-        }
-        ptx::fence_proxy_async_smem();
-        ptx::tc_fence_before_sync();
-        __syncthreads();
-        const T* mine = static_cast<const T*>(is_key ? a.k : a.q) + (row0 + token) * (is_key ? a.ldk : a.ldq) + (long long)hk * a.K;
-        Row<T, 16> other;                                      // of this token's key or query, a step ahead
-        other.template load<WIDE>(mine + side * (KD / 2), token < live ? a.K - side * (KD / 2) : 0);
-        ptx::mbar_wait_bounded(&bars.last, 0, abort_flag, a.max_polls);
-        ptx::tc_fence_after_sync();
-        // <S after, dS> = e^G_63 <S, dS> + sum over tokens of k . (e^(G_63 - G) beta E dS^T)
-        float after = eg[kPiece - 1] * inner, dot = 0.f;
-        const float x1 = is_key ? -eg[token] : a.scale * eg[token], x3 = ed[token] * be[token];
-#pragma unroll
-        for (int col = side * (KD / 2); col < (side + 1) * (KD / 2); col += 16) {
-            float x[16], y[16], z[16];
-            tmem_row<16>(lanes + W::d1 + col, x);
-            tmem_row<16>(lanes + W::d4 + col, y);
-            other.get(z);
-            if (col + 16 < (side + 1) * (KD / 2)) other.template load<WIDE>(mine + col + 16, token < live ? a.K - col - 16 : 0);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) x[j] = fmaf(x1, x[j], y[j]), dot = fmaf(z[j], x[j], dot);
-            if (is_key) {
-                float w[16];
-                tmem_row<16>(lanes + W::d3 + col, y);
-                tmem_row<16>(lanes + W::d5 + col, w);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    y[j] *= x3, after = fmaf(z[j], y[j], after);
-                    y[j] += w[j], dot = fmaf(-z[j], y[j], dot);
-                    x[j] += y[j];
-                }
-            }
-            if (token < live) {
-                if (shared_key) store_row<WIDE>((is_key ? a.dk_parts : a.dq_parts) + part0 + (long long)token * a.H * a.K + col, a.K - col, x);
-                else store_row<WIDE>(is_key ? dk + token * a.lddk + col : dq + token * a.lddq + col, a.K - col, x);
-            }
-        }
-        bars.dots[side * 2 + (is_key ? 0 : 1)][token] = dot;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) after += __shfl_xor_sync(0xffffffffu, after, d);
-        if (lane == 0) bars.sums[warp] = after;
-        ptx::tc_fence_before_sync();
-        __syncthreads();
-        if (warp == 0) {                                       // sums from the last token back, two tokens a lane
-            float last = 0.f;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) last += bars.sums[w];
-            auto total = [&](int i) { return (bars.dots[0][i] + bars.dots[1][i]) + (bars.dots[2][i] + bars.dots[3][i]); };
-            const float x1 = total(63 - 2 * lane), x0 = total(62 - 2 * lane);
-            float s = x0 + x1;
-#pragma unroll
-            for (int d = 1; d < 32; d *= 2) {
-                const float y = __shfl_up_sync(0xffffffffu, s, d);
-                if (lane >= d) s += y;
-            }
-            const int first = 62 - 2 * lane;
-            if (first < live) a.dg[(row0 + first) * a.lddg + h] = s + last;
-            if (first + 1 < live) a.dg[(row0 + first + 1) * a.lddg + h] = (s - x0) + last;
-        } else if (warp == 2 || warp == 3) {
-            const int r = (warp - 2) * 32 + lane, tiles = a.VP / 16;
-            const float* from = a.dbeta_parts + unit * tiles * kPiece + r;
-            float s = 0.f;
-            for (int i = 0; i < tiles; ++i) s += from[i * kPiece];
-            if (r < live) a.dbeta[(row0 + r) * a.lddbeta + h] = s;
-        }
-    }
-    if (warp == kWorkers / 32) {
         ptx::tc_fence_after_sync();
         ptx::tmem_dealloc(tmem, W::cols);
         if (lane == 0 && *abort_flag) atomicExch(a.timeout, 1u);
+        return;
+    }
+
+    const int quarter = warp & 3, row = quarter * 32 + lane, side = warp >> 2, token = row & (kPiece - 1);
+    const bool is_key = row < kPiece;
+    float inner = 0.f;                                         // <S, dS>
+    odd.fetch(a, unit, grads, live, NB, tid);                  // (nothing is read behind the last column)
+    if (warp == 4 || warp == 5) {                              // dbeta, a sum over the walk's columns
+        const int r = (warp - 4) * 32 + lane, tiles = a.VP / 16;
+        const float* from = a.dbeta_parts + unit * tiles * kPiece + r;
+        float s = 0.f;
+        for (int i = 0; i < tiles; ++i) s += from[i * kPiece];
+        if (r < live) a.dbeta[(row0 + r) * a.lddbeta + h] = s;
+    }
+    auto ready = [&] {                                         // for the products
+        ptx::fence_proxy_async_smem();
+        ptx::tc_fence_before_sync();
+        __syncthreads();
+    };
+    for (int j = 0; j < blocks; j += 2) {
+        if (j >= 2) ptx::mbar_wait_bounded(&bars.done[0], ((j >> 1) - 1) & 1, abort_flag, a.max_polls);
+        even.put(raw, inner, tid);
+        if (j + 2 < blocks) even.fetch(a, unit, grads, live, (j + 2) * NB, tid);
+        ready();
+        if (j + 1 < blocks) {
+            if (j >= 2) ptx::mbar_wait_bounded(&bars.done[1], ((j >> 1) - 1) & 1, abort_flag, a.max_polls);
+            odd.put(raw + W::block, inner, tid);
+            if (j + 3 < blocks) odd.fetch(a, unit, grads, live, (j + 3) * NB, tid);
+            ready();
+        }
+    }
+    ptx::mbar_wait_bounded(&bars.done[(blocks - 1) & 1], ((blocks - 1) >> 1) & 1, abort_flag, a.max_polls);
+    ptx::tc_fence_after_sync();
+    const float *eg = bars.factors, *ed = eg + kPiece, *be = eg + 2 * kPiece, *high = eg + 3 * kPiece, *low = eg + 4 * kPiece;
+    const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
+    {
+        float x[16];
+        tmem_row<16>(lanes + W::d2 + side * 16, x);
+        const float hi = high[token], lo = low[token], by = is_key ? -1.f : a.scale;
+        const int last = is_key ? token - 1 : token;           // (keys: j < i, queries: j <= i)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+            const int other = side * 16 + j;
+            const float4 h4 = *reinterpret_cast<const float4*>(high + other), l4 = *reinterpret_cast<const float4*>(low + other),
+                         b4 = *reinterpret_cast<const float4*>(be + other);
+            const float hs[4] = {h4.x, h4.y, h4.z, h4.w}, ls[4] = {l4.x, l4.y, l4.z, l4.w}, bs[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const float d = ex2(((hi - hs[n]) + (lo - ls[n])) * kLog2e) * bs[n] * by;
+                x[j + n] = other + n <= last ? d * x[j + n] : 0.f;
+            }
+        }
+        put_row<64, 16>(raw + W::keys, W::square_part, row, side * 16, x);
+    }
+    ready();
+    ptx::mbar_wait_bounded(&bars.keys, 0, abort_flag, a.max_polls);
+    ptx::mbar_wait_bounded(&bars.last, 0, abort_flag, a.max_polls);
+    ptx::tc_fence_after_sync();
+    // <S after, dS> = e^G_63 <S, dS> + sum over tokens of k . (e^(G_63 - G) beta E dS^T)
+    float after = eg[kPiece - 1] * inner, dot = 0.f;
+    const float x1 = is_key ? -eg[token] : a.scale * eg[token], x3 = ed[token] * be[token];
+    unsigned char* collected = raw + W::keys;                  // [128 rows][KD] of what goes out, fp32 for shared keys
+    const int bytes = shared_key ? 4 : (int)sizeof(T), units = KD * bytes / 16;
+    // unit u of row r, spread over the banks
+    auto collect_at = [&](int r, int u) { return (r * units + (u ^ (r & 7))) * 16; };
+    constexpr int SHARE = KD / 4;
+#pragma unroll
+    for (int i = 0; i < SHARE; i += 16) {
+        const int col = side * SHARE + i;
+        float x[16], y[16], z[16];
+        uint32_t v1[16], v3[16], v4[16], v5[16];
+        ptx::tmem_ld16(lanes + W::d1 + col, v1), ptx::tmem_ld16(lanes + W::d4 + col, v4);
+        if (is_key) ptx::tmem_ld16(lanes + W::d3 + col, v3), ptx::tmem_ld16(lanes + W::d5 + col, v5);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) z[j] = 0.f;
+#pragma unroll
+        for (int p = IN - 1; p >= 0; --p)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float f[8];
+                unpack(*reinterpret_cast<const Pack<bf16, 8>*>(raw + unit_at<64>(p * W::key_part + (col >> 6) * W::HALF, row, ((col & 63) >> 3) + u)), f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[8 * u + j] += f[j];
+            }
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[j] = fmaf(x1, __uint_as_float(v1[j]), __uint_as_float(v4[j])), dot = fmaf(z[j], x[j], dot);
+        if (is_key) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                y[j] = x3 * __uint_as_float(v3[j]), after = fmaf(z[j], y[j], after);
+                y[j] += __uint_as_float(v5[j]), dot = fmaf(-z[j], y[j], dot);
+                x[j] += y[j];
+            }
+        }
+        if (shared_key) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) *reinterpret_cast<float4*>(collected + collect_at(row, col / 4 + u)) = make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
+        } else {
+            constexpr int PER = 16 / (int)sizeof(T);
+#pragma unroll
+            for (int u = 0; u < 16 / PER; ++u) {
+                float f[PER];
+#pragma unroll
+                for (int j = 0; j < PER; ++j) f[j] = x[u * PER + j];
+                store_pack<T, PER>(reinterpret_cast<T*>(collected + collect_at(row, col / PER + u)), pack<T, PER>(f));
+            }
+        }
+    }
+    bars.dots[side * 2 + (is_key ? 0 : 1)][token] = dot;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) after += __shfl_xor_sync(0xffffffffu, after, d);
+    if (lane == 0) bars.sums[warp] = after;
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    // rows of dk, then of dq, whole lines at a time
+    if (WIDE) {
+        for (int i = tid; i < 2 * kPiece * units; i += W::WORKERS) {
+            const int r = i / units, u = i % units, t = r & (kPiece - 1), col = u * 16 / bytes;
+            if (t >= live || col >= a.K) continue;
+            const uint4 v = *reinterpret_cast<const uint4*>(collected + collect_at(r, u));
+            if (shared_key) *reinterpret_cast<uint4*>((r < kPiece ? a.dk_parts : a.dq_parts) + part0 + (long long)t * a.H * a.K + col) = v;
+            else *reinterpret_cast<uint4*>(r < kPiece ? dk + t * a.lddk + col : dq + t * a.lddq + col) = v;
+        }
+    } else {
+        for (int i = tid; i < 2 * kPiece * KD; i += W::WORKERS) {
+            const int r = i / KD, col = i % KD, t = r & (kPiece - 1);
+            if (t >= live || col >= a.K) continue;
+            const unsigned char* from = collected + collect_at(r, col * bytes / 16) + col * bytes % 16;
+            if (shared_key) (r < kPiece ? a.dk_parts : a.dq_parts)[part0 + (long long)t * a.H * a.K + col] = *reinterpret_cast<const float*>(from);
+            else *(r < kPiece ? dk + t * a.lddk + col : dq + t * a.lddq + col) = *reinterpret_cast<const T*>(from);
+        }
+    }
+    if (warp == 0) {                                           // sums from the last token back, two tokens a lane
+        float last = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) last += bars.sums[w];
+        auto total = [&](int i) {
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += bars.dots[j][i];
+            return s;
+        };
+        const float x1 = total(63 - 2 * lane), x0 = total(62 - 2 * lane);
+        float s = x0 + x1;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const float y = __shfl_up_sync(0xffffffffu, s, d);
+            if (lane >= d) s += y;
+        }
+        const int first = 62 - 2 * lane;
+        if (first < live) a.dg[(row0 + first) * a.lddg + h] = s + last;
+        if (first + 1 < live) a.dg[(row0 + first + 1) * a.lddg + h] = (s - x0) + last;
     }
 }
 
@@ -477,7 +542,7 @@ conv2d_status_t backward_pieces(const DeltaArgs& a, cudaStream_t stream)
     using W = Piecewise<T, KD>;
     static SmemLimit limit;
     if (raise_smem_limit((const void*)delta_bwd_pieces_kernel<T, KD, WIDE>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-    if (launch_pdl(delta_bwd_pieces_kernel<T, KD, WIDE>, dim3((unsigned)(a.B * a.H) * (unsigned)a.pieces), dim3(kPieceThreads), W::smem, stream, a) != cudaSuccess)
+    if (launch_pdl(delta_bwd_pieces_kernel<T, KD, WIDE>, dim3((unsigned)(a.B * a.H) * (unsigned)a.pieces), dim3(W::THREADS), W::smem, stream, a) != cudaSuccess)
         return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;

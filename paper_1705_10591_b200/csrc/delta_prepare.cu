@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a
     using S = Prepare<T, KD>;
     constexpr int IN = S::IN, HALF = 2 * kPiece * 128;         // bytes of 64 numbers of all rows
     extern __shared__ __align__(1024) unsigned char raw[];
-    __shared__ float high[kPiece], low[kPiece], betas[kPiece];
+    __shared__ alignas(16) float high[kPiece], low[kPiece], betas[kPiece];
     ptx::grid_dep_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int piece = blockIdx.x % a.pieces, bk = blockIdx.x / a.pieces, hk = bk % a.Hk, b = bk / a.Hk;
