@@ -227,45 +227,74 @@ struct PieceBars {
     alignas(16) float factors[kFactors * kPiece];              // (read in fours)
     float dots[8][kPiece], sums[16];
 };
-// What a thread has under way of 32 columns of V: quads, of what the passes kept its lanes have rows, of dO eight threads have a row.
+// A piece of a head, as one block finds it.
+struct Place {
+    int b, h, live, there;                                     // tokens of the sequence, rows of the tensors
+    long long row0;
+    size_t unit;
+    __device__ Place(const DeltaArgs& a, unsigned id)
+    {
+        const int piece = id % a.pieces, bh = id / a.pieces;
+        h = bh % a.H, b = bh / a.H, unit = id, row0 = (long long)b * a.L + (long long)piece * kPiece;
+        live = min(sequence_length(a.lengths, b, a.L) - piece * kPiece, kPiece), there = min(a.L - piece * kPiece, kPiece);
+    }
+};
+// What a thread has under way of 32 columns of V: quads.  Of what the passes kept two lanes have the two of a unit of 16 bytes and the next two the next row, so that
+// half a warp reads whole lines and fills every bank once; of dO eight threads have a row.
 template <typename T, int KD, bool WIDE>
 struct Quads {
     static constexpr int ACROSS = Piecewise<T, KD>::WORKERS / KD, N = 8 / ACROSS;        // quads of a row of S at once, of a thread
+    static __device__ __forceinline__ int quad(int tid, int rows) { return (tid & 1) + 2 * (tid / (2 * rows)); }
+    static __device__ __forceinline__ int row(int tid, int rows) { return (tid >> 1) % rows; }
     SavedRow<4> s[N], ds[N], dv, e;
     Row<T, 4> dout;
-    __device__ __forceinline__ void fetch(const DeltaArgs& a, size_t unit, const T* grads, int live, int v0, int tid)
+    __device__ __forceinline__ void fetch(const DeltaArgs& a, const Place& at, int v0, int tid)
     {
-        const int k = tid % KD, q = tid / KD, t = tid % kPiece, p = tid / kPiece, r = tid >> 3, c = (tid & 7) * 4;
+        const int k = row(tid, KD), q = quad(tid, KD), t = row(tid, kPiece), p = quad(tid, kPiece), r = tid >> 3, c = (tid & 7) * 4;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int v = v0 + 4 * (q + ACROSS * i);
-            s[i].load(a.states + quad_at(unit, a.VP, KD, v, k), KD, a.VP - v), ds[i].load(a.dstates + quad_at(unit, a.VP, KD, v, k), KD, a.VP - v);
+            s[i].load(a.states + quad_at(at.unit, a.VP, KD, v, k), KD, a.VP - v), ds[i].load(a.dstates + quad_at(at.unit, a.VP, KD, v, k), KD, a.VP - v);
         }
         const int v = v0 + 4 * p;
-        dv.load(a.dupdates + quad_at(unit, a.VP, kPiece, v, t), kPiece, a.VP - v), e.load(a.updates + quad_at(unit, a.VP, kPiece, v, t), kPiece, a.VP - v);
-        dout.template load<WIDE>(grads + r * a.lddo + v0 + c, r < live ? a.V - v0 - c : 0);
+        dv.load(a.dupdates + quad_at(at.unit, a.VP, kPiece, v, t), kPiece, a.VP - v), e.load(a.updates + quad_at(at.unit, a.VP, kPiece, v, t), kPiece, a.VP - v);
+        dout.template load<WIDE>(static_cast<const T*>(a.dout) + (at.row0 + r) * a.lddo + (long long)at.h * a.V + v0 + c, r < at.live ? a.V - v0 - c : 0);
     }
-    __device__ __forceinline__ void put(unsigned char* at, float& inner, int tid) const
+};
+// Their places in a block's tiles.
+template <typename T, int KD>
+struct QuadPlaces {
+    using W = Piecewise<T, KD>;
+    using Q = Quads<T, KD, true>;
+    int s[Q::N], row, dout;
+    __device__ explicit QuadPlaces(int tid)
     {
-        using W = Piecewise<T, KD>;
-        const int k = tid % KD, q = tid / KD, t = tid % kPiece, p = tid / kPiece, r = tid >> 3, c = (tid & 7) * 4;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            put_four<W::NB>(at + W::at_s, W::state_part, k, 4 * (q + ACROSS * i), s[i].q[0].e);
-            put_four<W::NB>(at + W::at_ds, W::state_part, k, 4 * (q + ACROSS * i), ds[i].q[0].e);
+        for (int i = 0; i < Q::N; ++i) s[i] = four_at<W::NB>(Q::row(tid, KD), 4 * (Q::quad(tid, KD) + Q::ACROSS * i));
+        row = four_at<W::NB>(Q::row(tid, kPiece), 4 * Q::quad(tid, kPiece)), dout = four_at<W::NB>(kPiece + (tid >> 3), (tid & 7) * 4);
+    }
+    template <bool WIDE>
+    __device__ __forceinline__ void put(unsigned char* at, const Quads<T, KD, WIDE>& x, float& inner) const
+    {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) inner = fmaf(s[i].q[0].e[n], ds[i].q[0].e[n], inner);
+        for (int i = 0; i < Q::N; ++i) {
+            put_four<kSum>(at + W::at_s + s[i], W::state_part, x.s[i].q[0].e);
+            put_four<kSum>(at + W::at_ds + s[i], W::state_part, x.ds[i].q[0].e);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) inner = fmaf(x.s[i].q[0].e[n], x.ds[i].q[0].e[n], inner);
         }
         float f[4];
-        dout.get(f);
-        put_four<W::NB>(at, W::rows_part, t, 4 * p, dv.q[0].e);
-        put_four<W::NB>(at + W::at_e, W::e_part, t, 4 * p, e.q[0].e);
-        put_four<W::NB>(at, W::rows_part, kPiece + r, c, f);
+        x.dout.get(f);
+        put_four<kSum>(at + row, W::rows_part, x.dv.q[0].e);
+        put_four<kSum>(at + W::at_e + row, W::e_part, x.e.q[0].e);
+        put_four<W::IN>(at + dout, W::rows_part, f);
     }
 };
 
+// A block takes pieces gridDim.x apart; the next one's first numbers are under way while this one's results go out, the others come to the L2 cache meanwhile.  (A block for
+// each piece: 240 us of a training step of 2048 of them, 17 us each, of which four pass between two blocks.)
 template <typename T, int KD, bool WIDE>
-__global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces_kernel(const DeltaArgs a)
+__global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces_kernel(const DeltaArgs a, unsigned total)
 {
     using W = Piecewise<T, KD>;
     constexpr int IN = W::IN, NB = W::NB;
@@ -274,30 +303,7 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
     unsigned char* raw = unaligned + ((1024 - (ptx::smem_u32(unaligned) & 1023)) & 1023);
     volatile uint32_t* abort_flag = &bars.abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int piece = blockIdx.x % a.pieces, bh = blockIdx.x / a.pieces, h = bh % a.H, b = bh / a.H, hk = h / a.share;
-    const long long row0 = (long long)b * a.L + (long long)piece * kPiece;
-    ptx::grid_dep_wait();
-    const int live = min(sequence_length(a.lengths, b, a.L) - piece * kPiece, kPiece), there = min(a.L - piece * kPiece, kPiece);
-    const bool shared_key = a.dq_parts != nullptr;
-    T *dq = static_cast<T*>(a.dq) + row0 * a.lddq + (long long)hk * a.K, *dk = static_cast<T*>(a.dk) + row0 * a.lddk + (long long)hk * a.K;
-    const long long part0 = (row0 * a.H + h) * a.K;
-    // padding
-    if (live < there) {
-        const int first = max(live, 0);
-        for (int i = tid; i < (there - first) * a.K; i += W::THREADS) {
-            const int row = first + i / a.K, col = i % a.K;
-            if (shared_key) a.dq_parts[part0 + (long long)row * a.H * a.K + col] = 0.f, a.dk_parts[part0 + (long long)row * a.H * a.K + col] = 0.f;
-            else dq[row * a.lddq + col] = from_float<T>(0.f), dk[row * a.lddk + col] = from_float<T>(0.f);
-        }
-        for (int i = first + tid; i < there; i += W::THREADS) a.dg[(row0 + i) * a.lddg + h] = 0.f, a.dbeta[(row0 + i) * a.lddbeta + h] = 0.f;
-    }
-    if (live <= 0) return;
-
-    const size_t unit = (size_t)bh * a.pieces + piece;
-    const T* grads = static_cast<const T*>(a.dout) + row0 * a.lddo + (long long)h * a.V;
-    Quads<T, KD, WIDE> even, odd;
-    const bool works = warp < W::WORKERS / 32;
-    if (works) even.fetch(a, unit, grads, live, 0, tid);
+    const bool works = warp < W::WORKERS / 32, shared_key = a.dq_parts != nullptr;
     if (tid == 0) {
         bars.abort = 0;
         ptx::mbar_init(&bars.done[0], 1), ptx::mbar_init(&bars.done[1], 1), ptx::mbar_init(&bars.keys, 1), ptx::mbar_init(&bars.last, 1);
@@ -307,47 +313,74 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
         ptx::tmem_alloc(&bars.tmem, W::cols);
         ptx::tmem_relinquish();
     }
-    for (int i = tid; i < kFactors * kPiece; i += W::THREADS) bars.factors[i] = reinterpret_cast<const float*>(a.prepared + unit * kPrepared + kSquares)[i];
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
-    const uint32_t tmem = bars.tmem, base = ptx::smem_u32(raw);
+    const uint32_t tmem = bars.tmem, base = ptx::smem_u32(raw), keys = base, squares = base + W::keys;
     const int blocks = (a.VP + NB - 1) / NB;
-    const uint32_t keys = base, squares = base + W::keys;
+    ptx::grid_dep_wait();
+
+    // padding of all its pieces; from then on only pieces with tokens
+    for (unsigned id = blockIdx.x; id < total; id += gridDim.x) {
+        const Place at(a, id);
+        if (at.live >= at.there) continue;
+        const int first = max(at.live, 0), hk = at.h / a.share;
+        for (int i = tid; i < (at.there - first) * a.K; i += W::THREADS) {
+            const long long r = at.row0 + first + i / a.K;
+            const int col = i % a.K;
+            if (shared_key) a.dq_parts[(r * a.H + at.h) * a.K + col] = 0.f, a.dk_parts[(r * a.H + at.h) * a.K + col] = 0.f;
+            else static_cast<T*>(a.dq)[r * a.lddq + (long long)hk * a.K + col] = from_float<T>(0.f), static_cast<T*>(a.dk)[r * a.lddk + (long long)hk * a.K + col] = from_float<T>(0.f);
+        }
+        for (int i = first + tid; i < at.there; i += W::THREADS) a.dg[(at.row0 + i) * a.lddg + at.h] = 0.f, a.dbeta[(at.row0 + i) * a.lddbeta + at.h] = 0.f;
+    }
+    auto following = [&](unsigned id) {
+        while (id < total && Place(a, id).live <= 0) id += gridDim.x;
+        return id;
+    };
+    // completions of done[0] and done[1] in a piece, and so far
+    const int first_of = (blocks + 1) / 2, second_of = blocks / 2;
+    int first_so_far = 0, second_so_far = 0, parity = 0;
+    const unsigned begin = following(blockIdx.x);
 
     if (!works) {
         const uint32_t elected = ptx::elect_one();
         constexpr uint32_t idk = ptx::idesc_b16(128, KD, false);
         // tiles of rows of 32 numbers, K-major: 64-byte swizzle
         auto narrow = [](uint32_t at) { return rows_as_k<32>(at, 512); };
-        for (int j = 0; j < blocks; ++j) {
-            __syncthreads();
+        bool alive = true;
+        for (unsigned id = begin; id < total; id = following(id + gridDim.x), parity ^= 1) {
+            const Place here(a, id);
+            for (int j = 0; j < blocks; ++j) {
+                __syncthreads();
+                ptx::tc_fence_after_sync();
+                const uint32_t at = base + (j & 1) * W::block;
+                auto rows = [&](int p, int k) { return narrow(at + p * W::rows_part + k * 32); };
+                auto e = [&](int p, int k) { return narrow(at + W::at_e + p * W::e_part + k * 32); };
+                multiply(tmem + W::d1, kSum, kSum, NB / 16, idk, elected, j > 0, rows, [&](int p, int k) { return narrow(at + W::at_s + p * W::state_part + k * 32); });
+                multiply(tmem + W::d2, kSum, kSum, NB / 16, ptx::idesc_b16(128, kPiece, false), elected, j > 0, rows, e);
+                multiply(tmem + W::d3, kSum, kSum, NB / 16, idk, elected, j > 0, e, [&](int p, int k) { return narrow(at + W::at_ds + p * W::state_part + k * 32); });
+                ptx::mma_commit(&bars.done[j & 1], elected);
+            }
+            first_so_far += first_of, second_so_far += second_of;
+            alive = alive && ptx::mbar_wait_bounded_warp(&bars.done[(blocks - 1) & 1], (((blocks - 1) & 1 ? second_so_far : first_so_far) - 1) & 1, abort_flag, a.max_polls);
+            if (alive && elected) {                            // (the tiles over V are done with)
+                ptx::mbar_arrive_expect_tx(&bars.keys, W::keys);
+                ptx::bulk_g2s(raw, a.keys + (((size_t)here.b * a.Hk + here.h / a.share) * a.pieces + id % a.pieces) * W::keys, W::keys, &bars.keys);
+            }
+            alive = alive && ptx::mbar_wait_bounded_warp(&bars.keys, parity, abort_flag, a.max_polls);
+            __syncthreads();                                   // [y; p] is there
             ptx::tc_fence_after_sync();
-            const uint32_t at = base + (j & 1) * W::block;
-            auto rows = [&](int p, int k) { return narrow(at + p * W::rows_part + k * 32); };
-            auto e = [&](int p, int k) { return narrow(at + W::at_e + p * W::e_part + k * 32); };
-            multiply(tmem + W::d1, kSum, kSum, NB / 16, idk, elected, j > 0, rows, [&](int p, int k) { return narrow(at + W::at_s + p * W::state_part + k * 32); });
-            multiply(tmem + W::d2, kSum, kSum, NB / 16, ptx::idesc_b16(128, kPiece, false), elected, j > 0, rows, e);
-            multiply(tmem + W::d3, kSum, kSum, NB / 16, idk, elected, j > 0, e, [&](int p, int k) { return narrow(at + W::at_ds + p * W::state_part + k * 32); });
-            ptx::mma_commit(&bars.done[j & 1], elected);
+            if (alive) {
+                auto tokens = [&](int p, int k) { return columns_as_m(keys + p * W::key_part + k * 16 * 128, W::HALF); };
+                multiply(tmem + W::d4, kSum, IN, kPiece / 16, idk | ptx::kIdescBMajorMN, elected, false,
+                         [&](int p, int k) { return rows_as_m(squares + p * W::square_part + k * 32); }, tokens);
+                multiply(tmem + W::d5, kSum, IN, 2 * kPiece / 16, idk | ptx::kIdescBMajorMN | kIdescAMajorM, elected, false,
+                         [&](int p, int k) { return columns_as_m(squares + p * W::square_part + k * 16 * 128, W::square_part); }, tokens);
+                ptx::mma_commit(&bars.last, elected);
+            }
+            __syncthreads();                                   // (results are collected)
+            __syncthreads();                                   // (and out)
         }
-        bool alive = ptx::mbar_wait_bounded_warp(&bars.done[(blocks - 1) & 1], ((blocks - 1) >> 1) & 1, abort_flag, a.max_polls);
-        if (alive && elected) {                                // (the tiles over V are done with)
-            ptx::mbar_arrive_expect_tx(&bars.keys, W::keys);
-            ptx::bulk_g2s(raw, a.keys + (((size_t)b * a.Hk + hk) * a.pieces + piece) * W::keys, W::keys, &bars.keys);
-        }
-        alive = alive && ptx::mbar_wait_bounded_warp(&bars.keys, 0, abort_flag, a.max_polls);
-        __syncthreads();                                       // [y; p] is there
-        ptx::tc_fence_after_sync();
-        if (alive) {
-            auto tokens = [&](int p, int k) { return columns_as_m(keys + p * W::key_part + k * 16 * 128, W::HALF); };
-            multiply(tmem + W::d4, kSum, IN, kPiece / 16, idk | ptx::kIdescBMajorMN, elected, false, [&](int p, int k) { return rows_as_m(squares + p * W::square_part + k * 32); },
-                     tokens);
-            multiply(tmem + W::d5, kSum, IN, 2 * kPiece / 16, idk | ptx::kIdescBMajorMN | kIdescAMajorM, elected, false,
-                     [&](int p, int k) { return columns_as_m(squares + p * W::square_part + k * 16 * 128, W::square_part); }, tokens);
-            ptx::mma_commit(&bars.last, elected);
-        }
-        __syncthreads();
         ptx::tc_fence_after_sync();
         ptx::tmem_dealloc(tmem, W::cols);
         if (lane == 0 && *abort_flag) atomicExch(a.timeout, 1u);
@@ -356,154 +389,177 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
 
     const int quarter = warp & 3, row = quarter * 32 + lane, side = warp >> 2, token = row & (kPiece - 1);
     const bool is_key = row < kPiece;
-    float inner = 0.f;                                         // <S, dS>
-    odd.fetch(a, unit, grads, live, NB, tid);                  // (nothing is read behind the last column)
-    if (warp == 4 || warp == 5) {                              // dbeta, a sum over the walk's columns
-        const int r = (warp - 4) * 32 + lane, tiles = a.VP / 16;
-        const float* from = a.dbeta_parts + unit * tiles * kPiece + r;
-        float s = 0.f;
-        for (int i = 0; i < tiles; ++i) s += from[i * kPiece];
-        if (r < live) a.dbeta[(row0 + r) * a.lddbeta + h] = s;
-    }
+    const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
+    const float *eg = bars.factors, *ed = eg + kPiece, *be = eg + 2 * kPiece, *high = eg + 3 * kPiece, *low = eg + 4 * kPiece;
+    const QuadPlaces<T, KD> places(tid);
+    Quads<T, KD, WIDE> next;
+    float factor = 0.f;
+    auto fetch = [&](unsigned id) {                            // a piece's first block and factors
+        if (id >= total) return;
+        const Place at(a, id);
+        next.fetch(a, at, 0, tid);
+        factor = load_masked<float, 1>(reinterpret_cast<const float*>(a.prepared + at.unit * kPrepared + kSquares) + tid, tid < kFactors * kPiece).e[0];
+    };
     auto ready = [&] {                                         // for the products
         ptx::fence_proxy_async_smem();
         ptx::tc_fence_before_sync();
         __syncthreads();
     };
-    for (int j = 0; j < blocks; j += 2) {
-        if (j >= 2) ptx::mbar_wait_bounded(&bars.done[0], ((j >> 1) - 1) & 1, abort_flag, a.max_polls);
-        even.put(raw, inner, tid);
-        if (j + 2 < blocks) even.fetch(a, unit, grads, live, (j + 2) * NB, tid);
-        ready();
-        if (j + 1 < blocks) {
-            if (j >= 2) ptx::mbar_wait_bounded(&bars.done[1], ((j >> 1) - 1) & 1, abort_flag, a.max_polls);
-            odd.put(raw + W::block, inner, tid);
-            if (j + 3 < blocks) odd.fetch(a, unit, grads, live, (j + 3) * NB, tid);
+    fetch(begin);
+    for (unsigned id = begin; id < total; parity ^= 1) {
+        const Place here(a, id);
+        const unsigned then = following(id + gridDim.x);
+        float inner = 0.f;                                     // <S, dS>
+        if (tid < kFactors * kPiece) bars.factors[tid] = factor;
+        if (tid < 4 && then < total) {
+            const size_t state = (size_t)KD * a.VP * 4, update = (size_t)kPiece * a.VP * 4;
+            const char* from = tid == 0 ? reinterpret_cast<const char*>(a.states) + then * state : tid == 1 ? reinterpret_cast<const char*>(a.dstates) + then * state
+                             : tid == 2 ? reinterpret_cast<const char*>(a.updates) + then * update : reinterpret_cast<const char*>(a.dupdates) + then * update;
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((unsigned)(tid < 2 ? state : update)) : "memory");
+        }
+        for (int j = 0; j < blocks; ++j) {
+            if (j >= 2) ptx::mbar_wait_bounded(&bars.done[j & 1], ((j & 1 ? second_so_far : first_so_far) + (j >> 1) - 1) & 1, abort_flag, a.max_polls);
+            places.put(raw + (j & 1) * W::block, next, inner);
+            if (j + 1 < blocks) next.fetch(a, here, (j + 1) * NB, tid);
             ready();
         }
-    }
-    ptx::mbar_wait_bounded(&bars.done[(blocks - 1) & 1], ((blocks - 1) >> 1) & 1, abort_flag, a.max_polls);
-    ptx::tc_fence_after_sync();
-    const float *eg = bars.factors, *ed = eg + kPiece, *be = eg + 2 * kPiece, *high = eg + 3 * kPiece, *low = eg + 4 * kPiece;
-    const uint32_t lanes = tmem + ((uint32_t)quarter << 21);
-    {
-        float x[16];
-        tmem_row<16>(lanes + W::d2 + side * 16, x);
-        const float hi = high[token], lo = low[token], by = is_key ? -1.f : a.scale;
-        const int last = is_key ? token - 1 : token;           // (keys: j < i, queries: j <= i)
-#pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-            const int other = side * 16 + j;
-            const float4 h4 = *reinterpret_cast<const float4*>(high + other), l4 = *reinterpret_cast<const float4*>(low + other),
-                         b4 = *reinterpret_cast<const float4*>(be + other);
-            const float hs[4] = {h4.x, h4.y, h4.z, h4.w}, ls[4] = {l4.x, l4.y, l4.z, l4.w}, bs[4] = {b4.x, b4.y, b4.z, b4.w};
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const float d = ex2(((hi - hs[n]) + (lo - ls[n])) * kLog2e) * bs[n] * by;
-                x[j + n] = other + n <= last ? d * x[j + n] : 0.f;
-            }
-        }
-        put_row<64, 16>(raw + W::keys, W::square_part, row, side * 16, x);
-    }
-    ready();
-    ptx::mbar_wait_bounded(&bars.keys, 0, abort_flag, a.max_polls);
-    ptx::mbar_wait_bounded(&bars.last, 0, abort_flag, a.max_polls);
-    ptx::tc_fence_after_sync();
-    // <S after, dS> = e^G_63 <S, dS> + sum over tokens of k . (e^(G_63 - G) beta E dS^T)
-    float after = eg[kPiece - 1] * inner, dot = 0.f;
-    const float x1 = is_key ? -eg[token] : a.scale * eg[token], x3 = ed[token] * be[token];
-    unsigned char* collected = raw + W::keys;                  // [128 rows][KD] of what goes out, fp32 for shared keys
-    const int bytes = shared_key ? 4 : (int)sizeof(T), units = KD * bytes / 16;
-    // unit u of row r, spread over the banks
-    auto collect_at = [&](int r, int u) { return (r * units + (u ^ (r & 7))) * 16; };
-    constexpr int SHARE = KD / 4;
-#pragma unroll
-    for (int i = 0; i < SHARE; i += 16) {
-        const int col = side * SHARE + i;
-        float x[16], y[16], z[16];
-        uint32_t v1[16], v3[16], v4[16], v5[16];
-        ptx::tmem_ld16(lanes + W::d1 + col, v1), ptx::tmem_ld16(lanes + W::d4 + col, v4);
-        if (is_key) ptx::tmem_ld16(lanes + W::d3 + col, v3), ptx::tmem_ld16(lanes + W::d5 + col, v5);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) z[j] = 0.f;
-#pragma unroll
-        for (int p = IN - 1; p >= 0; --p)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float f[8];
-                unpack(*reinterpret_cast<const Pack<bf16, 8>*>(raw + unit_at<64>(p * W::key_part + (col >> 6) * W::HALF, row, ((col & 63) >> 3) + u)), f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) z[8 * u + j] += f[j];
-            }
-        ptx::tmem_ld_wait();
-#pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = fmaf(x1, __uint_as_float(v1[j]), __uint_as_float(v4[j])), dot = fmaf(z[j], x[j], dot);
-        if (is_key) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                y[j] = x3 * __uint_as_float(v3[j]), after = fmaf(z[j], y[j], after);
-                y[j] += __uint_as_float(v5[j]), dot = fmaf(-z[j], y[j], dot);
-                x[j] += y[j];
-            }
-        }
-        if (shared_key) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) *reinterpret_cast<float4*>(collected + collect_at(row, col / 4 + u)) = make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
-        } else {
-            constexpr int PER = 16 / (int)sizeof(T);
-#pragma unroll
-            for (int u = 0; u < 16 / PER; ++u) {
-                float f[PER];
-#pragma unroll
-                for (int j = 0; j < PER; ++j) f[j] = x[u * PER + j];
-                store_pack<T, PER>(reinterpret_cast<T*>(collected + collect_at(row, col / PER + u)), pack<T, PER>(f));
-            }
-        }
-    }
-    bars.dots[side * 2 + (is_key ? 0 : 1)][token] = dot;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) after += __shfl_xor_sync(0xffffffffu, after, d);
-    if (lane == 0) bars.sums[warp] = after;
-    ptx::tc_fence_before_sync();
-    __syncthreads();
-    // rows of dk, then of dq, whole lines at a time
-    if (WIDE) {
-        for (int i = tid; i < 2 * kPiece * units; i += W::WORKERS) {
-            const int r = i / units, u = i % units, t = r & (kPiece - 1), col = u * 16 / bytes;
-            if (t >= live || col >= a.K) continue;
-            const uint4 v = *reinterpret_cast<const uint4*>(collected + collect_at(r, u));
-            if (shared_key) *reinterpret_cast<uint4*>((r < kPiece ? a.dk_parts : a.dq_parts) + part0 + (long long)t * a.H * a.K + col) = v;
-            else *reinterpret_cast<uint4*>(r < kPiece ? dk + t * a.lddk + col : dq + t * a.lddq + col) = v;
-        }
-    } else {
-        for (int i = tid; i < 2 * kPiece * KD; i += W::WORKERS) {
-            const int r = i / KD, col = i % KD, t = r & (kPiece - 1);
-            if (t >= live || col >= a.K) continue;
-            const unsigned char* from = collected + collect_at(r, col * bytes / 16) + col * bytes % 16;
-            if (shared_key) (r < kPiece ? a.dk_parts : a.dq_parts)[part0 + (long long)t * a.H * a.K + col] = *reinterpret_cast<const float*>(from);
-            else *(r < kPiece ? dk + t * a.lddk + col : dq + t * a.lddq + col) = *reinterpret_cast<const T*>(from);
-        }
-    }
-    if (warp == 0) {                                           // sums from the last token back, two tokens a lane
-        float last = 0.f;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) last += bars.sums[w];
-        auto total = [&](int i) {
+        if (warp == 4 || warp == 5) {                          // dbeta, a sum over the walk's columns
+            const int r = (warp - 4) * 32 + lane, tiles = a.VP / 16;
+            const float* from = a.dbeta_parts + here.unit * tiles * kPiece + r;
             float s = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s += bars.dots[j][i];
-            return s;
-        };
-        const float x1 = total(63 - 2 * lane), x0 = total(62 - 2 * lane);
-        float s = x0 + x1;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const float y = __shfl_up_sync(0xffffffffu, s, d);
-            if (lane >= d) s += y;
+            for (int i = 0; i < tiles; ++i) s += from[i * kPiece];
+            if (r < here.live) a.dbeta[(here.row0 + r) * a.lddbeta + here.h] = s;
         }
-        const int first = 62 - 2 * lane;
-        if (first < live) a.dg[(row0 + first) * a.lddg + h] = s + last;
-        if (first + 1 < live) a.dg[(row0 + first + 1) * a.lddg + h] = (s - x0) + last;
+        first_so_far += first_of, second_so_far += second_of;
+        ptx::mbar_wait_bounded(&bars.done[(blocks - 1) & 1], (((blocks - 1) & 1 ? second_so_far : first_so_far) - 1) & 1, abort_flag, a.max_polls);
+        ptx::tc_fence_after_sync();
+        {
+            float x[16];
+            tmem_row<16>(lanes + W::d2 + side * 16, x);
+            const float hi = high[token], lo = low[token], by = is_key ? -1.f : a.scale;
+            const int last = is_key ? token - 1 : token;       // (keys: j < i, queries: j <= i)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                const int other = side * 16 + j;
+                const float4 h4 = *reinterpret_cast<const float4*>(high + other), l4 = *reinterpret_cast<const float4*>(low + other),
+                             b4 = *reinterpret_cast<const float4*>(be + other);
+                const float hs[4] = {h4.x, h4.y, h4.z, h4.w}, ls[4] = {l4.x, l4.y, l4.z, l4.w}, bs[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const float d = ex2(((hi - hs[n]) + (lo - ls[n])) * kLog2e) * bs[n] * by;
+                    x[j + n] = other + n <= last ? d * x[j + n] : 0.f;
+                }
+            }
+            put_row<64, 16>(raw + W::keys, W::square_part, row, side * 16, x);
+        }
+        ready();
+        ptx::mbar_wait_bounded(&bars.keys, parity, abort_flag, a.max_polls);
+        ptx::mbar_wait_bounded(&bars.last, parity, abort_flag, a.max_polls);
+        ptx::tc_fence_after_sync();
+        // <S after, dS> = e^G_63 <S, dS> + sum over tokens of k . (e^(G_63 - G) beta E dS^T)
+        float after = eg[kPiece - 1] * inner, dot = 0.f;
+        const float x1 = is_key ? -eg[token] : a.scale * eg[token], x3 = ed[token] * be[token];
+        unsigned char* collected = raw + W::keys;              // [128 rows][KD] of what goes out, fp32 for shared keys
+        const int bytes = shared_key ? 4 : (int)sizeof(T), units = KD * bytes / 16;
+        // unit u of row r, spread over the banks
+        auto collect_at = [&](int r, int u) { return (r * units + (u ^ (r & 7))) * 16; };
+        constexpr int SHARE = KD / 4;
+#pragma unroll
+        for (int i = 0; i < SHARE; i += 16) {
+            const int col = side * SHARE + i;
+            float x[16], z[16];
+            uint32_t v[16], w[16];
+            ptx::tmem_ld16(lanes + W::d1 + col, v), ptx::tmem_ld16(lanes + W::d4 + col, w);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) z[j] = 0.f;
+#pragma unroll
+            for (int p = IN - 1; p >= 0; --p)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float f[8];
+                    unpack(*reinterpret_cast<const Pack<bf16, 8>*>(raw + unit_at<64>(p * W::key_part + (col >> 6) * W::HALF, row, ((col & 63) >> 3) + u)), f);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) z[8 * u + j] += f[j];
+                }
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[j] = fmaf(x1, __uint_as_float(v[j]), __uint_as_float(w[j])), dot = fmaf(z[j], x[j], dot);
+            if (is_key) {
+                ptx::tmem_ld16(lanes + W::d3 + col, v), ptx::tmem_ld16(lanes + W::d5 + col, w);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    float y = x3 * __uint_as_float(v[j]);
+                    after = fmaf(z[j], y, after);
+                    y += __uint_as_float(w[j]), dot = fmaf(-z[j], y, dot);
+                    x[j] += y;
+                }
+            }
+            if (shared_key) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) *reinterpret_cast<float4*>(collected + collect_at(row, col / 4 + u)) = make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
+            } else {
+                constexpr int PER = 16 / (int)sizeof(T);
+#pragma unroll
+                for (int u = 0; u < 16 / PER; ++u) {
+                    float f[PER];
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) f[j] = x[u * PER + j];
+                    store_pack<T, PER>(reinterpret_cast<T*>(collected + collect_at(row, col / PER + u)), pack<T, PER>(f));
+                }
+            }
+        }
+        id = then;
+        fetch(id);
+        bars.dots[side * 2 + (is_key ? 0 : 1)][token] = dot;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) after += __shfl_xor_sync(0xffffffffu, after, d);
+        if (lane == 0) bars.sums[warp] = after;
+        ptx::tc_fence_before_sync();
+        __syncthreads();
+        // rows of dk, then of dq, whole lines at a time
+        const int hk = here.h / a.share;
+        T *dq = static_cast<T*>(a.dq) + here.row0 * a.lddq + (long long)hk * a.K, *dk = static_cast<T*>(a.dk) + here.row0 * a.lddk + (long long)hk * a.K;
+        const long long part0 = (here.row0 * a.H + here.h) * a.K;
+        if (WIDE) {
+            for (int i = tid; i < 2 * kPiece * units; i += W::WORKERS) {
+                const int r = i / units, u = i % units, t = r & (kPiece - 1), col = u * 16 / bytes;
+                if (t >= here.live || col >= a.K) continue;
+                const uint4 v = *reinterpret_cast<const uint4*>(collected + collect_at(r, u));
+                if (shared_key) *reinterpret_cast<uint4*>((r < kPiece ? a.dk_parts : a.dq_parts) + part0 + (long long)t * a.H * a.K + col) = v;
+                else *reinterpret_cast<uint4*>(r < kPiece ? dk + t * a.lddk + col : dq + t * a.lddq + col) = v;
+            }
+        } else {
+            for (int i = tid; i < 2 * kPiece * KD; i += W::WORKERS) {
+                const int r = i / KD, col = i % KD, t = r & (kPiece - 1);
+                if (t >= here.live || col >= a.K) continue;
+                const unsigned char* from = collected + collect_at(r, col * bytes / 16) + col * bytes % 16;
+                if (shared_key) (r < kPiece ? a.dk_parts : a.dq_parts)[part0 + (long long)t * a.H * a.K + col] = *reinterpret_cast<const float*>(from);
+                else *(r < kPiece ? dk + t * a.lddk + col : dq + t * a.lddq + col) = *reinterpret_cast<const T*>(from);
+            }
+        }
+        if (warp == 0) {                                       // sums from the last token back, two tokens a lane
+            float last = 0.f;
+#pragma unroll
+            for (int w = 0; w < 16; ++w) last += bars.sums[w];
+            auto sum = [&](int i) {
+                float s = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s += bars.dots[j][i];
+                return s;
+            };
+            const float g1 = sum(63 - 2 * lane), g0 = sum(62 - 2 * lane);
+            float s = g0 + g1;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const float y = __shfl_up_sync(0xffffffffu, s, d);
+                if (lane >= d) s += y;
+            }
+            const int first = 62 - 2 * lane;
+            if (first < here.live) a.dg[(here.row0 + first) * a.lddg + here.h] = s + last;
+            if (first + 1 < here.live) a.dg[(here.row0 + first + 1) * a.lddg + here.h] = (s - g0) + last;
+        }
+        __syncthreads();
     }
 }
 
@@ -542,7 +598,8 @@ conv2d_status_t backward_pieces(const DeltaArgs& a, cudaStream_t stream)
     using W = Piecewise<T, KD>;
     static SmemLimit limit;
     if (raise_smem_limit((const void*)delta_bwd_pieces_kernel<T, KD, WIDE>, W::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-    if (launch_pdl(delta_bwd_pieces_kernel<T, KD, WIDE>, dim3((unsigned)(a.B * a.H) * (unsigned)a.pieces), dim3(W::THREADS), W::smem, stream, a) != cudaSuccess)
+    const unsigned total = (unsigned)(a.B * a.H) * (unsigned)a.pieces, most = (unsigned)sm_count();
+    if (launch_pdl(delta_bwd_pieces_kernel<T, KD, WIDE>, dim3(total < most ? total : most), dim3(W::THREADS), W::smem, stream, a, total) != cudaSuccess)
         return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;

@@ -88,15 +88,17 @@ __device__ __forceinline__ void put_row(unsigned char* tile, int part_bytes, int
     }
 }
 
-// Four numbers likewise.
-template <int NV>
-__device__ __forceinline__ void put_four(unsigned char* tile, int part_bytes, int row, int col, const float (&f)[4])
+// Four numbers, of which the first PARTS parts are not zero, likewise at place four_at() of a tile.
+template <int NV> __device__ __forceinline__ int four_at(int row, int col) { return (int)unit_at<NV>(0, row, col / 8) + (col & 4) * 2; }
+template <int PARTS>
+__device__ __forceinline__ void put_four(unsigned char* at, int part_bytes, const float (&f)[4])
 {
-    uint32_t w[2][kSum];
-    split<kSum>(f[0], f[1], w[0]);
-    split<kSum>(f[2], f[3], w[1]);
+    uint32_t w[2][PARTS];
+    split<PARTS>(f[0], f[1], w[0]);
+    split<PARTS>(f[2], f[3], w[1]);
 #pragma unroll
-    for (int p = 0; p < kSum; ++p) *reinterpret_cast<uint2*>(tile + p * part_bytes + unit_at<NV>(0, row, col / 8) + (col & 4) * 2) = make_uint2(w[0][p], w[1][p]);
+    for (int p = 0; p < kSum; ++p)
+        *reinterpret_cast<uint2*>(at + p * part_bytes) = p < PARTS ? make_uint2(w[0][p < PARTS ? p : 0], w[1][p < PARTS ? p : 0]) : make_uint2(0u, 0u);
 }
 
 template <bool WIDE, typename T, int N>
