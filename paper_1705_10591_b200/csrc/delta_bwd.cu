@@ -125,8 +125,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             const float eg = factors[token], ed = factors[kPiece + token], beta = factors[2 * kPiece + token], whole = factors[kPiece - 1];
             if (!is_key) {
                 Tile<T, NV>::get(values, token, col0, y);
-#pragma unroll
-                for (int j = 0; j < C; ++j) y[j] *= a.scale;
+                scaled(y, a.scale, y);
                 put_row<NV, C>(rows, W::rows_part, row, col0, y);
             }
             // D1: K dS
@@ -134,8 +133,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             ptx::tc_fence_after_sync();
             if (is_key) {
                 tmem_digits<C>(at, NV, X);
-#pragma unroll
-                for (int j = 0; j < C; ++j) X[j] *= ed, y[j] = beta * X[j];
+                scaled(X, ed, X);
+                scaled(y, beta, X);
                 put_row<NV, C>(rows, W::rows_part, row, col0, y);
             }
             ptx::fence_proxy_async_smem();
@@ -147,16 +146,13 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             float sum = 0.f;
             if (is_key) {
                 tmem_digits<C>(at + 3 * NV, NV, y);
+                add_scaled(y, 1.f, X);
 #pragma unroll
-                for (int j = 0; j < C; ++j) {
-                    y[j] += X[j];
-                    sum = fmaf(y[j], update.q[j / 4].e[j % 4], sum);
-                    X[j] = beta * y[j];
-                    y[j] = -eg * X[j];
-                }
+                for (int j = 0; j < C; ++j) sum = fmaf(y[j], update.q[j / 4].e[j % 4], sum);
+                scaled(X, beta, y);
+                scaled(y, -eg, X);
             } else {
-#pragma unroll
-                for (int j = 0; j < C; ++j) y[j] *= eg;
+                scaled(y, eg, y);
             }
             put_row<NV, C>(rows, W::rows_part, row, col0, y);
             ptx::fence_proxy_async_smem();
@@ -177,8 +173,9 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
             ptx::mbar_wait_bounded(&bars->done[2], parity, abort_flag, a.max_polls);
             ptx::tc_fence_after_sync();
             tmem_digits<C>(at, NV, y);
+            add_scaled(y, whole, S);
 #pragma unroll
-            for (int j = 0; j < C; ++j) S[j] = fmaf(whole, S[j], y[j]);
+            for (int j = 0; j < C; ++j) S[j] = y[j];
             if (i > 0) put_state(i - 1);
         }
         if (a.dstate_in && row < a.K) {

@@ -32,13 +32,11 @@ inline int parts_in(conv2d_operand_t t) { return t == CONV2D_OPERAND_BF16 ? 1 : 
 template <int N>
 __device__ __forceinline__ void split(float a, float b, uint32_t (&out)[N])
 {
+    float2 v = make_float2(a, b);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        out[i] = from_pair(make_float2(a, b), bf16());
-        if (i + 1 < N) {
-            const float2 f = to_pair(out[i], bf16());
-            a -= f.x, b -= f.y;
-        }
+        out[i] = from_pair(v, bf16());
+        if (i + 1 < N) v = __ffma2_rn(to_pair(out[i], bf16()), both(-1.f), v);
     }
 }
 

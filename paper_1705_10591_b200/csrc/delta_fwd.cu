@@ -119,13 +119,14 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
             if (is_key) {
                 float y[C];
                 Tile<T, NV>::get(values, token, col0, y);
+                add_scaled(y, -eg, X);
 #pragma unroll
-                for (int j = 0; j < C; ++j) X[j] = fmaf(-eg, X[j], y[j]), y[j] = beta * X[j];
+                for (int j = 0; j < C; ++j) X[j] = y[j];
+                scaled(y, beta, X);
                 put_row<NV, C>(rows, W::rows_part, row, col0, y);
                 ptx::fence_proxy_async_smem();
             } else {
-#pragma unroll
-                for (int j = 0; j < C; ++j) X[j] *= eg;
+                scaled(X, eg, X);
             }
             ptx::tc_fence_before_sync();
             __syncthreads();
@@ -134,12 +135,9 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
             ptx::tc_fence_after_sync();
             float y[C];
             tmem_digits<C>(at + 3 * NV, NV, y);
-#pragma unroll
-            for (int j = 0; j < C; ++j) X[j] += y[j];
+            add_scaled(X, 1.f, y);
             if (is_key) {
-                const float d = ed * beta;
-#pragma unroll
-                for (int j = 0; j < C; ++j) y[j] = d * X[j];
+                scaled(y, ed * beta, X);
                 put_row<NV, C>(rows, W::rows_part, row, col0, y);
                 ptx::fence_proxy_async_smem();
             }
@@ -148,16 +146,16 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
             if (is_key) {
                 if (a.updates) save_row<C>(a.updates + quad_at(unit0 + i, a.VP, kPiece, v, token), kPiece, saved, X);
             } else {
-#pragma unroll
-                for (int j = 0; j < C; ++j) X[j] *= a.scale;
+                scaled(X, a.scale, X);
                 Tile<T, NV>::put(outputs, token, col0, X);
             }
             // D3, in D1's place: S <- e^G_63 S + K^T (..)
             ptx::mbar_wait_bounded(&bars->done[2], parity, abort_flag, a.max_polls);
             ptx::tc_fence_after_sync();
             tmem_digits<C>(at, NV, y);
+            add_scaled(y, whole, S);
 #pragma unroll
-            for (int j = 0; j < C; ++j) S[j] = fmaf(whole, S[j], y[j]);
+            for (int j = 0; j < C; ++j) S[j] = y[j];
             if (i + 1 < pieces) put_state(i + 1);
         }
         if (a.state_out && row < a.K) {

@@ -24,7 +24,7 @@ struct Prepare {
 __device__ __forceinline__ uint32_t inverse_at(uint32_t base, int row, int unit) { return base + row * 32 + ((unit ^ ((row >> 2) & 1)) << 4); }
 
 template <typename T, int KD, bool WIDE>
-__global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a, bool squares)
+__global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a, bool squares, int heads)
 {
     using S = Prepare<T, KD>;
     constexpr int IN = S::IN, HALF = 2 * kPiece * 128;         // bytes of 64 numbers of all rows
@@ -32,7 +32,9 @@ __global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a
     __shared__ alignas(16) float high[kPiece], low[kPiece], betas[kPiece];
     ptx::grid_dep_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int piece = blockIdx.x % a.pieces, bk = blockIdx.x / a.pieces, hk = bk % a.Hk, b = bk / a.Hk;
+    // this block's heads: `heads` of those that share the key, from `first_head` on
+    const int groups = a.share / heads, key_unit = blockIdx.x / groups, first_head = blockIdx.x % groups * heads;
+    const int piece = key_unit % a.pieces, bk = key_unit / a.pieces, hk = bk % a.Hk, b = bk / a.Hk;
     const int live = sequence_length(a.lengths, b, a.L) - piece * kPiece;
     if (live <= 0) return;
     const uint32_t base = ptx::smem_u32(raw), inverse = base + S::at_inverse;
@@ -41,7 +43,7 @@ __global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a
     auto place = [&](int p, int row, int unit) { return unit_at<64>((p * (KD / 64) + (unit >> 3)) * HALF, row, unit & 7); };
 
     // keys and queries, as parts; all that a thread takes of one (of both, where elements are short) is under way together
-    unsigned char* tile = a.keys + (size_t)blockIdx.x * S::tile;
+    unsigned char* tile = a.keys + (size_t)key_unit * S::tile;
     constexpr int UNITS = KD / 8, EACH = kPiece * UNITS / S::THREADS, AT_ONCE = sizeof(T) == 2 ? 2 : 1;
 #pragma unroll
     for (int first = 0; first < 2; first += AT_ONCE) {
@@ -77,7 +79,7 @@ __global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a
 #pragma unroll
                 for (int p = 0; p < IN; ++p) {
                     const uint32_t at = place(p, (first + n) * kPiece + row, unit);
-                    *reinterpret_cast<uint4*>(tile + at) = v[p];
+                    if (first_head == 0) *reinterpret_cast<uint4*>(tile + at) = v[p];
                     if (squares) *reinterpret_cast<uint4*>(raw + at) = v[p];
                 }
             }
@@ -92,7 +94,7 @@ __global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a
             beta.x = token < live ? a.beta[(row0 + token) * a.ldbeta + h] : 0.f, beta.y = token + 1 < live ? a.beta[(row0 + token + 1) * a.ldbeta + h] : 0.f;
         }
     };
-    fetch(hk * a.share);
+    fetch(hk * a.share + first_head);
     __syncthreads();
 
     // rows 16 warp .. + 15 of K K^T and K Q^T, columns from there on
@@ -119,7 +121,7 @@ __global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a
     }
     __syncthreads();                                           // (their place is taken from here on)
 
-    for (int r = 0; r < a.share; ++r) {
+    for (int r = first_head; r < first_head + heads; ++r) {
         const int h = hk * a.share + r;
         const size_t unit = ((size_t)b * a.H + h) * a.pieces + piece;
         if (warp == 0) {
@@ -127,7 +129,7 @@ __global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a
             // (below -10000 taken as that: sums of infinities would have no differences; NaN stays)
             const double x[2] = {gate.x < -10000.f ? -10000.f : gate.x, gate.y < -10000.f ? -10000.f : gate.y};
             const float be[2] = {beta.x, beta.y};
-            if (r + 1 < a.share) fetch(h + 1);
+            if (r + 1 < first_head + heads) fetch(h + 1);
             const double sum = x[0] + x[1];
             double before = sum;
 #pragma unroll
@@ -296,8 +298,11 @@ conv2d_status_t prepare(const DeltaArgs& a, bool squares, cudaStream_t stream)
     using S = Prepare<T, KD>;
     static SmemLimit limit;
     if (raise_smem_limit((const void*)delta_prepare_kernel<T, KD, WIDE>, S::smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-    const long long blocks = (long long)a.B * a.Hk * a.pieces;
-    if (launch_pdl(delta_prepare_kernel<T, KD, WIDE>, dim3((unsigned)blocks), dim3(S::THREADS), S::smem, stream, a, squares) != cudaSuccess) return CONV2D_ERR_CUDA;
+    // one head a block while an SM has room for all at once: keys and queries are read and multiplied for each then, but heads do not wait for one another
+    const long long units = (long long)a.B * a.Hk * a.pieces;
+    const int heads = !squares || units * a.share > 3LL * sm_count() ? a.share : 1;
+    const long long blocks = units * (a.share / heads);
+    if (launch_pdl(delta_prepare_kernel<T, KD, WIDE>, dim3((unsigned)blocks), dim3(S::THREADS), S::smem, stream, a, squares, heads) != cudaSuccess) return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;
 }

@@ -4,7 +4,7 @@
 namespace conv2d_b200 {
 namespace {
 
-// Every state is read and written once, which is all the time there is.  A block of 128 threads has one head's rows of K for up to 32 * VW columns of V: all of
+// Every state is read and written once, which is all the time there is.  A block of 128 threads has one head's rows of K for up to 16 * VW columns of V: all of
 // a thread's numbers (row `group`, `group` + groups, ..., of VW adjacent columns) are under way together and stay in registers, and since
 //   o = scale (e^g S^T q + (k.q) u),
 // S^T k and S^T q are summed over rows at once: one barrier between reading and writing.
@@ -93,12 +93,12 @@ conv2d_status_t step(const DeltaArgs& a, int lanes, cudaStream_t stream)
 template <typename T, int VW>
 conv2d_status_t step_wide(const DeltaArgs& a, cudaStream_t stream)
 {
-    int lanes = 4;                                             // as many as a row of the state has, up to a warp
-    while (lanes < 32 && lanes * VW < a.V) lanes *= 2;
+    // as many as a row of the state has, up to 16: blocks of 64 columns hold 32 KB of a state of 128 x 128 in half the registers, and an SM has four of them where it
+    // had two (256 tokens of 32 such heads: 165 us, 6.6 TB/s; with 32 lanes 210, with 8 201)
+    int lanes = 4;
+    while (lanes < 16 && lanes * VW < a.V) lanes *= 2;
     const int rows = (a.K * lanes + 127) / 128;
-    if (rows <= 8) return step<T, VW, 8>(a, lanes, stream);
-    if (rows <= 16) return step<T, VW, 16>(a, lanes, stream);
-    return step<T, VW, 32>(a, lanes, stream);
+    return rows <= 8 ? step<T, VW, 8>(a, lanes, stream) : step<T, VW, 16>(a, lanes, stream);
 }
 
 template <typename T>

@@ -70,7 +70,29 @@ template <int N> __device__ __forceinline__ void tmem_digits(uint32_t at, uint32
         for (int p = 0; p < kSum; ++p) ptx::tmem_ld16(at + p * step + c, v[p]);
         ptx::tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) f[c + i] = (__uint_as_float(v[2][i]) + __uint_as_float(v[1][i])) + __uint_as_float(v[0][i]);
+        for (int i = 0; i < 16; i += 2) {
+            auto pair = [&](int p) { return make_float2(__uint_as_float(v[p][i]), __uint_as_float(v[p][i + 1])); };
+            const float2 sum = __fadd2_rn(__fadd2_rn(pair(2), pair(1)), pair(0));
+            f[c + i] = sum.x, f[c + i + 1] = sum.y;
+        }
+    }
+}
+
+// y <- a x + y, and x <- a x, two numbers at a time.
+template <int N> __device__ __forceinline__ void add_scaled(float (&y)[N], float a, const float (&x)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; j += 2) {
+        const float2 r = __ffma2_rn(both(a), make_float2(x[j], x[j + 1]), make_float2(y[j], y[j + 1]));
+        y[j] = r.x, y[j + 1] = r.y;
+    }
+}
+template <int N> __device__ __forceinline__ void scaled(float (&y)[N], float a, const float (&x)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; j += 2) {
+        const float2 r = __fmul2_rn(both(a), make_float2(x[j], x[j + 1]));
+        y[j] = r.x, y[j + 1] = r.y;
     }
 }
 
