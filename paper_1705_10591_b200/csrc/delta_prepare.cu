@@ -8,7 +8,7 @@ namespace {
 // owns rows j = 16 w .. + 15 of
 //   A^T_ji = e^(G_i - G_j) k_j.k_i (i > j),   P^T_ji = e^(G_i - G_j) k_j.q_i (i >= j),   t^T,   P'^T = P^T - t^T diag(beta) P^T,
 // so that every block of 16 x 16 that it has computed is the left operand of its next products straight from the accumulators.  t^T comes from
-// t^T (1 + diag(beta) A^T) = A^T from the left to the right: X_i = (A^T_ji - sum over k < i of X_k diag(beta) A^T_ki) (1 + diag(beta) A^T_ii)^-1, where the inverses
+// t^T (1 + diag(beta) A^T) = A^T from the left to the right: t^T_i = (A^T_ji - sum over k < i of t^T_k diag(beta) A^T_ki) (1 + diag(beta) A^T_ii)^-1, where the inverses
 // of the four diagonal blocks are found column by column, 16 steps of 16 lanes.  (Powers of A would do without those steps, but for keys that are alike they
 // grow to binomials, whose digits cancel.)  G is a scan over lanes in 64 bits: differences are taken of sums of decays that may be thousands, and a float would
 // leave them 2^-24 of those.  What bounds it is latency, 12 warps an SM: barriers and dependent steps.
@@ -208,59 +208,36 @@ __global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a
             }
         }
         __syncthreads();
-        // t^T: blocks of 16 columns from the diagonal on
+        // t^T and P'^T: a block of 16 columns of t^T is done when those before it have been taken off, and is taken off all behind it, of P^T too
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i < warp) continue;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (k >= i) break;
-                if (k < warp) continue;
-                float y[2][4];
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[n][e] = -betas[16 * k + 8 * n + c + (e & 1)] * X[2 * k + n][e];
-                uint32_t x[kSum][4];
-                left_of<kSum>(x, y[0], y[1]);
-#pragma unroll
-                for (int p = kSum - 1; p >= 0; --p) {
-                    uint32_t q[4];
-                    right_kn<64>(q, base + p * S::part, 16 * k, 16 * i, lane);
-                    mma_parts<kSum>(X[2 * i], X[2 * i + 1], x, q, p);
-                }
-            }
+        for (int k = 0; k < 4; ++k) {
+            if (k < warp) continue;
             uint32_t x[kSum][4];
             float out[2][4] = {};
-            left_of<kSum>(x, X[2 * i], X[2 * i + 1]);
+            left_of<kSum>(x, X[2 * k], X[2 * k + 1]);
 #pragma unroll
             for (int p = kSum - 1; p >= 0; --p) {
                 uint32_t q[4];
-                ldsm(q, inverse_at(inverse + p * S::inverse, 16 * i + ((lane >> 4) << 3) + (lane & 7), (lane >> 3) & 1));
+                ldsm(q, inverse_at(inverse + p * S::inverse, 16 * k + ((lane >> 4) << 3) + (lane & 7), (lane >> 3) & 1));
                 mma_parts<kSum>(out[0], out[1], x, q, p);
             }
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)                    // (below the diagonal is nothing but what rounding leaves there)
-                    X[2 * i + n][e] = i > warp || 8 * n + c + (e & 1) > g + 8 * (e >> 1) ? out[n][e] : 0.f;
-        }
-        // P'^T = P^T + (-t^T diag(beta)) P^T
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (k < warp) continue;
-            float y[2][4];
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[n][e] = -betas[16 * k + 8 * n + c + (e & 1)] * X[2 * k + n][e];
-            uint32_t x[kSum][4];
-            left_of<kSum>(x, y[0], y[1]);
+                for (int e = 0; e < 4; ++e) {                  // (below the diagonal is nothing but what rounding leaves there)
+                    X[2 * k + n][e] = k > warp || 8 * n + c + (e & 1) > g + 8 * (e >> 1) ? out[n][e] : 0.f;
+                    out[n][e] = -betas[16 * k + 8 * n + c + (e & 1)] * X[2 * k + n][e];
+                }
+            left_of<kSum>(x, out[0], out[1]);
 #pragma unroll
             for (int i = k; i < 4; ++i) {
 #pragma unroll
                 for (int p = kSum - 1; p >= 0; --p) {
                     uint32_t q[4];
+                    if (i > k) {
+                        right_kn<64>(q, base + p * S::part, 16 * k, 16 * i, lane);
+                        mma_parts<kSum>(X[2 * i], X[2 * i + 1], x, q, p);
+                    }
                     right_kn<64>(q, base + (kSum + p) * S::part, 16 * k, 16 * i, lane);
                     mma_parts<kSum>(P[2 * i], P[2 * i + 1], x, q, p);
                 }
