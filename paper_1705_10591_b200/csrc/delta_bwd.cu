@@ -611,7 +611,7 @@ conv2d_status_t backward_wide(const DeltaArgs& a, cudaStream_t stream)
                       rows_aligned(a.dq, a.lddq, sizeof(T), 16) && rows_aligned(a.dk, a.lddk, sizeof(T), 16);
     conv2d_status_t st = CONV2D_ERR_UNSUPPORTED;
     if constexpr (sizeof(T) == 2 || KD == 64) {
-        if (delta_columns<T>(a, wide_v) == 64) st = backward_walk<T, KD, 64, true>(a, stream);
+        if (delta_columns<T, KD, 2 * kPiece>(a, wide_v) == 64) st = backward_walk<T, KD, 64, true>(a, stream);
     }
     if (st == CONV2D_ERR_UNSUPPORTED) st = wide_v ? backward_walk<T, KD, 32, true>(a, stream) : backward_walk<T, KD, 32, false>(a, stream);
     if (st != CONV2D_OK) return st;

@@ -133,13 +133,13 @@ __device__ __forceinline__ void left_of(uint32_t (&a)[N][4], const float (&c0)[4
     for (int i = 0; i < N; ++i) a[i][3] = p[i];
 }
 
-// c0, c1 += the products of N parts of a left operand with part j of a right one, but for those that lie below the last part.
+// c0, c1 += the products of N parts of a left operand with part j of a right one, but for those that lie below the last part of a sum.
 template <int N>
 __device__ __forceinline__ void mma_parts(float (&c0)[4], float (&c1)[4], const uint32_t (&a)[N][4], const uint32_t (&b)[4], int j)
 {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        if (i + j < N) {
+        if (i + j < kSum) {
             mma(c0, a[i], b[0], b[1]);
             mma(c1, a[i], b[2], b[3]);
         }

@@ -197,7 +197,7 @@ conv2d_status_t walk_wide(const DeltaArgs& a, cudaStream_t stream)
 {
     const bool wide = a.V % (16 / sizeof(T)) == 0 && rows_aligned(a.v, a.ldv, sizeof(T), 16) && rows_aligned(a.o, a.ldo, sizeof(T), 16);
     if constexpr (sizeof(T) == 2 || KD == 64) {
-        if (delta_columns<T>(a, wide) == 64) return walk<T, KD, 64, true>(a, stream);
+        if (delta_columns<T, KD, kPiece>(a, wide) == 64) return walk<T, KD, 64, true>(a, stream);
     }
     return wide ? walk<T, KD, 32, true>(a, stream) : walk<T, KD, 32, false>(a, stream);
 }

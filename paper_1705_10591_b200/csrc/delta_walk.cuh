@@ -301,16 +301,18 @@ __device__ __forceinline__ void multiply(uint32_t d, int a_parts, int b_parts, i
     }
 }
 
-// Columns a block walks with: 32, or 64 where those are fewer rounds of the machine's SMs (a piece takes about half as long again then).  Keys of 128 fp32 numbers, in
-// three parts, leave room for 32, and rows that rule out accesses of 16 bytes are walked with 32.
-template <typename T>
+// Columns a block walks with: 32, or 64 where those are fewer rounds of the machine's SMs.  A piece takes 2.3 us with 32 columns and 3.4 with 64; where the keys of two
+// pieces do not fit beside 64 (fp16, in two parts) and are waited for, 4.5, so that two rounds of 32 are no slower.  Keys of 128 fp32 numbers, in three parts,
+// leave room for 32, and rows that rule out accesses of 16 bytes are walked with 32.
+template <typename T, int KD, int ROWS>
 int delta_columns(const DeltaArgs& a, bool wide)
 {
     if (!wide || a.V <= 32 || (sizeof(T) == 4 && a.K > 64)) return 32;
     const long long heads = (long long)a.B * a.H, sms = sm_count();
     const long long by32 = (heads * ceil_div_u(a.V, 32) + sms - 1) / sms, by64 = (heads * ceil_div_u(a.V, 64) + sms - 1) / sms;
-    const int dflt = 3 * by64 <= 2 * by32 ? 64 : 32;
-    return env_int("CONV2D_B200_DELTA_COLUMNS", dflt) == 64 ? 64 : 32;
+    bool two = false;
+    if constexpr (sizeof(T) == 2 || KD == 64) two = Walk<T, KD, 64, ROWS>::stages == 2;
+    return env_int("CONV2D_B200_DELTA_COLUMNS", (two ? 3 * by64 <= 2 * by32 : 2 * by64 < by32) ? 64 : 32) == 64 ? 64 : 32;
 }
 
 }  // namespace conv2d_b200

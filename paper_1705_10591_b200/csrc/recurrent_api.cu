@@ -161,14 +161,14 @@ conv2d_status_t norm_fwd_rms(const void* x, const void* residual, const void* z,
     if (st != CONV2D_OK) return st;
     if (!rows_ok(x, ldx, C) || !rows_ok(residual, ldr, C) || !rows_ok(z, ldz, C) || !rows_ok(y, ldy, C) || !rows_ok(h, ldh, C) || !rows_ok(y8, ld8, C))
         return CONV2D_ERR_SHAPE;
-    if ((y8 && (block <= 0 || block > C)) || !(eps >= 0.f) || isinf(eps)) return CONV2D_ERR_SHAPE;
+    if ((y8 && block <= 0) || !(eps >= 0.f) || isinf(eps)) return CONV2D_ERR_SHAPE;
     if (!known(type)) return CONV2D_ERR_UNSUPPORTED;
     if (!all_aligned(element_size(type), x, residual, z, y, h) || !all_aligned(4, gamma, scales, rstd)) return CONV2D_ERR_ALIGN;
     st = check_device();
     if (st != CONV2D_OK) return st;
     RmsArgs a{};
     a.x = x, a.residual = residual, a.z = z, a.gamma = gamma, a.y = y, a.h = h, a.y8 = y8, a.scales = scales, a.rstd = rstd;
-    a.M = M, a.C = C, a.G = G, a.block = block, a.ldx = ldx, a.ldr = ldr, a.ldz = ldz, a.ldy = ldy, a.ldh = ldh, a.ld8 = ld8, a.eps = eps;
+    a.M = M, a.C = C, a.G = G, a.block = block < C ? block : C, a.ldx = ldx, a.ldr = ldr, a.ldz = ldz, a.ldy = ldy, a.ldh = ldh, a.ld8 = ld8, a.eps = eps;
     return launch_rms_fwd(a, type, static_cast<cudaStream_t>(cuda_stream));
 }
 

@@ -336,12 +336,14 @@ def test_rms_norm(lib, case):  # noqa: F811
 
 @pytest.mark.parametrize("type, M, C, G, block, pad, gate", [("bf16", 5, 4096, 1, 128, 0, False), ("bf16", 7, 4096, 1, 4096, 0, False), ("fp16", 3, 1000, 1, 128, 8, True),
                                                              ("fp16", 4, 288, 6, 128, 0, False), ("bf16", 2, 77, 7, 10, 1, False), ("fp32", 3, 96, 3, 7, 0, True),
-                                                             ("fp32", 2, 260, 1, 64, 0, False), ("bf16", 9, 24, 3, 1, 0, False), ("bf16", 300, 64, 1, 64, 0, True)])
+                                                             ("fp32", 2, 260, 1, 64, 0, False), ("bf16", 9, 24, 3, 1, 0, False), ("bf16", 300, 64, 1, 64, 0, True),
+                                                             ("bf16", 4, 72, 1, 128, 0, False), ("fp16", 2, 45, 3, 1 << 30, 2, True)])
 def test_output_in_8_bits(lib, type, M, C, G, block, pad, gate):  # noqa: F811
     t = TYPES[type]
     x, z = draw(910, M, C, dtype=t), draw(911, M, C, dtype=t)
     x[0], gamma = 0, draw(912, C // G, shift=1.0).float().to(F)
     xr, zr, y8, n = Rows((M, C), t, pad, 0, x), Rows((M, C), t, pad, 0, z), torch.full((M, C + pad + 3), 9, dtype=torch.uint8, device="cuda"), -(-C // block)
+    wide = min(block, C)
     gr, scales, yr = cuda(gamma), Rows((M, n), torch.float32), Rows((M, C), t)
     for y in (0, yr.ptr):                                      # with and without an output of the type
         lib.norm_fwd_rms(xr.ptr, 0, zr.ptr if gate else 0, gr.data_ptr(), y, 0, y8.data_ptr(), scales.ptr, 0, M, C, G, block, xr.ld, 0, zr.ld, C, 0, C + pad + 3,
@@ -349,12 +351,12 @@ def test_output_in_8_bits(lib, type, M, C, G, block, pad, gate):  # noqa: F811
     (want, size), _ = ref.rms_fwd(x, z if gate else None, gamma, G, 1e-5)
     check(yr.result(), want, size, 50, "y")
     assert (y8[:, C:] == 9).all()
-    blocks = torch.nn.functional.pad(want, (0, n * block - C)).reshape(M, n, block)
+    blocks = torch.nn.functional.pad(want, (0, n * wide - C)).reshape(M, n, wide)
     s = (blocks.abs().amax(-1) / 448).clamp(min=2.0 ** -126)
-    grow = torch.nn.functional.pad(size, (0, n * block - C)).reshape(M, n, block).amax(-1) / 448
+    grow = torch.nn.functional.pad(size, (0, n * wide - C)).reshape(M, n, wide).amax(-1) / 448
     check(scales.result(), s, torch.maximum(grow, s), 52, "scales")
-    values = y8[:, :C].view(torch.float8_e4m3fn).double().cpu() * scales.result().double().cpu().repeat_interleave(block, 1)[:, :C]
-    spread = s.repeat_interleave(block, 1)[:, :C]
+    values = y8[:, :C].view(torch.float8_e4m3fn).double().cpu() * scales.result().double().cpu().repeat_interleave(wide, 1)[:, :C]
+    spread = s.repeat_interleave(wide, 1)[:, :C]
     # half a step: 2^-4 of the value, 2^-10 of a scale below the smallest normal code; 60 roundings before
     assert ((values - want).abs() <= 2.0 ** -4 * want.abs() * (1 + 2.0 ** -17) + 2.0 ** -10 * spread + 60 * 2.0 ** -24 * (size + 448 * spread)).all()
     assert (values[0] == 0).all() and (scales.result()[0] == 2.0 ** -126).all()

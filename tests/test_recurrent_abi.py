@@ -67,7 +67,7 @@ def test_rms_refusals(lib):  # noqa: F811
     refused(lib, lib.norm_fwd_rms, fwd, own(shapes, fwd) + [
         (dict(x_ptr=0), NULL), (dict(y_ptr=0, y8_ptr=0, scales_ptr=0), NULL), (dict(y8_ptr=0), NULL), (dict(scales_ptr=0), NULL), (dict(h_ptr=0), NULL),
         (dict(residual_ptr=0), NULL), (dict(ldx=7), SHAPE), (dict(ldr=7), SHAPE), (dict(ldy=7), SHAPE), (dict(ld8=7), SHAPE), (dict(block=0), SHAPE),
-        (dict(block=9), SHAPE), (dict(eps=-1e-9), SHAPE), (dict(eps=float("nan")), SHAPE), (dict(eps=float("inf")), SHAPE), (dict(scales_ptr=OK + 2), ALIGN)])
+        (dict(block=-1), SHAPE), (dict(eps=-1e-9), SHAPE), (dict(eps=float("nan")), SHAPE), (dict(eps=float("inf")), SHAPE), (dict(scales_ptr=OK + 2), ALIGN)])
     need = lib.norm_bwd_rms_workspace_size(3, 8, 2)
     assert need > 0
     bwd = dict(h_ptr=OK, z_ptr=OK, gamma_ptr=OK, rstd_ptr=OK, dy_ptr=OK, dh_ptr=OK, dx_ptr=OK, dz_ptr=OK, dgamma_ptr=OK, M=3, C=8, G=2, ldh=8, ldz=8, lddy=8,
