@@ -6,25 +6,32 @@
 namespace conv2d_b200 {
 namespace {
 
-// A row lies in the registers of blockDim.x threads (whole warps), NP packs of V elements each, pack threadIdx.x + j * blockDim.x; blockDim.y rows a block.
+// A row lies in the registers of blockDim.x threads (whole warps), NP packs of V elements each, in places threadIdx.x + j * blockDim.x; blockDim.y rows a block.
 // What is summed over (a group), or shares a scale (a block of columns), is a run of packs:
 enum { kRow = 0, kLanes = 1, kShared = 2 };
 struct Runs {
-    int packs, count, how;        // packs of a run, runs of a row; over the row's threads, over 2^n adjacent lanes, or through shared memory
+    int packs, count, how, lanes; // packs of a run, runs of a row; over the row's threads, over `lanes` = 2^n adjacent lanes, or through shared memory
 };
+// The pack in place u, `packs` if there is none: groups of up to 32 packs are spread to 2^n lanes each, so that none lies in two warps.
+__device__ __forceinline__ int pack_of_place(int u, const Runs& groups, int packs)
+{
+    if (groups.lanes == groups.packs) return u < packs ? u : packs;
+    const int run = u / groups.lanes, at = u % groups.lanes;
+    return at < groups.packs && run < groups.count ? run * groups.packs + at : packs;
+}
 
 struct Sum { static __device__ float of(float a, float b) { return a + b; } };
 struct Max { static __device__ float of(float a, float b) { return fmaxf(a, b); } };
 
-// p[j], a value of each of this thread's packs, becomes that of the pack's run.  All threads of the block come here.
+// p[j], a value of each of this thread's packs (at[j], zero where there is none), becomes that of the pack's run.  All threads of the block come here.
 template <typename Op, int NP>
-__device__ __forceinline__ void reduce_runs(float (&p)[NP], const Runs& r, int packs, float* shared)
+__device__ __forceinline__ void reduce_runs(float (&p)[NP], const int (&at)[NP], const Runs& r, int packs, float* shared)
 {
     const int tx = threadIdx.x, lane = tx & 31, warp = tx >> 5, warps = blockDim.x >> 5;
     if (r.how == kLanes) {
 #pragma unroll
         for (int j = 0; j < NP; ++j)
-            for (int d = 1; d < r.packs; d *= 2) p[j] = Op::of(p[j], __shfl_xor_sync(0xffffffffu, p[j], d));
+            for (int d = 1; d < r.lanes; d *= 2) p[j] = Op::of(p[j], __shfl_xor_sync(0xffffffffu, p[j], d));
     } else if (r.how == kRow) {
         float s = p[0];
 #pragma unroll
@@ -46,7 +53,7 @@ __device__ __forceinline__ void reduce_runs(float (&p)[NP], const Runs& r, int p
         float *mine = shared + threadIdx.y * (packs + r.count), *runs = mine + packs;
 #pragma unroll
         for (int j = 0; j < NP; ++j)
-            if (tx + j * (int)blockDim.x < packs) mine[tx + j * blockDim.x] = p[j];
+            if (at[j] < packs) mine[at[j]] = p[j];
         __syncthreads();
         for (int i = warp; i < r.count; i += warps) {
             const int end = min((i + 1) * r.packs, packs);
@@ -59,7 +66,7 @@ __device__ __forceinline__ void reduce_runs(float (&p)[NP], const Runs& r, int p
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < NP; ++j)
-            if (tx + j * (int)blockDim.x < packs) p[j] = runs[(tx + j * blockDim.x) / r.packs];
+            if (at[j] < packs) p[j] = runs[at[j] / r.packs];
         __syncthreads();
     }
 }
@@ -99,13 +106,14 @@ __device__ __forceinline__ void store_codes(unsigned char* to, const float (&f)[
     store_pack<unsigned char, V>(to, p);
 }
 
-// (blocks of rows in packs have 512 threads at most, single elements 1024)
-template <int V> constexpr int kMostThreads = V > 1 ? 512 : 1024;
+constexpr int kMostThreads = 512;                              // of a block: 128 registers each
+// Places of a thread at most, for packs of V elements: 16384 elements in 512 threads.
+constexpr int most_places(int v) { return v > 2 ? 8 : v > 1 ? 16 : 32; }
 
 // Every row has its block, and an SM four of 256 threads at once: walks over rows with the next row's numbers under way, as the backward pass takes them, need the
 // registers of half of those (8192 x 4096 to 8 bits 74 us so, 53 without).
 template <typename T, int V, int NP>
-__global__ void __launch_bounds__(kMostThreads<V>, V > 1 && NP <= 2 ? 2 : 1) rms_fwd_kernel(const RmsArgs a, Runs groups, Runs blocks, int packs, int channels)
+__global__ void __launch_bounds__(kMostThreads, V > 2 && NP <= 2 ? 2 : 1) rms_fwd_kernel(const RmsArgs a, Runs groups, Runs blocks, int packs, int channels)
 {
     extern __shared__ float shared[];
     ptx::grid_dep_wait();
@@ -115,9 +123,10 @@ __global__ void __launch_bounds__(kMostThreads<V>, V > 1 && NP <= 2 ? 2 : 1) rms
     const float inverse = 1.f / channels;
     float f[NP][V], s[NP];
     Pack<T, V> px[NP], pr[NP], pz[NP];
+    int at[NP];
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-        const int p = threadIdx.x + j * blockDim.x;
+        const int p = at[j] = pack_of_place(threadIdx.x + j * blockDim.x, groups, packs);
         const bool there = real && p < packs;
         px[j] = load_masked<T, V>(x + p * V, there);
         if (a.residual) pr[j] = load_masked<T, V>(res + p * V, there);
@@ -125,7 +134,7 @@ __global__ void __launch_bounds__(kMostThreads<V>, V > 1 && NP <= 2 ? 2 : 1) rms
     }
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-        const int p = threadIdx.x + j * blockDim.x;
+        const int p = at[j];
         unpack<T, V>(px[j], f[j]);
         if (a.residual) {                                      // the sum as it is stored is what is normalised, so that the backward pass sees the same
             float r[V];
@@ -141,11 +150,11 @@ __global__ void __launch_bounds__(kMostThreads<V>, V > 1 && NP <= 2 ? 2 : 1) rms
         for (int e = 0; e < V; ++e) s[j] = fmaf(f[j][e], f[j][e], s[j]);
         s[j] *= inverse;                                       // (a mean does not overflow where its terms do not, a sum of thousands would)
     }
-    reduce_runs<Sum>(s, groups, packs, shared);
+    reduce_runs<Sum>(s, at, groups, packs, shared);
     float most[NP];
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-        const int p = threadIdx.x + j * blockDim.x;
+        const int p = at[j];
         const float r = rsqrtf(s[j] + a.eps);
         const bool there = real && p < packs;
         const int group = a.G > 1 ? p / groups.packs : 0;
@@ -167,10 +176,10 @@ __global__ void __launch_bounds__(kMostThreads<V>, V > 1 && NP <= 2 ? 2 : 1) rms
         for (int e = 0; e < V; ++e) most[j] = fmaxf(most[j], fabsf(f[j][e]));
     }
     if (!a.y8) return;
-    reduce_runs<Max>(most, blocks, packs, shared);
+    reduce_runs<Max>(most, at, blocks, packs, shared);
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-        const int p = threadIdx.x + j * blockDim.x;
+        const int p = at[j];
         if (!real || p >= packs) continue;
         const float scale = fmaxf(most[j] * (1.f / 448.f), 1.17549435e-38f), up = 1.f / scale;
         const int block = blocks.count > 1 ? p / blocks.packs : 0;
@@ -184,19 +193,19 @@ __global__ void __launch_bounds__(kMostThreads<V>, V > 1 && NP <= 2 ? 2 : 1) rms
 // Backward: with n = dy gamma silu(z) and m = h r,   dx = r (n - m mean(n m)) + dh.  A block takes rows gridDim.x * blockDim.y apart, the next one's numbers under way
 // while it computes, and keeps its sums for gamma in registers until the end, when they are added over its rows and groups.
 template <typename T, int V, int NP>
-__global__ void __launch_bounds__(kMostThreads<V>, 1) rms_bwd_kernel(const RmsArgs a, Runs groups, int packs, int channels)
+__global__ void __launch_bounds__(kMostThreads, 1) rms_bwd_kernel(const RmsArgs a, Runs groups, int packs, int channels)
 {
     extern __shared__ float shared[];
     ptx::grid_dep_wait();
     const float inverse = 1.f / channels;
     float w[NP][V], dw[NP][V], r[NP];
-    int group[NP];
+    int group[NP], at[NP];
     Pack<T, V> ph[NP], py[NP], pd[NP], pz[NP];
     const long long step = (long long)gridDim.x * blockDim.y;
     auto fetch = [&](long long row) {
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
-            const int p = threadIdx.x + j * blockDim.x;
+            const int p = at[j];
             const bool there = row < a.M && p < packs;
             ph[j] = load_masked<T, V>(static_cast<const T*>(a.x) + row * a.ldx + p * V, there);
             py[j] = load_masked<T, V>(static_cast<const T*>(a.dy) + row * a.lddy + p * V, there);
@@ -207,7 +216,7 @@ __global__ void __launch_bounds__(kMostThreads<V>, 1) rms_bwd_kernel(const RmsAr
     };
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-        const int p = threadIdx.x + j * blockDim.x;
+        const int p = at[j] = pack_of_place(threadIdx.x + j * blockDim.x, groups, packs);
         group[j] = a.G > 1 ? p / groups.packs : 0;
         if (p < packs) load_gamma<V>(a.gamma, (p - group[j] * groups.packs) * V, w[j]);
 #pragma unroll
@@ -220,7 +229,7 @@ __global__ void __launch_bounds__(kMostThreads<V>, 1) rms_bwd_kernel(const RmsAr
         float m[NP][V], n[NP][V], d[NP][V], s[NP], rr[NP];
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
-            const int p = threadIdx.x + j * blockDim.x;
+            const int p = at[j];
             unpack<T, V>(ph[j], m[j]);
             unpack<T, V>(py[j], n[j]);
             if (a.dh) unpack<T, V>(pd[j], d[j]);
@@ -247,10 +256,10 @@ __global__ void __launch_bounds__(kMostThreads<V>, 1) rms_bwd_kernel(const RmsAr
             }
         }
         fetch(row + step);
-        reduce_runs<Sum>(s, groups, packs, shared);
+        reduce_runs<Sum>(s, at, groups, packs, shared);
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
-            const int p = threadIdx.x + j * blockDim.x;
+            const int p = at[j];
             const float mean = s[j] * inverse;
 #pragma unroll
             for (int e = 0; e < V; ++e) n[j][e] = rr[j] * fmaf(-m[j][e], mean, n[j][e]);
@@ -266,7 +275,7 @@ __global__ void __launch_bounds__(kMostThreads<V>, 1) rms_bwd_kernel(const RmsAr
     float* mine = shared + threadIdx.y * a.C;
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-        const int p = threadIdx.x + j * blockDim.x;
+        const int p = at[j];
         if (p >= packs) continue;
 #pragma unroll
         for (int e = 0; e < V; ++e) mine[p * V + e] = dw[j][e];
@@ -298,33 +307,50 @@ __global__ void __launch_bounds__(1024) rms_gamma_kernel(const float* __restrict
     if (threadIdx.x == 0 && blockIdx.x * 32 + threadIdx.y < channels) out[blockIdx.x * 32 + threadIdx.y] = s;
 }
 
-// How a row's packs are spread: at least two a thread (four single elements), up to 512 threads (1024); small rows share a block of about 256.
+// How a row's packs are spread: at least two a thread (four of one or two elements), up to 512 threads; small rows share a block of about 256.
 struct RowPlan {
     int v, packs, threads, rows, np;
-    RowPlan(int C, int v_) : v(v_), packs(C / v_)
+    Runs groups;
+    RowPlan(int C, int G, int v_) : v(v_), packs(C / v_)
     {
-        const int each = v > 1 ? 2 : 4;
-        threads = (packs + each - 1) / each;
-        const int most = v > 1 ? 512 : 1024;
-        threads = threads > most ? most : (threads + 31) / 32 * 32;
-        np = (packs + threads - 1) / threads;
+        groups = Runs{packs / G, G, kShared, packs / G};
+        if (G == 1) groups.how = kRow;
+        else if (groups.packs <= 32) {
+            groups.how = kLanes;
+            for (groups.lanes = 1; groups.lanes < groups.packs;) groups.lanes *= 2;
+        }
+        spread();
+        if (np > most_places(v)) {                             // (the largest rows have no room for places without a pack)
+            groups.how = kShared, groups.lanes = groups.packs;
+            spread();
+        }
+    }
+    void spread()
+    {
+        const int places = groups.lanes * groups.count, each = v > 2 ? 2 : 4;
+        threads = (places + each - 1) / each;
+        threads = threads > kMostThreads ? kMostThreads : (threads + 31) / 32 * 32;
+        np = (places + threads - 1) / threads;
         rows = threads >= 256 ? 1 : 256 / threads;
     }
+    // runs that share a scale
+    Runs blocks(int elements) const
+    {
+        const int n = elements / v;
+        Runs r{n, (packs + n - 1) / n, kShared, n};
+        if (r.count == 1) r.how = kRow;
+        else if (n == groups.packs && groups.how == kLanes) return groups;
+        else if (groups.lanes == groups.packs && n <= 32 && (n & (n - 1)) == 0) r.how = kLanes;
+        return r;
+    }
 };
-Runs runs_of(int elements, const RowPlan& p)
-{
-    Runs r{elements / p.v, (p.packs + elements / p.v - 1) / (elements / p.v), kShared};
-    if (r.count == 1) r.how = kRow;
-    else if (r.packs <= 32 && (r.packs & (r.packs - 1)) == 0) r.how = kLanes;
-    return r;
-}
 size_t shared_bytes(const RowPlan& p, const Runs& r) { return r.how == kShared ? (size_t)p.rows * (p.packs + r.count) * 4 : r.how == kRow ? p.rows * 32 * 4 : 0; }
 
 template <typename T, int V, int NP>
 conv2d_status_t forward(const RmsArgs& a, const RowPlan& p, cudaStream_t stream)
 {
     static SmemLimit limit;
-    const Runs groups = runs_of(a.C / a.G, p), blocks = runs_of(a.y8 ? a.block : a.C, p);
+    const Runs groups = p.groups, blocks = p.blocks(a.y8 ? a.block : a.C);
     const size_t one = shared_bytes(p, groups), two = shared_bytes(p, blocks), smem = one > two ? one : two;
     if (raise_smem_limit((const void*)rms_fwd_kernel<T, V, NP>, smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
     if (launch_pdl(rms_fwd_kernel<T, V, NP>, dim3(ceil_div_u(a.M, p.rows)), dim3(p.threads, p.rows), smem, stream, a, groups, blocks, p.packs, a.C / a.G) !=
@@ -345,7 +371,7 @@ template <typename T, int V, int NP>
 conv2d_status_t backward(const RmsArgs& a, const RowPlan& p, cudaStream_t stream)
 {
     static SmemLimit limit;
-    const Runs groups = runs_of(a.C / a.G, p);
+    const Runs groups = p.groups;
     const size_t runs = shared_bytes(p, groups), sums = a.dgamma ? (size_t)p.rows * a.C * 4 : 0, smem = runs > sums ? runs : sums;
     if (raise_smem_limit((const void*)rms_bwd_kernel<T, V, NP>, smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
     const int blocks = bwd_blocks(a.M, p.rows), channels = a.C / a.G;
@@ -357,37 +383,48 @@ conv2d_status_t backward(const RmsArgs& a, const RowPlan& p, cudaStream_t stream
     return CONV2D_OK;
 }
 
-// Whether rows can be moved in packs of 16 bytes of which none lies in two groups or two blocks of a scale.
+// Whether rows can be moved in packs of V elements of which none lies in two groups or two blocks of a scale.
 template <typename T>
 bool packs_fit(const RmsArgs& a, int V)
 {
-    const int e = sizeof(T);
-    return (a.C / a.G) % V == 0 && (!a.y8 || (a.block % V == 0 && rows_aligned(a.y8, a.ld8, 1, V))) && rows_aligned(a.x, a.ldx, e, 16) && rows_aligned(a.residual, a.ldr, e, 16) &&
-           rows_aligned(a.z, a.ldz, e, 16) && rows_aligned(a.y, a.ldy, e, 16) && rows_aligned(a.h, a.ldh, e, 16) && rows_aligned(a.dy, a.lddy, e, 16) &&
-           rows_aligned(a.dh, a.lddh, e, 16) && rows_aligned(a.dx, a.lddx, e, 16) && rows_aligned(a.dz, a.lddz, e, 16);
+    const int e = sizeof(T), n = V * e;
+    return (a.C / a.G) % V == 0 && (!a.y8 || (a.block % V == 0 && rows_aligned(a.y8, a.ld8, 1, V))) && rows_aligned(a.x, a.ldx, e, n) && rows_aligned(a.residual, a.ldr, e, n) &&
+           rows_aligned(a.z, a.ldz, e, n) && rows_aligned(a.y, a.ldy, e, n) && rows_aligned(a.h, a.ldh, e, n) && rows_aligned(a.dy, a.lddy, e, n) &&
+           rows_aligned(a.dh, a.lddh, e, n) && rows_aligned(a.dx, a.lddx, e, n) && rows_aligned(a.dz, a.lddz, e, n);
 }
 
-template <typename T>
-conv2d_status_t rms_typed(const RmsArgs& a, bool bwd, cudaStream_t stream)
+template <typename T, int V, int NP>
+conv2d_status_t either(const RmsArgs& a, const RowPlan& p, bool bwd, cudaStream_t stream)
 {
-    constexpr int V = 16 / (int)sizeof(T);
-    if (packs_fit<T>(a, V)) {
-        const RowPlan p(a.C, V);
-        if (p.np == 1) return bwd ? backward<T, V, 1>(a, p, stream) : forward<T, V, 1>(a, p, stream);
-        if (p.np == 2) return bwd ? backward<T, V, 2>(a, p, stream) : forward<T, V, 2>(a, p, stream);
-        if (V == 8 || p.np <= 4) return bwd ? backward<T, V, 4>(a, p, stream) : forward<T, V, 4>(a, p, stream);
-        return bwd ? backward<T, V, 4 * 8 / V>(a, p, stream) : forward<T, V, 4 * 8 / V>(a, p, stream);
+    return bwd ? backward<T, V, NP>(a, p, stream) : forward<T, V, NP>(a, p, stream);
+}
+// Packs of V elements, or the next smaller that fit.
+template <typename T, int V>
+conv2d_status_t rms_packed(const RmsArgs& a, bool bwd, cudaStream_t stream)
+{
+    if constexpr (V > 2) {
+        if (packs_fit<T>(a, V)) {
+            const RowPlan p(a.C, a.G, V);
+            if (p.np == 1) return either<T, V, 1>(a, p, bwd, stream);
+            if (p.np == 2) return either<T, V, 2>(a, p, bwd, stream);
+            return p.np <= 4 ? either<T, V, 4>(a, p, bwd, stream) : either<T, V, 8>(a, p, bwd, stream);
+        }
+        return rms_packed<T, V / 2>(a, bwd, stream);
+    } else {
+        if (V == 2 && !packs_fit<T>(a, V)) return rms_packed<T, 1>(a, bwd, stream);
+        const RowPlan p(a.C, a.G, V);
+        if (p.np <= 4) return either<T, V, 4>(a, p, bwd, stream);
+        if (p.np <= 8) return either<T, V, 8>(a, p, bwd, stream);
+        if (V == 2 || p.np <= 16) return either<T, V, 16>(a, p, bwd, stream);
+        return either<T, 1, 32>(a, p, bwd, stream);
     }
-    const RowPlan p(a.C, 1);
-    if (p.np <= 4) return bwd ? backward<T, 1, 4>(a, p, stream) : forward<T, 1, 4>(a, p, stream);
-    return bwd ? backward<T, 1, 16>(a, p, stream) : forward<T, 1, 16>(a, p, stream);
 }
 
 conv2d_status_t rms(const RmsArgs& a, conv2d_operand_t type, bool bwd, cudaStream_t stream)
 {
-    if (type == CONV2D_OPERAND_BF16) return rms_typed<bf16>(a, bwd, stream);
-    if (type == CONV2D_OPERAND_FP16) return rms_typed<fp16>(a, bwd, stream);
-    return rms_typed<float>(a, bwd, stream);
+    if (type == CONV2D_OPERAND_BF16) return rms_packed<bf16, 8>(a, bwd, stream);
+    if (type == CONV2D_OPERAND_FP16) return rms_packed<fp16, 8>(a, bwd, stream);
+    return rms_packed<float, 4>(a, bwd, stream);
 }
 
 }  // namespace

@@ -287,6 +287,13 @@ RMS = [  # type, M, C, G, residual, gate, pad, offset
     ("bf16", 700, 40, 5, True, False, 0, 0),
     ("fp32", 3, 6, 6, True, True, 2, 2),
     ("fp16", 2, 11000, 1, True, False, 0, 0),
+    ("bf16", 21, 1792, 32, True, True, 0, 0),
+    ("bf16", 5, 1084, 1, True, False, 0, 0),
+    ("fp16", 6, 1162, 7, False, True, 0, 0),
+    ("fp32", 3, 16383, 129, True, True, 1, 1),
+    ("fp16", 2, 16320, 60, True, True, 0, 4),
+    ("bf16", 2, 16383, 1, True, False, 0, 1),
+    ("fp32", 9, 90, 5, True, True, 0, 2),
 ]
 
 
