@@ -6,6 +6,8 @@
 namespace conv2d_b200 {
 namespace {
 
+constexpr int kMostThreads = 512, kMostWarps = kMostThreads / 32;  // of a row, and of a block: 128 registers each
+
 // A row lies in the registers of blockDim.x threads (whole warps), NP packs of V elements each, in places threadIdx.x + j * blockDim.x; blockDim.y rows a block.
 // What is summed over (a group), or shares a scale (a block of columns), is a run of packs:
 enum { kRow = 0, kLanes = 1, kShared = 2 };
@@ -23,34 +25,46 @@ __device__ __forceinline__ int pack_of_place(int u, const Runs& groups, int pack
 struct Sum { static __device__ float of(float a, float b) { return a + b; } };
 struct Max { static __device__ float of(float a, float b) { return fmaxf(a, b); } };
 
+// The sum or the largest of 32 lanes' numbers (none below zero there, so that their bits are in order).
+__device__ __forceinline__ float over_lanes(float v, Sum)
+{
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+__device__ __forceinline__ float over_lanes(float v, Max) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v))); }
+
 // p[j], a value of each of this thread's packs (at[j], zero where there is none), becomes that of the pack's run.  All threads of the block come here.
-template <typename Op, int NP>
-__device__ __forceinline__ void reduce_runs(float (&p)[NP], const int (&at)[NP], const Runs& r, int packs, float* shared)
+// `turn` alternates between the two halves of the memory that whole rows' warps meet in: a half is written again after the other's barrier, so one is enough.
+// What other runs meet in lies behind it.
+template <typename Op, int HOW, int NP>
+__device__ __forceinline__ void reduce_runs(float (&p)[NP], const int (&at)[NP], const Runs& r, int packs, float* shared, int& turn)
 {
     const int tx = threadIdx.x, lane = tx & 31, warp = tx >> 5, warps = blockDim.x >> 5;
-    if (r.how == kLanes) {
+    const int how = HOW < 0 ? r.how : HOW;
+    if (how == kLanes) {
 #pragma unroll
         for (int j = 0; j < NP; ++j)
             for (int d = 1; d < r.lanes; d *= 2) p[j] = Op::of(p[j], __shfl_xor_sync(0xffffffffu, p[j], d));
-    } else if (r.how == kRow) {
+    } else if (how == kRow) {
         float s = p[0];
 #pragma unroll
         for (int j = 1; j < NP; ++j) s = Op::of(s, p[j]);
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) s = Op::of(s, __shfl_xor_sync(0xffffffffu, s, d));
+        s = over_lanes(s, Op());
         if (warps > 1) {
-            float* mine = shared + threadIdx.y * 32;
+            float* mine = shared + turn + threadIdx.y * kMostWarps;
+            turn ^= blockDim.y * kMostWarps;
             if (lane == 0) mine[warp] = s;
             __syncthreads();
-            s = lane < warps ? mine[lane] : 0.f;               // (neutral for the maximum of absolute values too)
+            s = mine[0];
 #pragma unroll
-            for (int d = 1; d < 32; d *= 2) s = Op::of(s, __shfl_xor_sync(0xffffffffu, s, d));
-            __syncthreads();
+            for (int w = 1; w < kMostWarps; ++w)
+                if (w < warps) s = Op::of(s, mine[w]);
         }
 #pragma unroll
         for (int j = 0; j < NP; ++j) p[j] = s;
     } else {
-        float *mine = shared + threadIdx.y * (packs + r.count), *runs = mine + packs;
+        float *mine = shared + blockDim.y * 2 * kMostWarps + threadIdx.y * (packs + r.count), *runs = mine + packs;
 #pragma unroll
         for (int j = 0; j < NP; ++j)
             if (at[j] < packs) mine[at[j]] = p[j];
@@ -106,168 +120,301 @@ __device__ __forceinline__ void store_codes(unsigned char* to, const float (&f)[
     store_pack<unsigned char, V>(to, p);
 }
 
-constexpr int kMostThreads = 512;                              // of a block: 128 registers each
 // Places of a thread at most, for packs of V elements: 16384 elements in 512 threads.
 constexpr int most_places(int v) { return v > 2 ? 8 : v > 1 ? 16 : 32; }
 
-// Every row has its block, and an SM four of 256 threads at once: walks over rows with the next row's numbers under way, as the backward pass takes them, need the
-// registers of half of those (8192 x 4096 to 8 bits 74 us so, 53 without).
-template <typename T, int V, int NP>
-__global__ void __launch_bounds__(kMostThreads, V > 2 && NP <= 2 ? 2 : 1) rms_fwd_kernel(const RmsArgs a, Runs groups, Runs blocks, int packs, int channels)
+// Arithmetic of a pack's numbers, two at a time: these kernels are bound by what they issue next to what they move.
+template <int V> __device__ __forceinline__ void add(float (&a)[V], const float (&b)[V])
 {
-    extern __shared__ float shared[];
+#pragma unroll
+    for (int e = 0; e + 1 < V; e += 2) {
+        const float2 r = __fadd2_rn(make_float2(a[e], a[e + 1]), make_float2(b[e], b[e + 1]));
+        a[e] = r.x, a[e + 1] = r.y;
+    }
+    if (V % 2) a[V - 1] += b[V - 1];
+}
+template <int V> __device__ __forceinline__ void times(float (&a)[V], const float (&b)[V])
+{
+#pragma unroll
+    for (int e = 0; e + 1 < V; e += 2) {
+        const float2 r = __fmul2_rn(make_float2(a[e], a[e + 1]), make_float2(b[e], b[e + 1]));
+        a[e] = r.x, a[e + 1] = r.y;
+    }
+    if (V % 2) a[V - 1] *= b[V - 1];
+}
+template <int V> __device__ __forceinline__ void times(float (&a)[V], float b)
+{
+#pragma unroll
+    for (int e = 0; e + 1 < V; e += 2) {
+        const float2 r = __fmul2_rn(make_float2(a[e], a[e + 1]), both(b));
+        a[e] = r.x, a[e + 1] = r.y;
+    }
+    if (V % 2) a[V - 1] *= b;
+}
+// c <- c + a b
+template <int V> __device__ __forceinline__ void add_times(float (&c)[V], const float (&a)[V], const float (&b)[V])
+{
+#pragma unroll
+    for (int e = 0; e + 1 < V; e += 2) {
+        const float2 r = __ffma2_rn(make_float2(a[e], a[e + 1]), make_float2(b[e], b[e + 1]), make_float2(c[e], c[e + 1]));
+        c[e] = r.x, c[e + 1] = r.y;
+    }
+    if (V % 2) c[V - 1] = fmaf(a[V - 1], b[V - 1], c[V - 1]);
+}
+template <int V> __device__ __forceinline__ void add_times(float (&c)[V], const float (&a)[V], float b)
+{
+#pragma unroll
+    for (int e = 0; e + 1 < V; e += 2) {
+        const float2 r = __ffma2_rn(make_float2(a[e], a[e + 1]), both(b), make_float2(c[e], c[e + 1]));
+        c[e] = r.x, c[e + 1] = r.y;
+    }
+    if (V % 2) c[V - 1] = fmaf(a[V - 1], b, c[V - 1]);
+}
+template <int V> __device__ __forceinline__ float dot(const float (&a)[V], const float (&b)[V])
+{
+    if constexpr (V == 1) return a[0] * b[0];
+    float2 s = __fmul2_rn(make_float2(a[0], a[V > 1]), make_float2(b[0], b[V > 1]));
+#pragma unroll
+    for (int e = 2; e + 1 < V; e += 2) s = __ffma2_rn(make_float2(a[e], a[e + 1]), make_float2(b[e], b[e + 1]), s);
+    return s.x + s.y;
+}
+// The element of a row-major tensor: two factors of 31 bits.
+__device__ __forceinline__ long long element(int row, long long ld, int col) { return (long long)row * (int)ld + col; }
+
+// A thread's places in a ring of `stages` rows of TENSORS tensors, each for itself: it copies its own packs ahead and reads them back, with no barrier.  Without stages it
+// loads them when they are needed, which is right where no block has a second row (and where not even one row of a pass fits).
+template <typename T, int V, int NP>
+struct Ahead {
+    static constexpr int bytes = V * (int)sizeof(T);
+    static constexpr bool async = bytes >= 4;
+    unsigned char* mine;
+    int pitch, tensors, stages;
+    __device__ Ahead(void* ring, int tensors_, int stages_) : pitch(blockDim.x * blockDim.y * bytes), tensors(tensors_), stages(async ? stages_ : 0)
+    {
+        mine = static_cast<unsigned char*>(ring) + (threadIdx.y * blockDim.x + threadIdx.x) * bytes;
+    }
+    __device__ unsigned char* slot(int stage, int tensor, int j) const { return mine + ((stage * tensors + tensor) * NP + j) * pitch; }
+    // Tensor number `tensor` of a row; zeros where `there` says so.
+    __device__ void fetch(int stage, int tensor, const void* from, int row, long long ld, const int (&col)[NP], const bool (&there)[NP]) const
+    {
+        if constexpr (async) {
+#pragma unroll
+            for (int j = 0; j < NP; ++j) copy_async<bytes>(slot(stage, tensor, j), static_cast<const T*>(from) + element(row, ld, col[j]), there[j]);
+        }
+    }
+    __device__ Pack<T, V> get(int stage, int tensor, const void* from, int row, long long ld, int j, int col, bool there) const
+    {
+        if (async && stages) return *reinterpret_cast<const Pack<T, V>*>(slot(stage, tensor, j));
+        return load_masked<T, V>(static_cast<const T*>(from) + element(row, ld, col), there);
+    }
+    // until the oldest of `stages` rows under way is there
+    __device__ void wait() const
+    {
+        if (stages == 4) copies_wait<3>();
+        else if (stages == 3) copies_wait<2>();
+        else if (stages == 2) copies_wait<1>();
+        else if (stages == 1) copies_wait<0>();
+    }
+};
+
+// What a call has, as constants of its kernel: whether there is a second tensor to add (residual, dh), a gate, y and y8, and which lanes share groups and scales.  The
+// branches on them and what they keep apart would be a third of all that these kernels issue, and these are bound by that (8192 x 4096 with a residual to 8 bits: 50M
+// instructions and 67 us so, 35M and 48 with constants; 16384 x 2048 to 16 bits: 56 us and 41).  kAny looks at the arguments: calls that are rare, and rows
+// too large for two packs a thread.
+enum { kSecond = 1, kGate = 2, kY = 4, kY8 = 8, kGroupLanes = 16, kBlockLanes = 32, kAny = -1 };
+template <int KIND> __device__ __forceinline__ bool has(int what, const void* given) { return KIND < 0 ? given != nullptr : (KIND & what) != 0; }
+template <int KIND>
+struct Ways { static constexpr int group = KIND < 0 ? -1 : KIND & kGroupLanes ? kLanes : kRow, block = KIND < 0 ? -1 : KIND & kBlockLanes ? kLanes : kRow; };
+
+// A block takes rows gridDim.x * blockDim.y apart, the next ones' numbers under way while it computes.
+template <typename T, int V, int NP, int KIND>
+__global__ void __launch_bounds__(kMostThreads, V > 2 && NP <= 2 ? 2 : 1) rms_fwd_kernel(const RmsArgs a, Runs groups, Runs blocks, int packs, int channels, int stages, int ring)
+{
+    extern __shared__ float4 shared4[];
+    float* shared = reinterpret_cast<float*>(shared4);
     ptx::grid_dep_wait();
-    const long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
-    const bool real = row < a.M;
-    const T *x = static_cast<const T*>(a.x) + row * a.ldx, *res = static_cast<const T*>(a.residual) + (a.residual ? row * a.ldr : 0);
     const float inverse = 1.f / channels;
-    float f[NP][V], s[NP];
-    Pack<T, V> px[NP], pr[NP], pz[NP];
-    int at[NP];
+    const bool second = has<KIND>(kSecond, a.residual), gated = has<KIND>(kGate, a.z), whole = has<KIND>(kY, a.y), coded = has<KIND>(kY8, a.y8);
+    const int gate = second ? 2 : 1, step = gridDim.x * blockDim.y;
+    const Ahead<T, V, NP> ahead(shared4 + ring, gate + (gated ? 1 : 0), stages);
+    stages = ahead.stages;
+    int at[NP], col[NP], group[NP], block[NP];
+    float w[NP][V];
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
         const int p = at[j] = pack_of_place(threadIdx.x + j * blockDim.x, groups, packs);
-        const bool there = real && p < packs;
-        px[j] = load_masked<T, V>(x + p * V, there);
-        if (a.residual) pr[j] = load_masked<T, V>(res + p * V, there);
-        if (a.z) pz[j] = load_masked<T, V>(static_cast<const T*>(a.z) + row * a.ldz + p * V, there);
+        col[j] = p < packs ? p * V : 0;
+        group[j] = a.G > 1 ? p / groups.packs : 0;
+        block[j] = blocks.count > 1 ? p / blocks.packs : 0;
+        load_gamma<V>(a.gamma, p < packs ? (p - group[j] * groups.packs) * V : 0, w[j]);
     }
+    auto fetch = [&](int stage, int row) {
+        bool there[NP];
 #pragma unroll
-    for (int j = 0; j < NP; ++j) {
-        const int p = at[j];
-        unpack<T, V>(px[j], f[j]);
-        if (a.residual) {                                      // the sum as it is stored is what is normalised, so that the backward pass sees the same
-            float r[V];
-            unpack<T, V>(pr[j], r);
+        for (int j = 0; j < NP; ++j) there[j] = row < a.M && at[j] < packs;
+        row = row < a.M ? row : 0;
+        ahead.fetch(stage, 0, a.x, row, a.ldx, col, there);
+        if (second) ahead.fetch(stage, 1, a.residual, row, a.ldr, col, there);
+        if (gated) ahead.fetch(stage, gate, a.z, row, a.ldz, col, there);
+        copies_commit();
+    };
+    int row = blockIdx.x * blockDim.y + threadIdx.y, stage = 0, turn = 0;
+    for (int i = 0; i < stages; ++i) fetch(i, row + i * step);
+    for (int row0 = blockIdx.x * blockDim.y; row0 < a.M; row0 += step, row += step) {
+        float f[NP][V], s[NP];
+        Pack<T, V> px[NP], pr[NP], pz[NP];
+        bool there[NP];
+        ahead.wait();
 #pragma unroll
-            for (int e = 0; e < V; ++e) f[j][e] += r[e];
-            const Pack<T, V> sum = pack<T, V>(f[j]);
-            unpack<T, V>(sum, f[j]);
-            if (real && p < packs) store_pack<T, V>(static_cast<T*>(a.h) + row * a.ldh + p * V, sum);
+        for (int j = 0; j < NP; ++j) {
+            there[j] = row < a.M && at[j] < packs;
+            px[j] = ahead.get(stage, 0, a.x, row, a.ldx, j, col[j], there[j]);
+            if (second) pr[j] = ahead.get(stage, 1, a.residual, row, a.ldr, j, col[j], there[j]);
+            if (gated) pz[j] = ahead.get(stage, gate, a.z, row, a.ldz, j, col[j], there[j]);
         }
-        s[j] = 0.f;
 #pragma unroll
-        for (int e = 0; e < V; ++e) s[j] = fmaf(f[j][e], f[j][e], s[j]);
-        s[j] *= inverse;                                       // (a mean does not overflow where its terms do not, a sum of thousands would)
-    }
-    reduce_runs<Sum>(s, at, groups, packs, shared);
-    float most[NP];
-#pragma unroll
-    for (int j = 0; j < NP; ++j) {
-        const int p = at[j];
-        const float r = rsqrtf(s[j] + a.eps);
-        const bool there = real && p < packs;
-        const int group = a.G > 1 ? p / groups.packs : 0;
-        if (a.rstd && there && p == group * groups.packs) a.rstd[row * a.G + group] = r;
-        float w[V];
-        if (there) load_gamma<V>(a.gamma, (p - group * groups.packs) * V, w);
-#pragma unroll
-        for (int e = 0; e < V; ++e) f[j][e] = there ? f[j][e] * r * w[e] : 0.f;
-        if (a.z) {
-            float z[V];
-            unpack<T, V>(pz[j], z);
-            activate(z, CONV2D_ACT_SILU);
-#pragma unroll
-            for (int e = 0; e < V; ++e) f[j][e] *= z[e];
+        for (int j = 0; j < NP; ++j) {
+            unpack<T, V>(px[j], f[j]);
+            if (second) {                                  // the sum as it is stored is what is normalised, so that the backward pass sees the same
+                float r[V];
+                unpack<T, V>(pr[j], r);
+                add<V>(f[j], r);
+                const Pack<T, V> sum = pack<T, V>(f[j]);
+                unpack<T, V>(sum, f[j]);
+                if (there[j]) store_pack<T, V>(static_cast<T*>(a.h) + element(row, a.ldh, col[j]), sum);
+            }
+            s[j] = dot<V>(f[j], f[j]) * inverse;               // (a mean does not overflow where its terms do not, a sum of thousands would)
         }
-        if (a.y && there) store_pack<T, V>(static_cast<T*>(a.y) + row * a.ldy + p * V, pack<T, V>(f[j]));
-        most[j] = 0.f;
+        reduce_runs<Sum, Ways<KIND>::group>(s, at, groups, packs, shared, turn);
+        if (stages) {
+            fetch(stage, row + stages * step);
+            stage = stage + 1 == stages ? 0 : stage + 1;
+        }
+        float most[NP];
 #pragma unroll
-        for (int e = 0; e < V; ++e) most[j] = fmaxf(most[j], fabsf(f[j][e]));
-    }
-    if (!a.y8) return;
-    reduce_runs<Max>(most, at, blocks, packs, shared);
+        for (int j = 0; j < NP; ++j) {
+            const float r = rsqrtf(s[j] + a.eps);
+            if (a.rstd && there[j] && at[j] == group[j] * groups.packs) a.rstd[(long long)row * a.G + group[j]] = r;
+            times<V>(f[j], r);
+            times<V>(f[j], w[j]);
+            if (gated) {
+                float z[V];
+                unpack<T, V>(pz[j], z);
+                activate(z, CONV2D_ACT_SILU);
+                times<V>(f[j], z);
+            }
+            if (whole && there[j]) store_pack<T, V>(static_cast<T*>(a.y) + element(row, a.ldy, col[j]), pack<T, V>(f[j]));
+            most[j] = 0.f;
 #pragma unroll
-    for (int j = 0; j < NP; ++j) {
-        const int p = at[j];
-        if (!real || p >= packs) continue;
-        const float scale = fmaxf(most[j] * (1.f / 448.f), 1.17549435e-38f), up = 1.f / scale;
-        const int block = blocks.count > 1 ? p / blocks.packs : 0;
-        if (p == block * blocks.packs) a.scales[row * blocks.count + block] = scale;
+            for (int e = 0; e < V; ++e) most[j] = fmaxf(most[j], fabsf(f[j][e]));
+            if (!there[j]) most[j] = 0.f;
+        }
+        if (!coded) continue;
+        reduce_runs<Max, Ways<KIND>::block>(most, at, blocks, packs, shared, turn);
 #pragma unroll
-        for (int e = 0; e < V; ++e) f[j][e] *= up;
-        store_codes<V>(static_cast<unsigned char*>(a.y8) + row * a.ld8 + p * V, f[j]);
+        for (int j = 0; j < NP; ++j) {
+            if (!there[j]) continue;
+            const float scale = fmaxf(most[j] * (1.f / 448.f), 1.17549435e-38f);
+            if (at[j] == block[j] * blocks.packs) a.scales[(long long)row * blocks.count + block[j]] = scale;
+            times<V>(f[j], 1.f / scale);
+            store_codes<V>(static_cast<unsigned char*>(a.y8) + element(row, a.ld8, col[j]), f[j]);
+        }
     }
 }
 
-// Backward: with n = dy gamma silu(z) and m = h r,   dx = r (n - m mean(n m)) + dh.  A block takes rows gridDim.x * blockDim.y apart, the next one's numbers under way
-// while it computes, and keeps its sums for gamma in registers until the end, when they are added over its rows and groups.
-template <typename T, int V, int NP>
-__global__ void __launch_bounds__(kMostThreads, 1) rms_bwd_kernel(const RmsArgs a, Runs groups, int packs, int channels)
+// Backward: with n = dy gamma silu(z) and m = h r,   dx = r (n - m mean(n m)) + dh.  Rows as in the forward pass; a block keeps its sums for gamma in registers until the
+// end, when they are added over its rows and groups.
+template <typename T, int V, int NP, int KIND>
+__global__ void __launch_bounds__(kMostThreads, 1) rms_bwd_kernel(const RmsArgs a, Runs groups, int packs, int channels, int stages, int ring)
 {
-    extern __shared__ float shared[];
+    extern __shared__ float4 shared4[];
+    float* shared = reinterpret_cast<float*>(shared4);
     ptx::grid_dep_wait();
     const float inverse = 1.f / channels;
-    float w[NP][V], dw[NP][V], r[NP];
-    int group[NP], at[NP];
-    Pack<T, V> ph[NP], py[NP], pd[NP], pz[NP];
-    const long long step = (long long)gridDim.x * blockDim.y;
-    auto fetch = [&](long long row) {
-#pragma unroll
-        for (int j = 0; j < NP; ++j) {
-            const int p = at[j];
-            const bool there = row < a.M && p < packs;
-            ph[j] = load_masked<T, V>(static_cast<const T*>(a.x) + row * a.ldx + p * V, there);
-            py[j] = load_masked<T, V>(static_cast<const T*>(a.dy) + row * a.lddy + p * V, there);
-            if (a.dh) pd[j] = load_masked<T, V>(static_cast<const T*>(a.dh) + row * a.lddh + p * V, there);
-            if (a.z) pz[j] = load_masked<T, V>(static_cast<const T*>(a.z) + row * a.ldz + p * V, there);
-            r[j] = load_masked<float, 1>(a.rstd_in + row * a.G + group[j], there).e[0];
-        }
-    };
+    const bool second = has<KIND>(kSecond, a.dh), gated = has<KIND>(kGate, a.z);
+    const int gate = second ? 3 : 2, step = gridDim.x * blockDim.y;
+    const Ahead<T, V, NP> ahead(shared4 + ring, gate + (gated ? 1 : 0), stages);
+    stages = ahead.stages;
+    float w[NP][V], dw[NP][V], next[NP];
+    int at[NP], col[NP], group[NP];
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
         const int p = at[j] = pack_of_place(threadIdx.x + j * blockDim.x, groups, packs);
-        group[j] = a.G > 1 ? p / groups.packs : 0;
-        if (p < packs) load_gamma<V>(a.gamma, (p - group[j] * groups.packs) * V, w[j]);
+        col[j] = p < packs ? p * V : 0;
+        group[j] = a.G > 1 && p < packs ? p / groups.packs : 0;
+        load_gamma<V>(a.gamma, p < packs ? (p - group[j] * groups.packs) * V : 0, w[j]);
 #pragma unroll
-        for (int e = 0; e < V; ++e) dw[j][e] = 0.f, w[j][e] = p < packs ? w[j][e] : 0.f;
+        for (int e = 0; e < V; ++e) dw[j][e] = 0.f;
     }
-    fetch((long long)blockIdx.x * blockDim.y + threadIdx.y);
-    for (long long row0 = (long long)blockIdx.x * blockDim.y; row0 < a.M; row0 += step) {
-        const long long row = row0 + threadIdx.y;
-        const bool real = row < a.M;
-        float m[NP][V], n[NP][V], d[NP][V], s[NP], rr[NP];
+    auto fetch = [&](int stage, int row) {
+        bool there[NP];
+#pragma unroll
+        for (int j = 0; j < NP; ++j) there[j] = row < a.M && at[j] < packs;
+        row = row < a.M ? row : 0;
+        ahead.fetch(stage, 0, a.x, row, a.ldx, col, there);
+        ahead.fetch(stage, 1, a.dy, row, a.lddy, col, there);
+        if (second) ahead.fetch(stage, 2, a.dh, row, a.lddh, col, there);
+        if (gated) ahead.fetch(stage, gate, a.z, row, a.ldz, col, there);
+        copies_commit();
+    };
+    auto fetch_r = [&](int row) {
+#pragma unroll
+        for (int j = 0; j < NP; ++j) next[j] = load_masked<float, 1>(a.rstd_in + (long long)row * a.G + group[j], row < a.M && at[j] < packs).e[0];
+    };
+    int row = blockIdx.x * blockDim.y + threadIdx.y, stage = 0, turn = 0;
+    for (int i = 0; i < stages; ++i) fetch(i, row + i * step);
+    fetch_r(row);
+    for (int row0 = blockIdx.x * blockDim.y; row0 < a.M; row0 += step, row += step) {
+        float m[NP][V], n[NP][V], s[NP], r[NP];
+        Pack<T, V> ph[NP], py[NP], pd[NP], pz[NP];
+        bool there[NP];
+        ahead.wait();
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
-            const int p = at[j];
+            there[j] = row < a.M && at[j] < packs;
+            ph[j] = ahead.get(stage, 0, a.x, row, a.ldx, j, col[j], there[j]);
+            py[j] = ahead.get(stage, 1, a.dy, row, a.lddy, j, col[j], there[j]);
+            if (second) pd[j] = ahead.get(stage, 2, a.dh, row, a.lddh, j, col[j], there[j]);
+            if (gated) pz[j] = ahead.get(stage, gate, a.z, row, a.ldz, j, col[j], there[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
             unpack<T, V>(ph[j], m[j]);
             unpack<T, V>(py[j], n[j]);
-            if (a.dh) unpack<T, V>(pd[j], d[j]);
-            rr[j] = r[j];
-#pragma unroll
-            for (int e = 0; e < V; ++e) m[j][e] *= rr[j];
-            if (a.z) {
+            r[j] = next[j];
+            times<V>(m[j], r[j]);
+            if (gated) {
                 float z[V], dz[V];
                 unpack<T, V>(pz[j], z);
 #pragma unroll
-                for (int e = 0; e < V; ++e) dz[e] = n[j][e] * w[j][e] * m[j][e];
+                for (int e = 0; e < V; ++e) dz[e] = n[j][e];
+                times<V>(dz, w[j]);
+                times<V>(dz, m[j]);
                 times_slope(dz, z, CONV2D_ACT_SILU);
                 activate(z, CONV2D_ACT_SILU);
-#pragma unroll
-                for (int e = 0; e < V; ++e) n[j][e] *= z[e];
-                if (real && p < packs) store_pack<T, V>(static_cast<T*>(a.dz) + row * a.lddz + p * V, pack<T, V>(dz));
+                times<V>(n[j], z);
+                if (there[j]) store_pack<T, V>(static_cast<T*>(a.dz) + element(row, a.lddz, col[j]), pack<T, V>(dz));
             }
-            s[j] = 0.f;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                dw[j][e] = fmaf(n[j][e], m[j][e], dw[j][e]);
-                n[j][e] *= w[j][e];
-                s[j] = fmaf(n[j][e], m[j][e], s[j]);
-            }
+            add_times<V>(dw[j], n[j], m[j]);
+            times<V>(n[j], w[j]);
+            s[j] = dot<V>(n[j], m[j]);
         }
-        fetch(row + step);
-        reduce_runs<Sum>(s, at, groups, packs, shared);
+        fetch_r(row + step);
+        reduce_runs<Sum, Ways<KIND>::group>(s, at, groups, packs, shared, turn);
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
-            const int p = at[j];
-            const float mean = s[j] * inverse;
-#pragma unroll
-            for (int e = 0; e < V; ++e) n[j][e] = rr[j] * fmaf(-m[j][e], mean, n[j][e]);
-            if (a.dh) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) n[j][e] += d[j][e];
+            add_times<V>(n[j], m[j], -s[j] * inverse);
+            times<V>(n[j], r[j]);
+            if (second) {
+                float d[V];
+                unpack<T, V>(pd[j], d);
+                add<V>(n[j], d);
             }
-            if (real && p < packs) store_pack<T, V>(static_cast<T*>(a.dx) + row * a.lddx + p * V, pack<T, V>(n[j]));
+            if (there[j]) store_pack<T, V>(static_cast<T*>(a.dx) + element(row, a.lddx, col[j]), pack<T, V>(n[j]));
+        }
+        if (stages) {
+            fetch(stage, row + stages * step);
+            stage = stage + 1 == stages ? 0 : stage + 1;
         }
     }
     if (!a.dgamma) return;
@@ -344,41 +491,60 @@ struct RowPlan {
         return r;
     }
 };
-size_t shared_bytes(const RowPlan& p, const Runs& r) { return r.how == kShared ? (size_t)p.rows * (p.packs + r.count) * 4 : r.how == kRow ? p.rows * 32 * 4 : 0; }
+size_t shared_bytes(const RowPlan& p, const Runs& r) { return r.how == kLanes ? 0 : (size_t)p.rows * (2 * kMostWarps + (r.how == kShared ? p.packs + r.count : 0)) * 4; }
 
-template <typename T, int V, int NP>
+// Blocks of a pass with `regs` registers a thread: as many as run at once, and the rows that each has under way, up to four, in the shared memory that `used` bytes leave.
+struct Spread {
+    int blocks, stages;
+    Spread(const RmsArgs& a, const RowPlan& p, int regs, int row_bytes, size_t used)
+    {
+        const int each = p.threads * p.rows * regs, resident = 65536 / each > 1 ? 65536 / each : 1;
+        const long long all = ((long long)a.M + p.rows - 1) / p.rows, most = (long long)resident * sm_count();
+        blocks = (int)(all < most ? all : most);
+        const size_t room = 220 * 1024 / resident, left = room > used ? room - used : 0, fit = left / ((size_t)row_bytes * p.rows);
+        const long long rows = (all + blocks - 1) / blocks;    // of a block
+        stages = (int)(fit < 4 ? fit : 4);
+        if (stages > rows) stages = (int)rows;
+        if (rows == 1) stages = 0;
+    }
+};
+
+template <typename T, int V, int NP, int KIND>
 conv2d_status_t forward(const RmsArgs& a, const RowPlan& p, cudaStream_t stream)
 {
     static SmemLimit limit;
     const Runs groups = p.groups, blocks = p.blocks(a.y8 ? a.block : a.C);
-    const size_t one = shared_bytes(p, groups), two = shared_bytes(p, blocks), smem = one > two ? one : two;
-    if (raise_smem_limit((const void*)rms_fwd_kernel<T, V, NP>, smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-    if (launch_pdl(rms_fwd_kernel<T, V, NP>, dim3(ceil_div_u(a.M, p.rows)), dim3(p.threads, p.rows), smem, stream, a, groups, blocks, p.packs, a.C / a.G) !=
-        cudaSuccess)
+    const size_t one = shared_bytes(p, groups), two = shared_bytes(p, blocks), sums = ((one > two ? one : two) + 15) / 16 * 16;
+    const int row_bytes = (1 + !!a.residual + !!a.z) * NP * p.threads * V * (int)sizeof(T);
+    const Spread spread(a, p, V > 2 && NP <= 2 ? 64 : 128, row_bytes, sums);
+    const size_t smem = sums + (size_t)spread.stages * row_bytes * p.rows;
+    if (raise_smem_limit((const void*)rms_fwd_kernel<T, V, NP, KIND>, smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+    if (launch_pdl(rms_fwd_kernel<T, V, NP, KIND>, dim3(spread.blocks), dim3(p.threads, p.rows), smem, stream, a, groups, blocks, p.packs, a.C / a.G, spread.stages,
+                   (int)(sums / 16)) != cudaSuccess)
         return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;
 }
 
-// Blocks of the backward pass: two for every SM, whose partial sums are added afterwards.
-int bwd_blocks(int M, int rows)
-{
-    const long long all = ((long long)M + rows - 1) / rows, most = 2LL * sm_count();
-    return (int)(all < most ? all : most);
-}
+// Most blocks of the backward pass, whose partial sums are added afterwards.
+int most_bwd_blocks(int M) { return M < 4 * sm_count() ? M : 4 * sm_count(); }
 
-template <typename T, int V, int NP>
+template <typename T, int V, int NP, int KIND>
 conv2d_status_t backward(const RmsArgs& a, const RowPlan& p, cudaStream_t stream)
 {
     static SmemLimit limit;
     const Runs groups = p.groups;
-    const size_t runs = shared_bytes(p, groups), sums = a.dgamma ? (size_t)p.rows * a.C * 4 : 0, smem = runs > sums ? runs : sums;
-    if (raise_smem_limit((const void*)rms_bwd_kernel<T, V, NP>, smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
-    const int blocks = bwd_blocks(a.M, p.rows), channels = a.C / a.G;
-    if (launch_pdl(rms_bwd_kernel<T, V, NP>, dim3(blocks), dim3(p.threads, p.rows), smem, stream, a, groups, p.packs, channels) != cudaSuccess) return CONV2D_ERR_CUDA;
+    const size_t runs = shared_bytes(p, groups), dw = a.dgamma ? (size_t)p.rows * a.C * 4 : 0, sums = ((runs > dw ? runs : dw) + 15) / 16 * 16;
+    const int row_bytes = (2 + !!a.dh + !!a.z) * NP * p.threads * V * (int)sizeof(T), channels = a.C / a.G;
+    const Spread spread(a, p, 128, row_bytes, sums);
+    const size_t smem = sums + (size_t)spread.stages * row_bytes * p.rows;
+    if (raise_smem_limit((const void*)rms_bwd_kernel<T, V, NP, KIND>, smem, limit) != cudaSuccess) return CONV2D_ERR_CUDA;
+    if (launch_pdl(rms_bwd_kernel<T, V, NP, KIND>, dim3(spread.blocks), dim3(p.threads, p.rows), smem, stream, a, groups, p.packs, channels, spread.stages,
+                   (int)(sums / 16)) != cudaSuccess)
+        return CONV2D_ERR_CUDA;
     count_launch();
     if (!a.dgamma) return CONV2D_OK;
-    if (launch_pdl(rms_gamma_kernel, dim3(ceil_div_u(channels, 32)), dim3(32, 32), 0, stream, a.ws, a.dgamma, blocks, channels) != cudaSuccess) return CONV2D_ERR_CUDA;
+    if (launch_pdl(rms_gamma_kernel, dim3(ceil_div_u(channels, 32)), dim3(32, 32), 0, stream, a.ws, a.dgamma, spread.blocks, channels) != cudaSuccess) return CONV2D_ERR_CUDA;
     count_launch();
     return CONV2D_OK;
 }
@@ -393,10 +559,31 @@ bool packs_fit(const RmsArgs& a, int V)
            rows_aligned(a.dh, a.lddh, e, n) && rows_aligned(a.dx, a.lddx, e, n) && rows_aligned(a.dz, a.lddz, e, n);
 }
 
+// The kernel for what the call has, of the kinds named, or the one for any.
+template <typename T, int V, int NP, int KIND, int... MORE>
+conv2d_status_t forward_of(int kind, const RmsArgs& a, const RowPlan& p, cudaStream_t stream)
+{
+    if constexpr (KIND == kAny) return forward<T, V, NP, kAny>(a, p, stream);
+    else return kind == KIND ? forward<T, V, NP, KIND>(a, p, stream) : forward_of<T, V, NP, MORE...>(kind, a, p, stream);
+}
+template <typename T, int V, int NP, int KIND, int... MORE>
+conv2d_status_t backward_of(int kind, const RmsArgs& a, const RowPlan& p, cudaStream_t stream)
+{
+    if constexpr (KIND == kAny) return backward<T, V, NP, kAny>(a, p, stream);
+    else return kind == KIND ? backward<T, V, NP, KIND>(a, p, stream) : backward_of<T, V, NP, MORE...>(kind, a, p, stream);
+}
 template <typename T, int V, int NP>
 conv2d_status_t either(const RmsArgs& a, const RowPlan& p, bool bwd, cudaStream_t stream)
 {
-    return bwd ? backward<T, V, NP>(a, p, stream) : forward<T, V, NP>(a, p, stream);
+    if constexpr (V * sizeof(T) == 16 && NP <= 2) {            // kinds: the norm at a layer's entry, of its heads, at its exit
+        const Runs blocks = p.blocks(a.y8 ? a.block : a.C);
+        int kind = (a.residual || a.dh ? kSecond : 0) | (a.z ? kGate : 0) | (a.y ? kY : 0) | (a.y8 ? kY8 : 0) | (p.groups.how == kLanes ? kGroupLanes : 0) |
+                   (a.y8 && blocks.how == kLanes ? kBlockLanes : 0);
+        if (p.groups.how == kShared || blocks.how == kShared) kind = kAny;
+        if (bwd) return backward_of<T, V, NP, kSecond, 0, kGate, kGroupLanes, kGate | kGroupLanes, kAny>(kind, a, p, stream);
+        return forward_of<T, V, NP, kSecond | kY, kSecond | kY8, kSecond | kY8 | kBlockLanes, kY, kGate | kY, kGroupLanes | kY, kGroupLanes | kGate | kY, kAny>(kind, a, p, stream);
+    }
+    return bwd ? backward<T, V, NP, kAny>(a, p, stream) : forward<T, V, NP, kAny>(a, p, stream);
 }
 // Packs of V elements, or the next smaller that fit.
 template <typename T, int V>
@@ -430,7 +617,7 @@ conv2d_status_t rms(const RmsArgs& a, conv2d_operand_t type, bool bwd, cudaStrea
 }  // namespace
 
 // (a row of partial sums for every block, whichever way the rows are spread)
-size_t rms_bwd_workspace_bytes(int M, int C, int G) { return ((size_t)bwd_blocks(M, 1) * (C / G) * 4 + 15) / 16 * 16; }
+size_t rms_bwd_workspace_bytes(int M, int C, int G) { return ((size_t)most_bwd_blocks(M) * (C / G) * 4 + 15) / 16 * 16; }
 conv2d_status_t launch_rms_fwd(const RmsArgs& a, conv2d_operand_t type, cudaStream_t stream) { return rms(a, type, false, stream); }
 conv2d_status_t launch_rms_bwd(const RmsArgs& a, conv2d_operand_t type, cudaStream_t stream) { return rms(a, type, true, stream); }
 
