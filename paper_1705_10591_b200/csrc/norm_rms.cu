@@ -181,8 +181,8 @@ template <int V> __device__ __forceinline__ float dot(const float (&a)[V], const
 // The element of a row-major tensor: two factors of 31 bits.
 __device__ __forceinline__ long long element(int row, long long ld, int col) { return (long long)row * (int)ld + col; }
 
-// A thread's places in a ring of `stages` rows of TENSORS tensors, each for itself: it copies its own packs ahead and reads them back, with no barrier.  Without stages it
-// loads them when they are needed, which is right where no block has a second row (and where not even one row of a pass fits).
+// A thread's places in a ring of `stages` rows of TENSORS tensors, each for itself: it copies its own packs ahead and reads them back, with no barrier.  Without stages, where
+// not even one row of a pass fits, it loads them when they are needed.
 template <typename T, int V, int NP>
 struct Ahead {
     static constexpr int bytes = V * (int)sizeof(T);
@@ -246,7 +246,6 @@ __global__ void __launch_bounds__(kMostThreads, V > 2 && NP <= 2 ? 2 : 1) rms_fw
         col[j] = p < packs ? p * V : 0;
         group[j] = a.G > 1 ? p / groups.packs : 0;
         block[j] = blocks.count > 1 ? p / blocks.packs : 0;
-        load_gamma<V>(a.gamma, p < packs ? (p - group[j] * groups.packs) * V : 0, w[j]);
     }
     auto fetch = [&](int stage, int row) {
         bool there[NP];
@@ -260,6 +259,8 @@ __global__ void __launch_bounds__(kMostThreads, V > 2 && NP <= 2 ? 2 : 1) rms_fw
     };
     int row = blockIdx.x * blockDim.y + threadIdx.y, stage = 0, turn = 0;
     for (int i = 0; i < stages; ++i) fetch(i, row + i * step);
+#pragma unroll
+    for (int j = 0; j < NP; ++j) load_gamma<V>(a.gamma, at[j] < packs ? (at[j] - group[j] * groups.packs) * V : 0, w[j]);
     for (int row0 = blockIdx.x * blockDim.y; row0 < a.M; row0 += step, row += step) {
         float f[NP][V], s[NP];
         Pack<T, V> px[NP], pr[NP], pz[NP];
@@ -342,7 +343,6 @@ __global__ void __launch_bounds__(kMostThreads, 1) rms_bwd_kernel(const RmsArgs 
         const int p = at[j] = pack_of_place(threadIdx.x + j * blockDim.x, groups, packs);
         col[j] = p < packs ? p * V : 0;
         group[j] = a.G > 1 && p < packs ? p / groups.packs : 0;
-        load_gamma<V>(a.gamma, p < packs ? (p - group[j] * groups.packs) * V : 0, w[j]);
 #pragma unroll
         for (int e = 0; e < V; ++e) dw[j][e] = 0.f;
     }
@@ -364,6 +364,8 @@ __global__ void __launch_bounds__(kMostThreads, 1) rms_bwd_kernel(const RmsArgs 
     int row = blockIdx.x * blockDim.y + threadIdx.y, stage = 0, turn = 0;
     for (int i = 0; i < stages; ++i) fetch(i, row + i * step);
     fetch_r(row);
+#pragma unroll
+    for (int j = 0; j < NP; ++j) load_gamma<V>(a.gamma, at[j] < packs ? (at[j] - group[j] * groups.packs) * V : 0, w[j]);
     for (int row0 = blockIdx.x * blockDim.y; row0 < a.M; row0 += step, row += step) {
         float m[NP][V], n[NP][V], s[NP], r[NP];
         Pack<T, V> ph[NP], py[NP], pd[NP], pz[NP];
@@ -505,7 +507,6 @@ struct Spread {
         const long long rows = (all + blocks - 1) / blocks;    // of a block
         stages = (int)(fit < 4 ? fit : 4);
         if (stages > rows) stages = (int)rows;
-        if (rows == 1) stages = 0;
     }
 };
 
