@@ -26,6 +26,7 @@ extern "C" {
  * Products run on the tensor cores, sums and states as operands in three bf16 numbers each (24 bits).
  * states (optional): what the backward pass continues from, delta_states_size bytes, aligned to 16; the caller keeps it until then.
  * B * H * ceil(L / 64) * ceil(V / 16) is below 2^31.
+ * Waits on the device are bounded; should one expire, the results are not defined and conv2d_get_status(NULL, cuda_stream) says so (CONV2D_ERR_DEVICE_TIMEOUT).
  */
 conv2d_status_t delta_states_size(int B, int L, int Hk, int H, int K, int V, conv2d_operand_t type, size_t* bytes);
 conv2d_status_t delta_fwd_gated_workspace_size(int B, int L, int Hk, int H, int K, int V, conv2d_operand_t type, size_t* bytes);
@@ -56,13 +57,14 @@ conv2d_status_t delta_bwd_gated(const void* q, const void* k, const int* lengths
 /*
  * RMS norm of M rows of C <= 16384 channels in G groups (G divides C), each normalised by itself:
  *   h = x + residual, rounded to `type` (h = x where residual is NULL),   r = 1 / sqrt(mean(h^2) + eps),   n = gamma[c % (C/G)] h r,
- *   y = n * silu(z)   (y = n where z is NULL).
+ *   y = n * silu(z)   (y = n where z is NULL).   With eps of zero a group of zeros becomes NaN.
  *   x, residual (optional), z (optional), y [M][C] (ldx, ldr, ldz, ldy); gamma [C/G] fp32, optional (1); eps >= 0.
  *   h [M][C] (ldh): required exactly where residual is given; the residual of the next layer.  It may be the same tensor as residual, or x.
  *   rstd [M][G] fp32, optional: r, for the backward pass.
  *   y8 [M][C] bytes (ld8), scales [M][ceil(C/block)] fp32: y in 8 bits (e4m3), both or neither; at least one of y and y8.  Every `block` adjacent columns of
  *   a row (the last ones may be fewer) share a scale s = max |y| / 448, at least 2^-126, and y8 = y / s, rounded to nearest, even.
- *   A block of more than C columns is the row.  block is not looked at without y8.  What is rounded is y before it is rounded to `type`.
+ *   A block of more than C columns is the row.  block is not looked at without y8.  What is rounded is y before it is rounded to `type`,
+ *   times 1 / s in fp32.  A NaN keeps its place and does not count for the scale; a block with an infinity has an infinite scale.
  */
 conv2d_status_t norm_fwd_rms(const void* x, const void* residual, const void* z, const float* gamma, void* y, void* h,
                              void* y8, float* scales, float* rstd, int M, int C, int G, int block,

@@ -28,6 +28,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
         bars->abort = 0;
         ptx::mbar_init(&bars->keys[0], 1), ptx::mbar_init(&bars->keys[1], 1), ptx::mbar_init(&bars->squares, 1);
         for (int i = 0; i < 3; ++i) ptx::mbar_init(&bars->done[i], 1);
+        ptx::mbar_init(&bars->settled, 1);
         ptx::fence_mbar_init();
     }
     if (warp == kWorkers / 32) {
@@ -42,17 +43,22 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
     const int len = sequence_length(a.lengths, b, a.L), pieces = (len + kPiece - 1) / kPiece;
     const size_t unit0 = (size_t)bh * a.pieces;
 
+    int keys_copied = 0, squares_copied = 0;                   // pieces whose copies have been started
     if (warp == kWorkers / 32) {
         const uint32_t elected = ptx::elect_one();
         const unsigned char* key_tiles = a.keys + ((size_t)b * a.Hk + hk) * a.pieces * W::keys;
         auto load_keys = [&](int s) {                          // the s-th piece from the end
-            if (!elected || s >= pieces) return;
+            if (s >= pieces) return;
+            ++keys_copied;
+            if (!elected) return;
             uint64_t* bar = &bars->keys[STAGES == 2 ? s & 1 : 0];
             ptx::mbar_arrive_expect_tx(bar, W::keys);
             ptx::bulk_g2s(raw + (STAGES == 2 ? s & 1 : 0) * W::keys, key_tiles + (size_t)(pieces - 1 - s) * W::keys, W::keys, bar);
         };
         auto load_squares = [&](int s) {
-            if (!elected || s >= pieces) return;
+            if (s >= pieces) return;
+            ++squares_copied;
+            if (!elected) return;
             ptx::mbar_arrive_expect_tx(&bars->squares, W::squares);
             ptx::bulk_g2s(squares, a.prepared + (unit0 + pieces - 1 - s) * kPrepared, W::squares, &bars->squares);
         };
@@ -194,8 +200,13 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
     __syncthreads();
     if (warp == kWorkers / 32) {
         ptx::tc_fence_after_sync();
+        if (*abort_flag) {
+            settle(&bars->keys[0], STAGES == 2 ? (keys_copied + 1) / 2 : keys_copied), settle(&bars->keys[1], STAGES == 2 ? keys_copied / 2 : 0);
+            settle(&bars->squares, squares_copied);
+            settle_products(&bars->settled, ptx::elect_one());
+            if (lane == 0) atomicExch(a.timeout, 1u);
+        }
         ptx::tmem_dealloc(tmem, W::cols);
-        if (lane == 0 && *abort_flag) atomicExch(a.timeout, 1u);
     }
 }
 
@@ -219,7 +230,7 @@ struct Piecewise {
     static constexpr uint32_t cols = 4 * KD;
 };
 struct PieceBars {
-    uint64_t done[2], keys, last;
+    uint64_t done[2], keys, last, settled;
     uint32_t tmem, abort;
     alignas(16) float factors[kFactors * kPiece];              // (read in fours)
     float dots[8][kPiece], sums[16];
@@ -303,7 +314,7 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
     const bool works = warp < W::WORKERS / 32, shared_key = a.dq_parts != nullptr;
     if (tid == 0) {
         bars.abort = 0;
-        ptx::mbar_init(&bars.done[0], 1), ptx::mbar_init(&bars.done[1], 1), ptx::mbar_init(&bars.keys, 1), ptx::mbar_init(&bars.last, 1);
+        ptx::mbar_init(&bars.done[0], 1), ptx::mbar_init(&bars.done[1], 1), ptx::mbar_init(&bars.keys, 1), ptx::mbar_init(&bars.last, 1), ptx::mbar_init(&bars.settled, 1);
         ptx::fence_mbar_init();
     }
     if (!works) {
@@ -345,6 +356,7 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
         // tiles of rows of 32 numbers, K-major: 64-byte swizzle
         auto narrow = [](uint32_t at) { return rows_as_k<32>(at, 512); };
         bool alive = true;
+        int copied = 0;
         for (unsigned id = begin; id < total; id = following(id + gridDim.x), parity ^= 1) {
             const Place here(a, id);
             for (int j = 0; j < blocks; ++j) {
@@ -360,6 +372,7 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
             }
             first_so_far += first_of, second_so_far += second_of;
             alive = alive && ptx::mbar_wait_bounded_warp(&bars.done[(blocks - 1) & 1], (((blocks - 1) & 1 ? second_so_far : first_so_far) - 1) & 1, abort_flag, a.max_polls);
+            copied += alive;
             if (alive && elected) {                            // (the tiles over V are done with)
                 ptx::mbar_arrive_expect_tx(&bars.keys, W::keys);
                 ptx::bulk_g2s(raw, a.keys + (((size_t)here.b * a.Hk + here.h / a.share) * a.pieces + id % a.pieces) * W::keys, W::keys, &bars.keys);
@@ -379,8 +392,12 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
             __syncthreads();                                   // (and out)
         }
         ptx::tc_fence_after_sync();
+        if (*abort_flag) {
+            settle(&bars.keys, copied);
+            settle_products(&bars.settled, elected);
+            if (lane == 0) atomicExch(a.timeout, 1u);
+        }
         ptx::tmem_dealloc(tmem, W::cols);
-        if (lane == 0 && *abort_flag) atomicExch(a.timeout, 1u);
         return;
     }
 

@@ -21,6 +21,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
         bars->abort = 0;
         ptx::mbar_init(&bars->keys[0], 1), ptx::mbar_init(&bars->keys[1], 1), ptx::mbar_init(&bars->squares, 1);
         for (int i = 0; i < 3; ++i) ptx::mbar_init(&bars->done[i], 1);
+        ptx::mbar_init(&bars->settled, 1);
         ptx::fence_mbar_init();
     }
     if (warp == kWorkers / 32) {
@@ -35,17 +36,22 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
     const int len = sequence_length(a.lengths, b, a.L), pieces = (len + kPiece - 1) / kPiece;
     const size_t unit0 = (size_t)bh * a.pieces;
 
+    int keys_copied = 0, squares_copied = 0;                   // pieces whose copies have been started
     if (warp == kWorkers / 32) {
         const uint32_t elected = ptx::elect_one();
         const unsigned char* key_tiles = a.keys + ((size_t)b * a.Hk + hk) * a.pieces * W::keys;
         auto load_keys = [&](int i) {
-            if (!elected || i >= pieces) return;
+            if (i >= pieces) return;
+            ++keys_copied;
+            if (!elected) return;
             uint64_t* bar = &bars->keys[STAGES == 2 ? i & 1 : 0];
             ptx::mbar_arrive_expect_tx(bar, W::keys);
             ptx::bulk_g2s(raw + (STAGES == 2 ? i & 1 : 0) * W::keys, key_tiles + (size_t)i * W::keys, W::keys, bar);
         };
         auto load_squares = [&](int i) {
-            if (!elected || i >= pieces) return;
+            if (i >= pieces) return;
+            ++squares_copied;
+            if (!elected) return;
             ptx::mbar_arrive_expect_tx(&bars->squares, W::squares);
             ptx::bulk_g2s(squares, a.prepared + (unit0 + i) * kPrepared, W::squares, &bars->squares);
         };
@@ -174,8 +180,13 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_fwd_kernel(const DeltaA
     __syncthreads();
     if (warp == kWorkers / 32) {
         ptx::tc_fence_after_sync();
+        if (*abort_flag) {
+            settle(&bars->keys[0], STAGES == 2 ? (keys_copied + 1) / 2 : keys_copied), settle(&bars->keys[1], STAGES == 2 ? keys_copied / 2 : 0);
+            settle(&bars->squares, squares_copied);
+            settle_products(&bars->settled, ptx::elect_one());
+            if (lane == 0) atomicExch(a.timeout, 1u);
+        }
         ptx::tmem_dealloc(tmem, W::cols);
-        if (lane == 0 && *abort_flag) atomicExch(a.timeout, 1u);
     }
 }
 

@@ -170,9 +170,20 @@ __device__ __forceinline__ void zero_rows(T* to, long long ld, int first, int L,
 
 // Barriers of a block, 128 bytes at most.
 struct WalkBars {
-    uint64_t keys[2], squares, done[3];
+    uint64_t keys[2], squares, done[3], settled;
     uint32_t tmem, abort;
 };
+// Behind a wait that gave up: before a block ends, its copies (`issued` onto a barrier, the last of which may be under way) and its products are waited for, with a limit.
+__device__ __forceinline__ void settle(uint64_t* bar, int issued)
+{
+    for (uint32_t i = 0; issued > 0 && i < (1u << 22); ++i)
+        if (ptx::mbar_try_wait(bar, (issued - 1) & 1)) return;
+}
+__device__ __forceinline__ void settle_products(uint64_t* unused, uint32_t elected)
+{
+    ptx::mma_commit(unused, elected);
+    settle(unused, 1);
+}
 
 // Tiles of 64 tokens x NV elements as they lie in their tensor, in units of 16 bytes swizzled like the operands.
 template <typename T, int NV>

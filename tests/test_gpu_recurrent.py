@@ -253,6 +253,78 @@ def test_delta_captured_and_on_another_stream(lib):  # noqa: F811
     assert all(torch.equal(a.result(), b) for a, b in zip(grads.values(), want[1][2:]))
 
 
+@pytest.mark.parametrize("columns", ["32", "64"])
+@pytest.mark.parametrize("case", [("bf16", 2, 200, 2, 4, 128, 128, [200, 65]), ("fp16", 1, 150, 1, 2, 100, 96, None), ("fp32", 1, 130, 1, 1, 64, 72, None)],
+                         ids=lambda c: f"{c[0]}-{c[5]}x{c[6]}")
+def test_walks_of_either_width(lib, monkeypatch, case, columns):  # noqa: F811
+    """Blocks of 32 and of 64 columns, whatever the rule says."""
+    monkeypatch.setenv("CONV2D_B200_DELTA_COLUMNS", columns)
+    c = Delta(lib, *case)
+    wanted = c.wanted()
+    o, last = c.forward(keep=True)
+    c.check({"o": o, "state": last}, wanted)
+    c.check(c.backward(), wanted)
+
+
+def test_one_workspace_for_calls_one_after_the_other(lib):  # noqa: F811
+    """Two graphs that share a workspace, and calls of other sizes on it, in turn; nothing is expected of what it holds."""
+    c, d = Delta(lib, "bf16", 1, 200, 1, 2, 64, 64), Delta(lib, "fp32", 2, 70, 1, 1, 128, 40, seed=810)
+    op = {"bf16": lib.OPERAND_BF16, "fp32": lib.OPERAND_FP32}
+    need = max(f(*x.dims, op[x.type]) for x in (c, d) for f in (lib.delta_fwd_gated_workspace_size, lib.delta_bwd_gated_workspace_size))
+    ws = workspace(need)
+    ws.fill_(0xff)
+    want, outs, graphs = [], [], []
+    for x in (c, d):
+        o, last = x.forward(keep=True, ws=ws)
+        want.append([o.result(), last.result()] + [r.result() for r in x.backward(ws=ws).values()])
+    torch.cuda.synchronize()
+    for x in (c, d):
+        o, last = x.rows(x.dims[3] * x.dims[5], x.t), Rows((x.dims[0], x.dims[3], x.dims[4], x.dims[5]), torch.float32)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            x.forward(keep=True, o=o, last=last, ws=ws)
+            grads = x.backward(ws=ws)
+        graphs.append(graph), outs.append([o, last, *grads.values()])
+    for i in (0, 1, 1, 0):
+        ws.fill_(0xff)
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.result(), b) for a, b in zip(outs[i], want[i]))
+
+
+@pytest.mark.parametrize("V, columns", [(65536, None), (4100, "32")])
+def test_many_columns(lib, monkeypatch, V, columns):  # noqa: F811
+    if columns:
+        monkeypatch.setenv("CONV2D_B200_DELTA_COLUMNS", columns)
+    c = Delta(lib, "bf16", 1, 70 if V < 65536 else 3, 1, 1, 5, V)
+    wanted = c.wanted()
+    o, last = c.forward(keep=True)
+    c.check({"o": o, "state": last}, wanted)
+    c.check(c.backward(), wanted)
+
+
+def test_an_expired_wait_is_reported(lib, monkeypatch):  # noqa: F811
+    """With no patience at all every wait gives up: the kernels wait for what they have under way, return, and the status says so, once; the next calls are right."""
+    c = Delta(lib, "bf16", 2, 140, 1, 2, 64, 64)
+    wanted = c.wanted()
+    c.forward(keep=True)
+    torch.cuda.synchronize()
+    for call in (c.forward, c.backward):
+        monkeypatch.setenv("CONV2D_B200_DELTA_MAX_POLLS", "0")
+        call()
+        with pytest.raises(lib.Conv2dError) as e:
+            lib.conv2d_get_status(0, stream())
+        assert e.value.status == 8                              # CONV2D_ERR_DEVICE_TIMEOUT
+        torch.cuda.synchronize()
+        lib.conv2d_get_status(0, stream())
+        monkeypatch.delenv("CONV2D_B200_DELTA_MAX_POLLS")
+    o, last = c.forward(keep=True)
+    c.check({"o": o, "state": last}, wanted)
+    c.check(c.backward(), wanted)
+    lib.conv2d_get_status(0, stream())
+
+
 def test_delta_beyond_32_bit_offsets(lib):  # noqa: F811
     """Rows so far apart that the last sequence lies beyond 2^31 elements."""
     B, L, K, V = 3, 70, 64, 32
@@ -294,6 +366,13 @@ RMS = [  # type, M, C, G, residual, gate, pad, offset
     ("fp16", 2, 16320, 60, True, True, 0, 4),
     ("bf16", 2, 16383, 1, True, False, 0, 1),
     ("fp32", 9, 90, 5, True, True, 0, 2),
+    # (several rows a block, the last ones fewer)
+    ("bf16", 3001, 1280, 1, True, False, 0, 0),
+    ("fp16", 6001, 520, 5, False, True, 0, 0),
+    ("fp32", 4003, 300, 3, True, True, 1, 1),
+    ("bf16", 5003, 264, 1, False, True, 0, 0),
+    ("fp32", 1300, 4096, 32, False, False, 0, 0),
+    ("bf16", 1501, 8200, 1, True, True, 0, 0),
 ]
 
 
@@ -344,7 +423,9 @@ def test_rms_norm(lib, case):  # noqa: F811
 @pytest.mark.parametrize("type, M, C, G, block, pad, gate", [("bf16", 5, 4096, 1, 128, 0, False), ("bf16", 7, 4096, 1, 4096, 0, False), ("fp16", 3, 1000, 1, 128, 8, True),
                                                              ("fp16", 4, 288, 6, 128, 0, False), ("bf16", 2, 77, 7, 10, 1, False), ("fp32", 3, 96, 3, 7, 0, True),
                                                              ("fp32", 2, 260, 1, 64, 0, False), ("bf16", 9, 24, 3, 1, 0, False), ("bf16", 300, 64, 1, 64, 0, True),
-                                                             ("bf16", 4, 72, 1, 128, 0, False), ("fp16", 2, 45, 3, 1 << 30, 2, True)])
+                                                             ("bf16", 4, 72, 1, 128, 0, False), ("fp16", 2, 45, 3, 1 << 30, 2, True),
+                                                             ("bf16", 6001, 512, 1, 128, 0, False), ("fp32", 5003, 256, 1, 256, 0, False),
+                                                             ("fp16", 4001, 500, 1, 100, 0, True)])
 def test_output_in_8_bits(lib, type, M, C, G, block, pad, gate):  # noqa: F811
     t = TYPES[type]
     x, z = draw(910, M, C, dtype=t), draw(911, M, C, dtype=t)
