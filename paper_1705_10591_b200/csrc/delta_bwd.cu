@@ -212,22 +212,27 @@ __global__ void __launch_bounds__(kWalkThreads, 1) delta_bwd_walk_kernel(const D
 
 // One block for one piece of one value head: products over V in blocks of 32 columns, two in turn (while one's products run, the threads split the next one's numbers, and
 // those of the one after it are under way), then products over tokens.
-//   D1 [dV; dO] S^T,   D2 [dV; dO] E^T,   D3 E dS^T (64 rows; the others are of what lies behind),   then of D2 [y; p],
+//   D1 [dV; dO] S^T,   D2 [dV; dO] E^T,   D3 E dS^T (64 rows),   then of D2 [y; p],
 //   D4 [y; p] K,   D5 [y; p]^T [K; Q] (64 rows likewise).
 // In the last step a thread has a quarter of a row of a and c (keys) or of dq (queries).  What bounds it: the MMAs of 128 rows, of which those of keys alone are half, six for
-// every pair of numbers in three parts, are a half of its time; the rest is one thing after the other, since tensor memory has room for one block.
+// every pair of numbers in three parts, are a half of its time; the rest is one thing after the other, since tensor memory has room for one piece.
 template <typename T, int KD>
 struct Piecewise {
     static constexpr int IN = Parts<T>::in, NB = 32, HALF = 2 * kPiece * 128, WORKERS = 512, THREADS = WORKERS + 32;
-    static constexpr int rows_part = 2 * kPiece * NB * 2, e_part = kPiece * NB * 2, state_part = KD * NB * 2;
-    static constexpr int at_e = kSum * rows_part, at_s = at_e + kSum * e_part, at_ds = at_s + kSum * state_part, block = at_ds + kSum * state_part;
+    static constexpr int rows_part = 2 * kPiece * NB * 2, half = kPiece * NB * 2, state_part = KD * NB * 2;
+    // E lies as [zeros, E0, E1, zeros, E2], 64 rows each
+    static constexpr int at_e = kSum * rows_part, at_s = at_e + 5 * half, at_ds = at_s + kSum * state_part, block = at_ds + kSum * state_part;
     static constexpr int keys = IN * (KD / 64) * HALF, key_part = (KD / 64) * HALF, square_part = 2 * kPiece * 128;
     // over V: two blocks; over tokens: keys and queries, [y; p], in whose place the results are collected; (the 64 rows more reach as far as one tile
     // behind the last one)
     static constexpr int over_v = 2 * block, over_tokens = keys + kSum * square_part + square_part, results = keys + 2 * kPiece * KD * 4;
-    static constexpr int most = over_v > over_tokens ? over_v : over_tokens, smem = (most > results ? most : results) + 1024;      // (1024 to the first boundary of the swizzle)
-    static constexpr uint32_t d1 = 0, d3 = KD, d4 = 2 * KD, d2 = 3 * KD, d5 = 3 * KD;         // columns of tensor memory (D2 has been read when D5 is written)
-    static constexpr uint32_t cols = 4 * KD;
+    static constexpr int at_small3 = over_tokens > results ? over_tokens : results, behind = at_small3 + kPiece * KD * 4;
+    static constexpr int smem = (over_v > behind ? over_v : behind) + 1024;       // (1024 to the first boundary of the swizzle)
+    static_assert(smem + 4096 <= 232448, "a piece does not fit");                 // (4096: what else a block keeps)
+    // Columns of tensor memory.  Products of first parts have a sum of their own: an MMA cuts what it adds off at the last digit of its sum, of small terms nearly all
+    // (dq of 128 and 256 columns of V 0.8e-6 and 1.6e-6 off with one sum, 0.3e-6 so).  The small sums of D1 and D2 lie where D4 and D5 come later; those of D3
+    // are its rows 64 and on, of E1 beside E0 and of E0 and E2 behind 64 rows of zeros, and are handed over through shared memory.
+    static constexpr uint32_t d1 = 0, d3 = KD, d4 = 2 * KD, d2 = 3 * KD, d5 = 3 * KD, small1 = d4, small2 = d2 + kPiece, cols = 512;
 };
 struct PieceBars {
     uint64_t done[2], keys, last, settled;
@@ -294,7 +299,11 @@ struct QuadPlaces {
         float f[4];
         x.dout.get(f);
         put_four<kSum>(at + row, W::rows_part, x.dv.q[0].e);
-        put_four<kSum>(at + W::at_e + row, W::e_part, x.e.q[0].e);
+        uint32_t w[2][kSum];
+        split<kSum>(x.e.q[0].e[0], x.e.q[0].e[1], w[0]);
+        split<kSum>(x.e.q[0].e[2], x.e.q[0].e[3], w[1]);
+#pragma unroll
+        for (int p = 0; p < kSum; ++p) *reinterpret_cast<uint2*>(at + W::at_e + (p == 2 ? 4 : 1 + p) * W::half + row) = make_uint2(w[0][p], w[1][p]);
         put_four<W::IN>(at + dout, W::rows_part, f);
     }
 };
@@ -364,10 +373,21 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
                 ptx::tc_fence_after_sync();
                 const uint32_t at = base + (j & 1) * W::block;
                 auto rows = [&](int p, int k) { return narrow(at + p * W::rows_part + k * 32); };
-                auto e = [&](int p, int k) { return narrow(at + W::at_e + p * W::e_part + k * 32); };
-                multiply(tmem + W::d1, kSum, kSum, NB / 16, idk, elected, j > 0, rows, [&](int p, int k) { return narrow(at + W::at_s + p * W::state_part + k * 32); });
-                multiply(tmem + W::d2, kSum, kSum, NB / 16, ptx::idesc_b16(128, kPiece, false), elected, j > 0, rows, e);
-                multiply(tmem + W::d3, kSum, kSum, NB / 16, idk, elected, j > 0, e, [&](int p, int k) { return narrow(at + W::at_ds + p * W::state_part + k * 32); });
+                auto e = [&](int p, int k) { return narrow(at + W::at_e + (p == 2 ? 4 : 1 + p) * W::half + k * 32); };
+                auto s = [&](int p, int k) { return narrow(at + W::at_s + p * W::state_part + k * 32); };
+                auto ds = [&](int p, int k) { return narrow(at + W::at_ds + p * W::state_part + k * 32); };
+                constexpr uint32_t id64 = ptx::idesc_b16(128, kPiece, false);
+                multiply_first(tmem + W::d1, NB / 16, idk, elected, j > 0, rows, s);
+                multiply_small(tmem + W::small1, NB / 16, idk, elected, j > 0, rows, s);
+                multiply_first(tmem + W::d2, NB / 16, id64, elected, j > 0, rows, e);
+                multiply_small(tmem + W::small2, NB / 16, id64, elected, j > 0, rows, e);
+                // (of rows 0 to 63 and 64 on: zeros and E0 dS2, zeros and E2 dS0, zeros and E0 dS1, E1 dS1 and zeros, E0 dS0 and E1 dS0)
+                auto third = [&](int half, int part, bool more) {
+#pragma unroll
+                    for (int k = 0; k < NB / 16; ++k) ptx::mma_b16(tmem + W::d3, narrow(at + W::at_e + half * W::half + k * 32), ds(part, k), idk, more || k > 0, elected);
+                };
+                third(0, 2, j > 0), third(3, 0, true), third(0, 1, true);
+                third(2, 1, true), third(1, 0, true);
                 ptx::mma_commit(&bars.done[j & 1], elected);
             }
             first_so_far += first_of, second_so_far += second_of;
@@ -419,6 +439,9 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
         ptx::tc_fence_before_sync();
         __syncthreads();
     };
+    constexpr int SHARE = KD / 4;                              // columns of a thread
+    // D3's small sums, [64][KD] in units of 16 bytes spread over the banks
+    auto small3_at = [&](int col) { return reinterpret_cast<float4*>(raw + W::at_small3) + token * (KD / 4) + ((col >> 2) ^ (token & 7)); };
     fetch(begin);
     for (unsigned id = begin; id < total; parity ^= 1) {
         const Place here(a, id);
@@ -434,6 +457,12 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
         for (int j = 0; j < blocks; ++j) {
             if (j >= 2) ptx::mbar_wait_bounded(&bars.done[j & 1], ((j & 1 ? second_so_far : first_so_far) + (j >> 1) - 1) & 1, abort_flag, a.max_polls);
             places.put(raw + (j & 1) * W::block, next, inner);
+            // (the rows of zeros: tiles of other products have lain there)
+            if (j < 2) {
+                static_assert(2 * W::half / 16 == W::WORKERS, "a unit a thread");
+                const int z = tid < W::WORKERS / 2 ? tid : tid + 2 * W::WORKERS / 2;         // units of the first and of the fourth 64 rows
+                *reinterpret_cast<uint4*>(raw + j * W::block + W::at_e + z * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
             if (j + 1 < blocks) next.fetch(a, here, (j + 1) * NB, tid);
             ready();
         }
@@ -449,7 +478,29 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
         ptx::tc_fence_after_sync();
         {
             float x[16];
-            tmem_row<16>(lanes + W::d2 + side * 16, x);
+            {
+                float y[16];
+                tmem_row<16>(lanes + W::d2 + side * 16, x);
+                tmem_row<16>(lanes + W::small2 + side * 16, y);
+#pragma unroll
+                for (int n = 0; n < 16; ++n) x[n] += y[n];
+            }
+#pragma unroll
+            for (int i = 0; i < SHARE; i += 16) {
+                const int col = side * SHARE + i;
+                uint32_t v[16], w[16];
+                ptx::tmem_ld16(lanes + W::d1 + col, v), ptx::tmem_ld16(lanes + W::small1 + col, w);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int n = 0; n < 16; ++n) v[n] = __float_as_uint(__uint_as_float(v[n]) + __uint_as_float(w[n]));
+                ptx::tmem_st16(lanes + W::d1 + col, v);
+                if (is_key) continue;                          // (whole warps)
+                float y[16];
+                tmem_row<16>(lanes + W::d3 + col, y);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) *small3_at(col + 4 * u) = make_float4(y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]);
+            }
+            ptx::tmem_st_wait();
             const float hi = high[token], lo = low[token], by = is_key ? -1.f : a.scale;
             const int last = is_key ? token - 1 : token;       // (keys: j < i, queries: j <= i)
 #pragma unroll
@@ -477,7 +528,6 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
         const int bytes = shared_key ? 4 : (int)sizeof(T), units = KD * bytes / 16;
         // unit u of row r, spread over the banks
         auto collect_at = [&](int r, int u) { return (r * units + (u ^ (r & 7))) * 16; };
-        constexpr int SHARE = KD / 4;
 #pragma unroll
         for (int i = 0; i < SHARE; i += 16) {
             const int col = side * SHARE + i;
@@ -500,10 +550,13 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
             for (int j = 0; j < 16; ++j) x[j] = fmaf(x1, __uint_as_float(v[j]), __uint_as_float(w[j])), dot = fmaf(z[j], x[j], dot);
             if (is_key) {
                 ptx::tmem_ld16(lanes + W::d3 + col, v), ptx::tmem_ld16(lanes + W::d5 + col, w);
+                float rest[16];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) *reinterpret_cast<float4*>(rest + 4 * u) = *small3_at(col + 4 * u);
                 ptx::tmem_ld_wait();
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    float y = x3 * __uint_as_float(v[j]);
+                    float y = x3 * (__uint_as_float(v[j]) + rest[j]);
                     after = fmaf(z[j], y, after);
                     y += __uint_as_float(w[j]), dot = fmaf(-z[j], y, dot);
                     x[j] += y;

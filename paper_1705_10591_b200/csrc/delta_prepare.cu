@@ -109,13 +109,23 @@ __global__ void __launch_bounds__(128, 3) delta_prepare_kernel(const DeltaArgs a
 #pragma unroll
         for (int n = 0; n < 8; n += 2) {
             if (n * 8 < m0) continue;
+            auto products = [&](float (&k1)[4], float (&k2)[4], float (&q1)[4], float (&q2)[4]) {
 #pragma unroll
-            for (int p = IN - 1; p >= 0; --p) {
-                uint32_t r[4];
-                right_nk<64>(r, part(p), n * 8, k0 % 64, lane);
-                mma_parts<IN>(kk[n], kk[n + 1], ak, r, p);
-                right_nk<64>(r, part(p), kPiece + n * 8, k0 % 64, lane);
-                mma_parts<IN>(kq[n], kq[n + 1], ak, r, p);
+                for (int p = IN - 1; p >= 0; --p) {
+                    uint32_t r[4];
+                    right_nk<64>(r, part(p), n * 8, k0 % 64, lane);
+                    mma_parts<IN>(k1, k2, ak, r, p);
+                    right_nk<64>(r, part(p), kPiece + n * 8, k0 % 64, lane);
+                    mma_parts<IN>(q1, q2, ak, r, p);
+                }
+            };
+            if constexpr (IN == kSum) {                        // (an MMA cuts off what it adds, towards zero: o of keys of 128 fp32 numbers 1.0e-6 off with one sum, 3e-7 so)
+                float s[4][4] = {};
+                products(s[0], s[1], s[2], s[3]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) kk[n][e] += s[0][e], kk[n + 1][e] += s[1][e], kq[n][e] += s[2][e], kq[n + 1][e] += s[3][e];
+            } else {
+                products(kk[n], kk[n + 1], kq[n], kq[n + 1]);
             }
         }
     }

@@ -312,6 +312,27 @@ __device__ __forceinline__ void multiply(uint32_t d, int a_parts, int b_parts, i
     }
 }
 
+// Of numbers in three parts, the products of first parts, and all others that count, small ones first.
+template <typename DescA, typename DescB>
+__device__ __forceinline__ void multiply_first(uint32_t d, int ks, uint32_t idesc, uint32_t elected, bool more, DescA desc_a, DescB desc_b)
+{
+#pragma unroll
+    for (int k = 0; k < ks; ++k) ptx::mma_b16(d, desc_a(0, k), desc_b(0, k), idesc, more || k > 0, elected);
+}
+template <typename DescA, typename DescB>
+__device__ __forceinline__ void multiply_small(uint32_t d, int ks, uint32_t idesc, uint32_t elected, bool more, DescA desc_a, DescB desc_b)
+{
+#pragma unroll
+    for (int digits = kSum - 1; digits >= 1; --digits)
+#pragma unroll
+        for (int p = 0; p <= digits; ++p)
+#pragma unroll
+            for (int k = 0; k < ks; ++k) {
+                ptx::mma_b16(d, desc_a(p, k), desc_b(digits - p, k), idesc, more, elected);
+                more = true;
+            }
+}
+
 // Columns a block walks with: 32, or 64 where those are fewer rounds of the machine's SMs.  A piece takes 2.3 us with 32 columns and 3.4 with 64; where the keys of two
 // pieces do not fit beside 64 (fp16, in two parts) and are waited for, 4.5, so that two rounds of 32 are no slower.  Keys of 128 fp32 numbers, in three parts,
 // leave room for 32, and rows that rule out accesses of 16 bytes are walked with 32.
