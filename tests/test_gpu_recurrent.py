@@ -475,6 +475,66 @@ def test_rms_extremes_and_graphs(lib):  # noqa: F811
     check(y, want, size, 40, "y")
 
 
+@pytest.mark.parametrize("type, M, C, G", [("bf16", 1500, 2048, 1), ("fp32", 700, 96, 3), ("fp16", 3, 5000, 1)])
+def test_rms_training_captured_in_place_and_on_two_streams(lib, type, M, C, G):  # noqa: F811
+    """Forward and backward as a training step calls them, h in place of x and dx in place of dh: eager on two streams at once, and in a graph replayed on other inputs."""
+    t, op, eps = TYPES[type], operand(lib, type), 1e-5
+    need = lib.norm_bwd_rms_workspace_size(M, C, G)
+
+    class Step:
+        def __init__(self, seed):
+            new = lambda i, *s: draw(seed + i, *s).to(t).cuda()  # noqa: E731
+            self.x, self.res, self.dy, self.dh = (new(i, M, C) for i in range(4))
+            self.gamma = draw(seed + 4, C // G, shift=1.0).float().cuda()
+            self.y, self.rstd, self.dgamma, self.ws = torch.empty_like(self.x), torch.empty(M, G, device="cuda"), torch.empty(C // G, device="cuda"), workspace(need)
+            self.given = [v.clone() for v in (self.x, self.res, self.dy, self.dh, self.gamma)]
+
+        def reset(self, other=None):
+            for v, w in zip((self.x, self.res, self.dy, self.dh, self.gamma), (other or self).given):
+                v.copy_(w)
+
+        def run(self, on):
+            p = lambda v: v.data_ptr()  # noqa: E731
+            lib.norm_fwd_rms(p(self.x), p(self.res), 0, p(self.gamma), p(self.y), p(self.x), 0, 0, p(self.rstd), M, C, G, 0, C, C, 0, C, C, 0, eps, op, on)
+            lib.norm_bwd_rms(p(self.x), 0, p(self.gamma), p(self.rstd), p(self.dy), p(self.dh), p(self.dh), 0, p(self.dgamma), M, C, G, C, 0, C, C, C, 0, op,
+                             p(self.ws), need, on)
+
+        def results(self):
+            return [v.clone() for v in (self.x, self.y, self.rstd, self.dh, self.dgamma)]
+
+    steps = [Step(950), Step(970)]
+    want = []
+    for s in steps:
+        h = (s.given[0].float() + s.given[1].float()).to(t)
+        s.run(stream())
+        want.append(s.results())
+        assert torch.equal(s.x, h)
+        kept = h.double().cpu()
+        (y, size), _ = ref.rms_fwd(kept, None, s.given[4].double().cpu(), G, eps)
+        dx, _, _ = ref.rms_bwd(kept, None, s.given[4].double().cpu(), G, eps, s.given[2].double().cpu(), s.given[3].double().cpu())
+        adds = min(C // G, 16) + 12
+        check(s.y, y, size, adds + 16, "y")
+        check(s.dh, *dx, 3 * adds + 40, "dx")
+        s.reset()
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s, side in zip(steps, sides):
+        s.run(side.cuda_stream)
+    torch.cuda.synchronize()
+    for s, w in zip(steps, want):
+        assert all(torch.equal(a, b) for a, b in zip(s.results(), w))
+        s.reset()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        steps[0].run(stream())
+    for i in (1, 0):
+        steps[0].reset(steps[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(steps[0].results(), want[i]))
+
+
 # ---------------------------------------------------------------------------------------------------------------- a layer
 
 def test_a_layer_of_them_with_the_convolution(lib):  # noqa: F811
