@@ -64,7 +64,7 @@ conv2d_status_t delta_bwd_gated(const void* q, const void* k, const int* lengths
  *   y8 [M][C] bytes (ld8), scales [M][ceil(C/block)] fp32: y in 8 bits (e4m3), both or neither; at least one of y and y8.  Every `block` adjacent columns of
  *   a row (the last ones may be fewer) share a scale s = max |y| / 448, at least 2^-126, and y8 = y / s, rounded to nearest, even.
  *   A block of more than C columns is the row.  block is not looked at without y8.  What is rounded is y before it is rounded to `type`.
- *   A NaN keeps its place and does not count for the scale; a block with an infinity has an infinite scale.
+ *   A NaN keeps its place and does not count for the scale; a block with an infinity has an infinite scale, its finite numbers become zeros, its infinities NaN.
  */
 conv2d_status_t norm_fwd_rms(const void* x, const void* residual, const void* z, const float* gamma, void* y, void* h,
                              void* y8, float* scales, float* rstd, int M, int C, int G, int block,

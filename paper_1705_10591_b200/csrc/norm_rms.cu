@@ -317,12 +317,14 @@ __global__ void __launch_bounds__(kMostThreads, V > 2 && NP <= 2 ? 2 : 1) rms_fw
             if (!there[j]) continue;
             const float scale = fmaxf(most[j] / 448.f, 1.17549435e-38f);
             if (at[j] == block[j] * blocks.packs) a.scales[(long long)row * blocks.count + block[j]] = scale;
-            const float up = 1.f / scale;
-            float q[V];                                        // the quotient, put right by what it leaves: not one rounding more than a division's before the codes'
+            // the quotient, put right by what it leaves: not one rounding more than a division's before the codes'.  Over an infinite scale it leaves nothing:
+            // finite numbers are zero (times the scale they would be NaN), infinite ones NaN
+            const float up = 1.f / scale, down = up > 0.f ? -scale : 0.f;
+            float q[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) q[e] = f[j][e];
             times<V>(q, up);
-            add_times<V>(f[j], q, -scale);
+            add_times<V>(f[j], q, down);
             add_times<V>(q, f[j], up);
             store_codes<V>(static_cast<unsigned char*>(a.y8) + element(row, a.ld8, col[j]), q);
         }
