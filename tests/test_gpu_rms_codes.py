@@ -1,9 +1,9 @@
-"""RMS norm's output in 8 bits: blocks of columns with infinities and NaN."""
+"""RMS norm's output in 8 bits: blocks of columns with infinities and NaN, and the sum with a residual, as a layer's entry calls it."""
 import pytest
 import torch
 
 import recurrent_reference as ref
-from sequence_reference import TYPES
+from sequence_reference import TYPES, check
 from test_gpu_sequence import Rows, cuda, draw, lib, operand, stream  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -66,3 +66,41 @@ def test_blocks_with_infinities_and_nan(lib, type, M, C, G, block, residual, gat
     (want, size), _ = ref.rms_fwd(h, z if gate else None, gamma, G, 1e-5)
     seen = check_codes(y8, scales.result(), want, size, block)
     assert all(seen[:3]), seen                                  # blocks with an infinity, finite numbers in them, and such as have no value
+
+
+@pytest.mark.parametrize("type, M, C, block, pad", [
+    ("bf16", 1300, 4096, 128, 0), ("bf16", 1201, 4096, 4096, 0), ("bf16", 6001, 512, 128, 0), ("bf16", 37, 8192, 128, 0), ("bf16", 5, 16384, 16384, 0), ("fp16", 33, 1000, 128, 8),
+    ("fp16", 3001, 264, 264, 0), ("fp16", 9, 4096, 32, 0), ("fp32", 1400, 2048, 128, 0), ("fp32", 40, 2048, 1 << 30, 4), ("fp32", 7, 300, 24, 1), ("bf16", 11, 77, 10, 3)])
+@pytest.mark.parametrize("place", ["h", "x", "residual"])
+def test_entry_of_a_layer_in_8_bits(lib, type, M, C, block, pad, place):  # noqa: F811
+    """With a residual, alone and beside an output of the type; h in a tensor of its own, in place of x, of the residual."""
+    t = TYPES[type]
+    x, res = draw(1020, M, C, dtype=t), draw(1021, M, C, scale=2.0, dtype=t)
+    x[0], res[0] = 0, 0
+    gamma, h = draw(1022, C, shift=1.0, scale=0.2).float().to(F), (x + res).float().to(t).to(F)
+    (want, size), r = ref.rms_fwd(h, None, gamma, 1, 1e-5)
+    gr = cuda(gamma)
+    codes = []
+    for both in (False, True):
+        R = lambda v=None: Rows((M, C), t, pad, 0, v)  # noqa: E731
+        xr, rr, hr, yr = R(x), R(res), R(), R()
+        into = {"h": hr, "x": xr, "residual": rr}[place]
+        y8, scales, rstd = torch.full((M, C + pad + 3), 9, dtype=torch.uint8, device="cuda"), Rows((M, -(-C // block)), torch.float32), Rows((M, 1), torch.float32)
+        ld8 = C if pad == 0 else C + pad + 3
+        lib.norm_fwd_rms(xr.ptr, rr.ptr, 0, gr.data_ptr(), yr.ptr if both else 0, into.ptr, y8.data_ptr(), scales.ptr, rstd.ptr if both else 0, M, C, 1, block,
+                         xr.ld, rr.ld, 0, yr.ld, into.ld, ld8, 1e-5, operand(lib, type), stream())
+        assert torch.equal(into.result().double().cpu(), h)
+        flat = y8.reshape(-1)
+        rows = flat.as_strided((M, C), (ld8, 1)).clone()
+        flat.as_strided((M, C), (ld8, 1)).fill_(9)
+        assert (flat == 9).all(), "written outside the codes"
+        assert check_codes(rows, scales.result(), want, size, block)[:3] == (0, 0, 0)
+        assert (rows[0] & 127 == 0).all() and (scales.result()[0] == 2.0 ** -126).all()
+        if both:
+            adds = 16 + 12
+            check(yr.result(), want, size, adds + 16, "y")
+            check(rstd.result(), r, r, adds + 4, "rstd")
+        codes.append((rows, scales.result()))
+    # two kernels: y is off by 44 roundings in each, so a code only where a border between two lies within 88 * 2^-24 of a quotient, of steps of 2^-4: in one of 10^4 at most
+    a, b = (v.to(torch.int32) for v, _ in codes)
+    assert ((a - b).abs() <= 1).all() and (a != b).sum() <= max(1, M * C // 10000)
