@@ -1,0 +1,61 @@
+"""The gated delta rule where its kernels go round: several pieces for every block of the gradients, several heads of a shared key for a block of the first kernel, walks
+of 64 columns by the rule itself; empty and short sequences between long ones, one to five blocks of columns."""
+import pytest
+import torch
+
+from test_gpu_recurrent import Delta
+from test_gpu_sequence import Rows, lib  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+# B * H * ceil(L / 64) is 448 to 640 everywhere, more than three for each of a B200's 148 SMs
+CASES = [  # type, B, L, Hk, H, K, V, lengths, pad, offset
+    ("bf16", 6, 832, 2, 6, 16, 32, [832, 0, 700, 65, 1, 800], 0, 0),
+    ("bf16", 10, 1000, 1, 3, 128, 96, [1000, 1000, 0, 0, 0, 64, 999, 1, 128, 640], 0, 0),
+    ("bf16", 16, 500, 2, 4, 64, 128, [500, 0, 450, 500, 64, 65, 0, 1, 500, 321, 500, 500, 0, 128, 500, 63], 0, 0),
+    ("bf16", 4, 2048, 4, 4, 64, 64, None, 0, 0),
+    ("bf16", 10, 3000, 1, 1, 24, 160, [3000, 0, 0, 2900, 1, 3000, 64, 0, 3000, 1500], 0, 0),
+    ("fp16", 5, 1030, 2, 6, 64, 128, [1030, 0, 1025, 513, 0], 0, 0),
+    ("fp16", 5, 1000, 3, 6, 100, 64, None, 8, 8),
+    ("fp32", 12, 777, 1, 3, 64, 64, [777, 0, 0, 700, 1, 64, 777, 128, 0, 650, 777, 777], 0, 0),
+    ("fp32", 8, 640, 3, 6, 40, 50, [640, 0, 640, 1, 600, 64, 0, 639], 1, 1),
+    ("fp32", 5, 1024, 3, 6, 128, 32, None, 0, 0),
+    ("fp32", 10, 700, 1, 5, 128, 100, [700, 700, 64, 0, 0, 0, 0, 1, 300, 700], 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{c[0]}-{'x'.join(map(str, c[1:7]))}-{c[8]}")
+def test_blocks_of_several_pieces_and_heads(lib, case):  # noqa: F811
+    type, B, L, Hk, H, K, V, lengths, pad, offset = case
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert B * H * -(-L // 64) > 3 * sms
+    c = Delta(lib, type, B, L, Hk, H, K, V, lengths, pad, offset, seed=1200)
+    wanted = c.wanted()
+    o, last = c.forward(keep=True)
+    c.check({"o": o, "state": last}, wanted)
+    first = c.backward()
+    c.check(first, wanted)
+    again, end = c.forward(keep=True)
+    assert torch.equal(again.result(), o.result()) and torch.equal(end.result(), last.result())
+    for name, x in c.backward().items():
+        assert torch.equal(x.result(), first[name].result()), name
+
+
+def test_a_sequence_does_not_see_its_batch(lib):  # noqa: F811
+    """The same sequences one by one and in a batch whose blocks take several pieces and heads: the same bits."""
+    B, L, Hk, H, K, V = 7, 900, 2, 6, 32, 32
+    lengths = [900, 0, 257, 900, 64, 1, 850]
+    c = Delta(lib, "bf16", B, L, Hk, H, K, V, lengths, seed=1220)
+    o, last = c.forward(keep=True)
+    grads = {n: x.result().reshape(B, -1) for n, x in c.backward().items()}
+    o, last = o.result(), last.result()
+    for b in (0, 2, 6):
+        one = Delta(lib, "bf16", 1, L, Hk, H, K, V, [lengths[b]], seed=1220)
+        for x in ("qr", "kr", "vr", "gr", "br", "dr"):
+            rows = getattr(c, x)
+            setattr(one, x, Rows((1, L, rows.width), rows.buf.dtype, 0, 0, rows.view().reshape(B, L, -1)[b]))
+        one.sd, one.dld = c.sd[b:b + 1].contiguous(), c.dld[b:b + 1].contiguous()
+        oo, ll = one.forward(keep=True)
+        assert torch.equal(oo.result()[0], o[b]) and torch.equal(ll.result()[0], last[b])
+        for n, x in one.backward().items():
+            assert torch.equal(x.result().reshape(-1), grads[n][b]), n
