@@ -58,6 +58,8 @@ conv2d_status_t delta_bwd_gated(const void* q, const void* k, const int* lengths
  * RMS norm of M rows of C <= 16384 channels in G groups (G divides C), each normalised by itself:
  *   h = x + residual, rounded to `type` (h = x where residual is NULL),   r = 1 / sqrt(mean(h^2) + eps),   n = gamma[c % (C/G)] h r,
  *   y = n * silu(z)   (y = n where z is NULL).   With eps of zero a group of zeros becomes NaN.
+ *   The mean is of squares in fp32: numbers up to 2^63 are normalised; from 2^64 on it is infinite and the group becomes zeros.  Squares of numbers below 2^-63 lose
+ *   digits, and vanish below 2^-75, which only an eps as small shows.
  *   x, residual (optional), z (optional), y [M][C] (ldx, ldr, ldz, ldy); gamma [C/G] fp32, optional (1); eps >= 0.
  *   h [M][C] (ldh): required exactly where residual is given; the residual of the next layer.  It may be the same tensor as residual, or x.
  *   rstd [M][G] fp32, optional: r, for the backward pass.

@@ -284,7 +284,11 @@ __global__ void __launch_bounds__(kMostThreads, V > 2 && NP <= 2 ? 2 : 1) rms_fw
                 unpack<T, V>(sum, f[j]);
                 if (there[j]) store_pack<T, V>(static_cast<T*>(a.h) + element(row, a.ldh, col[j]), sum);
             }
-            s[j] = dot<V>(f[j], f[j]) * inverse;               // (a mean does not overflow where its terms do not, a sum of thousands would)
+            float part[V];                                     // of the mean: each square by itself, since a mean does not overflow where its terms do not, but a sum of two may
+#pragma unroll
+            for (int e = 0; e < V; ++e) part[e] = f[j][e];
+            times<V>(part, inverse);
+            s[j] = dot<V>(f[j], part);
         }
         reduce_runs<Sum, Ways<KIND>::group>(s, at, groups, packs, shared, turn);
         if (stages) {
@@ -407,13 +411,17 @@ __global__ void __launch_bounds__(kMostThreads, 1) rms_bwd_kernel(const RmsArgs 
             }
             add_times<V>(dw[j], n[j], m[j]);
             times<V>(n[j], w[j]);
-            s[j] = dot<V>(n[j], m[j]);
+            float part[V];                                     // (likewise)
+#pragma unroll
+            for (int e = 0; e < V; ++e) part[e] = m[j][e];
+            times<V>(part, inverse);
+            s[j] = dot<V>(n[j], part);
         }
         fetch_r(row + step);
         reduce_runs<Sum, Ways<KIND>::group>(s, at, groups, packs, shared, turn);
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
-            add_times<V>(n[j], m[j], -s[j] * inverse);
+            add_times<V>(n[j], m[j], -s[j]);
             times<V>(n[j], r[j]);
             if (second) {
                 float d[V];
