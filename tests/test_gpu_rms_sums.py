@@ -1,10 +1,10 @@
-"""RMS norm's sums of large numbers, whose squares are near the end of fp32."""
+"""RMS norm's sums: rows of large numbers, whose squares are near the end of fp32, and the gradient of gamma, of integers so that a row that is left out or counted twice shows."""
 import pytest
 import torch
 
 import recurrent_reference as ref
 from sequence_reference import TYPES, check
-from test_gpu_sequence import Rows, cuda, draw, lib, operand, stream  # noqa: F401
+from test_gpu_sequence import Rows, cuda, draw, lib, operand, stream, workspace  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 F = torch.float64
@@ -76,3 +76,36 @@ def test_large_gradients(lib, case, gate):  # noqa: F811
     check(dxr.result(), *dx, 3 * adds + 40, "dx")
     if gate:
         check(dzr.result(), *dz, adds + 40, "dz")
+
+
+GAMMA = SPREADS + [("fp16", 2, 11000, 1, 0, 0), ("bf16", 3001, 1280, 1, 0, 0), ("fp16", 6001, 520, 5, 0, 0), ("fp32", 4003, 300, 3, 1, 1), ("bf16", 5003, 264, 1, 0, 0),
+                   ("fp32", 1300, 4096, 32, 0, 0), ("bf16", 1501, 8200, 1, 0, 0), ("bf16", 700, 40, 5, 0, 0), ("fp16", 16411, 24, 3, 0, 0), ("bf16", 2377, 661, 1, 0, 0),
+                   ("bf16", 593, 256, 1, 0, 0), ("fp32", 2049, 7, 7, 0, 0)]
+
+
+@pytest.mark.parametrize("gate", [False, True])
+@pytest.mark.parametrize("case", GAMMA, ids=name)
+def test_every_row_counts_once_for_gamma(lib, case, gate):  # noqa: F811
+    """h of -1 and 1, rstd of one and small whole dy: every sum of the M * G terms is a whole number below 2^24, exact in any order.  With a gate, z of 64, whose silu is 64 but
+    for 4 roundings: terms of 64 each; a sum of them is off by 2^-24 for each of at most 160 additions one after the other and those 4, below half a term here."""
+    type, M, C, G, pad, offset = case
+    t, n = TYPES[type], C // G
+    assert 3 * M * G < 1 << 24
+    whole = lambda seed, most: torch.randint(-most, most + 1, (M, C), generator=torch.Generator().manual_seed(seed)).to(F)  # noqa: E731
+    h = 2.0 * (whole(1120, 1) > 0) - 1
+    dy = whole(1121, 3) if not gate else 2.0 * (whole(1122, 1) > 0) - 1
+    dh, z = whole(1123, 3), torch.full((M, C), 64.0, dtype=F)
+    R = lambda v=None: Rows((M, C), t, pad, offset, v)  # noqa: E731
+    hr, zr, dyr, dhr, dxr, dzr, rstd, dg = R(h), R(z), R(dy), R(dh), R(), R(), torch.ones(M, G, device="cuda"), Rows((n,), torch.float32)
+    need = lib.norm_bwd_rms_workspace_size(M, C, G)
+    ws = workspace(need)
+    want = (dy * h).reshape(M, G, n).sum((0, 1)) * (64 if gate else 1)
+    for with_dh in (False, True):
+        lib.norm_bwd_rms(hr.ptr, zr.ptr if gate else 0, 0, rstd.data_ptr(), dyr.ptr, dhr.ptr if with_dh else 0, dxr.ptr, dzr.ptr if gate else 0, dg.ptr, M, C, G, hr.ld, zr.ld,
+                         dyr.ld, dhr.ld, dxr.ld, dzr.ld, operand(lib, type), ws.data_ptr(), need, stream())
+        got = dg.result().double().cpu()
+        if gate:
+            assert 164 * 2.0 ** -24 * M * G < 0.5
+            assert ((got - want).abs() <= 64 * 164 * 2.0 ** -24 * M * G).all()
+        else:
+            assert torch.equal(got, want)
