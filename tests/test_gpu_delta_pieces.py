@@ -59,3 +59,21 @@ def test_a_sequence_does_not_see_its_batch(lib):  # noqa: F811
         assert torch.equal(oo.result()[0], o[b]) and torch.equal(ll.result()[0], last[b])
         for n, x in one.backward().items():
             assert torch.equal(x.result().reshape(-1), grads[n][b]), n
+
+
+@pytest.mark.parametrize("type", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("K, V, share, pad", [(128, 128, 1, 0), (64, 96, 3, 0), (33, 20, 2, 1)])
+def test_a_gate_without_a_state_has_no_gradient(lib, type, K, V, share, pad):  # noqa: F811
+    """The first decay of a sequence that begins without a state has nothing to decay: its gradient is zero, not what rounding leaves of sums."""
+    lengths = [1, 2, 64, 65, 130, 0]
+    c = Delta(lib, type, 6, 130, 2, 2 * share, K, V, lengths, pad, pad, state=False, seed=1240)
+    c.beta[3, :40] = 0
+    c.br = Rows((6, 130, 2 * share), torch.float32, pad, pad, torch.where((torch.arange(130)[None] < torch.tensor(lengths)[:, None])[..., None], c.beta, float("nan")))
+    wanted = c.wanted()
+    o, last = c.forward(keep=True)
+    c.check({"o": o, "state": last}, wanted)
+    grads = c.backward()
+    c.check(grads, wanted)
+    dg = grads["dg"].result()
+    assert (dg[:, 0] == 0).all()
+    assert (o.result()[3, :40] == 0).all()
