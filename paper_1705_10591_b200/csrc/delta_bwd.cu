@@ -485,8 +485,8 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
             float x[16];
             {
                 float y[16];
-                tmem_row<16>(lanes + W::d2 + side * 16, x);
-                tmem_row<16>(lanes + W::small2 + side * 16, y);
+                tmem_row(lanes + W::d2 + side * 16, x);
+                tmem_row(lanes + W::small2 + side * 16, y);
 #pragma unroll
                 for (int n = 0; n < 16; ++n) x[n] += y[n];
             }
@@ -501,7 +501,7 @@ __global__ void __launch_bounds__(Piecewise<T, KD>::THREADS, 1) delta_bwd_pieces
                 ptx::tmem_st16(lanes + W::d1 + col, v);
                 if (is_key) continue;                          // (whole warps)
                 float y[16];
-                tmem_row<16>(lanes + W::d3 + col, y);
+                tmem_row(lanes + W::d3 + col, y);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) *small3_at(col + 4 * u) = make_float4(y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]);
             }

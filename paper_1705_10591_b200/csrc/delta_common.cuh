@@ -108,11 +108,6 @@ template <int W> __device__ __forceinline__ void left_mk(uint32_t (&r)[4], uint3
 {
     ldsm(r, unit_at<W>(base, m0 + (lane & 15), (k0 >> 3) + (lane >> 4)));
 }
-//   rows along k, m inside them
-template <int W> __device__ __forceinline__ void left_km(uint32_t (&r)[4], uint32_t base, int k0, int m0, int lane)
-{
-    ldsm_t(r, unit_at<W>(base, k0 + ((lane >> 4) << 3) + (lane & 7), (m0 >> 3) + ((lane >> 3) & 1)));
-}
 
 // The left operand of 16 columns from accumulators of two tiles of 8, as N parts.
 template <int N>

@@ -93,8 +93,8 @@ conv2d_status_t step(const DeltaArgs& a, int lanes, cudaStream_t stream)
 template <typename T, int VW>
 conv2d_status_t step_wide(const DeltaArgs& a, cudaStream_t stream)
 {
-    // as many as a row of the state has, up to 16: blocks of 64 columns hold 32 KB of a state of 128 x 128 in half the registers, and an SM has four of them where it
-    // had two (256 tokens of 32 such heads: 165 us, 6.6 TB/s; with 32 lanes 210, with 8 201)
+    // as many as a row of the state has, from 4 up to 16: blocks of 64 columns hold 32 KB of a state of 128 x 128 in half the registers, and an SM has four of them where
+    // it had two (256 tokens of 32 such heads, 1.08 GB, 60 calls in a row: 165 us, 6.5 TB/s, with 32 lanes 210, with 8 201; from some 900 calls in a row on 180)
     int lanes = 4;
     while (lanes < 16 && lanes * VW < a.V) lanes *= 2;
     const int rows = (a.K * lanes + 127) / 128;

@@ -47,18 +47,13 @@ __device__ __forceinline__ uint64_t rows_as_k(uint32_t at, uint32_t next)
 }
 constexpr uint32_t kIdescAMajorM = 1u << 15;
 
-template <int N> __device__ __forceinline__ void tmem_get(uint32_t at, uint32_t (&v)[N])
+__device__ __forceinline__ void tmem_row(uint32_t at, float (&f)[16])
 {
-    if constexpr (N == 16) ptx::tmem_ld16(at, v);
-    else ptx::tmem_ld32(at, v);
-}
-template <int N> __device__ __forceinline__ void tmem_row(uint32_t at, float (&f)[N])
-{
-    uint32_t v[N];
-    tmem_get<N>(at, v);
+    uint32_t v[16];
+    ptx::tmem_ld16(at, v);
     ptx::tmem_ld_wait();
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = __uint_as_float(v[i]);
+    for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(v[i]);
 }
 // The sum of products whose digits lie in three places, `step` columns apart.
 template <int N> __device__ __forceinline__ void tmem_digits(uint32_t at, uint32_t step, float (&f)[N])
@@ -123,24 +118,6 @@ __device__ __forceinline__ void put_four(unsigned char* at, int part_bytes, cons
         *reinterpret_cast<uint2*>(at + p * part_bytes) = p < PARTS ? make_uint2(w[0][p < PARTS ? p : 0], w[1][p < PARTS ? p : 0]) : make_uint2(0u, 0u);
 }
 
-template <bool WIDE, typename T, int N>
-__device__ __forceinline__ void store_row(T* to, int there, const float (&f)[N])
-{
-    constexpr int PER = 16 / (int)sizeof(T);
-    if (WIDE) {
-#pragma unroll
-        for (int i = 0; i < N; i += PER) {
-            float x[PER];
-#pragma unroll
-            for (int j = 0; j < PER; ++j) x[j] = f[i + j];
-            if (i < there) store_pack<T, PER>(to + i, pack<T, PER>(x));
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (i < there) to[i] = from_float<T>(f[i]);
-    }
-}
 // What a pass keeps of a piece lies as [V/4][rows][4], so that the lanes of a warp, a row each, write and read whole lines (rows of V as they come: every
 // access of a warp touched 32 lines, and a training step's walks waited twice as long for their stores as for everything else).
 __device__ __forceinline__ size_t quad_at(size_t unit, int VP, int rows, int v, int row) { return unit * ((size_t)rows * VP) + ((size_t)(v >> 2) * rows + row) * 4; }
