@@ -77,3 +77,33 @@ def test_a_gate_without_a_state_has_no_gradient(lib, type, K, V, share, pad):  #
     dg = grads["dg"].result()
     assert (dg[:, 0] == 0).all()
     assert (o.result()[3, :40] == 0).all()
+
+
+@pytest.mark.parametrize("type, K, V", [("bf16", 64, 96), ("fp32", 128, 32), ("fp16", 33, 20)])
+@pytest.mark.parametrize("what", ["qr", "kr", "vr", "gr", "br", "dr"])
+def test_what_is_not_finite_stays_in_its_head(lib, type, K, V, what):  # noqa: F811
+    """A NaN and an infinity in one sequence, seen by the value heads of one key head at most: all other results, and the pieces before it, are the same bits."""
+    B, L, Hk, share = 9, 1030, 1, 3
+    H = Hk * share
+    lengths = [1030, 0, 1030, 700, 1, 64, 1030, 1000, 129]
+    results = []
+    for spoil in (False, True):
+        c = Delta(lib, type, B, L, 2 * Hk, 2 * H, K, V, lengths, seed=1260)
+        if spoil:
+            rows = getattr(c, what).view().view(B, L, -1)
+            width = rows.shape[-1] // 2                         # of the first half of the heads
+            rows[2, 70, width - 1], rows[2, 300, 0] = float("nan"), float("inf")
+        o, last = c.forward(keep=True)
+        grads = c.backward()
+        results.append({"o": o.result().reshape(B, L, 2, -1), "state": last.result().reshape(B, 1, 2, -1),
+                        **{n: x.result().reshape(B, 1 if n == "dstate" else L, 2, -1) for n, x in grads.items()}})
+    bits = lambda x: x.view(torch.int32 if x.element_size() == 4 else torch.int16)  # noqa: E731
+    for name, x in results[0].items():
+        y = results[1][name]
+        one, two = bits(x).clone(), bits(y).clone()
+        assert torch.equal(one[:, :, 1], two[:, :, 1]), name   # the other half of the heads
+        if name == "o":
+            assert torch.equal(one[2, :64], two[2, :64])
+        one[2, :, 0], two[2, :, 0] = 0, 0
+        assert torch.equal(one, two), name                     # the other sequences
+    assert not all(torch.isfinite(x[2].float()).all() for x in results[1].values())
