@@ -22,9 +22,12 @@ extern "C" {
  *   state_in, state_out [B][H][K][V] fp32, dense, optional (zeros); state_out is S after the last token (state_in, or zeros, for a sequence
  *   without tokens) and may be the same buffer as state_in.
  * g is a log decay: 0 keeps, -infinity forgets (below -10000 is taken as that).  Sequences are computed in pieces of 64 tokens: a key, value,
- * query or gate that is not finite spoils the whole piece that it is in and all that follows in its head and sequence.
+ * query, beta or other decay that is not finite spoils the whole piece that it is in and all that follows in its head and sequence (and, backward, what comes before
+ * it there), and nothing else.
  * Products run on the tensor cores, sums and states as operands in three bf16 numbers each (24 bits).
- * states (optional): what the backward pass continues from, delta_states_size bytes, aligned to 16; the caller keeps it until then.
+ * states (optional): what the backward pass continues from, delta_states_size bytes, aligned to 16; the caller keeps it until then.  For every 64 tokens of a head
+ * 49 KB and 4 (K' + 64) V' bytes, K' = 64 or 128, V' = V rounded up to 16 (8192 tokens of 16 heads of 128 x 128: 305 MB, nine times v in bf16).
+ * A batch can be taken in pieces.
  * B * H * ceil(L / 64) * ceil(V / 16) is below 2^31.
  * Waits on the device are bounded; should one expire, the results are not defined and conv2d_get_status(NULL, cuda_stream) says so (CONV2D_ERR_DEVICE_TIMEOUT).
  */

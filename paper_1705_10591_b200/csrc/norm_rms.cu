@@ -219,8 +219,8 @@ struct Ahead {
 
 // What a call has, as constants of its kernel: whether there is a second tensor to add (residual, dh), a gate, y and y8, and which lanes share groups and scales.  The
 // branches on them and what they keep apart would be a third of all that these kernels issue, and these are bound by that (8192 x 4096 with a residual to 8 bits: 50M
-// instructions and 67 us so, 35M and 48 with constants; 16384 x 2048 to 16 bits: 56 us and 41).  kAny looks at the arguments: calls that are rare, and rows
-// too large for two packs a thread.
+// instructions and 67 us so, 36M and 48 with constants; 16384 x 2048 to 16 bits: 56 us and 41).  kAny looks at the arguments: the other
+// calls (to 8 bits with a gate, of heads 61 to 66 us, of rows 68, or without a residual, 52 to 56: 8192 x 4096 of bf16), and rows too large for two packs a thread.
 enum { kSecond = 1, kGate = 2, kY = 4, kY8 = 8, kGroupLanes = 16, kBlockLanes = 32, kAny = -1 };
 template <int KIND> __device__ __forceinline__ bool has(int what, const void* given) { return KIND < 0 ? given != nullptr : (KIND & what) != 0; }
 template <int KIND>
@@ -592,7 +592,7 @@ conv2d_status_t backward_of(int kind, const RmsArgs& a, const RowPlan& p, cudaSt
 template <typename T, int V, int NP>
 conv2d_status_t either(const RmsArgs& a, const RowPlan& p, bool bwd, cudaStream_t stream)
 {
-    if constexpr (V * sizeof(T) == 16 && NP <= 2) {            // kinds: the norm at a layer's entry, of its heads, at its exit
+    if constexpr (V * sizeof(T) == 16 && NP <= 2) {            // kinds: the norm at a layer's entry, of its heads, at its exit but for one in 8 bits
         const Runs blocks = p.blocks(a.y8 ? a.block : a.C);
         int kind = (a.residual || a.dh ? kSecond : 0) | (a.z ? kGate : 0) | (a.y ? kY : 0) | (a.y8 ? kY8 : 0) | (p.groups.how == kLanes ? kGroupLanes : 0) |
                    (a.y8 && blocks.how == kLanes ? kBlockLanes : 0);
